@@ -596,6 +596,81 @@ emr_status emr_ann_forward(int32_t P, int32_t n_in, int32_t n_out, int32_t max_h
                            const float *conn_w, int32_t K, const float *patterns, int32_t steps, float *out,
                            void *stream);
 
+/* ---- dense substrate layers in 8-bit floating point ------------------------------- */
+
+/* A HyperNEAT substrate may connect every source to every position: emr_eval's
+ * materialised outputs of one genome are then a dense weight matrix (slots x
+ * positions). The calls below run such layers, y = act(x W^T + b), on the tensor
+ * cores in 8-bit floating point and train them.
+ *
+ * emr_q8: batch matrices [rows][cols] held as e4m3 codes (device, [batch][rows]
+ * [cols rounded up to 128], zero past cols) and one power-of-two scale byte (127 +
+ * exponent) for every 128 consecutive columns of a row (device, [batch][rows / 128]
+ * [column blocks / 4] tiles of 512 bytes: byte (r % 32) * 16 + (r / 32 % 4) * 4 +
+ * kb % 4 of its tile belongs to row r, block kb). The scale is the least 2^e, e in
+ * [-126, 127], with the block's largest finite magnitude <= 448 * 2^e (1 for a block
+ * of zeros), so scaling is exact and only the rounding to e4m3 (nearest even: 3
+ * fraction bits) loses anything. Infinities and NaN become the NaN code and do not
+ * enter the maximum. Sizes in bytes: emr_q8_size. Both buffers are 16-byte aligned.
+ * Errors of all calls: EMR_ERR_ARG (null or misaligned pointer, size below 1, sizes
+ * that do not match, unknown type), EMR_ERR_RANGE (a size of 2^31 - 256 or more, or
+ * more tiles than a launch has blocks), EMR_ERR_CAPACITY (workspace), EMR_ERR_CUDA. */
+enum { EMR_F32 = 0, EMR_BF16 = 1, EMR_F16 = 2 };
+typedef struct {
+    int32_t batch;
+    int32_t reserved;
+    int64_t rows, cols;
+    uint8_t *values, *scales;
+} emr_q8;
+
+/* Bytes of the two buffers. Host only. */
+emr_status emr_q8_size(int32_t batch, int64_t rows, int64_t cols, size_t *value_bytes, size_t *scale_bytes);
+
+/* Quantise batch matrices src[b * batch_stride + r * row_stride + c * col_stride]
+ * (strides in elements, >= 0; type EMR_F32, EMR_BF16 or EMR_F16) into q ([rows]
+ * [cols], blocks along the columns) and, or instead, into qt ([cols][rows], the
+ * transpose with blocks along the source's rows: the operand of the backward
+ * products). Either may be NULL, not both. Reads src once. */
+emr_status emr_q8_quantize(const void *src, int32_t dtype, int32_t batch, int64_t rows, int64_t cols,
+                           int64_t batch_stride, int64_t row_stride, int64_t col_stride, const emr_q8 *q,
+                           const emr_q8 *qt, void *stream);
+
+/* qt ([cols][rows]) receives the values that q stands for, quantised again with
+ * blocks along q's rows. As the scales are powers of two this is exact except for
+ * values that fall below the normal range of their new block. */
+emr_status emr_q8_transpose(const emr_q8 *q, const emr_q8 *qt, void *stream);
+
+/* The values that q stands for, as a dense [batch][rows][cols] array of dtype. */
+emr_status emr_q8_dequantize(const emr_q8 *q, void *out, int32_t dtype, void *stream);
+
+/* Backward of an activation from its 8-bit checkpoint: dz = dy * d, with dy dense
+ * [batch][rows][cols] of dtype and d the slope that emr_q8_matmul kept (NULL: dz =
+ * dy). Writes dz in 8 bits with blocks along the columns (dz, NULL for none) and,
+ * transposed, along the rows (dzt, NULL for none), and the column sums of dz
+ * before that rounding, db [batch][cols] of db_dtype (NULL for none; summed in 32
+ * bits in a fixed order). One pass over dy. ws: emr_q8_slope_workspace_size bytes
+ * (only used for db). */
+emr_status emr_q8_slope_workspace_size(int32_t batch, int64_t rows, int64_t cols, size_t *bytes);
+emr_status emr_q8_slope(const void *dy, int32_t dtype, int32_t batch, int64_t rows, int64_t cols, const emr_q8 *d,
+                        const emr_q8 *dz, const emr_q8 *dzt, void *db, int32_t db_dtype, void *ws, size_t ws_bytes,
+                        void *stream);
+
+/* out[b][m][n] = act(sum_k a[b][m][k] w[b][n][k] + bias[b][n]): the product of two
+ * 8-bit matrices with equal cols, sums in 32 bits, one rounding to out_dtype. An
+ * operand with batch 1 serves every b. sum_batch != 0 sums over b as well: out is
+ * [1][m][n] (the gradient of an input that all networks share; act must then be
+ * EMR_ACT_IDENTITY and bias NULL). bias: device float [batch][n] or NULL. slope
+ * (NULL for none): receives act'(z) in 8 bits, [batch][m][n] with blocks along n,
+ * which is all that the backward pass needs to keep of z. act: EMR_ACT_*; the
+ * slope of abs at 0 is 0. out is dense. A device-side wait that gives up (none is
+ * expected) leaves out undefined and is reported by emr_device_error. */
+emr_status emr_q8_matmul(const emr_q8 *a, const emr_q8 *w, const float *bias, int32_t act, int32_t sum_batch,
+                         void *out, int32_t out_dtype, const emr_q8 *slope, void *stream);
+
+/* Whether a bounded device-side wait of this library has given up since the last
+ * call: *code receives 0, or the number of the wait. Synchronises the stream. */
+emr_status emr_device_error(int32_t *code, void *stream);
+
 /* ---- misc -------------------------------------------------------------------- */
 
 /* Static description of a status code. */

@@ -1,0 +1,536 @@
+// Product of two block-scaled 8-bit matrices on the tensor cores:
+//   out[b][m][n] = act(sum_k a[b][m][k] w[b][n][k] + bias[b][n]),
+// optionally with act'(z) kept in 8 bits for the backward pass.
+//
+// With a = s_a q_a and w = s_w q_w and one scale for each row and block of 128
+// columns, z = sum_kb s_a(m, kb) s_w(n, kb) sum_{k in kb} q_a q_w. The scales are
+// powers of two in the format and granularity (a byte for each row, four blocks to a
+// word) that the block-scaled matrix instruction reads from tensor memory, so they
+// are applied inside it and no accumulator leaves tensor memory before the end of
+// the contraction; the instruction's own blocks of 32 columns all take the byte of
+// their block of 128.
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <mutex>
+
+#include "emr_q8.h"
+
+namespace {
+
+using namespace emr;
+
+// Number of a device-side wait that gave up (0: none); read by emr_device_error.
+__device__ int g_wait_error = 0;
+constexpr long long kWaitClocks = 4000000000ll;  // about 2 s
+
+// ---- barriers and copies -----------------------------------------------------------
+
+__device__ __forceinline__ uint32_t smem_at(const void* p) { return uint32_t(__cvta_generic_to_shared(p)); }
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(done)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return done != 0;
+}
+// Waits for the phase; gives up after kWaitClocks, or as soon as another wait of the
+// block has, and then records `code` once.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* gave_up, int code) {
+  if (bar_try(bar, parity)) return true;
+  const long long t0 = clock64();
+  while (!bar_try(bar, parity)) {
+    if (*gave_up) return false;
+    if (clock64() - t0 > kWaitClocks) {
+      *gave_up = code;
+      atomicCAS(&g_wait_error, 0, code);
+      return false;
+    }
+  }
+  return true;
+}
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+               "r"(bytes), "r"(bar)
+               : "memory");
+}
+
+// ---- tensor core -------------------------------------------------------------------
+
+// Operand tile: rows of 128 bytes, swizzled by 128 bytes, groups of 8 rows 1024 bytes apart.
+__device__ __forceinline__ uint64_t operand_desc(uint32_t addr) {
+  return uint64_t((addr & 0x3ffff) >> 4) | (uint64_t(1024 >> 4) << 32) | (uint64_t(1) << 46) | (uint64_t(2) << 61);
+}
+// Scale tile: 32 rows of 16 bytes, not swizzled, groups of 8 rows 128 bytes apart.
+__device__ __forceinline__ uint64_t scale_desc(uint32_t addr) {
+  return uint64_t((addr & 0x3ffff) >> 4) | (uint64_t(128 >> 4) << 32) | (uint64_t(1) << 46);
+}
+__device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc) {
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+__device__ __forceinline__ void mma_scaled(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb,
+                                           bool accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(uint32_t(accumulate))
+      : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// 32 columns of this warp's 32 accumulator rows: v[i] = column i of row `lane`.
+__device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
+  uint32_t r[32];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(addr));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < 32; i++) v[i] = __uint_as_float(r[i]);
+}
+
+// ---- activations and their slopes ----------------------------------------------------
+// sigmoid and tanh are taken from t = e^-|z| or e^-2|z| and r = 1 / (1 + t): every
+// form below is a product of positive terms, so the slopes keep their relative
+// precision where the functions saturate (1 - y^2 would lose it).
+
+template <bool kSlope>
+__device__ __forceinline__ void activate(int act, float (&z)[32], float (&d)[32]) {
+  switch (act) {
+    case EMR_ACT_SIGMOID:
+#pragma unroll
+      for (int i = 0; i < 32; i++) {
+        const float t = __expf(-fabsf(z[i])), r = __fdividef(1.f, 1.f + t);
+        if (kSlope) d[i] = t * r * r;
+        z[i] = z[i] >= 0.f ? r : t * r;
+      }
+      break;
+    case EMR_ACT_TANH:
+#pragma unroll
+      for (int i = 0; i < 32; i++) {
+        const float t = __expf(-2.f * fabsf(z[i])), r = __fdividef(1.f, 1.f + t);
+        if (kSlope) d[i] = 4.f * t * r * r;
+        // below 1/8 the odd series, whose next term is 17 z^7 / 315 (relative 3e-7)
+        const float q = z[i] * z[i];
+        const float series = z[i] * fmaf(q, fmaf(q, 2.f / 15.f, -1.f / 3.f), 1.f);
+        z[i] = fabsf(z[i]) < 0.125f ? series : copysignf((1.f - t) * r, z[i]);
+      }
+      break;
+    case EMR_ACT_GAUSS:
+#pragma unroll
+      for (int i = 0; i < 32; i++) {
+        const float y = __expf(-z[i] * z[i]);
+        if (kSlope) d[i] = y == 0.f ? 0.f : -2.f * z[i] * y;  // an infinite z has slope 0
+        z[i] = y;
+      }
+      break;
+    case EMR_ACT_SIN:
+#pragma unroll
+      for (int i = 0; i < 32; i++) {
+        float s, c;
+        sincosf(z[i], &s, &c);
+        if (kSlope) d[i] = c;
+        z[i] = s;
+      }
+      break;
+    case EMR_ACT_ABS:
+#pragma unroll
+      for (int i = 0; i < 32; i++) {
+        if (kSlope) d[i] = z[i] > 0.f ? 1.f : z[i] < 0.f ? -1.f : z[i];  // 0 at 0, NaN at NaN
+        z[i] = fabsf(z[i]);
+      }
+      break;
+    default:
+      if (kSlope) {
+#pragma unroll
+        for (int i = 0; i < 32; i++) d[i] = 1.f;
+      }
+  }
+}
+
+// ---- tiles ---------------------------------------------------------------------------
+
+constexpr int kTileM = 128, kTileN = 128, kTileK = 128;
+constexpr int kStages = 6;
+constexpr int kOperandBytes = 128 * 128;
+constexpr int kStageBytes = 2 * kOperandBytes;
+constexpr int kScaleBytes = 1024;           // 512 for each operand
+constexpr int kStagingBytes = 4 * 32 * 128; // for each epilogue warp 32 rows of 128 bytes
+constexpr int kThreads = 192;               // copy warp, matrix warp, four epilogue warps
+constexpr int kTmemColumns = 512;
+constexpr uint32_t kTmemScales = 256;       // behind the two accumulators of 128 columns
+constexpr int kSmemBytes = 1024 + kStages * (kStageBytes + kScaleBytes) + kStagingBytes;
+
+struct Params {
+  int64_t M, N;
+  int64_t m_tiles, n_tiles, tiles;  // tiles: over the batches of the output
+  int32_t k_blocks, k_chunks;       // blocks of 128 columns, and scale chunks of four of them
+  int32_t sum;                      // batches that one output sums over
+  int32_t a_one, w_one;             // operand with batch 1
+  const uint8_t *a_scales, *w_scales;
+  const float* bias;
+  int32_t act;
+  void* out;
+  int32_t out_dtype, store_bytes;   // store_bytes: widest store that every row of out is aligned to
+  uint8_t *slope, *slope_scales;
+};
+
+struct Tile {
+  int64_t b, m, n;
+};
+// Tiles in groups of 16 row tiles, so that the operand rows in use at a time stay in L2.
+__device__ __forceinline__ Tile tile_at(const Params& p, int64_t t) {
+  const int64_t per = p.m_tiles * p.n_tiles, b = t / per;
+  t -= b * per;
+  const int64_t group = t / (16 * p.n_tiles), first = group * 16;
+  const int64_t rows = p.m_tiles - first < 16 ? p.m_tiles - first : 16;
+  t -= first * p.n_tiles;
+  return {b, first + t % rows, t / rows};
+}
+
+// A warp's 32 staged rows of 128 bytes to global rows, `width` bytes a lane, neighbouring
+// lanes neighbouring addresses. `bytes` are valid in each row, `rows` rows.
+template <typename T>
+__device__ __forceinline__ void store_rows(const uint8_t* staged, uint8_t* out, int64_t pitch, int rows, int bytes, int lane) {
+  constexpr int kPer = 128 / int(sizeof(T));
+  for (int i = lane; i < 32 * kPer; i += 32) {
+    const int r = i / kPer, at = (i % kPer) * int(sizeof(T));
+    if (r < rows && at < bytes)
+      *reinterpret_cast<T*>(out + r * pitch + at) =
+          *reinterpret_cast<const T*>(staged + r * 128 + (((at >> 4) ^ (r & 7)) << 4) + (at & 15));
+  }
+}
+__device__ __forceinline__ void store_staged(const uint8_t* staged, uint8_t* out, int64_t pitch, int rows, int bytes, int width,
+                                             int lane) {
+  __syncwarp();
+  if (width == 16) store_rows<uint4>(staged, out, pitch, rows, bytes, lane);
+  else if (width == 8) store_rows<uint2>(staged, out, pitch, rows, bytes, lane);
+  else if (width == 4) store_rows<uint32_t>(staged, out, pitch, rows, bytes, lane);
+  else store_rows<uint16_t>(staged, out, pitch, rows, bytes, lane);
+  __syncwarp();
+}
+__device__ __forceinline__ void stage16(uint8_t* staged, int row, int unit, uint4 v) {
+  *reinterpret_cast<uint4*>(staged + row * 128 + ((unit ^ (row & 7)) << 4)) = v;
+}
+__device__ __forceinline__ uint32_t pack_half(int dtype, float a, float b) {
+  if (dtype == EMR_BF16) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// One row of 32 finished values, columns 32 c .. 32 c + 31 of the tile, to the staging rows
+// and, when 128 bytes of a row are there, to out.
+__device__ __forceinline__ void put_out(const Params& p, const Tile& t, int c, const float (&y)[32], uint8_t* staged,
+                                        int64_t row0, int lane) {
+  const int rows = int(p.M - row0 < 32 ? p.M - row0 : 32);  // may be below 1: nothing is stored
+  const int64_t n0 = t.n * kTileN;
+  if (p.out_dtype == EMR_F32) {
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+      stage16(staged, lane, i, make_uint4(__float_as_uint(y[4 * i]), __float_as_uint(y[4 * i + 1]),
+                                          __float_as_uint(y[4 * i + 2]), __float_as_uint(y[4 * i + 3])));
+    const int64_t left = (p.N - n0 - c * 32) * 4;
+    store_staged(staged, static_cast<uint8_t*>(p.out) + ((t.b * p.M + row0) * p.N + n0 + c * 32) * 4, p.N * 4, rows,
+                 int(left < 128 ? left : 128), p.store_bytes, lane);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; i++)
+    stage16(staged, lane, (c & 1) * 4 + i,
+            make_uint4(pack_half(p.out_dtype, y[8 * i], y[8 * i + 1]), pack_half(p.out_dtype, y[8 * i + 2], y[8 * i + 3]),
+                       pack_half(p.out_dtype, y[8 * i + 4], y[8 * i + 5]), pack_half(p.out_dtype, y[8 * i + 6], y[8 * i + 7])));
+  if (c & 1) {
+    const int64_t first = n0 + (c - 1) * 32, left = (p.N - first) * 2;
+    store_staged(staged, static_cast<uint8_t*>(p.out) + ((t.b * p.M + row0) * p.N + first) * 2, p.N * 2, rows,
+                 int(left < 128 ? left : 128), p.store_bytes, lane);
+  }
+}
+
+// The slopes of one row's 128 columns as 8-bit codes with their scale.
+__device__ __forceinline__ void put_slope(const Params& p, const Tile& t, float (&d)[4][32], uint8_t* staged, int64_t row0,
+                                          int lane) {
+  const int64_t n0 = t.n * kTileN;
+  const int left = int(p.N - n0 < 128 ? p.N - n0 : 128);
+  uint32_t top = 0;
+#pragma unroll
+  for (int c = 0; c < 4; c++)
+#pragma unroll
+    for (int i = 0; i < 32; i++) {
+      if (c * 32 + i >= left) d[c][i] = 0.f;
+      top = max(top, q8_magnitude(d[c][i]));
+    }
+  const uint32_t byte = q8_scale_byte(top);
+  const float inv = q8_inverse(byte);
+#pragma unroll
+  for (int u = 0; u < 8; u++) {
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+      const int i = (u & 1) * 16 + j * 4;
+      w[j] = q8_pack4(d[u >> 1][i], d[u >> 1][i + 1], d[u >> 1][i + 2], d[u >> 1][i + 3], inv);
+    }
+    stage16(staged, lane, u, make_uint4(w[0], w[1], w[2], w[3]));
+  }
+  const int rows = int(p.M - row0 < 32 ? p.M - row0 : 32);
+  const int64_t row_bytes = q8_row_bytes(p.N);
+  store_staged(staged, p.slope + (t.b * p.M + row0) * row_bytes + n0, row_bytes, rows, 128, 16, lane);
+  if (lane < rows)
+    p.slope_scales[t.b * q8_scale_batch(p.M, p.N) + q8_scale_at(q8_scale_chunks(p.N), row0 + lane, t.n)] = uint8_t(byte);
+}
+
+// Persistent: a block takes tiles blockIdx.x, + gridDim.x, ... Warp 0 copies operand and
+// scale tiles into a ring of stages, warp 1 issues the matrix instructions, warps 2..5
+// finish a tile while the next one accumulates in the other half of tensor memory.
+template <bool kSlope>
+__global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_constant__ CUtensorMap a_map,
+                                                                const __grid_constant__ CUtensorMap w_map,
+                                                                const __grid_constant__ Params p) {
+  extern __shared__ uint8_t raw[];
+  __shared__ uint64_t bars[2 * kStages + 4];
+  __shared__ uint32_t tmem_base;
+  __shared__ int gave_up;
+  uint8_t* const sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* const scales_sm = sm + kStages * kStageBytes;
+  uint8_t* const staging = scales_sm + kStages * kScaleBytes;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t full = smem_at(bars), empty = full + 8 * kStages, acc_full = empty + 8 * kStages, acc_empty = acc_full + 16;
+  volatile int* const stop = &gave_up;
+
+  if (threadIdx.x == 0) {
+    gave_up = 0;
+    for (int i = 0; i < kStages; i++) bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, 1);
+    for (int i = 0; i < 2; i++) bar_init(acc_full + 8 * i, 1), bar_init(acc_empty + 8 * i, 4);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&a_map) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&w_map) : "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&tmem_base)), "n"(kTmemColumns)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    fence_before();
+  }
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = tmem_base;
+  const int steps = p.sum * p.k_blocks;
+
+  if (warp == 0 && lane == 0) {
+    int64_t it = 0;
+    for (int64_t t = blockIdx.x; t < p.tiles && !*stop; t += gridDim.x) {
+      const Tile tile = tile_at(p, t);
+      for (int k = 0; k < steps; k++, it++) {
+        const int s = int(it % kStages);
+        if (it >= kStages && !bar_wait(empty + 8 * s, uint32_t(it / kStages - 1) & 1, stop, 1)) break;
+        const int sb = k / p.k_blocks, kb = k - sb * p.k_blocks;
+        const int64_t b = tile.b + sb, ab = p.a_one ? 0 : b, wb = p.w_one ? 0 : b;
+        const uint32_t bar = full + 8 * s, dst = smem_at(sm) + s * kStageBytes;
+        const bool scales = (kb & 3) == 0;
+        bar_expect(bar, kStageBytes + (scales ? kScaleBytes : 0));
+        tma_load(dst, &a_map, kb * kTileK, int(tile.m * kTileM), int(ab), bar);
+        tma_load(dst + kOperandBytes, &w_map, kb * kTileK, int(tile.n * kTileN), int(wb), bar);
+        if (scales) {
+          const uint32_t at = smem_at(scales_sm) + s * kScaleBytes;
+          bulk_load(at, p.a_scales + ((ab * p.m_tiles + tile.m) * p.k_chunks + (kb >> 2)) * 512, 512, bar);
+          bulk_load(at + 512, p.w_scales + ((wb * p.n_tiles + tile.n) * p.k_chunks + (kb >> 2)) * 512, 512, bar);
+        }
+      }
+    }
+    if (*stop) {  // copies in flight end before the block does
+      const int64_t from = it > kStages ? it - kStages : 0;
+      for (int64_t i = from; i < it; i++) {
+        const long long t0 = clock64();
+        while (!bar_try(full + 8 * int(i % kStages), uint32_t(i / kStages) & 1) && clock64() - t0 < kWaitClocks) {
+        }
+      }
+    }
+  } else if (warp == 1 && lane == 0) {
+    const uint32_t idesc = (1u << 23) | (uint32_t(kTileN >> 3) << 17) | (uint32_t(kTileM >> 4) << 24);
+    int64_t it = 0;
+    uint32_t n_tile = 0, chunk = 0;
+    for (int64_t t = blockIdx.x; t < p.tiles && !*stop; t += gridDim.x, n_tile++) {
+      const uint32_t acc = n_tile & 1;
+      if (n_tile >= 2 && !bar_wait(acc_empty + 8 * acc, ((n_tile >> 1) - 1) & 1, stop, 2)) break;
+      fence_after();
+      uint32_t sf = 0;
+      for (int k = 0; k < steps; k++, it++) {
+        const int s = int(it % kStages), kb = k % p.k_blocks;
+        if (!bar_wait(full + 8 * s, uint32_t(it / kStages) & 1, stop, 3)) break;
+        fence_after();
+        if ((kb & 3) == 0) {
+          sf = tmem + kTmemScales + 8 * (chunk++ & 1);
+          const uint32_t at = smem_at(scales_sm) + s * kScaleBytes;
+          copy_scales(sf, scale_desc(at));
+          copy_scales(sf + 4, scale_desc(at + 512));
+        }
+        const uint32_t at = smem_at(sm) + s * kStageBytes;
+        const uint64_t a = operand_desc(at), w = operand_desc(at + kOperandBytes);
+        const uint32_t id = idesc | (uint32_t(kb & 3) << 4) | (uint32_t(kb & 3) << 29);
+#pragma unroll
+        for (int j = 0; j < 4; j++)  // 32 columns each: 32 bytes further in the tile
+          mma_scaled(tmem + acc * kTileN, a + 2 * j, w + 2 * j, id, sf, sf + 4, k > 0 || j > 0);
+        mma_commit(empty + 8 * s);
+      }
+      mma_commit(acc_full + 8 * acc);
+    }
+  } else if (warp >= 2) {
+    const int quadrant = warp & 3;  // tensor memory lanes that this warp may read
+    uint8_t* const staged = staging + (warp - 2) * 32 * 128;
+    uint32_t n_tile = 0;
+    for (int64_t t = blockIdx.x; t < p.tiles; t += gridDim.x, n_tile++) {
+      const uint32_t acc = n_tile & 1;
+      const bool ok = __all_sync(0xffffffffu, bar_wait(acc_full + 8 * acc, (n_tile >> 1) & 1, stop, 4));
+      if (!ok) break;
+      fence_after();
+      const Tile tile = tile_at(p, t);
+      const int64_t row0 = tile.m * kTileM + quadrant * 32, n0 = tile.n * kTileN;
+      const float* bias = p.bias ? p.bias + tile.b * p.N + n0 : nullptr;
+      const uint32_t addr = tmem + acc * kTileN + (uint32_t(quadrant * 32) << 16);
+      float d[kSlope ? 4 : 1][32];
+#pragma unroll(kSlope ? 4 : 1)
+      for (int c = 0; c < 4; c++) {
+        float z[32];
+        tmem_load32(addr + c * 32, z);
+        if (c == 3) {
+          fence_before();
+          if (lane == 0) bar_arrive(acc_empty + 8 * acc);
+        }
+        if (bias) {
+          const float own = n0 + c * 32 + lane < p.N ? __ldg(bias + c * 32 + lane) : 0.f;
+#pragma unroll
+          for (int i = 0; i < 32; i++) z[i] += __shfl_sync(0xffffffffu, own, i);
+        }
+        activate<kSlope>(p.act, z, d[kSlope ? c : 0]);
+        put_out(p, tile, c, z, staged, row0, lane);
+      }
+      if constexpr (kSlope) put_slope(p, tile, d, staged, row0, lane);
+    }
+  }
+  __syncwarp();
+  fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(kTmemColumns) : "memory");
+  }
+}
+
+// ---- host ------------------------------------------------------------------------------
+
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encode_tiled() {
+  static std::once_flag once;
+  static EncodeTiled fn = nullptr;
+  std::call_once(once, [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) == cudaSuccess &&
+        found == cudaDriverEntryPointSuccess)
+      fn = reinterpret_cast<EncodeTiled>(p);
+  });
+  return fn;
+}
+
+// Boxes of 128 rows x 128 columns of a q8 matrix; rows past it read as zeros.
+bool operand_map(const emr_q8* q, CUtensorMap* map) {
+  const EncodeTiled fn = encode_tiled();
+  if (!fn) return false;
+  const cuuint64_t row_bytes = cuuint64_t(q8_row_bytes(q->cols));
+  const cuuint64_t dims[3] = {row_bytes, cuuint64_t(q->rows), cuuint64_t(q->batch)};
+  const cuuint64_t strides[2] = {row_bytes, row_bytes * cuuint64_t(q->rows)};
+  const cuuint32_t box[3] = {128, 128, 1}, ones[3] = {1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, q->values, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <bool kSlope>
+emr_status launch(const CUtensorMap& a, const CUtensorMap& w, const Params& p, cudaStream_t st) {
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+      cudaFuncSetAttribute(q8_matmul_kernel<kSlope>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes) != cudaSuccess)
+    return EMR_ERR_CUDA;
+  q8_matmul_kernel<kSlope><<<unsigned(p.tiles < sms ? p.tiles : sms), kThreads, kSmemBytes, st>>>(a, w, p);
+  return cudaGetLastError() == cudaSuccess ? EMR_OK : EMR_ERR_CUDA;
+}
+
+}  // namespace
+
+extern "C" emr_status emr_q8_matmul(const emr_q8* a, const emr_q8* w, const float* bias, int32_t act, int32_t sum_batch,
+                                    void* out, int32_t out_dtype, const emr_q8* slope, void* stream) {
+  if (!q8_ok(a) || !q8_ok(w) || a->cols != w->cols || !out || !dtype_ok(out_dtype) || act < EMR_ACT_IDENTITY ||
+      act > EMR_ACT_ABS || (a->batch != w->batch && a->batch != 1 && w->batch != 1))
+    return EMR_ERR_ARG;
+  const int32_t batch = a->batch > w->batch ? a->batch : w->batch;
+  if (sum_batch && (act != EMR_ACT_IDENTITY || bias || slope)) return EMR_ERR_ARG;
+  if (slope && (!q8_ok(slope) || slope->batch != batch || slope->rows != a->rows || slope->cols != w->rows)) return EMR_ERR_ARG;
+  const int size = dtype_bytes(out_dtype);
+  if (reinterpret_cast<uintptr_t>(out) % size || (bias && reinterpret_cast<uintptr_t>(bias) % 4)) return EMR_ERR_ARG;
+  Params p{};
+  p.M = a->rows, p.N = w->rows;
+  p.m_tiles = q8_blocks(p.M), p.n_tiles = q8_blocks(p.N);
+  const __int128 tiles = __int128(p.m_tiles) * p.n_tiles * (sum_batch ? 1 : batch);
+  const __int128 steps = __int128(q8_blocks(a->cols)) * (sum_batch ? batch : 1);
+  const int64_t reach = q8_row_bytes(a->cols) * (p.M > p.N ? p.M : p.N);  // bytes between two batches
+  if (tiles > INT64_MAX / 2 || steps > INT32_MAX || reach >= (int64_t(1) << 40)) return EMR_ERR_RANGE;
+  p.tiles = int64_t(tiles);
+  p.k_blocks = int32_t(q8_blocks(a->cols)), p.k_chunks = int32_t(q8_scale_chunks(a->cols));
+  p.sum = sum_batch ? batch : 1;
+  p.a_one = a->batch == 1, p.w_one = w->batch == 1;
+  p.a_scales = a->scales, p.w_scales = w->scales;
+  p.bias = bias, p.act = act, p.out = out, p.out_dtype = out_dtype;
+  p.store_bytes = 16;
+  while (p.store_bytes > size && (reinterpret_cast<uintptr_t>(out) % p.store_bytes || (p.N * size) % p.store_bytes)) p.store_bytes >>= 1;
+  if (slope) p.slope = slope->values, p.slope_scales = slope->scales;
+  CUtensorMap a_map, w_map;
+  if (!operand_map(a, &a_map) || !operand_map(w, &w_map)) return EMR_ERR_CUDA;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return slope ? launch<true>(a_map, w_map, p, st) : launch<false>(a_map, w_map, p, st);
+}
+
+extern "C" emr_status emr_device_error(int32_t* code, void* stream) {
+  if (!code) return EMR_ERR_ARG;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  int32_t got = 0;
+  const int32_t zero = 0;
+  if (cudaMemcpyFromSymbolAsync(&got, g_wait_error, 4, 0, cudaMemcpyDeviceToHost, st) != cudaSuccess ||
+      cudaStreamSynchronize(st) != cudaSuccess)
+    return EMR_ERR_CUDA;
+  if (got && (cudaMemcpyToSymbolAsync(g_wait_error, &zero, 4, 0, cudaMemcpyHostToDevice, st) != cudaSuccess ||
+              cudaStreamSynchronize(st) != cudaSuccess))
+    return EMR_ERR_CUDA;
+  *code = got;
+  return EMR_OK;
+}

@@ -97,6 +97,14 @@ def lib() -> C.CDLL:
             "emr_compact_workspace_size": [vp, i32, vp],
             "emr_compact": [vp, vp, vp, i32, vp, vp, i64, vp, vp, vp, sz, vp],
             "emr_compact_records": [vp, vp, vp, vp, sz, vp, vp, vp, i64, vp, vp, vp, sz, vp],
+            "emr_q8_size": [i32, i64, i64, vp, vp],
+            "emr_q8_quantize": [vp, i32, i32, i64, i64, i64, i64, i64, vp, vp, vp],
+            "emr_q8_transpose": [vp, vp, vp],
+            "emr_q8_dequantize": [vp, vp, i32, vp],
+            "emr_q8_slope_workspace_size": [i32, i64, i64, vp],
+            "emr_q8_slope": [vp, i32, i32, i64, i64, vp, vp, vp, vp, i32, vp, sz, vp],
+            "emr_q8_matmul": [vp, vp, vp, i32, i32, vp, i32, vp, vp],
+            "emr_device_error": [vp, vp],
             "emr_version": [],
             "emr_probe_alu": [i32, i32, i32, vp, vp, vp, vp],
         }
@@ -566,6 +574,227 @@ def ann_forward(nets: Networks, patterns, steps: int, device="cuda", stream=None
                                  _ptr(src), _ptr(dst), _ptr(w), K, _ptr(pat), steps, _ptr(out), _stream(stream)),
            "emr_ann_forward")
     return out
+
+
+# ---- dense substrate layers in 8-bit floating point ----------------------------------------
+
+ACT_IDENTITY, ACT_SIGMOID, ACT_TANH, ACT_GAUSS, ACT_SIN, ACT_ABS = range(6)
+EMR_F32, EMR_BF16, EMR_F16 = range(3)
+_DTYPES = {torch.float32: EMR_F32, torch.bfloat16: EMR_BF16, torch.float16: EMR_F16}
+
+
+class Q8C(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("reserved", C.c_int32), ("rows", C.c_int64), ("cols", C.c_int64),
+                ("values", C.c_void_p), ("scales", C.c_void_p)]
+
+
+def _dtype(t, what: str) -> int:
+    d = _DTYPES.get(t)
+    if d is None:
+        raise ValueError("%s: float32, bfloat16 or float16 is wanted, got %s" % (what, t))
+    return d
+
+
+def _matrices(x, what: str):
+    """x as [batch, rows, cols] on the GPU (a view)."""
+    if not isinstance(x, torch.Tensor) or x.dim() not in (2, 3):
+        raise ValueError("%s: a tensor of two or three dimensions is wanted" % what)
+    if x.device.type != "cuda":
+        raise ValueError("%s: a tensor on the GPU is wanted" % what)
+    return x if x.dim() == 3 else x.unsqueeze(0)
+
+
+def _on(stream):
+    """Allocations for work on `stream` belong to it (the caching allocator reuses memory by stream)."""
+    return torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream())
+
+
+class Q8:
+    """Matrices [batch, rows, cols] in 8-bit floating point with one power-of-two scale for each block of
+    128 columns of a row (emr_q8): values uint8 [batch, rows, cols rounded up to 128] (e4m3 codes), scales
+    uint8 (tiles of 128 rows x 4 blocks)."""
+
+    def __init__(self, batch: int, rows: int, cols: int, device="cuda"):
+        n, m = C.c_size_t(), C.c_size_t()
+        _check(lib().emr_q8_size(batch, rows, cols, C.byref(n), C.byref(m)), "emr_q8_size")
+        self.batch, self.rows, self.cols = batch, rows, cols
+        self.values = torch.empty(n.value, dtype=torch.uint8, device=device)
+        self.scales = torch.empty(m.value, dtype=torch.uint8, device=device)
+        self.c = Q8C(batch, 0, rows, cols, self.values.data_ptr(), self.scales.data_ptr())
+
+    @property
+    def ref(self):
+        return C.byref(self.c)
+
+    @property
+    def device(self):
+        return self.values.device
+
+    @property
+    def shape(self):
+        return self.batch, self.rows, self.cols
+
+
+def _ref(q):
+    return q.ref if q is not None else None
+
+
+def q8_quantize(x, q: Q8 | None = None, qt: Q8 | None = None, stream=None):
+    """emr_q8_quantize: x [batch, rows, cols] or [rows, cols], any strides, into q (blocks along the columns)
+    and, or instead, qt (the transpose, blocks along the rows). With neither, a new q. Returns (q, qt)."""
+    x = _matrices(x, "x")
+    with _on(stream):
+        if q is None and qt is None:
+            q = Q8(*x.shape, device=x.device)
+        _check(lib().emr_q8_quantize(x.data_ptr(), _dtype(x.dtype, "x"), *x.shape, *x.stride(), _ref(q), _ref(qt),
+                                     _stream(stream)), "emr_q8_quantize")
+    return q, qt
+
+
+def q8_transpose(q: Q8, qt: Q8 | None = None, stream=None) -> Q8:
+    """emr_q8_transpose: the transpose of what q holds, with blocks along q's rows."""
+    with _on(stream):
+        if qt is None:
+            qt = Q8(q.batch, q.cols, q.rows, device=q.device)
+        _check(lib().emr_q8_transpose(q.ref, qt.ref, _stream(stream)), "emr_q8_transpose")
+    return qt
+
+
+def q8_dequantize(q: Q8, dtype=torch.float32, stream=None):
+    """emr_q8_dequantize: the values that q stands for, a new [batch, rows, cols] tensor."""
+    with _on(stream):
+        out = torch.empty(q.shape, dtype=dtype, device=q.device)
+        _check(lib().emr_q8_dequantize(q.ref, out.data_ptr(), _dtype(dtype, "dtype"), _stream(stream)),
+               "emr_q8_dequantize")
+    return out
+
+
+def q8_matmul(a: Q8, w: Q8, bias=None, act: int = ACT_IDENTITY, out_dtype=torch.float32, slope: Q8 | None = None,
+              sum_batch: bool = False, out=None, stream=None):
+    """emr_q8_matmul: act(a w^T + bias), [batch, a.rows, w.rows] ([1, ...] with sum_batch). An operand of
+    batch 1 serves every batch; slope receives act'(z) in 8 bits."""
+    batch = max(a.batch, w.batch)
+    shape = (1 if sum_batch else batch, a.rows, w.rows)
+    if bias is not None and (bias.dtype != torch.float32 or not bias.is_contiguous() or
+                             bias.numel() != batch * w.rows or bias.device != a.device):
+        raise ValueError("bias: a contiguous float32 tensor [batch, rows of w] on the operands' GPU is wanted")
+    if a.device != w.device or (slope is not None and slope.device != a.device):
+        raise ValueError("operands on one GPU are wanted")
+    with _on(stream):
+        if out is None:
+            out = torch.empty(shape, dtype=out_dtype, device=a.device)
+        elif tuple(out.shape) != shape or not out.is_contiguous() or out.device != a.device:
+            raise ValueError("out: a contiguous tensor %s is wanted" % (shape,))
+        _check(lib().emr_q8_matmul(a.ref, w.ref, _ptr(bias), act, 1 if sum_batch else 0, out.data_ptr(),
+                                   _dtype(out.dtype, "out"), _ref(slope), _stream(stream)), "emr_q8_matmul")
+    return out
+
+
+def q8_slope(dy, d: Q8 | None, dz: Q8 | None = None, dzt: Q8 | None = None, db=None, stream=None):
+    """emr_q8_slope: dz = dy * d into dz and, transposed, dzt, and its column sums into db [batch, cols]."""
+    dy = _matrices(dy, "dy")
+    batch, rows, cols = dy.shape
+    if db is not None and (db.numel() != batch * cols or not db.is_contiguous() or db.device != dy.device):
+        raise ValueError("db: a contiguous tensor [batch, cols] is wanted")
+    n = C.c_size_t()
+    with _on(stream):
+        dy, ws = dy.contiguous(), None
+        if db is not None:
+            _check(lib().emr_q8_slope_workspace_size(batch, rows, cols, C.byref(n)), "emr_q8_slope_workspace_size")
+            ws = torch.empty(n.value, dtype=torch.uint8, device=dy.device)
+        _check(lib().emr_q8_slope(dy.data_ptr(), _dtype(dy.dtype, "dy"), batch, rows, cols, _ref(d), _ref(dz),
+                                  _ref(dzt), _ptr(db), _dtype(db.dtype, "db") if db is not None else 0, _ptr(ws),
+                                  C.c_size_t(n.value), _stream(stream)), "emr_q8_slope")
+
+
+def device_error(stream=None) -> int:
+    """emr_device_error: 0, or the number of a device-side wait that gave up since the last call."""
+    code = C.c_int32()
+    _check(lib().emr_device_error(C.byref(code), _stream(stream)), "emr_device_error")
+    return code.value
+
+
+class DenseLayer:
+    """y = act(x w^T + b) for one network, or for a batch of networks with weights of their own, in 8-bit
+    floating point with 32-bit sums: a HyperNEAT substrate that connects every source to every position
+    (w: outputs x sources, any strides, so the transpose of emr_eval's materialised [slots, positions] output
+    is taken as it is).
+
+    w [n, k] or [nets, n, k] (float32, bfloat16, float16), b [n] or [nets, n] float32 or None. x is [m, k],
+    [1, m, k] (shared by all networks) or [nets, m, k]; results are three-dimensional. The layer keeps the
+    weights in 8 bits (with train=True also their transpose, which the backward pass reads), not w itself:
+    after an update of w call set_weights. A training step keeps x and act'(z) in 8 bits, 2 bytes in all for
+    each pair, and takes its gradients from those.
+    """
+
+    def __init__(self, w, b=None, act: int = ACT_IDENTITY, train: bool = False, stream=None):
+        w = _matrices(w, "w")
+        if not ACT_IDENTITY <= act <= ACT_ABS:
+            raise ValueError("act: one of ACT_* is wanted, got %r" % (act,))
+        self.nets, self.n, self.k = w.shape
+        self.act, self.train = act, train
+        with _on(stream):
+            self.w8 = Q8(*w.shape, device=w.device)
+            self.w8t = Q8(self.nets, self.k, self.n, device=w.device) if train else None
+        self.set_weights(w, b, stream)
+
+    def set_weights(self, w, b=None, stream=None):
+        """Lay out new weights (same shape) and keep the bias (None: no bias)."""
+        w = _matrices(w, "w")
+        if tuple(w.shape) != (self.nets, self.n, self.k) or w.device != self.w8.device:
+            raise ValueError("w: shape %s on %s is wanted" % ((self.nets, self.n, self.k), self.w8.device))
+        if b is not None:
+            if b.dtype != torch.float32 or b.numel() != self.nets * self.n or b.device != w.device:
+                raise ValueError("b: a float32 tensor [%d, %d] on the layer's GPU is wanted" % (self.nets, self.n))
+            with _on(stream):
+                b = b.contiguous()
+        self.b = b
+        q8_quantize(w, self.w8, self.w8t, stream)
+
+    def _x(self, x):
+        x = _matrices(x, "x")
+        if x.shape[2] != self.k or x.shape[0] not in (1, self.nets) or x.device != self.w8.device:
+            raise ValueError("x: [m, %d], [1, m, %d] or [%d, m, %d] on the layer's GPU is wanted, got %s" %
+                             (self.k, self.k, self.nets, self.k, tuple(x.shape)))
+        return x
+
+    def forward(self, x, out_dtype=torch.float32, stream=None):
+        """y [nets, m, n] of out_dtype. m = 0 gives an empty result."""
+        x = self._x(x)
+        if x.shape[1] == 0:
+            return torch.empty(self.nets, 0, self.n, dtype=out_dtype, device=x.device)
+        q, _ = q8_quantize(x, stream=stream)
+        return q8_matmul(q, self.w8, self.b, self.act, out_dtype, stream=stream)
+
+    def forward_train(self, x, out_dtype=torch.float32, stream=None):
+        """(y, saved): saved holds x and act'(z) in 8 bits for backward."""
+        if not self.train:
+            raise ValueError("forward_train: the layer was made with train=False")
+        x = self._x(x)
+        if x.shape[1] == 0:
+            raise ValueError("x: at least one row is wanted for training")
+        q, _ = q8_quantize(x, stream=stream)
+        slope = None
+        if self.act != ACT_IDENTITY:
+            with _on(stream):
+                slope = Q8(self.nets, x.shape[1], self.n, device=x.device)
+        return q8_matmul(q, self.w8, self.b, self.act, out_dtype, slope, stream=stream), (q, slope)
+
+    def backward(self, dy, saved, out_dtype=torch.float32, stream=None):
+        """(dx, dw, db) of out_dtype for dy [nets, m, n]: dx in the shape that forward_train took x in (summed
+        over the networks where x was shared), dw [nets, n, k], db [nets, n] (also without a bias)."""
+        q, slope = saved
+        dy = _matrices(dy, "dy")
+        if tuple(dy.shape) != (self.nets, q.rows, self.n) or dy.device != q.device:
+            raise ValueError("dy: shape %s is wanted, got %s" % ((self.nets, q.rows, self.n), tuple(dy.shape)))
+        with _on(stream):
+            dz = Q8(self.nets, q.rows, self.n, device=q.device)
+            dzt = Q8(self.nets, self.n, q.rows, device=q.device)
+            db = torch.empty(self.nets, self.n, dtype=out_dtype, device=q.device)
+        q8_slope(dy, slope, dz, dzt, db, stream)
+        dx = q8_matmul(dz, self.w8t, out_dtype=out_dtype, sum_batch=q.batch < self.nets, stream=stream)
+        dw = q8_matmul(dzt, q8_transpose(q, stream=stream), out_dtype=out_dtype, stream=stream)
+        return dx, dw, db
 
 
 # ---- ALU probes (roofline denominators) -------------------------------------------------
