@@ -671,6 +671,34 @@ emr_status emr_q8_matmul(const emr_q8 *a, const emr_q8 *w, const float *bias, in
  * call: *code receives 0, or the number of the wait. Synchronises the stream. */
 emr_status emr_device_error(int32_t *code, void *stream);
 
+/* ---- sampling from scores ----------------------------------------------------- */
+
+/* One index for each row of scores, drawn from given random numbers. scores: device
+ * [rows][n] of dtype, row r at scores + r * row_stride elements; noise: device float
+ * [rows][n], row r at noise + r * noise_stride, positive Exp(1) draws.
+ * With T, k, p and q a row's temperature, top-k, top-p and min-p (device arrays of
+ * rows, or NULL for the scalar beside them), s_max its largest score and
+ * w_i = exp((s_i - s_max) / T): scores of -infinity and NaN are masked; the entries
+ * are ordered by score, larger first, then by index; the first k stay (k <= 0: all);
+ * of those, entry i stays when the sum of w before it is below p times the sum of w
+ * over them (p >= 1: all); then those with w_i >= q. index[r] is the entry with the
+ * largest w_i / noise_i among those that stay (ties: the lowest index), which is a draw
+ * with probabilities w_i / sum w; logp[r] (NULL for none) is the log of that
+ * probability. T <= 0 takes the largest score (lowest index) with logp 0. A row with
+ * nothing left (all masked) gives index -1 and logp -infinity; a score of +infinity
+ * leaves only the entries that equal it. q above 1 counts as 1 and p below 0 as 0: the
+ * largest score always stays. Sums of w are taken in fixed point (steps of 2^-44, for n
+ * above 2^18 of 2^-43 and so on), so results do not depend on the order of execution.
+ * Reads scores once where a row's share of them fits into the shared memory of its
+ * blocks (up to about 350,000 entries of 4 bytes). Errors: EMR_ERR_ARG (null or
+ * misaligned pointer, size below 1, negative stride, unknown type), EMR_ERR_RANGE (n
+ * above 2^31 - 1, rows above 2^27), EMR_ERR_CUDA. */
+emr_status emr_sample(const void *scores, int32_t dtype, int32_t rows, int64_t n, int64_t row_stride,
+                      const float *noise, int64_t noise_stride, const float *temperature, float temperature_all,
+                      const int32_t *top_k, int32_t top_k_all, const float *top_p, float top_p_all,
+                      const float *min_p, float min_p_all, int32_t *index, float *logp,
+                      void *stream);
+
 /* ---- misc -------------------------------------------------------------------- */
 
 /* Static description of a status code. */

@@ -105,6 +105,7 @@ def lib() -> C.CDLL:
             "emr_q8_slope": [vp, i32, i32, i64, i64, vp, vp, vp, vp, i32, vp, sz, vp],
             "emr_q8_matmul": [vp, vp, vp, i32, i32, vp, i32, vp, vp],
             "emr_device_error": [vp, vp],
+            "emr_sample": [vp, i32, i32, i64, i64, vp, i64, vp, f32, vp, i32, vp, f32, vp, f32, vp, vp, vp],
             "emr_version": [],
             "emr_probe_alu": [i32, i32, i32, vp, vp, vp, vp],
         }
@@ -795,6 +796,47 @@ class DenseLayer:
         dx = q8_matmul(dz, self.w8t, out_dtype=out_dtype, sum_batch=q.batch < self.nets, stream=stream)
         dw = q8_matmul(dzt, q8_transpose(q, stream=stream), out_dtype=out_dtype, stream=stream)
         return dx, dw, db
+
+
+# ---- sampling from scores -------------------------------------------------------------------
+
+def _per_row(v, rows: int, dtype, device, what: str):
+    """(device array or None, scalar) of a parameter given for all rows or for each."""
+    if not isinstance(v, torch.Tensor):
+        return None, v
+    if v.shape != (rows,) or v.dtype != dtype or v.device != device or not v.is_contiguous():
+        raise ValueError("%s: a number or a contiguous %s tensor [%d] on the scores' GPU is wanted" % (what, dtype, rows))
+    return v.data_ptr(), 0
+
+
+def sample(scores, noise, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, stream=None):
+    """emr_sample: one index for each row of scores [rows, n] (or [n]; float32, bfloat16, float16), drawn with
+    the given Exp(1) noise (float32, same shape). Parameters are numbers, or tensors [rows] (float32; top_k
+    int32). Returns (index int32 [rows], log probability float32 [rows])."""
+    if not isinstance(scores, torch.Tensor) or scores.dim() not in (1, 2) or scores.device.type != "cuda":
+        raise ValueError("scores: a tensor [rows, n] or [n] on the GPU is wanted")
+    if noise.shape != scores.shape or noise.dtype != torch.float32 or noise.device != scores.device:
+        raise ValueError("noise: a float32 tensor in the shape of scores on the same GPU is wanted")
+    if scores.dim() == 1:
+        scores, noise = scores.unsqueeze(0), noise.unsqueeze(0)
+    rows, n = scores.shape
+    kind = _dtype(scores.dtype, "scores")
+    dev = scores.device
+    t = _per_row(temperature, rows, torch.float32, dev, "temperature")
+    k = _per_row(top_k, rows, torch.int32, dev, "top_k")
+    p = _per_row(top_p, rows, torch.float32, dev, "top_p")
+    q = _per_row(min_p, rows, torch.float32, dev, "min_p")
+    with _on(stream):
+        if scores.stride(1) != 1:
+            scores = scores.contiguous()
+        if noise.stride(1) != 1:
+            noise = noise.contiguous()
+        index = torch.empty(rows, dtype=torch.int32, device=dev)
+        logp = torch.empty(rows, dtype=torch.float32, device=dev)
+        if rows:
+            _check(lib().emr_sample(scores.data_ptr(), kind, rows, n, scores.stride(0), noise.data_ptr(), noise.stride(0),
+                                    *t, *k, *p, *q, index.data_ptr(), logp.data_ptr(), _stream(stream)), "emr_sample")
+    return index, logp
 
 
 # ---- ALU probes (roofline denominators) -------------------------------------------------
