@@ -18,25 +18,20 @@ using namespace emr;
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 
-__device__ __forceinline__ uint32_t warp_max(uint32_t v) { return __reduce_max_sync(0xffffffffu, v); }
-__device__ __forceinline__ uint32_t magnitude4(float4 v) {
-  return max(max(q8_magnitude(v.x), q8_magnitude(v.y)), max(q8_magnitude(v.z), q8_magnitude(v.w)));
-}
-
-// Sources: four columns c .. c + 3 of row r, zero past the matrix.
-struct DenseSource {
-  const void* p;
-  int dtype;
-  int64_t row_stride, col_stride;
-  bool vector;  // col_stride 1 and every row aligned to four elements
-  __device__ __forceinline__ float4 four(int64_t base, int64_t r, int64_t c, int64_t cols) const {
-    const int64_t at = base + r * row_stride;
-    if (vector && c + 4 <= cols) return load_four(p, dtype, at + c);
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (c < cols) v.x = load_scalar(p, dtype, at + c * col_stride);
-    if (c + 1 < cols) v.y = load_scalar(p, dtype, at + (c + 1) * col_stride);
-    if (c + 2 < cols) v.z = load_scalar(p, dtype, at + (c + 2) * col_stride);
-    if (c + 3 < cols) v.w = load_scalar(p, dtype, at + (c + 3) * col_stride);
+// Dense source: four columns c .. c + 3 of a row, zero past the matrix. kVector: columns
+// are neighbours and every row is aligned to four elements.
+template <typename T, bool kVector>
+struct Dense {
+  const T* p;
+  int64_t batch_stride, row_stride, col_stride;
+  __device__ __forceinline__ Four<T> four(const T* row, int64_t c, int64_t cols) const {
+    Four<T> v;
+    if (kVector && c + 4 <= cols) {
+      v.load(row + c);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; j++) v.set(j, c + j < cols ? row[(c + j) * (kVector ? 1 : col_stride)] : T(0.f));
+    }
     return v;
   }
 };
@@ -50,25 +45,31 @@ __device__ __forceinline__ float4 q8_four(const uint8_t* values, const uint8_t* 
 
 // Row blocks only: one warp takes four blocks of 128 columns of one row, whose four
 // scale bytes are one word.
-__global__ void __launch_bounds__(kThreads) q8_rows_kernel(DenseSource src, int64_t batch_stride, int64_t rows,
-                                                           int64_t cols, int64_t units, emr_q8 q) {
+template <typename T, bool kVector>
+__global__ void __launch_bounds__(kThreads) q8_rows_kernel(Dense<T, kVector> src, int64_t rows, int64_t cols, int64_t units,
+                                                           emr_q8 q) {
   const int64_t chunks = q8_scale_chunks(cols), blocks = q8_blocks(cols), row_bytes = q8_row_bytes(cols);
   const int64_t unit = int64_t(blockIdx.x) * kWarps + (threadIdx.x >> 5);
   if (unit >= units) return;
   const int lane = threadIdx.x & 31;
-  const int64_t chunk = unit % chunks, row = unit / chunks, b = row / rows, r = row - b * rows;
-  float4 v[4];
+  // divisions in 32 bits where they suffice: they cost as much as a block's work otherwise
+  const bool small = units <= UINT32_MAX;
+  const int64_t row = small ? uint32_t(unit) / uint32_t(chunks) : unit / chunks, chunk = unit - row * chunks;
+  const int64_t b = small ? uint32_t(row) / uint32_t(rows) : row / rows, r = row - b * rows;
+  const T* from = src.p + b * src.batch_stride + r * src.row_stride;
+  const int64_t c = chunk * 512 + lane * 4;
+  Four<T> u[4];
 #pragma unroll
-  for (int j = 0; j < 4; j++) v[j] = src.four(b * batch_stride, r, (chunk * 4 + j) * 128 + lane * 4, cols);
-  uint8_t* out = q.values + (b * rows + r) * row_bytes;
+  for (int j = 0; j < 4; j++) u[j] = src.four(from, c + j * 128, cols);
+  uint8_t* out = q.values + row * row_bytes + c;
   uint32_t word = 0;
 #pragma unroll
   for (int j = 0; j < 4; j++) {
-    const uint32_t byte = q8_scale_byte(warp_max(magnitude4(v[j])));
+    float4 v = u[j].floats();
+    const uint32_t byte = q8_warp_scale(v);
     word |= byte << (8 * j);
     if (chunk * 4 + j < blocks)
-      *reinterpret_cast<uint32_t*>(out + (chunk * 4 + j) * 128 + lane * 4) =
-          q8_pack4(v[j].x, v[j].y, v[j].z, v[j].w, q8_inverse(byte));
+      *reinterpret_cast<uint32_t*>(out + j * 128) = q8_pack4(v.x, v.y, v.z, v.w, q8_inverse(byte));
   }
   if (lane == 0)
     *reinterpret_cast<uint32_t*>(q.scales + b * q8_scale_batch(rows, cols) + q8_scale_at(chunks, r, chunk * 4)) = word;
@@ -76,68 +77,91 @@ __global__ void __launch_bounds__(kThreads) q8_rows_kernel(DenseSource src, int6
 
 // One 128 x 128 tile: row blocks to q, column blocks (the transpose) to qt, column
 // sums to sums[b][row tile][cols]. Mode 0: a dense source; 1: the values of an 8-bit
-// matrix; 2: the product of a dense matrix and an 8-bit one.
-template <int kMode>
-__global__ void __launch_bounds__(kThreads) q8_tile_kernel(DenseSource src, int64_t batch_stride, emr_q8 other,
-                                                           int64_t rows, int64_t cols, emr_q8 q, emr_q8 qt,
-                                                           float* sums) {
+// matrix; 2: the product of a dense matrix and an 8-bit one. A warp has the rows
+// 16 warp .. 16 warp + 15 and loads eight of them before it uses the first.
+template <int kMode, typename T, bool kVector>
+__global__ void __launch_bounds__(kThreads, 3) q8_tile_kernel(Dense<T, kVector> src, emr_q8 other, int64_t rows, int64_t cols,
+                                                              emr_q8 q, emr_q8 qt, float* sums) {
   extern __shared__ float4 tile[];  // [128][32]
+  __shared__ uint8_t row_scales[128], col_scales[128];
   const int64_t row_tiles = q8_blocks(rows), col_tiles = q8_blocks(cols);
   const int64_t ct = blockIdx.x % col_tiles, rest = blockIdx.x / col_tiles, rt = rest % row_tiles, b = rest / row_tiles;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t chunks = q8_scale_chunks(cols), row_bytes = q8_row_bytes(cols), scale_batch = q8_scale_batch(rows, cols);
   const int64_t c = ct * 128 + lane * 4;
-  uint8_t* qv = q.values ? q.values + b * rows * row_bytes : nullptr;
-  uint8_t* qs = q.values ? q.scales + b * scale_batch : nullptr;
-#pragma unroll 4
-  for (int i = warp; i < 128; i += kWarps) {
-    const int64_t r = rt * 128 + i;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (r < rows) {
-      if (kMode != 1) v = src.four(b * batch_stride, r, c, cols);
-      if (kMode != 0) {
-        const float4 u = q8_four(other.values + b * rows * row_bytes, other.scales + b * scale_batch, row_bytes, chunks, r, c);
-        // one rounding each, so that the values are those of the plain product
-        v = kMode == 1 ? u : make_float4(__fmul_rn(v.x, u.x), __fmul_rn(v.y, u.y), __fmul_rn(v.z, u.z), __fmul_rn(v.w, u.w));
+  const int64_t left = rows - rt * 128;
+  const int have = int(left < 128 ? left : 128);  // rows of the tile
+  const int wide = int(cols - ct * 128 < 128 ? cols - ct * 128 : 128);
+  const int first = warp * 16;
+  const T* from = kMode != 1 ? src.p + b * src.batch_stride + (rt * 128 + first) * src.row_stride : nullptr;
+  const int64_t at = (b * rows + rt * 128 + first) * row_bytes + c;  // of the warp's first row in 8-bit matrices of this shape
+  const uint8_t* codes = kMode != 0 ? other.values + at : nullptr;
+  uint8_t* out = q.values ? q.values + at : nullptr;
+  uint32_t scale_bytes = 127;
+  if (kMode != 0 && lane < 16 && first + lane < have)
+    scale_bytes = other.scales[b * scale_batch + q8_scale_at(chunks, rt * 128 + first + lane, ct)];
+#pragma unroll
+  for (int i0 = 0; i0 < 16; i0 += 8) {
+    Four<T> u[8];
+    uint32_t code[8];
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+      if (first + i0 + i < have) {
+        if (kMode != 1) u[i] = src.four(from + (i0 + i) * src.row_stride, c, cols);
+        if (kMode != 0) code[i] = *reinterpret_cast<const uint32_t*>(codes + (i0 + i) * row_bytes);
+      }
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      const int r = first + i0 + i;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (r < have) {
+        if (kMode != 1) v = u[i].floats();
+        if (kMode != 0) {
+          const float s = q8_scale(__shfl_sync(0xffffffffu, scale_bytes, i0 + i));
+          float4 d = q8_unpack4(code[i]);
+          d = make_float4(d.x * s, d.y * s, d.z * s, d.w * s);
+          // one rounding each, so that the values are those of the plain product
+          v = kMode == 1 ? d : make_float4(__fmul_rn(v.x, d.x), __fmul_rn(v.y, d.y), __fmul_rn(v.z, d.z), __fmul_rn(v.w, d.w));
+        }
+      }
+      tile[r * 32 + (lane ^ ((r >> 2) & 7))] = v;
+      if (out && r < have) {
+        const uint32_t byte = q8_warp_scale(v);
+        *reinterpret_cast<uint32_t*>(out + (i0 + i) * row_bytes) = q8_pack4(v.x, v.y, v.z, v.w, q8_inverse(byte));
+        if (lane == 0) row_scales[r] = uint8_t(byte);
       }
     }
-    if (qv && r < rows) {
-      const uint32_t byte = q8_scale_byte(warp_max(magnitude4(v)));
-      *reinterpret_cast<uint32_t*>(qv + r * row_bytes + c) = q8_pack4(v.x, v.y, v.z, v.w, q8_inverse(byte));
-      if (lane == 0) qs[q8_scale_at(chunks, r, ct)] = uint8_t(byte);
-    }
-    if (qt.values || sums) tile[i * 32 + (lane ^ ((i >> 2) & 7))] = v;
   }
-  if (!qt.values && !sums) return;
   __syncthreads();
-  const int64_t t_chunks = q8_scale_chunks(rows), t_row_bytes = q8_row_bytes(rows);
-  uint8_t* tv = qt.values ? qt.values + b * cols * t_row_bytes : nullptr;
-  uint8_t* ts = qt.values ? qt.scales + b * q8_scale_batch(cols, rows) : nullptr;
+  const int64_t t_row_bytes = q8_row_bytes(rows);
+  uint8_t* tout = qt.values ? qt.values + (b * cols + ct * 128) * t_row_bytes + rt * 128 + lane * 4 : nullptr;
   for (int i = warp; i < 32; i += kWarps) {  // columns 4 i .. 4 i + 3, rows 4 lane .. 4 lane + 3
     float4 v[4];
 #pragma unroll
     for (int j = 0; j < 4; j++) v[j] = tile[(lane * 4 + j) * 32 + (i ^ (lane & 7))];
-    const float col[4][4] = {{v[0].x, v[1].x, v[2].x, v[3].x}, {v[0].y, v[1].y, v[2].y, v[3].y},
-                             {v[0].z, v[1].z, v[2].z, v[3].z}, {v[0].w, v[1].w, v[2].w, v[3].w}};
+    float4 col[4] = {make_float4(v[0].x, v[1].x, v[2].x, v[3].x), make_float4(v[0].y, v[1].y, v[2].y, v[3].y),
+                     make_float4(v[0].z, v[1].z, v[2].z, v[3].z), make_float4(v[0].w, v[1].w, v[2].w, v[3].w)};
 #pragma unroll
     for (int j = 0; j < 4; j++) {
-      const int64_t n = ct * 128 + i * 4 + j;
-      if (tv) {
-        const uint32_t byte = q8_scale_byte(warp_max(magnitude4(make_float4(col[j][0], col[j][1], col[j][2], col[j][3]))));
-        if (n < cols) {
-          *reinterpret_cast<uint32_t*>(tv + n * t_row_bytes + rt * 128 + lane * 4) =
-              q8_pack4(col[j][0], col[j][1], col[j][2], col[j][3], q8_inverse(byte));
-          if (lane == 0) ts[q8_scale_at(t_chunks, n, rt)] = uint8_t(byte);
-        }
-      }
+      const int n = i * 4 + j;
       if (sums) {
-        float s = (col[j][0] + col[j][1]) + (col[j][2] + col[j][3]);
+        float s = (col[j].x + col[j].y) + (col[j].z + col[j].w);
 #pragma unroll
         for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-        if (lane == 0 && n < cols) sums[(b * row_tiles + rt) * cols + n] = s;
+        if (lane == 0 && n < wide) sums[(b * row_tiles + rt) * cols + ct * 128 + n] = s;
+      }
+      if (tout && n < wide) {
+        const uint32_t byte = q8_warp_scale(col[j]);
+        *reinterpret_cast<uint32_t*>(tout + n * t_row_bytes) = q8_pack4(col[j].x, col[j].y, col[j].z, col[j].w, q8_inverse(byte));
+        if (lane == 0) col_scales[n] = uint8_t(byte);
       }
     }
   }
+  __syncthreads();
+  const int i = threadIdx.x;
+  if (out && i < have) q.scales[b * scale_batch + q8_scale_at(chunks, rt * 128 + i, ct)] = row_scales[i];
+  if (tout && i >= 128 && i - 128 < wide)
+    qt.scales[b * q8_scale_batch(cols, rows) + q8_scale_at(q8_scale_chunks(rows), ct * 128 + i - 128, rt)] = col_scales[i - 128];
 }
 
 // Sum of the row tiles' column sums, in the order of the tiles.
@@ -168,18 +192,46 @@ __global__ void __launch_bounds__(kThreads) q8_dequantize_kernel(emr_q8 q, int64
 constexpr int64_t kMaxGrid = (int64_t(1) << 31) - 1;
 constexpr int kTileBytes = 128 * 128 * 4;
 
-template <int kMode>
-emr_status launch_tile(const DenseSource& src, int64_t batch_stride, const emr_q8* other, int64_t batch, int64_t rows,
-                       int64_t cols, const emr_q8* q, const emr_q8* qt, float* sums, cudaStream_t st) {
+template <int kMode, typename T, bool kVector>
+emr_status launch_tile(const Dense<T, kVector>& src, const emr_q8* other, int64_t batch, int64_t rows, int64_t cols,
+                       const emr_q8* q, const emr_q8* qt, float* sums, cudaStream_t st) {
   const int64_t tiles = batch * q8_blocks(rows) * q8_blocks(cols);
   if (tiles > kMaxGrid) return EMR_ERR_RANGE;
-  const int smem = qt || sums ? kTileBytes : 0;
-  if (smem && cudaFuncSetAttribute(q8_tile_kernel<kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+  if (cudaFuncSetAttribute(q8_tile_kernel<kMode, T, kVector>, cudaFuncAttributeMaxDynamicSharedMemorySize, kTileBytes) != cudaSuccess)
     return EMR_ERR_CUDA;
   const emr_q8 none{};
-  q8_tile_kernel<kMode><<<unsigned(tiles), kThreads, smem, st>>>(src, batch_stride, other ? *other : none, rows, cols,
-                                                                 q ? *q : none, qt ? *qt : none, sums);
+  q8_tile_kernel<kMode, T, kVector><<<unsigned(tiles), kThreads, kTileBytes, st>>>(
+      src, other ? *other : none, rows, cols, q ? *q : none, qt ? *qt : none, sums);
   return cudaGetLastError() == cudaSuccess ? EMR_OK : EMR_ERR_CUDA;
+}
+
+template <typename T, bool kVector>
+emr_status launch_rows(const Dense<T, kVector>& src, int64_t batch, int64_t rows, int64_t cols, const emr_q8* q, cudaStream_t st) {
+  const int64_t units = batch * rows * q8_scale_chunks(cols), grid = (units + kWarps - 1) / kWarps;
+  if (grid > kMaxGrid) return EMR_ERR_RANGE;
+  q8_rows_kernel<T, kVector><<<unsigned(grid), kThreads, 0, st>>>(src, rows, cols, units, *q);
+  return cudaGetLastError() == cudaSuccess ? EMR_OK : EMR_ERR_CUDA;
+}
+
+struct DenseArgs {
+  const void* p;
+  int32_t dtype;
+  int64_t batch, rows, cols, batch_stride, row_stride, col_stride;
+};
+template <typename Fn, typename T>
+emr_status with_vector(const DenseArgs& a, Fn fn) {
+  const bool vector = a.col_stride == 1 && reinterpret_cast<uintptr_t>(a.p) % (4 * sizeof(T)) == 0 &&
+                      (a.rows == 1 || a.row_stride % 4 == 0) && (a.batch == 1 || a.batch_stride % 4 == 0);
+  const T* p = static_cast<const T*>(a.p);
+  return vector ? fn(Dense<T, true>{p, a.batch_stride, a.row_stride, a.col_stride})
+                : fn(Dense<T, false>{p, a.batch_stride, a.row_stride, a.col_stride});
+}
+// fn with the source in its type, and as vectors where its layout allows.
+template <typename Fn>
+emr_status with_dense(const DenseArgs& a, Fn fn) {
+  if (a.dtype == EMR_F32) return with_vector<Fn, float>(a, fn);
+  if (a.dtype == EMR_BF16) return with_vector<Fn, __nv_bfloat16>(a, fn);
+  return with_vector<Fn, __half>(a, fn);
 }
 
 bool same_shape(const emr_q8* q, int64_t batch, int64_t rows, int64_t cols) {
@@ -213,21 +265,16 @@ extern "C" emr_status emr_q8_quantize(const void* src, int32_t dtype, int32_t ba
     const emr_q8* t = q;
     q = qt, qt = t;
   }
-  const int size = dtype_bytes(dtype);
-  DenseSource d{src, dtype, row_stride, col_stride, false};
-  d.vector = col_stride == 1 && reinterpret_cast<uintptr_t>(src) % (4 * size) == 0 && (rows == 1 || row_stride % 4 == 0) &&
-             (batch == 1 || batch_stride % 4 == 0);
+  const DenseArgs args{src, dtype, batch, rows, cols, batch_stride, row_stride, col_stride};
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (qt) return launch_tile<0>(d, batch_stride, nullptr, batch, rows, cols, q, qt, nullptr, st);
-  const int64_t units = int64_t(batch) * rows * q8_scale_chunks(cols), grid = (units + kWarps - 1) / kWarps;
-  if (grid > kMaxGrid) return EMR_ERR_RANGE;
-  q8_rows_kernel<<<unsigned(grid), kThreads, 0, st>>>(d, batch_stride, rows, cols, units, *q);
-  return cudaGetLastError() == cudaSuccess ? EMR_OK : EMR_ERR_CUDA;
+  return with_dense(args, [&](auto d) {
+    return qt ? launch_tile<0>(d, nullptr, batch, rows, cols, q, qt, nullptr, st) : launch_rows(d, batch, rows, cols, q, st);
+  });
 }
 
 extern "C" emr_status emr_q8_transpose(const emr_q8* q, const emr_q8* qt, void* stream) {
   if (!q8_ok(q) || !same_shape(qt, q->batch, q->cols, q->rows)) return EMR_ERR_ARG;
-  return launch_tile<1>(DenseSource{}, 0, q, q->batch, q->rows, q->cols, nullptr, qt, nullptr,
+  return launch_tile<1>(Dense<float, true>{}, q, q->batch, q->rows, q->cols, nullptr, qt, nullptr,
                         static_cast<cudaStream_t>(stream));
 }
 
@@ -264,12 +311,13 @@ extern "C" emr_status emr_q8_slope(const void* dy, int32_t dtype, int32_t batch,
                                                         reinterpret_cast<uintptr_t>(ws) % 4)))
     return EMR_ERR_ARG;
   if (db && ws_bytes < need) return EMR_ERR_CAPACITY;
-  DenseSource src{dy, dtype, cols, 1, false};
-  src.vector = reinterpret_cast<uintptr_t>(dy) % (4 * size) == 0 && cols % 4 == 0;
+  const DenseArgs args{dy, dtype, batch, rows, cols, rows * cols, cols, 1};
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   float* sums = db ? static_cast<float*>(ws) : nullptr;
-  const emr_status e = d ? launch_tile<2>(src, rows * cols, d, batch, rows, cols, dz, dzt, sums, st)
-                         : launch_tile<0>(src, rows * cols, nullptr, batch, rows, cols, dz, dzt, sums, st);
+  const emr_status e = with_dense(args, [&](auto src) {
+    return d ? launch_tile<2>(src, d, batch, rows, cols, dz, dzt, sums, st)
+             : launch_tile<0>(src, nullptr, batch, rows, cols, dz, dzt, sums, st);
+  });
   if (e != EMR_OK || !db) return e;
   const int64_t total = int64_t(batch) * cols, grid = (total + kThreads - 1) / kThreads;
   if (grid > kMaxGrid) return EMR_ERR_RANGE;

@@ -48,14 +48,27 @@ __device__ __forceinline__ uint32_t q8_magnitude(float v) {
 __device__ __forceinline__ float q8_finite_or_nan(float v) {
   return (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u ? __uint_as_float(0x7fc00000u) : v;
 }
-// Four values times inv as e4m3 codes, rounded to nearest even; v0 is the low byte.
+// Four values times inv as e4m3 codes, rounded to nearest even; v0 is the low byte. NaN
+// gives the NaN code; an infinity would saturate (q8_finite_or_nan first).
 __device__ __forceinline__ uint32_t q8_pack4(float v0, float v1, float v2, float v3, float inv) {
   uint16_t lo, hi;
-  const float a = q8_finite_or_nan(v0) * inv, b = q8_finite_or_nan(v1) * inv;
-  const float c = q8_finite_or_nan(v2) * inv, d = q8_finite_or_nan(v3) * inv;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(v1 * inv), "f"(v0 * inv));
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(v3 * inv), "f"(v2 * inv));
   return uint32_t(lo) | (uint32_t(hi) << 16);
+}
+// Largest magnitude of four values; NaN only where all are.
+__device__ __forceinline__ float q8_top4(float4 v) {
+  return fmaxf(fmaxf(fabsf(v.x), fabsf(v.y)), fmaxf(fabsf(v.z), fabsf(v.w)));
+}
+// Scale byte of a block spread over a warp, four values a lane. Blocks with an infinity
+// or nothing but NaN in some lane take the second look; there infinities turn into NaN.
+__device__ __forceinline__ uint32_t q8_warp_scale(float4& v) {
+  uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(q8_top4(v)) & 0x7fffffffu);
+  if (top >= 0x7f800000u) {
+    top = __reduce_max_sync(0xffffffffu, max(max(q8_magnitude(v.x), q8_magnitude(v.y)), max(q8_magnitude(v.z), q8_magnitude(v.w))));
+    v = make_float4(q8_finite_or_nan(v.x), q8_finite_or_nan(v.y), q8_finite_or_nan(v.z), q8_finite_or_nan(v.w));
+  }
+  return q8_scale_byte(top);
 }
 // The values that four codes stand for, before the scale.
 __device__ __forceinline__ float4 q8_unpack4(uint32_t p) {
@@ -68,30 +81,29 @@ __device__ __forceinline__ float4 q8_unpack4(uint32_t p) {
 }
 
 // Element i of an array of the given emr_dtype.
-__device__ __forceinline__ float load_scalar(const void* p, int dtype, int64_t i) {
-  if (dtype == EMR_F32) return static_cast<const float*>(p)[i];
-  if (dtype == EMR_BF16) return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
-  return __half2float(static_cast<const __half*>(p)[i]);
-}
 __device__ __forceinline__ void store_scalar(void* p, int dtype, int64_t i, float v) {
   if (dtype == EMR_F32) static_cast<float*>(p)[i] = v;
   else if (dtype == EMR_BF16) static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
   else static_cast<__half*>(p)[i] = __float2half_rn(v);
 }
-// Elements i .. i + 3, aligned to their four-element size.
-__device__ __forceinline__ float4 load_four(const void* p, int dtype, int64_t i) {
-  if (dtype == EMR_F32) return *reinterpret_cast<const float4*>(static_cast<const float*>(p) + i);
-  const uint2 u = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + i);
-  float2 a, b;
-  if (dtype == EMR_BF16) {
-    a = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u.x));
-    b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u.y));
-  } else {
-    a = __half22float2(*reinterpret_cast<const __half2*>(&u.x));
-    b = __half22float2(*reinterpret_cast<const __half2*>(&u.y));
+// Four neighbouring elements as they lie in memory, and as floats.
+template <typename T>
+struct Four {
+  uint2 u;
+  __device__ __forceinline__ void load(const T* p) { u = *reinterpret_cast<const uint2*>(p); }
+  __device__ __forceinline__ void set(int j, T v) { reinterpret_cast<T*>(&u)[j] = v; }
+  __device__ __forceinline__ float4 floats() const {
+    const T* e = reinterpret_cast<const T*>(&u);
+    return make_float4(float(e[0]), float(e[1]), float(e[2]), float(e[3]));
   }
-  return make_float4(a.x, a.y, b.x, b.y);
-}
+};
+template <>
+struct Four<float> {
+  float4 u;
+  __device__ __forceinline__ void load(const float* p) { u = *reinterpret_cast<const float4*>(p); }
+  __device__ __forceinline__ void set(int j, float v) { reinterpret_cast<float*>(&u)[j] = v; }
+  __device__ __forceinline__ float4 floats() const { return u; }
+};
 __host__ __device__ inline int dtype_bytes(int dtype) { return dtype == EMR_F32 ? 4 : 2; }
 inline bool dtype_ok(int dtype) { return dtype == EMR_F32 || dtype == EMR_BF16 || dtype == EMR_F16; }
 

@@ -287,6 +287,7 @@ __device__ __forceinline__ void put_slope(const Params& p, const Tile& t, float 
 #pragma unroll
     for (int i = 0; i < 32; i++) {
       if (c * 32 + i >= left) d[c][i] = 0.f;
+      d[c][i] = q8_finite_or_nan(d[c][i]);
       top = max(top, q8_magnitude(d[c][i]));
     }
   const uint32_t byte = q8_scale_byte(top);
