@@ -3,10 +3,8 @@
 //
 // All of it is bound by memory. Every kernel reads its source once: a row block of
 // 128 columns is one warp's registers (four columns a lane), so its maximum is one
-// warp reduction and its codes one 128-byte store. The transposed copy goes through
-// a 64 KB tile in shared memory whose 16-byte columns are exchanged by (row / 4) % 8,
-// which makes both the row-wise stores and the column-wise loads (a lane takes four
-// rows x four columns) free of bank conflicts.
+// warp reduction and its codes one 128-byte store; the transposed copy is made from
+// the same registers through a 16 KB tile of codes.
 #include <cuda_runtime.h>
 
 #include "emr_q8.h"
@@ -17,6 +15,7 @@ using namespace emr;
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
+constexpr int kTileThreads = 512;
 
 // Dense source: four columns c .. c + 3 of a row, zero past the matrix. kVector: columns
 // are neighbours and every row is aligned to four elements.
@@ -43,125 +42,173 @@ __device__ __forceinline__ float4 q8_four(const uint8_t* values, const uint8_t* 
   return make_float4(v.x * s, v.y * s, v.z * s, v.w * s);
 }
 
-// Row blocks only: one warp takes four blocks of 128 columns of one row, whose four
-// scale bytes are one word.
+// Row blocks only: a warp has one row and takes 512 columns of it at a time (four
+// blocks, whose scale bytes are one word), blockIdx.y of gridDim.y such pieces apart.
+// The next piece is loaded before the present one is worked on.
 template <typename T, bool kVector>
-__global__ void __launch_bounds__(kThreads) q8_rows_kernel(Dense<T, kVector> src, int64_t rows, int64_t cols, int64_t units,
+__global__ void __launch_bounds__(kThreads) q8_rows_kernel(Dense<T, kVector> src, int64_t rows, int64_t cols, int64_t all_rows,
                                                            emr_q8 q) {
-  const int64_t chunks = q8_scale_chunks(cols), blocks = q8_blocks(cols), row_bytes = q8_row_bytes(cols);
-  const int64_t unit = int64_t(blockIdx.x) * kWarps + (threadIdx.x >> 5);
-  if (unit >= units) return;
+  const int64_t row = int64_t(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+  if (row >= all_rows) return;
   const int lane = threadIdx.x & 31;
-  // divisions in 32 bits where they suffice: they cost as much as a block's work otherwise
-  const bool small = units <= UINT32_MAX;
-  const int64_t row = small ? uint32_t(unit) / uint32_t(chunks) : unit / chunks, chunk = unit - row * chunks;
-  const int64_t b = small ? uint32_t(row) / uint32_t(rows) : row / rows, r = row - b * rows;
+  const int64_t b = all_rows <= UINT32_MAX ? uint32_t(row) / uint32_t(rows) : row / rows, r = row - b * rows;
+  const int chunks = int(q8_scale_chunks(cols)), blocks = int(q8_blocks(cols));
   const T* from = src.p + b * src.batch_stride + r * src.row_stride;
-  const int64_t c = chunk * 512 + lane * 4;
+  uint8_t* out = q.values + row * q8_row_bytes(cols) + lane * 4;
+  uint8_t* scales = q.scales + b * q8_scale_batch(rows, cols) + q8_scale_at(chunks, r, 0);
   Four<T> u[4];
 #pragma unroll
-  for (int j = 0; j < 4; j++) u[j] = src.four(from, c + j * 128, cols);
-  uint8_t* out = q.values + row * row_bytes + c;
-  uint32_t word = 0;
+  for (int j = 0; j < 4; j++) u[j] = src.four(from, int64_t(blockIdx.y) * 512 + j * 128 + lane * 4, cols);
+  for (int chunk = blockIdx.y; chunk < chunks; chunk += gridDim.y) {
+    Four<T> now[4];
 #pragma unroll
-  for (int j = 0; j < 4; j++) {
-    float4 v = u[j].floats();
-    const uint32_t byte = q8_warp_scale(v);
-    word |= byte << (8 * j);
-    if (chunk * 4 + j < blocks)
-      *reinterpret_cast<uint32_t*>(out + j * 128) = q8_pack4(v.x, v.y, v.z, v.w, q8_inverse(byte));
+    for (int j = 0; j < 4; j++) now[j] = u[j];
+    const int next = chunk + gridDim.y;
+    if (next < chunks) {
+#pragma unroll
+      for (int j = 0; j < 4; j++) u[j] = src.four(from, int64_t(next) * 512 + j * 128 + lane * 4, cols);
+    }
+    uint32_t word = 0;
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+      float4 v = now[j].floats();
+      const uint32_t byte = q8_warp_scale(v);
+      word |= byte << (8 * j);
+      if (chunk * 4 + j < blocks)
+        *reinterpret_cast<uint32_t*>(out + int64_t(chunk) * 512 + j * 128) = q8_pack4(v.x, v.y, v.z, v.w, q8_inverse(byte));
+    }
+    if (lane == 0) *reinterpret_cast<uint32_t*>(scales + int64_t(chunk) * 512) = word;
   }
-  if (lane == 0)
-    *reinterpret_cast<uint32_t*>(q.scales + b * q8_scale_batch(rows, cols) + q8_scale_at(chunks, r, chunk * 4)) = word;
 }
 
 // One 128 x 128 tile: row blocks to q, column blocks (the transpose) to qt, column
 // sums to sums[b][row tile][cols]. Mode 0: a dense source; 1: the values of an 8-bit
-// matrix; 2: the product of a dense matrix and an 8-bit one. A warp has the rows
-// 16 warp .. 16 warp + 15 and loads eight of them before it uses the first.
+// matrix; 2: the product of a dense matrix and an 8-bit one. A warp holds the rows
+// 8 warp .. 8 warp + 7 in registers, a lane four columns of each. Column maxima and
+// sums meet in shared memory over the 16 warps (the sums in their order); codes of four rows are one word of the
+// transposed byte tile, at (row / 4) ^ (column / 4 % 32) of its column, so that neither
+// the stores (lanes: columns 4 apart) nor the loads (lanes: one column) have conflicts.
 template <int kMode, typename T, bool kVector>
-__global__ void __launch_bounds__(kThreads, 3) q8_tile_kernel(Dense<T, kVector> src, emr_q8 other, int64_t rows, int64_t cols,
-                                                              emr_q8 q, emr_q8 qt, float* sums) {
-  extern __shared__ float4 tile[];  // [128][32]
-  __shared__ uint8_t row_scales[128], col_scales[128];
-  const int64_t row_tiles = q8_blocks(rows), col_tiles = q8_blocks(cols);
-  const int64_t ct = blockIdx.x % col_tiles, rest = blockIdx.x / col_tiles, rt = rest % row_tiles, b = rest / row_tiles;
+__global__ void __launch_bounds__(kTileThreads, 2) q8_tile_kernel(Dense<T, kVector> src, emr_q8 other, int64_t rows, int64_t cols,
+                                                                  emr_q8 q, emr_q8 qt, float* sums) {
+  __shared__ float4 part[16][32];
+  __shared__ uint32_t bytes[128 * 32];
+  __shared__ uint32_t tops[4][32];  // [j][lane]: largest magnitude of column 4 lane + j
+  const uint32_t row_tiles = uint32_t(q8_blocks(rows)), col_tiles = uint32_t(q8_blocks(cols));
+  const uint32_t rest = blockIdx.x / col_tiles;
+  const int64_t ct = blockIdx.x - rest * col_tiles, b = rest / row_tiles, rt = rest - uint32_t(b) * row_tiles;
+  if (threadIdx.x < 128) tops[0][threadIdx.x] = 0;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t chunks = q8_scale_chunks(cols), row_bytes = q8_row_bytes(cols), scale_batch = q8_scale_batch(rows, cols);
   const int64_t c = ct * 128 + lane * 4;
   const int64_t left = rows - rt * 128;
-  const int have = int(left < 128 ? left : 128);  // rows of the tile
   const int wide = int(cols - ct * 128 < 128 ? cols - ct * 128 : 128);
-  const int first = warp * 16;
+  const int first = warp * 8;
+  const int have = int(left < 128 ? left : 128) - first;  // rows of this warp, may be below 1
   const T* from = kMode != 1 ? src.p + b * src.batch_stride + (rt * 128 + first) * src.row_stride : nullptr;
   const int64_t at = (b * rows + rt * 128 + first) * row_bytes + c;  // of the warp's first row in 8-bit matrices of this shape
-  const uint8_t* codes = kMode != 0 ? other.values + at : nullptr;
-  uint8_t* out = q.values ? q.values + at : nullptr;
-  uint32_t scale_bytes = 127;
-  if (kMode != 0 && lane < 16 && first + lane < have)
-    scale_bytes = other.scales[b * scale_batch + q8_scale_at(chunks, rt * 128 + first + lane, ct)];
-#pragma unroll
-  for (int i0 = 0; i0 < 16; i0 += 8) {
+  float4 v[8];
+  {
     Four<T> u[8];
     uint32_t code[8];
+    uint32_t scale_bytes = 127;
+    if (kMode != 0 && lane < 8 && lane < have)
+      scale_bytes = other.scales[b * scale_batch + q8_scale_at(chunks, rt * 128 + first + lane, ct)];
 #pragma unroll
     for (int i = 0; i < 8; i++)
-      if (first + i0 + i < have) {
-        if (kMode != 1) u[i] = src.four(from + (i0 + i) * src.row_stride, c, cols);
-        if (kMode != 0) code[i] = *reinterpret_cast<const uint32_t*>(codes + (i0 + i) * row_bytes);
+      if (i < have) {
+        if (kMode != 1) u[i] = src.four(from + i * src.row_stride, c, cols);
+        if (kMode != 0) code[i] = *reinterpret_cast<const uint32_t*>(other.values + at + i * row_bytes);
       }
 #pragma unroll
     for (int i = 0; i < 8; i++) {
-      const int r = first + i0 + i;
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (r < have) {
-        if (kMode != 1) v = u[i].floats();
+      v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (i < have) {
+        if (kMode != 1) v[i] = u[i].floats();
         if (kMode != 0) {
-          const float s = q8_scale(__shfl_sync(0xffffffffu, scale_bytes, i0 + i));
+          const float s = q8_scale(__shfl_sync(0xffffffffu, scale_bytes, i));
           float4 d = q8_unpack4(code[i]);
           d = make_float4(d.x * s, d.y * s, d.z * s, d.w * s);
           // one rounding each, so that the values are those of the plain product
-          v = kMode == 1 ? d : make_float4(__fmul_rn(v.x, d.x), __fmul_rn(v.y, d.y), __fmul_rn(v.z, d.z), __fmul_rn(v.w, d.w));
+          v[i] = kMode == 1 ? d : make_float4(__fmul_rn(v[i].x, d.x), __fmul_rn(v[i].y, d.y), __fmul_rn(v[i].z, d.z), __fmul_rn(v[i].w, d.w));
         }
       }
-      tile[r * 32 + (lane ^ ((r >> 2) & 7))] = v;
-      if (out && r < have) {
-        const uint32_t byte = q8_warp_scale(v);
-        *reinterpret_cast<uint32_t*>(out + (i0 + i) * row_bytes) = q8_pack4(v.x, v.y, v.z, v.w, q8_inverse(byte));
-        if (lane == 0) row_scales[r] = uint8_t(byte);
-      }
     }
   }
+  if (sums) {
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < 8; i++) s.x += v[i].x, s.y += v[i].y, s.z += v[i].z, s.w += v[i].w;
+    part[warp][lane] = s;
+    __syncthreads();
+    if (threadIdx.x < wide) {
+      float t = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; i++) t += reinterpret_cast<const float*>(part[i])[threadIdx.x];
+      sums[(b * row_tiles + rt) * cols + ct * 128 + threadIdx.x] = t;
+    }
+    __syncthreads();
+  }
+  if (q.values) {
+    uint8_t* out = q.values + at;
+    uint32_t mine = 0;
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+      if (i < have) {
+        const uint32_t byte = q8_warp_scale(v[i]);
+        *reinterpret_cast<uint32_t*>(out + i * row_bytes) = q8_pack4(v[i].x, v[i].y, v[i].z, v[i].w, q8_inverse(byte));
+        if (lane == i) mine = byte;
+      }
+    if (lane < 8 && lane < have) q.scales[b * scale_batch + q8_scale_at(chunks, rt * 128 + first + lane, ct)] = uint8_t(mine);
+  }
+  if (!qt.values) return;
+  if (!sums) __syncthreads();  // tops are cleared
+  float4 top = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int i = 0; i < 8; i++)
+    top = make_float4(fmaxf(top.x, fabsf(v[i].x)), fmaxf(top.y, fabsf(v[i].y)), fmaxf(top.z, fabsf(v[i].z)), fmaxf(top.w, fabsf(v[i].w)));
+  // NaN is passed over by the maxima; where an infinity is, the finite magnitudes are taken again
+  const float most = q8_top4(top);
+  if (most == INFINITY) {
+    uint32_t m[4] = {};
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      m[0] = max(m[0], q8_magnitude(v[i].x)), m[1] = max(m[1], q8_magnitude(v[i].y));
+      m[2] = max(m[2], q8_magnitude(v[i].z)), m[3] = max(m[3], q8_magnitude(v[i].w));
+      v[i] = make_float4(q8_finite_or_nan(v[i].x), q8_finite_or_nan(v[i].y), q8_finite_or_nan(v[i].z), q8_finite_or_nan(v[i].w));
+    }
+    top = make_float4(__uint_as_float(m[0]), __uint_as_float(m[1]), __uint_as_float(m[2]), __uint_as_float(m[3]));
+  }
+  atomicMax(&tops[0][lane], __float_as_uint(top.x));
+  atomicMax(&tops[1][lane], __float_as_uint(top.y));
+  atomicMax(&tops[2][lane], __float_as_uint(top.z));
+  atomicMax(&tops[3][lane], __float_as_uint(top.w));
   __syncthreads();
+  const uint32_t scale[4] = {q8_scale_byte(tops[0][lane]), q8_scale_byte(tops[1][lane]), q8_scale_byte(tops[2][lane]),
+                             q8_scale_byte(tops[3][lane])};
+  const float inv[4] = {q8_inverse(scale[0]), q8_inverse(scale[1]), q8_inverse(scale[2]), q8_inverse(scale[3])};
   const int64_t t_row_bytes = q8_row_bytes(rows);
-  uint8_t* tout = qt.values ? qt.values + (b * cols + ct * 128) * t_row_bytes + rt * 128 + lane * 4 : nullptr;
-  for (int i = warp; i < 32; i += kWarps) {  // columns 4 i .. 4 i + 3, rows 4 lane .. 4 lane + 3
-    float4 v[4];
+  if (warp == 0) {
+    uint8_t* ts = qt.scales + b * q8_scale_batch(cols, rows);
 #pragma unroll
-    for (int j = 0; j < 4; j++) v[j] = tile[(lane * 4 + j) * 32 + (i ^ (lane & 7))];
-    float4 col[4] = {make_float4(v[0].x, v[1].x, v[2].x, v[3].x), make_float4(v[0].y, v[1].y, v[2].y, v[3].y),
-                     make_float4(v[0].z, v[1].z, v[2].z, v[3].z), make_float4(v[0].w, v[1].w, v[2].w, v[3].w)};
+    for (int j = 0; j < 4; j++)
+      if (lane * 4 + j < wide) ts[q8_scale_at(q8_scale_chunks(rows), c + j, rt)] = uint8_t(scale[j]);
+  }
 #pragma unroll
-    for (int j = 0; j < 4; j++) {
-      const int n = i * 4 + j;
-      if (sums) {
-        float s = (col[j].x + col[j].y) + (col[j].z + col[j].w);
-#pragma unroll
-        for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-        if (lane == 0 && n < wide) sums[(b * row_tiles + rt) * cols + ct * 128 + n] = s;
-      }
-      if (tout && n < wide) {
-        const uint32_t byte = q8_warp_scale(col[j]);
-        *reinterpret_cast<uint32_t*>(tout + n * t_row_bytes) = q8_pack4(col[j].x, col[j].y, col[j].z, col[j].w, q8_inverse(byte));
-        if (lane == 0) col_scales[n] = uint8_t(byte);
-      }
-    }
+  for (int h = 0; h < 2; h++) {
+    const int w = (warp * 2 + h) ^ lane;  // word of rows first + 4 h ..., columns 4 lane + j
+    bytes[(lane * 4 + 0) * 32 + w] = q8_pack4(v[4 * h].x, v[4 * h + 1].x, v[4 * h + 2].x, v[4 * h + 3].x, inv[0]);
+    bytes[(lane * 4 + 1) * 32 + w] = q8_pack4(v[4 * h].y, v[4 * h + 1].y, v[4 * h + 2].y, v[4 * h + 3].y, inv[1]);
+    bytes[(lane * 4 + 2) * 32 + w] = q8_pack4(v[4 * h].z, v[4 * h + 1].z, v[4 * h + 2].z, v[4 * h + 3].z, inv[2]);
+    bytes[(lane * 4 + 3) * 32 + w] = q8_pack4(v[4 * h].w, v[4 * h + 1].w, v[4 * h + 2].w, v[4 * h + 3].w, inv[3]);
   }
   __syncthreads();
-  const int i = threadIdx.x;
-  if (out && i < have) q.scales[b * scale_batch + q8_scale_at(chunks, rt * 128 + i, ct)] = row_scales[i];
-  if (tout && i >= 128 && i - 128 < wide)
-    qt.scales[b * q8_scale_batch(cols, rows) + q8_scale_at(q8_scale_chunks(rows), ct * 128 + i - 128, rt)] = col_scales[i - 128];
+  uint8_t* out = qt.values + (b * cols + ct * 128) * t_row_bytes + rt * 128 + lane * 4;
+#pragma unroll
+  for (int i = 0; i < 8; i++) {
+    const int n = first + i;
+    if (n < wide) *reinterpret_cast<uint32_t*>(out + n * t_row_bytes) = bytes[n * 32 + (lane ^ (n >> 2))];
+  }
 }
 
 // Sum of the row tiles' column sums, in the order of the tiles.
@@ -190,26 +237,27 @@ __global__ void __launch_bounds__(kThreads) q8_dequantize_kernel(emr_q8 q, int64
 }
 
 constexpr int64_t kMaxGrid = (int64_t(1) << 31) - 1;
-constexpr int kTileBytes = 128 * 128 * 4;
 
 template <int kMode, typename T, bool kVector>
 emr_status launch_tile(const Dense<T, kVector>& src, const emr_q8* other, int64_t batch, int64_t rows, int64_t cols,
                        const emr_q8* q, const emr_q8* qt, float* sums, cudaStream_t st) {
   const int64_t tiles = batch * q8_blocks(rows) * q8_blocks(cols);
   if (tiles > kMaxGrid) return EMR_ERR_RANGE;
-  if (cudaFuncSetAttribute(q8_tile_kernel<kMode, T, kVector>, cudaFuncAttributeMaxDynamicSharedMemorySize, kTileBytes) != cudaSuccess)
-    return EMR_ERR_CUDA;
   const emr_q8 none{};
-  q8_tile_kernel<kMode, T, kVector><<<unsigned(tiles), kThreads, kTileBytes, st>>>(
+  q8_tile_kernel<kMode, T, kVector><<<unsigned(tiles), kTileThreads, 0, st>>>(
       src, other ? *other : none, rows, cols, q ? *q : none, qt ? *qt : none, sums);
   return cudaGetLastError() == cudaSuccess ? EMR_OK : EMR_ERR_CUDA;
 }
 
 template <typename T, bool kVector>
 emr_status launch_rows(const Dense<T, kVector>& src, int64_t batch, int64_t rows, int64_t cols, const emr_q8* q, cudaStream_t st) {
-  const int64_t units = batch * rows * q8_scale_chunks(cols), grid = (units + kWarps - 1) / kWarps;
+  const int64_t all = batch * rows, grid = (all + kWarps - 1) / kWarps, chunks = q8_scale_chunks(cols);
   if (grid > kMaxGrid) return EMR_ERR_RANGE;
-  q8_rows_kernel<T, kVector><<<unsigned(grid), kThreads, 0, st>>>(src, rows, cols, units, *q);
+  // a warp takes whole rows where they are many, else a row is shared out: about 16 blocks for each of 152 SMs
+  int64_t pieces = (16 * 152 + grid - 1) / grid;
+  if (pieces > chunks) pieces = chunks;
+  if (pieces > 65535) pieces = 65535;
+  q8_rows_kernel<T, kVector><<<dim3(unsigned(grid), unsigned(pieces)), kThreads, 0, st>>>(src, rows, cols, all, *q);
   return cudaGetLastError() == cudaSuccess ? EMR_OK : EMR_ERR_CUDA;
 }
 

@@ -32,9 +32,8 @@ __host__ __device__ inline int64_t q8_scale_at(int64_t chunks, int64_t r, int64_
 // for the least e with top <= 448 * 2^e (448 = 1.75 * 2^8 is e4m3's largest value);
 // e is at least -126, and 0 for a block of zeros.
 __device__ __forceinline__ uint32_t q8_scale_byte(uint32_t top) {
-  if (top == 0) return 127u;
-  const int b = int(top >> 23) - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
-  return uint32_t(b < 1 ? 1 : b);
+  const int b = int((top + 0x1fffffu) >> 23) - 8;  // a fraction above 0x600000 carries into the exponent
+  return top == 0 ? 127u : uint32_t(max(b, 1));
 }
 __device__ __forceinline__ float q8_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
 __device__ __forceinline__ float q8_inverse(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
@@ -63,7 +62,7 @@ __device__ __forceinline__ float q8_top4(float4 v) {
 // Scale byte of a block spread over a warp, four values a lane. Blocks with an infinity
 // or nothing but NaN in some lane take the second look; there infinities turn into NaN.
 __device__ __forceinline__ uint32_t q8_warp_scale(float4& v) {
-  uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(q8_top4(v)) & 0x7fffffffu);
+  uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(q8_top4(v)));
   if (top >= 0x7f800000u) {
     top = __reduce_max_sync(0xffffffffu, max(max(q8_magnitude(v.x), q8_magnitude(v.y)), max(q8_magnitude(v.z), q8_magnitude(v.w))));
     v = make_float4(q8_finite_or_nan(v.x), q8_finite_or_nan(v.y), q8_finite_or_nan(v.z), q8_finite_or_nan(v.w));

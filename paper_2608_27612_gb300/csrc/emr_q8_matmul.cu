@@ -62,6 +62,18 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
   }
   return true;
 }
+// The same by a whole warp, with one answer for it.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* gave_up, int code) {
+  return __all_sync(0xffffffffu, bar_wait(bar, parity, gave_up, code));
+}
+// One lane of a converged warp. The copy and matrix loops run in whole warps, whose addresses and
+// descriptors then are uniform values, and only the instructions themselves belong to one lane:
+// with the loops inside a branch of one lane each step took 690 clocks whatever it did.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p != 0;
+}
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
   asm volatile(
       "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
@@ -116,10 +128,32 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
   for (int i = 0; i < 32; i++) v[i] = __uint_as_float(r[i]);
 }
 
+// After a wait gave up: longer than any copy or matrix instruction in flight takes.
+__device__ __forceinline__ void settle() {
+  const long long t0 = clock64();
+  while (clock64() - t0 < 4000000) {
+  }
+}
+
 // ---- activations and their slopes ----------------------------------------------------
 // sigmoid and tanh are taken from t = e^-|z| or e^-2|z| and r = 1 / (1 + t): every
 // form below is a product of positive terms, so the slopes keep their relative
 // precision where the functions saturate (1 - y^2 would lose it).
+
+// Element i of sin and cos where the argument is large; i is not known at compile time, so the
+// element is picked by comparison instead of by an address.
+template <bool kSlope>
+__device__ __forceinline__ void sin_far(float (&z)[32], float (&d)[32], int i) {
+  float v = 0.f, c;
+#pragma unroll
+  for (int j = 0; j < 32; j++) v = j == i ? z[j] : v;
+  sincosf(v, &v, &c);
+#pragma unroll
+  for (int j = 0; j < 32; j++) {
+    z[j] = j == i ? v : z[j];
+    if (kSlope) d[j] = j == i ? c : d[j];
+  }
+}
 
 template <bool kSlope>
 __device__ __forceinline__ void activate(int act, float (&z)[32], float (&d)[32]) {
@@ -151,15 +185,26 @@ __device__ __forceinline__ void activate(int act, float (&z)[32], float (&d)[32]
         z[i] = y;
       }
       break;
-    case EMR_ACT_SIN:
+    case EMR_ACT_SIN: {
+      // reduced by 2 pi in two parts (fp32 value and remainder) and taken by the special
+      // function unit, good to 1e-6 up to 8192; beyond that, and for NaN, by sincosf
+      float most = 0.f;
 #pragma unroll
-      for (int i = 0; i < 32; i++) {
-        float s, c;
-        sincosf(z[i], &s, &c);
-        if (kSlope) d[i] = c;
-        z[i] = s;
+      for (int i = 0; i < 32; i++) most = fabsf(z[i]) <= most ? most : fabsf(z[i]);
+      if (most < 8192.f) {
+#pragma unroll
+        for (int i = 0; i < 32; i++) {
+          const float k = rintf(z[i] * 0x1.45f306p-3f);
+          const float r = fmaf(-k, -0x1.777a5cp-23f, fmaf(-k, 0x1.921fb6p+2f, z[i]));
+          if (kSlope) d[i] = __cosf(r);
+          z[i] = __sinf(r);
+        }
+      } else {
+#pragma unroll 1
+        for (int i = 0; i < 32; i++) sin_far<kSlope>(z, d, i);
       }
       break;
+    }
     case EMR_ACT_ABS:
 #pragma unroll
       for (int i = 0; i < 32; i++) {
@@ -215,6 +260,17 @@ __device__ __forceinline__ Tile tile_at(const Params& p, int64_t t) {
   return {b, first + t % rows, t / rows};
 }
 
+// Place in the ring of stages: counted up, not divided, since the copy and matrix loops are
+// one thread each and a block of 128 columns gives them 256 clocks.
+template <int kCount>
+struct Ring {
+  int stage = 0;
+  uint32_t round = 0;  // parity of the rounds made
+  __device__ __forceinline__ void next() {
+    if (++stage == kCount) stage = 0, round ^= 1;
+  }
+};
+
 // A warp's 32 staged rows of 128 bytes to global rows, `width` bytes a lane, neighbouring
 // lanes neighbouring addresses. `bytes` are valid in each row, `rows` rows.
 template <typename T>
@@ -249,7 +305,7 @@ __device__ __forceinline__ uint32_t pack_half(int dtype, float a, float b) {
 }
 
 // One row of 32 finished values, columns 32 c .. 32 c + 31 of the tile, to the staging rows
-// and, when 128 bytes of a row are there, to out.
+// and, when 128 bytes of a row are there, to out. c falls from 3 to 0.
 __device__ __forceinline__ void put_out(const Params& p, const Tile& t, int c, const float (&y)[32], uint8_t* staged,
                                         int64_t row0, int lane) {
   const int rows = int(p.M - row0 < 32 ? p.M - row0 : 32);  // may be below 1: nothing is stored
@@ -269,8 +325,8 @@ __device__ __forceinline__ void put_out(const Params& p, const Tile& t, int c, c
     stage16(staged, lane, (c & 1) * 4 + i,
             make_uint4(pack_half(p.out_dtype, y[8 * i], y[8 * i + 1]), pack_half(p.out_dtype, y[8 * i + 2], y[8 * i + 3]),
                        pack_half(p.out_dtype, y[8 * i + 4], y[8 * i + 5]), pack_half(p.out_dtype, y[8 * i + 6], y[8 * i + 7])));
-  if (c & 1) {
-    const int64_t first = n0 + (c - 1) * 32, left = (p.N - first) * 2;
+  if (!(c & 1)) {
+    const int64_t first = n0 + c * 32, left = (p.N - first) * 2;
     store_staged(staged, static_cast<uint8_t*>(p.out) + ((t.b * p.M + row0) * p.N + first) * 2, p.N * 2, rows,
                  int(left < 128 ? left : 128), p.store_bytes, lane);
   }
@@ -307,6 +363,32 @@ __device__ __forceinline__ void put_slope(const Params& p, const Tile& t, float 
   store_staged(staged, p.slope + (t.b * p.M + row0) * row_bytes + n0, row_bytes, rows, 128, 16, lane);
   if (lane < rows)
     p.slope_scales[t.b * q8_scale_batch(p.M, p.N) + q8_scale_at(q8_scale_chunks(p.N), row0 + lane, t.n)] = uint8_t(byte);
+}
+
+// A warp's 32 rows of one 128-column accumulator block at tensor memory address addr: bias,
+// activation, output and, with kSlope, slope. read(c) is called when columns 32 c ..
+// 32 c + 31 have been read.
+template <bool kSlope, typename Read>
+__device__ __forceinline__ void finish_block(const Params& p, const Tile& t, uint32_t addr, uint8_t* staged, int64_t row0, int lane,
+                                             Read read) {
+  const int64_t n0 = t.n * kTileN;
+  const float* bias = p.bias ? p.bias + t.b * p.N + n0 : nullptr;
+  float d[kSlope ? 4 : 1][32];
+#pragma unroll(kSlope ? 4 : 1)
+  for (int c = 3; c >= 0; c--) {
+    float z[32];
+    tmem_load32(addr + c * 32, z);
+    fence_before();
+    read(c);
+    if (bias) {
+      const float own = n0 + c * 32 + lane < p.N ? __ldg(bias + c * 32 + lane) : 0.f;
+#pragma unroll
+      for (int i = 0; i < 32; i++) z[i] += __shfl_sync(0xffffffffu, own, i);
+    }
+    activate<kSlope>(p.act, z, d[kSlope ? c : 0]);
+    put_out(p, t, c, z, staged, row0, lane);
+  }
+  if constexpr (kSlope) put_slope(p, t, d, staged, row0, lane);
 }
 
 // Persistent: a block takes tiles blockIdx.x, + gridDim.x, ... Warp 0 copies operand and
@@ -346,63 +428,74 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
   const uint32_t tmem = tmem_base;
   const int steps = p.sum * p.k_blocks;
 
-  if (warp == 0 && lane == 0) {
-    int64_t it = 0;
+  if (warp == 0) {
+    Ring<kStages> ring;
     for (int64_t t = blockIdx.x; t < p.tiles && !*stop; t += gridDim.x) {
       const Tile tile = tile_at(p, t);
-      for (int k = 0; k < steps; k++, it++) {
-        const int s = int(it % kStages);
-        if (it >= kStages && !bar_wait(empty + 8 * s, uint32_t(it / kStages - 1) & 1, stop, 1)) break;
-        const int sb = k / p.k_blocks, kb = k - sb * p.k_blocks;
-        const int64_t b = tile.b + sb, ab = p.a_one ? 0 : b, wb = p.w_one ? 0 : b;
-        const uint32_t bar = full + 8 * s, dst = smem_at(sm) + s * kStageBytes;
-        const bool scales = (kb & 3) == 0;
-        bar_expect(bar, kStageBytes + (scales ? kScaleBytes : 0));
-        tma_load(dst, &a_map, kb * kTileK, int(tile.m * kTileM), int(ab), bar);
-        tma_load(dst + kOperandBytes, &w_map, kb * kTileK, int(tile.n * kTileN), int(wb), bar);
-        if (scales) {
-          const uint32_t at = smem_at(scales_sm) + s * kScaleBytes;
-          bulk_load(at, p.a_scales + ((ab * p.m_tiles + tile.m) * p.k_chunks + (kb >> 2)) * 512, 512, bar);
-          bulk_load(at + 512, p.w_scales + ((wb * p.n_tiles + tile.n) * p.k_chunks + (kb >> 2)) * 512, 512, bar);
+      const int m = int(tile.m * kTileM), n = int(tile.n * kTileN);
+      bool ok = true;
+      for (int sb = 0; sb < p.sum && ok; sb++) {
+        const int64_t b = tile.b + sb;
+        const int ab = p.a_one ? 0 : int(b), wb = p.w_one ? 0 : int(b);
+        const uint8_t* a_scales = p.a_scales + (ab * p.m_tiles + tile.m) * p.k_chunks * 512;
+        const uint8_t* w_scales = p.w_scales + (wb * p.n_tiles + tile.n) * p.k_chunks * 512;
+        for (int kb = 0; kb < p.k_blocks; kb++, ring.next()) {
+          // a new ring is empty: the wait for the round before the first returns at once
+          if (!(ok = warp_wait(empty + 8 * ring.stage, ring.round ^ 1, stop, 1))) break;
+          const uint32_t bar = full + 8 * ring.stage, dst = smem_at(sm) + ring.stage * kStageBytes;
+          const bool scales = (kb & 3) == 0;
+          if (elect_one()) {
+            bar_expect(bar, kStageBytes + (scales ? kScaleBytes : 0));
+            tma_load(dst, &a_map, kb * kTileK, m, ab, bar);
+            tma_load(dst + kOperandBytes, &w_map, kb * kTileK, n, wb, bar);
+            if (scales) {
+              const uint32_t at = smem_at(scales_sm) + ring.stage * kScaleBytes;
+              bulk_load(at, a_scales, 512, bar);
+              bulk_load(at + 512, w_scales, 512, bar);
+            }
+          }
+          __syncwarp();
+          if (scales) a_scales += 512, w_scales += 512;
         }
       }
     }
-    if (*stop) {  // copies in flight end before the block does
-      const int64_t from = it > kStages ? it - kStages : 0;
-      for (int64_t i = from; i < it; i++) {
-        const long long t0 = clock64();
-        while (!bar_try(full + 8 * int(i % kStages), uint32_t(i / kStages) & 1) && clock64() - t0 < kWaitClocks) {
-        }
-      }
-    }
-  } else if (warp == 1 && lane == 0) {
+    if (*stop) settle();
+  } else if (warp == 1) {
     const uint32_t idesc = (1u << 23) | (uint32_t(kTileN >> 3) << 17) | (uint32_t(kTileM >> 4) << 24);
-    int64_t it = 0;
+    Ring<kStages> ring;
     uint32_t n_tile = 0, chunk = 0;
     for (int64_t t = blockIdx.x; t < p.tiles && !*stop; t += gridDim.x, n_tile++) {
       const uint32_t acc = n_tile & 1;
-      if (n_tile >= 2 && !bar_wait(acc_empty + 8 * acc, ((n_tile >> 1) - 1) & 1, stop, 2)) break;
+      if (n_tile >= 2 && !warp_wait(acc_empty + 8 * acc, ((n_tile >> 1) - 1) & 1, stop, 2)) break;
       fence_after();
       uint32_t sf = 0;
-      for (int k = 0; k < steps; k++, it++) {
-        const int s = int(it % kStages), kb = k % p.k_blocks;
-        if (!bar_wait(full + 8 * s, uint32_t(it / kStages) & 1, stop, 3)) break;
+      for (int k = 0, kb = 0; k < steps; k++, ring.next()) {
+        const int s = ring.stage;
+        if (!warp_wait(full + 8 * s, ring.round, stop, 3)) break;
         fence_after();
         if ((kb & 3) == 0) {
           sf = tmem + kTmemScales + 8 * (chunk++ & 1);
           const uint32_t at = smem_at(scales_sm) + s * kScaleBytes;
-          copy_scales(sf, scale_desc(at));
-          copy_scales(sf + 4, scale_desc(at + 512));
+          if (elect_one()) {
+            copy_scales(sf, scale_desc(at));
+            copy_scales(sf + 4, scale_desc(at + 512));
+          }
+          __syncwarp();
         }
         const uint32_t at = smem_at(sm) + s * kStageBytes;
         const uint64_t a = operand_desc(at), w = operand_desc(at + kOperandBytes);
         const uint32_t id = idesc | (uint32_t(kb & 3) << 4) | (uint32_t(kb & 3) << 29);
+        if (elect_one()) {
 #pragma unroll
-        for (int j = 0; j < 4; j++)  // 32 columns each: 32 bytes further in the tile
-          mma_scaled(tmem + acc * kTileN, a + 2 * j, w + 2 * j, id, sf, sf + 4, k > 0 || j > 0);
-        mma_commit(empty + 8 * s);
+          for (int j = 0; j < 4; j++)  // 32 columns each: 32 bytes further in the tile
+            mma_scaled(tmem + acc * kTileN, a + 2 * j, w + 2 * j, id, sf, sf + 4, k > 0 || j > 0);
+          mma_commit(empty + 8 * s);
+        }
+        __syncwarp();
+        if (++kb == p.k_blocks) kb = 0;
       }
-      mma_commit(acc_full + 8 * acc);
+      if (elect_one()) mma_commit(acc_full + 8 * acc);
+      __syncwarp();
     }
   } else if (warp >= 2) {
     const int quadrant = warp & 3;  // tensor memory lanes that this warp may read
@@ -410,31 +503,15 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
     uint32_t n_tile = 0;
     for (int64_t t = blockIdx.x; t < p.tiles; t += gridDim.x, n_tile++) {
       const uint32_t acc = n_tile & 1;
-      const bool ok = __all_sync(0xffffffffu, bar_wait(acc_full + 8 * acc, (n_tile >> 1) & 1, stop, 4));
+      const bool ok = warp_wait(acc_full + 8 * acc, (n_tile >> 1) & 1, stop, 4);
       if (!ok) break;
       fence_after();
       const Tile tile = tile_at(p, t);
-      const int64_t row0 = tile.m * kTileM + quadrant * 32, n0 = tile.n * kTileN;
-      const float* bias = p.bias ? p.bias + tile.b * p.N + n0 : nullptr;
+      const int64_t row0 = tile.m * kTileM + quadrant * 32;
       const uint32_t addr = tmem + acc * kTileN + (uint32_t(quadrant * 32) << 16);
-      float d[kSlope ? 4 : 1][32];
-#pragma unroll(kSlope ? 4 : 1)
-      for (int c = 0; c < 4; c++) {
-        float z[32];
-        tmem_load32(addr + c * 32, z);
-        if (c == 3) {
-          fence_before();
-          if (lane == 0) bar_arrive(acc_empty + 8 * acc);
-        }
-        if (bias) {
-          const float own = n0 + c * 32 + lane < p.N ? __ldg(bias + c * 32 + lane) : 0.f;
-#pragma unroll
-          for (int i = 0; i < 32; i++) z[i] += __shfl_sync(0xffffffffu, own, i);
-        }
-        activate<kSlope>(p.act, z, d[kSlope ? c : 0]);
-        put_out(p, tile, c, z, staged, row0, lane);
-      }
-      if constexpr (kSlope) put_slope(p, tile, d, staged, row0, lane);
+      finish_block<kSlope>(p, tile, addr, staged, row0, lane, [&](int c) {
+        if (c == 0 && lane == 0) bar_arrive(acc_empty + 8 * acc);
+      });
     }
   }
   __syncwarp();
@@ -443,6 +520,229 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
   if (warp == 1) {
     fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(kTmemColumns) : "memory");
+  }
+}
+
+// ---- pairs of SMs --------------------------------------------------------------------
+// For large products the 128 x 128 tile is bound by what L2 delivers: 32 KB an SM for each
+// 256 clocks of matrix work. Two SMs of a cluster on one 256 x 256 tile take 32 KB each for
+// 512 clocks: either block stages 128 rows of each operand, and the matrix instructions,
+// issued by the first block, read both blocks' shared memory and write 128 x 256
+// accumulators in each. Two such accumulators fill tensor memory, so the scales of one tile
+// live in the last 24 columns of the other tile's accumulators, which the epilogue reads
+// first.
+
+constexpr int kPairStages = 5;
+constexpr int kPairScaleBytes = 1536;  // 512 of a, 1024 of w
+constexpr int kPairThreads = 384;      // copy warp, matrix warp, two that only wait, eight epilogue warps
+constexpr int kPairSmemBytes = 1024 + kPairStages * (kStageBytes + kPairScaleBytes) + 8 * 32 * 128;
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// The address, in the cluster's window, of the first block's copy of a shared address.
+__device__ __forceinline__ uint32_t at_first(uint32_t addr) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
+  return r;
+}
+__device__ __forceinline__ void bar_arrive_cluster(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void pair_load(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void pair_load_scales(uint32_t dst, const CUtensorMap* map, int tile, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+      "l"(map), "r"(0), "r"(tile), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void pair_copy_scales(uint32_t tmem, uint64_t desc) {
+  asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+__device__ __forceinline__ void pair_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, bool accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(uint32_t(accumulate))
+      : "memory");
+}
+// Arrives at the barrier's address in both blocks when the work issued so far is done.
+__device__ __forceinline__ void pair_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+               "h"(uint16_t(3))
+               : "memory");
+}
+
+// Tile t of the pairs' raster: b, and row and column of 256 (groups of 8 row tiles).
+__device__ __forceinline__ Tile pair_tile_at(const Params& p, int64_t t) {
+  const int64_t mp = (p.m_tiles + 1) / 2, np = (p.n_tiles + 1) / 2, per = mp * np, b = t / per;
+  t -= b * per;
+  const int64_t group = t / (8 * np), first = group * 8, rows = mp - first < 8 ? mp - first : 8;
+  t -= first * np;
+  return {b, first + t % rows, t / rows};
+}
+
+template <bool kSlope>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
+    q8_pair_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap w_map,
+                   const __grid_constant__ CUtensorMap a_scale_map, const __grid_constant__ CUtensorMap w_scale_map,
+                   const __grid_constant__ Params p) {
+  extern __shared__ uint8_t raw[];
+  __shared__ uint64_t bars[2 * kPairStages + 6];
+  __shared__ uint32_t tmem_base;
+  __shared__ int gave_up;
+  // the dynamic part starts at the same address in both blocks
+  uint8_t* const sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* const scales_sm = sm + kPairStages * kStageBytes;
+  uint8_t* const staging = scales_sm + kPairStages * kPairScaleBytes;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_rank();
+  const uint32_t full = smem_at(bars), empty = full + 8 * kPairStages, acc_full = empty + 8 * kPairStages,
+                 acc_empty = acc_full + 16, tail = acc_empty + 16;
+  volatile int* const stop = &gave_up;
+
+  if (threadIdx.x == 0) {
+    gave_up = 0;
+    for (int i = 0; i < kPairStages; i++) bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, 1);
+    for (int i = 0; i < 2; i++) bar_init(acc_full + 8 * i, 1), bar_init(acc_empty + 8 * i, 16), bar_init(tail + 8 * i, 8);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&a_map) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&w_map) : "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&tmem_base)), "n"(kTmemColumns)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    fence_before();
+  }
+  __syncthreads();
+  cluster_sync();
+  fence_after();
+  const uint32_t tmem = tmem_base;
+  const int steps = p.sum * p.k_blocks;
+  const int64_t stride = gridDim.x / 2, start = blockIdx.x / 2;
+  // A row's 128 slopes stay in registers: the launch's 3 x 168 become 56 + 2 x 224 for the
+  // three groups of four warps.
+  if (warp < 4) {
+  if (kSlope) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+  if (warp == 0) {
+    Ring<kPairStages> ring;
+    for (int64_t t = start; t < p.tiles && !*stop; t += stride) {
+      const Tile tile = pair_tile_at(p, t);
+      const int64_t m = tile.m * 2 + rank, n = tile.n * 2 + rank;
+      const int64_t m_scale = m < p.m_tiles ? m : p.m_tiles - 1;
+      const int next = tile.n * 2 + 1 < p.n_tiles ? p.k_chunks : 0;  // scale tiles on to w's second 128 rows
+      bool ok = true;
+      for (int sb = 0; sb < p.sum && ok; sb++) {
+        const int64_t b = tile.b + sb;
+        const int ab = p.a_one ? 0 : int(b), wb = p.w_one ? 0 : int(b);
+        int a_scales = int((ab * p.m_tiles + m_scale) * p.k_chunks), w_scales = int((wb * p.n_tiles + tile.n * 2) * p.k_chunks);
+        for (int kb = 0; kb < p.k_blocks; kb++, ring.next()) {
+          if (!(ok = warp_wait(empty + 8 * ring.stage, ring.round ^ 1, stop, 5))) break;
+          const uint32_t dst = smem_at(sm) + ring.stage * kStageBytes, bar = at_first(full + 8 * ring.stage);
+          const bool scales = (kb & 3) == 0;
+          if (elect_one()) {
+            if (rank == 0) bar_expect(full + 8 * ring.stage, 2 * (kStageBytes + (scales ? kPairScaleBytes : 0)));
+            pair_load(dst, &a_map, kb * kTileK, int(m * kTileM), ab, bar);
+            pair_load(dst + kOperandBytes, &w_map, kb * kTileK, int(n * kTileN), wb, bar);
+            if (scales) {
+              const uint32_t at = smem_at(scales_sm) + ring.stage * kPairScaleBytes;
+              pair_load_scales(at, &a_scale_map, a_scales, bar);
+              pair_load_scales(at + 512, &w_scale_map, w_scales, bar);
+              pair_load_scales(at + 1024, &w_scale_map, w_scales + next, bar);
+            }
+          }
+          __syncwarp();
+          if (scales) a_scales++, w_scales++;
+        }
+      }
+    }
+    if (*stop) settle();
+  } else if (warp == 1 && rank == 0) {
+    const uint32_t idesc = (1u << 23) | (uint32_t(256 >> 3) << 17) | (uint32_t(256 >> 4) << 24);
+    Ring<kPairStages> ring;
+    uint32_t n_tile = 0, chunk = 0;
+    for (int64_t t = start; t < p.tiles && !*stop; t += stride, n_tile++) {
+      const uint32_t acc = n_tile & 1, other = acc ^ 1;
+      if (n_tile >= 2 && !warp_wait(acc_empty + 8 * acc, ((n_tile >> 1) - 1) & 1, stop, 6)) break;
+      if (n_tile >= 1 && !warp_wait(tail + 8 * other, ((n_tile - 1) >> 1) & 1, stop, 7)) break;
+      fence_after();
+      uint32_t sfa = 0, sfw = 0;
+      for (int k = 0, kb = 0; k < steps; k++, ring.next()) {
+        const int s = ring.stage;
+        if (!warp_wait(full + 8 * s, ring.round, stop, 8)) break;
+        fence_after();
+        if ((kb & 3) == 0) {
+          const uint32_t turn = chunk++ & 1, at = smem_at(scales_sm) + s * kPairScaleBytes;
+          sfw = tmem + other * 256 + 232 + 8 * turn;
+          sfa = tmem + other * 256 + 248 + 4 * turn;
+          if (elect_one()) {
+            pair_copy_scales(sfa, scale_desc(at));
+            pair_copy_scales(sfw, scale_desc(at + 512));
+            pair_copy_scales(sfw + 4, scale_desc(at + 1024));
+          }
+          __syncwarp();
+        }
+        const uint32_t at = smem_at(sm) + s * kStageBytes;
+        const uint64_t a = operand_desc(at), w = operand_desc(at + kOperandBytes);
+        const uint32_t id = idesc | (uint32_t(kb & 3) << 4) | (uint32_t(kb & 3) << 29);
+        if (elect_one()) {
+#pragma unroll
+          for (int j = 0; j < 4; j++) pair_mma(tmem + acc * 256, a + 2 * j, w + 2 * j, id, sfa, sfw, k > 0 || j > 0);
+          pair_commit(empty + 8 * s);
+        }
+        __syncwarp();
+        if (++kb == p.k_blocks) kb = 0;
+      }
+      if (elect_one()) pair_commit(acc_full + 8 * acc);
+      __syncwarp();
+    }
+  }
+  } else {
+    if (kSlope) asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+    const int quadrant = warp & 3, half = (warp - 4) >> 2;
+    uint8_t* const staged = staging + (warp - 4) * 32 * 128;
+    uint32_t n_tile = 0;
+    for (int64_t t = start; t < p.tiles; t += stride, n_tile++) {
+      const uint32_t acc = n_tile & 1;
+      const bool ok = warp_wait(acc_full + 8 * acc, (n_tile >> 1) & 1, stop, 9);
+      if (!ok) break;
+      fence_after();
+      const Tile pair = pair_tile_at(p, t), tile{pair.b, pair.m * 2 + rank, pair.n * 2 + half};
+      const int64_t row0 = tile.m * kTileM + quadrant * 32;
+      const uint32_t addr = tmem + acc * 256 + half * 128 + (uint32_t(quadrant * 32) << 16);
+      const uint32_t done = at_first(acc_empty + 8 * acc), last = at_first(tail + 8 * acc);
+      if (tile.n >= p.n_tiles || row0 >= p.M) {  // nothing of this warp's block is in the matrix
+        if (lane == 0) {
+          if (half) bar_arrive_cluster(last);
+          bar_arrive_cluster(done);
+        }
+        __syncwarp();
+        continue;
+      }
+      finish_block<kSlope>(p, tile, addr, staged, row0, lane, [&](int c) {
+        if (c == 3 && half && lane == 0) bar_arrive_cluster(last);
+        if (c == 0 && lane == 0) bar_arrive_cluster(done);
+      });
+    }
+  }
+  __syncwarp();
+  fence_before();
+  __syncthreads();
+  cluster_sync();
+  if (warp == 1) {
+    fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(kTmemColumns) : "memory");
   }
 }
 
@@ -477,14 +777,45 @@ bool operand_map(const emr_q8* q, CUtensorMap* map) {
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The 512-byte scale tiles of a q8 matrix, one a row.
+bool scale_map(const emr_q8* q, CUtensorMap* map) {
+  const EncodeTiled fn = encode_tiled();
+  if (!fn) return false;
+  const cuuint64_t tiles = cuuint64_t(q->batch) * q8_scale_batch(q->rows, q->cols) / 512;
+  const cuuint64_t dims[2] = {128, tiles}, strides[1] = {512};
+  const cuuint32_t box[2] = {128, 1}, ones[2] = {1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, q->scales, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <bool kSlope>
-emr_status launch(const CUtensorMap& a, const CUtensorMap& w, const Params& p, cudaStream_t st) {
-  int dev = 0, sms = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
-      cudaFuncSetAttribute(q8_matmul_kernel<kSlope>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes) != cudaSuccess)
+emr_status launch_pairs(const emr_q8* a, const emr_q8* w, const CUtensorMap& a_map, const CUtensorMap& w_map, Params p, int sms,
+                        cudaStream_t st) {
+  CUtensorMap a_scales, w_scales;
+  if (!scale_map(a, &a_scales) || !scale_map(w, &w_scales)) return EMR_ERR_CUDA;
+  if (cudaFuncSetAttribute(q8_pair_kernel<kSlope>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPairSmemBytes) != cudaSuccess)
+    return EMR_ERR_CUDA;
+  p.tiles = p.tiles / (p.m_tiles * p.n_tiles) * ((p.m_tiles + 1) / 2) * ((p.n_tiles + 1) / 2);
+  const int64_t pairs = sms / 2;
+  q8_pair_kernel<kSlope><<<unsigned(2 * (p.tiles < pairs ? p.tiles : pairs)), kPairThreads, kPairSmemBytes, st>>>(
+      a_map, w_map, a_scales, w_scales, p);
+  return cudaGetLastError() == cudaSuccess ? EMR_OK : EMR_ERR_CUDA;
+}
+
+template <bool kSlope>
+emr_status launch(const CUtensorMap& a, const CUtensorMap& w, const Params& p, int sms, cudaStream_t st) {
+  if (cudaFuncSetAttribute(q8_matmul_kernel<kSlope>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes) != cudaSuccess)
     return EMR_ERR_CUDA;
   q8_matmul_kernel<kSlope><<<unsigned(p.tiles < sms ? p.tiles : sms), kThreads, kSmemBytes, st>>>(a, w, p);
   return cudaGetLastError() == cudaSuccess ? EMR_OK : EMR_ERR_CUDA;
+}
+
+// Pairs of SMs where their rounds of 256 x 256 tiles take less time than the rounds of
+// 128 x 128 tiles.
+bool use_pairs(const Params& p, int sms) {
+  const int64_t pair_tiles = p.tiles / (p.m_tiles * p.n_tiles) * ((p.m_tiles + 1) / 2) * ((p.n_tiles + 1) / 2);
+  const int64_t pairs = sms / 2;
+  return pairs > 0 && (pair_tiles + pairs - 1) / pairs * 5 <= (p.tiles + sms - 1) / sms * 3;
 }
 
 }  // namespace
@@ -505,7 +836,9 @@ extern "C" emr_status emr_q8_matmul(const emr_q8* a, const emr_q8* w, const floa
   const __int128 tiles = __int128(p.m_tiles) * p.n_tiles * (sum_batch ? 1 : batch);
   const __int128 steps = __int128(q8_blocks(a->cols)) * (sum_batch ? batch : 1);
   const int64_t reach = q8_row_bytes(a->cols) * (p.M > p.N ? p.M : p.N);  // bytes between two batches
-  if (tiles > INT64_MAX / 2 || steps > INT32_MAX || reach >= (int64_t(1) << 40)) return EMR_ERR_RANGE;
+  const int64_t scale_tiles = q8_scale_batch(p.M > p.N ? p.M : p.N, a->cols) / 512;
+  if (tiles > INT64_MAX / 2 || steps > INT32_MAX || reach >= (int64_t(1) << 40) || __int128(scale_tiles) * batch > INT32_MAX)
+    return EMR_ERR_RANGE;
   p.tiles = int64_t(tiles);
   p.k_blocks = int32_t(q8_blocks(a->cols)), p.k_chunks = int32_t(q8_scale_chunks(a->cols));
   p.sum = sum_batch ? batch : 1;
@@ -518,7 +851,12 @@ extern "C" emr_status emr_q8_matmul(const emr_q8* a, const emr_q8* w, const floa
   CUtensorMap a_map, w_map;
   if (!operand_map(a, &a_map) || !operand_map(w, &w_map)) return EMR_ERR_CUDA;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return slope ? launch<true>(a_map, w_map, p, st) : launch<false>(a_map, w_map, p, st);
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return EMR_ERR_CUDA;
+  if (use_pairs(p, sms))
+    return slope ? launch_pairs<true>(a, w, a_map, w_map, p, sms, st) : launch_pairs<false>(a, w, a_map, w_map, p, sms, st);
+  return slope ? launch<true>(a_map, w_map, p, sms, st) : launch<false>(a_map, w_map, p, sms, st);
 }
 
 extern "C" emr_status emr_device_error(int32_t* code, void* stream) {
