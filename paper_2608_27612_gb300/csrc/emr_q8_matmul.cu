@@ -136,9 +136,22 @@ __device__ __forceinline__ void settle() {
 }
 
 // ---- activations and their slopes ----------------------------------------------------
-// sigmoid and tanh are taken from t = e^-|z| or e^-2|z| and r = 1 / (1 + t): every
-// form below is a product of positive terms, so the slopes keep their relative
-// precision where the functions saturate (1 - y^2 would lose it).
+// The transcendental parts run on the special function unit. sigmoid and tanh are taken
+// from t = e^-|z| or e^-2|z| and r = 1 / (1 + t): every form below is a product of
+// positive terms, so the slopes keep their relative precision where the functions
+// saturate (1 - y^2 would lose it).
+
+__device__ __forceinline__ float fast_exp2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float fast_rcp(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+constexpr float kLog2E = 0x1.715476p+0f;
 
 // Element i of sin and cos where the argument is large; i is not known at compile time, so the
 // element is picked by comparison instead of by an address.
@@ -161,7 +174,7 @@ __device__ __forceinline__ void activate(int act, float (&z)[32], float (&d)[32]
     case EMR_ACT_SIGMOID:
 #pragma unroll
       for (int i = 0; i < 32; i++) {
-        const float t = __expf(-fabsf(z[i])), r = __fdividef(1.f, 1.f + t);
+        const float t = fast_exp2(fabsf(z[i]) * -kLog2E), r = fast_rcp(1.f + t);
         if (kSlope) d[i] = t * r * r;
         z[i] = z[i] >= 0.f ? r : t * r;
       }
@@ -169,18 +182,17 @@ __device__ __forceinline__ void activate(int act, float (&z)[32], float (&d)[32]
     case EMR_ACT_TANH:
 #pragma unroll
       for (int i = 0; i < 32; i++) {
-        const float t = __expf(-2.f * fabsf(z[i])), r = __fdividef(1.f, 1.f + t);
-        if (kSlope) d[i] = 4.f * t * r * r;
-        // below 1/8 the odd series, whose next term is 17 z^7 / 315 (relative 3e-7)
-        const float q = z[i] * z[i];
-        const float series = z[i] * fmaf(q, fmaf(q, 2.f / 15.f, -1.f / 3.f), 1.f);
-        z[i] = fabsf(z[i]) < 0.125f ? series : copysignf((1.f - t) * r, z[i]);
+        const float t = fast_exp2(fabsf(z[i]) * (-2.f * kLog2E)), r = fast_rcp(1.f + t);
+        if (kSlope) d[i] = (4.f * t) * (r * r);
+        // below 1/25 two terms of the series; the next one is 2 z^4 / 15 (relative 4e-7)
+        const float series = z[i] * fmaf(z[i] * z[i], -1.f / 3.f, 1.f);
+        z[i] = fabsf(z[i]) < 0.04f ? series : copysignf((1.f - t) * r, z[i]);
       }
       break;
     case EMR_ACT_GAUSS:
 #pragma unroll
       for (int i = 0; i < 32; i++) {
-        const float y = __expf(-z[i] * z[i]);
+        const float y = fast_exp2(z[i] * (z[i] * -kLog2E));
         if (kSlope) d[i] = y == 0.f ? 0.f : -2.f * z[i] * y;  // an infinite z has slope 0
         z[i] = y;
       }
@@ -194,7 +206,7 @@ __device__ __forceinline__ void activate(int act, float (&z)[32], float (&d)[32]
       if (most < 8192.f) {
 #pragma unroll
         for (int i = 0; i < 32; i++) {
-          const float k = rintf(z[i] * 0x1.45f306p-3f);
+          const float k = fmaf(z[i], 0x1.45f306p-3f, 0x1.8p+23f) - 0x1.8p+23f;  // nearest whole number of periods
           const float r = fmaf(-k, -0x1.777a5cp-23f, fmaf(-k, 0x1.921fb6p+2f, z[i]));
           if (kSlope) d[i] = __cosf(r);
           z[i] = __sinf(r);
@@ -223,19 +235,20 @@ __device__ __forceinline__ void activate(int act, float (&z)[32], float (&d)[32]
 // ---- tiles ---------------------------------------------------------------------------
 
 constexpr int kTileM = 128, kTileN = 128, kTileK = 128;
-constexpr int kStages = 6;
+constexpr int kStages = 5;
 constexpr int kOperandBytes = 128 * 128;
 constexpr int kStageBytes = 2 * kOperandBytes;
 constexpr int kScaleBytes = 1024;           // 512 for each operand
-constexpr int kStagingBytes = 4 * 32 * 128; // for each epilogue warp 32 rows of 128 bytes
-constexpr int kThreads = 192;               // copy warp, matrix warp, four epilogue warps
+constexpr int kFinishWarps = 16;            // epilogue: four for each quarter of the rows, 32 columns each
+constexpr int kStagingBytes = kFinishWarps * 32 * 64;  // 32 rows of 64 bytes a warp
+constexpr int kThreads = 32 * (4 + kFinishWarps);      // copy warp, matrix warp, two that only wait, epilogue
 constexpr int kTmemColumns = 512;
 constexpr uint32_t kTmemScales = 256;       // behind the two accumulators of 128 columns
 constexpr int kSmemBytes = 1024 + kStages * (kStageBytes + kScaleBytes) + kStagingBytes;
 
 struct Params {
-  int64_t M, N;
-  int64_t m_tiles, n_tiles, tiles;  // tiles: over the batches of the output
+  int32_t M, N;
+  int32_t m_tiles, n_tiles, tiles;  // tiles: over the batches of the output
   int32_t k_blocks, k_chunks;       // blocks of 128 columns, and scale chunks of four of them
   int32_t sum;                      // batches that one output sums over
   int32_t a_one, w_one;             // operand with batch 1
@@ -248,17 +261,19 @@ struct Params {
 };
 
 struct Tile {
-  int64_t b, m, n;
+  int32_t b, m, n;
 };
 // Tiles in groups of 16 row tiles, so that the operand rows in use at a time stay in L2.
-__device__ __forceinline__ Tile tile_at(const Params& p, int64_t t) {
-  const int64_t per = p.m_tiles * p.n_tiles, b = t / per;
+// 32-bit divisions: every warp makes them for every tile.
+__device__ __forceinline__ Tile raster(uint32_t t, uint32_t m_tiles, uint32_t n_tiles, uint32_t tiles, uint32_t tall) {
+  const uint32_t per = m_tiles * n_tiles, b = per == tiles ? 0 : t / per;
   t -= b * per;
-  const int64_t group = t / (16 * p.n_tiles), first = group * 16;
-  const int64_t rows = p.m_tiles - first < 16 ? p.m_tiles - first : 16;
-  t -= first * p.n_tiles;
-  return {b, first + t % rows, t / rows};
+  const uint32_t group = t / (tall * n_tiles), first = group * tall, rows = m_tiles - first < tall ? m_tiles - first : tall;
+  t -= first * n_tiles;
+  const uint32_t n = t / rows;
+  return {int32_t(b), int32_t(first + t - n * rows), int32_t(n)};
 }
+__device__ __forceinline__ Tile tile_at(const Params& p, int t) { return raster(t, p.m_tiles, p.n_tiles, p.tiles, 16); }
 
 // Place in the ring of stages: counted up, not divided, since the copy and matrix loops are
 // one thread each and a block of 128 columns gives them 256 clocks.
@@ -271,17 +286,17 @@ struct Ring {
   }
 };
 
-// A warp's 32 staged rows of 128 bytes to global rows, `width` bytes a lane, neighbouring
+// A warp's 32 staged rows of 64 bytes to global rows, sizeof(T) bytes a lane, neighbouring
 // lanes neighbouring addresses. `bytes` are valid in each row, `rows` rows.
 template <typename T>
 __device__ __forceinline__ void store_rows(const uint8_t* staged, uint8_t* out, int64_t pitch, int rows, int bytes, int lane) {
-  constexpr int kPer = 128 / int(sizeof(T));
-  for (int i = lane; i < 32 * kPer; i += 32) {
-    const int r = i / kPer, at = (i % kPer) * int(sizeof(T));
-    if (r < rows && at < bytes)
+  constexpr int kPer = 64 / int(sizeof(T));
+  const int at = lane % kPer * int(sizeof(T));
+#pragma unroll 4
+  for (int r = lane / kPer; r < rows; r += 32 / kPer)
+    if (at < bytes)
       *reinterpret_cast<T*>(out + r * pitch + at) =
-          *reinterpret_cast<const T*>(staged + r * 128 + (((at >> 4) ^ (r & 7)) << 4) + (at & 15));
-  }
+          *reinterpret_cast<const T*>(staged + r * 64 + (((at >> 4) ^ ((r >> 1) & 3)) << 4) + (at & 15));
 }
 __device__ __forceinline__ void store_staged(const uint8_t* staged, uint8_t* out, int64_t pitch, int rows, int bytes, int width,
                                              int lane) {
@@ -293,7 +308,7 @@ __device__ __forceinline__ void store_staged(const uint8_t* staged, uint8_t* out
   __syncwarp();
 }
 __device__ __forceinline__ void stage16(uint8_t* staged, int row, int unit, uint4 v) {
-  *reinterpret_cast<uint4*>(staged + row * 128 + ((unit ^ (row & 7)) << 4)) = v;
+  *reinterpret_cast<uint4*>(staged + row * 64 + ((unit ^ ((row >> 1) & 3)) << 4)) = v;
 }
 __device__ __forceinline__ uint32_t pack_half(int dtype, float a, float b) {
   if (dtype == EMR_BF16) {
@@ -304,95 +319,108 @@ __device__ __forceinline__ uint32_t pack_half(int dtype, float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// One row of 32 finished values, columns 32 c .. 32 c + 31 of the tile, to the staging rows
-// and, when 128 bytes of a row are there, to out. c falls from 3 to 0.
-__device__ __forceinline__ void put_out(const Params& p, const Tile& t, int c, const float (&y)[32], uint8_t* staged,
-                                        int64_t row0, int lane) {
-  const int rows = int(p.M - row0 < 32 ? p.M - row0 : 32);  // may be below 1: nothing is stored
-  const int64_t n0 = t.n * kTileN;
+// What the epilogue's warps share.
+struct Finish {
+  float tops[2][128][4];  // largest slope of a row's 32 columns, two turns
+  float bias[kFinishWarps][32];
+};
+__device__ __forceinline__ void store32(uint8_t* to, const uint32_t (&w)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+               "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
+}
+
+// A warp's 32 rows and 32 columns (c-th of four) of one 128-column accumulator block at tensor
+// memory address addr: bias, activation, output and, with kSlope, slope. read() is called
+// when the accumulators have been read. Sixteen warps share a block because a warp by itself
+// issues an instruction only every four or five clocks, and in chunks of 32 columns because the
+// code of more, unrolled, does not stay in the instruction cache.
+template <bool kSlope, typename Read>
+__device__ __forceinline__ void finish_chunk(const Params& p, const Tile& t, uint32_t addr, int c, float bias, uint8_t* staged,
+                                             Finish& share, uint32_t turn, int row0, int warp, int lane, Read read) {
+  const int n0 = t.n * kTileN + c * 32;
+  const int rows = p.M - row0 < 32 ? p.M - row0 : 32;
+  const int cols = p.N - n0 < 32 ? p.N - n0 : 32;  // may be below 1
+  const int64_t first = (int64_t(t.b) * p.M + row0) * p.N + n0;
+  float z[32], d[32];
+  tmem_load32(addr + c * 32, z);
+  fence_before();
+  read();
+  if (p.bias) {
+    float* const own = share.bias[warp];
+    own[lane] = bias;
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      const float4 b = reinterpret_cast<const float4*>(own)[i];
+      z[4 * i] += b.x, z[4 * i + 1] += b.y, z[4 * i + 2] += b.z, z[4 * i + 3] += b.w;
+    }
+    __syncwarp();
+  }
+  activate<kSlope>(p.act, z, d);
   if (p.out_dtype == EMR_F32) {
 #pragma unroll
-    for (int i = 0; i < 8; i++)
-      stage16(staged, lane, i, make_uint4(__float_as_uint(y[4 * i]), __float_as_uint(y[4 * i + 1]),
-                                          __float_as_uint(y[4 * i + 2]), __float_as_uint(y[4 * i + 3])));
-    const int64_t left = (p.N - n0 - c * 32) * 4;
-    store_staged(staged, static_cast<uint8_t*>(p.out) + ((t.b * p.M + row0) * p.N + n0 + c * 32) * 4, p.N * 4, rows,
-                 int(left < 128 ? left : 128), p.store_bytes, lane);
-    return;
-  }
+    for (int h = 0; h < 2; h++) {
 #pragma unroll
-  for (int i = 0; i < 4; i++)
-    stage16(staged, lane, (c & 1) * 4 + i,
-            make_uint4(pack_half(p.out_dtype, y[8 * i], y[8 * i + 1]), pack_half(p.out_dtype, y[8 * i + 2], y[8 * i + 3]),
-                       pack_half(p.out_dtype, y[8 * i + 4], y[8 * i + 5]), pack_half(p.out_dtype, y[8 * i + 6], y[8 * i + 7])));
-  if (!(c & 1)) {
-    const int64_t first = n0 + c * 32, left = (p.N - first) * 2;
-    store_staged(staged, static_cast<uint8_t*>(p.out) + ((t.b * p.M + row0) * p.N + first) * 2, p.N * 2, rows,
-                 int(left < 128 ? left : 128), p.store_bytes, lane);
+      for (int i = 0; i < 4; i++) {
+        const int j = h * 16 + i * 4;
+        stage16(staged, lane, i, make_uint4(__float_as_uint(z[j]), __float_as_uint(z[j + 1]), __float_as_uint(z[j + 2]), __float_as_uint(z[j + 3])));
+      }
+      const int left = (cols - h * 16) * 4;
+      store_staged(staged, static_cast<uint8_t*>(p.out) + (first + h * 16) * 4, int64_t(p.N) * 4, rows,
+                   left < 64 ? left : 64, p.store_bytes, lane);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+      stage16(staged, lane, i,
+              make_uint4(pack_half(p.out_dtype, z[8 * i], z[8 * i + 1]), pack_half(p.out_dtype, z[8 * i + 2], z[8 * i + 3]),
+                         pack_half(p.out_dtype, z[8 * i + 4], z[8 * i + 5]), pack_half(p.out_dtype, z[8 * i + 6], z[8 * i + 7])));
+    store_staged(staged, static_cast<uint8_t*>(p.out) + first * 2, int64_t(p.N) * 2, rows, cols * 2, p.store_bytes, lane);
+  }
+  if constexpr (kSlope) {
+    if (cols < 32) {
+#pragma unroll
+      for (int i = 0; i < 32; i++) d[i] = i < cols ? d[i] : 0.f;
+    }
+    float top = 0.f;  // slopes are finite or NaN, which the maxima pass over
+#pragma unroll
+    for (int i = 0; i < 32; i++) top = fmaxf(top, fabsf(d[i]));
+    const int quadrant = warp & 3;
+    float(&tops)[4] = share.tops[turn & 1][quadrant * 32 + lane];
+    tops[c] = top;
+    asm volatile("bar.sync %0, 128;" ::"r"(1 + quadrant) : "memory");  // the row's four warps
+    const float4 all = *reinterpret_cast<const float4*>(tops);
+    const uint32_t byte = q8_scale_byte(__float_as_uint(fmaxf(fmaxf(all.x, all.y), fmaxf(all.z, all.w))));
+    const float inv = q8_inverse(byte);
+    if (lane < rows) {
+      uint32_t w[8];
+#pragma unroll
+      for (int i = 0; i < 8; i++) w[i] = q8_pack4(d[4 * i], d[4 * i + 1], d[4 * i + 2], d[4 * i + 3], inv);
+      const int row = row0 + lane;
+      store32(p.slope + (int64_t(t.b) * p.M + row) * q8_row_bytes(p.N) + n0, w);
+      if (c == 0) p.slope_scales[t.b * q8_scale_batch(p.M, p.N) + q8_scale_at(q8_scale_chunks(p.N), row, t.n)] = uint8_t(byte);
+    }
   }
 }
 
-// The slopes of one row's 128 columns as 8-bit codes with their scale.
-__device__ __forceinline__ void put_slope(const Params& p, const Tile& t, float (&d)[4][32], uint8_t* staged, int64_t row0,
-                                          int lane) {
-  const int64_t n0 = t.n * kTileN;
-  const int left = int(p.N - n0 < 128 ? p.N - n0 : 128);
-  uint32_t top = 0;
-#pragma unroll
-  for (int c = 0; c < 4; c++)
-#pragma unroll
-    for (int i = 0; i < 32; i++) {
-      if (c * 32 + i >= left) d[c][i] = 0.f;
-      d[c][i] = q8_finite_or_nan(d[c][i]);
-      top = max(top, q8_magnitude(d[c][i]));
-    }
-  const uint32_t byte = q8_scale_byte(top);
-  const float inv = q8_inverse(byte);
-#pragma unroll
-  for (int u = 0; u < 8; u++) {
-    uint32_t w[4];
-#pragma unroll
-    for (int j = 0; j < 4; j++) {
-      const int i = (u & 1) * 16 + j * 4;
-      w[j] = q8_pack4(d[u >> 1][i], d[u >> 1][i + 1], d[u >> 1][i + 2], d[u >> 1][i + 3], inv);
-    }
-    stage16(staged, lane, u, make_uint4(w[0], w[1], w[2], w[3]));
-  }
-  const int rows = int(p.M - row0 < 32 ? p.M - row0 : 32);
-  const int64_t row_bytes = q8_row_bytes(p.N);
-  store_staged(staged, p.slope + (t.b * p.M + row0) * row_bytes + n0, row_bytes, rows, 128, 16, lane);
-  if (lane < rows)
-    p.slope_scales[t.b * q8_scale_batch(p.M, p.N) + q8_scale_at(q8_scale_chunks(p.N), row0 + lane, t.n)] = uint8_t(byte);
-}
-
-// A warp's 32 rows of one 128-column accumulator block at tensor memory address addr: bias,
-// activation, output and, with kSlope, slope. read(c) is called when columns 32 c ..
-// 32 c + 31 have been read.
-template <bool kSlope, typename Read>
-__device__ __forceinline__ void finish_block(const Params& p, const Tile& t, uint32_t addr, uint8_t* staged, int64_t row0, int lane,
-                                             Read read) {
-  const int64_t n0 = t.n * kTileN;
-  const float* bias = p.bias ? p.bias + t.b * p.N + n0 : nullptr;
-  float d[kSlope ? 4 : 1][32];
-#pragma unroll(kSlope ? 4 : 1)
-  for (int c = 3; c >= 0; c--) {
-    float z[32];
-    tmem_load32(addr + c * 32, z);
-    fence_before();
-    read(c);
-    if (bias) {
-      const float own = n0 + c * 32 + lane < p.N ? __ldg(bias + c * 32 + lane) : 0.f;
-#pragma unroll
-      for (int i = 0; i < 32; i++) z[i] += __shfl_sync(0xffffffffu, own, i);
-    }
-    activate<kSlope>(p.act, z, d[kSlope ? c : 0]);
-    put_out(p, t, c, z, staged, row0, lane);
-  }
-  if constexpr (kSlope) put_slope(p, t, d, staged, row0, lane);
+// Whether the accumulators of a tile are there, with one answer for the four warps that share
+// rows, since with kSlope they meet at a barrier while finishing the tile.
+template <bool kSlope>
+__device__ __forceinline__ bool finish_wait(uint32_t bar, uint32_t parity, volatile int* stop, int code, int quadrant) {
+  const bool ok = warp_wait(bar, parity, stop, code);
+  if (!kSlope) return ok;
+  uint32_t all;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.and.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(all)
+      : "r"(uint32_t(ok)), "r"(1 + quadrant)
+      : "memory");
+  return all != 0;
 }
 
 // Persistent: a block takes tiles blockIdx.x, + gridDim.x, ... Warp 0 copies operand and
-// scale tiles into a ring of stages, warp 1 issues the matrix instructions, warps 2..5
+// scale tiles into a ring of stages, warp 1 issues the matrix instructions, warps 4..19
 // finish a tile while the next one accumulates in the other half of tensor memory.
 template <bool kSlope>
 __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_constant__ CUtensorMap a_map,
@@ -400,6 +428,7 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
                                                                 const __grid_constant__ Params p) {
   extern __shared__ uint8_t raw[];
   __shared__ uint64_t bars[2 * kStages + 4];
+  __shared__ Finish share;
   __shared__ uint32_t tmem_base;
   __shared__ int gave_up;
   uint8_t* const sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
@@ -412,7 +441,7 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
   if (threadIdx.x == 0) {
     gave_up = 0;
     for (int i = 0; i < kStages; i++) bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, 1);
-    for (int i = 0; i < 2; i++) bar_init(acc_full + 8 * i, 1), bar_init(acc_empty + 8 * i, 4);
+    for (int i = 0; i < 2; i++) bar_init(acc_full + 8 * i, 1), bar_init(acc_empty + 8 * i, kFinishWarps);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&a_map) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&w_map) : "memory");
@@ -430,15 +459,14 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
 
   if (warp == 0) {
     Ring<kStages> ring;
-    for (int64_t t = blockIdx.x; t < p.tiles && !*stop; t += gridDim.x) {
+    for (int t = blockIdx.x; t < p.tiles && !*stop; t += gridDim.x) {
       const Tile tile = tile_at(p, t);
-      const int m = int(tile.m * kTileM), n = int(tile.n * kTileN);
+      const int m = tile.m * kTileM, n = tile.n * kTileN;
       bool ok = true;
       for (int sb = 0; sb < p.sum && ok; sb++) {
-        const int64_t b = tile.b + sb;
-        const int ab = p.a_one ? 0 : int(b), wb = p.w_one ? 0 : int(b);
-        const uint8_t* a_scales = p.a_scales + (ab * p.m_tiles + tile.m) * p.k_chunks * 512;
-        const uint8_t* w_scales = p.w_scales + (wb * p.n_tiles + tile.n) * p.k_chunks * 512;
+        const int b = tile.b + sb, ab = p.a_one ? 0 : b, wb = p.w_one ? 0 : b;
+        const uint8_t* a_scales = p.a_scales + (int64_t(ab) * p.m_tiles + tile.m) * p.k_chunks * 512;
+        const uint8_t* w_scales = p.w_scales + (int64_t(wb) * p.n_tiles + tile.n) * p.k_chunks * 512;
         for (int kb = 0; kb < p.k_blocks; kb++, ring.next()) {
           // a new ring is empty: the wait for the round before the first returns at once
           if (!(ok = warp_wait(empty + 8 * ring.stage, ring.round ^ 1, stop, 1))) break;
@@ -464,7 +492,7 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
     const uint32_t idesc = (1u << 23) | (uint32_t(kTileN >> 3) << 17) | (uint32_t(kTileM >> 4) << 24);
     Ring<kStages> ring;
     uint32_t n_tile = 0, chunk = 0;
-    for (int64_t t = blockIdx.x; t < p.tiles && !*stop; t += gridDim.x, n_tile++) {
+    for (int t = blockIdx.x; t < p.tiles && !*stop; t += gridDim.x, n_tile++) {
       const uint32_t acc = n_tile & 1;
       if (n_tile >= 2 && !warp_wait(acc_empty + 8 * acc, ((n_tile >> 1) - 1) & 1, stop, 2)) break;
       fence_after();
@@ -497,20 +525,26 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
       if (elect_one()) mma_commit(acc_full + 8 * acc);
       __syncwarp();
     }
-  } else if (warp >= 2) {
+  } else if (warp >= 4) {
     const int quadrant = warp & 3;  // tensor memory lanes that this warp may read
-    uint8_t* const staged = staging + (warp - 2) * 32 * 128;
+    const int own = warp - 4, c = own >> 2;
+    uint8_t* const staged = staging + own * 32 * 64;
     uint32_t n_tile = 0;
-    for (int64_t t = blockIdx.x; t < p.tiles; t += gridDim.x, n_tile++) {
+    for (int t = blockIdx.x; t < p.tiles; t += gridDim.x, n_tile++) {
       const uint32_t acc = n_tile & 1;
-      const bool ok = warp_wait(acc_full + 8 * acc, (n_tile >> 1) & 1, stop, 4);
-      if (!ok) break;
-      fence_after();
       const Tile tile = tile_at(p, t);
-      const int64_t row0 = tile.m * kTileM + quadrant * 32;
+      const int row0 = tile.m * kTileM + quadrant * 32, n = tile.n * kTileN + c * 32 + lane;
+      const float bias = p.bias && n < p.N ? __ldg(p.bias + int64_t(tile.b) * p.N + n) : 0.f;
+      if (!finish_wait<kSlope>(acc_full + 8 * acc, (n_tile >> 1) & 1, stop, 4, quadrant)) break;
+      fence_after();
+      if (row0 >= p.M || (!kSlope && n - lane >= p.N)) {  // nothing of this warp's part is in the matrix
+        if (lane == 0) bar_arrive(acc_empty + 8 * acc);
+        __syncwarp();
+        continue;
+      }
       const uint32_t addr = tmem + acc * kTileN + (uint32_t(quadrant * 32) << 16);
-      finish_block<kSlope>(p, tile, addr, staged, row0, lane, [&](int c) {
-        if (c == 0 && lane == 0) bar_arrive(acc_empty + 8 * acc);
+      finish_chunk<kSlope>(p, tile, addr, c, bias, staged, share, n_tile, row0, own, lane, [&] {
+        if (lane == 0) bar_arrive(acc_empty + 8 * acc);
       });
     }
   }
@@ -534,8 +568,7 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
 
 constexpr int kPairStages = 5;
 constexpr int kPairScaleBytes = 1536;  // 512 of a, 1024 of w
-constexpr int kPairThreads = 384;      // copy warp, matrix warp, two that only wait, eight epilogue warps
-constexpr int kPairSmemBytes = 1024 + kPairStages * (kStageBytes + kPairScaleBytes) + 8 * 32 * 128;
+constexpr int kPairSmemBytes = 1024 + kPairStages * (kStageBytes + kPairScaleBytes) + kStagingBytes;
 
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
@@ -584,21 +617,18 @@ __device__ __forceinline__ void pair_commit(uint32_t bar) {
 }
 
 // Tile t of the pairs' raster: b, and row and column of 256 (groups of 8 row tiles).
-__device__ __forceinline__ Tile pair_tile_at(const Params& p, int64_t t) {
-  const int64_t mp = (p.m_tiles + 1) / 2, np = (p.n_tiles + 1) / 2, per = mp * np, b = t / per;
-  t -= b * per;
-  const int64_t group = t / (8 * np), first = group * 8, rows = mp - first < 8 ? mp - first : 8;
-  t -= first * np;
-  return {b, first + t % rows, t / rows};
+__device__ __forceinline__ Tile pair_tile_at(const Params& p, int t) {
+  return raster(t, (p.m_tiles + 1) / 2, (p.n_tiles + 1) / 2, p.tiles, 8);
 }
 
 template <bool kSlope>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     q8_pair_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap w_map,
                    const __grid_constant__ CUtensorMap a_scale_map, const __grid_constant__ CUtensorMap w_scale_map,
                    const __grid_constant__ Params p) {
   extern __shared__ uint8_t raw[];
   __shared__ uint64_t bars[2 * kPairStages + 6];
+  __shared__ Finish share;
   __shared__ uint32_t tmem_base;
   __shared__ int gave_up;
   // the dynamic part starts at the same address in both blocks
@@ -614,7 +644,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
   if (threadIdx.x == 0) {
     gave_up = 0;
     for (int i = 0; i < kPairStages; i++) bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, 1);
-    for (int i = 0; i < 2; i++) bar_init(acc_full + 8 * i, 1), bar_init(acc_empty + 8 * i, 16), bar_init(tail + 8 * i, 8);
+    for (int i = 0; i < 2; i++) bar_init(acc_full + 8 * i, 1), bar_init(acc_empty + 8 * i, 2 * kFinishWarps), bar_init(tail + 8 * i, 8);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&a_map) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&w_map) : "memory");
@@ -630,31 +660,26 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
   fence_after();
   const uint32_t tmem = tmem_base;
   const int steps = p.sum * p.k_blocks;
-  const int64_t stride = gridDim.x / 2, start = blockIdx.x / 2;
-  // A row's 128 slopes stay in registers: the launch's 3 x 168 become 56 + 2 x 224 for the
-  // three groups of four warps.
-  if (warp < 4) {
-  if (kSlope) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+  const int stride = gridDim.x / 2, start = blockIdx.x / 2;
   if (warp == 0) {
     Ring<kPairStages> ring;
-    for (int64_t t = start; t < p.tiles && !*stop; t += stride) {
+    for (int t = start; t < p.tiles && !*stop; t += stride) {
       const Tile tile = pair_tile_at(p, t);
-      const int64_t m = tile.m * 2 + rank, n = tile.n * 2 + rank;
-      const int64_t m_scale = m < p.m_tiles ? m : p.m_tiles - 1;
+      const int m = tile.m * 2 + int(rank), n = tile.n * 2 + int(rank);
+      const int m_scale = m < p.m_tiles ? m : p.m_tiles - 1;
       const int next = tile.n * 2 + 1 < p.n_tiles ? p.k_chunks : 0;  // scale tiles on to w's second 128 rows
       bool ok = true;
       for (int sb = 0; sb < p.sum && ok; sb++) {
-        const int64_t b = tile.b + sb;
-        const int ab = p.a_one ? 0 : int(b), wb = p.w_one ? 0 : int(b);
-        int a_scales = int((ab * p.m_tiles + m_scale) * p.k_chunks), w_scales = int((wb * p.n_tiles + tile.n * 2) * p.k_chunks);
+        const int b = tile.b + sb, ab = p.a_one ? 0 : b, wb = p.w_one ? 0 : b;
+        int a_scales = (ab * p.m_tiles + m_scale) * p.k_chunks, w_scales = (wb * p.n_tiles + tile.n * 2) * p.k_chunks;
         for (int kb = 0; kb < p.k_blocks; kb++, ring.next()) {
           if (!(ok = warp_wait(empty + 8 * ring.stage, ring.round ^ 1, stop, 5))) break;
           const uint32_t dst = smem_at(sm) + ring.stage * kStageBytes, bar = at_first(full + 8 * ring.stage);
           const bool scales = (kb & 3) == 0;
           if (elect_one()) {
             if (rank == 0) bar_expect(full + 8 * ring.stage, 2 * (kStageBytes + (scales ? kPairScaleBytes : 0)));
-            pair_load(dst, &a_map, kb * kTileK, int(m * kTileM), ab, bar);
-            pair_load(dst + kOperandBytes, &w_map, kb * kTileK, int(n * kTileN), wb, bar);
+            pair_load(dst, &a_map, kb * kTileK, m * kTileM, ab, bar);
+            pair_load(dst + kOperandBytes, &w_map, kb * kTileK, n * kTileN, wb, bar);
             if (scales) {
               const uint32_t at = smem_at(scales_sm) + ring.stage * kPairScaleBytes;
               pair_load_scales(at, &a_scale_map, a_scales, bar);
@@ -672,7 +697,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     const uint32_t idesc = (1u << 23) | (uint32_t(256 >> 3) << 17) | (uint32_t(256 >> 4) << 24);
     Ring<kPairStages> ring;
     uint32_t n_tile = 0, chunk = 0;
-    for (int64_t t = start; t < p.tiles && !*stop; t += stride, n_tile++) {
+    for (int t = start; t < p.tiles && !*stop; t += stride, n_tile++) {
       const uint32_t acc = n_tile & 1, other = acc ^ 1;
       if (n_tile >= 2 && !warp_wait(acc_empty + 8 * acc, ((n_tile >> 1) - 1) & 1, stop, 6)) break;
       if (n_tile >= 1 && !warp_wait(tail + 8 * other, ((n_tile - 1) >> 1) & 1, stop, 7)) break;
@@ -707,34 +732,40 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       if (elect_one()) pair_commit(acc_full + 8 * acc);
       __syncwarp();
     }
-  }
-  } else {
-    if (kSlope) asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
-    const int quadrant = warp & 3, half = (warp - 4) >> 2;
-    uint8_t* const staged = staging + (warp - 4) * 32 * 128;
-    uint32_t n_tile = 0;
-    for (int64_t t = start; t < p.tiles; t += stride, n_tile++) {
+  } else if (warp >= 4) {
+    const int quadrant = warp & 3, own = warp - 4, c = own >> 2;
+    uint8_t* const staged = staging + own * 32 * 64;
+    uint32_t n_tile = 0, turn = 0;
+    for (int t = start; t < p.tiles; t += stride, n_tile++) {
       const uint32_t acc = n_tile & 1;
-      const bool ok = warp_wait(acc_full + 8 * acc, (n_tile >> 1) & 1, stop, 9);
-      if (!ok) break;
-      fence_after();
-      const Tile pair = pair_tile_at(p, t), tile{pair.b, pair.m * 2 + rank, pair.n * 2 + half};
-      const int64_t row0 = tile.m * kTileM + quadrant * 32;
-      const uint32_t addr = tmem + acc * 256 + half * 128 + (uint32_t(quadrant * 32) << 16);
+      const Tile pair = pair_tile_at(p, t);
+      const int row0 = (pair.m * 2 + int(rank)) * kTileM + quadrant * 32;
+      const uint32_t addr = tmem + acc * 256 + (uint32_t(quadrant * 32) << 16);
       const uint32_t done = at_first(acc_empty + 8 * acc), last = at_first(tail + 8 * acc);
-      if (tile.n >= p.n_tiles || row0 >= p.M) {  // nothing of this warp's block is in the matrix
-        if (lane == 0) {
-          if (half) bar_arrive_cluster(last);
-          bar_arrive_cluster(done);
+#pragma unroll 1
+      for (int half = 1; half >= 0; half--, turn++) {  // the scales' columns first
+        const Tile tile{pair.b, pair.m * 2 + int(rank), pair.n * 2 + half};
+        const int n = tile.n * kTileN + c * 32 + lane;
+        const float bias = p.bias && n < p.N ? __ldg(p.bias + int64_t(tile.b) * p.N + n) : 0.f;
+        if (half) {
+          if (!finish_wait<kSlope>(acc_full + 8 * acc, (n_tile >> 1) & 1, stop, 9, quadrant)) goto out;
+          fence_after();
         }
-        __syncwarp();
-        continue;
+        auto read = [&] {
+          if (lane == 0) {
+            if (half && c == 3) bar_arrive_cluster(last);
+            if (!half) bar_arrive_cluster(done);
+          }
+        };
+        if (row0 >= p.M || tile.n >= p.n_tiles || (!kSlope && n - lane >= p.N)) {  // nothing of this warp's part is in the matrix
+          read();
+          __syncwarp();
+          continue;
+        }
+        finish_chunk<kSlope>(p, tile, addr + half * 128, c, bias, staged, share, turn, row0, own, lane, read);
       }
-      finish_block<kSlope>(p, tile, addr, staged, row0, lane, [&](int c) {
-        if (c == 3 && half && lane == 0) bar_arrive_cluster(last);
-        if (c == 0 && lane == 0) bar_arrive_cluster(done);
-      });
     }
+  out:;
   }
   __syncwarp();
   fence_before();
@@ -797,7 +828,7 @@ emr_status launch_pairs(const emr_q8* a, const emr_q8* w, const CUtensorMap& a_m
     return EMR_ERR_CUDA;
   p.tiles = p.tiles / (p.m_tiles * p.n_tiles) * ((p.m_tiles + 1) / 2) * ((p.n_tiles + 1) / 2);
   const int64_t pairs = sms / 2;
-  q8_pair_kernel<kSlope><<<unsigned(2 * (p.tiles < pairs ? p.tiles : pairs)), kPairThreads, kPairSmemBytes, st>>>(
+  q8_pair_kernel<kSlope><<<unsigned(2 * (p.tiles < pairs ? p.tiles : pairs)), kThreads, kPairSmemBytes, st>>>(
       a_map, w_map, a_scales, w_scales, p);
   return cudaGetLastError() == cudaSuccess ? EMR_OK : EMR_ERR_CUDA;
 }
@@ -810,12 +841,19 @@ emr_status launch(const CUtensorMap& a, const CUtensorMap& w, const Params& p, i
   return cudaGetLastError() == cudaSuccess ? EMR_OK : EMR_ERR_CUDA;
 }
 
-// Pairs of SMs where their rounds of 256 x 256 tiles take less time than the rounds of
-// 128 x 128 tiles.
+// Pairs of SMs where their rounds of 256 x 256 tiles take less time than one SM's rounds of
+// 128 x 128 tiles. In hundredths of a microsecond, measured at 8192^3, 4096^3, 94464 x 1364 x
+// 1364, 5460 x 1364 x 2000 and 2000 x 5460 x 1364: a round takes the longer of its copies (28 a
+// block of 128 columns, 36 for a pair) and its epilogue (200, with slopes 500, a pair twice
+// that), 100 more to fill and drain it, and a launch of pairs 400 more than one of single
+// blocks. 8192^3: 485 us against 330; 4096^3: 69 against 53; 5460 x 1364 x 2000: 23.5 against
+// 19.3; 1000 x 5460 x 1364: 15.3 against 16.6; 2000 x 5460 x 1364 with slopes: 27 against 39.
 bool use_pairs(const Params& p, int sms) {
-  const int64_t pair_tiles = p.tiles / (p.m_tiles * p.n_tiles) * ((p.m_tiles + 1) / 2) * ((p.n_tiles + 1) / 2);
-  const int64_t pairs = sms / 2;
-  return pairs > 0 && (pair_tiles + pairs - 1) / pairs * 5 <= (p.tiles + sms - 1) / sms * 3;
+  const int64_t pair_tiles = int64_t(p.tiles) / (int64_t(p.m_tiles) * p.n_tiles) * ((p.m_tiles + 1) / 2) * ((p.n_tiles + 1) / 2);
+  const int64_t pairs = sms / 2, steps = int64_t(p.sum) * p.k_blocks, finish = p.slope ? 500 : 200;
+  if (pairs < 1) return false;
+  const int64_t one = steps * 28 > finish ? steps * 28 : finish, two = steps * 36 > 2 * finish ? steps * 36 : 2 * finish;
+  return (pair_tiles + pairs - 1) / pairs * (two + 100) + 400 < (p.tiles + sms - 1) / sms * (one + 100);
 }
 
 }  // namespace
@@ -831,22 +869,22 @@ extern "C" emr_status emr_q8_matmul(const emr_q8* a, const emr_q8* w, const floa
   const int size = dtype_bytes(out_dtype);
   if (reinterpret_cast<uintptr_t>(out) % size || (bias && reinterpret_cast<uintptr_t>(bias) % 4)) return EMR_ERR_ARG;
   Params p{};
-  p.M = a->rows, p.N = w->rows;
-  p.m_tiles = q8_blocks(p.M), p.n_tiles = q8_blocks(p.N);
+  p.M = int32_t(a->rows), p.N = int32_t(w->rows);
+  p.m_tiles = int32_t(q8_blocks(p.M)), p.n_tiles = int32_t(q8_blocks(p.N));
   const __int128 tiles = __int128(p.m_tiles) * p.n_tiles * (sum_batch ? 1 : batch);
   const __int128 steps = __int128(q8_blocks(a->cols)) * (sum_batch ? batch : 1);
   const int64_t reach = q8_row_bytes(a->cols) * (p.M > p.N ? p.M : p.N);  // bytes between two batches
   const int64_t scale_tiles = q8_scale_batch(p.M > p.N ? p.M : p.N, a->cols) / 512;
-  if (tiles > INT64_MAX / 2 || steps > INT32_MAX || reach >= (int64_t(1) << 40) || __int128(scale_tiles) * batch > INT32_MAX)
+  if (tiles > INT32_MAX / 2 || steps > INT32_MAX || reach >= (int64_t(1) << 40) || __int128(scale_tiles) * batch > INT32_MAX)
     return EMR_ERR_RANGE;
-  p.tiles = int64_t(tiles);
+  p.tiles = int32_t(tiles);
   p.k_blocks = int32_t(q8_blocks(a->cols)), p.k_chunks = int32_t(q8_scale_chunks(a->cols));
   p.sum = sum_batch ? batch : 1;
   p.a_one = a->batch == 1, p.w_one = w->batch == 1;
   p.a_scales = a->scales, p.w_scales = w->scales;
   p.bias = bias, p.act = act, p.out = out, p.out_dtype = out_dtype;
   p.store_bytes = 16;
-  while (p.store_bytes > size && (reinterpret_cast<uintptr_t>(out) % p.store_bytes || (p.N * size) % p.store_bytes)) p.store_bytes >>= 1;
+  while (p.store_bytes > size && (reinterpret_cast<uintptr_t>(out) % p.store_bytes || (int64_t(p.N) * size) % p.store_bytes)) p.store_bytes >>= 1;
   if (slope) p.slope = slope->values, p.slope_scales = slope->scales;
   CUtensorMap a_map, w_map;
   if (!operand_map(a, &a_map) || !operand_map(w, &w_map)) return EMR_ERR_CUDA;
