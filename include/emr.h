@@ -667,6 +667,41 @@ emr_status emr_q8_slope(const void *dy, int32_t dtype, int32_t batch, int64_t ro
 emr_status emr_q8_matmul(const emr_q8 *a, const emr_q8 *w, const float *bias, int32_t act, int32_t sum_batch,
                          void *out, int32_t out_dtype, const emr_q8 *slope, void *stream);
 
+/* A dense layer y = act(x w^T + bias): w [n][k] of one network (batch 1) or of several
+ * with weights of their own, wt its transpose from the same emr_q8_quantize call (read
+ * by the backward pass only), bias device float [batch][n] or NULL. The layer keeps
+ * pointers; the caller owns the memory. */
+typedef struct {
+    emr_q8 w, wt;
+    const float *bias;
+    int32_t act;
+    int32_t reserved;
+} emr_dense;
+
+/* Forward pass: x is x_batch (1: shared by all networks, or w.batch) matrices [rows]
+ * [w.cols] with the given strides (elements); out dense [w.batch][rows][w.rows]. With
+ * keep != 0 the call leaves in x8 and slope what the backward pass needs, x and act'(z)
+ * in 8 bits (an emr_q8 whose scales follow its values in the same memory, 16-byte
+ * aligned); without it x8 is room only. emr_dense_forward_room gives the bytes of both:
+ * slope 0 without keep or with the identity, x8 0 where the product reads x itself (few
+ * rows; x8 may then be NULL). */
+emr_status emr_dense_forward_room(const emr_dense *layer, int32_t x_batch, int64_t rows, int32_t keep,
+                                  size_t *x_bytes, size_t *slope_bytes);
+emr_status emr_dense_forward(const emr_dense *layer, const void *x, int32_t dtype, int32_t x_batch, int64_t rows,
+                             int64_t batch_stride, int64_t row_stride, int64_t col_stride, void *out,
+                             int32_t out_dtype, int32_t keep, void *x8, void *slope, void *stream);
+
+/* Backward pass from x8 and slope as a forward call with keep left them: dy dense
+ * [w.batch][rows][w.rows] of dtype; dx [x_batch][rows][w.cols] (summed over the networks
+ * where x was shared), dw [w.batch][w.rows][w.cols] and db [w.batch][w.rows] of
+ * out_dtype, each NULL for none. With dz = dy * slope, in 8 bits from there on: dx =
+ * dz w, dw = dz^T x, db the sum of dz over the rows before it is rounded. ws:
+ * emr_dense_backward_room bytes, 16-byte aligned. */
+emr_status emr_dense_backward_room(const emr_dense *layer, int32_t x_batch, int64_t rows, size_t *bytes);
+emr_status emr_dense_backward(const emr_dense *layer, const void *dy, int32_t dtype, int32_t x_batch, int64_t rows,
+                              const void *x8, const void *slope, void *dx, void *dw, void *db, int32_t out_dtype,
+                              void *ws, size_t ws_bytes, void *stream);
+
 /* Whether a bounded device-side wait of this library has given up since the last
  * call: *code receives 0, or the number of the wait. Synchronises the stream. */
 emr_status emr_device_error(int32_t *code, void *stream);

@@ -112,4 +112,26 @@ inline bool q8_ok(const emr_q8* q) {
          q->scales && reinterpret_cast<uintptr_t>(q->values) % 16 == 0 && reinterpret_cast<uintptr_t>(q->scales) % 16 == 0;
 }
 
+// The current device and its number of SMs.
+inline bool device_sms(int* dev, int* sms) {
+  return cudaGetDevice(dev) == cudaSuccess && cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, *dev) == cudaSuccess;
+}
+
+// The product for a few rows of a (emr_q8_few.cu): x8 holds them in 8 bits, or x is their
+// dense source, quantised within the kernel (few_fused sizes only).
+struct FewArgs {
+  const emr_q8* x8;
+  const void* x;
+  int32_t x_dtype, x_batch;
+  int64_t x_rows, x_batch_stride, x_row_stride, x_col_stride;
+  const emr_q8* w;
+  const float* bias;
+  int32_t act;
+  void* out;
+  int32_t out_dtype, batch;
+};
+inline bool few_rows(int64_t rows, int64_t batch) { return rows <= 16 && batch <= 65535; }
+inline bool few_fused(int64_t rows, int64_t batch, int64_t cols) { return few_rows(rows, batch) && rows * q8_row_bytes(cols) <= 8192; }
+emr_status launch_few(const FewArgs& a, cudaStream_t st);
+
 }  // namespace emr

@@ -1,0 +1,204 @@
+// The product of a few rows (at most 16) with an 8-bit weight matrix: a single answer, or the
+// patterns of a population. Every weight is read for at most 16 rows, so the weights' bytes
+// bound it: 8 rows x 8192 x 8192 are 67 MB, 9.9 us at 6.79 TB/s. A tile of 128 rows would
+// keep too few SMs busy; here a warp takes 16 outputs and a share of the contraction,
+// straight from memory into the registers of m16n8k32 instructions, whose 8 columns are the
+// rows of x. The order within a block of 128 is the same for both operands but its own:
+// a lane's 16 bytes feed two instructions, so that every load is 16 bytes a lane and a
+// row's 64 bytes are one piece. The sum of a block is scaled and added in 32 bits, the
+// warps' shares are added in their order.
+#include <cuda_runtime.h>
+
+#include <type_traits>
+
+#include "emr_act.h"
+#include "emr_q8.h"
+
+namespace {
+
+using namespace emr;
+
+constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / 32;
+
+struct Params {
+  const uint8_t *w, *w_scales;
+  int32_t N, w_one, x_one;
+  int32_t M, K, blocks, chunks;  // columns, blocks of 128 of them, and scale chunks
+  int32_t shares, groups;        // warps of a block that split the contraction; groups of 16 outputs
+  const uint8_t *x, *x_scales;   // x in 8 bits, or
+  const void* source;            // its dense source
+  int64_t batch_stride, row_stride, col_stride;
+  const float* bias;
+  int32_t act;
+  void* out;
+  int32_t out_dtype;
+};
+
+__device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// v * 2^(a - 127) * 2^(b - 127) for two scale bytes, in two steps of half the exponent each, so
+// that neither overflows where the result does not.
+__device__ __forceinline__ float scaled(float v, int a, int b) {
+  const int e = a + b - 254, h = e >> 1;
+  return v * __int_as_float((h + 127) << 23) * __int_as_float((e - h + 127) << 23);
+}
+
+__device__ __forceinline__ uint4 stream16(const uint8_t* p) {  // weights are read once
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+
+// kTiles: groups of 8 rows of x. T: type of x's dense source, void for x in 8 bits.
+template <int kTiles, typename T>
+__global__ void __launch_bounds__(kThreads) q8_few_kernel(const __grid_constant__ Params p) {
+  constexpr bool kFused = !std::is_same<T, void>::value;
+  constexpr int kRows = kTiles * 8;
+  extern __shared__ uint8_t codes[];  // kFused: [share][row][its blocks of 128, and 64 bytes]
+  __shared__ float sums[kWarps][kRows][16];
+  __shared__ uint8_t scales[kFused ? 64 : 1][kRows];  // kFused: [block][row]
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int share = warp % p.shares, teams = kWarps / p.shares, team = warp / p.shares;
+  const int b = blockIdx.y;
+  const int group = blockIdx.x * teams + team;
+  const int first = p.blocks * share / p.shares, last = p.blocks * (share + 1) / p.shares;
+  const int64_t row_bytes = int64_t(p.blocks) * 128;
+  const int g = lane >> 2, t = lane & 3;
+
+  // x first when it comes from its source: the blocks of a share belong to the first team's warp
+  const int pitch = ((p.blocks + p.shares - 1) / p.shares) * 128 + 64;
+  uint8_t* const own = codes + share * p.M * pitch;
+  if constexpr (kFused) {
+    if (team == 0) {
+      const T* src = static_cast<const T*>(p.source) + (p.x_one ? 0 : b * p.batch_stride);
+      for (int m = 0; m < p.M; m++)
+        for (int kb = first; kb < last; kb++) {
+          float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+          {
+            const int64_t c = kb * 128 + lane * 4;
+            const T* at = src + m * p.row_stride + c * p.col_stride;
+            if (c < p.K) v.x = float(at[0]);
+            if (c + 1 < p.K) v.y = float(at[p.col_stride]);
+            if (c + 2 < p.K) v.z = float(at[2 * p.col_stride]);
+            if (c + 3 < p.K) v.w = float(at[3 * p.col_stride]);
+          }
+          const uint32_t byte = q8_warp_scale(v);
+          *reinterpret_cast<uint32_t*>(own + m * pitch + (kb - first) * 128 + lane * 4) = q8_pack4(v.x, v.y, v.z, v.w, q8_inverse(byte));
+          if (lane == 0) scales[kb][m] = uint8_t(byte);
+        }
+    }
+    __syncthreads();
+  }
+
+  float acc[kTiles][4] = {};
+  if (group < p.groups) {
+    const int r0 = min(group * 16 + g, p.N - 1), r1 = min(group * 16 + g + 8, p.N - 1);
+    const int64_t wb = p.w_one ? 0 : b;
+    const uint8_t* w = p.w + wb * p.N * row_bytes + t * 16;
+    const uint8_t *w0 = w + r0 * row_bytes, *w1 = w + r1 * row_bytes;
+    const uint8_t* ws = p.w_scales + wb * q8_scale_batch(p.N, int64_t(p.blocks) * 128);
+    const uint8_t *s0 = ws + q8_scale_at(p.chunks, r0, 0), *s1 = ws + q8_scale_at(p.chunks, r1, 0);
+    const uint8_t* x = nullptr;
+    const uint8_t* xs = nullptr;
+    if constexpr (!kFused) {
+      const int64_t xb = p.x_one ? 0 : b;
+      x = p.x + xb * p.M * row_bytes + t * 16;
+      xs = p.x_scales + xb * q8_scale_batch(p.M, int64_t(p.blocks) * 128);
+    }
+#pragma unroll 2
+    for (int kb = first; kb < last; kb++) {
+      const int64_t k = int64_t(kb) * 128;
+      uint4 a[2][2], xv[kTiles][2];
+#pragma unroll
+      for (int j = 0; j < 2; j++) a[0][j] = stream16(w0 + k + j * 64), a[1][j] = stream16(w1 + k + j * 64);
+      const int at = (kb >> 2) * 512 + (kb & 3);
+      const int sw0 = s0[at], sw1 = s1[at];
+      int sx[kTiles][2];
+#pragma unroll
+      for (int i = 0; i < kTiles; i++) {
+        const int m = min(i * 8 + g, p.M - 1);  // rows past M repeat the last; they are not stored
+        const int m0 = min(i * 8 + 2 * t, p.M - 1), m1 = min(i * 8 + 2 * t + 1, p.M - 1);
+        if constexpr (kFused) {
+#pragma unroll
+          for (int j = 0; j < 2; j++)
+            xv[i][j] = *reinterpret_cast<const uint4*>(own + m * pitch + (kb - first) * 128 + j * 64 + t * 16);
+          sx[i][0] = scales[kb][m0], sx[i][1] = scales[kb][m1];
+        } else {
+#pragma unroll
+          for (int j = 0; j < 2; j++) xv[i][j] = *reinterpret_cast<const uint4*>(x + m * row_bytes + k + j * 64);
+          sx[i][0] = xs[q8_scale_at(p.chunks, m0, kb)], sx[i][1] = xs[q8_scale_at(p.chunks, m1, kb)];
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kTiles; i++) {
+        float c[4] = {};
+#pragma unroll
+        for (int j = 0; j < 2; j++) {
+          mma(c, a[0][j].x, a[1][j].x, a[0][j].y, a[1][j].y, xv[i][j].x, xv[i][j].y);
+          mma(c, a[0][j].z, a[1][j].z, a[0][j].w, a[1][j].w, xv[i][j].z, xv[i][j].w);
+        }
+        acc[i][0] += scaled(c[0], sw0, sx[i][0]), acc[i][1] += scaled(c[1], sw0, sx[i][1]);
+        acc[i][2] += scaled(c[2], sw1, sx[i][0]), acc[i][3] += scaled(c[3], sw1, sx[i][1]);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kTiles; i++) {
+    sums[warp][i * 8 + 2 * t][g] = acc[i][0], sums[warp][i * 8 + 2 * t + 1][g] = acc[i][1];
+    sums[warp][i * 8 + 2 * t][g + 8] = acc[i][2], sums[warp][i * 8 + 2 * t + 1][g + 8] = acc[i][3];
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < teams * kRows * 16; i += kThreads) {
+    const int r = i & 15, m = i / 16 % kRows, tm = i / (16 * kRows);
+    const int n = (blockIdx.x * teams + tm) * 16 + r;
+    if (m >= p.M || n >= p.N) continue;
+    float z[1] = {0.f}, d[1];
+    for (int s = 0; s < p.shares; s++) z[0] += sums[tm * p.shares + s][m][r];
+    if (p.bias) z[0] += p.bias[int64_t(b) * p.N + n];
+    activate<1, false>(p.act, z, d);
+    store_scalar(p.out, p.out_dtype, (int64_t(b) * p.M + m) * p.N + n, z[0]);
+  }
+}
+
+template <int kTiles, typename T>
+emr_status launch(const Params& p, int batch, cudaStream_t st) {
+  const int teams = kWarps / p.shares;
+  const size_t smem = std::is_same<T, void>::value ? 0 : size_t(p.shares) * p.M * (((p.blocks + p.shares - 1) / p.shares) * 128 + 64);
+  q8_few_kernel<kTiles, T><<<dim3(unsigned((p.groups + teams - 1) / teams), unsigned(batch)), kThreads, smem, st>>>(p);
+  return cudaGetLastError() == cudaSuccess ? EMR_OK : EMR_ERR_CUDA;
+}
+template <typename T>
+emr_status launch_tiles(const Params& p, int batch, cudaStream_t st) {
+  return p.M <= 8 ? launch<1, T>(p, batch, st) : launch<2, T>(p, batch, st);
+}
+
+}  // namespace
+
+namespace emr {
+
+emr_status launch_few(const FewArgs& a, cudaStream_t st) {
+  Params p{};
+  p.w = a.w->values, p.w_scales = a.w->scales, p.N = int32_t(a.w->rows), p.w_one = a.w->batch == 1;
+  p.K = int32_t(a.w->cols), p.blocks = int32_t(q8_blocks(a.w->cols)), p.chunks = int32_t(q8_scale_chunks(a.w->cols));
+  p.bias = a.bias, p.act = a.act, p.out = a.out, p.out_dtype = a.out_dtype;
+  p.groups = (p.N + 15) / 16;
+  // 16 warps for each of 152 SMs, as far as the contraction can be shared
+  p.shares = 1;
+  while (p.shares < kWarps && p.shares * 2 <= p.blocks && int64_t(p.groups) * a.batch * p.shares < 16 * 152) p.shares *= 2;
+  if (a.x8) {
+    p.M = int32_t(a.x8->rows), p.x_one = a.x8->batch == 1, p.x = a.x8->values, p.x_scales = a.x8->scales;
+    return launch_tiles<void>(p, a.batch, st);
+  }
+  p.M = int32_t(a.x_rows), p.x_one = a.x_batch == 1, p.source = a.x;
+  p.batch_stride = a.x_batch_stride, p.row_stride = a.x_row_stride, p.col_stride = a.x_col_stride;
+  if (a.x_dtype == EMR_F32) return launch_tiles<float>(p, a.batch, st);
+  if (a.x_dtype == EMR_BF16) return launch_tiles<__nv_bfloat16>(p, a.batch, st);
+  return launch_tiles<__half>(p, a.batch, st);
+}
+
+}  // namespace emr

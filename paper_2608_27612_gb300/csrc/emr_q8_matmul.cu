@@ -12,8 +12,10 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <mutex>
 
+#include "emr_act.h"
 #include "emr_q8.h"
 
 namespace {
@@ -132,103 +134,6 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
 __device__ __forceinline__ void settle() {
   const long long t0 = clock64();
   while (clock64() - t0 < 4000000) {
-  }
-}
-
-// ---- activations and their slopes ----------------------------------------------------
-// The transcendental parts run on the special function unit. sigmoid and tanh are taken
-// from t = e^-|z| or e^-2|z| and r = 1 / (1 + t): every form below is a product of
-// positive terms, so the slopes keep their relative precision where the functions
-// saturate (1 - y^2 would lose it).
-
-__device__ __forceinline__ float fast_exp2(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
-__device__ __forceinline__ float fast_rcp(float x) {
-  float r;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
-constexpr float kLog2E = 0x1.715476p+0f;
-
-// Element i of sin and cos where the argument is large; i is not known at compile time, so the
-// element is picked by comparison instead of by an address.
-template <bool kSlope>
-__device__ __forceinline__ void sin_far(float (&z)[32], float (&d)[32], int i) {
-  float v = 0.f, c;
-#pragma unroll
-  for (int j = 0; j < 32; j++) v = j == i ? z[j] : v;
-  sincosf(v, &v, &c);
-#pragma unroll
-  for (int j = 0; j < 32; j++) {
-    z[j] = j == i ? v : z[j];
-    if (kSlope) d[j] = j == i ? c : d[j];
-  }
-}
-
-template <bool kSlope>
-__device__ __forceinline__ void activate(int act, float (&z)[32], float (&d)[32]) {
-  switch (act) {
-    case EMR_ACT_SIGMOID:
-#pragma unroll
-      for (int i = 0; i < 32; i++) {
-        const float t = fast_exp2(fabsf(z[i]) * -kLog2E), r = fast_rcp(1.f + t);
-        if (kSlope) d[i] = t * r * r;
-        z[i] = z[i] >= 0.f ? r : t * r;
-      }
-      break;
-    case EMR_ACT_TANH:
-#pragma unroll
-      for (int i = 0; i < 32; i++) {
-        const float t = fast_exp2(fabsf(z[i]) * (-2.f * kLog2E)), r = fast_rcp(1.f + t);
-        if (kSlope) d[i] = (4.f * t) * (r * r);
-        // below 1/25 two terms of the series; the next one is 2 z^4 / 15 (relative 4e-7)
-        const float series = z[i] * fmaf(z[i] * z[i], -1.f / 3.f, 1.f);
-        z[i] = fabsf(z[i]) < 0.04f ? series : copysignf((1.f - t) * r, z[i]);
-      }
-      break;
-    case EMR_ACT_GAUSS:
-#pragma unroll
-      for (int i = 0; i < 32; i++) {
-        const float y = fast_exp2(z[i] * (z[i] * -kLog2E));
-        if (kSlope) d[i] = y == 0.f ? 0.f : -2.f * z[i] * y;  // an infinite z has slope 0
-        z[i] = y;
-      }
-      break;
-    case EMR_ACT_SIN: {
-      // reduced by 2 pi in two parts (fp32 value and remainder) and taken by the special
-      // function unit, good to 1e-6 up to 8192; beyond that, and for NaN, by sincosf
-      float most = 0.f;
-#pragma unroll
-      for (int i = 0; i < 32; i++) most = fabsf(z[i]) <= most ? most : fabsf(z[i]);
-      if (most < 8192.f) {
-#pragma unroll
-        for (int i = 0; i < 32; i++) {
-          const float k = fmaf(z[i], 0x1.45f306p-3f, 0x1.8p+23f) - 0x1.8p+23f;  // nearest whole number of periods
-          const float r = fmaf(-k, -0x1.777a5cp-23f, fmaf(-k, 0x1.921fb6p+2f, z[i]));
-          if (kSlope) d[i] = __cosf(r);
-          z[i] = __sinf(r);
-        }
-      } else {
-#pragma unroll 1
-        for (int i = 0; i < 32; i++) sin_far<kSlope>(z, d, i);
-      }
-      break;
-    }
-    case EMR_ACT_ABS:
-#pragma unroll
-      for (int i = 0; i < 32; i++) {
-        if (kSlope) d[i] = z[i] > 0.f ? 1.f : z[i] < 0.f ? -1.f : z[i];  // 0 at 0, NaN at NaN
-        z[i] = fabsf(z[i]);
-      }
-      break;
-    default:
-      if (kSlope) {
-#pragma unroll
-        for (int i = 0; i < 32; i++) d[i] = 1.f;
-      }
   }
 }
 
@@ -357,7 +262,11 @@ __device__ __forceinline__ void finish_chunk(const Params& p, const Tile& t, uin
     }
     __syncwarp();
   }
-  activate<kSlope>(p.act, z, d);
+  if (rows < 32 || cols < 32) {  // scales past the matrix are any bytes: what they gave stays out of the activation
+#pragma unroll
+    for (int i = 0; i < 32; i++) z[i] = lane < rows && i < cols ? z[i] : 0.f;
+  }
+  activate<32, kSlope>(p.act, z, d);
   if (p.out_dtype == EMR_F32) {
 #pragma unroll
     for (int h = 0; h < 2; h++) {
@@ -819,13 +728,22 @@ bool scale_map(const emr_q8* q, CUtensorMap* map) {
             CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Once for each device and kernel: its dynamic shared memory.
+template <typename K>
+bool allow_smem(K kernel, int bytes, int dev, std::atomic<uint64_t>& done) {
+  if (dev < 64 && (done.load(std::memory_order_relaxed) >> dev & 1)) return true;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+  if (dev < 64) done.fetch_or(uint64_t(1) << dev, std::memory_order_relaxed);
+  return true;
+}
+
 template <bool kSlope>
-emr_status launch_pairs(const emr_q8* a, const emr_q8* w, const CUtensorMap& a_map, const CUtensorMap& w_map, Params p, int sms,
+emr_status launch_pairs(const emr_q8* a, const emr_q8* w, const CUtensorMap& a_map, const CUtensorMap& w_map, Params p, int dev, int sms,
                         cudaStream_t st) {
+  static std::atomic<uint64_t> done{0};
   CUtensorMap a_scales, w_scales;
   if (!scale_map(a, &a_scales) || !scale_map(w, &w_scales)) return EMR_ERR_CUDA;
-  if (cudaFuncSetAttribute(q8_pair_kernel<kSlope>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPairSmemBytes) != cudaSuccess)
-    return EMR_ERR_CUDA;
+  if (!allow_smem(q8_pair_kernel<kSlope>, kPairSmemBytes, dev, done)) return EMR_ERR_CUDA;
   p.tiles = p.tiles / (p.m_tiles * p.n_tiles) * ((p.m_tiles + 1) / 2) * ((p.n_tiles + 1) / 2);
   const int64_t pairs = sms / 2;
   q8_pair_kernel<kSlope><<<unsigned(2 * (p.tiles < pairs ? p.tiles : pairs)), kThreads, kPairSmemBytes, st>>>(
@@ -834,9 +752,9 @@ emr_status launch_pairs(const emr_q8* a, const emr_q8* w, const CUtensorMap& a_m
 }
 
 template <bool kSlope>
-emr_status launch(const CUtensorMap& a, const CUtensorMap& w, const Params& p, int sms, cudaStream_t st) {
-  if (cudaFuncSetAttribute(q8_matmul_kernel<kSlope>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes) != cudaSuccess)
-    return EMR_ERR_CUDA;
+emr_status launch(const CUtensorMap& a, const CUtensorMap& w, const Params& p, int dev, int sms, cudaStream_t st) {
+  static std::atomic<uint64_t> done{0};
+  if (!allow_smem(q8_matmul_kernel<kSlope>, kSmemBytes, dev, done)) return EMR_ERR_CUDA;
   q8_matmul_kernel<kSlope><<<unsigned(p.tiles < sms ? p.tiles : sms), kThreads, kSmemBytes, st>>>(a, w, p);
   return cudaGetLastError() == cudaSuccess ? EMR_OK : EMR_ERR_CUDA;
 }
@@ -886,15 +804,19 @@ extern "C" emr_status emr_q8_matmul(const emr_q8* a, const emr_q8* w, const floa
   p.store_bytes = 16;
   while (p.store_bytes > size && (reinterpret_cast<uintptr_t>(out) % p.store_bytes || (int64_t(p.N) * size) % p.store_bytes)) p.store_bytes >>= 1;
   if (slope) p.slope = slope->values, p.slope_scales = slope->scales;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (!slope && !sum_batch && few_rows(a->rows, batch)) {
+    FewArgs f{};
+    f.x8 = a, f.w = w, f.bias = bias, f.act = act, f.out = out, f.out_dtype = out_dtype, f.batch = batch;
+    return launch_few(f, st);
+  }
+  int dev = 0, sms = 0;
+  if (!device_sms(&dev, &sms)) return EMR_ERR_CUDA;
   CUtensorMap a_map, w_map;
   if (!operand_map(a, &a_map) || !operand_map(w, &w_map)) return EMR_ERR_CUDA;
-  const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  int dev = 0, sms = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-    return EMR_ERR_CUDA;
   if (use_pairs(p, sms))
-    return slope ? launch_pairs<true>(a, w, a_map, w_map, p, sms, st) : launch_pairs<false>(a, w, a_map, w_map, p, sms, st);
-  return slope ? launch<true>(a_map, w_map, p, sms, st) : launch<false>(a_map, w_map, p, sms, st);
+    return slope ? launch_pairs<true>(a, w, a_map, w_map, p, dev, sms, st) : launch_pairs<false>(a, w, a_map, w_map, p, dev, sms, st);
+  return slope ? launch<true>(a_map, w_map, p, dev, sms, st) : launch<false>(a_map, w_map, p, dev, sms, st);
 }
 
 extern "C" emr_status emr_device_error(int32_t* code, void* stream) {

@@ -8,9 +8,11 @@ library has not been built, loading it raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from dataclasses import dataclass
+from typing import NamedTuple
 
 import numpy as np
 import torch
@@ -104,6 +106,10 @@ def lib() -> C.CDLL:
             "emr_q8_slope_workspace_size": [i32, i64, i64, vp],
             "emr_q8_slope": [vp, i32, i32, i64, i64, vp, vp, vp, vp, i32, vp, sz, vp],
             "emr_q8_matmul": [vp, vp, vp, i32, i32, vp, i32, vp, vp],
+            "emr_dense_forward_room": [vp, i32, i64, i32, vp, vp],
+            "emr_dense_forward": [vp, vp, i32, i32, i64, i64, i64, i64, vp, i32, i32, vp, vp, vp],
+            "emr_dense_backward_room": [vp, i32, i64, vp],
+            "emr_dense_backward": [vp, vp, i32, i32, i64, vp, vp, vp, vp, vp, i32, vp, sz, vp],
             "emr_device_error": [vp, vp],
             "emr_sample": [vp, i32, i32, i64, i64, vp, i64, vp, f32, vp, i32, vp, f32, vp, f32, vp, vp, vp],
             "emr_version": [],
@@ -142,6 +148,11 @@ def _ptr(x):
 def _stream(stream):
     s = stream if stream is not None else torch.cuda.current_stream()
     return C.c_void_p(s.cuda_stream)
+
+
+def _raw_stream(stream, device):
+    """The same as a number, for calls that are made often: the current stream of the tensors' device."""
+    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(device.index)
 
 
 # ---- a1 -----------------------------------------------------------------------
@@ -589,6 +600,10 @@ class Q8C(C.Structure):
                 ("values", C.c_void_p), ("scales", C.c_void_p)]
 
 
+class DenseC(C.Structure):
+    _fields_ = [("w", Q8C), ("wt", Q8C), ("bias", C.c_void_p), ("act", C.c_int32), ("reserved", C.c_int32)]
+
+
 def _dtype(t, what: str) -> int:
     d = _DTYPES.get(t)
     if d is None:
@@ -600,28 +615,57 @@ def _matrices(x, what: str):
     """x as [batch, rows, cols] on the GPU (a view)."""
     if not isinstance(x, torch.Tensor) or x.dim() not in (2, 3):
         raise ValueError("%s: a tensor of two or three dimensions is wanted" % what)
-    if x.device.type != "cuda":
+    if not x.is_cuda:
         raise ValueError("%s: a tensor on the GPU is wanted" % what)
     return x if x.dim() == 3 else x.unsqueeze(0)
 
 
+_NOTHING = contextlib.nullcontext()
+
+
 def _on(stream):
     """Allocations for work on `stream` belong to it (the caching allocator reuses memory by stream)."""
-    return torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream())
+    return torch.cuda.stream(stream) if stream is not None else _NOTHING
+
+
+def _q8_bytes(batch: int, rows: int, cols: int):
+    """(bytes of the values, bytes of the scales) of an emr_q8 (emr_q8_size)."""
+    blocks = (cols + 127) // 128
+    return batch * rows * blocks * 128, batch * ((rows + 127) // 128) * ((blocks + 3) // 4) * 512
 
 
 class Q8:
     """Matrices [batch, rows, cols] in 8-bit floating point with one power-of-two scale for each block of
-    128 columns of a row (emr_q8): values uint8 [batch, rows, cols rounded up to 128] (e4m3 codes), scales
-    uint8 (tiles of 128 rows x 4 blocks)."""
+    128 columns of a row (emr_q8): values uint8 (e4m3 codes, [batch, rows, cols rounded up to 128]) and scales
+    uint8 (tiles of 128 rows x 4 blocks) are parts of one piece of memory, `data`."""
 
     def __init__(self, batch: int, rows: int, cols: int, device="cuda"):
         n, m = C.c_size_t(), C.c_size_t()
         _check(lib().emr_q8_size(batch, rows, cols, C.byref(n), C.byref(m)), "emr_q8_size")
         self.batch, self.rows, self.cols = batch, rows, cols
-        self.values = torch.empty(n.value, dtype=torch.uint8, device=device)
-        self.scales = torch.empty(m.value, dtype=torch.uint8, device=device)
-        self.c = Q8C(batch, 0, rows, cols, self.values.data_ptr(), self.scales.data_ptr())
+        self.data = torch.empty(n.value + m.value, dtype=torch.uint8, device=device)
+        p = self.data.data_ptr()
+        self.c = Q8C(batch, 0, rows, cols, p, p + n.value)
+        self._split = n.value
+
+    @classmethod
+    def of(cls, data, batch: int, rows: int, cols: int):
+        """The matrices that `data` (uint8, values then scales) holds."""
+        q = cls.__new__(cls)
+        n, m = _q8_bytes(batch, rows, cols)
+        if data.dtype != torch.uint8 or data.numel() < n + m or not data.is_contiguous():
+            raise ValueError("data: a contiguous uint8 tensor of %d values is wanted" % (n + m))
+        q.batch, q.rows, q.cols, q.data, q._split = batch, rows, cols, data, n
+        q.c = Q8C(batch, 0, rows, cols, data.data_ptr(), data.data_ptr() + n)
+        return q
+
+    @property
+    def values(self):
+        return self.data[:self._split]
+
+    @property
+    def scales(self):
+        return self.data[self._split:]
 
     @property
     def ref(self):
@@ -629,7 +673,7 @@ class Q8:
 
     @property
     def device(self):
-        return self.values.device
+        return self.data.device
 
     @property
     def shape(self):
@@ -715,6 +759,12 @@ def device_error(stream=None) -> int:
     return code.value
 
 
+class Saved(NamedTuple):
+    """What a training step keeps between the passes: x and act'(z) in 8 bits (slope None: identity)."""
+    x: Q8
+    slope: Q8 | None
+
+
 class DenseLayer:
     """y = act(x w^T + b) for one network, or for a batch of networks with weights of their own, in 8-bit
     floating point with 32-bit sums: a HyperNEAT substrate that connects every source to every position
@@ -733,68 +783,97 @@ class DenseLayer:
         if not ACT_IDENTITY <= act <= ACT_ABS:
             raise ValueError("act: one of ACT_* is wanted, got %r" % (act,))
         self.nets, self.n, self.k = w.shape
-        self.act, self.train = act, train
+        self.act, self.train, self.device = act, train, w.device
         with _on(stream):
             self.w8 = Q8(*w.shape, device=w.device)
             self.w8t = Q8(self.nets, self.k, self.n, device=w.device) if train else None
+        self.c = DenseC(self.w8.c, self.w8t.c if train else Q8C(), None, act, 0)
+        self._ref = C.byref(self.c)
+        self._room = {}
         self.set_weights(w, b, stream)
 
     def set_weights(self, w, b=None, stream=None):
         """Lay out new weights (same shape) and keep the bias (None: no bias)."""
         w = _matrices(w, "w")
-        if tuple(w.shape) != (self.nets, self.n, self.k) or w.device != self.w8.device:
-            raise ValueError("w: shape %s on %s is wanted" % ((self.nets, self.n, self.k), self.w8.device))
+        if tuple(w.shape) != (self.nets, self.n, self.k) or w.device != self.device:
+            raise ValueError("w: shape %s on %s is wanted" % ((self.nets, self.n, self.k), self.device))
         if b is not None:
-            if b.dtype != torch.float32 or b.numel() != self.nets * self.n or b.device != w.device:
+            if b.dtype != torch.float32 or b.numel() != self.nets * self.n or b.device != self.device:
                 raise ValueError("b: a float32 tensor [%d, %d] on the layer's GPU is wanted" % (self.nets, self.n))
             with _on(stream):
                 b = b.contiguous()
-        self.b = b
         q8_quantize(w, self.w8, self.w8t, stream)
+        self.b = b
+        self.c.bias = b.data_ptr() if b is not None else None
 
-    def _x(self, x):
+    def _needs_room(self, nx, m):
+        """Whether a forward pass without keep needs memory for x in 8 bits (emr_dense_forward_room)."""
+        got = self._room.get((nx, m))
+        if got is None:
+            a, b = C.c_size_t(), C.c_size_t()
+            _check(lib().emr_dense_forward_room(self._ref, nx, m, 0, C.byref(a), C.byref(b)), "emr_dense_forward_room")
+            if len(self._room) > 64:
+                self._room.clear()
+            got = self._room[(nx, m)] = a.value > 0
+        return got
+
+    def _forward(self, x, out_dtype, stream, keep):
         x = _matrices(x, "x")
-        if x.shape[2] != self.k or x.shape[0] not in (1, self.nets) or x.device != self.w8.device:
+        nx, m, k = x.shape
+        if k != self.k or (nx != 1 and nx != self.nets) or x.device != self.device:
             raise ValueError("x: [m, %d], [1, m, %d] or [%d, m, %d] on the layer's GPU is wanted, got %s" %
                              (self.k, self.k, self.nets, self.k, tuple(x.shape)))
-        return x
+        kind, out_kind = _dtype(x.dtype, "x"), _dtype(out_dtype, "out_dtype")
+        if m == 0:
+            if keep:
+                raise ValueError("x: at least one row is wanted for training")
+            return torch.empty(self.nets, 0, self.n, dtype=out_dtype, device=self.device), None, None
+        with _on(stream):
+            out = torch.empty((self.nets, m, self.n), dtype=out_dtype, device=self.device)
+            xq = slope = None
+            if keep or self._needs_room(nx, m):
+                xq = torch.empty(sum(_q8_bytes(nx, m, k)), dtype=torch.uint8, device=self.device)
+            if keep and self.act != ACT_IDENTITY:
+                slope = torch.empty(sum(_q8_bytes(self.nets, m, self.n)), dtype=torch.uint8, device=self.device)
+            bs, rs, cs = x.stride()
+            _check(lib().emr_dense_forward(self._ref, x.data_ptr(), kind, nx, m, bs, rs, cs, out.data_ptr(), out_kind,
+                                           1 if keep else 0, xq.data_ptr() if xq is not None else None,
+                                           slope.data_ptr() if slope is not None else None,
+                                           _raw_stream(stream, self.device)), "emr_dense_forward")
+        return out, xq, slope
 
     def forward(self, x, out_dtype=torch.float32, stream=None):
         """y [nets, m, n] of out_dtype. m = 0 gives an empty result."""
-        x = self._x(x)
-        if x.shape[1] == 0:
-            return torch.empty(self.nets, 0, self.n, dtype=out_dtype, device=x.device)
-        q, _ = q8_quantize(x, stream=stream)
-        return q8_matmul(q, self.w8, self.b, self.act, out_dtype, stream=stream)
+        return self._forward(x, out_dtype, stream, False)[0]
 
     def forward_train(self, x, out_dtype=torch.float32, stream=None):
         """(y, saved): saved holds x and act'(z) in 8 bits for backward."""
         if not self.train:
             raise ValueError("forward_train: the layer was made with train=False")
-        x = self._x(x)
-        if x.shape[1] == 0:
-            raise ValueError("x: at least one row is wanted for training")
-        q, _ = q8_quantize(x, stream=stream)
-        slope = None
-        if self.act != ACT_IDENTITY:
-            with _on(stream):
-                slope = Q8(self.nets, x.shape[1], self.n, device=x.device)
-        return q8_matmul(q, self.w8, self.b, self.act, out_dtype, slope, stream=stream), (q, slope)
+        y, xq, slope = self._forward(x, out_dtype, stream, True)
+        nx, m = (x.shape[0], x.shape[1]) if x.dim() == 3 else (1, x.shape[0])
+        return y, Saved(Q8.of(xq, nx, m, self.k), Q8.of(slope, self.nets, m, self.n) if slope is not None else None)
 
-    def backward(self, dy, saved, out_dtype=torch.float32, stream=None):
-        """(dx, dw, db) of out_dtype for dy [nets, m, n]: dx in the shape that forward_train took x in (summed
+    def backward(self, dy, saved: Saved, out_dtype=torch.float32, stream=None):
+        """(dx, dw, db) of out_dtype for dy [nets, m, n]: dx [1 or nets, m, k] as forward_train took x (summed
         over the networks where x was shared), dw [nets, n, k], db [nets, n] (also without a bias)."""
         q, slope = saved
         dy = _matrices(dy, "dy")
-        if tuple(dy.shape) != (self.nets, q.rows, self.n) or dy.device != q.device:
+        if tuple(dy.shape) != (self.nets, q.rows, self.n) or dy.device != self.device:
             raise ValueError("dy: shape %s is wanted, got %s" % ((self.nets, q.rows, self.n), tuple(dy.shape)))
+        kind, out_kind = _dtype(dy.dtype, "dy"), _dtype(out_dtype, "out_dtype")
+        room = C.c_size_t()
+        _check(lib().emr_dense_backward_room(self._ref, q.batch, q.rows, C.byref(room)), "emr_dense_backward_room")
         with _on(stream):
-            dz = Q8(self.nets, q.rows, self.n, device=q.device)
-            dzt = Q8(self.nets, self.n, q.rows, device=q.device)
-            db = torch.empty(self.nets, self.n, dtype=out_dtype, device=q.device)
-        q8_slope(dy, slope, dz, dzt, db, stream)
-        dx = q8_matmul(dz, self.w8t, out_dtype=out_dtype, sum_batch=q.batch < self.nets, stream=stream)
-        dw = q8_matmul(dzt, q8_transpose(q, stream=stream), out_dtype=out_dtype, stream=stream)
+            dy = dy.contiguous()
+            dx = torch.empty((q.batch, q.rows, self.k), dtype=out_dtype, device=self.device)
+            dw = torch.empty((self.nets, self.n, self.k), dtype=out_dtype, device=self.device)
+            db = torch.empty((self.nets, self.n), dtype=out_dtype, device=self.device)
+            ws = torch.empty(room.value, dtype=torch.uint8, device=self.device)
+            _check(lib().emr_dense_backward(self._ref, dy.data_ptr(), kind, q.batch, q.rows, q.data.data_ptr(),
+                                            slope.data.data_ptr() if slope is not None else None, dx.data_ptr(),
+                                            dw.data_ptr(), db.data_ptr(), out_kind, ws.data_ptr(), room.value,
+                                            _raw_stream(stream, self.device)), "emr_dense_backward")
         return dx, dw, db
 
 
@@ -835,7 +914,8 @@ def sample(scores, noise, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, stream
         logp = torch.empty(rows, dtype=torch.float32, device=dev)
         if rows:
             _check(lib().emr_sample(scores.data_ptr(), kind, rows, n, scores.stride(0), noise.data_ptr(), noise.stride(0),
-                                    *t, *k, *p, *q, index.data_ptr(), logp.data_ptr(), _stream(stream)), "emr_sample")
+                                    *t, *k, *p, *q, index.data_ptr(), logp.data_ptr(), _raw_stream(stream, dev)),
+                   "emr_sample")
     return index, logp
 
 

@@ -141,11 +141,12 @@ def test_product_bias_activation_and_slope(act, m, dtype):
     d = emr.Q8(nets, m, n)
     out = f64(emr.q8_matmul(a, w, b, ACT[act], dtype, slope=d))
     plain = f64(emr.q8_matmul(a, w, b, ACT[act], dtype))
-    assert same(out, plain)                          # keeping the slope changes nothing
+    assert m <= 16 or same(out, plain)               # keeping the slope changes nothing (few rows sum in another order)
     z, mag = OD.product(back(a), back(w), f64(b))
     dz = (k + 3) * 2.0 ** -23 * mag
     y = OD.act(z, act)
-    assert np.all(np.abs(out - y) <= dz + (2e-6 if act not in ("identity", "abs") else 0.0) + ULP[dtype] * np.abs(y) * 1.01 + 2.0 ** -25)
+    for got in (out, plain):
+        assert np.all(np.abs(got - y) <= dz + (2e-6 if act not in ("identity", "abs") else 0.0) + ULP[dtype] * np.abs(y) * 1.01 + 2.0 ** -25)
     s = OD.slope(z, act)
     got = back(d)
     scale = np.repeat(OD.block_scales(s), 128, -1)[..., :n]
@@ -156,6 +157,55 @@ def test_product_bias_activation_and_slope(act, m, dtype):
         return
     # half a step of e4m3: 2^-4 relative, or 2^-10 of twice the scale (near a scale's edge it may double)
     assert np.all(np.abs(got - s) <= near + 2.0 ** -4 * (np.abs(s) + near) + 2.0 ** -9 * scale)
+
+
+@pytest.mark.parametrize("nets,m,n,k,total,slope", [(1, 3100, 2400, 2100, False, False), (3, 3100, 2400, 700, True, False),
+                                                    (2, 1500, 2433, 3000, False, False), (1, 3100, 2400, 5100, False, True)])
+def test_product_of_pairs(nets, m, n, k, total, slope):
+    """Sizes that go to pairs of SMs, with odd numbers of row and column tiles."""
+    a, w = product_case(nets, nets, m, n, k)
+    b = None if total else normal(9, nets, n, spread=0.0)
+    d = emr.Q8(nets, m, n) if slope else None
+    act = emr.ACT_TANH if slope else emr.ACT_IDENTITY
+    out = emr.q8_matmul(a, w, b, act, slope=d, sum_batch=total)
+    assert torch.equal(out, emr.q8_matmul(a, w, b, act, slope=d, sum_batch=total))
+    x, y = emr.q8_dequantize(a, torch.float32).double(), emr.q8_dequantize(w).double()
+    z, mag = x @ y.mT, x.abs() @ y.abs().mT
+    if b is not None:
+        z, mag = z + b.double()[:, None], mag + b.double().abs()[:, None]
+    if total:
+        z, mag, k = z.sum(0, keepdim=True), mag.sum(0, keepdim=True), k * nets
+    bound = (k + 3) * 2.0 ** -23 * mag + (2e-6 if slope else 0)
+    assert bool(((out.double() - (torch.tanh(z) if slope else z)).abs() <= bound).all())
+    if slope:
+        s = OD.slope(z.cpu().numpy(), "tanh")
+        scale = np.repeat(OD.block_scales(s), 128, -1)[..., :n]
+        near = 2 * bound.cpu().numpy()
+        assert np.all(np.abs(back(d) - s) <= near + 2.0 ** -4 * (s + near) + 2.0 ** -9 * scale)
+
+
+@pytest.mark.parametrize("nets,shared", [(1, False), (3, False), (5, True)])
+@pytest.mark.parametrize("m,n,k", [(1, 1, 1), (1, 40, 8192), (3, 333, 129), (4, 340, 256), (8, 70, 1024), (8, 130, 1300),
+                                   (9, 100, 300), (16, 65, 512), (16, 200, 4000)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_layer_of_few_rows(nets, shared, m, n, k, dtype):
+    """x quantised within the product, or before it; any strides of x."""
+    w, b = normal(40, nets, n, k, spread=0.3) / np.sqrt(k), normal(41, nets, n, spread=0.0)
+    x = normal(42, 1 if shared else nets, m, k, dtype=dtype)
+    layer = emr.DenseLayer(w, b, emr.ACT_SIGMOID)
+    y = layer.forward(x)
+    z, mag = OD.product(OD.held(f64(x)), OD.held(f64(w)), f64(b))
+    assert np.all(np.abs(f64(y) - OD.act(z, "sigmoid")) <= (k + 3) * 2.0 ** -23 * mag + 2e-6)
+    assert torch.equal(y, layer.forward(x.transpose(1, 2).contiguous().transpose(1, 2)))
+    assert torch.equal(y, emr.q8_matmul(emr.q8_quantize(x)[0], layer.w8, b, emr.ACT_SIGMOID))
+
+
+def test_product_of_few_rows_with_extreme_scales():
+    x, w = normal(43, 1, 5, 300) * 2.0 ** 100, normal(44, 1, 33, 300) * 2.0 ** -110
+    x[0, 2] *= 2.0 ** -120
+    out = f64(emr.DenseLayer(w).forward(x))
+    z, mag = OD.product(OD.held(f64(x)), OD.held(f64(w)))
+    assert np.all(np.abs(out - z) <= 302 * 2.0 ** -23 * mag + 2.0 ** -149)
 
 
 def test_product_sums_over_the_networks():
@@ -216,7 +266,7 @@ def test_layer_gradients(act, nets, shared, m, n, k):
     dy = normal(13, nets, m, n, spread=0.5)
     layer = emr.DenseLayer(w, b, ACT[act], train=True)
     y, saved = layer.forward_train(x)
-    assert same(f64(y), f64(layer.forward(x)))
+    assert m <= 16 or same(f64(y), f64(layer.forward(x)))
     dx, dw, db = layer.backward(dy, saved)
     xh, wh = OD.held(f64(x)), OD.held(f64(w))
     assert same(back(saved[0]), xh)
