@@ -7,6 +7,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "../../include/emr.h"
 
 namespace emr {
@@ -90,6 +92,7 @@ template <typename T>
 struct Four {
   uint2 u;
   __device__ __forceinline__ void load(const T* p) { u = *reinterpret_cast<const uint2*>(p); }
+  __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<uint2*>(p) = u; }
   __device__ __forceinline__ void set(int j, T v) { reinterpret_cast<T*>(&u)[j] = v; }
   __device__ __forceinline__ float4 floats() const {
     const T* e = reinterpret_cast<const T*>(&u);
@@ -100,6 +103,7 @@ template <>
 struct Four<float> {
   float4 u;
   __device__ __forceinline__ void load(const float* p) { u = *reinterpret_cast<const float4*>(p); }
+  __device__ __forceinline__ void store(float* p) const { *reinterpret_cast<float4*>(p) = u; }
   __device__ __forceinline__ void set(int j, float v) { reinterpret_cast<float*>(&u)[j] = v; }
   __device__ __forceinline__ float4 floats() const { return u; }
 };
@@ -116,6 +120,17 @@ inline bool q8_ok(const emr_q8* q) {
 inline bool device_sms(int* dev, int* sms) {
   return cudaGetDevice(dev) == cudaSuccess && cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, *dev) == cudaSuccess;
 }
+
+// Once for each device and kernel: its dynamic shared memory.
+template <typename K>
+bool allow_smem(K kernel, int bytes, int dev, std::atomic<uint64_t>& done) {
+  if (dev < 64 && (done.load(std::memory_order_relaxed) >> dev & 1)) return true;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+  if (dev < 64) done.fetch_or(uint64_t(1) << dev, std::memory_order_relaxed);
+  return true;
+}
+
+constexpr int kMostSmem = 227 * 1024 - 2048;  // dynamic, beside at most 2 KB of static arrays
 
 // The product for a few rows of a (emr_q8_few.cu): x8 holds them in 8 bits, or x is their
 // dense source, quantised within the kernel (few_fused sizes only).

@@ -12,7 +12,6 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
-#include <atomic>
 #include <mutex>
 
 #include "emr_act.h"
@@ -726,15 +725,6 @@ bool scale_map(const emr_q8* q, CUtensorMap* map) {
   const cuuint32_t box[2] = {128, 1}, ones[2] = {1, 1};
   return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, q->scales, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
             CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-// Once for each device and kernel: its dynamic shared memory.
-template <typename K>
-bool allow_smem(K kernel, int bytes, int dev, std::atomic<uint64_t>& done) {
-  if (dev < 64 && (done.load(std::memory_order_relaxed) >> dev & 1)) return true;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
-  if (dev < 64) done.fetch_or(uint64_t(1) << dev, std::memory_order_relaxed);
-  return true;
 }
 
 template <bool kSlope>
