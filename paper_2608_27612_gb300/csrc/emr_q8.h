@@ -130,7 +130,7 @@ bool allow_smem(K kernel, int bytes, int dev, std::atomic<uint64_t>& done) {
   return true;
 }
 
-constexpr int kMostSmem = 227 * 1024 - 2048;  // dynamic, beside at most 2 KB of static arrays
+constexpr int kMostSmem = 227 * 1024 - 3072;  // dynamic, beside at most 3 KB of static arrays
 
 // The product for a few rows of a (emr_q8_few.cu): x8 holds them in 8 bits, or x is their
 // dense source, quantised within the kernel (few_fused sizes only).

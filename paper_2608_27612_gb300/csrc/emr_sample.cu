@@ -64,22 +64,26 @@ __device__ __forceinline__ float key_score(uint32_t k) {
   return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
 }
 
-struct Best {  // larger key first, then the lower index
-  float key;
-  int32_t at;
+// A draw's best entry, the larger key first, then the lower index; its keys are non-negative
+// floats as integers, one up, so that 0 stands for none.
+struct Drawn {
+  uint32_t key, at;
+  float mass;       // w of what was drawn from
+  uint32_t unsure;  // the largest rough key that might stand before the best
 };
-__device__ __forceinline__ Best better(Best a, Best b) {
-  return b.key > a.key || (b.key == a.key && uint32_t(b.at) < uint32_t(a.at)) ? b : a;
+__device__ __forceinline__ uint32_t draw_key(float k) { return k >= 0.f ? __float_as_uint(k) + 1 : 0; }
+__device__ __forceinline__ float draw_value(uint32_t k) { return k ? __uint_as_float(k - 1) : -1.f; }
+__device__ __forceinline__ void join(Drawn& x, const Drawn& y) {
+  if (y.key > x.key || (y.key == x.key && y.at < x.at)) x.key = y.key, x.at = y.at;
+  x.mass += y.mass;
+  x.unsure = max(x.unsure, y.unsure);
 }
-struct Mass {
-  float sum, unused;
-};
 
-template <typename T>
+template <typename T, int kAhead>
 struct Row {
   cg::cluster_group cluster;
   const Args& a;
-  int tid, threads, lane, warp, warps, rank, blocks, phase;
+  int tid, threads, lane, warp, warps, rank, blocks, phase, turn;
   int64_t lo;       // first entry of this block's slice
   int count, held;  // its entries, and those in shared memory
   const T* global;  // the slice in memory
@@ -87,121 +91,176 @@ struct Row {
   const float* noise;
   uint32_t *counts, *lacks;
   u64 *sums, *list, *sorted;
-  u64* scratch;     // [64]
-  u64* slots;       // [2][kMaxCluster]
-  int* list_size;
+  uint4* scratch;   // [2][32], by turns: a turn's values are read by all before the next but one writes
+  uint4* slots;     // [2][kMaxCluster]
+  u64* found;       // [2]: what one thread found for all
+  int* list_size;   // [3]: of the first, second and third list of the row
+  u64 *coarse;      // [2][64]: w and entries of 64 groups of steps
+  float* rest;      // w of the last step
+  int lists;
+  bool counted;     // a histogram has been made
   float s_max, temperature, min_w, exp2_per;
   bool top_infinite;  // only the entries of +infinity count, as score 0
-  // the draw
-  Best best;
-  float bar, mass;
+  // the draw: a thread's largest and second largest w / noise as computed roughly, and its w
+  float rough, rough_second, mass;
+  int32_t rough_at;
+  u64 bound;        // where the first block knows it: the last entry that stays
 
   __device__ __forceinline__ float value(T v) const {
     const float s = float(v);
     return top_infinite ? (s == INFINITY ? 0.f : -INFINITY) : s;
   }
-  // fn(score, entry of the slice) for every entry of this block, four at a time.
+  // fn(score, entry of the slice) for every entry of this block.
   template <typename Fn>
   __device__ __forceinline__ void each(Fn fn) const {
-    each4([&](const float(&s)[4], int i, int have) {
+    each4([&](const float (&s)[kAhead][4], int i, int have) {
 #pragma unroll
-      for (int j = 0; j < 4; j++)
-        if (j < have) fn(s[j], i + j);
+      for (int u = 0; u < kAhead; u++) {
+        if (u * threads * 4 >= have) break;
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+          if (u * threads * 4 + j < have) fn(s[u][j], i + u * threads * 4 + j);
+      }
     });
   }
+  // fn(scores, i, have) for kAhead groups of four entries at i, i + 4 threads, ..., loaded together;
+  // have: entries of the slice from i on. Past the slice scores are -infinity.
   template <typename Fn>
   __device__ __forceinline__ void each4(Fn fn) const {
-    for (int i = tid * 4; i < count; i += threads * 4) {
-      const int have = count - i < 4 ? count - i : 4;
-      float s[4];
-      if (i < held || (a.vector && have == 4)) {  // held entries end at a multiple of 4 or with the slice
-        Four<T> u;
-        if (i < held) u.load(data + i);
-        else u.load(global + i);
-        const float4 f = u.floats();
-        s[0] = f.x, s[1] = f.y, s[2] = f.z, s[3] = f.w;
-      } else {
+    for (int i = tid * 4; i < count; i += threads * 4 * kAhead) {
+      Four<T> g[kAhead];
 #pragma unroll
-        for (int j = 0; j < 4; j++) s[j] = j < have ? float(global[i + j]) : -INFINITY;
-      }
-      if (top_infinite) {
+      for (int u = 0; u < kAhead; u++) {
+        const int at = i + u * threads * 4;
+        if (at < held) {  // what is held ends at a multiple of four, padded
+          g[u].load(data + at);
+        } else if (a.vector && at + 4 <= count) {
+          g[u].load(global + at);
+        } else {
 #pragma unroll
-        for (int j = 0; j < 4; j++) s[j] = s[j] == INFINITY ? 0.f : -INFINITY;
+          for (int j = 0; j < 4; j++) g[u].set(j, at + j < count ? global[at + j] : T(-INFINITY));
+        }
       }
-      fn(s, i, have);
+      float s[kAhead][4];
+#pragma unroll
+      for (int u = 0; u < kAhead; u++) {
+        const float4 f = g[u].floats();
+        s[u][0] = f.x, s[u][1] = f.y, s[u][2] = f.z, s[u][3] = f.w;
+        if (top_infinite) {
+#pragma unroll
+          for (int j = 0; j < 4; j++) s[u][j] = s[u][j] == INFINITY ? 0.f : -INFINITY;
+        }
+      }
+      fn(s, i, count - i);
     }
   }
   __device__ __forceinline__ float weight(float s) const { return expf(__fdiv_rn(s - s_max, temperature)); }
   __device__ __forceinline__ float rough_weight(float s) const { return fast_exp2((s - s_max) * exp2_per); }
   __device__ __forceinline__ u64 fixed(float w) const { return __float2ull_rn(w * __int_as_float((127 + a.fix) << 23)); }
-  __device__ __forceinline__ float step_at(float s, float per) const { return fminf((s_max - s) * per, float(a.bins - 1)); }
+  // Step of a score, as a number in float: rises as the score falls. Rounded with the 2^23 shift, not
+  // converted: conversions take a quarter of the rate.
+  __device__ __forceinline__ float step_at(float s, float per, float* t) const {
+    *t = fminf((s_max - s) * per, float(a.bins - 1));
+    return fmaxf(*t - 0.5f, 0.f) + 0x1p+23f;
+  }
+  __device__ __forceinline__ int step_of(float s, float per) const {
+    float t;
+    return int(__float_as_uint(step_at(s, per, &t)) & 0x7fffffu);
+  }
 
   __device__ void sync() {
     if (blocks > 1) cluster.sync();
     else __syncthreads();
   }
-  template <typename V>
-  __device__ __forceinline__ static V shfl_xor(V v, int o) {
-    u64 u;
-    memcpy(&u, &v, 8);
-    u = __shfl_xor_sync(0xffffffffu, u, o);
-    memcpy(&v, &u, 8);
-    return v;
-  }
-  // Reduction over the row's threads, in an order of its own; every thread gets the result.
-  template <typename V, typename Op>
-  __device__ V reduce_block(V v, Op op) {
-    static_assert(sizeof(V) == 8, "slots hold 8 bytes");
-#pragma unroll
-    for (int o = 16; o; o >>= 1) v = op(v, shfl_xor(v, o));
-    __syncthreads();
-    V* const part = reinterpret_cast<V*>(scratch);
+  // One barrier for each of these: what a warp finds is combined by every warp again.
+  __device__ uint32_t block_max(uint32_t v) {
+    uint32_t* const part = reinterpret_cast<uint32_t*>(scratch + 32 * (turn ^= 1));
+    v = __reduce_max_sync(0xffffffffu, v);
     if (lane == 0) part[warp] = v;
     __syncthreads();
-    v = part[lane < warps ? lane : 0];
-    for (int o = warps >> 1; o; o >>= 1) v = op(v, shfl_xor(v, o));  // warps is a power of two
-    u64 u;
-    memcpy(&u, &v, 8);
-    u = __shfl_sync(0xffffffffu, u, 0);
-    memcpy(&v, &u, 8);
+    return __reduce_max_sync(0xffffffffu, lane < warps ? part[lane] : 0);
+  }
+  __device__ static float warp_sum(float v) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
   }
-  template <typename V, typename Op>
-  __device__ V reduce(V v, Op op) {
-    v = reduce_block(v, op);
-    if (blocks > 1) {
-      V* const mine = reinterpret_cast<V*>(slots + phase * kMaxCluster);
-      if (tid < blocks) *cluster.map_shared_rank(mine + rank, tid) = v;
-      cluster.sync();
-      v = mine[0];
-      for (int i = 1; i < blocks; i++) v = op(v, mine[i]);
-      phase ^= 1;  // a slot is written again only after the next reduction's barrier
-    }
-    return v;
+  __device__ float block_sum(float v) {
+    float* const part = reinterpret_cast<float*>(scratch + 32 * (turn ^= 1));
+    v = warp_sum(v);
+    if (lane == 0) part[warp] = v;
+    __syncthreads();
+    return warp_sum(lane < warps ? part[lane] : 0.f);
   }
-  // Exclusive sum over the block's threads in order; *total gets the whole sum.
+  __device__ static Drawn warp_best(Drawn d) {
+    const uint32_t key = __reduce_max_sync(0xffffffffu, d.key);
+    d.at = __reduce_min_sync(0xffffffffu, d.key == key ? d.at : 0xffffffffu);
+    d.key = key;
+    d.mass = warp_sum(d.mass);
+    d.unsure = __reduce_max_sync(0xffffffffu, d.unsure);
+    return d;
+  }
+  __device__ Drawn block_best(Drawn d) {
+    Drawn* const part = reinterpret_cast<Drawn*>(scratch + 32 * (turn ^= 1));
+    d = warp_best(d);
+    if (lane == 0) part[warp] = d;
+    __syncthreads();
+    return warp_best(lane < warps ? part[lane] : Drawn{0, 0xffffffffu, 0.f, 0});
+  }
+  // What every block has, to every block of the row: fn(value of block r), in the order of blocks.
+  template <typename V, typename Fn>
+  __device__ void exchange(const V& v, Fn fn) {
+    static_assert(sizeof(V) <= 16, "slots hold 16 bytes");
+    uint4* const mine = slots + phase * kMaxCluster;
+    phase ^= 1;  // a slot is written again only after the next exchange's barrier
+    if (tid < blocks) *reinterpret_cast<V*>(cluster.map_shared_rank(mine + rank, tid)) = v;
+    cluster.sync();
+    for (int i = 0; i < blocks; i++) fn(*reinterpret_cast<const V*>(mine + i));
+  }
+  __device__ u64 row_max(u64 v) {  // of values that all threads of a block share
+    if (blocks == 1) return v;
+    u64 most = 0;
+    exchange(v, [&](u64 x) { most = x > most ? x : most; });
+    return most;
+  }
+  __device__ Drawn row_best(Drawn d) {
+    d = block_best(d);
+    if (blocks == 1) return d;
+    Drawn all{0, 0xffffffffu, 0.f, 0};
+    exchange(d, [&](const Drawn& x) { join(all, x); });
+    return all;
+  }
+  // Exclusive sum over the block's threads in order, of values below 2^62; *total gets the whole sum.
   __device__ u64 scan(u64 v, u64* total) {
+    u64* const part = reinterpret_cast<u64*>(scratch + 32 * (turn ^= 1));
     u64 in = v;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const u64 u = __shfl_up_sync(0xffffffffu, in, o);
       if (lane >= o) in += u;
     }
+    if (lane == 31) part[warp] = in;
     __syncthreads();
-    if (lane == 31) scratch[warp] = in;
-    __syncthreads();
-    u64 part = lane < warps ? scratch[lane] : 0, sum = part;
+    const u64 w = lane < warps ? part[lane] : 0;
+    u64 before = 0, all = 0;  // in pieces of 22 bits, whose sums over 32 lanes fit into 32
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const u64 u = __shfl_up_sync(0xffffffffu, sum, o);
-      if (lane >= o) sum += u;
+    for (int i = 0; i < 3; i++) {
+      const uint32_t piece = uint32_t(w >> (22 * i)) & 0x3fffffu;
+      all += u64(__reduce_add_sync(0xffffffffu, piece)) << (22 * i);
+      before += u64(__reduce_add_sync(0xffffffffu, lane < warp ? piece : 0)) << (22 * i);
     }
-    *total = __shfl_sync(0xffffffffu, sum, 31);
-    return __shfl_sync(0xffffffffu, sum - part, warp) + in - v;
+    *total = all;
+    return before + in - v;
   }
-  // Largest of a value over the block.
-  __device__ u64 block_max(u64 v) {
-    return reduce_block(v, [](u64 x, u64 y) { return x > y ? x : y; });
+  // p times total, rounded up: p in (0, 1) is m 2^-s with 24 bits of m.
+  __device__ static u64 share_of(u64 total, float p) {
+    const uint32_t bits = __float_as_uint(p), e = bits >> 23;
+    const uint32_t m = (bits & 0x7fffffu) | (e ? 0x800000u : 0);
+    const int s = 150 - int(e ? e : 1);  // at least 24
+    const u64 lo = total * m, hi = __umul64hi(total, m);
+    const u64 kept = s >= 128 ? 0 : s >= 64 ? hi >> (s - 64) : (hi << (64 - s)) | (lo >> s);
+    const bool more = s >= 128 ? (hi | lo) != 0 : s >= 64 ? (hi << 1 << (127 - s)) != 0 || lo != 0 : lo << (64 - s) != 0;
+    return kept + more;
   }
 
   __device__ __forceinline__ bool kept(uint32_t key, int64_t at, uint32_t bound_key, int64_t bound_at) const {
@@ -210,33 +269,30 @@ struct Row {
 
   // ---- lists -----------------------------------------------------------------------------
 
-  __device__ void list_clear() {
-    if (tid == 0) *list_size = 0;
-    sync();
-  }
   // One entry to the list of the row's first block (dropped past its room, but counted).
   __device__ __forceinline__ void list_add(uint32_t key, int64_t at) {
-    int* const size = blocks > 1 ? cluster.map_shared_rank(list_size, 0) : list_size;
+    int* const size = blocks > 1 ? cluster.map_shared_rank(list_size + lists, 0) : list_size + lists;
     u64* const to = blocks > 1 ? cluster.map_shared_rank(list, 0) : list;
     const int place = atomicAdd(size, 1);
     if (place < a.cap) to[place] = (u64(key) << 32) | uint32_t(~uint32_t(at));
   }
   __device__ int list_end() {
     sync();
-    const int got = blocks > 1 ? *cluster.map_shared_rank(list_size, 0) : *list_size;
-    sync();  // the size is read before it is set again
+    const int got = blocks > 1 ? *cluster.map_shared_rank(list_size + lists, 0) : list_size[lists];
+    lists++;
     return got;
   }
   // The list's m entries in order, in `sorted` of the row's first block: an entry's place
-  // is the number of larger ones.
+  // is the number of larger ones, counted by a warp.
   __device__ void order(int m) {
     if (rank == 0)
-      for (int j = tid; j < m; j += threads) {
+      for (int j = warp; j < m; j += warps) {
         const u64 e = list[j];
-        int place = 0;
-#pragma unroll 8
-        for (int i = 0; i < m; i++) place += list[i] > e;
-        sorted[place] = e;
+        int larger = 0;
+#pragma unroll 4
+        for (int i = lane; i < m; i += 32) larger += list[i] > e;
+        larger = __reduce_add_sync(0xffffffffu, larger);
+        if (lane == 0) sorted[larger] = e;
       }
     __syncthreads();
   }
@@ -249,46 +305,125 @@ struct Row {
     u64 before;    // entries, or w, before it
     u64 target;
   };
-  // Of `bins` steps, summed over the row (value(b) their entries or w, size(b) their entries): the
-  // last one with entries before which less than the target lies. by_mass with target 0: p
-  // times the whole.
-  template <typename Value, typename Size>
-  __device__ Found locate(bool by_mass, int bins, u64 target, double p, u64 base, Value value, Size size) {
-    const int per = (bins + threads - 1) / threads, b0 = tid * per;
-    u64 mine = 0, total = 0;
-    for (int b = b0; b < b0 + per && b < bins; b++) mine += value(b);
-    u64 before = base + scan(mine, &total);
-    Found f{-1, 0, 0, target};
-    if (by_mass && target == 0) {
-      const double t = ceil(double(total) * p);
-      f.target = t < 1. ? 1 : u64(t);  // one entry stays at least
-    }
-    u64 pick = 0, pick_before = 0, pick_size = 0;  // pick: (bin + 1) of a candidate
-    for (int b = b0; b < b0 + per && b < bins; b++) {
-      const u64 c = size(b);
-      if (c && before < f.target) pick = u64(b) + 1, pick_before = before, pick_size = c;
-      before += value(b);
-    }
-    const u64 last = block_max(pick);  // every block finds the same
-    __syncthreads();
-    if (pick && pick == last) scratch[0] = pick_before, scratch[1] = pick_size;
-    __syncthreads();
-    f.bin = int(last) - 1;
-    f.before = scratch[0];
-    f.size = last ? int64_t(scratch[1]) : 0;
-    sync();  // histograms are read before they are cleared
-    return f;
+  // What a step counts for: its entries, its w from entries and lacks, or its w as summed.
+  enum Kind { kEntries, kLacks, kSums };
+  __device__ __forceinline__ u64 step_value(Kind kind, int b, u64 c, u64 l) const {
+    if (kind == kEntries) return c;
+    if (kind == kSums) return l;
+    if (b == a.bins - 1) return fixed(*rest);  // one block's; see locate
+    return __float2ull_rn(float((c << 20) - l) * expf(float(b) * (-kSpan / float(a.bins - 1))) * __int_as_float((127 + a.fix - 20) << 23));
   }
-  __device__ __forceinline__ u64 over_blocks(const uint32_t* c, int b) const {
-    u64 v = 0;
-    for (int r = 0; r < blocks; r++) v += blocks > 1 ? cluster.map_shared_rank(c, r)[b] : c[b];
-    return v;
+  __device__ __forceinline__ u64 second(Kind kind, int b) const { return kind == kSums ? sums[b] : kind == kLacks ? lacks[b] : 0; }
+  template <typename V>
+  __device__ __forceinline__ const V* of_block(const V* p, int r) const { return cluster.map_shared_rank(p, r); }
+
+  // The last step with entries before which less than the target lies. With several blocks first
+  // among 64 groups of steps, then among the steps of one, so that a thread reads few values of
+  // the other blocks. By w with target 0: p times the whole.
+  __device__ Found locate(Kind kind, int bins, u64 target, float p, u64 base) {
+    const int q = bins > threads ? bins / threads : 1;  // steps of a thread, at most 4
+    const int b0 = tid * q;
+    u64 v = 0, c = 0;
+    if (b0 < bins)
+      for (int j = 0; j < q; j++) {
+        const u64 n = counts[b0 + j];
+        c += n;
+        if (n) v += step_value(kind, b0 + j, n, second(kind, b0 + j));
+      }
+    Found f{-1, 0, base, target};
+    int first = 0, many = bins, each_has = q;
+    if (blocks > 1) {
+      const int team = bins / 64 / q;  // threads of a group: a power of two up to 16
+      u64 gv = v, gc = c;
+      for (int o = team >> 1; o; o >>= 1) gv += __shfl_xor_sync(0xffffffffu, gv, o), gc += __shfl_xor_sync(0xffffffffu, gc, o);
+      if (b0 < bins && tid % team == 0) coarse[tid / team] = gv, coarse[64 + tid / team] = gc;
+      sync();
+      v = c = 0;
+      if (tid < 64) {
+#pragma unroll
+        for (int r = 0; r < kMaxCluster; r++)
+          if (r < blocks) v += of_block(coarse, r)[tid], c += of_block(coarse, r)[64 + tid];
+      }
+      many = 64, each_has = 1;
+    }
+    for (int level = 0;; level++) {
+      u64 total;
+      if (tid == 0) found[0] = ~u64(0);
+      u64 before = f.before + scan(v, &total);
+      if (level == 0 && kind != kEntries && target == 0) {
+        f.target = share_of(total, p);
+        if (f.target == 0) f.target = 1;  // one entry stays at least
+      }
+      // the step, or group, in which the target lies
+      const auto ends_here = [&](u64 from, u64 size, u64 entries, int b) {
+        if (entries && from < f.target && f.target <= from + size) found[0] = from, found[1] = entries, found[2] = u64(b);
+      };
+      if (each_has == 1) {
+        if (tid < many) ends_here(before, v, c, first + tid);
+      } else if (b0 < bins && before < f.target && f.target <= before + v) {
+        for (int j = 0; j < q; j++) {
+          const u64 n = counts[b0 + j], w = n ? step_value(kind, b0 + j, n, second(kind, b0 + j)) : 0;
+          ends_here(before, w, n, b0 + j);
+          before += w;
+        }
+      }
+      __syncthreads();
+      if (found[0] == ~u64(0)) {  // roundings have left the target past the end: the last one with entries
+        int last_b = -1;
+        u64 last_n = 0, last_from = 0;
+        if (each_has == 1) {
+          if (tid < many && c) last_b = first + tid, last_n = c, last_from = before;
+        } else if (b0 < bins) {
+          for (int j = 0; j < q; j++) {
+            const u64 n = counts[b0 + j];
+            if (n) last_b = b0 + j, last_n = n, last_from = before;
+            if (n) before += step_value(kind, b0 + j, n, second(kind, b0 + j));
+          }
+        }
+        const uint32_t b = block_max(uint32_t(last_b + 1));
+        if (b && last_b + 1 == int(b)) found[0] = last_from, found[1] = last_n, found[2] = u64(last_b);
+        __syncthreads();
+      }
+      f.before = found[0], f.size = int64_t(found[1]), f.bin = int(found[2]);
+      __syncthreads();  // read before it is written again
+      if (blocks == 1 || level == 1) return f;
+      // the steps of the group, over the blocks
+      many = bins / 64;
+      first = f.bin * many;
+      v = c = 0;
+      if (tid < many) {
+        const int b = first + tid;
+        u64 l = 0;
+#pragma unroll
+        for (int r = 0; r < kMaxCluster; r++)
+          if (r < blocks) {
+            c += of_block(counts, r)[b];
+            if (kind == kSums) l += of_block(sums, r)[b];
+            if (kind == kLacks) l += of_block(lacks, r)[b];
+          }
+        if (kind == kLacks && b == a.bins - 1) {
+          for (int r = 0; r < blocks; r++) v += fixed(*of_block(rest, r));
+        } else if (c) {
+          v = step_value(kind, b, c, l);
+        }
+      }
+    }
+  }
+  // Before a histogram: the one before it has been read by every block.
+  __device__ void histogram_begin(int bins, bool wide) {
+    if (counted) sync();
+    counted = true;
+    for (int i = tid; i < bins; i += threads) {
+      counts[i] = 0;
+      if (wide) sums[i] = 0;
+      else lacks[i] = 0;
+    }
+    __syncthreads();
   }
   // By steps given by bin(score, key, index), with w in full integers.
   template <typename In, typename Bin>
   __device__ Found find(bool by_mass, int bins, u64 target, In in, Bin bin, u64 base) {
-    for (int i = tid; i < bins; i += threads) counts[i] = 0, sums[i] = 0;
-    __syncthreads();
+    histogram_begin(bins, true);
     each([&](float s, int i) {
       const uint32_t key = order_key(s);
       if (key && in(key, lo + i)) {
@@ -297,49 +432,38 @@ struct Row {
         if (by_mass) atomicAdd(&sums[at], fixed(weight(s)));
       }
     });
-    sync();
-    return locate(by_mass, bins, target, 0., base,
-                  [&](int b) {
-                    if (!by_mass) return over_blocks(counts, b);
-                    u64 v = 0;
-                    for (int r = 0; r < blocks; r++) v += blocks > 1 ? cluster.map_shared_rank(sums, r)[b] : sums[b];
-                    return v;
-                  },
-                  [&](int b) { return over_blocks(counts, b); });
+    __syncthreads();
+    return locate(by_mass ? kSums : kEntries, bins, target, 0.f, base);
   }
   // By equal steps of (s_max - s) / T.
   template <typename In>
-  __device__ Found find_step(bool by_mass, u64 target, double p, float per, In in) {
-    for (int i = tid; i < a.bins; i += threads) counts[i] = 0, lacks[i] = 0;
-    __syncthreads();
+  __device__ Found find_step(bool by_mass, u64 target, float p, float per, In in) {
+    histogram_begin(a.bins, false);
     const float width = kSpan / float(a.bins - 1);
     const int last = a.bins - 1;
-    float rest = 0.f;
+    float below = 0.f;
     each([&](float s, int i) {
       if (!(s > -INFINITY) || !in(s, lo + i)) return;
-      const float t = step_at(s, per);
-      const int at = int(t);
+      float t;
+      const float step = step_at(s, per, &t);
+      const int at = int(__float_as_uint(step) & 0x7fffffu);
       atomicAdd(&counts[at], 1u);
       if (by_mass) {
         if (at == last) {
-          rest += rough_weight(s);
+          below += rough_weight(s);
         } else {  // 1 - e^-x to x^4 / 24 < 3e-7
-          const float x = (t - float(at)) * width;
-          atomicAdd(&lacks[at], uint32_t(x * fmaf(x, fmaf(x, 1.f / 6.f, -0.5f), 1.f) * kLackUnit + 0.5f));
+          const float x = fmaxf(t - (step - 0x1p+23f), 0.f) * width;
+          const float lack = x * fmaf(x, fmaf(x, 1.f / 6.f, -0.5f), 1.f) * kLackUnit + 0x1p+23f;
+          atomicAdd(&lacks[at], __float_as_uint(lack) & 0x7fffffu);
         }
       }
     });
-    if (by_mass) rest = reduce(Mass{rest, 0.f}, [](Mass x, Mass y) { return Mass{x.sum + y.sum, 0.f}; }).sum;
-    sync();
-    return locate(by_mass, a.bins, target, p, 0,
-                  [&](int b) {
-                    const u64 c = over_blocks(counts, b);
-                    if (!by_mass) return c;
-                    if (b == last) return fixed(rest);
-                    const float parts = float((c << 20) - over_blocks(lacks, b));
-                    return __float2ull_rn(parts * expf(float(b) * -width) * __int_as_float((127 + a.fix - 20) << 23));
-                  },
-                  [&](int b) { return over_blocks(counts, b); });
+    if (__syncthreads_or(below > 0.f)) below = block_sum(below);
+    if (by_mass) {
+      if (tid == 0) *rest = below;
+      __syncthreads();
+    }
+    return locate(by_mass ? kLacks : kEntries, a.bins, target, p, 0);
   }
 
   // ---- selection -------------------------------------------------------------------------
@@ -347,7 +471,7 @@ struct Row {
   // Moves the bound (key, index) to the end of the prefix: `k` entries, or, by mass, the entries
   // before which less than p times the kept w lies. With by_mass the entries of the steps
   // before the last are drawn from on the way, and *drawn tells that only the list remains.
-  __device__ void select(bool by_mass, int64_t k, double p, uint32_t& bound_key, int64_t& bound_at, bool* drawn) {
+  __device__ void select(bool by_mass, int64_t k, float p, uint32_t& bound_key, int64_t& bound_at, bool* drawn) {
     const uint32_t bk = bound_key;
     const int64_t ba = bound_at;
     const float bs = bk ? key_score(bk) : -INFINITY;
@@ -358,7 +482,7 @@ struct Row {
     uint32_t prefix = 0;
     int shift = 32;  // key bits from `shift` up are fixed to prefix
     auto in = [&](uint32_t key, int64_t at) {
-      return kept(key, at, bk, ba) && (shift == 32 || (key >> shift) == prefix) && int(step_at(key_score(key), per)) == step;
+      return kept(key, at, bk, ba) && (shift == 32 || (key >> shift) == prefix) && step_of(key_score(key), per) == step;
     };
     u64 before = f.before;
     int64_t size = f.size;
@@ -373,12 +497,11 @@ struct Row {
     }
     if (size <= a.cap) {
       const bool with_draw = by_mass && shift == 32;
-      list_clear();
       if (with_draw) {
         *drawn = true;
         draw4([&](float s, int64_t at) {
           if (!(s > bs || (s == bs && at <= ba))) return false;
-          const int b = int(step_at(s, per));
+          const int b = step_of(s, per);
           if (b == step) list_add(order_key(s), at);
           return b < step;
         });
@@ -396,7 +519,8 @@ struct Row {
           e = sorted[int64_t(target) - int64_t(before) - 1];
         } else {
           // the last entry before which less than the target lies
-          u64 run = before, found = 0;
+          u64 run = before;
+          uint32_t last = 0;
           for (int j0 = 0; j0 < m; j0 += threads) {
             const int j = j0 + tid;
             u64 all;
@@ -404,17 +528,20 @@ struct Row {
             const u64 w = j < m ? fixed(weight(s)) : 0;
             const u64 ahead = run + scan(w, &all);
             if (j < m && ahead < target) {
-              found = u64(j) + 1;
-              if (with_draw) consider(s, int64_t(uint32_t(~uint32_t(sorted[j]))), noise[uint32_t(~uint32_t(sorted[j]))]);
+              last = uint32_t(j) + 1;
+              if (with_draw) consider(true, s, int64_t(uint32_t(~uint32_t(sorted[j]))), noise[uint32_t(~uint32_t(sorted[j]))]);
             }
             run += all;
           }
-          found = block_max(found);
-          e = sorted[found - 1];
+          last = block_max(last);
+          e = sorted[last - 1];
         }
       }
-      if (with_draw) return;  // nothing more asks for the bound
-      e = reduce(e, [](u64 x, u64 y) { return x > y ? x : y; });
+      if (with_draw) {
+        bound = e;
+        return;
+      }
+      e = row_max(e);
       bound_key = uint32_t(e >> 32);
       bound_at = int64_t(uint32_t(~uint32_t(e)));
       return;
@@ -454,10 +581,11 @@ struct Row {
       __syncthreads();
       u64 all;
       const u64 c = tid < 256 ? counts[tid] : 0, ahead = before + scan(c, &all);
-      const u64 pick = block_max(tid < 256 && c && ahead < u64(k) ? (u64(tid) + 1) << 32 | ahead : 0);
       if (before + all < u64(k)) return 1;  // fewer threads than k have an entry
-      prefix = prefix << 8 | (255 - uint32_t((pick >> 32) - 1));
-      before = uint32_t(pick);
+      if (c && ahead < u64(k) && u64(k) <= ahead + c) found[0] = ahead, found[1] = u64(tid);
+      __syncthreads();
+      prefix = prefix << 8 | (255 - uint32_t(found[1]));
+      before = uint32_t(found[0]);
       __syncthreads();
     }
     return prefix << 16;
@@ -465,54 +593,90 @@ struct Row {
 
   // ---- the draw --------------------------------------------------------------------------
 
-  __device__ __forceinline__ void consider(float s, int64_t at, float e) {
-    const float w = rough_weight(s);
-    if (w >= min_w) mass += w;
-    if (w * fast_rcp(e) > bar) {
-      const float exact = weight(s);
-      if (exact >= min_w) {
-        best = better(best, Best{exact > 0.f ? __fdiv_rn(exact, e) : 0.f, int32_t(at)});
-        bar = best.key * (1.f - kNear);
-      }
+  __device__ __forceinline__ void consider(bool stays, float s, int64_t at, float e) {
+    const float w = stays ? rough_weight(s) : 0.f;
+    mass += w >= min_w ? w : 0.f;
+    const float key = stays && w >= min_w * (1.f - kNear) ? w * fast_rcp(e) : -1.f;
+    rough_second = fmaxf(rough_second, fminf(rough, key));
+    const bool first = key > rough;
+    rough = first ? key : rough;
+    rough_at = first ? int32_t(at) : rough_at;
+  }
+  // An entry's key in full; 0 for one that min-p leaves out.
+  __device__ __forceinline__ uint32_t exact(float s, float e) const {
+    const float w = weight(s);
+    return w >= min_w ? draw_key(w > 0.f ? __fdiv_rn(w, e) : 0.f) : 0;
+  }
+  // The thread's candidate in full; unsure where it has another one near or its w is near the least
+  // that stays.
+  __device__ __forceinline__ Drawn candidate(float s) const {
+    Drawn d{0, 0xffffffffu, mass, draw_key(rough_second)};
+    if (rough_at >= 0) {
+      d.key = exact(s, noise[rough_at]);
+      if (d.key) d.at = uint32_t(rough_at);
+      else d.unsure = draw_key(rough);
     }
+    return d;
+  }
+  __device__ __forceinline__ bool sure(const Drawn& d) const {
+    return !d.unsure || draw_value(d.unsure) < draw_value(d.key) * (1.f - kNear);
   }
   // Draws from the entries for which in(score, index) holds.
   template <typename In>
   __device__ __forceinline__ void draw4(In in) {
-    each4([&](const float(&s)[4], int i, int have) {
-      bool stay[4];
-      bool any = false;
+    each4([&](const float(&s)[kAhead][4], int i, int have) {
+      bool stay[kAhead][4];
+      float e[kAhead][4];
 #pragma unroll
-      for (int j = 0; j < 4; j++) {
-        stay[j] = j < have && s[j] > -INFINITY && in(s[j], lo + i + j);
-        any |= stay[j];
+      for (int u = 0; u < kAhead; u++) {
+        const int at = i + u * threads * 4;
+        const bool there = u * threads * 4 < have;
+        bool any = false;
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+          stay[u][j] = there && s[u][j] > -INFINITY && in(s[u][j], lo + at + j);
+          any |= stay[u][j];
+        }
+        if (any && a.noise_vector && u * threads * 4 + 4 <= have) {
+          const float4 f = __ldcs(reinterpret_cast<const float4*>(noise + lo + at));
+          e[u][0] = f.x, e[u][1] = f.y, e[u][2] = f.z, e[u][3] = f.w;
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; j++) e[u][j] = stay[u][j] ? noise[lo + at + j] : 1.f;
+        }
       }
-      if (!any) return;
-      float e[4];
-      if (a.noise_vector && have == 4) {
-        const float4 f = __ldcs(reinterpret_cast<const float4*>(noise + lo + i));
-        e[0] = f.x, e[1] = f.y, e[2] = f.z, e[3] = f.w;
-      } else {
 #pragma unroll
-        for (int j = 0; j < 4; j++) e[j] = stay[j] ? noise[lo + i + j] : 1.f;
+      for (int u = 0; u < kAhead; u++) {
+        if (u * threads * 4 >= have) break;
+#pragma unroll
+        for (int j = 0; j < 4; j++) consider(stay[u][j], s[u][j], lo + i + u * threads * 4 + j, e[u][j]);
       }
-#pragma unroll
-      for (int j = 0; j < 4; j++)
-        if (stay[j]) consider(s[j], lo + i + j, e[j]);
     });
   }
-  __device__ void finish(int32_t* index, float* logp) {
-    const Best top = reduce(best, [](Best x, Best y) { return better(x, y); });
-    const float sum = reduce(Mass{mass, 0.f}, [](Mass x, Mass y) { return Mass{x.sum + y.sum, 0.f}; }).sum;
-    if (top.at < 0) {  // no positive noise among what stays
-      if (rank == 0 && tid == 0) {
-        *index = -1;
-        if (logp) *logp = -INFINITY;
-      }
-    } else if (top.at >= lo && top.at < lo + count && tid == 0) {
-      *index = top.at;
-      if (logp) *logp = __fdiv_rn(value(global[top.at - lo]) - s_max, temperature) - logf(sum);
+  // kept(score, index): what was drawn from.
+  template <typename Kept>
+  __device__ void finish(Kept kept_by, int32_t* index, float* logp) {
+    const float s = rough_at >= 0 ? value(global[rough_at - lo]) : 0.f;  // of the row, not only of the slice
+    Drawn got = row_best(candidate(s));
+    if (!sure(got)) {
+      // two candidates this close: every entry is computed in full (rows of equal scores and
+      // noise; else about one row in 25,000)
+      const u64 e = row_max(bound);
+      Drawn all{0, 0xffffffffu, 0.f, 0};
+      each([&](float v, int i) {
+        const int64_t at = lo + i;
+        if (!(v > -INFINITY) || !kept_by(v, at, e)) return;
+        const uint32_t key = exact(v, noise[at]);
+        if (key > all.key) all.key = key, all.at = uint32_t(at);
+      });
+      const Drawn best = row_best(all);
+      got.key = best.key, got.at = best.at;
     }
+    if (rank == 0 && tid == 0) put(got, got.key ? value(global[got.at - lo]) : 0.f, index, logp);
+  }
+  __device__ void put(const Drawn& d, float s, int32_t* index, float* logp) const {
+    *index = d.key ? int32_t(d.at) : -1;  // none: no positive noise among what stays
+    if (logp) *logp = d.key ? __fdiv_rn(s - s_max, temperature) - logf(d.mass) : -INFINITY;
   }
   // The first k of the list (m entries) hold all that stays: top-p and the draw on them, by the
   // row's first block.
@@ -525,21 +689,11 @@ struct Row {
     const int64_t at = tid < have ? int64_t(uint32_t(~uint32_t(sorted[tid]))) : 0;
     if (p < 1.f) {
       before = scan(tid < have ? fixed(weight(s)) : 0, &total);
-      const double t = ceil(double(total) * double(p));
-      target = t < 1. ? 1 : u64(t);
+      target = p > 0.f ? share_of(total, p) : 1;
     }
-    if (tid < have && before < target) consider(s, at, noise[at]);
-    const Best top = reduce_block(best, [](Best x, Best y) { return better(x, y); });
-    const float sum = reduce_block(Mass{mass, 0.f}, [](Mass x, Mass y) { return Mass{x.sum + y.sum, 0.f}; }).sum;
-    if (top.at < 0) {
-      if (tid == 0) {
-        *index = -1;
-        if (logp) *logp = -INFINITY;
-      }
-    } else if (tid < have && at == top.at) {
-      *index = top.at;
-      if (logp) *logp = __fdiv_rn(s - s_max, temperature) - logf(sum);
-    }
+    if (tid < have && before < target) consider(true, s, at, noise[at]);  // one entry a thread: its candidate is sure
+    const Drawn got = block_best(candidate(s));
+    if (got.key ? tid < have && at == int64_t(got.at) : tid == 0) put(got, s, index, logp);
   }
 };
 
@@ -547,12 +701,17 @@ struct Row {
 template <typename T, int kThreads, bool kFree>
 __global__ void __launch_bounds__(kThreads, 2048 / kThreads > 4 ? 4 : kThreads == 512 ? 2 : 1) sample_kernel(const __grid_constant__ Args a) {
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ u64 scratch[64], slots[2 * kMaxCluster];
-  __shared__ int list_size;
-  Row<T> r{cg::this_cluster(), a};
+  constexpr int kAhead = kThreads == 1024 ? 2 : 4;  // 64 registers a thread
+  __shared__ uint4 scratch[64], slots[2 * kMaxCluster];
+  __shared__ u64 coarse[128], found[3];
+  __shared__ int list_size[3];
+  __shared__ float rest;
+  Row<T, kAhead> r{cg::this_cluster(), a};
   r.tid = threadIdx.x, r.threads = kThreads, r.lane = r.tid & 31, r.warp = r.tid >> 5, r.warps = kThreads / 32;
-  r.rank = int(r.cluster.block_rank()), r.blocks = int(r.cluster.num_blocks()), r.phase = 0;
-  r.scratch = scratch, r.slots = slots, r.list_size = &list_size;
+  r.rank = int(r.cluster.block_rank()), r.blocks = int(r.cluster.num_blocks()), r.phase = r.turn = 0;
+  r.scratch = scratch, r.slots = slots, r.found = found, r.list_size = list_size, r.coarse = coarse, r.rest = &rest;
+  r.lists = 0, r.counted = false;
+  if (threadIdx.x < 3) list_size[threadIdx.x] = 0;
   r.sums = reinterpret_cast<u64*>(smem);  // the first 256 steps; shares its memory with lacks
   r.lacks = reinterpret_cast<uint32_t*>(smem);
   r.counts = r.lacks + a.bins;
@@ -566,7 +725,7 @@ __global__ void __launch_bounds__(kThreads, 2048 / kThreads > 4 ? 4 : kThreads =
   r.global = static_cast<const T*>(a.scores) + row * a.row_stride + r.lo;
   r.noise = a.noise + row * a.noise_stride;
   r.top_infinite = false;
-  r.best = Best{-1.f, -1}, r.bar = -1.f, r.mass = 0.f;
+  r.rough = r.rough_second = -1.f, r.rough_at = -1, r.mass = 0.f, r.bound = 0;
   int32_t* index = a.index + row;
   float* logp = a.logp ? a.logp + row : nullptr;
 
@@ -587,7 +746,7 @@ __global__ void __launch_bounds__(kThreads, 2048 / kThreads > 4 ? 4 : kThreads =
   }
   r.held = r.count < a.room ? r.count : a.room;
   const uint32_t own = order_key(top);
-  const u64 top_key = r.reduce(u64(own), [](u64 x, u64 y) { return x > y ? x : y; });
+  const u64 top_key = r.row_max(r.block_max(own));
   if (top_key == 0) {  // nothing left
     if (r.rank == 0 && r.tid == 0) {
       *index = -1;
@@ -605,60 +764,65 @@ __global__ void __launch_bounds__(kThreads, 2048 / kThreads > 4 ? 4 : kThreads =
   __syncthreads();  // the scores are in shared memory
 
   if (!(r.temperature > 0.f)) {  // the largest score
-    int64_t at = INT64_MAX;
+    uint32_t first = 0;  // counted from the end, so that the lowest index is the largest
     r.each([&](float s, int i) {
-      if (s == r.s_max && r.lo + i < at) at = r.lo + i;
+      if (s == r.s_max) first = max(first, 0xffffffffu - uint32_t(r.lo + i));
     });
-    at = r.reduce(at, [](int64_t x, int64_t y) { return x < y ? x : y; });
+    const u64 at = r.row_max(r.block_max(first));
     if (r.rank == 0 && r.tid == 0) {
-      *index = int32_t(at);
+      *index = int32_t(0xffffffffu - uint32_t(at));
       if (logp) *logp = 0.f;
     }
-    r.sync();
     return;
   }
   if constexpr (kFree) {
     r.draw4([](float, int64_t) { return true; });
-    r.finish(index, logp);
+    r.finish([](float, int64_t, u64) { return true; }, index, logp);
   } else {
     uint32_t bound_key = 0;
     int64_t bound_at = INT64_MAX;
-    bool done = false;
     if (k > 0 && k < a.n) {
       if (k <= kThreads / 4) {
         // the k-th largest of one block's threads bounds the row's from below: the best of the blocks'
-        const u64 least = r.reduce(u64(r.floor_key(r.top_infinite ? (top == INFINITY ? order_key(0.f) : 0) : own, int(k))),
-                                   [](u64 x, u64 y) { return x > y ? x : y; });
+        const u64 least = r.row_max(r.floor_key(r.top_infinite ? (top == INFINITY ? order_key(0.f) : 0) : own, int(k)));
         const float low = least > 1 ? key_score(uint32_t(least)) : -INFINITY;
-        r.list_clear();
-        r.each4([&](const float(&s)[4], int i, int have) {
-          if (!(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])) >= low)) return;
+        r.each4([&](const float(&s)[kAhead][4], int i, int) {
 #pragma unroll
-          for (int j = 0; j < 4; j++)
-            if (j < have && s[j] >= low && s[j] > -INFINITY) r.list_add(order_key(s[j]), r.lo + i + j);
+          for (int u = 0; u < kAhead; u++) {
+            if (!(fmaxf(fmaxf(s[u][0], s[u][1]), fmaxf(s[u][2], s[u][3])) >= low)) continue;
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+              if (s[u][j] >= low && s[u][j] > -INFINITY) r.list_add(order_key(s[u][j]), r.lo + i + u * kThreads * 4 + j);
+          }
         });
         const int m = r.list_end();
-        if (m <= a.cap) r.finish_list(int(k), m, p, index, logp), done = true;
+        if (m <= a.cap) {
+          r.finish_list(int(k), m, p, index, logp);
+          r.sync();  // the list's size was read from the first block
+          return;
+        }
       }
-      if (!done) {
-        // a score is masked or counted: where fewer than k are left all of them stay
-        u64 valid = 0;
-        r.each([&](float s, int) { valid += s > -INFINITY; });
-        valid = r.reduce(valid, [](u64 x, u64 y) { return x + y; });
-        if (u64(k) < valid) r.select(false, k, 0., bound_key, bound_at, nullptr);
-      }
+      // a score is masked or counted: where fewer than k are left all of them stay
+      uint32_t own_valid = 0;
+      r.each([&](float s, int) { own_valid += s > -INFINITY; });
+      u64 valid = 0, block_valid;
+      r.scan(own_valid, &block_valid);
+      if (r.blocks > 1) r.exchange(block_valid, [&](u64 x) { valid += x; });
+      else valid = block_valid;
+      if (u64(k) < valid) r.select(false, k, 0.f, bound_key, bound_at, nullptr);
     }
-    if (!done) {
-      bool drawn = false;
-      if (p < 1.f) r.select(true, 0, double(p), bound_key, bound_at, &drawn);
-      if (!drawn) {
-        const float bs = bound_key ? key_score(bound_key) : -INFINITY;
-        r.draw4([&](float s, int64_t at) { return s > bs || (s == bs && at <= bound_at); });
-      }
-      r.finish(index, logp);
-    }
+    bool drawn = false;
+    if (p < 1.f) r.select(true, 0, fmaxf(p, 0.f), bound_key, bound_at, &drawn);
+    const float bs = bound_key ? key_score(bound_key) : -INFINITY;
+    if (!drawn) r.draw4([&](float s, int64_t at) { return s > bs || (s == bs && at <= bound_at); });
+    r.finish(
+        [&](float s, int64_t at, u64 e) {  // e: the bound that a drawing selection left, 0 for none
+          if (e) return r.kept(order_key(s), at, uint32_t(e >> 32), int64_t(uint32_t(~uint32_t(e))));
+          return s > bs || (s == bs && at <= bound_at);
+        },
+        index, logp);
   }
-  r.sync();  // no block ends while another may still read its memory
+  // After the last exchange of a row no block reads another's memory: any may end first.
 }
 
 template <typename T, int kThreads, bool kFree>
@@ -691,7 +855,7 @@ emr_status plan(Args a, int rows, bool free, int dev, int sms, cudaStream_t st) 
   a.bins = free ? 0 : !wide ? 512 : crowd ? 2048 : 4096;
   a.cap = free ? 0 : !wide ? 512 : crowd ? 1024 : 2048;
   size_t smem = size_t(a.bins) * 8 + size_t(a.cap) * 8;
-  const size_t most = wide && !crowd ? kMostSmem : 112 * 1024;
+  const size_t most = wide && !crowd ? kMostSmem : 110 * 1024;
   const size_t want = size_t(a.slice) * sizeof(T), room = most > smem ? most - smem : 0;
   a.room = int32_t((want < room ? want : room) / sizeof(T) / 4 * 4);
   smem += size_t(a.room) * sizeof(T);
