@@ -35,7 +35,7 @@ extern "C" emr_status emr_dense_forward_room(const emr_dense* layer, int32_t x_b
   if (!x_bytes || !slope_bytes) return EMR_ERR_ARG;
   const emr_status s = check(layer, x_batch, rows);
   if (s != EMR_OK) return s;
-  *x_bytes = !keep && few_fused(rows, layer->w.batch, layer->w.cols) ? 0 : packed_bytes(x_batch, rows, layer->w.cols);
+  *x_bytes = !keep && few_fused(rows, layer->w) ? 0 : packed_bytes(x_batch, rows, layer->w.cols);
   *slope_bytes = keep && layer->act != EMR_ACT_IDENTITY ? packed_bytes(layer->w.batch, rows, layer->w.rows) : 0;
   return EMR_OK;
 }

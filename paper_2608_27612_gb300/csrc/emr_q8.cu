@@ -48,6 +48,8 @@ __device__ __forceinline__ float4 q8_four(const uint8_t* values, const uint8_t* 
 template <typename T, bool kVector>
 __global__ void __launch_bounds__(kThreads) q8_rows_kernel(Dense<T, kVector> src, int64_t rows, int64_t cols, int64_t all_rows,
                                                            emr_q8 q) {
+  grid_wait();
+  grid_go();
   const int64_t row = int64_t(blockIdx.x) * kWarps + (threadIdx.x >> 5);
   if (row >= all_rows) return;
   const int lane = threadIdx.x & 31;
@@ -98,6 +100,8 @@ __global__ void __launch_bounds__(kTileThreads, 2) q8_tile_kernel(Dense<T, kVect
   const uint32_t rest = blockIdx.x / col_tiles;
   const int64_t ct = blockIdx.x - rest * col_tiles, b = rest / row_tiles, rt = rest - uint32_t(b) * row_tiles;
   if (threadIdx.x < 128) tops[0][threadIdx.x] = 0;
+  grid_wait();
+  grid_go();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t chunks = q8_scale_chunks(cols), row_bytes = q8_row_bytes(cols), scale_batch = q8_scale_batch(rows, cols);
   const int64_t c = ct * 128 + lane * 4;
@@ -214,6 +218,8 @@ __global__ void __launch_bounds__(kTileThreads, 2) q8_tile_kernel(Dense<T, kVect
 // Sum of the row tiles' column sums, in the order of the tiles.
 __global__ void __launch_bounds__(kThreads) q8_sums_kernel(const float* sums, int64_t row_tiles, int64_t cols,
                                                            int64_t total, void* db, int dtype) {
+  grid_wait();
+  grid_go();
   const int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x;
   if (i >= total) return;
   const int64_t b = i / cols, n = i - b * cols;
@@ -244,9 +250,8 @@ emr_status launch_tile(const Dense<T, kVector>& src, const emr_q8* other, int64_
   const int64_t tiles = batch * q8_blocks(rows) * q8_blocks(cols);
   if (tiles > kMaxGrid) return EMR_ERR_RANGE;
   const emr_q8 none{};
-  q8_tile_kernel<kMode, T, kVector><<<unsigned(tiles), kTileThreads, 0, st>>>(
-      src, other ? *other : none, rows, cols, q ? *q : none, qt ? *qt : none, sums);
-  return cudaGetLastError() == cudaSuccess ? EMR_OK : EMR_ERR_CUDA;
+  return launch_after(q8_tile_kernel<kMode, T, kVector>, dim3(unsigned(tiles)), kTileThreads, 0, st, src, other ? *other : none, rows,
+                      cols, q ? *q : none, qt ? *qt : none, sums);
 }
 
 template <typename T, bool kVector>
@@ -257,8 +262,7 @@ emr_status launch_rows(const Dense<T, kVector>& src, int64_t batch, int64_t rows
   int64_t pieces = (16 * 152 + grid - 1) / grid;
   if (pieces > chunks) pieces = chunks;
   if (pieces > 65535) pieces = 65535;
-  q8_rows_kernel<T, kVector><<<dim3(unsigned(grid), unsigned(pieces)), kThreads, 0, st>>>(src, rows, cols, all, *q);
-  return cudaGetLastError() == cudaSuccess ? EMR_OK : EMR_ERR_CUDA;
+  return launch_after(q8_rows_kernel<T, kVector>, dim3(unsigned(grid), unsigned(pieces)), kThreads, 0, st, src, rows, cols, all, *q);
 }
 
 struct DenseArgs {
@@ -369,6 +373,5 @@ extern "C" emr_status emr_q8_slope(const void* dy, int32_t dtype, int32_t batch,
   if (e != EMR_OK || !db) return e;
   const int64_t total = int64_t(batch) * cols, grid = (total + kThreads - 1) / kThreads;
   if (grid > kMaxGrid) return EMR_ERR_RANGE;
-  q8_sums_kernel<<<unsigned(grid), kThreads, 0, st>>>(sums, q8_blocks(rows), cols, total, db, db_dtype);
-  return cudaGetLastError() == cudaSuccess ? EMR_OK : EMR_ERR_CUDA;
+  return launch_after(q8_sums_kernel, dim3(unsigned(grid)), kThreads, 0, st, sums, q8_blocks(rows), cols, total, db, db_dtype);
 }

@@ -116,6 +116,26 @@ inline bool q8_ok(const emr_q8* q) {
          q->scales && reinterpret_cast<uintptr_t>(q->values) % 16 == 0 && reinterpret_cast<uintptr_t>(q->scales) % 16 == 0;
 }
 
+// Launches of this library's dense-layer kernels overlap: each begins its set-up while the one
+// before it in the stream ends, waits (grid_wait) before it touches memory, and then lets
+// the next one begin (grid_go).
+__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void grid_go() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+template <typename... P, typename... A>
+emr_status launch_after(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, const A&... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(unsigned(threads));
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, P(args)...) == cudaSuccess ? EMR_OK : EMR_ERR_CUDA;
+}
+
 // The current device and its number of SMs.
 inline bool device_sms(int* dev, int* sms) {
   return cudaGetDevice(dev) == cudaSuccess && cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, *dev) == cudaSuccess;
@@ -132,10 +152,8 @@ bool allow_smem(K kernel, int bytes, int dev, std::atomic<uint64_t>& done) {
 
 constexpr int kMostSmem = 227 * 1024 - 3072;  // dynamic, beside at most 3 KB of static arrays
 
-// The product for a few rows of a (emr_q8_few.cu): x8 holds them in 8 bits, or x is their
-// dense source, quantised within the kernel (few_fused sizes only).
+// The product of a few rows of x, quantised within the kernel (emr_q8_few.cu).
 struct FewArgs {
-  const emr_q8* x8;
   const void* x;
   int32_t x_dtype, x_batch;
   int64_t x_rows, x_batch_stride, x_row_stride, x_col_stride;
@@ -145,8 +163,10 @@ struct FewArgs {
   void* out;
   int32_t out_dtype, batch;
 };
-inline bool few_rows(int64_t rows, int64_t batch) { return rows <= 16 && batch <= 65535; }
-inline bool few_fused(int64_t rows, int64_t batch, int64_t cols) { return few_rows(rows, batch) && rows * q8_row_bytes(cols) <= 8192; }
+inline bool few_fused(int64_t rows, const emr_q8& w) {
+  const int64_t row = q8_row_bytes(w.cols);
+  return rows <= 16 && rows * row <= 8192 && w.batch <= 65535 && double(w.batch) * double(w.rows) * double(row) <= double(1 << 24);
+}
 emr_status launch_few(const FewArgs& a, cudaStream_t st);
 
 }  // namespace emr

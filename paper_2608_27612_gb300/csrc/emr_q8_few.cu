@@ -1,15 +1,14 @@
-// The product of a few rows (at most 16) with an 8-bit weight matrix: a single answer, or the
-// patterns of a population. Every weight is read for at most 16 rows, so the weights' bytes
-// bound it: 8 rows x 8192 x 8192 are 67 MB, 9.9 us at 6.79 TB/s. A tile of 128 rows would
-// keep too few SMs busy; here a warp takes 16 outputs and a share of the contraction,
-// straight from memory into the registers of m16n8k32 instructions, whose 8 columns are the
-// rows of x. The order within a block of 128 is the same for both operands but its own:
-// a lane's 16 bytes feed two instructions, so that every load is 16 bytes a lane and a
-// row's 64 bytes are one piece. The sum of a block is scaled and added in 32 bits, the
-// warps' shares are added in their order.
+// The product of a few rows (at most 16, 8192 values in all) with an 8-bit weight matrix of at
+// most 16 MB in one launch: a single answer, where a launch of its own to quantise x would cost as
+// much as the product. Every block quantises x by itself. A warp takes 16 outputs and a share
+// of the contraction, straight from memory into the registers of m16n8k32 instructions, whose 8
+// columns are the rows of x. The order within a block of 128 is the same for both operands but
+// its own: a lane's 16 bytes feed two instructions, so that every load is 16 bytes a lane and
+// a row's 64 bytes are one piece. The sum of a block is scaled and added in 32 bits, the
+// warps' shares are added in their order. One row, 5460 x 1364: 5.0 us, where quantising and
+// the tensor-memory kernel take 3 + 5.8; it reaches 3.2 TB/s of weights against that kernel's 7,
+// so larger weights go there.
 #include <cuda_runtime.h>
-
-#include <type_traits>
 
 #include "emr_act.h"
 #include "emr_q8.h"
@@ -26,8 +25,7 @@ struct Params {
   int32_t N, w_one, x_one;
   int32_t M, K, blocks, chunks;  // columns, blocks of 128 of them, and scale chunks
   int32_t shares, groups;        // warps of a block that split the contraction; groups of 16 outputs
-  const uint8_t *x, *x_scales;   // x in 8 bits, or
-  const void* source;            // its dense source
+  const void* source;            // x
   int64_t batch_stride, row_stride, col_stride;
   const float* bias;
   int32_t act;
@@ -54,14 +52,13 @@ __device__ __forceinline__ uint4 stream16(const uint8_t* p) {  // weights are re
   return v;
 }
 
-// kTiles: groups of 8 rows of x. T: type of x's dense source, void for x in 8 bits.
+// kTiles: groups of 8 rows of x.
 template <int kTiles, typename T>
 __global__ void __launch_bounds__(kThreads) q8_few_kernel(const __grid_constant__ Params p) {
-  constexpr bool kFused = !std::is_same<T, void>::value;
   constexpr int kRows = kTiles * 8;
-  extern __shared__ uint8_t codes[];  // kFused: [share][row][its blocks of 128, and 64 bytes]
+  extern __shared__ uint8_t codes[];  // [share][row][its blocks of 128, and 64 bytes]
   __shared__ float sums[kWarps][kRows][16];
-  __shared__ uint8_t scales[kFused ? 64 : 1][kRows];  // kFused: [block][row]
+  __shared__ uint8_t scales[64][kRows];  // [block][row]
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int share = warp % p.shares, teams = kWarps / p.shares, team = warp / p.shares;
   const int b = blockIdx.y;
@@ -73,7 +70,9 @@ __global__ void __launch_bounds__(kThreads) q8_few_kernel(const __grid_constant_
   // x first when it comes from its source: the blocks of a share belong to the first team's warp
   const int pitch = ((p.blocks + p.shares - 1) / p.shares) * 128 + 64;
   uint8_t* const own = codes + share * p.M * pitch;
-  if constexpr (kFused) {
+  grid_wait();
+  grid_go();
+  {
     if (team == 0) {
       const T* src = static_cast<const T*>(p.source) + (p.x_one ? 0 : b * p.batch_stride);
       for (int m = 0; m < p.M; m++)
@@ -103,13 +102,6 @@ __global__ void __launch_bounds__(kThreads) q8_few_kernel(const __grid_constant_
     const uint8_t *w0 = w + r0 * row_bytes, *w1 = w + r1 * row_bytes;
     const uint8_t* ws = p.w_scales + wb * q8_scale_batch(p.N, int64_t(p.blocks) * 128);
     const uint8_t *s0 = ws + q8_scale_at(p.chunks, r0, 0), *s1 = ws + q8_scale_at(p.chunks, r1, 0);
-    const uint8_t* x = nullptr;
-    const uint8_t* xs = nullptr;
-    if constexpr (!kFused) {
-      const int64_t xb = p.x_one ? 0 : b;
-      x = p.x + xb * p.M * row_bytes + t * 16;
-      xs = p.x_scales + xb * q8_scale_batch(p.M, int64_t(p.blocks) * 128);
-    }
 #pragma unroll 2
     for (int kb = first; kb < last; kb++) {
       const int64_t k = int64_t(kb) * 128;
@@ -123,16 +115,9 @@ __global__ void __launch_bounds__(kThreads) q8_few_kernel(const __grid_constant_
       for (int i = 0; i < kTiles; i++) {
         const int m = min(i * 8 + g, p.M - 1);  // rows past M repeat the last; they are not stored
         const int m0 = min(i * 8 + 2 * t, p.M - 1), m1 = min(i * 8 + 2 * t + 1, p.M - 1);
-        if constexpr (kFused) {
 #pragma unroll
-          for (int j = 0; j < 2; j++)
-            xv[i][j] = *reinterpret_cast<const uint4*>(own + m * pitch + (kb - first) * 128 + j * 64 + t * 16);
-          sx[i][0] = scales[kb][m0], sx[i][1] = scales[kb][m1];
-        } else {
-#pragma unroll
-          for (int j = 0; j < 2; j++) xv[i][j] = *reinterpret_cast<const uint4*>(x + m * row_bytes + k + j * 64);
-          sx[i][0] = xs[q8_scale_at(p.chunks, m0, kb)], sx[i][1] = xs[q8_scale_at(p.chunks, m1, kb)];
-        }
+        for (int j = 0; j < 2; j++) xv[i][j] = *reinterpret_cast<const uint4*>(own + m * pitch + (kb - first) * 128 + j * 64 + t * 16);
+        sx[i][0] = scales[kb][m0], sx[i][1] = scales[kb][m1];
       }
 #pragma unroll
       for (int i = 0; i < kTiles; i++) {
@@ -168,9 +153,8 @@ __global__ void __launch_bounds__(kThreads) q8_few_kernel(const __grid_constant_
 template <int kTiles, typename T>
 emr_status launch(const Params& p, int batch, cudaStream_t st) {
   const int teams = kWarps / p.shares;
-  const size_t smem = std::is_same<T, void>::value ? 0 : size_t(p.shares) * p.M * (((p.blocks + p.shares - 1) / p.shares) * 128 + 64);
-  q8_few_kernel<kTiles, T><<<dim3(unsigned((p.groups + teams - 1) / teams), unsigned(batch)), kThreads, smem, st>>>(p);
-  return cudaGetLastError() == cudaSuccess ? EMR_OK : EMR_ERR_CUDA;
+  const size_t smem = size_t(p.shares) * p.M * (((p.blocks + p.shares - 1) / p.shares) * 128 + 64);
+  return launch_after(q8_few_kernel<kTiles, T>, dim3(unsigned((p.groups + teams - 1) / teams), unsigned(batch)), kThreads, smem, st, p);
 }
 template <typename T>
 emr_status launch_tiles(const Params& p, int batch, cudaStream_t st) {
@@ -190,10 +174,6 @@ emr_status launch_few(const FewArgs& a, cudaStream_t st) {
   // 16 warps for each of 152 SMs, as far as the contraction can be shared
   p.shares = 1;
   while (p.shares < kWarps && p.shares * 2 <= p.blocks && int64_t(p.groups) * a.batch * p.shares < 16 * 152) p.shares *= 2;
-  if (a.x8) {
-    p.M = int32_t(a.x8->rows), p.x_one = a.x8->batch == 1, p.x = a.x8->values, p.x_scales = a.x8->scales;
-    return launch_tiles<void>(p, a.batch, st);
-  }
   p.M = int32_t(a.x_rows), p.x_one = a.x_batch == 1, p.source = a.x;
   p.batch_stride = a.x_batch_stride, p.row_stride = a.x_row_stride, p.col_stride = a.x_col_stride;
   if (a.x_dtype == EMR_F32) return launch_tiles<float>(p, a.batch, st);

@@ -363,6 +363,8 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
   __syncthreads();
   fence_after();
   const uint32_t tmem = tmem_base;
+  grid_wait();
+  grid_go();
   const int steps = p.sum * p.k_blocks;
 
   if (warp == 0) {
@@ -567,6 +569,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   cluster_sync();
   fence_after();
   const uint32_t tmem = tmem_base;
+  grid_wait();
+  grid_go();
   const int steps = p.sum * p.k_blocks;
   const int stride = gridDim.x / 2, start = blockIdx.x / 2;
   if (warp == 0) {
@@ -685,6 +689,214 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   }
 }
 
+// ---- at most 128 rows ---------------------------------------------------------------
+// With few rows of a the weights' bytes bound the product, and a tile of 128 outputs for
+// each SM leaves most of them without work. Here the operands change places: 128 rows of
+// w are the instruction's rows and the rows of a, 16 to 128 of them, its columns, so a
+// block streams little but weights; two blocks share an SM, and the blocks of a cluster
+// share the contraction of one tile and add their accumulators, through each other's
+// shared memory, in the order of their ranks. A lane of the epilogue has one output of
+// each row, so its stores are neighbours.
+
+constexpr int kThinStages = 4;
+constexpr int kThinThreads = 192;  // copy warp, matrix warp, four epilogue warps
+constexpr int kThinColumns = 256;  // of tensor memory: half of it
+constexpr int kThinMaxSplit = 8;
+
+struct ThinParams {
+  Params p;
+  int32_t wide;   // rows of a, rounded up to 16, 32, 64 or 128
+  int32_t split;  // blocks of a cluster
+};
+__host__ __device__ inline int thin_stage_bytes(int wide) { return kOperandBytes + wide * 128 + kScaleBytes; }
+
+__device__ __forceinline__ void tmem_load16(uint32_t addr, float (&v)[16]) {
+  uint32_t r[16];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(addr));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < 16; i++) v[i] = __uint_as_float(r[i]);
+}
+// The address, in the cluster's window, of block `rank`'s copy of a shared address.
+__device__ __forceinline__ uint32_t at_rank(uint32_t addr, int rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ float4 cluster_load4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+
+__global__ void __launch_bounds__(kThinThreads, 2) q8_thin_kernel(const __grid_constant__ CUtensorMap a_map,
+                                                                  const __grid_constant__ CUtensorMap w_map,
+                                                                  const __grid_constant__ ThinParams q) {
+  extern __shared__ uint8_t raw[];
+  __shared__ uint64_t bars[2 * kThinStages + 4];
+  __shared__ uint32_t tmem_base;
+  __shared__ int gave_up;
+  const Params& p = q.p;
+  uint8_t* const sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+  const int wide_bytes = q.wide * 128;
+  uint8_t* const rows_sm = sm + kThinStages * kOperandBytes;
+  uint8_t* const scales_sm = rows_sm + kThinStages * wide_bytes;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t full = smem_at(bars), empty = full + 8 * kThinStages, acc_full = empty + 8 * kThinStages, acc_empty = acc_full + 16;
+  volatile int* const stop = &gave_up;
+  const int rank = q.split > 1 ? int(cluster_rank()) : 0;
+  const int first = p.k_blocks * rank / q.split, last = p.k_blocks * (rank + 1) / q.split;
+  const int accs = q.wide <= 64 ? 2 : 1;  // accumulators at columns 0 and 64, scales from 128 on (wide 128: from 128)
+
+  if (threadIdx.x == 0) {
+    gave_up = 0;
+    for (int i = 0; i < kThinStages; i++) bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, 1);
+    for (int i = 0; i < 2; i++) bar_init(acc_full + 8 * i, 1), bar_init(acc_empty + 8 * i, 4);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&a_map) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&w_map) : "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&tmem_base)), "n"(kThinColumns)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    fence_before();
+  }
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = tmem_base;
+  grid_wait();
+  grid_go();
+  const int stride = int(gridDim.x) / q.split, start = int(blockIdx.x) / q.split;
+
+  if (warp == 0) {
+    Ring<kThinStages> ring;
+    for (int t = start; t < p.tiles && !*stop; t += stride) {
+      const int b = p.n_tiles == p.tiles ? 0 : t / p.n_tiles, n = t - b * p.n_tiles;
+      const int ab = p.a_one ? 0 : b, wb = p.w_one ? 0 : b;
+      const uint8_t* a_scales = p.a_scales + int64_t(ab) * p.k_chunks * 512;
+      const uint8_t* w_scales = p.w_scales + (int64_t(wb) * p.n_tiles + n) * p.k_chunks * 512;
+      for (int kb = first; kb < last; kb++, ring.next()) {
+        if (!warp_wait(empty + 8 * ring.stage, ring.round ^ 1, stop, 10)) break;
+        if (elect_one()) {
+          const uint32_t bar = full + 8 * ring.stage;
+          const bool scales = kb == first || (kb & 3) == 0;
+          bar_expect(bar, kOperandBytes + wide_bytes + (scales ? kScaleBytes : 0));
+          tma_load(smem_at(sm) + ring.stage * kOperandBytes, &w_map, kb * kTileK, n * kTileN, wb, bar);
+          tma_load(smem_at(rows_sm) + ring.stage * wide_bytes, &a_map, kb * kTileK, 0, ab, bar);
+          if (scales) {
+            const uint32_t at = smem_at(scales_sm) + ring.stage * kScaleBytes;
+            bulk_load(at, w_scales + (kb >> 2) * 512, 512, bar);
+            bulk_load(at + 512, a_scales + (kb >> 2) * 512, 512, bar);
+          }
+        }
+        __syncwarp();
+      }
+    }
+    if (*stop) settle();
+  } else if (warp == 1) {
+    const uint32_t idesc = (1u << 23) | (uint32_t(q.wide >> 3) << 17) | (uint32_t(128 >> 4) << 24);
+    Ring<kThinStages> ring;
+    uint32_t n_tile = 0, chunk = 0;
+    for (int t = start; t < p.tiles && !*stop; t += stride, n_tile++) {
+      const uint32_t acc = accs == 2 ? n_tile & 1 : 0, use = accs == 2 ? n_tile >> 1 : n_tile;
+      if (use >= 1 && !warp_wait(acc_empty + 8 * acc, (use - 1) & 1, stop, 11)) break;
+      fence_after();
+      uint32_t sf = 0;
+      for (int kb = first; kb < last; kb++, ring.next()) {
+        const int s = ring.stage;
+        if (!warp_wait(full + 8 * s, ring.round, stop, 12)) break;
+        fence_after();
+        if (kb == first || (kb & 3) == 0) {
+          sf = tmem + 128 + 8 * (chunk++ & 1);
+          const uint32_t at = smem_at(scales_sm) + s * kScaleBytes;
+          if (elect_one()) {
+            copy_scales(sf, scale_desc(at));
+            copy_scales(sf + 4, scale_desc(at + 512));
+          }
+          __syncwarp();
+        }
+        const uint64_t w = operand_desc(smem_at(sm) + s * kOperandBytes), a = operand_desc(smem_at(rows_sm) + s * wide_bytes);
+        const uint32_t id = idesc | (uint32_t(kb & 3) << 4) | (uint32_t(kb & 3) << 29);
+        if (elect_one()) {
+#pragma unroll
+          for (int j = 0; j < 4; j++) mma_scaled(tmem + acc * 64, w + 2 * j, a + 2 * j, id, sf, sf + 4, kb > first || j > 0);
+          mma_commit(empty + 8 * s);
+        }
+        __syncwarp();
+      }
+      if (elect_one()) mma_commit(acc_full + 8 * acc);
+      __syncwarp();
+    }
+  } else {
+    const int row = (warp & 3) * 32 + lane;  // of the tile's 128 outputs
+    uint32_t n_tile = 0;
+    for (int t = start; t < p.tiles; t += stride, n_tile++) {
+      const int b = p.n_tiles == p.tiles ? 0 : t / p.n_tiles, n = (t - b * p.n_tiles) * kTileN + row;
+      const uint32_t acc = accs == 2 ? n_tile & 1 : 0, use = accs == 2 ? n_tile >> 1 : n_tile;
+      const float bias = q.split == 1 && p.bias && n < p.N ? __ldg(p.bias + int64_t(b) * p.N + n) : 0.f;
+      if (!warp_wait(acc_full + 8 * acc, use & 1, stop, 13)) break;
+      fence_after();
+      const uint32_t addr = tmem + acc * 64 + (uint32_t((warp & 3) * 32) << 16);
+#pragma unroll 1
+      for (int c = 0; c < q.wide; c += 16) {
+        float z[16], d[16];
+        tmem_load16(addr + c, z);
+        if (q.split > 1) {  // this block's share, [row of a][output]; the stages are done with
+          float* const share = reinterpret_cast<float*>(sm);
+#pragma unroll
+          for (int i = 0; i < 16; i++) share[(c + i) * 128 + row] = z[i];
+          continue;
+        }
+        if (n < p.N) {
+#pragma unroll
+          for (int i = 0; i < 16; i++) z[i] = c + i < p.M ? z[i] + bias : 0.f;
+          activate<16, false>(p.act, z, d);
+#pragma unroll
+          for (int i = 0; i < 16; i++)
+            if (c + i < p.M) store_scalar(p.out, p.out_dtype, (int64_t(b) * p.M + c + i) * p.N + n, z[i]);
+        }
+      }
+      fence_before();
+      if (lane == 0) bar_arrive(acc_empty + 8 * acc);
+      __syncwarp();
+    }
+  }
+  __syncwarp();
+  fence_before();
+  __syncthreads();
+  if (q.split > 1) {  // one tile a cluster
+    cluster_sync();
+    const int t = start, b = p.n_tiles == p.tiles ? 0 : t / p.n_tiles, n0 = (t - b * p.n_tiles) * kTileN;
+    const bool fine = !*stop;
+    // four neighbouring outputs of a row at a time, rows shared out over the blocks
+    for (int i = threadIdx.x; i < 32 * ((p.M - rank + q.split - 1) / q.split); i += kThinThreads) {
+      const int m = (i >> 5) * q.split + rank, r = (i & 31) * 4;
+      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int s = 0; s < q.split; s++) {
+        const float4 v = cluster_load4(at_rank(smem_at(sm) + (m * 128 + r) * 4, s));
+        sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
+      }
+      float z[4] = {sum.x, sum.y, sum.z, sum.w}, d[4];
+#pragma unroll
+      for (int j = 0; j < 4; j++) z[j] = n0 + r + j < p.N ? z[j] + (p.bias ? __ldg(p.bias + int64_t(b) * p.N + n0 + r + j) : 0.f) : 0.f;
+      activate<4, false>(p.act, z, d);
+#pragma unroll
+      for (int j = 0; j < 4; j++)
+        if (fine && n0 + r + j < p.N) store_scalar(p.out, p.out_dtype, (int64_t(b) * p.M + m) * p.N + n0 + r + j, z[j]);
+    }
+    cluster_sync();  // no block ends while another reads its share
+  }
+  if (warp == 1) {
+    fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(kThinColumns) : "memory");
+  }
+}
+
 // ---- host ------------------------------------------------------------------------------
 
 typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
@@ -704,14 +916,14 @@ EncodeTiled encode_tiled() {
   return fn;
 }
 
-// Boxes of 128 rows x 128 columns of a q8 matrix; rows past it read as zeros.
-bool operand_map(const emr_q8* q, CUtensorMap* map) {
+// Boxes of `rows` rows x 128 columns of a q8 matrix; rows past it read as zeros.
+bool operand_map(const emr_q8* q, CUtensorMap* map, int rows = 128) {
   const EncodeTiled fn = encode_tiled();
   if (!fn) return false;
   const cuuint64_t row_bytes = cuuint64_t(q8_row_bytes(q->cols));
   const cuuint64_t dims[3] = {row_bytes, cuuint64_t(q->rows), cuuint64_t(q->batch)};
   const cuuint64_t strides[2] = {row_bytes, row_bytes * cuuint64_t(q->rows)};
-  const cuuint32_t box[3] = {128, 128, 1}, ones[3] = {1, 1, 1};
+  const cuuint32_t box[3] = {128, cuuint32_t(rows), 1}, ones[3] = {1, 1, 1};
   return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, q->values, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -736,17 +948,44 @@ emr_status launch_pairs(const emr_q8* a, const emr_q8* w, const CUtensorMap& a_m
   if (!allow_smem(q8_pair_kernel<kSlope>, kPairSmemBytes, dev, done)) return EMR_ERR_CUDA;
   p.tiles = p.tiles / (p.m_tiles * p.n_tiles) * ((p.m_tiles + 1) / 2) * ((p.n_tiles + 1) / 2);
   const int64_t pairs = sms / 2;
-  q8_pair_kernel<kSlope><<<unsigned(2 * (p.tiles < pairs ? p.tiles : pairs)), kThreads, kPairSmemBytes, st>>>(
-      a_map, w_map, a_scales, w_scales, p);
-  return cudaGetLastError() == cudaSuccess ? EMR_OK : EMR_ERR_CUDA;
+  return launch_after(q8_pair_kernel<kSlope>, dim3(unsigned(2 * (p.tiles < pairs ? p.tiles : pairs))), kThreads, kPairSmemBytes, st, a_map,
+                      w_map, a_scales, w_scales, p);
 }
 
 template <bool kSlope>
 emr_status launch(const CUtensorMap& a, const CUtensorMap& w, const Params& p, int dev, int sms, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
   if (!allow_smem(q8_matmul_kernel<kSlope>, kSmemBytes, dev, done)) return EMR_ERR_CUDA;
-  q8_matmul_kernel<kSlope><<<unsigned(p.tiles < sms ? p.tiles : sms), kThreads, kSmemBytes, st>>>(a, w, p);
-  return cudaGetLastError() == cudaSuccess ? EMR_OK : EMR_ERR_CUDA;
+  return launch_after(q8_matmul_kernel<kSlope>, dim3(unsigned(p.tiles < sms ? p.tiles : sms)), kThreads, kSmemBytes, st, a, w, p);
+}
+
+emr_status launch_thin(const emr_q8* a, const emr_q8* w, const Params& p, int dev, int sms, cudaStream_t st) {
+  static std::atomic<uint64_t> done{0};
+  ThinParams q{};
+  q.p = p;
+  q.wide = p.M <= 16 ? 16 : p.M <= 32 ? 32 : p.M <= 64 ? 64 : 128;
+  // As many blocks to a tile as find room, with two blocks of columns for each.
+  q.split = 1;
+  const int64_t room = q.wide <= 64 ? 2 * sms : sms;  // 100 KB a block up to 64 rows
+  while (q.split < kThinMaxSplit && int64_t(p.tiles) * q.split * 2 <= room && p.k_blocks >= 4 * q.split) q.split *= 2;
+  CUtensorMap a_map, w_map;
+  if (!operand_map(a, &a_map, q.wide) || !operand_map(w, &w_map)) return EMR_ERR_CUDA;
+  const int smem = 1024 + kThinStages * thin_stage_bytes(q.wide);  // the shares, wide rows of 512 bytes, fit in w's stages
+  if (!allow_smem(q8_thin_kernel, 1024 + kThinStages * thin_stage_bytes(128), dev, done)) return EMR_ERR_CUDA;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(unsigned(q.split > 1 ? p.tiles * q.split : p.tiles < room ? p.tiles : room));
+  cfg.blockDim = dim3(kThinThreads);
+  cfg.dynamicSmemBytes = size_t(smem);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2]{};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = unsigned(q.split);
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = q.split > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, q8_thin_kernel, a_map, w_map, q) == cudaSuccess ? EMR_OK : EMR_ERR_CUDA;
 }
 
 // Pairs of SMs where their rounds of 256 x 256 tiles take less time than one SM's rounds of
@@ -795,13 +1034,9 @@ extern "C" emr_status emr_q8_matmul(const emr_q8* a, const emr_q8* w, const floa
   while (p.store_bytes > size && (reinterpret_cast<uintptr_t>(out) % p.store_bytes || (int64_t(p.N) * size) % p.store_bytes)) p.store_bytes >>= 1;
   if (slope) p.slope = slope->values, p.slope_scales = slope->scales;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (!slope && !sum_batch && few_rows(a->rows, batch)) {
-    FewArgs f{};
-    f.x8 = a, f.w = w, f.bias = bias, f.act = act, f.out = out, f.out_dtype = out_dtype, f.batch = batch;
-    return launch_few(f, st);
-  }
   int dev = 0, sms = 0;
   if (!device_sms(&dev, &sms)) return EMR_ERR_CUDA;
+  if (!slope && !sum_batch && p.M <= 128) return launch_thin(a, w, p, dev, sms, st);
   CUtensorMap a_map, w_map;
   if (!operand_map(a, &a_map) || !operand_map(w, &w_map)) return EMR_ERR_CUDA;
   if (use_pairs(p, sms))
