@@ -16,6 +16,9 @@ using namespace emr;
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kTileThreads = 512;
+// Tiles from which row blocks alone are worked on by tiles too: 8192 x 8192 bfloat16 58 -> 53 us,
+// 94464 x 1364 114 -> 95; with fewer than two tiles an SM the row kernel keeps more SMs busy.
+constexpr int64_t kTiledFrom = 304;
 
 // Dense source: four columns c .. c + 3 of a row, zero past the matrix. kVector: columns
 // are neighbours and every row is aligned to four elements.
@@ -83,135 +86,186 @@ __global__ void __launch_bounds__(kThreads) q8_rows_kernel(Dense<T, kVector> src
   }
 }
 
-// One 128 x 128 tile: row blocks to q, column blocks (the transpose) to qt, column
-// sums to sums[b][row tile][cols]. Mode 0: a dense source; 1: the values of an 8-bit
-// matrix; 2: the product of a dense matrix and an 8-bit one. A warp holds the rows
-// 8 warp .. 8 warp + 7 in registers, a lane four columns of each. Column maxima and
-// sums meet in shared memory over the 16 warps (the sums in their order); codes of four rows are one word of the
-// transposed byte tile, at (row / 4) ^ (column / 4 % 32) of its column, so that neither
-// the stores (lanes: columns 4 apart) nor the loads (lanes: one column) have conflicts.
+// 8 or 16 bytes from memory into shared memory, past `have` bytes zeros.
+template <int kBytes>
+__device__ __forceinline__ void copy_ahead(void* to, const void* from, int have) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(uint32_t(__cvta_generic_to_shared(to))), "l"(from), "n"(kBytes),
+               "r"(have)
+               : "memory");
+}
+
+// 128 x 128 tiles: row blocks to q, column blocks (the transpose) to qt, column sums to
+// sums[b][row tile][cols]. Mode 0: a dense source; 1: the values of an 8-bit matrix; 2: the
+// product of a dense matrix and an 8-bit one. A block goes through tiles gridDim.x apart
+// and copies the next one into shared memory while it works on one; of the dense source a
+// thread reads back only what it copied itself. A warp holds the rows 8 warp .. 8 warp + 7 in registers, a
+// lane four columns of each. Column maxima and sums meet in shared memory over the 16
+// warps (the sums in their order); codes of four rows are one word of the transposed byte
+// tile, at (row / 4) ^ (column / 4 % 32) of its column, so that neither the stores (lanes:
+// columns 4 apart) nor the loads (lanes: one column) have conflicts.
 template <int kMode, typename T, bool kVector>
 __global__ void __launch_bounds__(kTileThreads, 2) q8_tile_kernel(Dense<T, kVector> src, emr_q8 other, int64_t rows, int64_t cols,
-                                                                  emr_q8 q, emr_q8 qt, float* sums) {
+                                                                  uint32_t tiles, emr_q8 q, emr_q8 qt, float* sums) {
+  extern __shared__ __align__(16) uint8_t ahead[];  // [8][threads] of the dense source, then two tiles of codes
   __shared__ float4 part[16][32];
   __shared__ uint32_t bytes[128 * 32];
-  __shared__ uint32_t tops[4][32];  // [j][lane]: largest magnitude of column 4 lane + j
+  __shared__ uint32_t tops[2][4][32];  // by turns: [j][lane], largest magnitude of column 4 lane + j
   const uint32_t row_tiles = uint32_t(q8_blocks(rows)), col_tiles = uint32_t(q8_blocks(cols));
-  const uint32_t rest = blockIdx.x / col_tiles;
-  const int64_t ct = blockIdx.x - rest * col_tiles, b = rest / row_tiles, rt = rest - uint32_t(b) * row_tiles;
-  if (threadIdx.x < 128) tops[0][threadIdx.x] = 0;
-  grid_wait();
-  grid_go();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, first = warp * 8;
   const int64_t chunks = q8_scale_chunks(cols), row_bytes = q8_row_bytes(cols), scale_batch = q8_scale_batch(rows, cols);
-  const int64_t c = ct * 128 + lane * 4;
-  const int64_t left = rows - rt * 128;
-  const int wide = int(cols - ct * 128 < 128 ? cols - ct * 128 : 128);
-  const int first = warp * 8;
-  const int have = int(left < 128 ? left : 128) - first;  // rows of this warp, may be below 1
-  const T* from = kMode != 1 ? src.p + b * src.batch_stride + (rt * 128 + first) * src.row_stride : nullptr;
-  const int64_t at = (b * rows + rt * 128 + first) * row_bytes + c;  // of the warp's first row in 8-bit matrices of this shape
-  float4 v[8];
-  {
-    Four<T> u[8];
-    uint32_t code[8];
-    uint32_t scale_bytes = 127;
-    if (kMode != 0 && lane < 8 && lane < have)
-      scale_bytes = other.scales[b * scale_batch + q8_scale_at(chunks, rt * 128 + first + lane, ct)];
+  const int64_t t_row_bytes = q8_row_bytes(rows), t_chunks = q8_scale_chunks(rows), t_scale_batch = q8_scale_batch(cols, rows);
+  Four<T>* const dense = reinterpret_cast<Four<T>*>(ahead) + threadIdx.x;
+  uint8_t* const codes = ahead + (kMode != 1 ? sizeof(Four<T>) * 8 * kTileThreads : 0);
+
+  struct Place {
+    int64_t b, rt, ct;
+    int have, wide;  // rows of this warp (may be below 1) and columns of the tile
+  };
+  const auto place = [&](uint32_t t) {
+    Place p;
+    const uint32_t rest = t / col_tiles;
+    p.ct = t - rest * col_tiles;
+    const uint32_t b = rest / row_tiles;
+    p.b = b, p.rt = rest - b * row_tiles;
+    const int64_t left = rows - p.rt * 128, right = cols - p.ct * 128;
+    p.have = int(left < 128 ? left : 128) - first;
+    p.wide = int(right < 128 ? right : 128);
+    return p;
+  };
+  uint32_t next_scale = 127;
+  const auto copy = [&](uint32_t t, uint32_t turn) {
+    const Place p = place(t);
+    const int64_t c = p.ct * 128 + lane * 4;
+    if (kMode != 1) {
+      const int n = p.wide - lane * 4, cells = n < 0 ? 0 : n < 4 ? n : 4;
+      const T* from = src.p + p.b * src.batch_stride + (p.rt * 128 + first) * src.row_stride;
 #pragma unroll
-    for (int i = 0; i < 8; i++)
-      if (i < have) {
-        if (kMode != 1) u[i] = src.four(from + i * src.row_stride, c, cols);
-        if (kMode != 0) code[i] = *reinterpret_cast<const uint32_t*>(other.values + at + i * row_bytes);
-      }
+      for (int i = 0; i < 8; i++) {
+        if constexpr (kVector) {
+          const bool in = i < p.have && cells > 0;
+          copy_ahead<int(sizeof(Four<T>))>(dense + i * kTileThreads, in ? from + i * src.row_stride + c : src.p, in ? cells * int(sizeof(T)) : 0);
+        } else {
+          Four<T> u;
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
-      v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (i < have) {
-        if (kMode != 1) v[i] = u[i].floats();
-        if (kMode != 0) {
-          const float s = q8_scale(__shfl_sync(0xffffffffu, scale_bytes, i));
-          float4 d = q8_unpack4(code[i]);
-          d = make_float4(d.x * s, d.y * s, d.z * s, d.w * s);
-          // one rounding each, so that the values are those of the plain product
-          v[i] = kMode == 1 ? d : make_float4(__fmul_rn(v[i].x, d.x), __fmul_rn(v[i].y, d.y), __fmul_rn(v[i].z, d.z), __fmul_rn(v[i].w, d.w));
+          for (int j = 0; j < 4; j++) u.set(j, i < p.have && j < cells ? from[i * src.row_stride + (c + j) * src.col_stride] : T(0.f));
+          dense[i * kTileThreads] = u;
         }
       }
     }
-  }
-  if (sums) {
-    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (kMode != 0) {
+      // 16 bytes a thread, to be read by other threads
+      const uint8_t* from = other.values + (p.b * rows + p.rt * 128) * row_bytes + p.ct * 128;
 #pragma unroll
-    for (int i = 0; i < 8; i++) s.x += v[i].x, s.y += v[i].y, s.z += v[i].z, s.w += v[i].w;
-    part[warp][lane] = s;
-    __syncthreads();
-    if (threadIdx.x < wide) {
-      float t = 0.f;
-#pragma unroll
-      for (int i = 0; i < 16; i++) t += reinterpret_cast<const float*>(part[i])[threadIdx.x];
-      sums[(b * row_tiles + rt) * cols + ct * 128 + threadIdx.x] = t;
-    }
-    __syncthreads();
-  }
-  if (q.values) {
-    uint8_t* out = q.values + at;
-    uint32_t mine = 0;
-#pragma unroll
-    for (int i = 0; i < 8; i++)
-      if (i < have) {
-        const uint32_t byte = q8_warp_scale(v[i]);
-        *reinterpret_cast<uint32_t*>(out + i * row_bytes) = q8_pack4(v[i].x, v[i].y, v[i].z, v[i].w, q8_inverse(byte));
-        if (lane == i) mine = byte;
+      for (int i = 0; i < 2; i++) {
+        const int r = (threadIdx.x >> 3) + i * 64, at = (threadIdx.x & 7) * 16;
+        const bool in = r < p.have + first;
+        copy_ahead<16>(codes + turn * 16384 + r * 128 + at, in ? from + r * row_bytes + at : other.values, in ? 16 : 0);
       }
-    if (lane < 8 && lane < have) q.scales[b * scale_batch + q8_scale_at(chunks, rt * 128 + first + lane, ct)] = uint8_t(mine);
-  }
-  if (!qt.values) return;
-  if (!sums) __syncthreads();  // tops are cleared
-  float4 top = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-  for (int i = 0; i < 8; i++)
-    top = make_float4(fmaxf(top.x, fabsf(v[i].x)), fmaxf(top.y, fabsf(v[i].y)), fmaxf(top.z, fabsf(v[i].z)), fmaxf(top.w, fabsf(v[i].w)));
-  // NaN is passed over by the maxima; where an infinity is, the finite magnitudes are taken again
-  const float most = q8_top4(top);
-  if (most == INFINITY) {
-    uint32_t m[4] = {};
+      next_scale = 127;
+      if (lane < 8 && lane < p.have) next_scale = other.scales[p.b * scale_batch + q8_scale_at(chunks, p.rt * 128 + first + lane, p.ct)];
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+
+  if (threadIdx.x < 256) (&tops[0][0][0])[threadIdx.x] = 0;
+  grid_wait();
+  grid_go();
+  copy(blockIdx.x, 0);
+  __syncthreads();
+  uint32_t turn = 0;
+  for (uint32_t t = blockIdx.x; t < tiles; t += gridDim.x, turn ^= 1) {
+    const Place p = place(t);
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    if (kMode != 0) __syncthreads();
+    float4 v[8];
+    const uint32_t scale_bytes = next_scale;
 #pragma unroll
     for (int i = 0; i < 8; i++) {
-      m[0] = max(m[0], q8_magnitude(v[i].x)), m[1] = max(m[1], q8_magnitude(v[i].y));
-      m[2] = max(m[2], q8_magnitude(v[i].z)), m[3] = max(m[3], q8_magnitude(v[i].w));
-      v[i] = make_float4(q8_finite_or_nan(v[i].x), q8_finite_or_nan(v[i].y), q8_finite_or_nan(v[i].z), q8_finite_or_nan(v[i].w));
+      if (kMode != 1) v[i] = dense[i * kTileThreads].floats();
+      if (kMode != 0) {
+        const float s = q8_scale(__shfl_sync(0xffffffffu, scale_bytes, i));
+        float4 d = q8_unpack4(*reinterpret_cast<const uint32_t*>(codes + turn * 16384 + (first + i) * 128 + lane * 4));
+        d = make_float4(d.x * s, d.y * s, d.z * s, d.w * s);
+        // one rounding each, so that the values are those of the plain product
+        v[i] = kMode == 1 ? d : make_float4(__fmul_rn(v[i].x, d.x), __fmul_rn(v[i].y, d.y), __fmul_rn(v[i].z, d.z), __fmul_rn(v[i].w, d.w));
+      }
     }
-    top = make_float4(__uint_as_float(m[0]), __uint_as_float(m[1]), __uint_as_float(m[2]), __uint_as_float(m[3]));
-  }
-  atomicMax(&tops[0][lane], __float_as_uint(top.x));
-  atomicMax(&tops[1][lane], __float_as_uint(top.y));
-  atomicMax(&tops[2][lane], __float_as_uint(top.z));
-  atomicMax(&tops[3][lane], __float_as_uint(top.w));
-  __syncthreads();
-  const uint32_t scale[4] = {q8_scale_byte(tops[0][lane]), q8_scale_byte(tops[1][lane]), q8_scale_byte(tops[2][lane]),
-                             q8_scale_byte(tops[3][lane])};
-  const float inv[4] = {q8_inverse(scale[0]), q8_inverse(scale[1]), q8_inverse(scale[2]), q8_inverse(scale[3])};
-  const int64_t t_row_bytes = q8_row_bytes(rows);
-  if (warp == 0) {
-    uint8_t* ts = qt.scales + b * q8_scale_batch(cols, rows);
+    if (t + gridDim.x < tiles) copy(t + gridDim.x, turn ^ 1);
+    if (sums) {
+      float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-    for (int j = 0; j < 4; j++)
-      if (lane * 4 + j < wide) ts[q8_scale_at(q8_scale_chunks(rows), c + j, rt)] = uint8_t(scale[j]);
-  }
+      for (int i = 0; i < 8; i++) s.x += v[i].x, s.y += v[i].y, s.z += v[i].z, s.w += v[i].w;
+      part[warp][lane] = s;
+      __syncthreads();
+      if (int(threadIdx.x) < p.wide) {
+        float sum = 0.f;
 #pragma unroll
-  for (int h = 0; h < 2; h++) {
-    const int w = (warp * 2 + h) ^ lane;  // word of rows first + 4 h ..., columns 4 lane + j
-    bytes[(lane * 4 + 0) * 32 + w] = q8_pack4(v[4 * h].x, v[4 * h + 1].x, v[4 * h + 2].x, v[4 * h + 3].x, inv[0]);
-    bytes[(lane * 4 + 1) * 32 + w] = q8_pack4(v[4 * h].y, v[4 * h + 1].y, v[4 * h + 2].y, v[4 * h + 3].y, inv[1]);
-    bytes[(lane * 4 + 2) * 32 + w] = q8_pack4(v[4 * h].z, v[4 * h + 1].z, v[4 * h + 2].z, v[4 * h + 3].z, inv[2]);
-    bytes[(lane * 4 + 3) * 32 + w] = q8_pack4(v[4 * h].w, v[4 * h + 1].w, v[4 * h + 2].w, v[4 * h + 3].w, inv[3]);
-  }
-  __syncthreads();
-  uint8_t* out = qt.values + (b * cols + ct * 128) * t_row_bytes + rt * 128 + lane * 4;
+        for (int i = 0; i < 16; i++) sum += reinterpret_cast<const float*>(part[i])[threadIdx.x];
+        sums[(p.b * row_tiles + p.rt) * cols + p.ct * 128 + threadIdx.x] = sum;
+      }
+    }
+    if (q.values) {
+      uint8_t* out = q.values + (p.b * rows + p.rt * 128 + first) * row_bytes + p.ct * 128 + lane * 4;
+      uint32_t mine = 0;
 #pragma unroll
-  for (int i = 0; i < 8; i++) {
-    const int n = first + i;
-    if (n < wide) *reinterpret_cast<uint32_t*>(out + n * t_row_bytes) = bytes[n * 32 + (lane ^ (n >> 2))];
+      for (int i = 0; i < 8; i++) {
+        const uint32_t byte = q8_warp_scale(v[i]);
+        if (i < p.have) *reinterpret_cast<uint32_t*>(out) = q8_pack4(v[i].x, v[i].y, v[i].z, v[i].w, q8_inverse(byte));
+        out += row_bytes;
+        if (lane == i) mine = byte;
+      }
+      if (lane < 8 && lane < p.have) q.scales[p.b * scale_batch + q8_scale_at(chunks, p.rt * 128 + first + lane, p.ct)] = uint8_t(mine);
+    }
+    if (!qt.values) {
+      if (sums) __syncthreads();  // the sums are read before the next ones are written
+      continue;
+    }
+    float4 top = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+      top = make_float4(fmaxf(top.x, fabsf(v[i].x)), fmaxf(top.y, fabsf(v[i].y)), fmaxf(top.z, fabsf(v[i].z)), fmaxf(top.w, fabsf(v[i].w)));
+    // NaN is passed over by the maxima; where an infinity is, the finite magnitudes are taken again
+    if (q8_top4(top) == INFINITY) {
+      uint32_t m[4] = {};
+#pragma unroll
+      for (int i = 0; i < 8; i++) {
+        m[0] = max(m[0], q8_magnitude(v[i].x)), m[1] = max(m[1], q8_magnitude(v[i].y));
+        m[2] = max(m[2], q8_magnitude(v[i].z)), m[3] = max(m[3], q8_magnitude(v[i].w));
+        v[i] = make_float4(q8_finite_or_nan(v[i].x), q8_finite_or_nan(v[i].y), q8_finite_or_nan(v[i].z), q8_finite_or_nan(v[i].w));
+      }
+      top = make_float4(__uint_as_float(m[0]), __uint_as_float(m[1]), __uint_as_float(m[2]), __uint_as_float(m[3]));
+    }
+    atomicMax(&tops[turn][0][lane], __float_as_uint(top.x));
+    atomicMax(&tops[turn][1][lane], __float_as_uint(top.y));
+    atomicMax(&tops[turn][2][lane], __float_as_uint(top.z));
+    atomicMax(&tops[turn][3][lane], __float_as_uint(top.w));
+    __syncthreads();
+    const uint32_t scale[4] = {q8_scale_byte(tops[turn][0][lane]), q8_scale_byte(tops[turn][1][lane]), q8_scale_byte(tops[turn][2][lane]),
+                               q8_scale_byte(tops[turn][3][lane])};
+    const float inv[4] = {q8_inverse(scale[0]), q8_inverse(scale[1]), q8_inverse(scale[2]), q8_inverse(scale[3])};
+    if (warp == 0) {
+      uint8_t* ts = qt.scales + p.b * t_scale_batch;
+#pragma unroll
+      for (int j = 0; j < 4; j++)
+        if (lane * 4 + j < p.wide) ts[q8_scale_at(t_chunks, p.ct * 128 + lane * 4 + j, p.rt)] = uint8_t(scale[j]);
+    }
+    if (warp < 4) tops[turn ^ 1][warp][lane] = 0;  // read by all before the barrier above
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+      const int w = (warp * 2 + h) ^ lane;  // word of rows first + 4 h ..., columns 4 lane + j
+      bytes[(lane * 4 + 0) * 32 + w] = q8_pack4(v[4 * h].x, v[4 * h + 1].x, v[4 * h + 2].x, v[4 * h + 3].x, inv[0]);
+      bytes[(lane * 4 + 1) * 32 + w] = q8_pack4(v[4 * h].y, v[4 * h + 1].y, v[4 * h + 2].y, v[4 * h + 3].y, inv[1]);
+      bytes[(lane * 4 + 2) * 32 + w] = q8_pack4(v[4 * h].z, v[4 * h + 1].z, v[4 * h + 2].z, v[4 * h + 3].z, inv[2]);
+      bytes[(lane * 4 + 3) * 32 + w] = q8_pack4(v[4 * h].w, v[4 * h + 1].w, v[4 * h + 2].w, v[4 * h + 3].w, inv[3]);
+    }
+    __syncthreads();
+    uint8_t* out = qt.values + (p.b * cols + p.ct * 128 + first) * t_row_bytes + p.rt * 128 + lane * 4;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      const int n = first + i;
+      if (n < p.wide) *reinterpret_cast<uint32_t*>(out) = bytes[n * 32 + (lane ^ (n >> 2))];
+      out += t_row_bytes;
+    }
   }
 }
 
@@ -249,9 +303,13 @@ emr_status launch_tile(const Dense<T, kVector>& src, const emr_q8* other, int64_
                        const emr_q8* q, const emr_q8* qt, float* sums, cudaStream_t st) {
   const int64_t tiles = batch * q8_blocks(rows) * q8_blocks(cols);
   if (tiles > kMaxGrid) return EMR_ERR_RANGE;
+  static std::atomic<uint64_t> done{0};
+  const int smem = (kMode != 1 ? int(sizeof(Four<T>)) * 8 * kTileThreads : 0) + (kMode != 0 ? 2 * 16384 : 0);
+  int dev = 0, sms = 0;
+  if (!device_sms(&dev, &sms) || !allow_smem(q8_tile_kernel<kMode, T, kVector>, smem, dev, done)) return EMR_ERR_CUDA;
   const emr_q8 none{};
-  return launch_after(q8_tile_kernel<kMode, T, kVector>, dim3(unsigned(tiles)), kTileThreads, 0, st, src, other ? *other : none, rows,
-                      cols, q ? *q : none, qt ? *qt : none, sums);
+  return launch_after(q8_tile_kernel<kMode, T, kVector>, dim3(unsigned(tiles < 2 * sms ? tiles : 2 * sms)), kTileThreads, size_t(smem), st,
+                      src, other ? *other : none, rows, cols, uint32_t(tiles), q ? *q : none, qt ? *qt : none, sums);
 }
 
 template <typename T, bool kVector>
@@ -320,7 +378,9 @@ extern "C" emr_status emr_q8_quantize(const void* src, int32_t dtype, int32_t ba
   const DenseArgs args{src, dtype, batch, rows, cols, batch_stride, row_stride, col_stride};
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   return with_dense(args, [&](auto d) {
-    return qt ? launch_tile<0>(d, nullptr, batch, rows, cols, q, qt, nullptr, st) : launch_rows(d, batch, rows, cols, q, st);
+    // row blocks alone: a warp a row while there are few tiles, else by tiles, which copy ahead
+    const bool tiled = qt || int64_t(batch) * q8_blocks(rows) * q8_blocks(cols) >= kTiledFrom;
+    return tiled ? launch_tile<0>(d, nullptr, batch, rows, cols, q, qt, nullptr, st) : launch_rows(d, batch, rows, cols, q, st);
   });
 }
 
