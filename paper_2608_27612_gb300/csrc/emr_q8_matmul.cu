@@ -689,24 +689,28 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   }
 }
 
-// ---- at most 128 rows ---------------------------------------------------------------
+// ---- few rows, or few tiles ---------------------------------------------------------
 // With few rows of a the weights' bytes bound the product, and a tile of 128 outputs for
 // each SM leaves most of them without work. Here the operands change places: 128 rows of
 // w are the instruction's rows and the rows of a, 16 to 128 of them, its columns, so a
 // block streams little but weights; two blocks share an SM, and the blocks of a cluster
 // share the contraction of one tile and add their accumulators, through each other's
 // shared memory, in the order of their ranks. A lane of the epilogue has one output of
-// each row, so its stores are neighbours.
+// each row, so its stores are neighbours. The same kernel serves larger a with few tiles
+// and a long contraction (the gradient of an input that many networks share). 8 x 8192 x
+// 8192: 9.3 us with the weights in L2, 23 from memory, where tiles of 128 rows took 21
+// and 31; 250 x 256 summed over 64 networks of 340: 57 -> 17 us.
 
-constexpr int kThinStages = 4;
-constexpr int kThinThreads = 192;  // copy warp, matrix warp, four epilogue warps
+constexpr int kThinStages = 6;     // at most; q.stages of them are used
+constexpr int kThinThreads = 320;  // copy warp, matrix warp, eight epilogue warps
 constexpr int kThinColumns = 256;  // of tensor memory: half of it
 constexpr int kThinMaxSplit = 8;
 
 struct ThinParams {
   Params p;
-  int32_t wide;   // rows of a, rounded up to 16, 32, 64 or 128
+  int32_t wide;   // rows of a in a tile: 16, 32, 64 or 128
   int32_t split;  // blocks of a cluster
+  int32_t stages;
 };
 __host__ __device__ inline int thin_stage_bytes(int wide) { return kOperandBytes + wide * 128 + kScaleBytes; }
 
@@ -743,19 +747,21 @@ __global__ void __launch_bounds__(kThinThreads, 2) q8_thin_kernel(const __grid_c
   const Params& p = q.p;
   uint8_t* const sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
   const int wide_bytes = q.wide * 128;
-  uint8_t* const rows_sm = sm + kThinStages * kOperandBytes;
-  uint8_t* const scales_sm = rows_sm + kThinStages * wide_bytes;
+  uint8_t* const rows_sm = sm + q.stages * kOperandBytes;
+  uint8_t* const scales_sm = rows_sm + q.stages * wide_bytes;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t full = smem_at(bars), empty = full + 8 * kThinStages, acc_full = empty + 8 * kThinStages, acc_empty = acc_full + 16;
   volatile int* const stop = &gave_up;
   const int rank = q.split > 1 ? int(cluster_rank()) : 0;
-  const int first = p.k_blocks * rank / q.split, last = p.k_blocks * (rank + 1) / q.split;
+  const int steps = p.sum * p.k_blocks;
+  const int first = int(int64_t(steps) * rank / q.split), last = int(int64_t(steps) * (rank + 1) / q.split);
+  const int first_sb = first / p.k_blocks, first_kb = first - first_sb * p.k_blocks;
   const int accs = q.wide <= 64 ? 2 : 1;  // accumulators at columns 0 and 64, scales from 128 on (wide 128: from 128)
 
   if (threadIdx.x == 0) {
     gave_up = 0;
     for (int i = 0; i < kThinStages; i++) bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, 1);
-    for (int i = 0; i < 2; i++) bar_init(acc_full + 8 * i, 1), bar_init(acc_empty + 8 * i, 4);
+    for (int i = 0; i < 2; i++) bar_init(acc_full + 8 * i, 1), bar_init(acc_empty + 8 * i, 8);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&a_map) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&w_map) : "memory");
@@ -774,44 +780,53 @@ __global__ void __launch_bounds__(kThinThreads, 2) q8_thin_kernel(const __grid_c
   const int stride = int(gridDim.x) / q.split, start = int(blockIdx.x) / q.split;
 
   if (warp == 0) {
-    Ring<kThinStages> ring;
+    int stage = 0;
+    uint32_t round = 0;
+    const auto next = [&] {
+      if (++stage == q.stages) stage = 0, round ^= 1;
+    };
     for (int t = start; t < p.tiles && !*stop; t += stride) {
-      const int b = p.n_tiles == p.tiles ? 0 : t / p.n_tiles, n = t - b * p.n_tiles;
-      const int ab = p.a_one ? 0 : b, wb = p.w_one ? 0 : b;
-      const uint8_t* a_scales = p.a_scales + int64_t(ab) * p.k_chunks * 512;
-      const uint8_t* w_scales = p.w_scales + (int64_t(wb) * p.n_tiles + n) * p.k_chunks * 512;
-      for (int kb = first; kb < last; kb++, ring.next()) {
-        if (!warp_wait(empty + 8 * ring.stage, ring.round ^ 1, stop, 10)) break;
+      const Tile tile = tile_at(p, t);
+      int kb = first_kb, sb = first_sb;
+      for (int i = first; i < last; i++, next()) {
+        if (!warp_wait(empty + 8 * stage, round ^ 1, stop, 10)) break;
+        const int b = tile.b + sb, ab = p.a_one ? 0 : b, wb = p.w_one ? 0 : b;
         if (elect_one()) {
-          const uint32_t bar = full + 8 * ring.stage;
-          const bool scales = kb == first || (kb & 3) == 0;
+          const uint32_t bar = full + 8 * stage;
+          const bool scales = i == first || (kb & 3) == 0;
           bar_expect(bar, kOperandBytes + wide_bytes + (scales ? kScaleBytes : 0));
-          tma_load(smem_at(sm) + ring.stage * kOperandBytes, &w_map, kb * kTileK, n * kTileN, wb, bar);
-          tma_load(smem_at(rows_sm) + ring.stage * wide_bytes, &a_map, kb * kTileK, 0, ab, bar);
+          tma_load(smem_at(sm) + stage * kOperandBytes, &w_map, kb * kTileK, tile.n * kTileN, wb, bar);
+          tma_load(smem_at(rows_sm) + stage * wide_bytes, &a_map, kb * kTileK, tile.m * kTileM, ab, bar);
           if (scales) {
-            const uint32_t at = smem_at(scales_sm) + ring.stage * kScaleBytes;
-            bulk_load(at, w_scales + (kb >> 2) * 512, 512, bar);
-            bulk_load(at + 512, a_scales + (kb >> 2) * 512, 512, bar);
+            const uint32_t at = smem_at(scales_sm) + stage * kScaleBytes;
+            bulk_load(at, p.w_scales + ((int64_t(wb) * p.n_tiles + tile.n) * p.k_chunks + (kb >> 2)) * 512, 512, bar);
+            bulk_load(at + 512, p.a_scales + ((int64_t(ab) * p.m_tiles + tile.m) * p.k_chunks + (kb >> 2)) * 512, 512, bar);
           }
         }
+        if (++kb == p.k_blocks) kb = 0, sb++;
         __syncwarp();
       }
     }
     if (*stop) settle();
   } else if (warp == 1) {
     const uint32_t idesc = (1u << 23) | (uint32_t(q.wide >> 3) << 17) | (uint32_t(128 >> 4) << 24);
-    Ring<kThinStages> ring;
+    int stage = 0;
+    uint32_t round = 0;
+    const auto next = [&] {
+      if (++stage == q.stages) stage = 0, round ^= 1;
+    };
     uint32_t n_tile = 0, chunk = 0;
     for (int t = start; t < p.tiles && !*stop; t += stride, n_tile++) {
       const uint32_t acc = accs == 2 ? n_tile & 1 : 0, use = accs == 2 ? n_tile >> 1 : n_tile;
       if (use >= 1 && !warp_wait(acc_empty + 8 * acc, (use - 1) & 1, stop, 11)) break;
       fence_after();
       uint32_t sf = 0;
-      for (int kb = first; kb < last; kb++, ring.next()) {
-        const int s = ring.stage;
-        if (!warp_wait(full + 8 * s, ring.round, stop, 12)) break;
+      int kb = first_kb;
+      for (int i = first; i < last; i++, next()) {
+        const int s = stage;
+        if (!warp_wait(full + 8 * s, round, stop, 12)) break;
         fence_after();
-        if (kb == first || (kb & 3) == 0) {
+        if (i == first || (kb & 3) == 0) {
           sf = tmem + 128 + 8 * (chunk++ & 1);
           const uint32_t at = smem_at(scales_sm) + s * kScaleBytes;
           if (elect_one()) {
@@ -824,26 +839,29 @@ __global__ void __launch_bounds__(kThinThreads, 2) q8_thin_kernel(const __grid_c
         const uint32_t id = idesc | (uint32_t(kb & 3) << 4) | (uint32_t(kb & 3) << 29);
         if (elect_one()) {
 #pragma unroll
-          for (int j = 0; j < 4; j++) mma_scaled(tmem + acc * 64, w + 2 * j, a + 2 * j, id, sf, sf + 4, kb > first || j > 0);
+          for (int j = 0; j < 4; j++) mma_scaled(tmem + acc * 64, w + 2 * j, a + 2 * j, id, sf, sf + 4, i > first || j > 0);
           mma_commit(empty + 8 * s);
         }
         __syncwarp();
+        if (++kb == p.k_blocks) kb = 0;
       }
       if (elect_one()) mma_commit(acc_full + 8 * acc);
       __syncwarp();
     }
   } else {
-    const int row = (warp & 3) * 32 + lane;  // of the tile's 128 outputs
+    const int row = (warp & 3) * 32 + lane;  // of the tile's 128 outputs; the second four warps take every other 16 rows of a
+    const int half = (warp - 2) >> 2;
     uint32_t n_tile = 0;
     for (int t = start; t < p.tiles; t += stride, n_tile++) {
-      const int b = p.n_tiles == p.tiles ? 0 : t / p.n_tiles, n = (t - b * p.n_tiles) * kTileN + row;
+      const Tile tile = tile_at(p, t);
+      const int b = tile.b, n = tile.n * kTileN + row, m0 = tile.m * kTileM;
       const uint32_t acc = accs == 2 ? n_tile & 1 : 0, use = accs == 2 ? n_tile >> 1 : n_tile;
       const float bias = q.split == 1 && p.bias && n < p.N ? __ldg(p.bias + int64_t(b) * p.N + n) : 0.f;
       if (!warp_wait(acc_full + 8 * acc, use & 1, stop, 13)) break;
       fence_after();
       const uint32_t addr = tmem + acc * 64 + (uint32_t((warp & 3) * 32) << 16);
 #pragma unroll 1
-      for (int c = 0; c < q.wide; c += 16) {
+      for (int c = half * 16; c < q.wide; c += 32) {
         float z[16], d[16];
         tmem_load16(addr + c, z);
         if (q.split > 1) {  // this block's share, [row of a][output]; the stages are done with
@@ -854,11 +872,11 @@ __global__ void __launch_bounds__(kThinThreads, 2) q8_thin_kernel(const __grid_c
         }
         if (n < p.N) {
 #pragma unroll
-          for (int i = 0; i < 16; i++) z[i] = c + i < p.M ? z[i] + bias : 0.f;
+          for (int i = 0; i < 16; i++) z[i] = m0 + c + i < p.M ? z[i] + bias : 0.f;
           activate<16, false>(p.act, z, d);
 #pragma unroll
           for (int i = 0; i < 16; i++)
-            if (c + i < p.M) store_scalar(p.out, p.out_dtype, (int64_t(b) * p.M + c + i) * p.N + n, z[i]);
+            if (m0 + c + i < p.M) store_scalar(p.out, p.out_dtype, (int64_t(b) * p.M + m0 + c + i) * p.N + n, z[i]);
         }
       }
       fence_before();
@@ -871,10 +889,11 @@ __global__ void __launch_bounds__(kThinThreads, 2) q8_thin_kernel(const __grid_c
   __syncthreads();
   if (q.split > 1) {  // one tile a cluster
     cluster_sync();
-    const int t = start, b = p.n_tiles == p.tiles ? 0 : t / p.n_tiles, n0 = (t - b * p.n_tiles) * kTileN;
+    const Tile tile = tile_at(p, start);
+    const int b = tile.b, n0 = tile.n * kTileN, m0 = tile.m * kTileM, have = p.M - m0 < q.wide ? p.M - m0 : q.wide;
     const bool fine = !*stop;
     // four neighbouring outputs of a row at a time, rows shared out over the blocks
-    for (int i = threadIdx.x; i < 32 * ((p.M - rank + q.split - 1) / q.split); i += kThinThreads) {
+    for (int i = threadIdx.x; i < 32 * ((have - rank + q.split - 1) / q.split); i += kThinThreads) {
       const int m = (i >> 5) * q.split + rank, r = (i & 31) * 4;
       float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
       for (int s = 0; s < q.split; s++) {
@@ -887,7 +906,7 @@ __global__ void __launch_bounds__(kThinThreads, 2) q8_thin_kernel(const __grid_c
       activate<4, false>(p.act, z, d);
 #pragma unroll
       for (int j = 0; j < 4; j++)
-        if (fine && n0 + r + j < p.N) store_scalar(p.out, p.out_dtype, (int64_t(b) * p.M + m) * p.N + n0 + r + j, z[j]);
+        if (fine && n0 + r + j < p.N) store_scalar(p.out, p.out_dtype, (int64_t(b) * p.M + m0 + m) * p.N + n0 + r + j, z[j]);
     }
     cluster_sync();  // no block ends while another reads its share
   }
@@ -967,10 +986,11 @@ emr_status launch_thin(const emr_q8* a, const emr_q8* w, const Params& p, int de
   // As many blocks to a tile as find room, with two blocks of columns for each.
   q.split = 1;
   const int64_t room = q.wide <= 64 ? 2 * sms : sms;  // 100 KB a block up to 64 rows
-  while (q.split < kThinMaxSplit && int64_t(p.tiles) * q.split * 2 <= room && p.k_blocks >= 4 * q.split) q.split *= 2;
+  while (q.split < kThinMaxSplit && int64_t(p.tiles) * q.split * 2 <= room && int64_t(p.sum) * p.k_blocks >= 4 * q.split) q.split *= 2;
   CUtensorMap a_map, w_map;
   if (!operand_map(a, &a_map, q.wide) || !operand_map(w, &w_map)) return EMR_ERR_CUDA;
-  const int smem = 1024 + kThinStages * thin_stage_bytes(q.wide);  // the shares, wide rows of 512 bytes, fit in w's stages
+  q.stages = q.wide <= 64 ? 4 : 6;
+  const int smem = 1024 + q.stages * thin_stage_bytes(q.wide);  // the shares, wide rows of 512 bytes, fit in w's stages
   if (!allow_smem(q8_thin_kernel, 1024 + kThinStages * thin_stage_bytes(128), dev, done)) return EMR_ERR_CUDA;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(unsigned(q.split > 1 ? p.tiles * q.split : p.tiles < room ? p.tiles : room));
@@ -986,6 +1006,12 @@ emr_status launch_thin(const emr_q8* a, const emr_q8* w, const Params& p, int de
   cfg.attrs = attr;
   cfg.numAttrs = q.split > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, q8_thin_kernel, a_map, w_map, q) == cudaSuccess ? EMR_OK : EMR_ERR_CUDA;
+}
+
+// At most 128 rows, or so few tiles of a long contraction that most SMs would have none.
+bool use_thin(const Params& p, int sms) {
+  if (p.M <= 128) return true;
+  return int64_t(p.tiles) * 2 <= sms && int64_t(p.sum) * p.k_blocks >= 16;
 }
 
 // Pairs of SMs where their rounds of 256 x 256 tiles take less time than one SM's rounds of
@@ -1036,7 +1062,7 @@ extern "C" emr_status emr_q8_matmul(const emr_q8* a, const emr_q8* w, const floa
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   int dev = 0, sms = 0;
   if (!device_sms(&dev, &sms)) return EMR_ERR_CUDA;
-  if (!slope && !sum_batch && p.M <= 128) return launch_thin(a, w, p, dev, sms, st);
+  if (!slope && use_thin(p, sms)) return launch_thin(a, w, p, dev, sms, st);
   CUtensorMap a_map, w_map;
   if (!operand_map(a, &a_map) || !operand_map(w, &w_map)) return EMR_ERR_CUDA;
   if (use_pairs(p, sms))
