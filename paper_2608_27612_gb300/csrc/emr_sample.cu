@@ -23,6 +23,8 @@
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
+#include <mutex>
+
 #include "emr_act.h"
 #include "emr_q8.h"
 
@@ -33,7 +35,7 @@ using namespace emr;
 typedef unsigned long long u64;
 
 constexpr int kMaxCluster = 8;
-constexpr float kSpan = 24.f;    // the equal steps cover w in (e^-24, 1]; the last one takes the rest
+constexpr float kSpan = 16.f;    // the equal steps cover w in (e^-16, 1]; the last one takes the rest
 constexpr float kNear = 4e-5f;   // of the draw's first computation
 constexpr float kLackUnit = 1048576.f;
 
@@ -49,8 +51,8 @@ struct Args {
   int32_t* index;
   float* logp;
   int32_t bins, cap;             // histogram steps, entries of the list
-  int32_t room;                  // entries of a slice that shared memory holds
-  int32_t vector, noise_vector;  // four entries at a time
+  int32_t room;                  // groups of 16 bytes of a slice that shared memory holds
+  int32_t noise_vector;          // rows of noise are aligned to 16 bytes
   int32_t fix;                   // sums of w are kept in steps of 2^-fix
 };
 
@@ -79,15 +81,26 @@ __device__ __forceinline__ void join(Drawn& x, const Drawn& y) {
   x.unsure = max(x.unsure, y.unsure);
 }
 
+// 16 bytes of scores.
+template <typename T>
+struct Group {
+  static constexpr int kSize = 16 / int(sizeof(T));
+  uint4 u;
+  __device__ __forceinline__ void set(int j, T v) { reinterpret_cast<T*>(&u)[j] = v; }
+  __device__ __forceinline__ float get(int j) const { return float(reinterpret_cast<const T*>(&u)[j]); }
+};
+
 template <typename T, int kAhead>
 struct Row {
+  static constexpr int kG = Group<T>::kSize;
   cg::cluster_group cluster;
   const Args& a;
   int tid, threads, lane, warp, warps, rank, blocks, phase, turn;
   int64_t lo;       // first entry of this block's slice
-  int count, held;  // its entries, and those in shared memory
+  int count;        // its entries, the first of them `skip` entries after a multiple of 16 bytes
+  int skip, groups, held;  // groups of 16 bytes that they lie in, and those in shared memory
   const T* global;  // the slice in memory
-  T* data;          // and in shared memory
+  uint4* data;      // and in shared memory
   const float* noise;
   uint32_t *counts, *lacks;
   u64 *sums, *list, *sorted;
@@ -110,49 +123,55 @@ struct Row {
     const float s = float(v);
     return top_infinite ? (s == INFINITY ? 0.f : -INFINITY) : s;
   }
-  // fn(score, entry of the slice) for every entry of this block.
+  // One group from memory; past the slice its scores are -infinity.
+  __device__ __forceinline__ Group<T> fetch(int g) const {
+    Group<T> v;
+    const int i = g * kG - skip;
+    if (i >= 0 && i + kG <= count) {
+      v.u = *reinterpret_cast<const uint4*>(global + i);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kG; j++) v.set(j, i + j >= 0 && i + j < count ? global[i + j] : T(-INFINITY));
+    }
+    return v;
+  }
+  // fn(scores, i) for kAhead groups, loaded together, of every block's: scores[u][j] is entry i + u
+  // threads kG + j of the slice, and -infinity past it (i may be below 0).
+  template <typename Fn>
+  __device__ __forceinline__ void each_group(Fn fn) const {
+    for (int g = tid; g < groups; g += threads * kAhead) {
+      Group<T> v[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; u++) {
+        const int at = g + u * threads;
+        if (at < held) v[u].u = data[at];
+        else v[u] = fetch(at);
+      }
+      float s[kAhead][kG];
+#pragma unroll
+      for (int u = 0; u < kAhead; u++)
+#pragma unroll
+        for (int j = 0; j < kG; j++) s[u][j] = v[u].get(j);
+      if (top_infinite) {
+#pragma unroll
+        for (int u = 0; u < kAhead; u++)
+#pragma unroll
+          for (int j = 0; j < kG; j++) s[u][j] = s[u][j] == INFINITY ? 0.f : -INFINITY;
+      }
+      fn(s, g * kG - skip);
+    }
+  }
+  // fn(score, entry of the slice); past the slice, too, with -infinity.
   template <typename Fn>
   __device__ __forceinline__ void each(Fn fn) const {
-    each4([&](const float (&s)[kAhead][4], int i, int have) {
+    each_group([&](const float (&s)[kAhead][kG], int i) {
 #pragma unroll
       for (int u = 0; u < kAhead; u++) {
-        if (u * threads * 4 >= have) break;
+        if (i + u * threads * kG >= count) break;
 #pragma unroll
-        for (int j = 0; j < 4; j++)
-          if (u * threads * 4 + j < have) fn(s[u][j], i + u * threads * 4 + j);
+        for (int j = 0; j < kG; j++) fn(s[u][j], i + u * threads * kG + j);
       }
     });
-  }
-  // fn(scores, i, have) for kAhead groups of four entries at i, i + 4 threads, ..., loaded together;
-  // have: entries of the slice from i on. Past the slice scores are -infinity.
-  template <typename Fn>
-  __device__ __forceinline__ void each4(Fn fn) const {
-    for (int i = tid * 4; i < count; i += threads * 4 * kAhead) {
-      Four<T> g[kAhead];
-#pragma unroll
-      for (int u = 0; u < kAhead; u++) {
-        const int at = i + u * threads * 4;
-        if (at < held) {  // what is held ends at a multiple of four, padded
-          g[u].load(data + at);
-        } else if (a.vector && at + 4 <= count) {
-          g[u].load(global + at);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 4; j++) g[u].set(j, at + j < count ? global[at + j] : T(-INFINITY));
-        }
-      }
-      float s[kAhead][4];
-#pragma unroll
-      for (int u = 0; u < kAhead; u++) {
-        const float4 f = g[u].floats();
-        s[u][0] = f.x, s[u][1] = f.y, s[u][2] = f.z, s[u][3] = f.w;
-        if (top_infinite) {
-#pragma unroll
-          for (int j = 0; j < 4; j++) s[u][j] = s[u][j] == INFINITY ? 0.f : -INFINITY;
-        }
-      }
-      fn(s, i, count - i);
-    }
   }
   __device__ __forceinline__ float weight(float s) const { return expf(__fdiv_rn(s - s_max, temperature)); }
   __device__ __forceinline__ float rough_weight(float s) const { return fast_exp2((s - s_max) * exp2_per); }
@@ -499,7 +518,7 @@ struct Row {
       const bool with_draw = by_mass && shift == 32;
       if (with_draw) {
         *drawn = true;
-        draw4([&](float s, int64_t at) {
+        draw([&](float s, int64_t at) {
           if (!(s > bs || (s == bs && at <= ba))) return false;
           const int b = step_of(s, per);
           if (b == step) list_add(order_key(s), at);
@@ -623,33 +642,37 @@ struct Row {
   }
   // Draws from the entries for which in(score, index) holds.
   template <typename In>
-  __device__ __forceinline__ void draw4(In in) {
-    each4([&](const float(&s)[kAhead][4], int i, int have) {
-      bool stay[kAhead][4];
-      float e[kAhead][4];
+  __device__ __forceinline__ void draw(In in) {
+    const bool vector = a.noise_vector && skip % 4 == 0;
+    each_group([&](const float(&s)[kAhead][kG], int i) {
+      bool stay[kAhead][kG];
+      float e[kAhead][kG];
 #pragma unroll
       for (int u = 0; u < kAhead; u++) {
-        const int at = i + u * threads * 4;
-        const bool there = u * threads * 4 < have;
+        const int at = i + u * threads * kG;
+        const bool there = at < count;
         bool any = false;
 #pragma unroll
-        for (int j = 0; j < 4; j++) {
+        for (int j = 0; j < kG; j++) {
           stay[u][j] = there && s[u][j] > -INFINITY && in(s[u][j], lo + at + j);
           any |= stay[u][j];
         }
-        if (any && a.noise_vector && u * threads * 4 + 4 <= have) {
-          const float4 f = __ldcs(reinterpret_cast<const float4*>(noise + lo + at));
-          e[u][0] = f.x, e[u][1] = f.y, e[u][2] = f.z, e[u][3] = f.w;
+        if (any && vector && at >= 0 && at + kG <= count) {
+#pragma unroll
+          for (int j = 0; j < kG; j += 4) {
+            const float4 f = __ldcs(reinterpret_cast<const float4*>(noise + lo + at + j));
+            e[u][j] = f.x, e[u][j + 1] = f.y, e[u][j + 2] = f.z, e[u][j + 3] = f.w;
+          }
         } else {
 #pragma unroll
-          for (int j = 0; j < 4; j++) e[u][j] = stay[u][j] ? noise[lo + at + j] : 1.f;
+          for (int j = 0; j < kG; j++) e[u][j] = stay[u][j] ? noise[lo + at + j] : 1.f;
         }
       }
 #pragma unroll
       for (int u = 0; u < kAhead; u++) {
-        if (u * threads * 4 >= have) break;
+        if (i + u * threads * kG >= count) break;
 #pragma unroll
-        for (int j = 0; j < 4; j++) consider(stay[u][j], s[u][j], lo + i + u * threads * 4 + j, e[u][j]);
+        for (int j = 0; j < kG; j++) consider(stay[u][j], s[u][j], lo + i + u * threads * kG + j, e[u][j]);
       }
     });
   }
@@ -701,7 +724,7 @@ struct Row {
 template <typename T, int kThreads, bool kFree>
 __global__ void __launch_bounds__(kThreads, 2048 / kThreads > 4 ? 4 : kThreads == 512 ? 2 : 1) sample_kernel(const __grid_constant__ Args a) {
   extern __shared__ __align__(16) uint8_t smem[];
-  constexpr int kAhead = kThreads == 1024 ? 2 : 4;  // 64 registers a thread
+  constexpr int kG = Group<T>::kSize, kAhead = (kFree && kThreads < 1024 ? 16 : 8) / kG;  // 64 registers a thread
   __shared__ uint4 scratch[64], slots[2 * kMaxCluster];
   __shared__ u64 coarse[128], found[3];
   __shared__ int list_size[3];
@@ -717,12 +740,13 @@ __global__ void __launch_bounds__(kThreads, 2048 / kThreads > 4 ? 4 : kThreads =
   r.counts = r.lacks + a.bins;
   r.sorted = r.sums;  // the histogram is done with when entries are ordered
   r.list = reinterpret_cast<u64*>(r.counts + a.bins);
-  r.data = reinterpret_cast<T*>(r.list + a.cap);
+  r.data = reinterpret_cast<uint4*>(r.list + a.cap);
   const int64_t row = blockIdx.x / unsigned(r.blocks);
   r.lo = r.rank * a.slice;
   r.count = int(a.n - r.lo < 0 ? 0 : a.n - r.lo < a.slice ? a.n - r.lo : a.slice);
-  r.held = 0;
   r.global = static_cast<const T*>(a.scores) + row * a.row_stride + r.lo;
+  r.skip = int(reinterpret_cast<uintptr_t>(r.global) % 16 / sizeof(T));
+  r.groups = (r.skip + r.count + kG - 1) / kG;
   r.noise = a.noise + row * a.noise_stride;
   r.top_infinite = false;
   r.rough = r.rough_second = -1.f, r.rough_at = -1, r.mass = 0.f, r.bound = 0;
@@ -731,20 +755,18 @@ __global__ void __launch_bounds__(kThreads, 2048 / kThreads > 4 ? 4 : kThreads =
 
   // scores once from memory: the thread's largest, and into shared memory
   float top = -INFINITY;
-#pragma unroll 4
-  for (int i = r.tid * 4; i < r.count; i += kThreads * 4) {
-    Four<T> u;
-    if (a.vector && i + 4 <= r.count) {
-      u.load(r.global + i);
-    } else {
+  for (int g = r.tid; g < r.groups; g += kThreads * 4) {
+    Group<T> v[4];
 #pragma unroll
-      for (int j = 0; j < 4; j++) u.set(j, i + j < r.count ? r.global[i + j] : T(-INFINITY));
+    for (int u = 0; u < 4; u++) v[u] = r.fetch(g + u * kThreads);
+#pragma unroll
+    for (int u = 0; u < 4; u++) {
+      if (g + u * kThreads < a.room) r.data[g + u * kThreads] = v[u].u;
+#pragma unroll
+      for (int j = 0; j < kG; j++) top = fmaxf(top, v[u].get(j));  // NaN is passed over
     }
-    if (i < a.room) u.store(r.data + i);
-    const float4 f = u.floats();
-    top = fmaxf(fmaxf(top, fmaxf(f.x, f.y)), fmaxf(f.z, f.w));  // NaN is passed over
   }
-  r.held = r.count < a.room ? r.count : a.room;
+  r.held = r.groups < a.room ? r.groups : a.room;
   const uint32_t own = order_key(top);
   const u64 top_key = r.row_max(r.block_max(own));
   if (top_key == 0) {  // nothing left
@@ -776,7 +798,7 @@ __global__ void __launch_bounds__(kThreads, 2048 / kThreads > 4 ? 4 : kThreads =
     return;
   }
   if constexpr (kFree) {
-    r.draw4([](float, int64_t) { return true; });
+    r.draw([](float, int64_t) { return true; });
     r.finish([](float, int64_t, u64) { return true; }, index, logp);
   } else {
     uint32_t bound_key = 0;
@@ -786,13 +808,16 @@ __global__ void __launch_bounds__(kThreads, 2048 / kThreads > 4 ? 4 : kThreads =
         // the k-th largest of one block's threads bounds the row's from below: the best of the blocks'
         const u64 least = r.row_max(r.floor_key(r.top_infinite ? (top == INFINITY ? order_key(0.f) : 0) : own, int(k)));
         const float low = least > 1 ? key_score(uint32_t(least)) : -INFINITY;
-        r.each4([&](const float(&s)[kAhead][4], int i, int) {
+        r.each_group([&](const float(&s)[kAhead][kG], int i) {
 #pragma unroll
           for (int u = 0; u < kAhead; u++) {
-            if (!(fmaxf(fmaxf(s[u][0], s[u][1]), fmaxf(s[u][2], s[u][3])) >= low)) continue;
+            float most = s[u][0];
 #pragma unroll
-            for (int j = 0; j < 4; j++)
-              if (s[u][j] >= low && s[u][j] > -INFINITY) r.list_add(order_key(s[u][j]), r.lo + i + u * kThreads * 4 + j);
+            for (int j = 1; j < kG; j++) most = fmaxf(most, s[u][j]);
+            if (!(most >= low)) continue;
+#pragma unroll
+            for (int j = 0; j < kG; j++)
+              if (s[u][j] >= low && s[u][j] > -INFINITY) r.list_add(order_key(s[u][j]), r.lo + i + u * kThreads * kG + j);
           }
         });
         const int m = r.list_end();
@@ -814,7 +839,7 @@ __global__ void __launch_bounds__(kThreads, 2048 / kThreads > 4 ? 4 : kThreads =
     bool drawn = false;
     if (p < 1.f) r.select(true, 0, fmaxf(p, 0.f), bound_key, bound_at, &drawn);
     const float bs = bound_key ? key_score(bound_key) : -INFINITY;
-    if (!drawn) r.draw4([&](float s, int64_t at) { return s > bs || (s == bs && at <= bound_at); });
+    if (!drawn) r.draw([&](float s, int64_t at) { return s > bs || (s == bs && at <= bound_at); });
     r.finish(
         [&](float s, int64_t at, u64 e) {  // e: the bound that a drawing selection left, 0 for none
           if (e) return r.kept(order_key(s), at, uint32_t(e >> 32), int64_t(uint32_t(~uint32_t(e))));
@@ -823,6 +848,27 @@ __global__ void __launch_bounds__(kThreads, 2048 / kThreads > 4 ? 4 : kThreads =
         index, logp);
   }
   // After the last exchange of a row no block reads another's memory: any may end first.
+}
+
+// How many clusters of each size, of blocks that fill an SM, run at the same time.
+void clusters_at_once(int* fit) {
+  for (int c = 1; c <= kMaxCluster; c++) {
+    fit[c] = 0;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(unsigned(c));
+    cfg.blockDim = dim3(1024);
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = unsigned(c);
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    cfg.dynamicSmemBytes = kMostSmem;
+    int n = 0;
+    if (cudaFuncSetAttribute(sample_kernel<float, 1024, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem) == cudaSuccess &&
+        cudaOccupancyMaxActiveClusters(&n, sample_kernel<float, 1024, false>, &cfg) == cudaSuccess)
+      fit[c] = n;
+  }
 }
 
 template <typename T, int kThreads, bool kFree>
@@ -845,9 +891,14 @@ emr_status launch(const Args& a, int rows, int cluster, size_t smem, int dev, cu
 
 template <typename T>
 emr_status plan(Args a, int rows, bool free, int dev, int sms, cudaStream_t st) {
-  // Blocks of a row: as many as find an SM each while a slice has 2048 entries.
+  // Blocks of a row: as many as find an SM each at the same time (clusters that do not fit into
+  // what is left of a group of SMs would wait) while a slice has 2048 entries.
+  static std::once_flag once;
+  static int fit[kMaxCluster + 1];
+  std::call_once(once, [&] { clusters_at_once(fit); });
   int cluster = 1;
-  while (cluster < kMaxCluster && int64_t(rows) * (cluster + 1) <= sms && a.n / (cluster + 1) >= 2048) cluster++;
+  for (int c = 2; c <= kMaxCluster; c++)
+    if (rows <= fit[c] && a.n / c >= 2048) cluster = c;
   a.slice = ((a.n + cluster - 1) / cluster + 15) / 16 * 16;
   const bool wide = a.slice > 8192, crowd = int64_t(rows) * cluster > sms;
   // Shared memory of a block: all of an SM's, half where two blocks of 512 threads share one,
@@ -856,9 +907,9 @@ emr_status plan(Args a, int rows, bool free, int dev, int sms, cudaStream_t st) 
   a.cap = free ? 0 : !wide ? 512 : crowd ? 1024 : 2048;
   size_t smem = size_t(a.bins) * 8 + size_t(a.cap) * 8;
   const size_t most = wide && !crowd ? kMostSmem : 110 * 1024;
-  const size_t want = size_t(a.slice) * sizeof(T), room = most > smem ? most - smem : 0;
-  a.room = int32_t((want < room ? want : room) / sizeof(T) / 4 * 4);
-  smem += size_t(a.room) * sizeof(T);
+  const size_t want = size_t(a.slice) * sizeof(T) + 16, room = most > smem ? most - smem : 0;
+  a.room = int32_t((want < room ? want : room) / 16);
+  smem += size_t(a.room) * 16;
   const int threads = !wide ? 256 : crowd ? 512 : 1024;
   if (free)
     return threads == 256 ? launch<T, 256, true>(a, rows, cluster, smem, dev, st)
@@ -890,7 +941,6 @@ extern "C" emr_status emr_sample(const void* scores, int32_t dtype, int32_t rows
   int bits = 0;
   while ((int64_t(1) << bits) < n) bits++;
   a.fix = bits <= 18 ? 44 : 62 - bits;
-  a.vector = reinterpret_cast<uintptr_t>(scores) % (4 * size) == 0 && (rows == 1 || row_stride % 4 == 0);
   a.noise_vector = reinterpret_cast<uintptr_t>(noise) % 16 == 0 && (rows == 1 || noise_stride % 4 == 0);
   const bool free = !top_k && !top_p && (top_k_all <= 0 || top_k_all >= n) && !(top_p_all < 1.f);
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
