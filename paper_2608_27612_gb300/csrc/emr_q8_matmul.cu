@@ -312,17 +312,19 @@ __device__ __forceinline__ void finish_chunk(const Params& p, const Tile& t, uin
   }
 }
 
-// Whether the accumulators of a tile are there, with one answer for the four warps that share
-// rows, since with kSlope they meet at a barrier while finishing the tile.
+constexpr int kFinishBarrier = 5;  // of all epilogue warps; 1 to 4 are the quarters
+__device__ __forceinline__ void finish_sync() { asm volatile("bar.sync %0, %1;" ::"n"(kFinishBarrier), "n"(32 * kFinishWarps) : "memory"); }
+// Whether the accumulators of a tile are there; with kSlope with one answer for all epilogue
+// warps, since they then meet at barriers while finishing the tile.
 template <bool kSlope>
-__device__ __forceinline__ bool finish_wait(uint32_t bar, uint32_t parity, volatile int* stop, int code, int quadrant) {
+__device__ __forceinline__ bool finish_wait(uint32_t bar, uint32_t parity, volatile int* stop, int code) {
   const bool ok = warp_wait(bar, parity, stop, code);
   if (!kSlope) return ok;
   uint32_t all;
   asm volatile(
-      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.and.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.and.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
       : "=r"(all)
-      : "r"(uint32_t(ok)), "r"(1 + quadrant)
+      : "r"(uint32_t(ok)), "n"(kFinishBarrier), "n"(32 * kFinishWarps)
       : "memory");
   return all != 0;
 }
@@ -445,7 +447,7 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
       const Tile tile = tile_at(p, t);
       const int row0 = tile.m * kTileM + quadrant * 32, n = tile.n * kTileN + c * 32 + lane;
       const float bias = p.bias && n < p.N ? __ldg(p.bias + int64_t(tile.b) * p.N + n) : 0.f;
-      if (!finish_wait<kSlope>(acc_full + 8 * acc, (n_tile >> 1) & 1, stop, 4, quadrant)) break;
+      if (!finish_wait<kSlope>(acc_full + 8 * acc, (n_tile >> 1) & 1, stop, 4)) break;
       fence_after();
       if (row0 >= p.M || (!kSlope && n - lane >= p.N)) {  // nothing of this warp's part is in the matrix
         if (lane == 0) bar_arrive(acc_empty + 8 * acc);
@@ -660,14 +662,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const int n = tile.n * kTileN + c * 32 + lane;
         const float bias = p.bias && n < p.N ? __ldg(p.bias + int64_t(tile.b) * p.N + n) : 0.f;
         if (half) {
-          if (!finish_wait<kSlope>(acc_full + 8 * acc, (n_tile >> 1) & 1, stop, 9, quadrant)) goto out;
+          if (!finish_wait<kSlope>(acc_full + 8 * acc, (n_tile >> 1) & 1, stop, 9)) goto out;
           fence_after();
         }
+        // The columns that the next tile's scales are waiting for are read before all others; without
+        // slopes the epilogue is short and the barrier costs more than it saves (94464 x 1364 x 1364:
+        // 170 us without, 185 with; with slopes 8192^3 375 us without, 350 with).
+        const bool scales = half && c == 3;
+        if (kSlope && half && !scales) finish_sync();
         auto read = [&] {
           if (lane == 0) {
-            if (half && c == 3) bar_arrive_cluster(last);
+            if (scales) bar_arrive_cluster(last);
             if (!half) bar_arrive_cluster(done);
           }
+          __syncwarp();
+          if (kSlope && scales) finish_sync();
         };
         if (row0 >= p.M || tile.n >= p.n_tiles || (!kSlope && n - lane >= p.N)) {  // nothing of this warp's part is in the matrix
           read();
@@ -1020,7 +1029,7 @@ bool use_thin(const Params& p, int sms) {
 // block of 128 columns, 36 for a pair) and its epilogue (200, with slopes 500, a pair twice
 // that), 100 more to fill and drain it, and a launch of pairs 400 more than one of single
 // blocks. 8192^3: 485 us against 330; 4096^3: 69 against 53; 5460 x 1364 x 2000: 23.5 against
-// 19.3; 1000 x 5460 x 1364: 15.3 against 16.6; 2000 x 5460 x 1364 with slopes: 27 against 39.
+// 19.3; 1000 x 5460 x 1364: 15.3 against 16.6; 2000 x 5460 x 1364 with slopes: 28 against 33.
 bool use_pairs(const Params& p, int sms) {
   const int64_t pair_tiles = int64_t(p.tiles) / (int64_t(p.m_tiles) * p.n_tiles) * ((p.m_tiles + 1) / 2) * ((p.n_tiles + 1) / 2);
   const int64_t pairs = sms / 2, steps = int64_t(p.sum) * p.k_blocks, finish = p.slope ? 500 : 200;
