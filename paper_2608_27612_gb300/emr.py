@@ -820,26 +820,32 @@ class DenseLayer:
     def _forward(self, x, out_dtype, stream, keep):
         x = _matrices(x, "x")
         nx, m, k = x.shape
-        if k != self.k or (nx != 1 and nx != self.nets) or x.device != self.device:
+        dev = self.device
+        if k != self.k or (nx != 1 and nx != self.nets) or x.device != dev:
             raise ValueError("x: [m, %d], [1, m, %d] or [%d, m, %d] on the layer's GPU is wanted, got %s" %
                              (self.k, self.k, self.nets, self.k, tuple(x.shape)))
-        kind, out_kind = _dtype(x.dtype, "x"), _dtype(out_dtype, "out_dtype")
+        kind, out_kind = _DTYPES.get(x.dtype), _DTYPES.get(out_dtype)
+        if kind is None or out_kind is None:
+            _dtype(x.dtype, "x"), _dtype(out_dtype, "out_dtype")
         if m == 0:
             if keep:
                 raise ValueError("x: at least one row is wanted for training")
-            return torch.empty(self.nets, 0, self.n, dtype=out_dtype, device=self.device), None, None
-        with _on(stream):
-            out = torch.empty((self.nets, m, self.n), dtype=out_dtype, device=self.device)
-            xq = slope = None
-            if keep or self._needs_room(nx, m):
-                xq = torch.empty(sum(_q8_bytes(nx, m, k)), dtype=torch.uint8, device=self.device)
-            if keep and self.act != ACT_IDENTITY:
-                slope = torch.empty(sum(_q8_bytes(self.nets, m, self.n)), dtype=torch.uint8, device=self.device)
-            bs, rs, cs = x.stride()
-            _check(lib().emr_dense_forward(self._ref, x.data_ptr(), kind, nx, m, bs, rs, cs, out.data_ptr(), out_kind,
-                                           1 if keep else 0, xq.data_ptr() if xq is not None else None,
-                                           slope.data_ptr() if slope is not None else None,
-                                           _raw_stream(stream, self.device)), "emr_dense_forward")
+            return torch.empty(self.nets, 0, self.n, dtype=out_dtype, device=dev), None, None
+        if stream is not None and stream != torch.cuda.current_stream(dev):
+            with torch.cuda.stream(stream):   # allocations belong to the stream that they are used on
+                return self._forward(x, out_dtype, None, keep)
+        out = torch.empty((self.nets, m, self.n), dtype=out_dtype, device=dev)
+        xq = slope = xp = sp = None
+        if keep or self._needs_room(nx, m):
+            xq = torch.empty(sum(_q8_bytes(nx, m, k)), dtype=torch.uint8, device=dev)
+            xp = xq.data_ptr()
+        if keep and self.act != ACT_IDENTITY:
+            slope = torch.empty(sum(_q8_bytes(self.nets, m, self.n)), dtype=torch.uint8, device=dev)
+            sp = slope.data_ptr()
+        status = _lib.emr_dense_forward(self._ref, x.data_ptr(), kind, nx, m, *x.stride(), out.data_ptr(), out_kind,
+                                        1 if keep else 0, xp, sp, torch._C._cuda_getCurrentRawStream(dev.index))
+        if status:
+            _check(status, "emr_dense_forward")
         return out, xq, slope
 
     def forward(self, x, out_dtype=torch.float32, stream=None):
@@ -880,42 +886,55 @@ class DenseLayer:
 # ---- sampling from scores -------------------------------------------------------------------
 
 def _per_row(v, rows: int, dtype, device, what: str):
-    """(device array or None, scalar) of a parameter given for all rows or for each."""
-    if not isinstance(v, torch.Tensor):
-        return None, v
+    """Address of a device array of a parameter given for each row."""
     if v.shape != (rows,) or v.dtype != dtype or v.device != device or not v.is_contiguous():
         raise ValueError("%s: a number or a contiguous %s tensor [%d] on the scores' GPU is wanted" % (what, dtype, rows))
-    return v.data_ptr(), 0
+    return v.data_ptr()
 
 
 def sample(scores, noise, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, stream=None):
     """emr_sample: one index for each row of scores [rows, n] (or [n]; float32, bfloat16, float16), drawn with
     the given Exp(1) noise (float32, same shape). Parameters are numbers, or tensors [rows] (float32; top_k
     int32). Returns (index int32 [rows], log probability float32 [rows])."""
-    if not isinstance(scores, torch.Tensor) or scores.dim() not in (1, 2) or scores.device.type != "cuda":
+    if not isinstance(scores, torch.Tensor) or scores.dim() not in (1, 2) or not scores.is_cuda:
         raise ValueError("scores: a tensor [rows, n] or [n] on the GPU is wanted")
-    if noise.shape != scores.shape or noise.dtype != torch.float32 or noise.device != scores.device:
+    dev = scores.device
+    if noise.shape != scores.shape or noise.dtype is not torch.float32 or noise.device != dev:
         raise ValueError("noise: a float32 tensor in the shape of scores on the same GPU is wanted")
+    if stream is not None and stream != torch.cuda.current_stream(dev):
+        with torch.cuda.stream(stream):   # allocations belong to the stream that they are used on
+            return sample(scores, noise, temperature, top_k, top_p, min_p)
     if scores.dim() == 1:
         scores, noise = scores.unsqueeze(0), noise.unsqueeze(0)
     rows, n = scores.shape
-    kind = _dtype(scores.dtype, "scores")
-    dev = scores.device
-    t = _per_row(temperature, rows, torch.float32, dev, "temperature")
-    k = _per_row(top_k, rows, torch.int32, dev, "top_k")
-    p = _per_row(top_p, rows, torch.float32, dev, "top_p")
-    q = _per_row(min_p, rows, torch.float32, dev, "min_p")
-    with _on(stream):
-        if scores.stride(1) != 1:
-            scores = scores.contiguous()
-        if noise.stride(1) != 1:
-            noise = noise.contiguous()
-        index = torch.empty(rows, dtype=torch.int32, device=dev)
-        logp = torch.empty(rows, dtype=torch.float32, device=dev)
-        if rows:
-            _check(lib().emr_sample(scores.data_ptr(), kind, rows, n, scores.stride(0), noise.data_ptr(), noise.stride(0),
-                                    *t, *k, *p, *q, index.data_ptr(), logp.data_ptr(), _raw_stream(stream, dev)),
-                   "emr_sample")
+    kind = _DTYPES.get(scores.dtype)
+    if kind is None:
+        _dtype(scores.dtype, "scores")
+    tp = kp = pp = qp = None
+    if isinstance(temperature, torch.Tensor):
+        tp, temperature = _per_row(temperature, rows, torch.float32, dev, "temperature"), 0.0
+    if isinstance(top_k, torch.Tensor):
+        kp, top_k = _per_row(top_k, rows, torch.int32, dev, "top_k"), 0
+    if isinstance(top_p, torch.Tensor):
+        pp, top_p = _per_row(top_p, rows, torch.float32, dev, "top_p"), 0.0
+    if isinstance(min_p, torch.Tensor):
+        qp, min_p = _per_row(min_p, rows, torch.float32, dev, "min_p"), 0.0
+    s_row, s_col = scores.stride()
+    e_row, e_col = noise.stride()
+    if s_col != 1:
+        scores = scores.contiguous()
+        s_row = n
+    if e_col != 1:
+        noise = noise.contiguous()
+        e_row = n
+    index = torch.empty(rows, dtype=torch.int32, device=dev)
+    logp = torch.empty(rows, dtype=torch.float32, device=dev)
+    if rows:
+        status = lib().emr_sample(scores.data_ptr(), kind, rows, n, s_row, noise.data_ptr(), e_row, tp, temperature, kp,
+                                  top_k, pp, top_p, qp, min_p, index.data_ptr(), logp.data_ptr(),
+                                  torch._C._cuda_getCurrentRawStream(dev.index))
+        if status:
+            _check(status, "emr_sample")
     return index, logp
 
 
