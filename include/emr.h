@@ -635,6 +635,12 @@ emr_status emr_q8_quantize(const void *src, int32_t dtype, int32_t batch, int64_
                            int64_t batch_stride, int64_t row_stride, int64_t col_stride, const emr_q8 *q,
                            const emr_q8 *qt, void *stream);
 
+/* The same into both, except that qt holds the values that q stands for (emr_q8_quantize
+ * and emr_q8_transpose in one pass over src): what a training step keeps of its input. */
+emr_status emr_q8_quantize_held(const void *src, int32_t dtype, int32_t batch, int64_t rows, int64_t cols,
+                                int64_t batch_stride, int64_t row_stride, int64_t col_stride, const emr_q8 *q,
+                                const emr_q8 *qt, void *stream);
+
 /* qt ([cols][rows]) receives the values that q stands for, quantised again with
  * blocks along q's rows. As the scales are powers of two this is exact except for
  * values that fall below the normal range of their new block. */
@@ -679,19 +685,20 @@ typedef struct {
 } emr_dense;
 
 /* Forward pass: x is x_batch (1: shared by all networks, or w.batch) matrices [rows]
- * [w.cols] with the given strides (elements); out dense [w.batch][rows][w.rows]. With
- * keep != 0 the call leaves in x8 and slope what the backward pass needs, x and act'(z)
- * in 8 bits (an emr_q8 whose scales follow its values in the same memory, 16-byte
- * aligned); without it x8 is room only. emr_dense_forward_room gives the bytes of both:
- * slope 0 without keep or with the identity, x8 0 where the product reads x itself (few
- * rows; x8 may then be NULL). */
+ * [w.cols] with the given strides (elements); out dense [w.batch][rows][w.rows]. x8 is
+ * room for x in 8 bits (16-byte aligned). With keep != 0 the call leaves in xt and slope
+ * what the backward pass needs, the transpose of the 8-bit x (emr_q8_quantize_held) and
+ * act'(z) in 8 bits, each an emr_q8 whose scales follow its values in the same memory,
+ * 16-byte aligned. emr_dense_forward_room gives the bytes of the three: xt and slope 0
+ * without keep, slope 0 with the identity, x8 0 where the product reads x itself (few
+ * rows); a pointer of 0 bytes may be NULL. */
 emr_status emr_dense_forward_room(const emr_dense *layer, int32_t x_batch, int64_t rows, int32_t keep,
-                                  size_t *x_bytes, size_t *slope_bytes);
+                                  size_t *x_bytes, size_t *xt_bytes, size_t *slope_bytes);
 emr_status emr_dense_forward(const emr_dense *layer, const void *x, int32_t dtype, int32_t x_batch, int64_t rows,
                              int64_t batch_stride, int64_t row_stride, int64_t col_stride, void *out,
-                             int32_t out_dtype, int32_t keep, void *x8, void *slope, void *stream);
+                             int32_t out_dtype, int32_t keep, void *x8, void *xt, void *slope, void *stream);
 
-/* Backward pass from x8 and slope as a forward call with keep left them: dy dense
+/* Backward pass from xt and slope as a forward call with keep left them: dy dense
  * [w.batch][rows][w.rows] of dtype; dx [x_batch][rows][w.cols] (summed over the networks
  * where x was shared), dw [w.batch][w.rows][w.cols] and db [w.batch][w.rows] of
  * out_dtype, each NULL for none. With dz = dy * slope, in 8 bits from there on: dx =
@@ -699,7 +706,7 @@ emr_status emr_dense_forward(const emr_dense *layer, const void *x, int32_t dtyp
  * emr_dense_backward_room bytes, 16-byte aligned. */
 emr_status emr_dense_backward_room(const emr_dense *layer, int32_t x_batch, int64_t rows, size_t *bytes);
 emr_status emr_dense_backward(const emr_dense *layer, const void *dy, int32_t dtype, int32_t x_batch, int64_t rows,
-                              const void *x8, const void *slope, void *dx, void *dw, void *db, int32_t out_dtype,
+                              const void *xt, const void *slope, void *dx, void *dw, void *db, int32_t out_dtype,
                               void *ws, size_t ws_bytes, void *stream);
 
 /* Whether a bounded device-side wait of this library has given up since the last

@@ -31,23 +31,24 @@ size_t padded(size_t n) { return (n + 255) / 256 * 256; }
 }  // namespace
 
 extern "C" emr_status emr_dense_forward_room(const emr_dense* layer, int32_t x_batch, int64_t rows, int32_t keep, size_t* x_bytes,
-                                             size_t* slope_bytes) {
-  if (!x_bytes || !slope_bytes) return EMR_ERR_ARG;
+                                             size_t* xt_bytes, size_t* slope_bytes) {
+  if (!x_bytes || !xt_bytes || !slope_bytes) return EMR_ERR_ARG;
   const emr_status s = check(layer, x_batch, rows);
   if (s != EMR_OK) return s;
   *x_bytes = !keep && few_fused(rows, layer->w) ? 0 : packed_bytes(x_batch, rows, layer->w.cols);
+  *xt_bytes = keep ? packed_bytes(x_batch, layer->w.cols, rows) : 0;
   *slope_bytes = keep && layer->act != EMR_ACT_IDENTITY ? packed_bytes(layer->w.batch, rows, layer->w.rows) : 0;
   return EMR_OK;
 }
 
 extern "C" emr_status emr_dense_forward(const emr_dense* layer, const void* x, int32_t dtype, int32_t x_batch, int64_t rows,
                                         int64_t batch_stride, int64_t row_stride, int64_t col_stride, void* out, int32_t out_dtype,
-                                        int32_t keep, void* x8, void* slope, void* stream) {
-  size_t x_bytes = 0, slope_bytes = 0;
-  const emr_status s = emr_dense_forward_room(layer, x_batch, rows, keep, &x_bytes, &slope_bytes);
+                                        int32_t keep, void* x8, void* xt, void* slope, void* stream) {
+  size_t x_bytes = 0, xt_bytes = 0, slope_bytes = 0;
+  const emr_status s = emr_dense_forward_room(layer, x_batch, rows, keep, &x_bytes, &xt_bytes, &slope_bytes);
   if (s != EMR_OK) return s;
   if (!x || !out || !dtype_ok(dtype) || !dtype_ok(out_dtype) || batch_stride < 0 || row_stride < 0 || col_stride < 0 ||
-      (x_bytes && !x8) || (slope_bytes && !slope))
+      (x_bytes && !x8) || (xt_bytes && !xt) || (slope_bytes && !slope))
     return EMR_ERR_ARG;
   if (!x_bytes) {
     const int size = dtype_bytes(dtype), out_size = dtype_bytes(out_dtype);
@@ -61,7 +62,10 @@ extern "C" emr_status emr_dense_forward(const emr_dense* layer, const void* x, i
     return launch_few(f, static_cast<cudaStream_t>(stream));
   }
   const emr_q8 q = packed(x8, x_batch, rows, layer->w.cols);
-  const emr_status e = emr_q8_quantize(x, dtype, x_batch, rows, layer->w.cols, batch_stride, row_stride, col_stride, &q, nullptr, stream);
+  const emr_q8 t = packed(xt, x_batch, layer->w.cols, rows);
+  const emr_status e =
+      keep ? emr_q8_quantize_held(x, dtype, x_batch, rows, layer->w.cols, batch_stride, row_stride, col_stride, &q, &t, stream)
+           : emr_q8_quantize(x, dtype, x_batch, rows, layer->w.cols, batch_stride, row_stride, col_stride, &q, nullptr, stream);
   if (e != EMR_OK) return e;
   const emr_q8 d = packed(slope, layer->w.batch, rows, layer->w.rows);
   return emr_q8_matmul(&q, &layer->w, layer->bias, layer->act, 0, out, out_dtype, slope_bytes ? &d : nullptr, stream);
@@ -71,21 +75,21 @@ extern "C" emr_status emr_dense_backward_room(const emr_dense* layer, int32_t x_
   if (!bytes) return EMR_ERR_ARG;
   const emr_status s = check(layer, x_batch, rows);
   if (s != EMR_OK) return s;
-  const int64_t nets = layer->w.batch, n = layer->w.rows, k = layer->w.cols;
+  const int64_t nets = layer->w.batch, n = layer->w.rows;
   size_t sums = 0;
   const emr_status e = emr_q8_slope_workspace_size(int32_t(nets), rows, n, &sums);
   if (e != EMR_OK) return e;
-  *bytes = padded(packed_bytes(nets, rows, n)) + padded(packed_bytes(nets, n, rows)) + padded(packed_bytes(x_batch, k, rows)) + sums;
+  *bytes = padded(packed_bytes(nets, rows, n)) + padded(packed_bytes(nets, n, rows)) + sums;
   return EMR_OK;
 }
 
 extern "C" emr_status emr_dense_backward(const emr_dense* layer, const void* dy, int32_t dtype, int32_t x_batch, int64_t rows,
-                                         const void* x8, const void* slope, void* dx, void* dw, void* db, int32_t out_dtype,
+                                         const void* xt, const void* slope, void* dx, void* dw, void* db, int32_t out_dtype,
                                          void* ws, size_t ws_bytes, void* stream) {
   size_t need = 0;
   emr_status s = emr_dense_backward_room(layer, x_batch, rows, &need);
   if (s != EMR_OK) return s;
-  if (!dy || !x8 || !ws || !dtype_ok(dtype) || !dtype_ok(out_dtype) || (!dx && !dw && !db) ||
+  if (!dy || (dw && !xt) || !ws || !dtype_ok(dtype) || !dtype_ok(out_dtype) || (!dx && !dw && !db) ||
       (layer->act != EMR_ACT_IDENTITY && !slope) || (dx && !q8_ok(&layer->wt)) || reinterpret_cast<uintptr_t>(ws) % 16)
     return EMR_ERR_ARG;
   const int64_t nets = layer->w.batch, n = layer->w.rows, k = layer->w.cols;
@@ -96,9 +100,7 @@ extern "C" emr_status emr_dense_backward(const emr_dense* layer, const void* dy,
   p += padded(packed_bytes(nets, rows, n));
   const emr_q8 dzt = packed(p, nets, n, rows);
   p += padded(packed_bytes(nets, n, rows));
-  const emr_q8 xt = packed(p, x_batch, k, rows);
-  p += padded(packed_bytes(x_batch, k, rows));
-  const emr_q8 x = packed(const_cast<void*>(x8), x_batch, rows, k), d = packed(const_cast<void*>(slope), nets, rows, n);
+  const emr_q8 x = packed(const_cast<void*>(xt), x_batch, k, rows), d = packed(const_cast<void*>(slope), nets, rows, n);
   s = emr_q8_slope(dy, dtype, int32_t(nets), rows, n, layer->act != EMR_ACT_IDENTITY ? &d : nullptr, dx ? &dz : nullptr,
                    dw ? &dzt : nullptr, db, out_dtype, p, ws_bytes - size_t(p - static_cast<uint8_t*>(ws)), stream);
   if (s != EMR_OK) return s;
@@ -106,10 +108,6 @@ extern "C" emr_status emr_dense_backward(const emr_dense* layer, const void* dy,
     s = emr_q8_matmul(&dz, &layer->wt, nullptr, EMR_ACT_IDENTITY, x_batch < nets, dx, out_dtype, nullptr, stream);
     if (s != EMR_OK) return s;
   }
-  if (dw) {
-    s = emr_q8_transpose(&x, &xt, stream);
-    if (s != EMR_OK) return s;
-    s = emr_q8_matmul(&dzt, &xt, nullptr, EMR_ACT_IDENTITY, 0, dw, out_dtype, nullptr, stream);
-  }
+  if (dw) s = emr_q8_matmul(&dzt, &x, nullptr, EMR_ACT_IDENTITY, 0, dw, out_dtype, nullptr, stream);
   return s;
 }

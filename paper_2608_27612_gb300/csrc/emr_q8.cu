@@ -96,7 +96,8 @@ __device__ __forceinline__ void copy_ahead(void* to, const void* from, int have)
 
 // 128 x 128 tiles: row blocks to q, column blocks (the transpose) to qt, column sums to
 // sums[b][row tile][cols]. Mode 0: a dense source; 1: the values of an 8-bit matrix; 2: the
-// product of a dense matrix and an 8-bit one. A block goes through tiles gridDim.x apart
+// product of a dense matrix and an 8-bit one; 3: a dense source whose transpose is made of
+// the values that q holds. A block goes through tiles gridDim.x apart
 // and copies the next one into shared memory while it works on one; of the dense source a
 // thread reads back only what it copied itself. A warp holds the rows 8 warp .. 8 warp + 7 in registers, a
 // lane four columns of each. Column maxima and sums meet in shared memory over the 16
@@ -106,6 +107,7 @@ __device__ __forceinline__ void copy_ahead(void* to, const void* from, int have)
 template <int kMode, typename T, bool kVector>
 __global__ void __launch_bounds__(kTileThreads, 2) q8_tile_kernel(Dense<T, kVector> src, emr_q8 other, int64_t rows, int64_t cols,
                                                                   uint32_t tiles, emr_q8 q, emr_q8 qt, float* sums) {
+  constexpr bool kFromQ8 = kMode == 1 || kMode == 2;
   extern __shared__ __align__(16) uint8_t ahead[];  // [8][threads] of the dense source, then two tiles of codes
   __shared__ float4 part[16][32];
   __shared__ uint32_t bytes[128 * 32];
@@ -152,7 +154,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) q8_tile_kernel(Dense<T, kVect
         }
       }
     }
-    if (kMode != 0) {
+    if (kFromQ8) {
       // 16 bytes a thread, to be read by other threads
       const uint8_t* from = other.values + (p.b * rows + p.rt * 128) * row_bytes + p.ct * 128;
 #pragma unroll
@@ -176,13 +178,13 @@ __global__ void __launch_bounds__(kTileThreads, 2) q8_tile_kernel(Dense<T, kVect
   for (uint32_t t = blockIdx.x; t < tiles; t += gridDim.x, turn ^= 1) {
     const Place p = place(t);
     asm volatile("cp.async.wait_group 0;" ::: "memory");
-    if (kMode != 0) __syncthreads();
+    if (kFromQ8) __syncthreads();
     float4 v[8];
     const uint32_t scale_bytes = next_scale;
 #pragma unroll
     for (int i = 0; i < 8; i++) {
       if (kMode != 1) v[i] = dense[i * kTileThreads].floats();
-      if (kMode != 0) {
+      if (kFromQ8) {
         const float s = q8_scale(__shfl_sync(0xffffffffu, scale_bytes, i));
         float4 d = q8_unpack4(*reinterpret_cast<const uint32_t*>(codes + turn * 16384 + (first + i) * 128 + lane * 4));
         d = make_float4(d.x * s, d.y * s, d.z * s, d.w * s);
@@ -210,7 +212,13 @@ __global__ void __launch_bounds__(kTileThreads, 2) q8_tile_kernel(Dense<T, kVect
 #pragma unroll
       for (int i = 0; i < 8; i++) {
         const uint32_t byte = q8_warp_scale(v[i]);
-        if (i < p.have) *reinterpret_cast<uint32_t*>(out) = q8_pack4(v[i].x, v[i].y, v[i].z, v[i].w, q8_inverse(byte));
+        const uint32_t codes4 = q8_pack4(v[i].x, v[i].y, v[i].z, v[i].w, q8_inverse(byte));
+        if (i < p.have) *reinterpret_cast<uint32_t*>(out) = codes4;
+        if (kMode == 3) {
+          const float4 d = q8_unpack4(codes4);
+          const float s = q8_scale(byte);
+          v[i] = make_float4(d.x * s, d.y * s, d.z * s, d.w * s);
+        }
         out += row_bytes;
         if (lane == i) mine = byte;
       }
@@ -304,7 +312,7 @@ emr_status launch_tile(const Dense<T, kVector>& src, const emr_q8* other, int64_
   const int64_t tiles = batch * q8_blocks(rows) * q8_blocks(cols);
   if (tiles > kMaxGrid) return EMR_ERR_RANGE;
   static std::atomic<uint64_t> done{0};
-  const int smem = (kMode != 1 ? int(sizeof(Four<T>)) * 8 * kTileThreads : 0) + (kMode != 0 ? 2 * 16384 : 0);
+  const int smem = (kMode != 1 ? int(sizeof(Four<T>)) * 8 * kTileThreads : 0) + (kMode == 1 || kMode == 2 ? 2 * 16384 : 0);
   int dev = 0, sms = 0;
   if (!device_sms(&dev, &sms) || !allow_smem(q8_tile_kernel<kMode, T, kVector>, smem, dev, done)) return EMR_ERR_CUDA;
   const emr_q8 none{};
@@ -381,6 +389,20 @@ extern "C" emr_status emr_q8_quantize(const void* src, int32_t dtype, int32_t ba
     // row blocks alone: a warp a row while there are few tiles, else by tiles, which copy ahead
     const bool tiled = qt || int64_t(batch) * q8_blocks(rows) * q8_blocks(cols) >= kTiledFrom;
     return tiled ? launch_tile<0>(d, nullptr, batch, rows, cols, q, qt, nullptr, st) : launch_rows(d, batch, rows, cols, q, st);
+  });
+}
+
+extern "C" emr_status emr_q8_quantize_held(const void* src, int32_t dtype, int32_t batch, int64_t rows, int64_t cols,
+                                           int64_t batch_stride, int64_t row_stride, int64_t col_stride, const emr_q8* q,
+                                           const emr_q8* qt, void* stream) {
+  if (!src || !dtype_ok(dtype) || batch < 1 || rows < 1 || cols < 1 || batch_stride < 0 || row_stride < 0 || col_stride < 0)
+    return EMR_ERR_ARG;
+  if (rows > kQ8MaxDim || cols > kQ8MaxDim) return EMR_ERR_RANGE;
+  if (!same_shape(q, batch, rows, cols) || !same_shape(qt, batch, cols, rows) || reinterpret_cast<uintptr_t>(src) % dtype_bytes(dtype))
+    return EMR_ERR_ARG;
+  const DenseArgs args{src, dtype, batch, rows, cols, batch_stride, row_stride, col_stride};
+  return with_dense(args, [&](auto d) {
+    return launch_tile<3>(d, nullptr, batch, rows, cols, q, qt, nullptr, static_cast<cudaStream_t>(stream));
   });
 }
 

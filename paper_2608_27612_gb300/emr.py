@@ -101,13 +101,14 @@ def lib() -> C.CDLL:
             "emr_compact_records": [vp, vp, vp, vp, sz, vp, vp, vp, i64, vp, vp, vp, sz, vp],
             "emr_q8_size": [i32, i64, i64, vp, vp],
             "emr_q8_quantize": [vp, i32, i32, i64, i64, i64, i64, i64, vp, vp, vp],
+            "emr_q8_quantize_held": [vp, i32, i32, i64, i64, i64, i64, i64, vp, vp, vp],
             "emr_q8_transpose": [vp, vp, vp],
             "emr_q8_dequantize": [vp, vp, i32, vp],
             "emr_q8_slope_workspace_size": [i32, i64, i64, vp],
             "emr_q8_slope": [vp, i32, i32, i64, i64, vp, vp, vp, vp, i32, vp, sz, vp],
             "emr_q8_matmul": [vp, vp, vp, i32, i32, vp, i32, vp, vp],
-            "emr_dense_forward_room": [vp, i32, i64, i32, vp, vp],
-            "emr_dense_forward": [vp, vp, i32, i32, i64, i64, i64, i64, vp, i32, i32, vp, vp, vp],
+            "emr_dense_forward_room": [vp, i32, i64, i32, vp, vp, vp],
+            "emr_dense_forward": [vp, vp, i32, i32, i64, i64, i64, i64, vp, i32, i32, vp, vp, vp, vp],
             "emr_dense_backward_room": [vp, i32, i64, vp],
             "emr_dense_backward": [vp, vp, i32, i32, i64, vp, vp, vp, vp, vp, i32, vp, sz, vp],
             "emr_device_error": [vp, vp],
@@ -696,6 +697,16 @@ def q8_quantize(x, q: Q8 | None = None, qt: Q8 | None = None, stream=None):
     return q, qt
 
 
+def q8_quantize_held(x, stream=None):
+    """emr_q8_quantize_held: (q, qt) of x, qt made of the values that q holds."""
+    x = _matrices(x, "x")
+    with _on(stream):
+        q, qt = Q8(*x.shape, device=x.device), Q8(x.shape[0], x.shape[2], x.shape[1], device=x.device)
+        _check(lib().emr_q8_quantize_held(x.data_ptr(), _dtype(x.dtype, "x"), *x.shape, *x.stride(), q.ref, qt.ref,
+                                          _stream(stream)), "emr_q8_quantize_held")
+    return q, qt
+
+
 def q8_transpose(q: Q8, qt: Q8 | None = None, stream=None) -> Q8:
     """emr_q8_transpose: the transpose of what q holds, with blocks along q's rows."""
     with _on(stream):
@@ -760,8 +771,9 @@ def device_error(stream=None) -> int:
 
 
 class Saved(NamedTuple):
-    """What a training step keeps between the passes: x and act'(z) in 8 bits (slope None: identity)."""
-    x: Q8
+    """What a training step keeps between the passes: the transpose [nx, k, m] of x in 8 bits, as the weight
+    gradient reads it, and act'(z) [nets, m, n] in 8 bits (None: identity)."""
+    xt: Q8
     slope: Q8 | None
 
 
@@ -810,8 +822,9 @@ class DenseLayer:
         """Whether a forward pass without keep needs memory for x in 8 bits (emr_dense_forward_room)."""
         got = self._room.get((nx, m))
         if got is None:
-            a, b = C.c_size_t(), C.c_size_t()
-            _check(lib().emr_dense_forward_room(self._ref, nx, m, 0, C.byref(a), C.byref(b)), "emr_dense_forward_room")
+            a, b, c = C.c_size_t(), C.c_size_t(), C.c_size_t()
+            _check(lib().emr_dense_forward_room(self._ref, nx, m, 0, C.byref(a), C.byref(b), C.byref(c)),
+                   "emr_dense_forward_room")
             if len(self._room) > 64:
                 self._room.clear()
             got = self._room[(nx, m)] = a.value > 0
@@ -835,18 +848,21 @@ class DenseLayer:
             with torch.cuda.stream(stream):   # allocations belong to the stream that they are used on
                 return self._forward(x, out_dtype, None, keep)
         out = torch.empty((self.nets, m, self.n), dtype=out_dtype, device=dev)
-        xq = slope = xp = sp = None
+        xq = xt = slope = xp = tp = sp = None
         if keep or self._needs_room(nx, m):
             xq = torch.empty(sum(_q8_bytes(nx, m, k)), dtype=torch.uint8, device=dev)
             xp = xq.data_ptr()
+        if keep:
+            xt = torch.empty(sum(_q8_bytes(nx, k, m)), dtype=torch.uint8, device=dev)
+            tp = xt.data_ptr()
         if keep and self.act != ACT_IDENTITY:
             slope = torch.empty(sum(_q8_bytes(self.nets, m, self.n)), dtype=torch.uint8, device=dev)
             sp = slope.data_ptr()
         status = _lib.emr_dense_forward(self._ref, x.data_ptr(), kind, nx, m, *x.stride(), out.data_ptr(), out_kind,
-                                        1 if keep else 0, xp, sp, torch._C._cuda_getCurrentRawStream(dev.index))
+                                        1 if keep else 0, xp, tp, sp, torch._C._cuda_getCurrentRawStream(dev.index))
         if status:
             _check(status, "emr_dense_forward")
-        return out, xq, slope
+        return out, xt, slope
 
     def forward(self, x, out_dtype=torch.float32, stream=None):
         """y [nets, m, n] of out_dtype. m = 0 gives an empty result."""
@@ -856,27 +872,28 @@ class DenseLayer:
         """(y, saved): saved holds x and act'(z) in 8 bits for backward."""
         if not self.train:
             raise ValueError("forward_train: the layer was made with train=False")
-        y, xq, slope = self._forward(x, out_dtype, stream, True)
+        y, xt, slope = self._forward(x, out_dtype, stream, True)
         nx, m = (x.shape[0], x.shape[1]) if x.dim() == 3 else (1, x.shape[0])
-        return y, Saved(Q8.of(xq, nx, m, self.k), Q8.of(slope, self.nets, m, self.n) if slope is not None else None)
+        return y, Saved(Q8.of(xt, nx, self.k, m), Q8.of(slope, self.nets, m, self.n) if slope is not None else None)
 
     def backward(self, dy, saved: Saved, out_dtype=torch.float32, stream=None):
         """(dx, dw, db) of out_dtype for dy [nets, m, n]: dx [1 or nets, m, k] as forward_train took x (summed
         over the networks where x was shared), dw [nets, n, k], db [nets, n] (also without a bias)."""
         q, slope = saved
+        m = q.cols
         dy = _matrices(dy, "dy")
-        if tuple(dy.shape) != (self.nets, q.rows, self.n) or dy.device != self.device:
-            raise ValueError("dy: shape %s is wanted, got %s" % ((self.nets, q.rows, self.n), tuple(dy.shape)))
+        if tuple(dy.shape) != (self.nets, m, self.n) or dy.device != self.device:
+            raise ValueError("dy: shape %s is wanted, got %s" % ((self.nets, m, self.n), tuple(dy.shape)))
         kind, out_kind = _dtype(dy.dtype, "dy"), _dtype(out_dtype, "out_dtype")
         room = C.c_size_t()
-        _check(lib().emr_dense_backward_room(self._ref, q.batch, q.rows, C.byref(room)), "emr_dense_backward_room")
+        _check(lib().emr_dense_backward_room(self._ref, q.batch, m, C.byref(room)), "emr_dense_backward_room")
         with _on(stream):
             dy = dy.contiguous()
-            dx = torch.empty((q.batch, q.rows, self.k), dtype=out_dtype, device=self.device)
+            dx = torch.empty((q.batch, m, self.k), dtype=out_dtype, device=self.device)
             dw = torch.empty((self.nets, self.n, self.k), dtype=out_dtype, device=self.device)
             db = torch.empty((self.nets, self.n), dtype=out_dtype, device=self.device)
             ws = torch.empty(room.value, dtype=torch.uint8, device=self.device)
-            _check(lib().emr_dense_backward(self._ref, dy.data_ptr(), kind, q.batch, q.rows, q.data.data_ptr(),
+            _check(lib().emr_dense_backward(self._ref, dy.data_ptr(), kind, q.batch, m, q.data.data_ptr(),
                                             slope.data.data_ptr() if slope is not None else None, dx.data_ptr(),
                                             dw.data_ptr(), db.data_ptr(), out_kind, ws.data_ptr(), room.value,
                                             _raw_stream(stream, self.device)), "emr_dense_backward")

@@ -108,6 +108,15 @@ def test_transpose(shape):
     assert same(back(emr.q8_transpose(q)), OD.held(np.swapaxes(back(q), 1, 2)))
 
 
+@pytest.mark.parametrize("shape", [(1, 1, 5), (2, 130, 257), (1, 400, 640)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_quantize_held(shape, dtype):
+    x = normal(3, *shape, spread=3.0, dtype=dtype)
+    for v in (x, x.transpose(1, 2).contiguous().transpose(1, 2)):
+        q, qt = emr.q8_quantize_held(v)
+        assert same(back(q), OD.held(f64(x))) and same(back(qt), OD.held(np.swapaxes(back(q), 1, 2)))
+
+
 # ---- the product --------------------------------------------------------------------------------------
 
 def product_case(nets_a, nets_w, m, n, k, seed=4):
@@ -270,10 +279,10 @@ def test_layer_gradients(act, nets, shared, m, n, k):
     assert m <= 16 or same(f64(y), f64(layer.forward(x)))
     dx, dw, db = layer.backward(dy, saved)
     xh, wh = OD.held(f64(x)), OD.held(f64(w))
-    assert same(back(saved[0]), xh)
+    assert same(back(saved.xt), OD.held(np.swapaxes(xh, 1, 2)))
     z, _ = OD.product(xh, wh, f64(b))
     # the formulas, from the slopes that were kept
-    d = back(saved[1]) if act != "identity" else np.ones_like(z)
+    d = back(saved.slope) if act != "identity" else np.ones_like(z)
     dz = np.float32(f64(dy)) * np.float32(d)         # one rounding in 32 bits, as kept
     dz = dz.astype(np.float64)
     assert np.all(np.abs(f64(db) - dz.sum(1)) <= (m + 2) * 2.0 ** -23 * np.abs(dz).sum(1))
