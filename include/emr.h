@@ -734,7 +734,7 @@ emr_status emr_device_error(int32_t *code, void *stream);
  * Reads scores once where a row's share of them fits into the shared memory of its
  * blocks (up to about 350,000 entries of 4 bytes). Errors: EMR_ERR_ARG (null or
  * misaligned pointer, size below 1, negative stride, unknown type), EMR_ERR_RANGE (n
- * above 2^31 - 1, rows above 2^27), EMR_ERR_CUDA. */
+ * above 2^31 - 2^20, rows above 2^27), EMR_ERR_CUDA. */
 emr_status emr_sample(const void *scores, int32_t dtype, int32_t rows, int64_t n, int64_t row_stride,
                       const float *noise, int64_t noise_stride, const float *temperature, float temperature_all,
                       const int32_t *top_k, int32_t top_k_all, const float *top_p, float top_p_all,

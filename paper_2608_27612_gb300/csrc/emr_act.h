@@ -22,6 +22,11 @@ __device__ __forceinline__ float fast_rcp(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
+__device__ __forceinline__ float fast_log2(float x) {
+  float r;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
 constexpr float kLog2E = 0x1.715476p+0f;
 
 // Element i of sin and cos where the argument is large; i is not known at compile time, so the

@@ -36,7 +36,7 @@ typedef unsigned long long u64;
 
 constexpr int kMaxCluster = 8;
 constexpr float kSpan = 16.f;    // the equal steps cover w in (e^-16, 1]; the last one takes the rest
-constexpr float kNear = 4e-5f;   // of the draw's first computation
+constexpr float kNear = 6e-5f;   // of the draw's first computation, in units of log2
 constexpr float kLackUnit = 1048576.f;
 
 struct Args {
@@ -62,6 +62,15 @@ __device__ __forceinline__ uint32_t order_key(float s) {
   const uint32_t u = __float_as_uint(s + 0.f);  // -0 counts as 0
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
+// Predicated, not branched around.
+__device__ __forceinline__ void shared_add(bool go, uint32_t at, uint32_t v) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p red.shared.add.u32 [%0], %1;\n\t}" ::"r"(at), "r"(v), "r"(uint32_t(go)) : "memory");
+}
+__device__ __forceinline__ uint4 shared_load(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
 __device__ __forceinline__ float key_score(uint32_t k) {
   return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
 }
@@ -71,7 +80,7 @@ __device__ __forceinline__ float key_score(uint32_t k) {
 struct Drawn {
   uint32_t key, at;
   float mass;       // w of what was drawn from
-  uint32_t unsure;  // the largest rough key that might stand before the best
+  uint32_t unsure;  // order_key of the largest rough key that might stand before the best
 };
 __device__ __forceinline__ uint32_t draw_key(float k) { return k >= 0.f ? __float_as_uint(k) + 1 : 0; }
 __device__ __forceinline__ float draw_value(uint32_t k) { return k ? __uint_as_float(k - 1) : -1.f; }
@@ -96,12 +105,13 @@ struct Row {
   cg::cluster_group cluster;
   const Args& a;
   int tid, threads, lane, warp, warps, rank, blocks, phase, turn;
-  int64_t lo;       // first entry of this block's slice
+  int lo;           // first entry of this block's slice
   int count;        // its entries, the first of them `skip` entries after a multiple of 16 bytes
   int skip, groups, held;  // groups of 16 bytes that they lie in, and those in shared memory
   const T* global;  // the slice in memory
   uint4* data;      // and in shared memory
-  const float* noise;
+  const float* noise;   // of the row
+  uint32_t data_at, counts_at, lacks_at;  // addresses in shared memory, for the inner loops
   uint32_t *counts, *lacks;
   u64 *sums, *list, *sorted;
   uint4* scratch;   // [2][32], by turns: a turn's values are read by all before the next but one writes
@@ -114,8 +124,11 @@ struct Row {
   bool counted;     // a histogram has been made
   float s_max, temperature, min_w, exp2_per;
   bool top_infinite;  // only the entries of +infinity count, as score 0
-  // the draw: a thread's largest and second largest w / noise as computed roughly, and its w
+  // the draw: a thread's largest and second largest log2(w / noise) as computed roughly, and its w
+  // (needed unless the histogram has told it)
   float rough, rough_second, mass;
+  bool need_mass;
+  float min_log2;   // least log2 w that stays, with the margin
   int32_t rough_at;
   u64 bound;        // where the first block knows it: the last entry that stays
 
@@ -144,7 +157,7 @@ struct Row {
 #pragma unroll
       for (int u = 0; u < kAhead; u++) {
         const int at = g + u * threads;
-        if (at < held) v[u].u = data[at];
+        if (at < held) v[u].u = shared_load(data_at + at * 16);
         else v[u] = fetch(at);
       }
       float s[kAhead][kG];
@@ -176,15 +189,12 @@ struct Row {
   __device__ __forceinline__ float weight(float s) const { return expf(__fdiv_rn(s - s_max, temperature)); }
   __device__ __forceinline__ float rough_weight(float s) const { return fast_exp2((s - s_max) * exp2_per); }
   __device__ __forceinline__ u64 fixed(float w) const { return __float2ull_rn(w * __int_as_float((127 + a.fix) << 23)); }
-  // Step of a score, as a number in float: rises as the score falls. Rounded with the 2^23 shift, not
+  // Step of a score, 2^23 up, as a float: rises as the score falls. Rounded by that shift, not
   // converted: conversions take a quarter of the rate.
-  __device__ __forceinline__ float step_at(float s, float per, float* t) const {
-    *t = fminf((s_max - s) * per, float(a.bins - 1));
-    return fmaxf(*t - 0.5f, 0.f) + 0x1p+23f;
-  }
+  __device__ __forceinline__ float step_up(float s, float per) const { return fmaxf(fmaf(s_max - s, per, -0.5f), 0.f) + 0x1p+23f; }
+  __device__ __forceinline__ float last_up() const { return float(a.bins - 1) + 0x1p+23f; }
   __device__ __forceinline__ int step_of(float s, float per) const {
-    float t;
-    return int(__float_as_uint(step_at(s, per, &t)) & 0x7fffffu);
+    return int(__float_as_uint(fminf(step_up(s, per), last_up())) & 0x7fffffu);
   }
 
   __device__ void sync() {
@@ -282,18 +292,18 @@ struct Row {
     return kept + more;
   }
 
-  __device__ __forceinline__ bool kept(uint32_t key, int64_t at, uint32_t bound_key, int64_t bound_at) const {
+  __device__ __forceinline__ bool kept(uint32_t key, uint32_t at, uint32_t bound_key, uint32_t bound_at) const {
     return key > bound_key || (key == bound_key && key != 0 && at <= bound_at);
   }
 
   // ---- lists -----------------------------------------------------------------------------
 
   // One entry to the list of the row's first block (dropped past its room, but counted).
-  __device__ __forceinline__ void list_add(uint32_t key, int64_t at) {
+  __device__ __forceinline__ void list_add(uint32_t key, uint32_t at) {
     int* const size = blocks > 1 ? cluster.map_shared_rank(list_size + lists, 0) : list_size + lists;
     u64* const to = blocks > 1 ? cluster.map_shared_rank(list, 0) : list;
     const int place = atomicAdd(size, 1);
-    if (place < a.cap) to[place] = (u64(key) << 32) | uint32_t(~uint32_t(at));
+    if (place < a.cap) to[place] = (u64(key) << 32) | uint32_t(~at);
   }
   __device__ int list_end() {
     sync();
@@ -462,19 +472,16 @@ struct Row {
     const int last = a.bins - 1;
     float below = 0.f;
     each([&](float s, int i) {
-      if (!(s > -INFINITY) || !in(s, lo + i)) return;
-      float t;
-      const float step = step_at(s, per, &t);
-      const int at = int(__float_as_uint(step) & 0x7fffffu);
-      atomicAdd(&counts[at], 1u);
+      const bool ok = (s > -INFINITY) & in(s, uint32_t(lo + i));
+      const float up = fminf(step_up(s, per), last_up());
+      const int at = int(__float_as_uint(up) & 0x7fffffu);
+      shared_add(ok, counts_at + at * 4, 1u);
       if (by_mass) {
-        if (at == last) {
-          below += rough_weight(s);
-        } else {  // 1 - e^-x to x^4 / 24 < 3e-7
-          const float x = fmaxf(t - (step - 0x1p+23f), 0.f) * width;
-          const float lack = x * fmaf(x, fmaf(x, 1.f / 6.f, -0.5f), 1.f) * kLackUnit + 0x1p+23f;
-          atomicAdd(&lacks[at], __float_as_uint(lack) & 0x7fffffu);
-        }
+        if (ok && at == last) below += rough_weight(s);
+        // 1 - e^-x to x^4 / 24 < 3e-7
+        const float x = fmaxf(fmaf(s_max - s, per, 0x1p+23f - up), 0.f) * width;
+        const float lack = x * fmaf(x, fmaf(x, 1.f / 6.f, -0.5f), 1.f) * kLackUnit + 0x1p+23f;
+        shared_add(ok & (at != last), lacks_at + at * 4, __float_as_uint(lack) & 0x7fffffu);
       }
     });
     if (__syncthreads_or(below > 0.f)) below = block_sum(below);
@@ -490,17 +497,17 @@ struct Row {
   // Moves the bound (key, index) to the end of the prefix: `k` entries, or, by mass, the entries
   // before which less than p times the kept w lies. With by_mass the entries of the steps
   // before the last are drawn from on the way, and *drawn tells that only the list remains.
-  __device__ void select(bool by_mass, int64_t k, float p, uint32_t& bound_key, int64_t& bound_at, bool* drawn) {
+  __device__ void select(bool by_mass, int64_t k, float p, uint32_t& bound_key, uint32_t& bound_at, bool* drawn) {
     const uint32_t bk = bound_key;
-    const int64_t ba = bound_at;
-    const float bs = bk ? key_score(bk) : -INFINITY;
+    const uint32_t ba = bound_at;
+    const float bs = bk ? key_score(bk) : -INFINITY;  // no bound: every score that is not masked is above it
     const float per = fminf(float(a.bins - 1) / (kSpan * temperature), 3e38f);
-    Found f = find_step(by_mass, by_mass ? 0 : u64(k), p, per, [&](float s, int64_t at) { return s > bs || (s == bs && at <= ba); });
+    Found f = find_step(by_mass, by_mass ? 0 : u64(k), p, per, [&](float s, uint32_t at) { return bool(int(s > bs) | (int(s == bs) & int(at <= ba))); });
     const u64 target = f.target;
     const int step = f.bin;
     uint32_t prefix = 0;
     int shift = 32;  // key bits from `shift` up are fixed to prefix
-    auto in = [&](uint32_t key, int64_t at) {
+    auto in = [&](uint32_t key, uint32_t at) {
       return kept(key, at, bk, ba) && (shift == 32 || (key >> shift) == prefix) && step_of(key_score(key), per) == step;
     };
     u64 before = f.before;
@@ -508,7 +515,7 @@ struct Row {
     while (size > a.cap && shift > 0) {
       const int next = shift - 8;
       // larger bytes first
-      f = find(by_mass, 256, target, in, [&](float, uint32_t key, int64_t) { return 255 - int((key >> next) & 255u); }, before);
+      f = find(by_mass, 256, target, in, [&](float, uint32_t key, uint32_t) { return 255 - int((key >> next) & 255u); }, before);
       prefix = (prefix << 8) | uint32_t(255 - f.bin);
       shift = next;
       before = f.before;
@@ -518,12 +525,28 @@ struct Row {
       const bool with_draw = by_mass && shift == 32;
       if (with_draw) {
         *drawn = true;
-        draw([&](float s, int64_t at) {
-          if (!(s > bs || (s == bs && at <= ba))) return false;
-          const int b = step_of(s, per);
-          if (b == step) list_add(order_key(s), at);
-          return b < step;
-        });
+        const float here = float(step) + 0x1p+23f;
+        // without min-p the histogram has the w of all entries before the step
+        need_mass = min_w > 0.f;
+        if (!need_mass && rank == 0 && tid == 0) mass = float(before) * __int_as_float((127 - a.fix) << 23);
+        draw([&](float s, uint32_t at) {
+               return bool(int(s > -INFINITY) & int(step_up(s, per) < here) & (int(s > bs) | (int(s == bs) & int(at <= ba))));
+             },
+             [&](const float(&s)[kAhead][kG], int i) {
+               bool any = false;
+#pragma unroll
+               for (int u = 0; u < kAhead; u++)
+#pragma unroll
+                 for (int j = 0; j < kG; j++) any |= fminf(step_up(s[u][j], per), last_up()) == here;
+               if (!any) return;
+#pragma unroll
+               for (int u = 0; u < kAhead; u++)
+#pragma unroll
+                 for (int j = 0; j < kG; j++) {
+                   const uint32_t key = order_key(s[u][j]), at = uint32_t(lo + i + u * threads * kG + j);
+                   if (kept(key, at, bk, ba) && step_of(s[u][j], per) == step) list_add(key, at);
+                 }
+             });
       } else {
         each([&](float s, int i) {
           const uint32_t key = order_key(s);
@@ -548,7 +571,7 @@ struct Row {
             const u64 ahead = run + scan(w, &all);
             if (j < m && ahead < target) {
               last = uint32_t(j) + 1;
-              if (with_draw) consider(true, s, int64_t(uint32_t(~uint32_t(sorted[j]))), noise[uint32_t(~uint32_t(sorted[j]))]);
+              if (with_draw) need_mass = true, consider(true, s, ~uint32_t(sorted[j]), noise[~uint32_t(sorted[j])]);
             }
             run += all;
           }
@@ -562,7 +585,7 @@ struct Row {
       }
       e = row_max(e);
       bound_key = uint32_t(e >> 32);
-      bound_at = int64_t(uint32_t(~uint32_t(e)));
+      bound_at = ~uint32_t(e);
       return;
     }
     // equal scores: the first `want` of them by index
@@ -580,13 +603,13 @@ struct Row {
       const int above = next + 8;
       const uint32_t fixed_bits = ahead;
       f = find(false, 256, u64(want),
-               [&](uint32_t x, int64_t at) { return x == key && at <= (x == bk ? ba : INT64_MAX) && (above == 32 || (uint32_t(at) >> above) == fixed_bits); },
-               [&](float, uint32_t, int64_t at) { return int((uint32_t(at) >> next) & 255u); }, passed);
+               [&](uint32_t x, uint32_t at) { return x == key && at <= (x == bk ? ba : 0xffffffffu) && (above == 32 || (at >> above) == fixed_bits); },
+               [&](float, uint32_t, uint32_t at) { return int((at >> next) & 255u); }, passed);
       ahead = (ahead << 8) | uint32_t(f.bin);
       passed = f.before;
     }
     bound_key = key;
-    bound_at = int64_t(ahead);
+    bound_at = ahead;
   }
 
   // A score that is at most the k-th largest of the row (its key), from the threads' own largest.
@@ -612,10 +635,13 @@ struct Row {
 
   // ---- the draw --------------------------------------------------------------------------
 
-  __device__ __forceinline__ void consider(bool stays, float s, int64_t at, float e) {
-    const float w = stays ? rough_weight(s) : 0.f;
-    mass += w >= min_w ? w : 0.f;
-    const float key = stays && w >= min_w * (1.f - kNear) ? w * fast_rcp(e) : -1.f;
+  __device__ __forceinline__ void consider(bool stays, float s, uint32_t at, float e) {
+    const float x = (s - s_max) * exp2_per;
+    if (need_mass) {
+      const float w = stays ? fast_exp2(x) : 0.f;
+      mass += w >= min_w ? w : 0.f;
+    }
+    const float key = stays && x >= min_log2 ? x - fast_log2(e) : -INFINITY;
     rough_second = fmaxf(rough_second, fminf(rough, key));
     const bool first = key > rough;
     rough = first ? key : rough;
@@ -629,45 +655,49 @@ struct Row {
   // The thread's candidate in full; unsure where it has another one near or its w is near the least
   // that stays.
   __device__ __forceinline__ Drawn candidate(float s) const {
-    Drawn d{0, 0xffffffffu, mass, draw_key(rough_second)};
+    Drawn d{0, 0xffffffffu, mass, order_key(rough_second)};
     if (rough_at >= 0) {
       d.key = exact(s, noise[rough_at]);
       if (d.key) d.at = uint32_t(rough_at);
-      else d.unsure = draw_key(rough);
+      else d.unsure = order_key(rough);
     }
     return d;
   }
   __device__ __forceinline__ bool sure(const Drawn& d) const {
-    return !d.unsure || draw_value(d.unsure) < draw_value(d.key) * (1.f - kNear);
+    return !d.unsure || key_score(d.unsure) < fast_log2(draw_value(d.key)) - kNear;
   }
-  // Draws from the entries for which in(score, index) holds.
-  template <typename In>
-  __device__ __forceinline__ void draw(In in) {
+  // Draws from the entries for which in(score, index) holds, which does for no masked score; also(scores,
+  // i) sees all.
+  template <typename In, typename Also>
+  __device__ __forceinline__ void draw(In in, Also also) {
     const bool vector = a.noise_vector && skip % 4 == 0;
+    const float* const own = noise + lo;
     each_group([&](const float(&s)[kAhead][kG], int i) {
       bool stay[kAhead][kG];
       float e[kAhead][kG];
 #pragma unroll
       for (int u = 0; u < kAhead; u++) {
         const int at = i + u * threads * kG;
-        const bool there = at < count;
         bool any = false;
 #pragma unroll
         for (int j = 0; j < kG; j++) {
-          stay[u][j] = there && s[u][j] > -INFINITY && in(s[u][j], lo + at + j);
+          stay[u][j] = in(s[u][j], uint32_t(lo + at + j));
           any |= stay[u][j];
         }
-        if (any && vector && at >= 0 && at + kG <= count) {
+        if (vector && at >= 0 && at + kG <= count) {
+          if (any) {
 #pragma unroll
-          for (int j = 0; j < kG; j += 4) {
-            const float4 f = __ldcs(reinterpret_cast<const float4*>(noise + lo + at + j));
-            e[u][j] = f.x, e[u][j + 1] = f.y, e[u][j + 2] = f.z, e[u][j + 3] = f.w;
+            for (int j = 0; j < kG; j += 4) {
+              const float4 f = __ldcs(reinterpret_cast<const float4*>(own + at + j));
+              e[u][j] = f.x, e[u][j + 1] = f.y, e[u][j + 2] = f.z, e[u][j + 3] = f.w;
+            }
           }
-        } else {
+        } else if (any) {
 #pragma unroll
-          for (int j = 0; j < kG; j++) e[u][j] = stay[u][j] ? noise[lo + at + j] : 1.f;
+          for (int j = 0; j < kG; j++) e[u][j] = stay[u][j] ? own[at + j] : 1.f;
         }
       }
+      also(s, i);
 #pragma unroll
       for (int u = 0; u < kAhead; u++) {
         if (i + u * threads * kG >= count) break;
@@ -687,15 +717,15 @@ struct Row {
       const u64 e = row_max(bound);
       Drawn all{0, 0xffffffffu, 0.f, 0};
       each([&](float v, int i) {
-        const int64_t at = lo + i;
+        const uint32_t at = uint32_t(lo + i);
         if (!(v > -INFINITY) || !kept_by(v, at, e)) return;
         const uint32_t key = exact(v, noise[at]);
-        if (key > all.key) all.key = key, all.at = uint32_t(at);
+        if (key > all.key) all.key = key, all.at = at;
       });
       const Drawn best = row_best(all);
       got.key = best.key, got.at = best.at;
     }
-    if (rank == 0 && tid == 0) put(got, got.key ? value(global[got.at - lo]) : 0.f, index, logp);
+    if (rank == 0 && tid == 0) put(got, got.key ? value(global[int(got.at) - lo]) : 0.f, index, logp);
   }
   __device__ void put(const Drawn& d, float s, int32_t* index, float* logp) const {
     *index = d.key ? int32_t(d.at) : -1;  // none: no positive noise among what stays
@@ -709,14 +739,14 @@ struct Row {
     const int have = k < m ? k : m;
     u64 before = 0, total = 0, target = ~u64(0);
     const float s = tid < have ? key_score(uint32_t(sorted[tid] >> 32)) : 0.f;
-    const int64_t at = tid < have ? int64_t(uint32_t(~uint32_t(sorted[tid]))) : 0;
+    const uint32_t at = tid < have ? ~uint32_t(sorted[tid]) : 0;
     if (p < 1.f) {
       before = scan(tid < have ? fixed(weight(s)) : 0, &total);
       target = p > 0.f ? share_of(total, p) : 1;
     }
     if (tid < have && before < target) consider(true, s, at, noise[at]);  // one entry a thread: its candidate is sure
     const Drawn got = block_best(candidate(s));
-    if (got.key ? tid < have && at == int64_t(got.at) : tid == 0) put(got, s, index, logp);
+    if (got.key ? tid < have && at == got.at : tid == 0) put(got, s, index, logp);
   }
 };
 
@@ -741,15 +771,18 @@ __global__ void __launch_bounds__(kThreads, 2048 / kThreads > 4 ? 4 : kThreads =
   r.sorted = r.sums;  // the histogram is done with when entries are ordered
   r.list = reinterpret_cast<u64*>(r.counts + a.bins);
   r.data = reinterpret_cast<uint4*>(r.list + a.cap);
+  r.data_at = uint32_t(__cvta_generic_to_shared(r.data));
+  r.counts_at = uint32_t(__cvta_generic_to_shared(r.counts)), r.lacks_at = uint32_t(__cvta_generic_to_shared(r.lacks));
   const int64_t row = blockIdx.x / unsigned(r.blocks);
-  r.lo = r.rank * a.slice;
-  r.count = int(a.n - r.lo < 0 ? 0 : a.n - r.lo < a.slice ? a.n - r.lo : a.slice);
+  const int64_t lo = r.rank * a.slice, left = a.n - lo;
+  r.lo = int(lo < a.n ? lo : a.n);
+  r.count = int(left < 0 ? 0 : left < a.slice ? left : a.slice);
   r.global = static_cast<const T*>(a.scores) + row * a.row_stride + r.lo;
   r.skip = int(reinterpret_cast<uintptr_t>(r.global) % 16 / sizeof(T));
   r.groups = (r.skip + r.count + kG - 1) / kG;
   r.noise = a.noise + row * a.noise_stride;
   r.top_infinite = false;
-  r.rough = r.rough_second = -1.f, r.rough_at = -1, r.mass = 0.f, r.bound = 0;
+  r.rough = r.rough_second = -INFINITY, r.rough_at = -1, r.need_mass = true, r.mass = 0.f, r.bound = 0;
   int32_t* index = a.index + row;
   float* logp = a.logp ? a.logp + row : nullptr;
 
@@ -781,6 +814,7 @@ __global__ void __launch_bounds__(kThreads, 2048 / kThreads > 4 ? 4 : kThreads =
   r.temperature = a.temperature ? a.temperature[row] : a.temperature_all;
   r.min_w = fminf(a.min_p ? a.min_p[row] : a.min_p_all, 1.f);
   r.exp2_per = fminf(kLog2E / r.temperature, 3e38f);
+  r.min_log2 = r.min_w > 0.f ? fast_log2(r.min_w) - kNear : -INFINITY;
   const int64_t k = kFree ? 0 : a.top_k ? a.top_k[row] : a.top_k_all;
   const float p = kFree ? 1.f : a.top_p ? a.top_p[row] : a.top_p_all;
   __syncthreads();  // the scores are in shared memory
@@ -798,11 +832,11 @@ __global__ void __launch_bounds__(kThreads, 2048 / kThreads > 4 ? 4 : kThreads =
     return;
   }
   if constexpr (kFree) {
-    r.draw([](float, int64_t) { return true; });
-    r.finish([](float, int64_t, u64) { return true; }, index, logp);
+    r.draw([](float s, uint32_t) { return s > -INFINITY; }, [](const auto&, int) {});
+    r.finish([](float, uint32_t, u64) { return true; }, index, logp);
   } else {
     uint32_t bound_key = 0;
-    int64_t bound_at = INT64_MAX;
+    uint32_t bound_at = 0xffffffffu;
     if (k > 0 && k < a.n) {
       if (k <= kThreads / 4) {
         // the k-th largest of one block's threads bounds the row's from below: the best of the blocks'
@@ -839,10 +873,11 @@ __global__ void __launch_bounds__(kThreads, 2048 / kThreads > 4 ? 4 : kThreads =
     bool drawn = false;
     if (p < 1.f) r.select(true, 0, fmaxf(p, 0.f), bound_key, bound_at, &drawn);
     const float bs = bound_key ? key_score(bound_key) : -INFINITY;
-    if (!drawn) r.draw([&](float s, int64_t at) { return s > bs || (s == bs && at <= bound_at); });
+    if (!drawn)
+      r.draw([&](float s, uint32_t at) { return bool(int(s > bs) | (int(s == bs) & int(at <= bound_at) & int(s > -INFINITY))); }, [](const auto&, int) {});
     r.finish(
-        [&](float s, int64_t at, u64 e) {  // e: the bound that a drawing selection left, 0 for none
-          if (e) return r.kept(order_key(s), at, uint32_t(e >> 32), int64_t(uint32_t(~uint32_t(e))));
+        [&](float s, uint32_t at, u64 e) {  // e: the bound that a drawing selection left, 0 for none
+          if (e) return r.kept(order_key(s), at, uint32_t(e >> 32), ~uint32_t(e));
           return s > bs || (s == bs && at <= bound_at);
         },
         index, logp);
@@ -925,7 +960,7 @@ extern "C" emr_status emr_sample(const void* scores, int32_t dtype, int32_t rows
                                  const int32_t* top_k, int32_t top_k_all, const float* top_p, float top_p_all,
                                  const float* min_p, float min_p_all, int32_t* index, float* logp, void* stream) {
   if (rows < 1 || n < 1 || !scores || !noise || !index || !dtype_ok(dtype) || row_stride < 0 || noise_stride < 0) return EMR_ERR_ARG;
-  if (n > INT32_MAX || rows > (1 << 27)) return EMR_ERR_RANGE;
+  if (n > INT32_MAX - (1 << 20) || rows > (1 << 27)) return EMR_ERR_RANGE;
   const int size = dtype_bytes(dtype);
   if (reinterpret_cast<uintptr_t>(scores) % size || reinterpret_cast<uintptr_t>(noise) % 4 ||
       reinterpret_cast<uintptr_t>(index) % 4 || reinterpret_cast<uintptr_t>(logp) % 4 || reinterpret_cast<uintptr_t>(temperature) % 4 ||
