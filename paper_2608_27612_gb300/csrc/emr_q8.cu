@@ -20,19 +20,20 @@ constexpr int kTileThreads = 512;
 // 94464 x 1364 114 -> 95; with fewer than two tiles an SM the row kernel keeps more SMs busy.
 constexpr int64_t kTiledFrom = 304;
 
-// Dense source: four columns c .. c + 3 of a row, zero past the matrix. kVector: columns
-// are neighbours and every row is aligned to four elements.
-template <typename T, bool kVector>
+// Dense source: four columns c .. c + 3 of a row, zero past the matrix. kRows: columns are
+// neighbours; kFours: and every row is aligned to four elements.
+enum Layout { kStrided, kRows, kFours };
+template <typename T, Layout kLayout>
 struct Dense {
   const T* p;
   int64_t batch_stride, row_stride, col_stride;
   __device__ __forceinline__ Four<T> four(const T* row, int64_t c, int64_t cols) const {
     Four<T> v;
-    if (kVector && c + 4 <= cols) {
+    if (kLayout == kFours && c + 4 <= cols) {
       v.load(row + c);
     } else {
 #pragma unroll
-      for (int j = 0; j < 4; j++) v.set(j, c + j < cols ? row[(c + j) * (kVector ? 1 : col_stride)] : T(0.f));
+      for (int j = 0; j < 4; j++) v.set(j, c + j < cols ? row[(c + j) * (kLayout == kStrided ? col_stride : 1)] : T(0.f));
     }
     return v;
   }
@@ -48,8 +49,8 @@ __device__ __forceinline__ float4 q8_four(const uint8_t* values, const uint8_t* 
 // Row blocks only: a warp has one row and takes 512 columns of it at a time (four
 // blocks, whose scale bytes are one word), blockIdx.y of gridDim.y such pieces apart.
 // The next piece is loaded before the present one is worked on.
-template <typename T, bool kVector>
-__global__ void __launch_bounds__(kThreads) q8_rows_kernel(Dense<T, kVector> src, int64_t rows, int64_t cols, int64_t all_rows,
+template <typename T, Layout kLayout>
+__global__ void __launch_bounds__(kThreads) q8_rows_kernel(Dense<T, kLayout> src, int64_t rows, int64_t cols, int64_t all_rows,
                                                            emr_q8 q) {
   grid_wait();
   grid_go();
@@ -86,7 +87,11 @@ __global__ void __launch_bounds__(kThreads) q8_rows_kernel(Dense<T, kVector> src
   }
 }
 
-// 8 or 16 bytes from memory into shared memory, past `have` bytes zeros.
+// An address that copies of no bytes may name.
+__device__ __forceinline__ const void* aligned_down(const void* p) {
+  return reinterpret_cast<const void*>(reinterpret_cast<uintptr_t>(p) & ~uintptr_t(15));
+}
+// 4, 8 or 16 bytes from memory into shared memory, past `have` bytes zeros.
 template <int kBytes>
 __device__ __forceinline__ void copy_ahead(void* to, const void* from, int have) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(uint32_t(__cvta_generic_to_shared(to))), "l"(from), "n"(kBytes),
@@ -104,10 +109,12 @@ __device__ __forceinline__ void copy_ahead(void* to, const void* from, int have)
 // warps (the sums in their order); codes of four rows are one word of the transposed byte
 // tile, at (row / 4) ^ (column / 4 % 32) of its column, so that neither the stores (lanes:
 // columns 4 apart) nor the loads (lanes: one column) have conflicts.
-template <int kMode, typename T, bool kVector>
-__global__ void __launch_bounds__(kTileThreads, 2) q8_tile_kernel(Dense<T, kVector> src, emr_q8 other, int64_t rows, int64_t cols,
+template <int kMode, typename T, Layout kLayout>
+__global__ void __launch_bounds__(kTileThreads, 2) q8_tile_kernel(Dense<T, kLayout> src, emr_q8 other, int64_t rows, int64_t cols,
                                                                   uint32_t tiles, emr_q8 q, emr_q8 qt, float* sums) {
   constexpr bool kFromQ8 = kMode == 1 || kMode == 2;
+  constexpr bool kPieces = kMode != 1 && kLayout == kRows && sizeof(T) == 2;
+  constexpr int kPitch = 17 * 16 + 16;  // of a row in pieces; the last 16 bytes are only read along
   extern __shared__ __align__(16) uint8_t ahead[];  // [8][threads] of the dense source, then two tiles of codes
   __shared__ float4 part[16][32];
   __shared__ uint32_t bytes[128 * 32];
@@ -117,7 +124,8 @@ __global__ void __launch_bounds__(kTileThreads, 2) q8_tile_kernel(Dense<T, kVect
   const int64_t chunks = q8_scale_chunks(cols), row_bytes = q8_row_bytes(cols), scale_batch = q8_scale_batch(rows, cols);
   const int64_t t_row_bytes = q8_row_bytes(rows), t_chunks = q8_scale_chunks(rows), t_scale_batch = q8_scale_batch(cols, rows);
   Four<T>* const dense = reinterpret_cast<Four<T>*>(ahead) + threadIdx.x;
-  uint8_t* const codes = ahead + (kMode != 1 ? sizeof(Four<T>) * 8 * kTileThreads : 0);
+  uint8_t* const rows_ahead = ahead + first * kPitch;
+  uint8_t* const codes = ahead + (kPieces ? 128 * kPitch : kMode != 1 ? sizeof(Four<T>) * 8 * kTileThreads : 0);
 
   struct Place {
     int64_t b, rt, ct;
@@ -141,9 +149,37 @@ __global__ void __launch_bounds__(kTileThreads, 2) q8_tile_kernel(Dense<T, kVect
     if (kMode != 1) {
       const int n = p.wide - lane * 4, cells = n < 0 ? 0 : n < 4 ? n : 4;
       const T* from = src.p + p.b * src.batch_stride + (p.rt * 128 + first) * src.row_stride;
+      if constexpr (kPieces) {
+        // two-byte elements at any address: a warp copies its rows in aligned pieces of 16 bytes, 17 of
+        // which hold a row's 128 elements, and reads them back shifted
 #pragma unroll
-      for (int i = 0; i < 8; i++) {
-        if constexpr (kVector) {
+        for (int k = 0; k < 5; k++) {
+          const int piece = lane + k * 32, i = piece / 17, at = (piece - i * 17) * 16;
+          if (piece >= 8 * 17) break;
+          const char* row = reinterpret_cast<const char*>(from + i * src.row_stride + p.ct * 128);
+          const char* piece_from = reinterpret_cast<const char*>(reinterpret_cast<uintptr_t>(row) & ~uintptr_t(15)) + at;
+          uint8_t* to = rows_ahead + i * kPitch + at;
+          const int64_t left = row + p.wide * 2 - piece_from;
+          if (i < p.have && piece_from < reinterpret_cast<const char*>(src.p)) {  // nothing is read from before the matrix
+#pragma unroll
+            for (int e = 0; e < 16; e += 2)
+              *reinterpret_cast<uint16_t*>(to + e) =
+                  piece_from + e >= row && e < left ? *reinterpret_cast<const uint16_t*>(piece_from + e) : uint16_t(0);
+          } else {
+            const int have = i >= p.have || left <= 0 ? 0 : left < 16 ? int(left) : 16;
+            copy_ahead<16>(to, have ? static_cast<const void*>(piece_from) : aligned_down(src.p), have);
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < (kPieces ? 0 : 8); i++) {
+        if constexpr (kLayout == kRows && sizeof(T) == 4) {
+#pragma unroll
+          for (int j = 0; j < 4; j++) {
+            const bool in = i < p.have && j < cells;
+            copy_ahead<4>(reinterpret_cast<uint32_t*>(dense + i * kTileThreads) + j, in ? from + i * src.row_stride + c + j : src.p, in ? 4 : 0);
+          }
+        } else if constexpr (kLayout == kFours) {
           const bool in = i < p.have && cells > 0;
           copy_ahead<int(sizeof(Four<T>))>(dense + i * kTileThreads, in ? from + i * src.row_stride + c : src.p, in ? cells * int(sizeof(T)) : 0);
         } else {
@@ -179,11 +215,28 @@ __global__ void __launch_bounds__(kTileThreads, 2) q8_tile_kernel(Dense<T, kVect
     const Place p = place(t);
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     if (kFromQ8) __syncthreads();
+    else if (kPieces) __syncwarp();
     float4 v[8];
     const uint32_t scale_bytes = next_scale;
 #pragma unroll
     for (int i = 0; i < 8; i++) {
-      if (kMode != 1) v[i] = dense[i * kTileThreads].floats();
+      if constexpr (kPieces) {
+        const uintptr_t start = reinterpret_cast<uintptr_t>(src.p + p.b * src.batch_stride + (p.rt * 128 + first + i) * src.row_stride + p.ct * 128);
+        const int at = int(start & 15) + lane * 8;
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(rows_ahead + i * kPitch + (at & ~3));
+        Four<T> u;
+        u.u = make_uint2(w[0], w[1]);
+        if (start & 2) u.u = make_uint2(__funnelshift_r(u.u.x, u.u.y, 16), __funnelshift_r(u.u.y, w[2], 16));
+        const int cells = p.wide - lane * 4;  // what lies after the row in its last piece is not of it
+        if (cells < 4) {
+#pragma unroll
+          for (int j = 0; j < 4; j++)
+            if (j >= cells) u.set(j, T(0.f));
+        }
+        v[i] = i < p.have ? u.floats() : make_float4(0.f, 0.f, 0.f, 0.f);
+      } else if constexpr (kMode != 1) {
+        v[i] = dense[i * kTileThreads].floats();
+      }
       if (kFromQ8) {
         const float s = q8_scale(__shfl_sync(0xffffffffu, scale_bytes, i));
         float4 d = q8_unpack4(*reinterpret_cast<const uint32_t*>(codes + turn * 16384 + (first + i) * 128 + lane * 4));
@@ -192,6 +245,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) q8_tile_kernel(Dense<T, kVect
         v[i] = kMode == 1 ? d : make_float4(__fmul_rn(v[i].x, d.x), __fmul_rn(v[i].y, d.y), __fmul_rn(v[i].z, d.z), __fmul_rn(v[i].w, d.w));
       }
     }
+    if (kPieces) __syncwarp();  // the rows are read before others take their place
     if (t + gridDim.x < tiles) copy(t + gridDim.x, turn ^ 1);
     if (sums) {
       float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -306,29 +360,30 @@ __global__ void __launch_bounds__(kThreads) q8_dequantize_kernel(emr_q8 q, int64
 
 constexpr int64_t kMaxGrid = (int64_t(1) << 31) - 1;
 
-template <int kMode, typename T, bool kVector>
-emr_status launch_tile(const Dense<T, kVector>& src, const emr_q8* other, int64_t batch, int64_t rows, int64_t cols,
+template <int kMode, typename T, Layout kLayout>
+emr_status launch_tile(const Dense<T, kLayout>& src, const emr_q8* other, int64_t batch, int64_t rows, int64_t cols,
                        const emr_q8* q, const emr_q8* qt, float* sums, cudaStream_t st) {
   const int64_t tiles = batch * q8_blocks(rows) * q8_blocks(cols);
   if (tiles > kMaxGrid) return EMR_ERR_RANGE;
   static std::atomic<uint64_t> done{0};
-  const int smem = (kMode != 1 ? int(sizeof(Four<T>)) * 8 * kTileThreads : 0) + (kMode == 1 || kMode == 2 ? 2 * 16384 : 0);
+  const bool pieces = kMode != 1 && kLayout == kRows && sizeof(T) == 2;
+  const int smem = (pieces ? 128 * 288 : kMode != 1 ? int(sizeof(Four<T>)) * 8 * kTileThreads : 0) + (kMode == 1 || kMode == 2 ? 2 * 16384 : 0);
   int dev = 0, sms = 0;
-  if (!device_sms(&dev, &sms) || !allow_smem(q8_tile_kernel<kMode, T, kVector>, smem, dev, done)) return EMR_ERR_CUDA;
+  if (!device_sms(&dev, &sms) || !allow_smem(q8_tile_kernel<kMode, T, kLayout>, smem, dev, done)) return EMR_ERR_CUDA;
   const emr_q8 none{};
-  return launch_after(q8_tile_kernel<kMode, T, kVector>, dim3(unsigned(tiles < 2 * sms ? tiles : 2 * sms)), kTileThreads, size_t(smem), st,
+  return launch_after(q8_tile_kernel<kMode, T, kLayout>, dim3(unsigned(tiles < 2 * sms ? tiles : 2 * sms)), kTileThreads, size_t(smem), st,
                       src, other ? *other : none, rows, cols, uint32_t(tiles), q ? *q : none, qt ? *qt : none, sums);
 }
 
-template <typename T, bool kVector>
-emr_status launch_rows(const Dense<T, kVector>& src, int64_t batch, int64_t rows, int64_t cols, const emr_q8* q, cudaStream_t st) {
+template <typename T, Layout kLayout>
+emr_status launch_rows(const Dense<T, kLayout>& src, int64_t batch, int64_t rows, int64_t cols, const emr_q8* q, cudaStream_t st) {
   const int64_t all = batch * rows, grid = (all + kWarps - 1) / kWarps, chunks = q8_scale_chunks(cols);
   if (grid > kMaxGrid) return EMR_ERR_RANGE;
   // a warp takes whole rows where they are many, else a row is shared out: about 16 blocks for each of 152 SMs
   int64_t pieces = (16 * 152 + grid - 1) / grid;
   if (pieces > chunks) pieces = chunks;
   if (pieces > 65535) pieces = 65535;
-  return launch_after(q8_rows_kernel<T, kVector>, dim3(unsigned(grid), unsigned(pieces)), kThreads, 0, st, src, rows, cols, all, *q);
+  return launch_after(q8_rows_kernel<T, kLayout>, dim3(unsigned(grid), unsigned(pieces)), kThreads, 0, st, src, rows, cols, all, *q);
 }
 
 struct DenseArgs {
@@ -341,8 +396,9 @@ emr_status with_vector(const DenseArgs& a, Fn fn) {
   const bool vector = a.col_stride == 1 && reinterpret_cast<uintptr_t>(a.p) % (4 * sizeof(T)) == 0 &&
                       (a.rows == 1 || a.row_stride % 4 == 0) && (a.batch == 1 || a.batch_stride % 4 == 0);
   const T* p = static_cast<const T*>(a.p);
-  return vector ? fn(Dense<T, true>{p, a.batch_stride, a.row_stride, a.col_stride})
-                : fn(Dense<T, false>{p, a.batch_stride, a.row_stride, a.col_stride});
+  if (vector) return fn(Dense<T, kFours>{p, a.batch_stride, a.row_stride, a.col_stride});
+  if (a.col_stride == 1) return fn(Dense<T, kRows>{p, a.batch_stride, a.row_stride, 1});
+  return fn(Dense<T, kStrided>{p, a.batch_stride, a.row_stride, a.col_stride});
 }
 // fn with the source in its type, and as vectors where its layout allows.
 template <typename Fn>
@@ -408,7 +464,7 @@ extern "C" emr_status emr_q8_quantize_held(const void* src, int32_t dtype, int32
 
 extern "C" emr_status emr_q8_transpose(const emr_q8* q, const emr_q8* qt, void* stream) {
   if (!q8_ok(q) || !same_shape(qt, q->batch, q->cols, q->rows)) return EMR_ERR_ARG;
-  return launch_tile<1>(Dense<float, true>{}, q, q->batch, q->rows, q->cols, nullptr, qt, nullptr,
+  return launch_tile<1>(Dense<float, kFours>{}, q, q->batch, q->rows, q->cols, nullptr, qt, nullptr,
                         static_cast<cudaStream_t>(stream));
 }
 
