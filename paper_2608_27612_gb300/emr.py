@@ -12,7 +12,6 @@ import contextlib
 import ctypes as C
 import os
 from dataclasses import dataclass
-from typing import NamedTuple
 
 import numpy as np
 import torch
@@ -770,11 +769,20 @@ def device_error(stream=None) -> int:
     return code.value
 
 
-class Saved(NamedTuple):
-    """What a training step keeps between the passes: the transpose [nx, k, m] of x in 8 bits, as the weight
-    gradient reads it, and act'(z) [nets, m, n] in 8 bits (None: identity)."""
-    xt: Q8
-    slope: Q8 | None
+class Saved:
+    """What a training step keeps between the passes, in 8 bits: xt, the transpose [nx, k, m] of x, as the weight
+    gradient reads it, and slope, act'(z) [nets, m, n] (None: identity). nx, m: batch and rows of x."""
+
+    def __init__(self, layer, nx: int, m: int, xt, slope):
+        self._layer, self.nx, self.m, self._xt, self._slope = layer, nx, m, xt, slope
+
+    @property
+    def xt(self) -> Q8:
+        return Q8.of(self._xt, self.nx, self._layer.k, self.m)
+
+    @property
+    def slope(self) -> Q8 | None:
+        return Q8.of(self._slope, self._layer.nets, self.m, self._layer.n) if self._slope is not None else None
 
 
 class DenseLayer:
@@ -801,20 +809,29 @@ class DenseLayer:
             self.w8t = Q8(self.nets, self.k, self.n, device=w.device) if train else None
         self.c = DenseC(self.w8.c, self.w8t.c if train else Q8C(), None, act, 0)
         self._ref = C.byref(self.c)
-        self._room = {}
+        self._room, self._back = {}, {}
+        self._w8 = self.w8.ref, self.w8t.ref if train else None
         self.set_weights(w, b, stream)
 
     def set_weights(self, w, b=None, stream=None):
         """Lay out new weights (same shape) and keep the bias (None: no bias)."""
         w = _matrices(w, "w")
-        if tuple(w.shape) != (self.nets, self.n, self.k) or w.device != self.device:
-            raise ValueError("w: shape %s on %s is wanted" % ((self.nets, self.n, self.k), self.device))
+        dev = self.device
+        if w.shape != (self.nets, self.n, self.k) or w.device != dev:
+            raise ValueError("w: shape %s on %s is wanted" % ((self.nets, self.n, self.k), dev))
+        kind = _DTYPES.get(w.dtype)
+        if kind is None:
+            _dtype(w.dtype, "w")
+        if stream is not None and stream != torch.cuda.current_stream(dev):
+            with torch.cuda.stream(stream):
+                return self.set_weights(w, b)
         if b is not None:
-            if b.dtype != torch.float32 or b.numel() != self.nets * self.n or b.device != self.device:
+            if b.dtype != torch.float32 or b.numel() != self.nets * self.n or b.device != dev:
                 raise ValueError("b: a float32 tensor [%d, %d] on the layer's GPU is wanted" % (self.nets, self.n))
-            with _on(stream):
-                b = b.contiguous()
-        q8_quantize(w, self.w8, self.w8t, stream)
+            b = b.contiguous()
+        q, qt = self._w8
+        _check(lib().emr_q8_quantize(w.data_ptr(), kind, self.nets, self.n, self.k, *w.stride(), q, qt,
+                                     torch._C._cuda_getCurrentRawStream(dev.index)), "emr_q8_quantize")
         self.b = b
         self.c.bias = b.data_ptr() if b is not None else None
 
@@ -873,30 +890,41 @@ class DenseLayer:
         if not self.train:
             raise ValueError("forward_train: the layer was made with train=False")
         y, xt, slope = self._forward(x, out_dtype, stream, True)
-        nx, m = (x.shape[0], x.shape[1]) if x.dim() == 3 else (1, x.shape[0])
-        return y, Saved(Q8.of(xt, nx, self.k, m), Q8.of(slope, self.nets, m, self.n) if slope is not None else None)
+        return y, Saved(self, x.shape[0] if x.dim() == 3 else 1, y.shape[1], xt, slope)
 
     def backward(self, dy, saved: Saved, out_dtype=torch.float32, stream=None):
         """(dx, dw, db) of out_dtype for dy [nets, m, n]: dx [1 or nets, m, k] as forward_train took x (summed
         over the networks where x was shared), dw [nets, n, k], db [nets, n] (also without a bias)."""
-        q, slope = saved
-        m = q.cols
         dy = _matrices(dy, "dy")
-        if tuple(dy.shape) != (self.nets, m, self.n) or dy.device != self.device:
-            raise ValueError("dy: shape %s is wanted, got %s" % ((self.nets, m, self.n), tuple(dy.shape)))
-        kind, out_kind = _dtype(dy.dtype, "dy"), _dtype(out_dtype, "out_dtype")
-        room = C.c_size_t()
-        _check(lib().emr_dense_backward_room(self._ref, q.batch, m, C.byref(room)), "emr_dense_backward_room")
-        with _on(stream):
-            dy = dy.contiguous()
-            dx = torch.empty((q.batch, m, self.k), dtype=out_dtype, device=self.device)
-            dw = torch.empty((self.nets, self.n, self.k), dtype=out_dtype, device=self.device)
-            db = torch.empty((self.nets, self.n), dtype=out_dtype, device=self.device)
-            ws = torch.empty(room.value, dtype=torch.uint8, device=self.device)
-            _check(lib().emr_dense_backward(self._ref, dy.data_ptr(), kind, q.batch, m, q.data.data_ptr(),
-                                            slope.data.data_ptr() if slope is not None else None, dx.data_ptr(),
-                                            dw.data_ptr(), db.data_ptr(), out_kind, ws.data_ptr(), room.value,
-                                            _raw_stream(stream, self.device)), "emr_dense_backward")
+        nx, m, dev = saved.nx, saved.m, self.device
+        if dy.shape != (self.nets, m, self.n) or dy.device != dev:
+            raise ValueError("dy: shape %s on %s is wanted, got %s" % ((self.nets, m, self.n), dev, tuple(dy.shape)))
+        if saved._layer is not self:
+            raise ValueError("saved: of another layer")
+        kind, out_kind = _DTYPES.get(dy.dtype), _DTYPES.get(out_dtype)
+        if kind is None or out_kind is None:
+            _dtype(dy.dtype, "dy"), _dtype(out_dtype, "out_dtype")
+        if stream is not None and stream != torch.cuda.current_stream(dev):
+            with torch.cuda.stream(stream):
+                return self.backward(dy, saved, out_dtype)
+        dy = dy.contiguous()
+        room = self._back.get((nx, m))
+        if room is None:
+            n = C.c_size_t()
+            _check(_lib.emr_dense_backward_room(self._ref, nx, m, C.byref(n)), "emr_dense_backward_room")
+            if len(self._back) > 64:
+                self._back.clear()
+            room = self._back[(nx, m)] = n.value
+        dx = torch.empty((nx, m, self.k), dtype=out_dtype, device=dev)
+        dw = torch.empty((self.nets, self.n, self.k), dtype=out_dtype, device=dev)
+        db = torch.empty((self.nets, self.n), dtype=out_dtype, device=dev)
+        ws = torch.empty(room, dtype=torch.uint8, device=dev)
+        status = _lib.emr_dense_backward(self._ref, dy.data_ptr(), kind, nx, m, saved._xt.data_ptr(),
+                                         saved._slope.data_ptr() if saved._slope is not None else None, dx.data_ptr(),
+                                         dw.data_ptr(), db.data_ptr(), out_kind, ws.data_ptr(), room,
+                                         torch._C._cuda_getCurrentRawStream(dev.index))
+        if status:
+            _check(status, "emr_dense_backward")
         return dx, dw, db
 
 
