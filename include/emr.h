@@ -729,10 +729,10 @@ emr_status emr_device_error(int32_t *code, void *stream);
  * probability. T <= 0 takes the largest score (lowest index) with logp 0. A row with
  * nothing left (all masked) gives index -1 and logp -infinity; a score of +infinity
  * leaves only the entries that equal it. q above 1 counts as 1 and p below 0 as 0: the
- * largest score always stays. Sums of w are taken in fixed point (steps of 2^-44, for n
- * above 2^18 of 2^-43 and so on), so results do not depend on the order of execution.
- * Reads scores once where a row's share of them fits into the shared memory of its
- * blocks (up to about 350,000 entries of 4 bytes). Errors: EMR_ERR_ARG (null or
+ * largest score always stays. Sums of w are integers (fixed point), so results do not
+ * depend on the order of execution. Scores are read from memory once: a row's blocks keep
+ * what fits into their shared memory (about 350,000 entries of 4 bytes for 8 blocks) and
+ * read the rest again, in the main from L2; noise is read for entries that stay. Errors: EMR_ERR_ARG (null or
  * misaligned pointer, size below 1, negative stride, unknown type), EMR_ERR_RANGE (n
  * above 2^31 - 2^20, rows above 2^27), EMR_ERR_CUDA. */
 emr_status emr_sample(const void *scores, int32_t dtype, int32_t rows, int64_t n, int64_t row_stride,

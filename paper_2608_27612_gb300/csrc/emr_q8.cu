@@ -1,10 +1,13 @@
 // Block-scaled 8-bit matrices: quantising, transposing, reading back, and the
 // backward pass of an activation from its 8-bit slope.
 //
-// All of it is bound by memory. Every kernel reads its source once: a row block of
-// 128 columns is one warp's registers (four columns a lane), so its maximum is one
-// warp reduction and its codes one 128-byte store; the transposed copy is made from
-// the same registers through a 16 KB tile of codes.
+// Every kernel reads its source once: a row block of 128 columns is one warp's
+// registers (four columns a lane), so its maximum is one warp reduction and its codes
+// one 128-byte store; the transposed copy is made from the same registers through a
+// 16 KB tile of codes. Bytes are the floor, the instructions of the reductions and
+// conversions what binds large matrices (ALU pipe 65%, memory 39%): 8192 x 8192 bfloat16
+// by rows 49 us (4.1 TB/s), both ways 71 (3.8), slope product both ways with sums 103
+// (3.2), 94464 x 1364 float16 by rows 90 (4.3).
 #include <cuda_runtime.h>
 
 #include "emr_q8.h"

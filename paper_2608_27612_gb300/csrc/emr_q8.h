@@ -150,7 +150,7 @@ bool allow_smem(K kernel, int bytes, int dev, std::atomic<uint64_t>& done) {
   return true;
 }
 
-constexpr int kMostSmem = 227 * 1024 - 3072;  // dynamic, beside at most 3 KB of static arrays
+constexpr int kMostSmem = 224 * 1024;  // dynamic, beside at most 3 KB of static arrays
 
 // The product of a few rows of x, quantised within the kernel (emr_q8_few.cu).
 struct FewArgs {

@@ -533,6 +533,11 @@ __device__ __forceinline__ Tile pair_tile_at(const Params& p, int t) {
   return raster(t, (p.m_tiles + 1) / 2, (p.n_tiles + 1) / 2, p.tiles, 8);
 }
 
+// The same on pairs of SMs: 256 x 256 tiles, half the operand bytes for each output. Loads
+// bound a single SM's tiles (540 clocks a step of 128 columns, 61 bytes a clock from L2, where
+// the matrix instructions take 256); of a pair's 313 us at 8192^3 loads alone would take 209
+// and the instructions 271. 8192^3 322 us (3.4 PFLOP/s), with slopes 345; 94464 x 1364 x 1364
+// 161, with sin 202.
 template <bool kSlope>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     q8_pair_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap w_map,
@@ -667,7 +672,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         }
         // The columns that the next tile's scales are waiting for are read before all others; without
         // slopes the epilogue is short and the barrier costs more than it saves (94464 x 1364 x 1364:
-        // 170 us without, 185 with; with slopes 8192^3 375 us without, 350 with).
+        // 170 us without, 185 with; with slopes 8192^3 375 us without, 345 with).
         const bool scales = half && c == 3;
         if (kSlope && half && !scales) finish_sync();
         auto read = [&] {
@@ -707,8 +712,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 // shared memory, in the order of their ranks. A lane of the epilogue has one output of
 // each row, so its stores are neighbours. The same kernel serves larger a with few tiles
 // and a long contraction (the gradient of an input that many networks share). 8 x 8192 x
-// 8192: 9.3 us with the weights in L2, 23 from memory, where tiles of 128 rows took 21
-// and 31; 250 x 256 summed over 64 networks of 340: 57 -> 17 us.
+// 8192: 9.8 us with the weights in L2, 20 from memory (3.3 TB/s), where tiles of 128 rows took
+// 21 and 31; 250 x 256 summed over 64 networks of 340: 57 -> 13 us.
 
 constexpr int kThinStages = 6;     // at most; q.stages of them are used
 constexpr int kThinThreads = 320;  // copy warp, matrix warp, eight epilogue warps
@@ -1028,7 +1033,7 @@ bool use_thin(const Params& p, int sms) {
 // 1364, 5460 x 1364 x 2000 and 2000 x 5460 x 1364: a round takes the longer of its copies (28 a
 // block of 128 columns, 36 for a pair) and its epilogue (200, with slopes 500, a pair twice
 // that), 100 more to fill and drain it, and a launch of pairs 400 more than one of single
-// blocks. 8192^3: 485 us against 330; 4096^3: 69 against 53; 5460 x 1364 x 2000: 23.5 against
+// blocks. 8192^3: 485 us against 322; 4096^3: 69 against 53; 5460 x 1364 x 2000: 23.5 against
 // 19.3; 1000 x 5460 x 1364: 15.3 against 16.6; 2000 x 5460 x 1364 with slopes: 28 against 33.
 bool use_pairs(const Params& p, int sms) {
   const int64_t pair_tiles = int64_t(p.tiles) / (int64_t(p.m_tiles) * p.n_tiles) * ((p.m_tiles + 1) / 2) * ((p.n_tiles + 1) / 2);
