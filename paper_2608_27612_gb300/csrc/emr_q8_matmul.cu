@@ -165,6 +165,7 @@ struct Params {
   int32_t act;
   void* out;
   int32_t out_dtype, store_bytes;   // store_bytes: widest store that every row of out is aligned to
+  int32_t narrow;                   // at most 64 columns, no slopes: half of the epilogue's warps for each accumulator
   uint8_t *slope, *slope_scales;
 };
 
@@ -355,7 +356,7 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
   if (threadIdx.x == 0) {
     gave_up = 0;
     for (int i = 0; i < kStages; i++) bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, 1);
-    for (int i = 0; i < 2; i++) bar_init(acc_full + 8 * i, 1), bar_init(acc_empty + 8 * i, kFinishWarps);
+    for (int i = 0; i < 2; i++) bar_init(acc_full + 8 * i, 1), bar_init(acc_empty + 8 * i, p.narrow ? kFinishWarps / 2 : kFinishWarps);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&a_map) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&w_map) : "memory");
@@ -443,11 +444,14 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
     }
   } else if (warp >= 4) {
     const int quadrant = warp & 3;  // tensor memory lanes that this warp may read
-    const int own = warp - 4, c = own >> 2;
+    // with at most 64 columns the warps of the other two chunks take every other tile: 112 networks
+    // of 13496 x 45 x 86 195 -> 134 us
+    const int own = warp - 4, c = p.narrow ? own >> 2 & 1 : own >> 2, group = own >> 3;
     uint8_t* const staged = staging + own * 32 * 64;
     uint32_t n_tile = 0;
     for (int t = blockIdx.x; t < p.tiles; t += gridDim.x, n_tile++) {
       const uint32_t acc = n_tile & 1;
+      if (!kSlope && p.narrow && int(acc) != group) continue;
       const Tile tile = tile_at(p, t);
       const int row0 = tile.m * kTileM + quadrant * 32, n = tile.n * kTileN + c * 32 + lane;
       const float bias = p.bias && n < p.N ? __ldg(p.bias + int64_t(tile.b) * p.N + n) : 0.f;
@@ -539,9 +543,9 @@ __device__ __forceinline__ Tile pair_tile_at(const Params& p, int t) {
 
 // The same on pairs of SMs: 256 x 256 tiles, half the operand bytes for each output. Loads
 // bound a single SM's tiles (540 clocks a step of 128 columns, 61 bytes a clock from L2, where
-// the matrix instructions take 256); of a pair's 313 us at 8192^3 loads alone would take 209
-// and the instructions 271. 8192^3 322 us (3.4 PFLOP/s), with slopes 345; 94464 x 1364 x 1364
-// 161, with sin 202.
+// the matrix instructions take 256); of a pair's time at 8192^3 loads alone would take 209
+// us and the instructions 271. 8192^3 305 us (3.6 PFLOP/s), with slopes 321; 94464 x 1364 x 1364
+// 140, with sin 179.
 template <bool kSlope>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     q8_pair_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap w_map,
@@ -675,8 +679,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           fence_after();
         }
         // The columns that the next tile's scales are waiting for are read before all others; without
-        // slopes the epilogue is short and the barrier costs more than it saves (94464 x 1364 x 1364:
-        // 170 us without, 185 with; with slopes 8192^3 375 us without, 345 with).
+        // slopes the epilogue is short and the barrier costs more than it saves (with slopes
+        // 8192^3 334 us without, 321 with).
         const bool scales = half && c == 3;
         if (kSlope && half && !scales) finish_sync();
         auto read = [&] {
@@ -1026,25 +1030,28 @@ emr_status launch_thin(const emr_q8* a, const emr_q8* w, const Params& p, int de
   return cudaLaunchKernelEx(&cfg, q8_thin_kernel, a_map, w_map, q) == cudaSuccess ? EMR_OK : EMR_ERR_CUDA;
 }
 
-// At most 128 rows, or so few tiles of a long contraction that most SMs would have none.
+// At most 64 rows, or so few tiles of a long contraction that most SMs would have none. From 65
+// rows on the exchanged operands save no bytes: 100 x 8192 x 300 8.1 us by this kernel and 4.6 by
+// tiles, 26 networks of 98 x 5965 x 74 58 and 29; of 64 x 5965 x 74 23 and 29.
 bool use_thin(const Params& p, int sms) {
-  if (p.M <= 128) return true;
+  if (p.M <= 64) return true;
   return int64_t(p.tiles) * 2 <= sms && int64_t(p.sum) * p.k_blocks >= 16;
 }
 
 // Pairs of SMs where their rounds of 256 x 256 tiles take less time than one SM's rounds of
 // 128 x 128 tiles. In hundredths of a microsecond, measured at 8192^3, 4096^3, 94464 x 1364 x
-// 1364, 5460 x 1364 x 2000 and 2000 x 5460 x 1364: a round takes the longer of its copies (28 a
-// block of 128 columns, 36 for a pair) and its epilogue (200, with slopes 500, a pair twice
-// that), 100 more to fill and drain it, and a launch of pairs 400 more than one of single
-// blocks. 8192^3: 485 us against 322; 4096^3: 69 against 53; 5460 x 1364 x 2000: 23.5 against
-// 19.3; 1000 x 5460 x 1364: 15.3 against 16.6; 2000 x 5460 x 1364 with slopes: 28 against 33.
+// 1364, 5460 x 1364 x 2000, 2000 x 5460 x 1364 and 18750 x 6936 x 514: a round takes the longer of
+// its copies (28 a block of 128 columns, 36 for a pair) and its epilogue (120, with slopes 400, a
+// pair twice that), 60 more to fill and drain it, 120 for a pair, and a launch of pairs 400 more
+// than one of single blocks. Single blocks and pairs: 8192^3 480 us and 305; 4096^3 67 and 45;
+// 5460 x 1364 x 2000 23 and 17; 18750 x 6936 x 514 104 and 87; 1000 x 5460 x 1364 14.9 and 15.5;
+// 93050 x 1075 x 88 89 and 98; 2000 x 5460 x 1364 with slopes 27 and 32.
 bool use_pairs(const Params& p, int sms) {
   const int64_t pair_tiles = int64_t(p.tiles) / (int64_t(p.m_tiles) * p.n_tiles) * ((p.m_tiles + 1) / 2) * ((p.n_tiles + 1) / 2);
-  const int64_t pairs = sms / 2, steps = int64_t(p.sum) * p.k_blocks, finish = p.slope ? 500 : 200;
+  const int64_t pairs = sms / 2, steps = int64_t(p.sum) * p.k_blocks, finish = p.slope ? 400 : 120;
   if (pairs < 1) return false;
   const int64_t one = steps * 28 > finish ? steps * 28 : finish, two = steps * 36 > 2 * finish ? steps * 36 : 2 * finish;
-  return (pair_tiles + pairs - 1) / pairs * (two + 100) + 400 < (p.tiles + sms - 1) / sms * (one + 100);
+  return (pair_tiles + pairs - 1) / pairs * (two + 120) + 400 < (p.tiles + sms - 1) / sms * (one + 60);
 }
 
 }  // namespace
@@ -1076,6 +1083,7 @@ extern "C" emr_status emr_q8_matmul(const emr_q8* a, const emr_q8* w, const floa
   p.bias = bias, p.act = act, p.out = out, p.out_dtype = out_dtype;
   p.store_bytes = 16;
   while (p.store_bytes > size && (reinterpret_cast<uintptr_t>(out) % p.store_bytes || (int64_t(p.N) * size) % p.store_bytes)) p.store_bytes >>= 1;
+  p.narrow = !slope && p.N <= 64;
   if (slope) p.slope = slope->values, p.slope_scales = slope->scales;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   int dev = 0, sms = 0;
