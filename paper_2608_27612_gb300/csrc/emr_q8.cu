@@ -2,12 +2,12 @@
 // backward pass of an activation from its 8-bit slope.
 //
 // Every kernel reads its source once: a row block of 128 columns is one warp's
-// registers (four columns a lane), so its maximum is one warp reduction and its codes
-// one 128-byte store; the transposed copy is made from the same registers through a
-// 16 KB tile of codes. Bytes are the floor, the instructions of the reductions and
-// conversions what binds large matrices (ALU pipe 65%, memory 39%): 8192 x 8192 bfloat16
-// by rows 49 us (4.1 TB/s), both ways 71 (3.8), slope product both ways with sums 103
-// (3.2), 94464 x 1364 float16 by rows 90 (4.3).
+// registers (four columns a lane, or sixteen of eight lanes), so its maximum is one
+// reduction over lanes and its codes one 128-byte store; the transposed copy is made
+// from the same registers through a 16 KB tile of codes. Bytes are the floor; by rows
+// 8192 x 8192 bfloat16 takes 33 us (6.1 TB/s), 94464 x 1364 float16 72 (5.5). The tiles of
+// both ways are bound by the instructions of the reductions and conversions (ALU pipe
+// 65%, memory 39%): 71 us (3.8 TB/s), the slope product with sums 103 (3.2).
 #include <cuda_runtime.h>
 
 #include "emr_q8.h"
@@ -19,27 +19,15 @@ using namespace emr;
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kTileThreads = 512;
-// Tiles from which row blocks alone are worked on by tiles too: 8192 x 8192 bfloat16 58 -> 53 us,
-// 94464 x 1364 114 -> 95; with fewer than two tiles an SM the row kernel keeps more SMs busy.
-constexpr int64_t kTiledFrom = 304;
 
-// Dense source: four columns c .. c + 3 of a row, zero past the matrix. kRows: columns are
-// neighbours; kFours: and every row is aligned to four elements.
+// Dense source. kRows: columns are neighbours; kFours: and every row is aligned to four elements.
 enum Layout { kStrided, kRows, kFours };
 template <typename T, Layout kLayout>
 struct Dense {
+  using Value = T;
+  static constexpr bool kWhole = kLayout != kStrided;  // rows lie in one piece
   const T* p;
   int64_t batch_stride, row_stride, col_stride;
-  __device__ __forceinline__ Four<T> four(const T* row, int64_t c, int64_t cols) const {
-    Four<T> v;
-    if (kLayout == kFours && c + 4 <= cols) {
-      v.load(row + c);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 4; j++) v.set(j, c + j < cols ? row[(c + j) * (kLayout == kStrided ? col_stride : 1)] : T(0.f));
-    }
-    return v;
-  }
 };
 
 __device__ __forceinline__ float4 q8_four(const uint8_t* values, const uint8_t* scales, int64_t row_bytes,
@@ -47,47 +35,6 @@ __device__ __forceinline__ float4 q8_four(const uint8_t* values, const uint8_t* 
   const float s = q8_scale(scales[q8_scale_at(chunks, r, c >> 7)]);
   const float4 v = q8_unpack4(*reinterpret_cast<const uint32_t*>(values + r * row_bytes + c));
   return make_float4(v.x * s, v.y * s, v.z * s, v.w * s);
-}
-
-// Row blocks only: a warp has one row and takes 512 columns of it at a time (four
-// blocks, whose scale bytes are one word), blockIdx.y of gridDim.y such pieces apart.
-// The next piece is loaded before the present one is worked on.
-template <typename T, Layout kLayout>
-__global__ void __launch_bounds__(kThreads) q8_rows_kernel(Dense<T, kLayout> src, int64_t rows, int64_t cols, int64_t all_rows,
-                                                           emr_q8 q) {
-  grid_wait();
-  grid_go();
-  const int64_t row = int64_t(blockIdx.x) * kWarps + (threadIdx.x >> 5);
-  if (row >= all_rows) return;
-  const int lane = threadIdx.x & 31;
-  const int64_t b = all_rows <= UINT32_MAX ? uint32_t(row) / uint32_t(rows) : row / rows, r = row - b * rows;
-  const int chunks = int(q8_scale_chunks(cols)), blocks = int(q8_blocks(cols));
-  const T* from = src.p + b * src.batch_stride + r * src.row_stride;
-  uint8_t* out = q.values + row * q8_row_bytes(cols) + lane * 4;
-  uint8_t* scales = q.scales + b * q8_scale_batch(rows, cols) + q8_scale_at(chunks, r, 0);
-  Four<T> u[4];
-#pragma unroll
-  for (int j = 0; j < 4; j++) u[j] = src.four(from, int64_t(blockIdx.y) * 512 + j * 128 + lane * 4, cols);
-  for (int chunk = blockIdx.y; chunk < chunks; chunk += gridDim.y) {
-    Four<T> now[4];
-#pragma unroll
-    for (int j = 0; j < 4; j++) now[j] = u[j];
-    const int next = chunk + gridDim.y;
-    if (next < chunks) {
-#pragma unroll
-      for (int j = 0; j < 4; j++) u[j] = src.four(from, int64_t(next) * 512 + j * 128 + lane * 4, cols);
-    }
-    uint32_t word = 0;
-#pragma unroll
-    for (int j = 0; j < 4; j++) {
-      float4 v = now[j].floats();
-      const uint32_t byte = q8_warp_scale(v);
-      word |= byte << (8 * j);
-      if (chunk * 4 + j < blocks)
-        *reinterpret_cast<uint32_t*>(out + int64_t(chunk) * 512 + j * 128) = q8_pack4(v.x, v.y, v.z, v.w, q8_inverse(byte));
-    }
-    if (lane == 0) *reinterpret_cast<uint32_t*>(scales + int64_t(chunk) * 512) = word;
-  }
 }
 
 // An address that copies of no bytes may name.
@@ -100,6 +47,132 @@ __device__ __forceinline__ void copy_ahead(void* to, const void* from, int have)
   asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(uint32_t(__cvta_generic_to_shared(to))), "l"(from), "n"(kBytes),
                "r"(have)
                : "memory");
+}
+
+// Row blocks only, of rows that lie in one piece. Eight lanes have a block, sixteen columns each, so
+// that what is done once for a block is done once for sixteen values of a lane. Blocks are a grid's
+// groups of eight apart; a lane copies those of its next turns into shared memory of its own in
+// aligned units of 16 bytes, out of which a row that starts elsewhere is shifted. What a unit holds
+// besides the row is not used, and nothing is read from outside the matrix. Addresses are counted up:
+// with them computed for every block the kernel was bound by its integer instructions (8192 x 8192
+// bfloat16 47 us, now 33).
+template <typename T>
+struct Rows16 {
+  static constexpr int kUnits = int(sizeof(T)) + 1;
+  static constexpr int kAhead = 2;  // turns
+  static constexpr int kSmem = (kAhead + 1) * kUnits * kThreads * 16;
+  static constexpr int kBlocks = sizeof(T) == 4 ? 3 : 5;  // of an SM
+};
+// Indices of blocks fit 32 bits: 2^32 of them are more than a device holds.
+template <typename T, bool kBatch>
+__global__ void __launch_bounds__(kThreads, Rows16<T>::kBlocks)
+    q8_rows16_kernel(const T* src, const T* last, int64_t batch_stride, int64_t row_stride, uint32_t rows, uint32_t blocks, int32_t tail,
+                     uint32_t all, emr_q8 q) {
+  constexpr int kUnits = Rows16<T>::kUnits, kAhead = Rows16<T>::kAhead;
+  extern __shared__ __align__(16) uint4 ring[];  // [turn][unit][thread]
+  const int lane = threadIdx.x & 31, part = (lane & 7) * 16;
+  const uint32_t stride = gridDim.x * kWarps * 4, far_rows = stride / blocks, far_blocks = stride - far_rows * blocks;
+  const int64_t scale_batch = q8_scale_batch(rows, int64_t(blocks) * 128);
+  const uint32_t chunks = (blocks + 3) / 4;
+  const int tail_cells = tail - part;  // of this lane in a row's last block
+  uint32_t g = (blockIdx.x * kWarps + (threadIdx.x >> 5)) * 4 + (lane >> 3), row = g / blocks, kb = g - row * blocks;
+  // the copies run kAhead turns before: block, and its address where it follows from the one before
+  uint32_t next_g = g, next_row = row, next_kb = kb, turn = 0, shifts = 0;
+  const T* at = src + int64_t(row) * row_stride + int64_t(kb) * 128 + part;
+  const int64_t step = int64_t(far_rows) * row_stride + int64_t(far_blocks) * 128, wrap = row_stride - int64_t(blocks) * 128;
+  const auto copy = [&] {
+    if (kBatch) {
+      const uint32_t b = next_row / rows;
+      at = src + int64_t(b) * batch_stride + int64_t(next_row - b * rows) * row_stride + int64_t(next_kb) * 128 + part;
+    }
+    const uint32_t shift = uint32_t(reinterpret_cast<uintptr_t>(at)) & 15;
+    shifts = shifts << 4 | shift;
+    if (next_g < all && (next_kb + 1 < blocks || tail_cells > 0)) {
+      uint4* const to = ring + turn * (kUnits * kThreads) + threadIdx.x;
+      const char* const unit = reinterpret_cast<const char*>(at) - shift;
+      if (unit >= reinterpret_cast<const char*>(src) && unit + kUnits * 16 <= reinterpret_cast<const char*>(last)) {
+#pragma unroll
+        for (int i = 0; i < kUnits; i++)
+          if (i + 1 < kUnits || shift) copy_ahead<16>(to + i * kThreads, unit + i * 16, 16);
+      } else {  // at the matrix's ends
+#pragma unroll
+        for (int i = 0; i < kUnits; i++) {
+#pragma unroll
+          for (int e = 0; e < 16; e += int(sizeof(T))) {
+            const T* const from = reinterpret_cast<const T*>(unit + i * 16 + e);
+            *reinterpret_cast<T*>(reinterpret_cast<char*>(to + i * kThreads) + e) = from >= src && from < last ? *from : T(0.f);
+          }
+        }
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    next_g += stride, next_row += far_rows, next_kb += far_blocks, at += step;
+    if (next_kb >= blocks) next_kb -= blocks, next_row++, at += wrap;
+    turn = turn == kAhead ? 0 : turn + 1;
+  };
+  grid_wait();
+  grid_go();
+#pragma unroll
+  for (int i = 0; i < kAhead; i++) copy();
+  uint8_t* out = q.values + int64_t(g) * 128 + part;
+  uint32_t own = 0;
+  while (__any_sync(0xffffffffu, g < all)) {
+    copy();
+    asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
+    uint32_t w[kUnits * 4];
+#pragma unroll
+    for (int i = 0; i < kUnits; i++)
+      *reinterpret_cast<uint4*>(w + 4 * i) = ring[(own * kUnits + i) * kThreads + threadIdx.x];
+    const uint32_t shift = shifts >> (4 * kAhead) & 15;
+    if (shift) {
+#pragma unroll
+      for (int i = 0; i < kUnits * 4 - 2; i++) w[i] = shift & 8 ? w[i + 2] : w[i];
+#pragma unroll
+      for (int i = 0; i < kUnits * 4 - 3; i++) w[i] = shift & 4 ? w[i + 1] : w[i];
+      if (sizeof(T) == 2) {
+        const uint32_t select = shift & 2 ? 0x5432 : 0x3210;
+#pragma unroll
+        for (int i = 0; i < kUnits * 4 - 4; i++) w[i] = __byte_perm(w[i], w[i + 1], select);
+      }
+    }
+    float v[16];
+#pragma unroll
+    for (int i = 0; i < 16; i++) v[i] = float(reinterpret_cast<const T*>(w)[i]);
+    const int cells = g >= all ? 0 : kb + 1 < blocks ? 16 : tail_cells;
+    if (cells < 16) {
+#pragma unroll
+      for (int i = 0; i < 16; i++) v[i] = i < cells ? v[i] : 0.f;
+    }
+    float most = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; i++) most = fmaxf(most, fabsf(v[i]));
+    uint32_t top = __float_as_uint(most);  // NaN is passed over
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 4));
+    if (__any_sync(0xffffffffu, top >= 0x7f800000u)) {  // an infinity: finite magnitudes again
+      top = 0;
+#pragma unroll
+      for (int i = 0; i < 16; i++) top = max(top, q8_magnitude(v[i])), v[i] = q8_finite_or_nan(v[i]);
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 4));
+    }
+    const uint32_t byte = q8_scale_byte(top);
+    const float inv = q8_inverse(byte);
+    if (g < all) {
+      *reinterpret_cast<uint4*>(out) = make_uint4(q8_pack4(v[0], v[1], v[2], v[3], inv), q8_pack4(v[4], v[5], v[6], v[7], inv),
+                                                  q8_pack4(v[8], v[9], v[10], v[11], inv), q8_pack4(v[12], v[13], v[14], v[15], inv));
+      if (part == 0) {
+        const uint32_t b = kBatch ? row / rows : 0, r = row - b * rows;
+        q.scales[(kBatch ? b * scale_batch : 0) + (int64_t(r >> 7) * chunks + (kb >> 2)) * 512 + (r & 31) * 16 + (r >> 5 & 3) * 4 + (kb & 3)] =
+            uint8_t(byte);
+      }
+    }
+    g += stride, out += int64_t(stride) * 128, row += far_rows, kb += far_blocks;
+    if (kb >= blocks) kb -= blocks, row++;
+    own = own == kAhead ? 0 : own + 1;
+  }
 }
 
 // 128 x 128 tiles: row blocks to q, column blocks (the transpose) to qt, column sums to
@@ -378,15 +451,21 @@ emr_status launch_tile(const Dense<T, kLayout>& src, const emr_q8* other, int64_
                       src, other ? *other : none, rows, cols, uint32_t(tiles), q ? *q : none, qt ? *qt : none, sums);
 }
 
-template <typename T, Layout kLayout>
-emr_status launch_rows(const Dense<T, kLayout>& src, int64_t batch, int64_t rows, int64_t cols, const emr_q8* q, cudaStream_t st) {
-  const int64_t all = batch * rows, grid = (all + kWarps - 1) / kWarps, chunks = q8_scale_chunks(cols);
-  if (grid > kMaxGrid) return EMR_ERR_RANGE;
-  // a warp takes whole rows where they are many, else a row is shared out: about 16 blocks for each of 152 SMs
-  int64_t pieces = (16 * 152 + grid - 1) / grid;
-  if (pieces > chunks) pieces = chunks;
-  if (pieces > 65535) pieces = 65535;
-  return launch_after(q8_rows_kernel<T, kLayout>, dim3(unsigned(grid), unsigned(pieces)), kThreads, 0, st, src, rows, cols, all, *q);
+template <typename T, bool kBatch>
+emr_status launch_rows16(const T* p, int64_t batch_stride, int64_t row_stride, int64_t batch, int64_t rows, int64_t cols, const emr_q8* q,
+                         cudaStream_t st) {
+  const int64_t blocks = q8_blocks(cols);
+  const __int128 all = __int128(batch) * rows * blocks;
+  int dev = 0, sms = 0;
+  if (!device_sms(&dev, &sms)) return EMR_ERR_CUDA;
+  const int64_t most = int64_t(sms) * Rows16<T>::kBlocks;
+  if (all > UINT32_MAX - 4 * most * kWarps * 4) return EMR_ERR_RANGE;
+  const int64_t need = (int64_t(all) + kWarps * 4 - 1) / (kWarps * 4);
+  static std::atomic<uint64_t> done{0};
+  if (!allow_smem(q8_rows16_kernel<T, kBatch>, Rows16<T>::kSmem, dev, done)) return EMR_ERR_CUDA;
+  return launch_after(q8_rows16_kernel<T, kBatch>, dim3(unsigned(need < most ? need : most)), kThreads, size_t(Rows16<T>::kSmem), st, p,
+                      p + (batch - 1) * batch_stride + (rows - 1) * row_stride + cols, batch_stride, row_stride, uint32_t(rows),
+                      uint32_t(blocks), int32_t(cols - (blocks - 1) * 128), uint32_t(all), *q);
 }
 
 struct DenseArgs {
@@ -445,9 +524,11 @@ extern "C" emr_status emr_q8_quantize(const void* src, int32_t dtype, int32_t ba
   const DenseArgs args{src, dtype, batch, rows, cols, batch_stride, row_stride, col_stride};
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   return with_dense(args, [&](auto d) {
-    // row blocks alone: a warp a row while there are few tiles, else by tiles, which copy ahead
-    const bool tiled = qt || int64_t(batch) * q8_blocks(rows) * q8_blocks(cols) >= kTiledFrom;
-    return tiled ? launch_tile<0>(d, nullptr, batch, rows, cols, q, qt, nullptr, st) : launch_rows(d, batch, rows, cols, q, st);
+    if constexpr (d.kWhole) {
+      if (!qt && batch == 1) return launch_rows16<typename decltype(d)::Value, false>(d.p, 0, d.row_stride, 1, rows, cols, q, st);
+      if (!qt) return launch_rows16<typename decltype(d)::Value, true>(d.p, d.batch_stride, d.row_stride, batch, rows, cols, q, st);
+    }
+    return launch_tile<0>(d, nullptr, batch, rows, cols, q, qt, nullptr, st);
   });
 }
 

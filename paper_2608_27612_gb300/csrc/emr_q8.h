@@ -91,8 +91,6 @@ __device__ __forceinline__ void store_scalar(void* p, int dtype, int64_t i, floa
 template <typename T>
 struct Four {
   uint2 u;
-  __device__ __forceinline__ void load(const T* p) { u = *reinterpret_cast<const uint2*>(p); }
-  __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<uint2*>(p) = u; }
   __device__ __forceinline__ void set(int j, T v) { reinterpret_cast<T*>(&u)[j] = v; }
   __device__ __forceinline__ float4 floats() const {
     const T* e = reinterpret_cast<const T*>(&u);
@@ -102,8 +100,6 @@ struct Four {
 template <>
 struct Four<float> {
   float4 u;
-  __device__ __forceinline__ void load(const float* p) { u = *reinterpret_cast<const float4*>(p); }
-  __device__ __forceinline__ void store(float* p) const { *reinterpret_cast<float4*>(p) = u; }
   __device__ __forceinline__ void set(int j, float v) { reinterpret_cast<float*>(&u)[j] = v; }
   __device__ __forceinline__ float4 floats() const { return u; }
 };
