@@ -7,7 +7,7 @@
 // from the same registers through a 16 KB tile of codes. Bytes are the floor; by rows
 // 8192 x 8192 bfloat16 takes 33 us (6.1 TB/s), 94464 x 1364 float16 72 (5.5). The tiles of
 // both ways are bound by the instructions of the reductions and conversions (ALU pipe
-// 65%, memory 39%): 71 us (3.8 TB/s), the slope product with sums 103 (3.2).
+// 65%, memory 40%): 64 us (4.2 TB/s), the slope product with sums 93 (3.6).
 #include <cuda_runtime.h>
 
 #include "emr_q8.h"
@@ -219,8 +219,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) q8_tile_kernel(Dense<T, kLayo
     return p;
   };
   uint32_t next_scale = 127;
-  const auto copy = [&](uint32_t t, uint32_t turn) {
-    const Place p = place(t);
+  const auto copy = [&](const Place& p, uint32_t turn) {
     const int64_t c = p.ct * 128 + lane * 4;
     if (kMode != 1) {
       const int n = p.wide - lane * 4, cells = n < 0 ? 0 : n < 4 ? n : 4;
@@ -247,6 +246,8 @@ __global__ void __launch_bounds__(kTileThreads, 2) q8_tile_kernel(Dense<T, kLayo
           }
         }
       }
+      const bool inner = p.have >= 8 && p.wide == 128;
+      const T* row = from + c;
 #pragma unroll
       for (int i = 0; i < (kPieces ? 0 : 8); i++) {
         if constexpr (kLayout == kRows && sizeof(T) == 4) {
@@ -256,6 +257,11 @@ __global__ void __launch_bounds__(kTileThreads, 2) q8_tile_kernel(Dense<T, kLayo
             copy_ahead<4>(reinterpret_cast<uint32_t*>(dense + i * kTileThreads) + j, in ? from + i * src.row_stride + c + j : src.p, in ? 4 : 0);
           }
         } else if constexpr (kLayout == kFours) {
+          if (inner) {
+            copy_ahead<int(sizeof(Four<T>))>(dense + i * kTileThreads, row, int(sizeof(Four<T>)));
+            row += src.row_stride;
+            continue;
+          }
           const bool in = i < p.have && cells > 0;
           copy_ahead<int(sizeof(Four<T>))>(dense + i * kTileThreads, in ? from + i * src.row_stride + c : src.p, in ? cells * int(sizeof(T)) : 0);
         } else {
@@ -284,11 +290,11 @@ __global__ void __launch_bounds__(kTileThreads, 2) q8_tile_kernel(Dense<T, kLayo
   if (threadIdx.x < 256) (&tops[0][0][0])[threadIdx.x] = 0;
   grid_wait();
   grid_go();
-  copy(blockIdx.x, 0);
+  Place p = place(blockIdx.x), after = p;
+  copy(p, 0);
   __syncthreads();
   uint32_t turn = 0;
-  for (uint32_t t = blockIdx.x; t < tiles; t += gridDim.x, turn ^= 1) {
-    const Place p = place(t);
+  for (uint32_t t = blockIdx.x; t < tiles; t += gridDim.x, turn ^= 1, p = after) {
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     if (kFromQ8) __syncthreads();
     else if (kPieces) __syncwarp();
@@ -322,7 +328,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) q8_tile_kernel(Dense<T, kLayo
       }
     }
     if (kPieces) __syncwarp();  // the rows are read before others take their place
-    if (t + gridDim.x < tiles) copy(t + gridDim.x, turn ^ 1);
+    if (t + gridDim.x < tiles) after = place(t + gridDim.x), copy(after, turn ^ 1);
     if (sums) {
       float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
@@ -338,19 +344,35 @@ __global__ void __launch_bounds__(kTileThreads, 2) q8_tile_kernel(Dense<T, kLayo
     }
     if (q.values) {
       uint8_t* out = q.values + (p.b * rows + p.rt * 128 + first) * row_bytes + p.ct * 128 + lane * 4;
-      uint32_t mine = 0;
+      // lane i has the largest magnitude of row i, so that all eight scales are made at once (8192 x
+      // 8192 bfloat16 both ways 70 us with one after the other, 64 so)
+      uint32_t most = 0;
 #pragma unroll
       for (int i = 0; i < 8; i++) {
-        const uint32_t byte = q8_warp_scale(v[i]);
-        const uint32_t codes4 = q8_pack4(v[i].x, v[i].y, v[i].z, v[i].w, q8_inverse(byte));
+        const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(q8_top4(v[i])));
+        most = lane == i ? top : most;
+      }
+      if (__any_sync(0xffffffffu, most >= 0x7f800000u)) {  // an infinity, or nothing but NaN in some lane
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+          const uint32_t top = __reduce_max_sync(0xffffffffu, max(max(q8_magnitude(v[i].x), q8_magnitude(v[i].y)),
+                                                                  max(q8_magnitude(v[i].z), q8_magnitude(v[i].w))));
+          most = lane == i ? top : most;
+          v[i] = make_float4(q8_finite_or_nan(v[i].x), q8_finite_or_nan(v[i].y), q8_finite_or_nan(v[i].z), q8_finite_or_nan(v[i].w));
+        }
+      }
+      const uint32_t mine = q8_scale_byte(most);
+      const float mine_inv = q8_inverse(mine);
+#pragma unroll
+      for (int i = 0; i < 8; i++) {
+        const uint32_t codes4 = q8_pack4(v[i].x, v[i].y, v[i].z, v[i].w, __shfl_sync(0xffffffffu, mine_inv, i));
         if (i < p.have) *reinterpret_cast<uint32_t*>(out) = codes4;
         if (kMode == 3) {
           const float4 d = q8_unpack4(codes4);
-          const float s = q8_scale(byte);
+          const float s = q8_scale(__shfl_sync(0xffffffffu, mine, i));
           v[i] = make_float4(d.x * s, d.y * s, d.z * s, d.w * s);
         }
         out += row_bytes;
-        if (lane == i) mine = byte;
       }
       if (lane < 8 && lane < p.have) q.scales[p.b * scale_batch + q8_scale_at(chunks, p.rt * 128 + first + lane, p.ct)] = uint8_t(mine);
     }
