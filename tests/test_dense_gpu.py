@@ -102,6 +102,50 @@ def test_quantize_extremes():
         assert same(back(qt), f32(OD.held(np.swapaxes(f64(x), 1, 2))))
 
 
+def test_quantize_extremes_by_rows():
+    """The rows of test_quantize_extremes that hold no finite value beyond 32 bits, at both alignments of a row."""
+    x = torch.zeros(1, 9, 261)
+    x[0, 1] = 1e-45
+    x[0, 2, ::3] = 3e-39
+    x[0, 3] = torch.linspace(-1, 1, 261)
+    x[0, 3, 9], x[0, 3, 130] = float("inf"), float("-inf")
+    x[0, 4] = torch.linspace(-3, 3, 261)
+    x[0, 4, 100] = float("nan")
+    x[0, 5] = float("nan")
+    x[0, 6] = float("inf")
+    x[0, 7, 0], x[0, 7, 1:] = 448.0, torch.arange(1, 261) / 64 + 16.5
+    x[0, 8, 128:] = -2.0 ** -126
+    for dtype in DTYPES:
+        v = x.cuda().to(dtype)
+        for w in (v, v[:, :, :256].contiguous(), v[:, 1:, 5:]):
+            q, _ = emr.q8_quantize(w)
+            assert same(back(q), OD.held(f64(w)))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("cols", [1, 15, 16, 17, 112, 127, 128, 130, 300])
+def test_quantize_rows_at_any_alignment(cols, dtype):
+    """Rows that start at every element of 16 bytes, with NaN all around them: nothing but the row counts."""
+    for start in range(16 // dtype.itemsize):
+        for gap in (0, 1, 3, 8):
+            base = torch.full((start + 7 * (cols + gap) + 64,), float("nan"), dtype=dtype, device="cuda")
+            x = base[start:start + 7 * (cols + gap)].view(7, cols + gap)[:, :cols].unsqueeze(0)
+            x.copy_(normal(start, 1, 7, cols, dtype=dtype))
+            q, _ = emr.q8_quantize(x)
+            assert same(back(q), OD.held(f64(x)))
+    one = normal(3, 1, 1, cols, dtype=dtype).expand(2, 5, cols)  # one row in the place of all
+    q, _ = emr.q8_quantize(one)
+    assert same(back(q), OD.held(f64(one)))
+
+
+@pytest.mark.parametrize("shape", [(1, 50001, 70), (3, 9000, 130), (30000, 3, 40), (1, 700, 20001)])
+def test_quantize_rows_of_many_turns(shape):
+    """More blocks than the device takes at a time; batches that end inside a turn."""
+    x = normal(5, *shape, dtype=torch.float16)
+    q, _ = emr.q8_quantize(x)
+    assert same(back(q), OD.held(f64(x)))
+
+
 @pytest.mark.parametrize("shape", [(1, 1, 5), (2, 130, 257), (1, 1000, 640)])
 def test_transpose(shape):
     q, _ = emr.q8_quantize(normal(3, *shape, spread=3.0))
@@ -135,6 +179,16 @@ SIZES = [(1, 1, 1, 1, 1), (1, 1, 1, 130, 128), (1, 1, 3, 5, 700), (1, 1, 8, 1364
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_product(nets_a, nets_w, m, n, k, dtype):
     a, w = product_case(nets_a, nets_w, m, n, k)
+    out = f64(emr.q8_matmul(a, w, out_dtype=dtype))
+    z, mag = OD.product(back(a), back(w))
+    assert np.all(np.abs(out - z) <= (k + 2) * 2.0 ** -23 * mag + ULP[dtype] * np.abs(z) * 1.01 + 2.0 ** -25)
+
+
+@pytest.mark.parametrize("nets,m,n,k", [(1, 65, 64, 300), (7, 5000, 45, 200), (40, 1500, 64, 130), (9, 2300, 30, 700), (3, 9000, 1, 90)])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_product_of_few_columns(nets, m, n, k, dtype):
+    """At most 64 columns and more tiles than there are SMs: the epilogue's warps take turns."""
+    a, w = product_case(1, nets, m, n, k)
     out = f64(emr.q8_matmul(a, w, out_dtype=dtype))
     z, mag = OD.product(back(a), back(w))
     assert np.all(np.abs(out - z) <= (k + 2) * 2.0 ** -23 * mag + ULP[dtype] * np.abs(z) * 1.01 + 2.0 ** -25)
