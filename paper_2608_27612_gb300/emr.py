@@ -773,16 +773,17 @@ class Saved:
     """What a training step keeps between the passes, in 8 bits: xt, the transpose [nx, k, m] of x, as the weight
     gradient reads it, and slope, act'(z) [nets, m, n] (None: identity). nx, m: batch and rows of x."""
 
-    def __init__(self, layer, nx: int, m: int, xt, slope):
-        self._layer, self.nx, self.m, self._xt, self._slope = layer, nx, m, xt, slope
+    def __init__(self, layer, nx: int, m: int, data, split: int):
+        # one piece of memory: xt, then, from `split` on (0: none), slope
+        self._layer, self.nx, self.m, self._data, self._split = layer, nx, m, data, split
 
     @property
     def xt(self) -> Q8:
-        return Q8.of(self._xt, self.nx, self._layer.k, self.m)
+        return Q8.of(self._data[:self._split or None], self.nx, self._layer.k, self.m)
 
     @property
     def slope(self) -> Q8 | None:
-        return Q8.of(self._slope, self._layer.nets, self.m, self._layer.n) if self._slope is not None else None
+        return Q8.of(self._data[self._split:], self._layer.nets, self.m, self._layer.n) if self._split else None
 
 
 class DenseLayer:
@@ -809,7 +810,7 @@ class DenseLayer:
             self.w8t = Q8(self.nets, self.k, self.n, device=w.device) if train else None
         self.c = DenseC(self.w8.c, self.w8t.c if train else Q8C(), None, act, 0)
         self._ref = C.byref(self.c)
-        self._room, self._back = {}, {}
+        self._room, self._kept, self._back = {}, {}, {}
         self._w8 = self.w8.ref, self.w8t.ref if train else None
         self.set_weights(w, b, stream)
 
@@ -836,7 +837,7 @@ class DenseLayer:
         self.c.bias = b.data_ptr() if b is not None else None
 
     def _needs_room(self, nx, m):
-        """Whether a forward pass without keep needs memory for x in 8 bits (emr_dense_forward_room)."""
+        """Bytes that a forward pass without keep needs for x in 8 bits (emr_dense_forward_room)."""
         got = self._room.get((nx, m))
         if got is None:
             a, b, c = C.c_size_t(), C.c_size_t(), C.c_size_t()
@@ -844,7 +845,17 @@ class DenseLayer:
                    "emr_dense_forward_room")
             if len(self._room) > 64:
                 self._room.clear()
-            got = self._room[(nx, m)] = a.value > 0
+            got = self._room[(nx, m)] = a.value
+        return got
+
+    def _kept_bytes(self, nx, m):
+        """Bytes of x in 8 bits, of its transpose and of the slopes (0: identity) in a training step."""
+        got = self._kept.get((nx, m))
+        if got is None:
+            if len(self._kept) > 64:
+                self._kept.clear()
+            slope = sum(_q8_bytes(self.nets, m, self.n)) if self.act != ACT_IDENTITY else 0
+            got = self._kept[(nx, m)] = sum(_q8_bytes(nx, m, self.k)), sum(_q8_bytes(nx, self.k, m)), slope
         return got
 
     def _forward(self, x, out_dtype, stream, keep):
@@ -860,26 +871,29 @@ class DenseLayer:
         if m == 0:
             if keep:
                 raise ValueError("x: at least one row is wanted for training")
-            return torch.empty(self.nets, 0, self.n, dtype=out_dtype, device=dev), None, None
+            return torch.empty(self.nets, 0, self.n, dtype=out_dtype, device=dev), None, 0
         if stream is not None and stream != torch.cuda.current_stream(dev):
             with torch.cuda.stream(stream):   # allocations belong to the stream that they are used on
                 return self._forward(x, out_dtype, None, keep)
         out = torch.empty((self.nets, m, self.n), dtype=out_dtype, device=dev)
-        xq = xt = slope = xp = tp = sp = None
-        if keep or self._needs_room(nx, m):
-            xq = torch.empty(sum(_q8_bytes(nx, m, k)), dtype=torch.uint8, device=dev)
-            xp = xq.data_ptr()
+        kept = xp = tp = sp = None
+        split = 0
         if keep:
-            xt = torch.empty(sum(_q8_bytes(nx, k, m)), dtype=torch.uint8, device=dev)
-            tp = xt.data_ptr()
-        if keep and self.act != ACT_IDENTITY:
-            slope = torch.empty(sum(_q8_bytes(self.nets, m, self.n)), dtype=torch.uint8, device=dev)
-            sp = slope.data_ptr()
+            room, xt_bytes, slope_bytes = self._kept_bytes(nx, m)
+            kept = torch.empty(xt_bytes + slope_bytes, dtype=torch.uint8, device=dev)
+            tp = kept.data_ptr()
+            if slope_bytes:
+                split, sp = xt_bytes, tp + xt_bytes
+        else:
+            room = self._needs_room(nx, m)
+        if room:
+            xq = torch.empty(room, dtype=torch.uint8, device=dev)
+            xp = xq.data_ptr()
         status = _lib.emr_dense_forward(self._ref, x.data_ptr(), kind, nx, m, *x.stride(), out.data_ptr(), out_kind,
                                         1 if keep else 0, xp, tp, sp, torch._C._cuda_getCurrentRawStream(dev.index))
         if status:
             _check(status, "emr_dense_forward")
-        return out, xt, slope
+        return out, kept, split
 
     def forward(self, x, out_dtype=torch.float32, stream=None):
         """y [nets, m, n] of out_dtype. m = 0 gives an empty result."""
@@ -889,8 +903,8 @@ class DenseLayer:
         """(y, saved): saved holds x and act'(z) in 8 bits for backward."""
         if not self.train:
             raise ValueError("forward_train: the layer was made with train=False")
-        y, xt, slope = self._forward(x, out_dtype, stream, True)
-        return y, Saved(self, x.shape[0] if x.dim() == 3 else 1, y.shape[1], xt, slope)
+        y, kept, split = self._forward(x, out_dtype, stream, True)
+        return y, Saved(self, x.shape[0] if x.dim() == 3 else 1, y.shape[1], kept, split)
 
     def backward(self, dy, saved: Saved, out_dtype=torch.float32, stream=None):
         """(dx, dw, db) of out_dtype for dy [nets, m, n]: dx [1 or nets, m, k] as forward_train took x (summed
@@ -919,9 +933,9 @@ class DenseLayer:
         dw = torch.empty((self.nets, self.n, self.k), dtype=out_dtype, device=dev)
         db = torch.empty((self.nets, self.n), dtype=out_dtype, device=dev)
         ws = torch.empty(room, dtype=torch.uint8, device=dev)
-        status = _lib.emr_dense_backward(self._ref, dy.data_ptr(), kind, nx, m, saved._xt.data_ptr(),
-                                         saved._slope.data_ptr() if saved._slope is not None else None, dx.data_ptr(),
-                                         dw.data_ptr(), db.data_ptr(), out_kind, ws.data_ptr(), room,
+        kept, split = saved._data.data_ptr(), saved._split
+        status = _lib.emr_dense_backward(self._ref, dy.data_ptr(), kind, nx, m, kept, kept + split if split else None,
+                                         dx.data_ptr(), dw.data_ptr(), db.data_ptr(), out_kind, ws.data_ptr(), room,
                                          torch._C._cuda_getCurrentRawStream(dev.index))
         if status:
             _check(status, "emr_dense_backward")
