@@ -721,12 +721,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 // each row, so its stores are neighbours. The same kernel serves larger a with few tiles
 // and a long contraction (the gradient of an input that many networks share). 8 x 8192 x
 // 8192: 9.8 us with the weights in L2, 20 from memory (3.3 TB/s), where tiles of 128 rows took
-// 21 and 31; 250 x 256 summed over 64 networks of 340: 57 -> 13 us.
+// 21 and 31; 250 x 256 summed over 64 networks of 340: 57 -> 11 us
+// (13 with clusters of 8).
 
 constexpr int kThinStages = 6;     // at most; q.stages of them are used
 constexpr int kThinThreads = 320;  // copy warp, matrix warp, eight epilogue warps
 constexpr int kThinColumns = 256;  // of tensor memory: half of it
-constexpr int kThinMaxSplit = 8;
 
 struct ThinParams {
   Params p;
@@ -1000,20 +1000,50 @@ emr_status launch(const CUtensorMap& a, const CUtensorMap& w, const Params& p, i
   return launch_after(q8_matmul_kernel<kSlope>, dim3(unsigned(p.tiles < sms ? p.tiles : sms)), kThreads, kSmemBytes, st, a, w, p);
 }
 
+// Clusters of 16 blocks of the thin kernel that run at once (0: none), asked once for each device
+// and kind of block.
+int clusters_of_16(int dev, bool small, size_t smem) {
+  static std::atomic<int> known[64][2];  // 1 + the answer
+  if (dev >= 64) return 0;
+  std::atomic<int>& slot = known[dev][small];
+  int n = slot.load(std::memory_order_relaxed);
+  if (n == 0) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(16);
+    cfg.blockDim = dim3(kThinThreads);
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = 16, attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int fit = 0;
+    if (cudaFuncSetAttribute(q8_thin_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&fit, q8_thin_kernel, &cfg) != cudaSuccess)
+      fit = 0, cudaGetLastError();  // the question's error is not the caller's
+    n = 1 + fit;
+    slot.store(n, std::memory_order_relaxed);
+  }
+  return n - 1;
+}
+
 emr_status launch_thin(const emr_q8* a, const emr_q8* w, const Params& p, int dev, int sms, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
   ThinParams q{};
   q.p = p;
   q.wide = p.M <= 16 ? 16 : p.M <= 32 ? 32 : p.M <= 64 ? 64 : 128;
-  // As many blocks to a tile as find room, with two blocks of columns for each.
+  // As many blocks to a tile as find room, with two blocks of columns for each; 16 of them, which not
+  // every device takes, where that many clusters run at once.
   q.split = 1;
   const int64_t room = q.wide <= 64 ? 2 * sms : sms;  // 100 KB a block up to 64 rows
-  while (q.split < kThinMaxSplit && int64_t(p.tiles) * q.split * 2 <= room && int64_t(p.sum) * p.k_blocks >= 4 * q.split) q.split *= 2;
+  const auto more = [&] { return int64_t(p.tiles) * q.split * 2 <= room && int64_t(p.sum) * p.k_blocks >= 4 * q.split; };
+  while (q.split < 8 && more()) q.split *= 2;
   CUtensorMap a_map, w_map;
   if (!operand_map(a, &a_map, q.wide) || !operand_map(w, &w_map)) return EMR_ERR_CUDA;
   q.stages = q.wide <= 64 ? 4 : 6;
   const int smem = 1024 + q.stages * thin_stage_bytes(q.wide);  // the shares, wide rows of 512 bytes, fit in w's stages
   if (!allow_smem(q8_thin_kernel, 1024 + kThinStages * thin_stage_bytes(128), dev, done)) return EMR_ERR_CUDA;
+  if (q.split == 8 && more() && p.tiles <= clusters_of_16(dev, q.wide <= 64, size_t(smem))) q.split = 16;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(unsigned(q.split > 1 ? p.tiles * q.split : p.tiles < room ? p.tiles : room));
   cfg.blockDim = dim3(kThinThreads);
