@@ -319,17 +319,17 @@ __device__ __forceinline__ void finish_chunk(const Params& p, const Tile& t, uin
 
 constexpr int kFinishBarrier = 5;  // of all epilogue warps; 1 to 4 are the quarters
 __device__ __forceinline__ void finish_sync() { asm volatile("bar.sync %0, %1;" ::"n"(kFinishBarrier), "n"(32 * kFinishWarps) : "memory"); }
-// Whether the accumulators of a tile are there; with kSlope with one answer for all epilogue
-// warps, since they then meet at barriers while finishing the tile.
+// Whether the accumulators of a tile are there; with kSlope with one answer for the warps that then
+// meet at barriers while finishing the tile: `count` threads at barrier `id`.
 template <bool kSlope>
-__device__ __forceinline__ bool finish_wait(uint32_t bar, uint32_t parity, volatile int* stop, int code) {
+__device__ __forceinline__ bool finish_wait(uint32_t bar, uint32_t parity, volatile int* stop, int code, int id, int count) {
   const bool ok = warp_wait(bar, parity, stop, code);
   if (!kSlope) return ok;
   uint32_t all;
   asm volatile(
       "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.and.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
       : "=r"(all)
-      : "r"(uint32_t(ok)), "n"(kFinishBarrier), "n"(32 * kFinishWarps)
+      : "r"(uint32_t(ok)), "r"(id), "r"(count)
       : "memory");
   return all != 0;
 }
@@ -455,7 +455,7 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
       const Tile tile = tile_at(p, t);
       const int row0 = tile.m * kTileM + quadrant * 32, n = tile.n * kTileN + c * 32 + lane;
       const float bias = p.bias && n < p.N ? __ldg(p.bias + int64_t(tile.b) * p.N + n) : 0.f;
-      if (!finish_wait<kSlope>(acc_full + 8 * acc, (n_tile >> 1) & 1, stop, 4)) break;
+      if (!finish_wait<kSlope>(acc_full + 8 * acc, (n_tile >> 1) & 1, stop, 4, 1 + quadrant, 128)) break;
       fence_after();
       if (row0 >= p.M || (!kSlope && n - lane >= p.N)) {  // nothing of this warp's part is in the matrix
         if (lane == 0) bar_arrive(acc_empty + 8 * acc);
@@ -675,7 +675,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const int n = tile.n * kTileN + c * 32 + lane;
         const float bias = p.bias && n < p.N ? __ldg(p.bias + int64_t(tile.b) * p.N + n) : 0.f;
         if (half) {
-          if (!finish_wait<kSlope>(acc_full + 8 * acc, (n_tile >> 1) & 1, stop, 9)) goto out;
+          if (!finish_wait<kSlope>(acc_full + 8 * acc, (n_tile >> 1) & 1, stop, 9, kFinishBarrier, 32 * kFinishWarps)) goto out;
           fence_after();
         }
         // The columns that the next tile's scales are waiting for are read before all others; without
