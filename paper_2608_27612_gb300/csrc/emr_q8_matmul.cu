@@ -167,6 +167,7 @@ struct Params {
   int32_t out_dtype, store_bytes;   // store_bytes: widest store that every row of out is aligned to
   int32_t narrow;                   // at most 64 columns, no slopes: half of the epilogue's warps for each accumulator
   uint8_t *slope, *slope_scales;
+  int32_t slope_whole;              // slope begins at a multiple of 32 bytes
 };
 
 struct Tile {
@@ -233,10 +234,16 @@ struct Finish {
   float tops[2][128][4];  // largest slope of a row's 32 columns, two turns
   float bias[kFinishWarps][32];
 };
-__device__ __forceinline__ void store32(uint8_t* to, const uint32_t (&w)[8]) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
-               "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-               : "memory");
+// 32 bytes to an address that is a multiple of 16; `whole`: of 32, which one store of them asks for.
+// Predicated: a branch made the pair kernel spill.
+__device__ __forceinline__ void store32(uint8_t* to, const uint32_t (&w)[8], int32_t whole) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %9, 0;\n\t"
+      "@p st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};\n\t"
+      "@!p st.global.v4.b32 [%0], {%1, %2, %3, %4};\n\t"
+      "@!p st.global.v4.b32 [%0 + 16], {%5, %6, %7, %8};\n\t}" ::"l"(to),
+      "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]), "r"(whole)
+      : "memory");
 }
 
 // A warp's 32 rows and 32 columns (c-th of four) of one 128-column accumulator block at tensor
@@ -311,7 +318,7 @@ __device__ __forceinline__ void finish_chunk(const Params& p, const Tile& t, uin
 #pragma unroll
       for (int i = 0; i < 8; i++) w[i] = q8_pack4(d[4 * i], d[4 * i + 1], d[4 * i + 2], d[4 * i + 3], inv);
       const int row = row0 + lane;
-      store32(p.slope + (int64_t(t.b) * p.M + row) * q8_row_bytes(p.N) + n0, w);
+      store32(p.slope + (int64_t(t.b) * p.M + row) * q8_row_bytes(p.N) + n0, w, p.slope_whole);
       if (c == 0) p.slope_scales[t.b * q8_scale_batch(p.M, p.N) + q8_scale_at(q8_scale_chunks(p.N), row, t.n)] = uint8_t(byte);
     }
   }
@@ -1114,7 +1121,7 @@ extern "C" emr_status emr_q8_matmul(const emr_q8* a, const emr_q8* w, const floa
   p.store_bytes = 16;
   while (p.store_bytes > size && (reinterpret_cast<uintptr_t>(out) % p.store_bytes || (int64_t(p.N) * size) % p.store_bytes)) p.store_bytes >>= 1;
   p.narrow = !slope && p.N <= 64;
-  if (slope) p.slope = slope->values, p.slope_scales = slope->scales;
+  if (slope) p.slope = slope->values, p.slope_scales = slope->scales, p.slope_whole = reinterpret_cast<uintptr_t>(slope->values) % 32 == 0;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   int dev = 0, sms = 0;
   if (!device_sms(&dev, &sms)) return EMR_ERR_CUDA;

@@ -1,0 +1,64 @@
+"""Dense layers at the edges of what their calls accept, against the same calls inside them or the definitions
+(oracle.dense; the bounds are those of test_dense_gpu.py)."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import dense as OD
+from paper_2608_27612_gb300 import emr
+
+pytestmark = pytest.mark.gpu
+
+
+def normal(seed, *shape, dtype=torch.float32):
+    return torch.from_numpy(np.random.default_rng(seed).standard_normal(shape).astype(np.float32)).cuda().to(dtype)
+
+
+def f64(t):
+    return t.double().cpu().numpy()
+
+
+def q8_at(offset, batch, rows, cols):
+    """A Q8 whose buffers begin `offset` bytes after a multiple of 256, filled with a byte, and its memory."""
+    n = sum(emr._q8_bytes(batch, rows, cols))
+    room = torch.full((n + 512,), 0x5a, dtype=torch.uint8, device="cuda")
+    start = -room.data_ptr() % 256 + offset
+    return emr.Q8.of(room[start:start + n], batch, rows, cols), room, start
+
+
+# few rows, single blocks' tiles, and pairs of SMs; a second batch of odd rows
+@pytest.mark.parametrize("nets,m,n,k", [(1, 5, 40, 64), (2, 150, 203, 300), (1, 3100, 2400, 5100)])
+@pytest.mark.parametrize("offset", [16, 48, 112, 240])
+def test_slopes_at_every_multiple_of_16_bytes(nets, m, n, k, offset):
+    a, w = (emr.q8_quantize(normal(s, nets, r, k) / np.sqrt(np.sqrt(k)))[0] for s, r in ((1, m), (2, n)))
+    want = emr.Q8(nets, m, n)
+    y = emr.q8_matmul(a, w, act=emr.ACT_TANH, slope=want)
+    got, room, start = q8_at(offset, nets, m, n)
+    assert got.values.data_ptr() % 32 == 16
+    assert torch.equal(y, emr.q8_matmul(a, w, act=emr.ACT_TANH, slope=got))
+    assert torch.equal(got.values, want.values)
+    assert torch.equal(emr.q8_dequantize(got), emr.q8_dequantize(want))
+    assert bool((room[:start] == 0x5a).all()) and bool((room[start + got.data.numel():] == 0x5a).all())
+    assert emr.device_error() == 0
+
+
+def test_training_step_into_memory_at_16_bytes():
+    """emr_dense_forward with x8, xt and slope at 16 bytes after a multiple of 32, and its backward pass."""
+    nets, m, n, k = 2, 70, 130, 90
+    layer = emr.DenseLayer(normal(3, nets, n, k) / 9, act=emr.ACT_GAUSS, train=True)
+    x, dy = normal(4, nets, m, k), normal(5, nets, m, n)
+    y, saved = layer.forward_train(x)
+    L, sizes = emr.lib(), [C.c_size_t() for _ in range(4)]
+    assert L.emr_dense_forward_room(layer._ref, nets, m, 1, *[C.byref(s) for s in sizes[:3]]) == emr.EMR_OK
+    assert L.emr_dense_backward_room(layer._ref, nets, m, C.byref(sizes[3])) == emr.EMR_OK
+    rooms = [torch.empty(s.value + 256, dtype=torch.uint8, device="cuda") for s in sizes]
+    x8, xt, slope, ws = (r.data_ptr() + (16 - r.data_ptr()) % 32 for r in rooms)
+    out, stream = torch.empty_like(y), torch.cuda.current_stream().cuda_stream
+    assert L.emr_dense_forward(layer._ref, x.data_ptr(), 0, nets, m, *x.stride(), out.data_ptr(), 0, 1, x8, xt, slope, stream) == emr.EMR_OK
+    dx, dw, db = (torch.empty(s, device="cuda") for s in ((nets, m, k), (nets, n, k), (nets, n)))
+    assert L.emr_dense_backward(layer._ref, dy.data_ptr(), 0, nets, m, xt, slope, dx.data_ptr(), dw.data_ptr(), db.data_ptr(), 0, ws,
+                                sizes[3], stream) == emr.EMR_OK
+    assert torch.equal(out, y)
+    assert all(torch.equal(a, b) for a, b in zip((dx, dw, db), layer.backward(dy, saved)))
