@@ -769,6 +769,8 @@ __global__ void __launch_bounds__(kThreads, 2048 / kThreads > 4 ? 4 : kThreads =
   r.scratch = scratch, r.slots = slots, r.found = found, r.list_size = list_size, r.coarse = coarse, r.rest = &rest;
   r.lists = 0, r.counted = false;
   if (threadIdx.x < 3) list_size[threadIdx.x] = 0;
+  // a block's shared memory is written by others only when it is known to run; waited for after the loads
+  if (r.blocks > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   r.sums = reinterpret_cast<u64*>(smem);  // the first 256 steps; shares its memory with lacks
   r.lacks = reinterpret_cast<uint32_t*>(smem);
   r.counts = r.lacks + a.bins;
@@ -805,6 +807,7 @@ __global__ void __launch_bounds__(kThreads, 2048 / kThreads > 4 ? 4 : kThreads =
   }
   r.held = r.groups < a.room ? r.groups : a.room;
   const uint32_t own = order_key(top);
+  if (r.blocks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   const u64 top_key = r.row_max(r.block_max(own));
   if (top_key == 0) {  // nothing left
     if (r.rank == 0 && r.tid == 0) {
