@@ -42,6 +42,10 @@ constexpr int kMaxCluster = 8;
 constexpr float kSpan = 16.f;    // the equal steps cover w in (e^-16, 1]; the last one takes the rest
 constexpr float kNear = 6e-5f;   // of the draw's first computation, in units of log2
 constexpr float kLackUnit = 1048576.f;
+// A step's lacks are summed in 32 bits. An entry's is at most 2^24 / (steps - 1), so (steps - 1) 127 entries of a
+// block stay below 2^31: 63 turns of each_group with the 8 entries a turn of a thread, at 4 steps a thread. Longer
+// slices carry what is above 2^31 into a second word every so many turns.
+constexpr int kCarryTurns = 63;
 
 struct Args {
   const void* scores;
@@ -58,6 +62,7 @@ struct Args {
   int32_t room;                  // groups of 16 bytes of a slice that shared memory holds
   int32_t noise_vector;          // rows of noise are aligned to 16 bytes
   int32_t fix;                   // sums of w are kept in steps of 2^-fix
+  int32_t carry;                 // lacks have a second word
 };
 
 // Order-preserving integer of a score that is not masked; masked ones give 0.
@@ -116,7 +121,7 @@ struct Row {
   uint4* data;      // and in shared memory
   const float* noise;   // of the row
   uint32_t data_at, counts_at, lacks_at;  // addresses in shared memory, for the inner loops
-  uint32_t *counts, *lacks;
+  uint32_t *counts, *lacks;  // and, with a.carry, the lacks' second words behind the counts
   u64 *sums, *list, *sorted;
   uint4* scratch;   // [2][32], by turns: a turn's values are read by all before the next but one writes
   uint4* slots;     // [2][kMaxCluster]
@@ -154,9 +159,10 @@ struct Row {
   }
   // fn(scores, i) for kAhead groups, loaded together, of every block's: scores[u][j] is entry i + u
   // threads kG + j of the slice, and -infinity past it (i may be below 0).
+  // Of the groups from first to before past, apart by whole turns.
   template <typename Fn>
-  __device__ __forceinline__ void each_group(Fn fn) const {
-    for (int g = tid; g < groups; g += threads * kAhead) {
+  __device__ __forceinline__ void each_group(Fn fn, int first, int past) const {
+    for (int g = first + tid; g < past; g += threads * kAhead) {
       Group<T> v[kAhead];
 #pragma unroll
       for (int u = 0; u < kAhead; u++) {
@@ -178,9 +184,11 @@ struct Row {
       fn(s, g * kG - skip);
     }
   }
+  template <typename Fn>
+  __device__ __forceinline__ void each_group(Fn fn) const { each_group(fn, 0, groups); }
   // fn(score, entry of the slice); past the slice, too, with -infinity.
   template <typename Fn>
-  __device__ __forceinline__ void each(Fn fn) const {
+  __device__ __forceinline__ void each(Fn fn, int first, int past) const {
     each_group([&](const float (&s)[kAhead][kG], int i) {
 #pragma unroll
       for (int u = 0; u < kAhead; u++) {
@@ -188,8 +196,10 @@ struct Row {
 #pragma unroll
         for (int j = 0; j < kG; j++) fn(s[u][j], i + u * threads * kG + j);
       }
-    });
+    }, first, past);
   }
+  template <typename Fn>
+  __device__ __forceinline__ void each(Fn fn) const { each(fn, 0, groups); }
   __device__ __forceinline__ float weight(float s) const { return expf(__fdiv_rn(s - s_max, temperature)); }
   __device__ __forceinline__ float rough_weight(float s) const { return fast_exp2((s - s_max) * exp2_per); }
   __device__ __forceinline__ u64 fixed(float w) const { return __float2ull_rn(w * __int_as_float((127 + a.fix) << 23)); }
@@ -346,7 +356,10 @@ struct Row {
     if (b == a.bins - 1) return fixed(*rest);  // one block's; see locate
     return __float2ull_rn(float((c << 20) - l) * expf(float(b) * (-kSpan / float(a.bins - 1))) * __int_as_float((127 + a.fix - 20) << 23));
   }
-  __device__ __forceinline__ u64 second(Kind kind, int b) const { return kind == kSums ? sums[b] : kind == kLacks ? lacks[b] : 0; }
+  __device__ __forceinline__ u64 lack(const uint32_t* of, int b) const {
+    return a.carry ? of[b] + (u64(of[2 * a.bins + b]) << 31) : of[b];
+  }
+  __device__ __forceinline__ u64 second(Kind kind, int b) const { return kind == kSums ? sums[b] : kind == kLacks ? lack(lacks, b) : 0; }
   template <typename V>
   __device__ __forceinline__ const V* of_block(const V* p, int r) const { return cluster.map_shared_rank(p, r); }
 
@@ -432,7 +445,7 @@ struct Row {
           if (r < blocks) {
             c += of_block(counts, r)[b];
             if (kind == kSums) l += of_block(sums, r)[b];
-            if (kind == kLacks) l += of_block(lacks, r)[b];
+            if (kind == kLacks) l += lack(of_block(lacks, r), b);
           }
         if (kind == kLacks && b == a.bins - 1) {
           for (int r = 0; r < blocks; r++) v += fixed(*of_block(rest, r));
@@ -450,6 +463,7 @@ struct Row {
       counts[i] = 0;
       if (wide) sums[i] = 0;
       else lacks[i] = 0;
+      if (!wide && a.carry) lacks[2 * a.bins + i] = 0;
     }
     __syncthreads();
   }
@@ -475,7 +489,7 @@ struct Row {
     const float width = kSpan / float(a.bins - 1);
     const int last = a.bins - 1;
     float below = 0.f;
-    each([&](float s, int i) {
+    const auto add = [&](float s, int i) {
       const bool ok = (s > -INFINITY) & in(s, uint32_t(lo + i));
       const float up = fminf(step_up(s, per), last_up());
       const int at = int(__float_as_uint(up) & 0x7fffffu);
@@ -487,7 +501,16 @@ struct Row {
         const float lack = x * fmaf(x, fmaf(x, 1.f / 6.f, -0.5f), 1.f) * kLackUnit + 0x1p+23f;
         shared_add(ok & (at != last), lacks_at + at * 4, __float_as_uint(lack) & 0x7fffffu);
       }
-    });
+    };
+    const int turns = a.carry ? kCarryTurns * threads * kAhead : groups;
+    for (int from = 0; from < groups; from += turns) {
+      if (from) {
+        __syncthreads();
+        for (int i = tid; i < a.bins; i += threads) lacks[2 * a.bins + i] += lacks[i] >> 31, lacks[i] &= 0x7fffffffu;
+        __syncthreads();
+      }
+      each(add, from, groups - from < turns ? groups : from + turns);
+    }
     if (__syncthreads_or(below > 0.f)) below = block_sum(below);
     if (by_mass) {
       if (tid == 0) *rest = below;
@@ -775,7 +798,7 @@ __global__ void __launch_bounds__(kThreads, 2048 / kThreads > 4 ? 4 : kThreads =
   r.lacks = reinterpret_cast<uint32_t*>(smem);
   r.counts = r.lacks + a.bins;
   r.sorted = r.sums;  // the histogram is done with when entries are ordered
-  r.list = reinterpret_cast<u64*>(r.counts + a.bins);
+  r.list = reinterpret_cast<u64*>(r.counts + (a.carry ? 2 : 1) * a.bins);
   r.data = reinterpret_cast<uint4*>(r.list + a.cap);
   r.data_at = uint32_t(__cvta_generic_to_shared(r.data));
   r.counts_at = uint32_t(__cvta_generic_to_shared(r.counts)), r.lacks_at = uint32_t(__cvta_generic_to_shared(r.lacks));
@@ -947,12 +970,13 @@ emr_status plan(Args a, int rows, bool free, int dev, int sms, cudaStream_t st) 
   // and what a short slice needs.
   a.bins = free ? 0 : !wide ? 512 : crowd ? 2048 : 4096;
   a.cap = free ? 0 : !wide ? 512 : crowd ? 1024 : 2048;
-  size_t smem = size_t(a.bins) * 8 + size_t(a.cap) * 8;
+  const int threads = !wide ? 256 : crowd ? 512 : 1024;
+  a.carry = !free && a.slice + 16 > int64_t(kCarryTurns) * threads * 8;
+  size_t smem = size_t(a.bins) * (a.carry ? 12 : 8) + size_t(a.cap) * 8;
   const size_t most = wide && !crowd ? kMostSmem : 110 * 1024;
   const size_t want = size_t(a.slice) * sizeof(T) + 16, room = most > smem ? most - smem : 0;
   a.room = int32_t((want < room ? want : room) / 16);
   smem += size_t(a.room) * 16;
-  const int threads = !wide ? 256 : crowd ? 512 : 1024;
   if (free)
     return threads == 256 ? launch<T, 256, true>(a, rows, cluster, smem, dev, st)
            : threads == 512 ? launch<T, 512, true>(a, rows, cluster, smem, dev, st) : launch<T, 1024, true>(a, rows, cluster, smem, dev, st);
