@@ -593,12 +593,11 @@ struct Row {
           for (int j0 = 0; j0 < m; j0 += threads) {
             const int j = j0 + tid;
             u64 all;
-            const float s = j < m ? key_score(uint32_t(sorted[j] >> 32)) : 0.f;
-            const u64 w = j < m ? fixed(weight(s)) : 0;
-            const u64 ahead = run + scan(w, &all);
+            const float s = j < m ? key_score(uint32_t(sorted[j] >> 32)) : 0.f, w = j < m ? weight(s) : 0.f;
+            const u64 ahead = run + scan(fixed(w), &all);
             if (j < m && ahead < target) {
               last = uint32_t(j) + 1;
-              if (with_draw) need_mass = true, consider(true, s, ~uint32_t(sorted[j]), noise[~uint32_t(sorted[j])]);
+              if (with_draw) list_consider(s, w, ~uint32_t(sorted[j]));
             }
             run += all;
           }
@@ -662,17 +661,34 @@ struct Row {
 
   // ---- the draw --------------------------------------------------------------------------
 
-  __device__ __forceinline__ void consider(bool stays, float s, uint32_t at, float e) {
+  // Whether the entry is so near the least that stays that recount has to look at it.
+  template <bool kMinP, bool kMass = true>
+  __device__ __forceinline__ bool consider(bool stays, float s, uint32_t at, float e) {
     const float x = (s - s_max) * exp2_per;
-    if (need_mass) {
+    if (kMass && need_mass) {
       const float w = stays ? fast_exp2(x) : 0.f;
-      mass += w >= min_w ? w : 0.f;
+      mass += !kMinP || w >= min_w ? w : 0.f;
     }
-    const float key = stays && x >= min_log2 ? x - fast_log2(e) : -INFINITY;
+    const bool in = stays && (!kMinP || x >= min_log2);
+    const float key = in ? x - fast_log2(e) : -INFINITY;
     rough_second = fmaxf(rough_second, fminf(rough, key));
     const bool first = key > rough;
     rough = first ? key : rough;
     rough_at = first ? int32_t(at) : rough_at;
+    return kMinP && in && x <= min_log2 + 2.f * kNear;
+  }
+  // The same of an entry whose w is known in full.
+  __device__ __forceinline__ void list_consider(float s, float w, uint32_t at) {
+    consider<true, false>(true, s, at, noise[at]);
+    mass += w >= min_w ? w : 0.f;
+  }
+  // Such an entry counts by its w in full, by which it is drawn or not, so that what is drawn is in the sum.
+  __device__ __forceinline__ void recount(float s) {
+    const float x = (s - s_max) * exp2_per;
+    if (x >= min_log2 && x <= min_log2 + 2.f * kNear) {
+      const float w = fast_exp2(x), full = weight(s);
+      mass += (full >= min_w ? full : 0.f) - (w >= min_w ? w : 0.f);
+    }
   }
   // An entry's key in full; 0 for one that min-p leaves out.
   __device__ __forceinline__ uint32_t exact(float s, float e) const {
@@ -697,6 +713,11 @@ struct Row {
   // i) sees all.
   template <typename In, typename Also>
   __device__ __forceinline__ void draw(In in, Also also) {
+    if (min_w > 0.f) draw_by<true>(in, also);
+    else draw_by<false>(in, also);
+  }
+  template <bool kMinP, typename In, typename Also>
+  __device__ __forceinline__ void draw_by(In in, Also also) {
     const bool vector = a.noise_vector && skip % 4 == 0;
     const float* const own = noise + lo;
     each_group([&](const float(&s)[kAhead][kG], int i) {
@@ -725,11 +746,21 @@ struct Row {
         }
       }
       also(s, i);
+      bool near = false;
 #pragma unroll
       for (int u = 0; u < kAhead; u++) {
         if (i + u * threads * kG >= count) break;
 #pragma unroll
-        for (int j = 0; j < kG; j++) consider(stay[u][j], s[u][j], lo + i + u * threads * kG + j, e[u][j]);
+        for (int j = 0; j < kG; j++) near |= consider<kMinP>(stay[u][j], s[u][j], lo + i + u * threads * kG + j, e[u][j]);
+      }
+      if (kMinP && near) {  // rare: read again, so that nothing is kept for it
+#pragma unroll 1
+        for (int j = 0; j < kAhead * kG; j++) {
+          const int at = i + j / kG * threads * kG + j % kG;
+          if (at < 0 || at >= count) continue;
+          const float v = value(global[at]);
+          if (in(v, uint32_t(lo + at))) recount(v);
+        }
       }
     });
   }
@@ -766,12 +797,14 @@ struct Row {
     const int have = k < m ? k : m;
     u64 before = 0, total = 0, target = ~u64(0);
     const float s = tid < have ? key_score(uint32_t(sorted[tid] >> 32)) : 0.f;
+    const float w = tid < have ? weight(s) : 0.f;
     const uint32_t at = tid < have ? ~uint32_t(sorted[tid]) : 0;
     if (p < 1.f) {
-      before = scan(tid < have ? fixed(weight(s)) : 0, &total);
+      before = scan(fixed(w), &total);
       target = p > 0.f ? share_of(total, p) : 1;
     }
-    if (tid < have && before < target) consider(true, s, at, noise[at]);  // one entry a thread: its candidate is sure
+    // one entry a thread: its candidate is sure
+    if (tid < have && before < target) list_consider(s, w, at);
     const Drawn got = block_best(candidate(s));
     if (got.key ? tid < have && at == got.at : tid == 0) put(got, s, index, logp);
   }

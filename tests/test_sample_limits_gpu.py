@@ -64,3 +64,33 @@ def test_top_p_of_long_rows_of_many_scores():
             e[0, order[place]] = 1e-30
             index, _ = emr.sample(s, e, top_p=p)
             assert (int(index) == int(order[place])) == stays, (p, place, kept)
+
+
+@pytest.mark.parametrize("n", [8, 9000])
+@pytest.mark.parametrize("kw", [dict(), dict(top_k=7), dict(top_p=0.9999)])
+@pytest.mark.parametrize("T", [1.0, 0.7])
+def test_what_min_p_keeps_is_what_the_probability_counts(kw, n, T):
+    """One entry of w = 1 and three equal ones whose w min-p names to within two units in the last place: they stay
+    or not, and if one is drawn, all that top-p leaves of the three are in the sum that its probability is taken of
+    (log w good to 4e-6 and the end of top-p to 1e-5, as in test_sample_gpu.py)."""
+    rows = 400
+    g = np.random.default_rng(3)
+    low = -g.uniform(0, 7, rows).astype(np.float32)
+    s = torch.full((rows, n), -np.inf, device="cuda")
+    s[:, 1] = 0.0
+    s[:, [0, 3, n - 1]] = torch.from_numpy(low).cuda()[:, None]
+    w = np.exp(low.astype(np.float64) / float(np.float32(T)))
+    e = torch.ones(rows, n, device="cuda")
+    e[:, 3] = 1e-20                                   # drawn whenever it stays
+    for ulps in (-2, -1, 0, 1, 2):
+        q = (w.astype(np.float32).view(np.int32) + ulps).view(np.float32)
+        index, logp = emr.sample(s, e, T, min_p=torch.from_numpy(q).cuda(), **kw)
+        index, logp = index.cpu().numpy(), logp.double().cpu().numpy()
+        assert np.isin(index, (1, 3)).all()
+        fits = np.zeros(rows, bool)
+        for p in (kw.get("top_p", 2.0) * (1 + x) for x in (-1e-5, 0.0, 1e-5)):
+            left = sum(1 + j * w < p * (1 + 3 * w) for j in range(3))        # of the three
+            near = lambda want: np.abs(logp - want) <= 4e-6 + 2.0 ** -23 * np.abs(want)
+            fits |= (index == 3) & (left >= 2) & near(np.log(w / (1 + left * w)))
+            fits |= (index == 1) & (near(0.0 * w) | (left <= 1) & near(-np.log(1 + left * w)))
+        assert fits.all(), (ulps, np.flatnonzero(~fits), index[~fits], logp[~fits])
