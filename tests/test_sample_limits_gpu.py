@@ -94,3 +94,27 @@ def test_what_min_p_keeps_is_what_the_probability_counts(kw, n, T):
             fits |= (index == 3) & (left >= 2) & near(np.log(w / (1 + left * w)))
             fits |= (index == 1) & (near(0.0 * w) | (left <= 1) & near(-np.log(1 + left * w)))
         assert fits.all(), (ulps, np.flatnonzero(~fits), index[~fits], logp[~fits])
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(min_p=0.3), dict(top_k=-3), dict(top_p=0.75)])
+@pytest.mark.parametrize("score", [-0.0078125, -0.26, -1.0])
+def test_probabilities_of_long_rows_of_equal_scores(score, kw):
+    """A block adds up 1.4 million equal w: the probability is as good as a short row's (the bounds of
+    test_sample_gpu.py; the end of top-p may be off by 1e-5 of the row, and its logarithm as much)."""
+    rows, n = 160, 1398100
+    s = torch.full((1, n), score, dtype=torch.bfloat16, device="cuda")
+    s[0, 0] = 0.0
+    w = float(torch.exp(s[0, 1].double()))
+    e = torch.ones(1, n, device="cuda")
+    e[0, 1000] = 1e-30
+    kw = dict(kw, top_k=n - 3) if "top_k" in kw else kw
+    index, logp = emr.sample(s.expand(rows, n), e.expand(rows, n), **kw)
+    total = 1 + (n - 1) * w
+    if "top_k" in kw:
+        total -= 3 * w
+    if "top_p" in kw:
+        total = 1 + w * np.ceil((0.75 * total - 1) / w)
+    want = np.log(w / total)
+    assert bool((index == 1000).all())
+    off = np.abs(logp.double().cpu().numpy() - want).max()
+    assert off <= 4e-6 + 2.0 ** -23 * abs(want) + (1e-5 / 0.75 if "top_p" in kw else 0.0), off
