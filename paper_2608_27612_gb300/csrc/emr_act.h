@@ -75,10 +75,11 @@ __device__ __forceinline__ void activate(int act, float (&z)[kN], float (&d)[kN]
       break;
     case EMR_ACT_SIN: {
       // reduced by 2 pi in two parts (fp32 value and remainder) and taken by the special
-      // function unit, good to 1e-6 up to 8192; beyond that, and for NaN, by sincosf
+      // function unit, good to 1e-6 up to 8192; beyond that, and for infinities, by sincosf. NaN is
+      // passed over by the maximum and stays NaN either way.
       float most = 0.f;
 #pragma unroll
-      for (int i = 0; i < kN; i++) most = fabsf(z[i]) <= most ? most : fabsf(z[i]);
+      for (int i = 0; i < kN; i++) most = fmaxf(most, fabsf(z[i]));
       if (most < 8192.f) {
 #pragma unroll
         for (int i = 0; i < kN; i++) {

@@ -62,3 +62,28 @@ def test_training_step_into_memory_at_16_bytes():
                                 sizes[3], stream) == emr.EMR_OK
     assert torch.equal(out, y)
     assert all(torch.equal(a, b) for a, b in zip((dx, dw, db), layer.backward(dy, saved)))
+
+
+@pytest.mark.parametrize("large", [3e4, 1e9, 1e13, 3e30, float("inf")])
+@pytest.mark.parametrize("m", [1, 20, 150])
+def test_sin_of_large_values_beside_nan(large, m):
+    """A column of NaN leaves the columns before and after it as they are: sin and its slope of a large value stay those
+    of the full range (to 2e-6; the slope in 8 bits to half a step, 2^-4 relative or 2^-10 of its block's scale)."""
+    n = 70
+    x, w = emr.q8_quantize(torch.zeros(1, m, 1, device="cuda"))[0], emr.q8_quantize(torch.zeros(1, n, 1, device="cuda"))[0]
+    b = torch.linspace(-3, 3, n, device="cuda")[None]
+    b[0, [2, 40]], b[0, [3, 41, 69]] = large, float("nan")
+    layer = emr.DenseLayer(torch.zeros(1, n, 1, device="cuda"), b, emr.ACT_SIN)
+    z = f64(b)[0]
+    with np.errstate(invalid="ignore"):
+        y, s = np.sin(z), np.cos(z)
+    d = emr.Q8(1, m, n)
+    for out in (layer.forward(torch.zeros(1, m, 1, device="cuda")), emr.q8_matmul(x, w, b, emr.ACT_SIN),
+                emr.q8_matmul(x, w, b, emr.ACT_SIN, slope=d)):
+        got = f64(out)[0]
+        assert np.array_equal(np.isnan(got), np.broadcast_to(np.isnan(y), got.shape))
+        assert np.nanmax(np.abs(got - y)) <= 2e-6
+    got = f64(emr.q8_dequantize(d))[0]
+    scale = OD.block_scales(np.nan_to_num(s))[0]
+    assert np.array_equal(np.isnan(got), np.broadcast_to(np.isnan(s), got.shape))
+    assert np.nanmax(np.abs(got - s) - 2.0 ** -4 * np.abs(s)) <= 4e-6 + 2.0 ** -10 * scale
