@@ -386,6 +386,13 @@ __global__ void __launch_bounds__(kTileThreads, 2) q8_tile_kernel(Dense<T, kLayo
       top = make_float4(fmaxf(top.x, fabsf(v[i].x)), fmaxf(top.y, fabsf(v[i].y)), fmaxf(top.z, fabsf(v[i].z)), fmaxf(top.w, fabsf(v[i].w)));
     // NaN is passed over by the maxima; where an infinity is, the finite magnitudes are taken again
     if (q8_top4(top) == INFINITY) {
+      if constexpr (kMode == 1 || kMode == 3) {
+        // codes stand for no infinity: it is 2^128, as which values from 1.9375 * 2^127 on are held and which
+        // 32 bits do not have. The largest of them is held as the same.
+        const auto held = [](float f) { return fabsf(f) == INFINITY ? copysignf(__uint_as_float(0x7f7fffffu), f) : f; };
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = make_float4(held(v[i].x), held(v[i].y), held(v[i].z), held(v[i].w));
+      }
       uint32_t m[4] = {};
 #pragma unroll
       for (int i = 0; i < 8; i++) {

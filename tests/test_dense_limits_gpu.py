@@ -20,6 +20,12 @@ def f64(t):
     return t.double().cpu().numpy()
 
 
+def f32(v):
+    """v as 32 bits give it: 2^128 is infinite there."""
+    with np.errstate(over="ignore"):
+        return v.astype(np.float32).astype(np.float64)
+
+
 def q8_at(offset, batch, rows, cols):
     """A Q8 whose buffers begin `offset` bytes after a multiple of 256, filled with a byte, and its memory."""
     n = sum(emr._q8_bytes(batch, rows, cols))
@@ -87,3 +93,25 @@ def test_sin_of_large_values_beside_nan(large, m):
     scale = OD.block_scales(np.nan_to_num(s))[0]
     assert np.array_equal(np.isnan(got), np.broadcast_to(np.isnan(s), got.shape))
     assert np.nanmax(np.abs(got - s) - 2.0 ** -4 * np.abs(s)) <= 4e-6 + 2.0 ** -10 * scale
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_transpose_of_the_largest_values(dtype):
+    """Values that are held as 2^128, which 32 bits do not have, are held as that in the transpose, too: only infinities
+    and NaN become NaN there."""
+    top = float(torch.finfo(dtype).max)
+    x = torch.zeros(2, 150, 261)
+    x[0, 3, 1], x[0, 7, 2], x[0, 100, 2], x[0, 140, 255], x[1, 0, 0] = -top, top, 1e37, 3.3e38, -3.2e38
+    x[1, 5], x[1, 9, 4], x[1, 130, 4], x[1, 131, 4] = top, float("inf"), -top, float("nan")
+    x = x.cuda().to(dtype)
+    once = OD.held(f64(x))
+    want = f32(OD.held(np.swapaxes(once, 1, 2)))
+    q, qt = emr.q8_quantize_held(x)
+    assert np.array_equal(f64(emr.q8_dequantize(q)), f32(once), equal_nan=True)
+    assert np.array_equal(f64(emr.q8_dequantize(qt)), want, equal_nan=True)
+    assert np.array_equal(f64(emr.q8_dequantize(emr.q8_transpose(q))), want, equal_nan=True)
+    # the values themselves are there: times 2^-120 they fit
+    w = emr.q8_quantize(torch.full((2, 1, 150), 2.0 ** -120, device="cuda"))[0]
+    got = f64(emr.q8_matmul(qt, w))[..., 0]
+    sums = np.swapaxes(once, 1, 2).sum(-1) * 2.0 ** -120
+    assert np.array_equal(np.isnan(got), np.isnan(sums)) and np.nanmax(np.abs(got - sums)) <= 152 * 2.0 ** -23 * 256 * 150
