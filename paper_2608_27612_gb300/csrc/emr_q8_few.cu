@@ -56,7 +56,7 @@ __device__ __forceinline__ uint4 stream16(const uint8_t* p) {  // weights are re
 template <int kTiles, typename T>
 __global__ void __launch_bounds__(kThreads) q8_few_kernel(const __grid_constant__ Params p) {
   constexpr int kRows = kTiles * 8;
-  extern __shared__ uint8_t codes[];  // [share][row][its blocks of 128, and 64 bytes]
+  extern __shared__ __align__(16) uint8_t codes[];  // [share][row][its blocks of 128, and 64 bytes]
   __shared__ float sums[kWarps][kRows][16];
   __shared__ uint8_t scales[64][kRows];  // [block][row]
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;

@@ -11,6 +11,7 @@
 // their block of 128.
 #include <cuda.h>
 #include <cuda_runtime.h>
+#include <stddef.h>
 
 #include <mutex>
 
@@ -229,11 +230,12 @@ __device__ __forceinline__ uint32_t pack_half(int dtype, float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// What the epilogue's warps share.
-struct Finish {
+// What the epilogue's warps share; read in pieces of 16 bytes.
+struct alignas(16) Finish {
   float tops[2][128][4];  // largest slope of a row's 32 columns, two turns
   float bias[kFinishWarps][32];
 };
+static_assert(offsetof(Finish, bias) % 16 == 0, "rows of bias begin at multiples of 16 bytes");
 // 32 bytes to an address that is a multiple of 16; `whole`: of 32, which one store of them asks for.
 // Predicated: a branch made the pair kernel spill.
 __device__ __forceinline__ void store32(uint8_t* to, const uint32_t (&w)[8], int32_t whole) {
