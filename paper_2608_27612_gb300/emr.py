@@ -150,11 +150,6 @@ def _stream(stream):
     return C.c_void_p(s.cuda_stream)
 
 
-def _raw_stream(stream, device):
-    """The same as a number, for calls that are made often: the current stream of the tensors' device."""
-    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(device.index)
-
-
 # ---- a1 -----------------------------------------------------------------------
 
 def grid_build(D: int, chunk: int = 0) -> Grid:
@@ -623,9 +618,28 @@ def _matrices(x, what: str):
 _NOTHING = contextlib.nullcontext()
 
 
-def _on(stream):
-    """Allocations for work on `stream` belong to it (the caching allocator reuses memory by stream)."""
-    return torch.cuda.stream(stream) if stream is not None else _NOTHING
+def _away(dev, stream):
+    """What a call on tensors of the GPU `dev` has to enter before it allocates and launches, None where it is
+    there: the library works on the current GPU, and allocations belong to the current stream (the caching
+    allocator reuses memory by stream)."""
+    if stream is None:
+        return None if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
+    if stream.device != dev:
+        raise ValueError("stream: one of %s is wanted, where the tensors are, got one of %s" % (dev, stream.device))
+    here = dev.index == torch.cuda.current_device() and stream == torch.cuda.current_stream(dev)
+    return None if here else torch.cuda.stream(stream)
+
+
+def _on(dev, stream):
+    """The same for a with statement."""
+    return _away(dev, stream) or _NOTHING
+
+
+def _together(dev, *others):
+    """Operands are read and written on one GPU."""
+    if dev.type != "cuda" or any(x is not None and x.device != dev for x in others):
+        raise ValueError("operands on one GPU are wanted, got them on %s" %
+                         ", ".join(str(d) for d in [dev] + [x.device for x in others if x is not None]))
 
 
 def _q8_bytes(batch: int, rows: int, cols: int):
@@ -688,7 +702,8 @@ def q8_quantize(x, q: Q8 | None = None, qt: Q8 | None = None, stream=None):
     """emr_q8_quantize: x [batch, rows, cols] or [rows, cols], any strides, into q (blocks along the columns)
     and, or instead, qt (the transpose, blocks along the rows). With neither, a new q. Returns (q, qt)."""
     x = _matrices(x, "x")
-    with _on(stream):
+    _together(x.device, q, qt)
+    with _on(x.device, stream):
         if q is None and qt is None:
             q = Q8(*x.shape, device=x.device)
         _check(lib().emr_q8_quantize(x.data_ptr(), _dtype(x.dtype, "x"), *x.shape, *x.stride(), _ref(q), _ref(qt),
@@ -699,7 +714,7 @@ def q8_quantize(x, q: Q8 | None = None, qt: Q8 | None = None, stream=None):
 def q8_quantize_held(x, stream=None):
     """emr_q8_quantize_held: (q, qt) of x, qt made of the values that q holds."""
     x = _matrices(x, "x")
-    with _on(stream):
+    with _on(x.device, stream):
         q, qt = Q8(*x.shape, device=x.device), Q8(x.shape[0], x.shape[2], x.shape[1], device=x.device)
         _check(lib().emr_q8_quantize_held(x.data_ptr(), _dtype(x.dtype, "x"), *x.shape, *x.stride(), q.ref, qt.ref,
                                           _stream(stream)), "emr_q8_quantize_held")
@@ -708,7 +723,8 @@ def q8_quantize_held(x, stream=None):
 
 def q8_transpose(q: Q8, qt: Q8 | None = None, stream=None) -> Q8:
     """emr_q8_transpose: the transpose of what q holds, with blocks along q's rows."""
-    with _on(stream):
+    _together(q.device, qt)
+    with _on(q.device, stream):
         if qt is None:
             qt = Q8(q.batch, q.cols, q.rows, device=q.device)
         _check(lib().emr_q8_transpose(q.ref, qt.ref, _stream(stream)), "emr_q8_transpose")
@@ -717,7 +733,8 @@ def q8_transpose(q: Q8, qt: Q8 | None = None, stream=None) -> Q8:
 
 def q8_dequantize(q: Q8, dtype=torch.float32, stream=None):
     """emr_q8_dequantize: the values that q stands for, a new [batch, rows, cols] tensor."""
-    with _on(stream):
+    _together(q.device)
+    with _on(q.device, stream):
         out = torch.empty(q.shape, dtype=dtype, device=q.device)
         _check(lib().emr_q8_dequantize(q.ref, out.data_ptr(), _dtype(dtype, "dtype"), _stream(stream)),
                "emr_q8_dequantize")
@@ -733,9 +750,8 @@ def q8_matmul(a: Q8, w: Q8, bias=None, act: int = ACT_IDENTITY, out_dtype=torch.
     if bias is not None and (bias.dtype != torch.float32 or not bias.is_contiguous() or
                              bias.numel() != batch * w.rows or bias.device != a.device):
         raise ValueError("bias: a contiguous float32 tensor [batch, rows of w] on the operands' GPU is wanted")
-    if a.device != w.device or (slope is not None and slope.device != a.device):
-        raise ValueError("operands on one GPU are wanted")
-    with _on(stream):
+    _together(a.device, w, slope)
+    with _on(a.device, stream):
         if out is None:
             out = torch.empty(shape, dtype=out_dtype, device=a.device)
         elif tuple(out.shape) != shape or not out.is_contiguous() or out.device != a.device:
@@ -751,8 +767,9 @@ def q8_slope(dy, d: Q8 | None, dz: Q8 | None = None, dzt: Q8 | None = None, db=N
     batch, rows, cols = dy.shape
     if db is not None and (db.numel() != batch * cols or not db.is_contiguous() or db.device != dy.device):
         raise ValueError("db: a contiguous tensor [batch, cols] is wanted")
+    _together(dy.device, d, dz, dzt)
     n = C.c_size_t()
-    with _on(stream):
+    with _on(dy.device, stream):
         dy, ws = dy.contiguous(), None
         if db is not None:
             _check(lib().emr_q8_slope_workspace_size(batch, rows, cols, C.byref(n)), "emr_q8_slope_workspace_size")
@@ -763,9 +780,11 @@ def q8_slope(dy, d: Q8 | None, dz: Q8 | None = None, dzt: Q8 | None = None, db=N
 
 
 def device_error(stream=None) -> int:
-    """emr_device_error: 0, or the number of a device-side wait that gave up since the last call."""
+    """emr_device_error: 0, or the number of a device-side wait that gave up since the last call, on the stream's
+    GPU (the current one)."""
     code = C.c_int32()
-    _check(lib().emr_device_error(C.byref(code), _stream(stream)), "emr_device_error")
+    with _on(stream.device, stream) if stream is not None else _NOTHING:
+        _check(lib().emr_device_error(C.byref(code), _stream(stream)), "emr_device_error")
     return code.value
 
 
@@ -805,7 +824,7 @@ class DenseLayer:
             raise ValueError("act: one of ACT_* is wanted, got %r" % (act,))
         self.nets, self.n, self.k = w.shape
         self.act, self.train, self.device = act, train, w.device
-        with _on(stream):
+        with _on(w.device, stream):
             self.w8 = Q8(*w.shape, device=w.device)
             self.w8t = Q8(self.nets, self.k, self.n, device=w.device) if train else None
         self.c = DenseC(self.w8.c, self.w8t.c if train else Q8C(), None, act, 0)
@@ -823,8 +842,9 @@ class DenseLayer:
         kind = _DTYPES.get(w.dtype)
         if kind is None:
             _dtype(w.dtype, "w")
-        if stream is not None and stream != torch.cuda.current_stream(dev):
-            with torch.cuda.stream(stream):
+        away = _away(dev, stream)
+        if away is not None:
+            with away:
                 return self.set_weights(w, b)
         if b is not None:
             if b.dtype != torch.float32 or b.numel() != self.nets * self.n or b.device != dev:
@@ -872,8 +892,9 @@ class DenseLayer:
             if keep:
                 raise ValueError("x: at least one row is wanted for training")
             return torch.empty(self.nets, 0, self.n, dtype=out_dtype, device=dev), None, 0
-        if stream is not None and stream != torch.cuda.current_stream(dev):
-            with torch.cuda.stream(stream):   # allocations belong to the stream that they are used on
+        away = _away(dev, stream)
+        if away is not None:
+            with away:
                 return self._forward(x, out_dtype, None, keep)
         out = torch.empty((self.nets, m, self.n), dtype=out_dtype, device=dev)
         kept = xp = tp = sp = None
@@ -918,8 +939,9 @@ class DenseLayer:
         kind, out_kind = _DTYPES.get(dy.dtype), _DTYPES.get(out_dtype)
         if kind is None or out_kind is None:
             _dtype(dy.dtype, "dy"), _dtype(out_dtype, "out_dtype")
-        if stream is not None and stream != torch.cuda.current_stream(dev):
-            with torch.cuda.stream(stream):
+        away = _away(dev, stream)
+        if away is not None:
+            with away:
                 return self.backward(dy, saved, out_dtype)
         dy = dy.contiguous()
         room = self._back.get((nx, m))
@@ -960,8 +982,9 @@ def sample(scores, noise, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, stream
     dev = scores.device
     if noise.shape != scores.shape or noise.dtype is not torch.float32 or noise.device != dev:
         raise ValueError("noise: a float32 tensor in the shape of scores on the same GPU is wanted")
-    if stream is not None and stream != torch.cuda.current_stream(dev):
-        with torch.cuda.stream(stream):   # allocations belong to the stream that they are used on
+    away = _away(dev, stream)
+    if away is not None:
+        with away:
             return sample(scores, noise, temperature, top_k, top_p, min_p)
     if scores.dim() == 1:
         scores, noise = scores.unsqueeze(0), noise.unsqueeze(0)
