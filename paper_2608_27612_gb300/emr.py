@@ -635,6 +635,15 @@ def _on(dev, stream):
     return _away(dev, stream) or _NOTHING
 
 
+def _lend(dev, *tensors):
+    """Memory that this module allocated on one stream is used by the current one: the allocator gives it to no one
+    else before that work is done."""
+    s = torch.cuda.current_stream(dev)
+    for t in tensors:
+        if t is not None:
+            t.record_stream(s)
+
+
 def _together(dev, *others):
     """Operands are read and written on one GPU."""
     if dev.type != "cuda" or any(x is not None and x.device != dev for x in others):
@@ -792,9 +801,9 @@ class Saved:
     """What a training step keeps between the passes, in 8 bits: xt, the transpose [nx, k, m] of x, as the weight
     gradient reads it, and slope, act'(z) [nets, m, n] (None: identity). nx, m: batch and rows of x."""
 
-    def __init__(self, layer, nx: int, m: int, data, split: int):
-        # one piece of memory: xt, then, from `split` on (0: none), slope
-        self._layer, self.nx, self.m, self._data, self._split = layer, nx, m, data, split
+    def __init__(self, layer, nx: int, m: int, data, split: int, home: int | None = None):
+        # one piece of memory: xt, then, from `split` on (0: none), slope; home: the stream that it was allocated on
+        self._layer, self.nx, self.m, self._data, self._split, self._home = layer, nx, m, data, split, home
 
     @property
     def xt(self) -> Q8:
@@ -827,6 +836,7 @@ class DenseLayer:
         with _on(w.device, stream):
             self.w8 = Q8(*w.shape, device=w.device)
             self.w8t = Q8(self.nets, self.k, self.n, device=w.device) if train else None
+            self._home = torch._C._cuda_getCurrentRawStream(w.device.index)
         self.c = DenseC(self.w8.c, self.w8t.c if train else Q8C(), None, act, 0)
         self._ref = C.byref(self.c)
         self._room, self._kept, self._back = {}, {}, {}
@@ -851,8 +861,10 @@ class DenseLayer:
                 raise ValueError("b: a float32 tensor [%d, %d] on the layer's GPU is wanted" % (self.nets, self.n))
             b = b.contiguous()
         q, qt = self._w8
-        _check(lib().emr_q8_quantize(w.data_ptr(), kind, self.nets, self.n, self.k, *w.stride(), q, qt,
-                                     torch._C._cuda_getCurrentRawStream(dev.index)), "emr_q8_quantize")
+        raw = torch._C._cuda_getCurrentRawStream(dev.index)
+        if raw != self._home:
+            _lend(dev, self.w8.data, self.w8t.data if qt else None)
+        _check(lib().emr_q8_quantize(w.data_ptr(), kind, self.nets, self.n, self.k, *w.stride(), q, qt, raw), "emr_q8_quantize")
         self.b = b
         self.c.bias = b.data_ptr() if b is not None else None
 
@@ -891,7 +903,7 @@ class DenseLayer:
         if m == 0:
             if keep:
                 raise ValueError("x: at least one row is wanted for training")
-            return torch.empty(self.nets, 0, self.n, dtype=out_dtype, device=dev), None, 0
+            return torch.empty(self.nets, 0, self.n, dtype=out_dtype, device=dev), None, 0, None
         away = _away(dev, stream)
         if away is not None:
             with away:
@@ -910,11 +922,14 @@ class DenseLayer:
         if room:
             xq = torch.empty(room, dtype=torch.uint8, device=dev)
             xp = xq.data_ptr()
+        raw = torch._C._cuda_getCurrentRawStream(dev.index)
+        if raw != self._home:
+            _lend(dev, self.w8.data, self.b)
         status = _lib.emr_dense_forward(self._ref, x.data_ptr(), kind, nx, m, *x.stride(), out.data_ptr(), out_kind,
-                                        1 if keep else 0, xp, tp, sp, torch._C._cuda_getCurrentRawStream(dev.index))
+                                        1 if keep else 0, xp, tp, sp, raw)
         if status:
             _check(status, "emr_dense_forward")
-        return out, kept, split
+        return out, kept, split, raw
 
     def forward(self, x, out_dtype=torch.float32, stream=None):
         """y [nets, m, n] of out_dtype. m = 0 gives an empty result."""
@@ -924,8 +939,8 @@ class DenseLayer:
         """(y, saved): saved holds x and act'(z) in 8 bits for backward."""
         if not self.train:
             raise ValueError("forward_train: the layer was made with train=False")
-        y, kept, split = self._forward(x, out_dtype, stream, True)
-        return y, Saved(self, x.shape[0] if x.dim() == 3 else 1, y.shape[1], kept, split)
+        y, kept, split, home = self._forward(x, out_dtype, stream, True)
+        return y, Saved(self, x.shape[0] if x.dim() == 3 else 1, y.shape[1], kept, split, home)
 
     def backward(self, dy, saved: Saved, out_dtype=torch.float32, stream=None):
         """(dx, dw, db) of out_dtype for dy [nets, m, n]: dx [1 or nets, m, k] as forward_train took x (summed
@@ -956,9 +971,13 @@ class DenseLayer:
         db = torch.empty((self.nets, self.n), dtype=out_dtype, device=dev)
         ws = torch.empty(room, dtype=torch.uint8, device=dev)
         kept, split = saved._data.data_ptr(), saved._split
+        raw = torch._C._cuda_getCurrentRawStream(dev.index)
+        if raw != saved._home:
+            _lend(dev, saved._data)
+        if raw != self._home:
+            _lend(dev, self.w8t.data)
         status = _lib.emr_dense_backward(self._ref, dy.data_ptr(), kind, nx, m, kept, kept + split if split else None,
-                                         dx.data_ptr(), dw.data_ptr(), db.data_ptr(), out_kind, ws.data_ptr(), room,
-                                         torch._C._cuda_getCurrentRawStream(dev.index))
+                                         dx.data_ptr(), dw.data_ptr(), db.data_ptr(), out_kind, ws.data_ptr(), room, raw)
         if status:
             _check(status, "emr_dense_backward")
         return dx, dw, db

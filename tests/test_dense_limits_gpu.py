@@ -115,3 +115,46 @@ def test_transpose_of_the_largest_values(dtype):
     got = f64(emr.q8_matmul(qt, w))[..., 0]
     sums = np.swapaxes(once, 1, 2).sum(-1) * 2.0 ** -120
     assert np.array_equal(np.isnan(got), np.isnan(sums)) and np.nanmax(np.abs(got - sums)) <= 152 * 2.0 ** -23 * 256 * 150
+
+
+def taken(n, ptr):
+    """Eight pieces of memory of n bytes, overwritten; none of them is the one at ptr."""
+    junk = [torch.full((n,), 0x38, dtype=torch.uint8, device="cuda") for _ in range(8)]
+    assert all(j.data_ptr() != ptr for j in junk)
+    return junk
+
+
+def late(side):
+    """Work given to `side` after this begins some 50 ms later."""
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)
+
+
+def test_a_layer_may_go_while_another_stream_uses_it():
+    w, b, x = normal(6, 1, 300, 400) / 20, normal(7, 1, 300), normal(8, 1, 50, 400)
+    want = emr.DenseLayer(w, b, emr.ACT_TANH).forward(x)
+    side = torch.cuda.Stream()
+    layer = emr.DenseLayer(w, b, emr.ACT_TANH)
+    late(side)
+    got = layer.forward(x, stream=side)
+    n, ptr = layer.w8.data.numel(), layer.w8.data.data_ptr()
+    del layer
+    taken(n, ptr)
+    side.synchronize()
+    assert torch.equal(got, want)
+
+
+def test_what_a_step_keeps_may_go_while_another_stream_uses_it():
+    w, x, dy = normal(9, 1, 300, 400) / 20, normal(10, 1, 200, 400), normal(11, 1, 200, 300)
+    layer, side = emr.DenseLayer(w, act=emr.ACT_GAUSS, train=True), torch.cuda.Stream()
+    _, saved = layer.forward_train(x)
+    want = layer.backward(dy, saved)
+    late(side)
+    got = layer.backward(dy, saved, stream=side)
+    kept = (saved._data.numel(), saved._data.data_ptr()), (layer.w8t.data.numel(), layer.w8t.data.data_ptr())
+    del saved, layer
+    for n, ptr in kept:
+        taken(n, ptr)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
