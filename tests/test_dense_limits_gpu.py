@@ -158,3 +158,37 @@ def test_what_a_step_keeps_may_go_while_another_stream_uses_it():
         taken(n, ptr)
     side.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("nets,shared,m,n,k", [(1, False, 4, 60, 200), (6, True, 40, 130, 90), (1, False, 700, 900, 1300)])
+def test_a_step_and_a_draw_in_a_captured_graph(nets, shared, m, n, k):
+    """An update of the weights, a training step, a forward pass and a draw, captured once and replayed on new
+    inputs: the same bits as the calls by themselves."""
+    def inputs(seed):
+        return (normal(seed, nets, n, k) / np.sqrt(k), normal(seed + 1, nets, n), normal(seed + 2, 1 if shared else nets, m, k),
+                normal(seed + 3, nets, m, n), torch.rand(nets * m, n, device="cuda") + 1e-3)
+
+    def step(w, b, x, dy, e):
+        layer.set_weights(w, b)
+        y, saved = layer.forward_train(x)
+        scores = layer.forward(x)
+        return (y, scores) + layer.backward(dy, saved) + emr.sample(scores.view(nets * m, n), e, top_k=20, top_p=0.9)
+
+    held = inputs(20)
+    layer = emr.DenseLayer(held[0], held[1], emr.ACT_SIGMOID, train=True)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):                     # what is asked of the device once is asked before
+        step(*held)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(*held)
+    for seed in (30, 40):
+        new = inputs(seed)
+        for a, v in zip(held, new):
+            a.copy_(v)
+        graph.replay()
+        out = [t.clone() for t in got]
+        want = step(*new)
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
