@@ -159,9 +159,11 @@ struct FewArgs {
   void* out;
   int32_t out_dtype, batch;
 };
+// Where it takes less time than two launches, or as much: up to 4 MB of weights for at most 8 rows; with one
+// or two rows, each of them quantised in every block, up to 8 MB, and 16 where a row is long enough to share out.
 inline bool few_fused(int64_t rows, const emr_q8& w) {
-  const int64_t row = q8_row_bytes(w.cols);
-  return rows <= 16 && rows * row <= 8192 && w.batch <= 65535 && double(w.batch) * double(w.rows) * double(row) <= double(1 << 24);
+  const int64_t row = q8_row_bytes(w.cols), most = rows > 2 ? 4 : row < 1024 ? 8 : 16;
+  return rows <= 8 && rows * row <= 8192 && w.batch <= 65535 && double(w.batch) * double(w.rows) * double(row) <= double(most << 20);
 }
 emr_status launch_few(const FewArgs& a, cudaStream_t st);
 

@@ -1,13 +1,21 @@
-// The product of a few rows (at most 16, 8192 values in all) with an 8-bit weight matrix of at
-// most 16 MB in one launch: a single answer, where a launch of its own to quantise x would cost as
-// much as the product. Every block quantises x by itself. A warp takes 16 outputs and a share
-// of the contraction, straight from memory into the registers of m16n8k32 instructions, whose 8
-// columns are the rows of x. The order within a block of 128 is the same for both operands but
-// its own: a lane's 16 bytes feed two instructions, so that every load is 16 bytes a lane and
-// a row's 64 bytes are one piece. The sum of a block is scaled and added in 32 bits, the
-// warps' shares are added in their order. One row, 5460 x 1364: 4.5 us, where quantising and
-// the tensor-memory kernel take 3 + 5.8; it reaches 3.2 TB/s of weights against that kernel's 7,
-// so larger weights go there.
+// The product of a few rows (at most 8, 8192 values in all) with a small 8-bit weight matrix in
+// one launch: a single answer, where a launch of its own to quantise x would cost as much as the
+// product. Every block quantises x by itself. A warp takes 16 outputs and a share of the
+// contraction, straight from memory into the registers of m16n8k32 instructions, whose 8 columns
+// are the rows of x. The order within a block of 128 is the same for both operands but its own: a
+// lane's 16 bytes feed two instructions, so that every load is 16 bytes a lane and a row's 64
+// bytes are one piece. The sum of a block is scaled and added in 32 bits, the warps' shares
+// are added in their order. What bounds it is latency: the wait for x, its quantising, and, as
+// weights grow, the loads that a warp has in flight. Its time and that of the two launches of
+// quantising and emr_q8_matmul, in a captured graph with the weights in L2 (us; few_fused is the rule):
+//   rows  columns   1 MB         4 MB         8 MB         16 MB of weights
+//   1     64        4.1   5.4    5.0   6.1    7.8   7.4    11.5   9.2
+//   1     1024      2.7   6.4    3.9   6.6    6.2   7.2     6.7   8.2
+//   2     4096      6.2   6.8    6.2   7.2    6.4   7.6     8.2   8.7
+//   4     256       4.1   5.6    5.0   5.6    7.4   6.5    12.3   8.2
+//   8     1024      5.0   6.4    6.2   6.7    9.9   7.2    14.5   8.0
+//   16    256       8.8   6.0    9.5   6.0   17.2   7.0    29.5   9.0
+// 5460 x 1364 with one row takes 4.5, and 7.2 by two launches.
 #include <cuda_runtime.h>
 
 #include "emr_act.h"
@@ -52,10 +60,10 @@ __device__ __forceinline__ uint4 stream16(const uint8_t* p) {  // weights are re
   return v;
 }
 
-// kTiles: groups of 8 rows of x.
-template <int kTiles, typename T>
+constexpr int kRows = 8;
+
+template <typename T>
 __global__ void __launch_bounds__(kThreads) q8_few_kernel(const __grid_constant__ Params p) {
-  constexpr int kRows = kTiles * 8;
   extern __shared__ __align__(16) uint8_t codes[];  // [share][row][its blocks of 128, and 64 bytes]
   __shared__ float sums[kWarps][kRows][16];
   __shared__ uint8_t scales[64][kRows];  // [block][row]
@@ -94,7 +102,7 @@ __global__ void __launch_bounds__(kThreads) q8_few_kernel(const __grid_constant_
     __syncthreads();
   }
 
-  float acc[kTiles][4] = {};
+  float acc[4] = {};
   if (group < p.groups) {
     const int r0 = min(group * 16 + g, p.N - 1), r1 = min(group * 16 + g + 8, p.N - 1);
     const int64_t wb = p.w_one ? 0 : b;
@@ -102,41 +110,30 @@ __global__ void __launch_bounds__(kThreads) q8_few_kernel(const __grid_constant_
     const uint8_t *w0 = w + r0 * row_bytes, *w1 = w + r1 * row_bytes;
     const uint8_t* ws = p.w_scales + wb * q8_scale_batch(p.N, int64_t(p.blocks) * 128);
     const uint8_t *s0 = ws + q8_scale_at(p.chunks, r0, 0), *s1 = ws + q8_scale_at(p.chunks, r1, 0);
+    const int m = min(g, p.M - 1), m0 = min(2 * t, p.M - 1), m1 = min(2 * t + 1, p.M - 1);  // rows past M repeat the last; they are not stored
 #pragma unroll 2
     for (int kb = first; kb < last; kb++) {
       const int64_t k = int64_t(kb) * 128;
-      uint4 a[2][2], xv[kTiles][2];
+      uint4 a[2][2], xv[2];
 #pragma unroll
       for (int j = 0; j < 2; j++) a[0][j] = stream16(w0 + k + j * 64), a[1][j] = stream16(w1 + k + j * 64);
       const int at = (kb >> 2) * 512 + (kb & 3);
       const int sw0 = s0[at], sw1 = s1[at];
-      int sx[kTiles][2];
 #pragma unroll
-      for (int i = 0; i < kTiles; i++) {
-        const int m = min(i * 8 + g, p.M - 1);  // rows past M repeat the last; they are not stored
-        const int m0 = min(i * 8 + 2 * t, p.M - 1), m1 = min(i * 8 + 2 * t + 1, p.M - 1);
+      for (int j = 0; j < 2; j++) xv[j] = *reinterpret_cast<const uint4*>(own + m * pitch + (kb - first) * 128 + j * 64 + t * 16);
+      const int sx0 = scales[kb][m0], sx1 = scales[kb][m1];
+      float c[4] = {};
 #pragma unroll
-        for (int j = 0; j < 2; j++) xv[i][j] = *reinterpret_cast<const uint4*>(own + m * pitch + (kb - first) * 128 + j * 64 + t * 16);
-        sx[i][0] = scales[kb][m0], sx[i][1] = scales[kb][m1];
+      for (int j = 0; j < 2; j++) {
+        mma(c, a[0][j].x, a[1][j].x, a[0][j].y, a[1][j].y, xv[j].x, xv[j].y);
+        mma(c, a[0][j].z, a[1][j].z, a[0][j].w, a[1][j].w, xv[j].z, xv[j].w);
       }
-#pragma unroll
-      for (int i = 0; i < kTiles; i++) {
-        float c[4] = {};
-#pragma unroll
-        for (int j = 0; j < 2; j++) {
-          mma(c, a[0][j].x, a[1][j].x, a[0][j].y, a[1][j].y, xv[i][j].x, xv[i][j].y);
-          mma(c, a[0][j].z, a[1][j].z, a[0][j].w, a[1][j].w, xv[i][j].z, xv[i][j].w);
-        }
-        acc[i][0] += scaled(c[0], sw0, sx[i][0]), acc[i][1] += scaled(c[1], sw0, sx[i][1]);
-        acc[i][2] += scaled(c[2], sw1, sx[i][0]), acc[i][3] += scaled(c[3], sw1, sx[i][1]);
-      }
+      acc[0] += scaled(c[0], sw0, sx0), acc[1] += scaled(c[1], sw0, sx1);
+      acc[2] += scaled(c[2], sw1, sx0), acc[3] += scaled(c[3], sw1, sx1);
     }
   }
-#pragma unroll
-  for (int i = 0; i < kTiles; i++) {
-    sums[warp][i * 8 + 2 * t][g] = acc[i][0], sums[warp][i * 8 + 2 * t + 1][g] = acc[i][1];
-    sums[warp][i * 8 + 2 * t][g + 8] = acc[i][2], sums[warp][i * 8 + 2 * t + 1][g + 8] = acc[i][3];
-  }
+  sums[warp][2 * t][g] = acc[0], sums[warp][2 * t + 1][g] = acc[1];
+  sums[warp][2 * t][g + 8] = acc[2], sums[warp][2 * t + 1][g + 8] = acc[3];
   __syncthreads();
   for (int i = threadIdx.x; i < teams * kRows * 16; i += kThreads) {
     const int r = i & 15, m = i / 16 % kRows, tm = i / (16 * kRows);
@@ -150,15 +147,11 @@ __global__ void __launch_bounds__(kThreads) q8_few_kernel(const __grid_constant_
   }
 }
 
-template <int kTiles, typename T>
+template <typename T>
 emr_status launch(const Params& p, int batch, cudaStream_t st) {
   const int teams = kWarps / p.shares;
   const size_t smem = size_t(p.shares) * p.M * (((p.blocks + p.shares - 1) / p.shares) * 128 + 64);
-  return launch_after(q8_few_kernel<kTiles, T>, dim3(unsigned((p.groups + teams - 1) / teams), unsigned(batch)), kThreads, smem, st, p);
-}
-template <typename T>
-emr_status launch_tiles(const Params& p, int batch, cudaStream_t st) {
-  return p.M <= 8 ? launch<1, T>(p, batch, st) : launch<2, T>(p, batch, st);
+  return launch_after(q8_few_kernel<T>, dim3(unsigned((p.groups + teams - 1) / teams), unsigned(batch)), kThreads, smem, st, p);
 }
 
 }  // namespace
@@ -176,9 +169,9 @@ emr_status launch_few(const FewArgs& a, cudaStream_t st) {
   while (p.shares < kWarps && p.shares * 2 <= p.blocks && int64_t(p.groups) * a.batch * p.shares < 16 * 152) p.shares *= 2;
   p.M = int32_t(a.x_rows), p.x_one = a.x_batch == 1, p.source = a.x;
   p.batch_stride = a.x_batch_stride, p.row_stride = a.x_row_stride, p.col_stride = a.x_col_stride;
-  if (a.x_dtype == EMR_F32) return launch_tiles<float>(p, a.batch, st);
-  if (a.x_dtype == EMR_BF16) return launch_tiles<__nv_bfloat16>(p, a.batch, st);
-  return launch_tiles<__half>(p, a.batch, st);
+  if (a.x_dtype == EMR_F32) return launch<float>(p, a.batch, st);
+  if (a.x_dtype == EMR_BF16) return launch<__nv_bfloat16>(p, a.batch, st);
+  return launch<__half>(p, a.batch, st);
 }
 
 }  // namespace emr
