@@ -136,7 +136,8 @@ struct Row {
   // the draw: a thread's largest and second largest log2(w / noise) as computed roughly, and its w
   // (needed unless the histogram has told it)
   float rough, rough_second, mass;
-  float part, lost;  // of mass: the w of one turn, and what the sum of the turns has rounded off
+  float part;        // of mass: the w of one turn
+  float2* turns;     // in shared memory, a thread's own: the sum of its turns, and what that has rounded off
   bool need_mass;
   float min_log2;   // least log2 w that stays, with the margin
   int32_t rough_at;
@@ -694,9 +695,9 @@ struct Row {
   // A turn's w to the sum, with the rounding kept: a thread may have thousands of turns, whose roundings
   // all go one way where scores are equal (1.6e-5 of the sum for 1.4 million entries of 512 threads).
   __device__ __forceinline__ void add_part() {
-    const float more = part - lost, sum = mass + more;
-    lost = (sum - mass) - more;
-    mass = sum;
+    const float2 had = turns[tid];
+    const float more = part - had.y, sum = had.x + more;
+    turns[tid] = make_float2(sum, (sum - had.x) - more);
     part = 0.f;
   }
   // An entry's key in full; 0 for one that min-p leaves out.
@@ -728,6 +729,7 @@ struct Row {
   template <bool kMinP, typename In, typename Also>
   __device__ __forceinline__ void draw_by(In in, Also also) {
     const bool vector = a.noise_vector && skip % 4 == 0;
+    turns[tid] = make_float2(0.f, 0.f);
     const float* const own = noise + lo;
     each_group([&](const float(&s)[kAhead][kG], int i) {
       bool stay[kAhead][kG];
@@ -771,8 +773,9 @@ struct Row {
           if (in(v, uint32_t(lo + at))) recount(v);
         }
       }
-      add_part();
+      if (need_mass) add_part();
     });
+    mass += turns[tid].x;
   }
   // kept(score, index): what was drawn from.
   template <typename Kept>
@@ -842,7 +845,8 @@ __global__ void __launch_bounds__(kThreads, 2048 / kThreads > 4 ? 4 : kThreads =
   r.counts = r.lacks + a.bins;
   r.sorted = r.sums;  // the histogram is done with when entries are ordered
   r.list = reinterpret_cast<u64*>(r.counts + (a.carry ? 2 : 1) * a.bins);
-  r.data = reinterpret_cast<uint4*>(r.list + a.cap);
+  r.turns = reinterpret_cast<float2*>(r.list + a.cap);
+  r.data = reinterpret_cast<uint4*>(r.turns + kThreads);
   r.data_at = uint32_t(__cvta_generic_to_shared(r.data));
   r.counts_at = uint32_t(__cvta_generic_to_shared(r.counts)), r.lacks_at = uint32_t(__cvta_generic_to_shared(r.lacks));
   const int64_t row = blockIdx.x / unsigned(r.blocks);
@@ -854,7 +858,7 @@ __global__ void __launch_bounds__(kThreads, 2048 / kThreads > 4 ? 4 : kThreads =
   r.groups = (r.skip + r.count + kG - 1) / kG;
   r.noise = a.noise + row * a.noise_stride;
   r.top_infinite = false;
-  r.rough = r.rough_second = -INFINITY, r.rough_at = -1, r.need_mass = true, r.mass = r.part = r.lost = 0.f, r.bound = 0;
+  r.rough = r.rough_second = -INFINITY, r.rough_at = -1, r.need_mass = true, r.mass = r.part = 0.f, r.bound = 0;
   int32_t* index = a.index + row;
   float* logp = a.logp ? a.logp + row : nullptr;
 
@@ -1015,7 +1019,7 @@ emr_status plan(Args a, int rows, bool free, int dev, int sms, cudaStream_t st) 
   a.cap = free ? 0 : !wide ? 512 : crowd ? 1024 : 2048;
   const int threads = !wide ? 256 : crowd ? 512 : 1024;
   a.carry = !free && a.slice + 16 > int64_t(kCarryTurns) * threads * 8;
-  size_t smem = size_t(a.bins) * (a.carry ? 12 : 8) + size_t(a.cap) * 8;
+  size_t smem = size_t(a.bins) * (a.carry ? 12 : 8) + size_t(a.cap + threads) * 8;
   const size_t most = wide && !crowd ? kMostSmem : 110 * 1024;
   const size_t want = size_t(a.slice) * sizeof(T) + 16, room = most > smem ? most - smem : 0;
   a.room = int32_t((want < room ? want : room) / 16);
