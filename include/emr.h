@@ -610,10 +610,12 @@ emr_status emr_ann_forward(int32_t P, int32_t n_in, int32_t n_out, int32_t max_h
  * kb % 4 of its tile belongs to row r, block kb). The scale is the least 2^e, e in
  * [-126, 127], with the block's largest finite magnitude <= 448 * 2^e (1 for a block
  * of zeros), so scaling is exact and only the rounding to e4m3 (nearest even: 3
- * fraction bits) loses anything. Infinities and NaN become the NaN code and do not
- * enter the maximum. Sizes in bytes: emr_q8_size. Both buffers are 16-byte aligned.
+ * fraction bits) loses anything. Values from 1.9375 * 2^127 on are held as 2^128,
+ * which a 32-bit output gives as infinity. Infinities and NaN become the NaN code and
+ * do not enter the maximum. Sizes in bytes: emr_q8_size. Both buffers are 16-byte
+ * aligned. All memory of a call lies on the current GPU.
  * Errors of all calls: EMR_ERR_ARG (null or misaligned pointer, size below 1, sizes
- * that do not match, unknown type), EMR_ERR_RANGE (a size of 2^31 - 256 or more, or
+ * that do not match, unknown type), EMR_ERR_RANGE (a size above 2^31 - 256, or
  * more tiles than a launch has blocks), EMR_ERR_CAPACITY (workspace), EMR_ERR_CUDA. */
 enum { EMR_F32 = 0, EMR_BF16 = 1, EMR_F16 = 2 };
 typedef struct {
@@ -667,9 +669,10 @@ emr_status emr_q8_slope(const void *dy, int32_t dtype, int32_t batch, int64_t ro
  * [1][m][n] (the gradient of an input that all networks share; act must then be
  * EMR_ACT_IDENTITY and bias NULL). bias: device float [batch][n] or NULL. slope
  * (NULL for none): receives act'(z) in 8 bits, [batch][m][n] with blocks along n,
- * which is all that the backward pass needs to keep of z. act: EMR_ACT_*; the
- * slope of abs at 0 is 0. out is dense. A device-side wait that gives up (none is
- * expected) leaves out undefined and is reported by emr_device_error. */
+ * which is all that the backward pass needs to keep of z. act: EMR_ACT_*, good to
+ * 2e-6 absolute of act(z) in 32 bits (so sin has no relative precision near its
+ * zeros); the slope of abs at 0 is 0. out is dense. A device-side wait that gives up
+ * (none is expected) leaves out undefined and is reported by emr_device_error. */
 emr_status emr_q8_matmul(const emr_q8 *a, const emr_q8 *w, const float *bias, int32_t act, int32_t sum_batch,
                          void *out, int32_t out_dtype, const emr_q8 *slope, void *stream);
 
@@ -702,15 +705,16 @@ emr_status emr_dense_forward(const emr_dense *layer, const void *x, int32_t dtyp
  * [w.batch][rows][w.rows] of dtype; dx [x_batch][rows][w.cols] (summed over the networks
  * where x was shared), dw [w.batch][w.rows][w.cols] and db [w.batch][w.rows] of
  * out_dtype, each NULL for none. With dz = dy * slope, in 8 bits from there on: dx =
- * dz w, dw = dz^T x, db the sum of dz over the rows before it is rounded. ws:
+ * dz w with the weights that layer holds now, dw = dz^T x, db the sum of dz over the
+ * rows before it is rounded. ws:
  * emr_dense_backward_room bytes, 16-byte aligned. */
 emr_status emr_dense_backward_room(const emr_dense *layer, int32_t x_batch, int64_t rows, size_t *bytes);
 emr_status emr_dense_backward(const emr_dense *layer, const void *dy, int32_t dtype, int32_t x_batch, int64_t rows,
                               const void *xt, const void *slope, void *dx, void *dw, void *db, int32_t out_dtype,
                               void *ws, size_t ws_bytes, void *stream);
 
-/* Whether a bounded device-side wait of this library has given up since the last
- * call: *code receives 0, or the number of the wait. Synchronises the stream. */
+/* Whether a bounded device-side wait of this library has given up on the current GPU
+ * since the last call: *code receives 0, or the number of the wait. Synchronises the stream. */
 emr_status emr_device_error(int32_t *code, void *stream);
 
 /* ---- sampling from scores ----------------------------------------------------- */
@@ -729,8 +733,8 @@ emr_status emr_device_error(int32_t *code, void *stream);
  * probability. T <= 0 takes the largest score (lowest index) with logp 0. A row with
  * nothing left (all masked) gives index -1 and logp -infinity; a score of +infinity
  * leaves only the entries that equal it. q above 1 counts as 1 and p below 0 as 0: the
- * largest score always stays. Sums of w are integers (fixed point), so results do not
- * depend on the order of execution. Scores are read from memory once: a row's blocks keep
+ * largest score always stays. What top-p keeps is decided by sums of w in integers
+ * (fixed point), so results do not depend on the order of execution. Scores are read from memory once: a row's blocks keep
  * what fits into their shared memory (about 350,000 entries of 4 bytes for 8 blocks) and
  * read the rest again, in the main from L2; noise is read for entries that stay. Errors: EMR_ERR_ARG (null or
  * misaligned pointer, size below 1, negative stride, unknown type), EMR_ERR_RANGE (n

@@ -20,10 +20,12 @@
 // within 4e-5 of the best so far is computed again in full. Sums that decide are
 // integers, so that no result depends on the order of atomics: a step's w is its first
 // value times (entries - sum of what each lacks to it, in steps of 2^-20).
-// Measured: 1000 x 5460 float32 without filters 11 us (memory's time for scores and noise:
-// 6.4), 256 x 87380 bfloat16 with top-k 50, top-p and min-p 27 (6.6 for the scores), 24 x
-// 349524 float32 with top-p 60 (9.9 with all noise): the last is bound by two shared-memory
-// atomics for an entry and by about ten exchanges of a cluster.
+// Measured in a captured graph, where L2 keeps a part of the inputs: 1000 x 5460 float32 without
+// filters 12 us (memory's time for scores and noise: 6.4), 256 x 87380 bfloat16 with top-k 50,
+// top-p and min-p 21 (6.6 for the scores), 24 x 349524 float32 with top-p 55 (9.9 with all
+// noise): the last is bound by two shared-memory atomics for an entry and by about ten
+// exchanges of a cluster. The probabilities' sums are floats: turns of 8 or 16 entries, added
+// with their rounding kept, so that the length of a row does not show in them.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 

@@ -753,7 +753,8 @@ def q8_dequantize(q: Q8, dtype=torch.float32, stream=None):
 def q8_matmul(a: Q8, w: Q8, bias=None, act: int = ACT_IDENTITY, out_dtype=torch.float32, slope: Q8 | None = None,
               sum_batch: bool = False, out=None, stream=None):
     """emr_q8_matmul: act(a w^T + bias), [batch, a.rows, w.rows] ([1, ...] with sum_batch). An operand of
-    batch 1 serves every batch; slope receives act'(z) in 8 bits."""
+    batch 1 serves every batch; slope receives act'(z) in 8 bits. If a device-side wait gives up, the result is
+    undefined and only device_error tells."""
     batch = max(a.batch, w.batch)
     shape = (1 if sum_batch else batch, a.rows, w.rows)
     if bias is not None and (bias.dtype != torch.float32 or not bias.is_contiguous() or
@@ -824,7 +825,11 @@ class DenseLayer:
     [1, m, k] (shared by all networks) or [nets, m, k]; results are three-dimensional. The layer keeps the
     weights in 8 bits (with train=True also their transpose, which the backward pass reads), not w itself:
     after an update of w call set_weights. A training step keeps x and act'(z) in 8 bits, 2 bytes in all for
-    each pair, and takes its gradients from those.
+    each pair, and takes its gradients from those and from the weights as they are laid out when backward is
+    called.
+
+    The kernels' waits on the device are bounded. None is expected to give up; if one does, the results of that
+    call are undefined, no exception is raised, and device_error tells (it waits for the stream).
     """
 
     def __init__(self, w, b=None, act: int = ACT_IDENTITY, train: bool = False, stream=None):
