@@ -745,6 +745,41 @@ emr_status emr_sample(const void *scores, int32_t dtype, int32_t rows, int64_t n
                       const float *min_p, float min_p_all, int32_t *index, float *logp,
                       void *stream);
 
+/* ---- log probabilities of answers ---------------------------------------------- */
+
+/* How likely given answers are, how sure each row is, and its best answers. scores: device [rows][n] of dtype,
+ * row r at scores + r * row_stride elements; T: temperature (device float [rows], or NULL for the scalar beside
+ * it). Scores of -infinity and NaN are masked. Over the entries that are not, with s_max the largest score,
+ * log p_i = (s_i - s_max) / T - log sum exp((s - s_max) / T), as emr_sample without filters draws.
+ *   logp[r]     log p of entry target[r] (device int32 [rows]); -infinity where it is masked, 0 for a target below 0
+ *               (no answer given), NaN for one of n or more. NULL for none; target may then be NULL too.
+ *   entropy[r]  -sum p log p. NULL for none.
+ *   top_index, top_logp [rows][top]  the top (0 to EMR_MAX_TOP) largest scores, larger first, then by index, and
+ *               their log p; past the entries that are not masked -1 and -infinity. Either may be NULL.
+ * T <= 0 (and NaN) stands for the limit that emr_sample takes: log p is 0 for the largest score (lowest index) and
+ * -infinity for the others. A score of +infinity leaves only the entries that equal it. An entry whose s - s_max is below
+ * the range of 32 bits has log p -infinity whatever T. A row with nothing left gives -infinity, entropy 0 and no best. Results are good to 6e-6 + 2^-22 |log p| and do not depend on the order of execution.
+ * Scores are read from memory once; a row's candidates for the best again, from L2. Errors: EMR_ERR_ARG (null
+ * or misaligned pointer, size below 1, negative stride, unknown type, nothing asked for), EMR_ERR_RANGE (n above
+ * 2^31 - 2^20, rows above 2^27, top above EMR_MAX_TOP), EMR_ERR_CUDA. */
+#define EMR_MAX_TOP 256
+emr_status emr_log_probs(const void *scores, int32_t dtype, int32_t rows, int64_t n, int64_t row_stride,
+                         const int32_t *target, const float *temperature, float temperature_all, int32_t top,
+                         float *logp, float *entropy, int32_t *top_index, float *top_logp, void *stream);
+
+/* The gradient of sum_r dlogp[r] logp[r] + dentropy[r] entropy[r] with respect to the scores:
+ * dscores[r][i] = (dlogp ([i = target] - p_i) - dentropy p_i (log p_i + entropy)) / T, 0 for masked entries, for
+ * rows with T <= 0 and for rows with nothing left; a row whose target is n or more is NaN, and one with a target
+ * below 0 has no part of dlogp. dlogp and dentropy: device float [rows], or NULL for the scalar beside them. logp
+ * and entropy (NULL for none) receive what emr_log_probs gives, so that a training step reads the scores from
+ * memory once. dscores: [rows] rows of d_dtype, d_stride (n or more) elements apart, outside the scores' memory. Errors:
+ * as above. */
+emr_status emr_log_probs_grad(const void *scores, int32_t dtype, int32_t rows, int64_t n, int64_t row_stride,
+                              const int32_t *target, const float *temperature, float temperature_all,
+                              const float *dlogp, float dlogp_all, const float *dentropy, float dentropy_all,
+                              float *logp, float *entropy, void *dscores, int32_t d_dtype, int64_t d_stride,
+                              void *stream);
+
 /* ---- misc -------------------------------------------------------------------- */
 
 /* Static description of a status code. */

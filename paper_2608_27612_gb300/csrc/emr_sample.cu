@@ -33,6 +33,7 @@
 
 #include "emr_act.h"
 #include "emr_q8.h"
+#include "emr_rows.h"
 
 namespace {
 
@@ -67,12 +68,6 @@ struct Args {
   int32_t carry;                 // lacks have a second word
 };
 
-// Order-preserving integer of a score that is not masked; masked ones give 0.
-__device__ __forceinline__ uint32_t order_key(float s) {
-  if (!(s > -INFINITY)) return 0;
-  const uint32_t u = __float_as_uint(s + 0.f);  // -0 counts as 0
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
-}
 // Predicated, not branched around.
 __device__ __forceinline__ void shared_add(bool go, uint32_t at, uint32_t v) {
   asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p red.shared.add.u32 [%0], %1;\n\t}" ::"r"(at), "r"(v), "r"(uint32_t(go)) : "memory");
@@ -82,10 +77,6 @@ __device__ __forceinline__ uint4 shared_load(uint32_t at) {
   asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
   return v;
 }
-__device__ __forceinline__ float key_score(uint32_t k) {
-  return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
-}
-
 // A draw's best entry, the larger key first, then the lower index; its keys are non-negative
 // floats as integers, one up, so that 0 stands for none.
 struct Drawn {
@@ -100,15 +91,6 @@ __device__ __forceinline__ void join(Drawn& x, const Drawn& y) {
   x.mass += y.mass;
   x.unsure = max(x.unsure, y.unsure);
 }
-
-// 16 bytes of scores.
-template <typename T>
-struct Group {
-  static constexpr int kSize = 16 / int(sizeof(T));
-  uint4 u;
-  __device__ __forceinline__ void set(int j, T v) { reinterpret_cast<T*>(&u)[j] = v; }
-  __device__ __forceinline__ float get(int j) const { return float(reinterpret_cast<const T*>(&u)[j]); }
-};
 
 template <typename T, int kAhead>
 struct Row {

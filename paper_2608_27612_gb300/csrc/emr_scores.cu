@@ -1,0 +1,351 @@
+// Log probabilities of given answers, entropies and best answers of rows of scores, and the gradient of the
+// first two.
+//
+// With d_i = (s_i - max) / T, w_i = e^d_i and Z = sum w: logp_i = d_i - log Z, the entropy is log Z - (sum w d) / Z,
+// and the gradient of a logp_t + b H is (a ([i = t] - p_i) - b p_i (log p_i + H)) / T. One pass over a row
+// finds all three sums: a thread keeps its own maximum and its sums relative to that, and moves them when the
+// maximum rises (rarely after its first entries); the threads', and the blocks', are joined in a fixed order. A
+// gradient takes a second pass, which finds the row in L1 or L2, and writes once.
+// Bound by memory where there are many rows: about seven operations and one exponential an entry, two of each in
+// a gradient, are a good half of what an SM can do while an entry comes in. A row belongs to a warp where rows
+// are short and many, to a block, or to a cluster of up to 8 blocks where rows are few.
+// The best k: the k-th largest of the threads' own maxima is at most the k-th largest score, so only threads whose
+// maximum reaches it look at their entries again, a warp for one thread at a time (20 of 512 threads' entries for
+// k = 20). What reaches it is collected and ordered. Rows with more such entries than the list holds (equal
+// scores) find their k-th entry first, by a histogram of each byte of (score, index).
+#include <cooperative_groups.h>
+#include <cuda_runtime.h>
+
+#include <mutex>
+#include <type_traits>
+
+#include "emr_score_rows.h"
+
+namespace {
+
+using namespace emr;
+using namespace emr::rows;
+typedef unsigned long long u64;
+
+struct Args : Rows {
+  const int32_t* target;
+  float *logp, *entropy;
+  const float *dlogp, *dentropy;
+  float dlogp_all, dentropy_all;
+  int32_t top;
+  int32_t* top_index;
+  float* top_logp;
+};
+
+// Shared memory of the search for the best.
+template <int kTeam>
+struct Best {
+  static constexpr int kTeams = kTeam == 32 ? 8 : 1, kCap = kTeam == 32 ? 128 : 1024, kTop = kTeam == 32 ? 32 : EMR_MAX_TOP;
+  u64 list[kTeams][kCap], sorted[kTeams][kTop], found[kTeams];
+  uint32_t counts[kTeams][256];
+  int size[kTeams][2];
+};
+
+// The search for the best entries of a row, after its sums have been taken.
+template <typename T, int kTeam>
+struct Search : Row<T, kTeam> {
+  typedef Row<T, kTeam> R;
+  using R::blocks, R::cluster, R::count, R::each_group, R::exchange, R::fetch, R::floats, R::global, R::groups, R::kAhead, R::kG, R::kWarps, R::lane,
+      R::lo, R::own, R::rank, R::row_sync, R::skip, R::team_sync, R::tid, R::warp;
+  using R::R;
+
+  template <typename V>
+  __device__ __forceinline__ V* of_block(V* p, int r) { return blocks > 1 ? cluster.map_shared_rank(p, r) : p; }
+  __device__ static u64 entry(uint32_t key, int at) { return (u64(key) << 32) | uint32_t(~at); }
+
+  // A key that at most the k-th largest of the row reaches, from the threads' own largest.
+  __device__ uint32_t floor_key(int k) {
+    const uint32_t mine = order_key(own.m);
+    uint32_t low = 0;
+    for (int bit = 31; bit >= (kTeam == 32 ? 0 : 16); bit--) {
+      const uint32_t more = low | 1u << bit;
+      const int n = kTeam == 32 ? __popc(__ballot_sync(0xffffffffu, mine >= more)) : __syncthreads_count(mine >= more);
+      if (n >= k) low = more;
+    }
+    if (blocks > 1) {
+      const uint32_t part = low;
+      exchange(part, [&](uint32_t x) { low = max(low, x); });
+    }
+    return low > 1 ? low : 1;
+  }
+  // The entries from `least` on to the list of the row's first block (dropped past its room, but counted), by the
+  // threads of a warp for one of them after the other.
+  __device__ int collect(u64 least, u64* list, int cap, int* size) {
+    const uint32_t low = uint32_t(least >> 32);
+    uint32_t hits = __ballot_sync(0xffffffffu, order_key(own.m) >= low);
+    u64* const to = of_block(list, 0);
+    int* const places = of_block(size, 0);
+    while (hits) {
+      const int who = __ffs(int(hits)) - 1;
+      hits &= hits - 1;
+      for (int g = warp * 32 + who + lane * kTeam; g < groups; g += 32 * kTeam) {
+        float s[kG];
+        floats(fetch(g), s);
+#pragma unroll
+        for (int j = 0; j < kG; j++) {
+          const u64 e = entry(order_key(s[j]), lo + g * kG - skip + j);
+          if (e < least) continue;
+          const int place = atomicAdd(places, 1);
+          if (place < cap) to[place] = e;
+        }
+      }
+    }
+    row_sync();
+    return *places;
+  }
+  // The k-th entry in order, of a row that has as many, or one after it and before the next.
+  __device__ u64 kth(int k, uint32_t* counts, u64* found) {
+    u64 prefix = 0;
+    for (int shift = 56;; shift -= 8) {
+      for (int b = tid; b < 256; b += kTeam) counts[b] = 0;
+      team_sync();
+      int bin = -1;  // equal entries that follow each other are counted together
+      uint32_t run = 0;
+      each_group([&](const float(&s)[kAhead][kG], int g) {
+#pragma unroll 1
+        for (int u = 0; u < kAhead; u++) {
+#pragma unroll
+          for (int j = 0; j < kG; j++) {
+            const uint32_t key = order_key(s[u][j]);
+            const u64 e = entry(key, lo + (g + u * kTeam) * kG - skip + j);
+            if (!key || (shift < 56 && e >> (shift + 8) != prefix)) continue;
+            const int b = 255 - int((e >> shift) & 255u);
+            if (b != bin) {
+              if (run) atomicAdd(counts + bin, run);
+              bin = b, run = 0;
+            }
+            run++;
+          }
+        }
+      });
+      if (run) atomicAdd(counts + bin, run);
+      row_sync();
+      // the step in which the k-th lies: a lane has eight, of all blocks
+      if (warp == 0) {
+        uint32_t c[8], sum = 0;
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+          c[j] = 0;
+          for (int r = 0; r < blocks; r++) c[j] += of_block(counts, r)[lane * 8 + j];
+          sum += c[j];
+        }
+        uint32_t before = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const uint32_t x = __shfl_up_sync(0xffffffffu, before, o);
+          if (lane >= o) before += x;
+        }
+        before -= sum;
+        if (before < uint32_t(k) && uint32_t(k) <= before + sum) {
+          for (int j = 0; j < 8; j++) {
+            if (before < uint32_t(k) && uint32_t(k) <= before + c[j])
+              *found = (u64(before) << 32) | (uint32_t(lane * 8 + j) << 1) | uint32_t(before + c[j] == uint32_t(k));
+            before += c[j];
+          }
+        }
+      }
+      team_sync();
+      const u64 f = *found;
+      k -= int(f >> 32);
+      prefix = prefix << 8 | (255 - (uint32_t(f) >> 1));
+      row_sync();  // read before it is written again, and by the other blocks
+      if (f & 1 || shift == 0) return prefix << shift;
+    }
+  }
+  // The list's m entries in order, in `sorted` of the row's first block, as far as it holds them: an entry's place is
+  // the number of larger ones.
+  __device__ void order(int m, const u64* list, u64* sorted, int room) {
+    if (rank == 0) {
+      if (kTeam == 32) {
+        for (int j = lane; j < m; j += 32) {
+          const u64 e = list[j];
+          int larger = 0;
+          for (int i = 0; i < m; i++) larger += list[i] > e;
+          if (larger < room) sorted[larger] = e;
+        }
+      } else {
+        for (int j = warp; j < m; j += kWarps) {
+          const u64 e = list[j];
+          int larger = 0;
+#pragma unroll 4
+          for (int i = lane; i < m; i += 32) larger += list[i] > e;
+          larger = __reduce_add_sync(0xffffffffu, larger);
+          if (lane == 0 && larger < room) sorted[larger] = e;
+        }
+      }
+    }
+    team_sync();
+  }
+  // The best k of the row, in b.sorted of the row's first block; their number.
+  __device__ int best(int k, Best<kTeam>& b, int team) {
+    int m = collect(u64(floor_key(k)) << 32, b.list[team], b.kCap, b.size[team]);
+    if (m > b.kCap) m = collect(kth(k, b.counts[team], b.found + team), b.list[team], b.kCap, b.size[team] + 1);
+    order(m, b.list[team], b.sorted[team], b.kTop);
+    return m < k ? m : k;
+  }
+
+};
+
+// What a kernel is asked for besides the sums.
+enum Ask { kSums, kTop, kGradient };
+
+template <typename T, int kTeam, int kAsk>
+__global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam) log_probs_kernel(const __grid_constant__ Args a) {
+  __shared__ uint4 scratch[kTeam == 32 ? 1 : 64], slots[2 * kMaxCluster];
+  __shared__ std::conditional_t<kAsk == kTop, Best<kTeam>, uint32_t> best;
+  const int team = kTeam == 32 ? threadIdx.x >> 5 : 0;
+  const int64_t row = kTeam == 32 ? int64_t(blockIdx.x) * 8 + team : int64_t(blockIdx.x / cg::this_cluster().num_blocks());
+  if (kTeam == 32 && row >= a.rows) return;
+  Search<T, kTeam> r(a, row, scratch, slots);
+  if constexpr (kAsk == kTop) {
+    if (r.tid < 2) best.size[team][r.tid] = 0;
+  }
+  // a block's shared memory is written by others only when it is known to run; waited for after the pass
+  if (r.blocks > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  const float temperature = a.temperature ? a.temperature[row] : a.temperature_all;
+  const bool greedy = !(temperature > 0.f);
+  const int64_t target = a.target ? a.target[row] : -1;
+  const float dlogp = kAsk == kGradient ? (a.dlogp ? a.dlogp[row] : a.dlogp_all) : 0.f;
+  const float dentropy = kAsk == kGradient ? (a.dentropy ? a.dentropy[row] : a.dentropy_all) : 0.f;
+  r.per = greedy ? 0.f : fminf(kLog2E / temperature, 3e38f);
+
+  r.begin();
+  r.each_group([&](const auto& s, int) { r.add(s); });
+  if (r.blocks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  Stat all = r.total();
+  if (all.m == INFINITY) {
+    r.top_infinite = true;
+    r.begin();
+    r.each_group([&](const auto& s, int) { r.add(s); });
+    all = r.total();
+  }
+  const bool empty = all.m == -INFINITY;
+  const float log_z = logf(all.s);
+  const float entropy = empty || greedy ? 0.f : fmaxf(log_z - kLn2 * __fdiv_rn(all.e, all.s), 0.f);
+  const auto log_prob = [&](float s) { return s - all.m > -INFINITY ? __fdiv_rn(s - all.m, temperature) - log_z : -INFINITY; };
+
+  const int64_t first = greedy && !empty && a.logp ? r.first(all.m) : -1;
+  if constexpr (kAsk == kTop) {
+    const int got = empty ? 0 : r.best(a.top, best, team);
+    if (r.rank == 0) {
+      for (int j = r.tid; j < a.top; j += kTeam) {
+        const u64 e = j < got ? best.sorted[team][j] : 0;
+        const int64_t at = row * a.top + j;
+        if (a.top_index) a.top_index[at] = e ? int32_t(~uint32_t(e)) : -1;
+        if (a.top_logp) a.top_logp[at] = !e ? -INFINITY : greedy ? (j == 0 ? 0.f : -INFINITY) : log_prob(key_score(uint32_t(e >> 32)));
+      }
+    }
+    if (r.blocks > 1) r.cluster.sync();  // the list's size was read from the first block
+  }
+  if (r.rank == 0 && r.tid == 0) {
+    if (a.logp) {
+      const T* const scores = static_cast<const T*>(a.scores) + row * a.row_stride;
+      float v = 0.f;
+      if (target >= a.n) v = NAN;
+      else if (target >= 0) v = greedy ? (target == first ? 0.f : -INFINITY) : log_prob(r.value(scores[target]));
+      a.logp[row] = v;
+    }
+    if (a.entropy) a.entropy[row] = entropy;
+  }
+  if constexpr (kAsk == kGradient) {
+    // p (log p + H) and p from l = log2 p
+    const float per_t = greedy ? 0.f : fminf(__fdiv_rn(1.f, temperature), 3e38f);
+    const float da = target < 0 ? 0.f : target >= a.n ? NAN : dlogp;
+    const float k1 = -dentropy * per_t * kLn2, k0 = -per_t * fmaf(dentropy, entropy, da), hit = da * per_t;
+    const float log2_z = empty ? 0.f : log2f(all.s);
+    const float m = empty ? 0.f : all.m;
+    const int at = target >= r.lo && target - r.lo < r.count ? int(target - r.lo) + r.skip : -1;
+    const typename Row<T, kTeam>::Out o = r.out(a, row);
+    constexpr int kG = Row<T, kTeam>::kG;
+    r.each_group([&](const auto& s, int g) {
+#pragma unroll
+      for (int u = 0; u < r.kAhead; u++) {
+        const int from = g + u * kTeam;
+        if (from >= r.groups) break;
+        float v[kG];
+#pragma unroll
+        for (int j = 0; j < kG; j++) {
+          const float l = fmaxf((s[u][j] - m) * r.per, kFar) - log2_z;
+          v[j] = fast_exp2(l) * fmaf(l, k1, k0);
+        }
+        if (unsigned(at - from * kG) < unsigned(kG)) {
+#pragma unroll
+          for (int j = 0; j < kG; j++)
+            if (at == from * kG + j && s[u][j] > -INFINITY) v[j] += hit;
+        }
+        r.store(o, from, v);
+      }
+    });
+  }
+}
+
+// The same for every kind of call, so that all of them sum a row in the same order.
+const int* fits() {
+  static std::once_flag once;
+  static int fit[kMaxCluster + 1];
+  std::call_once(once, [&] { clusters_at_once(log_probs_kernel<float, 512, kTop>, 512, fit); });
+  return fit;
+}
+
+template <typename T, int kAsk>
+emr_status log_probs(Args a, int sms, cudaStream_t st) {
+  int cluster;
+  const int team = plan(a, kAsk == kTop && a.top > Best<32>::kTop, sms, fits(), &cluster);
+  return team == 32    ? launch_rows(log_probs_kernel<T, 32, kAsk>, a, team, cluster, st)
+         : team == 256 ? launch_rows(log_probs_kernel<T, 256, kAsk>, a, team, cluster, st)
+                       : launch_rows(log_probs_kernel<T, 512, kAsk>, a, team, cluster, st);
+}
+template <int kAsk>
+emr_status log_probs(const Args& a, int dtype, int sms, cudaStream_t st) {
+  if (dtype == EMR_F32) return log_probs<float, kAsk>(a, sms, st);
+  if (dtype == EMR_BF16) return log_probs<__nv_bfloat16, kAsk>(a, sms, st);
+  return log_probs<__half, kAsk>(a, sms, st);
+}
+
+}  // namespace
+
+extern "C" emr_status emr_log_probs(const void* scores, int32_t dtype, int32_t rows, int64_t n, int64_t row_stride,
+                                    const int32_t* target, const float* temperature, float temperature_all, int32_t top, float* logp,
+                                    float* entropy, int32_t* top_index, float* top_logp, void* stream) {
+  const emr_status ok = check_scores(scores, dtype, rows, n, row_stride);
+  if (ok != EMR_OK) return ok;
+  if (top < 0 || (logp && !target) || !aligned(target, 4) || !aligned(temperature, 4) || !aligned(logp, 4) || !aligned(entropy, 4) ||
+      !aligned(top_index, 4) || !aligned(top_logp, 4) || (!logp && !entropy && !(top && (top_index || top_logp))))
+    return EMR_ERR_ARG;
+  if (top > EMR_MAX_TOP) return EMR_ERR_RANGE;
+  int dev = 0, sms = 0;
+  if (!device_sms(&dev, &sms)) return EMR_ERR_CUDA;
+  Args a{};
+  a.scores = scores, a.n = n, a.row_stride = row_stride, a.rows = rows;
+  a.temperature = temperature, a.temperature_all = temperature_all;
+  a.target = target, a.logp = logp, a.entropy = entropy;
+  a.top = top, a.top_index = top_index, a.top_logp = top_logp;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return top && (top_index || top_logp) ? log_probs<kTop>(a, dtype, sms, st) : log_probs<kSums>(a, dtype, sms, st);
+}
+
+extern "C" emr_status emr_log_probs_grad(const void* scores, int32_t dtype, int32_t rows, int64_t n, int64_t row_stride,
+                                         const int32_t* target, const float* temperature, float temperature_all, const float* dlogp,
+                                         float dlogp_all, const float* dentropy, float dentropy_all, float* logp, float* entropy,
+                                         void* dscores, int32_t d_dtype, int64_t d_stride, void* stream) {
+  const emr_status ok = check_scores(scores, dtype, rows, n, row_stride);
+  if (ok != EMR_OK) return ok;
+  if (!target || !dscores || !dtype_ok(d_dtype) || d_stride < n || !aligned(dscores, dtype_bytes(d_dtype)) || !aligned(target, 4) ||
+      !aligned(temperature, 4) || !aligned(dlogp, 4) || !aligned(dentropy, 4) || !aligned(logp, 4) || !aligned(entropy, 4) ||
+      overlap(scores, (rows - 1) * row_stride + n, dtype_bytes(dtype), dscores, (rows - 1) * d_stride + n, dtype_bytes(d_dtype)))
+    return EMR_ERR_ARG;
+  int dev = 0, sms = 0;
+  if (!device_sms(&dev, &sms)) return EMR_ERR_CUDA;
+  Args a{};
+  a.scores = scores, a.n = n, a.row_stride = row_stride, a.rows = rows;
+  a.temperature = temperature, a.temperature_all = temperature_all;
+  a.target = target, a.logp = logp, a.entropy = entropy;
+  a.dlogp = dlogp, a.dlogp_all = dlogp_all, a.dentropy = dentropy, a.dentropy_all = dentropy_all;
+  a.dscores = dscores, a.d_dtype = d_dtype, a.d_stride = d_stride;
+  return log_probs<kGradient>(a, dtype, sms, static_cast<cudaStream_t>(stream));
+}

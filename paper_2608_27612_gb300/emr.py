@@ -112,6 +112,8 @@ def lib() -> C.CDLL:
             "emr_dense_backward": [vp, vp, i32, i32, i64, vp, vp, vp, vp, vp, i32, vp, sz, vp],
             "emr_device_error": [vp, vp],
             "emr_sample": [vp, i32, i32, i64, i64, vp, i64, vp, f32, vp, i32, vp, f32, vp, f32, vp, vp, vp],
+            "emr_log_probs": [vp, i32, i32, i64, i64, vp, vp, f32, i32, vp, vp, vp, vp, vp],
+            "emr_log_probs_grad": [vp, i32, i32, i64, i64, vp, vp, f32, vp, f32, vp, f32, vp, vp, vp, i32, i64, vp],
             "emr_version": [],
             "emr_probe_alu": [i32, i32, i32, vp, vp, vp, vp],
         }
@@ -1042,6 +1044,112 @@ def sample(scores, noise, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, stream
         if status:
             _check(status, "emr_sample")
     return index, logp
+
+
+# ---- log probabilities of answers ------------------------------------------------------------
+
+MAX_TOP = 256
+
+
+@dataclass
+class LogProbs:
+    """What log_probs gives, tensors [rows] and [rows, top]; None for what was not asked for."""
+    logp: torch.Tensor | None
+    entropy: torch.Tensor
+    top_index: torch.Tensor | None
+    top_logp: torch.Tensor | None
+
+
+def _rows_of(scores):
+    """(scores [rows, n] with neighbouring columns, rows, n, row stride, emr_dtype) of scores [rows, n] or [n]."""
+    if scores.dim() == 1:
+        scores = scores.unsqueeze(0)
+    rows, n = scores.shape
+    kind = _DTYPES.get(scores.dtype)
+    if kind is None:
+        _dtype(scores.dtype, "scores")
+    stride, col = scores.stride()
+    if col != 1 and n > 1:
+        scores, stride = scores.contiguous(), n
+    return scores, rows, n, stride, kind
+
+
+def _check_scores(scores):
+    if not isinstance(scores, torch.Tensor) or scores.dim() not in (1, 2) or not scores.is_cuda:
+        raise ValueError("scores: a tensor [rows, n] or [n] on the GPU is wanted")
+    if scores.shape[-1] < 1:
+        raise ValueError("scores: rows of at least one entry are wanted")
+    return scores.shape[0] if scores.dim() == 2 else 1
+
+
+def _number_or_rows(v, rows: int, dev, what: str):
+    """(address, number) of a float parameter that is given for each row or for all."""
+    if isinstance(v, torch.Tensor):
+        return _per_row(v, rows, torch.float32, dev, what), 0.0
+    return None, float(v)
+
+
+def _targets(targets, rows: int, dev):
+    if not isinstance(targets, torch.Tensor):
+        raise ValueError("targets: an int32 tensor [%d] on the scores' GPU is wanted" % rows)
+    return _per_row(targets, rows, torch.int32, dev, "targets")
+
+
+def log_probs(scores, targets=None, temperature=1.0, top=0, stream=None) -> LogProbs:
+    """emr_log_probs: log probabilities of the answers targets (int32 [rows], below 0: none) under scores [rows, n] (or [n];
+    float32, bfloat16, float16), the rows' entropies, and the `top` (up to MAX_TOP) best answers of each row with
+    theirs. temperature: a number, or a float32 tensor [rows]."""
+    rows = _check_scores(scores)
+    dev = scores.device
+    if not 0 <= top <= MAX_TOP:
+        raise ValueError("top: 0 to %d is wanted, got %r" % (MAX_TOP, top))
+    tp = _targets(targets, rows, dev) if targets is not None else None
+    hp, heat = _number_or_rows(temperature, rows, dev, "temperature")
+    away = _away(dev, stream)
+    if away is not None:
+        with away:
+            return log_probs(scores, targets, temperature, top)
+    scores, rows, n, stride, kind = _rows_of(scores)
+    logp = torch.empty(rows, dtype=torch.float32, device=dev) if tp is not None else None
+    entropy = torch.empty(rows, dtype=torch.float32, device=dev)
+    index = torch.empty(rows, top, dtype=torch.int32, device=dev) if top else None
+    best = torch.empty(rows, top, dtype=torch.float32, device=dev) if top else None
+    if rows:
+        status = lib().emr_log_probs(scores.data_ptr(), kind, rows, n, stride, tp, hp, heat, top,
+                                     logp.data_ptr() if tp is not None else None, entropy.data_ptr(),
+                                     index.data_ptr() if top else None, best.data_ptr() if top else None,
+                                     torch._C._cuda_getCurrentRawStream(dev.index))
+        if status:
+            _check(status, "emr_log_probs")
+    return LogProbs(logp, entropy, index, best)
+
+
+def log_probs_grad(scores, targets, dlogp, dentropy=None, temperature=1.0, out_dtype=None, stream=None):
+    """emr_log_probs_grad: (dscores, logp, entropy), the gradient of sum(dlogp logp + dentropy entropy) in the shape of scores,
+    of out_dtype (None: the scores' type), with the values that log_probs gives. dlogp and dentropy: numbers, or float32
+    tensors [rows]; dentropy None: 0. The loss of a step of cross entropy is -logp with dlogp = -1 / rows."""
+    rows = _check_scores(scores)
+    dev, shape = scores.device, scores.shape
+    tp = _targets(targets, rows, dev)
+    ap, a = _number_or_rows(dlogp, rows, dev, "dlogp")
+    bp, b = _number_or_rows(0.0 if dentropy is None else dentropy, rows, dev, "dentropy")
+    hp, heat = _number_or_rows(temperature, rows, dev, "temperature")
+    out_kind = _dtype(scores.dtype if out_dtype is None else out_dtype, "out_dtype")
+    away = _away(dev, stream)
+    if away is not None:
+        with away:
+            return log_probs_grad(scores, targets, dlogp, dentropy, temperature, out_dtype)
+    scores, rows, n, stride, kind = _rows_of(scores)
+    dscores = torch.empty(shape, dtype=out_dtype or scores.dtype, device=dev)
+    logp = torch.empty(rows, dtype=torch.float32, device=dev)
+    entropy = torch.empty(rows, dtype=torch.float32, device=dev)
+    if rows:
+        status = lib().emr_log_probs_grad(scores.data_ptr(), kind, rows, n, stride, tp, hp, heat, ap, a, bp, b, logp.data_ptr(),
+                                          entropy.data_ptr(), dscores.data_ptr(), out_kind, n,
+                                          torch._C._cuda_getCurrentRawStream(dev.index))
+        if status:
+            _check(status, "emr_log_probs_grad")
+    return dscores, logp, entropy
 
 
 # ---- ALU probes (roofline denominators) -------------------------------------------------
