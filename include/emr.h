@@ -780,6 +780,31 @@ emr_status emr_log_probs_grad(const void *scores, int32_t dtype, int32_t rows, i
                               float *logp, float *entropy, void *dscores, int32_t d_dtype, int64_t d_stride,
                               void *stream);
 
+/* ---- distillation ---------------------------------------------------------------- */
+
+/* The loss of rows of scores (as for emr_log_probs; p = softmax(scores / T) over a row's entries that are not masked) against
+ * the best answers of a teacher, and its gradient. index, teacher: device [rows][k] (k from 1 to EMR_MAX_TOP), the
+ * entries (int32) and the teacher's log probabilities of them (of teacher_dtype), as emr_log_probs gives them; an index below 0 stands for
+ * none, an entry listed more than once counts with each of its values.
+ *   tail == 0  the list is all of the teacher: t = softmax(teacher) over it, so that scores will do as well as log
+ *              probabilities; loss = sum_j t_j (log t_j - log p[index_j])
+ *   tail != 0  what the list leaves over is one more answer: t_j = exp(teacher_j), t_r = max(0, 1 - sum t), p_r = the sum of p
+ *              over entries that are not listed; loss as above plus t_r (log t_r - log p_r). t_r is 0 where
+ *              no entry that is not listed is left
+ * Terms with t = 0 are 0. With M = sum t + t_r, the gradient of sum_r dloss[r] loss[r] is dloss (M p_i - t_i) / T for listed
+ * entries, dloss p_i (M - t_r / p_r) / T for others and 0 for masked ones; neither rises nor falls with T by itself
+ * (T * T is often put into dloss). The teacher has no gradient. A row in which an index is n or more, a listed
+ * teacher value is NaN, or T (where it is given for each row) is not above 0 has a loss and a gradient of NaN; a row with nothing left
+ * has gradient 0. loss: device float [rows], NULL for none. dloss: device float [rows], or NULL for the scalar beside
+ * it. dscores: as for emr_log_probs_grad, NULL for none. Results do not depend on the order of execution. One pass over memory with or
+ * without a gradient. Errors: EMR_ERR_ARG (null or misaligned pointer, size below 1, negative stride, unknown
+ * type, temperature_all not above 0, nothing asked for), EMR_ERR_RANGE (n above 2^31 - 2^20, rows above 2^27, k above EMR_MAX_TOP),
+ * EMR_ERR_CUDA. */
+emr_status emr_distill(const void *scores, int32_t dtype, int32_t rows, int64_t n, int64_t row_stride,
+                       const int32_t *index, const void *teacher, int32_t teacher_dtype, int32_t k,
+                       const float *temperature, float temperature_all, int32_t tail, const float *dloss,
+                       float dloss_all, float *loss, void *dscores, int32_t d_dtype, int64_t d_stride, void *stream);
+
 /* ---- misc -------------------------------------------------------------------- */
 
 /* Static description of a status code. */

@@ -62,3 +62,39 @@ def log_p_gradient(s, target, a, b, T=1.0):
         if on[target]:
             g[target] += a
     return g / T
+
+
+def distill(s, index, l, T=1.0, tail=True, with_gradient=True):
+    """(loss, its gradient, the sum of the magnitudes of the loss's terms) of a row's scores against a teacher's list."""
+    v, n = live(s), len(s)
+    index, l = np.asarray(index, np.int64), np.asarray(l, np.float64)
+    on = index >= 0
+    if (index >= n).any() or np.isnan(l[on]).any() or not T > 0:
+        return np.nan, np.full(n, np.nan), np.nan
+    index, l = index[on], l[on]
+    lp = log_p(s, T)
+    p = np.exp(lp)
+    rest = np.ones(n, bool)
+    rest[index] = False
+    rest &= v > -np.inf
+    t_rest = 0.0
+    if tail:
+        t = np.exp(l)
+        if rest.any():
+            t_rest = max(0.0, 1.0 - t.sum())
+    else:
+        e = np.exp(l - l.max()) if len(l) and l.max() > -np.inf else np.zeros(len(l))
+        t = e / e.sum() if e.sum() > 0 else e
+    some = t > 0
+    with np.errstate(divide="ignore"):
+        terms = t[some] * (np.log(t[some]) - lp[index[some]])
+        if t_rest > 0:
+            m = lp[rest].max()
+            lr = m + np.log(np.exp(lp[rest] - m).sum()) if m > -np.inf else -np.inf
+            terms = np.append(terms, t_rest * (np.log(t_rest) - lr))
+    g = (t.sum() + t_rest) * p
+    np.add.at(g, index, -t)
+    if t_rest > 0 and lr > -np.inf:
+        g[rest] -= t_rest * np.exp(lp[rest] - lr)
+    g[~(v > -np.inf)] = 0.0
+    return terms.sum(), g / T, np.abs(terms).sum()

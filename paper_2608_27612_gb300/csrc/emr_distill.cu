@@ -1,0 +1,254 @@
+// Distillation: the loss of rows of scores against the best answers of a teacher, and its gradient.
+//
+// The teacher's record of a row is a list of k (entry i_j, log probability l_j). With t_j = e^l_j, or softmax(l) where
+// the list stands for all of the teacher, and p = softmax(s / T): the loss is sum t_j (log t_j - log p_i_j), and where what the
+// list leaves over counts as one more answer ("tail"), plus t_r (log t_r - log p_r), with t_r = 1 - sum t_j and p_r the
+// sum of p over the rest, the entries that are not listed. dL/ds_i is M p_i - t_i for a listed entry, M = sum t + t_r, and
+// for one of the rest, e_i (M / Z - t_r / z_r) = e_i / z_r (p_r sum t - t_r p_l), p_l being 1 - p_r: without a small difference of
+// sums near 1. For the same reason the rest has sums of its own, in which listed entries are left out by a bit for
+// each entry (one byte of shared memory is looked at for 8 of them), and its own maximum, so that a
+// rest of 1e-30 has a softmax like any other.
+// As for log probabilities, one pass over the row for the sums and, for the gradient, a second one that finds it in
+// L1 or L2 and writes once; listed entries are written over after it, k of them. Bound by memory for many rows; for
+// few, by the chain list - scores of its entries - bits - pass - sums.
+#include <cooperative_groups.h>
+#include <cuda_runtime.h>
+
+#include <mutex>
+
+#include "emr_score_rows.h"
+
+namespace {
+
+using namespace emr;
+using namespace emr::rows;
+
+struct Args : Rows {
+  const int32_t* index;
+  const void* teacher;
+  int32_t teacher_dtype, k, tail;
+  const float* dloss;
+  float dloss_all;
+  float* loss;
+};
+
+// Shared memory of a row's list, and a bit for each entry of a piece of the slice.
+template <int kTeam>
+struct List {
+  static constexpr int kTeams = kTeam == 32 ? 8 : 1, kMost = kTeam == 32 ? 64 : EMR_MAX_TOP;
+  static constexpr int kBits = kTeam == 32 ? 2048 + 256 : 131072;  // a warp's rows are one piece
+  int at[kTeams][kMost];                                           // -1: none
+  float l[kTeams][kMost], t[kTeams][kMost], s[kTeams][kMost];
+  uint32_t bits[kTeams][kBits / 32];
+  int twice[kTeams];  // an entry is listed more than once
+};
+
+__device__ __forceinline__ float load_scalar(const void* p, int dtype, int64_t i) {
+  if (dtype == EMR_F32) return static_cast<const float*>(p)[i];
+  if (dtype == EMR_BF16) return float(static_cast<const __nv_bfloat16*>(p)[i]);
+  return float(static_cast<const __half*>(p)[i]);
+}
+
+template <typename T, int kTeam>
+__global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam) distill_kernel(const __grid_constant__ Args a) {
+  typedef Row<T, kTeam> R;
+  constexpr int kG = R::kG, kAhead = R::kAhead, kBits = List<kTeam>::kBits;
+  static_assert(kTeam == 32 || kBits % (R::kTurn * kG) == 0, "a piece is whole turns");
+  __shared__ uint4 scratch[kTeam == 32 ? 1 : 64], slots[2 * kMaxCluster];
+  __shared__ List<kTeam> lists;
+  const int team = kTeam == 32 ? threadIdx.x >> 5 : 0;
+  const int64_t row = kTeam == 32 ? int64_t(blockIdx.x) * 8 + team : int64_t(blockIdx.x / cg::this_cluster().num_blocks());
+  if (kTeam == 32 && row >= a.rows) return;
+  R r(a, row, scratch, slots);
+  if (r.blocks > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  int* const at = lists.at[team];
+  float *const l = lists.l[team], *const t = lists.t[team], *const s = lists.s[team];
+  uint32_t* const bits = lists.bits[team];
+  const T* const scores = static_cast<const T*>(a.scores) + row * a.row_stride;
+  const float temperature = a.temperature ? a.temperature[row] : a.temperature_all;
+  const bool heat = temperature > 0.f;
+  r.per = heat ? fminf(kLog2E / temperature, 3e38f) : 0.f;
+
+  // the list; what cannot be told from it turns the row into NaN
+  float wrong = heat ? 0.f : NAN;
+  uint32_t l_key = 0, s_key = 0;
+  for (int j = r.tid; j < a.k; j += kTeam) {
+    const int i = a.index[row * a.k + j];
+    const float v = load_scalar(a.teacher, a.teacher_dtype, row * a.k + j);
+    const bool in = i >= 0 && i < a.n;
+    if (i >= a.n || (in && isnan(v))) wrong = NAN;
+    at[j] = in ? i : -1;
+    l[j] = in ? v : -INFINITY;
+    s[j] = in ? float(scores[i]) : -INFINITY;
+    l_key = max(l_key, order_key(l[j]));
+    s_key = max(s_key, order_key(s[j]));
+  }
+  if (r.tid == 0) lists.twice[team] = 0;
+  s_key = r.team_max(s_key);
+  float l_max = 0.f;
+  if (!a.tail) {
+    l_key = r.team_max(l_key);
+    l_max = l_key ? key_score(l_key) : 0.f;
+  }
+  float part = 0.f;
+  for (int j = r.tid; j < a.k; j += kTeam) part += t[j] = expf(l[j] - l_max);
+  const float2 sums = r.team_sum(make_float2(part, wrong));
+  const float t_sum = (!a.tail && sums.x > 0.f ? 1.f : sums.x) + sums.y;
+  const float t_scale = !a.tail && sums.x > 0.f ? __fdiv_rn(1.f, sums.x) : 1.f;
+  const float l_base = !a.tail && sums.x > 0.f ? l_max + logf(sums.x) : 0.f;  // log t_j = l_j - l_base
+
+  // the rest's sums
+  bool waited = false;
+  const auto rest_of = [&] {
+    r.begin();
+    const int end = r.groups * kG;
+    for (int from = 0; from < end; from += kBits) {
+      const int size = end - from < kBits ? end - from : kBits;
+      if (from) r.team_sync();
+      for (int w = r.tid; w < (size + 31) / 32; w += kTeam) bits[w] = 0;
+      r.team_sync();
+      for (int j = r.tid; j < a.k; j += kTeam) {
+        const int b = at[j] - r.lo + r.skip - from;
+        if (at[j] >= r.lo && at[j] - r.lo < r.count && b >= 0 && b < size) {
+          const uint32_t bit = 1u << (b & 31);
+          if (atomicOr(bits + (b >> 5), bit) & bit) lists.twice[team] = 1;
+        }
+      }
+      r.team_sync();
+      const uint8_t* const of = reinterpret_cast<const uint8_t*>(bits);
+      r.each_group([&](const float(&v)[kAhead][kG], int g) {
+        float x[kAhead][kG];
+#pragma unroll
+        for (int u = 0; u < kAhead; u++) {
+          const int b = (g + u * kTeam) * kG - from;
+          uint32_t listed = 0;
+          if (b < size) listed = of[b >> 3] >> (b & 7);
+#pragma unroll
+          for (int j = 0; j < kG; j++) x[u][j] = listed >> j & 1 ? -INFINITY : v[u][j];
+        }
+        r.template add<false>(x);
+      }, from / kG, (from + size) / kG);
+    }
+    if (r.blocks > 1 && !waited) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // the row's other blocks run
+    waited = true;
+    return r.total();
+  };
+  Stat rest = rest_of();
+  float m_listed = s_key ? key_score(s_key) : -INFINITY;
+  if (rest.m == INFINITY || m_listed == INFINITY) {
+    r.top_infinite = true;
+    const bool listed = m_listed == INFINITY;
+    r.team_sync();
+    for (int j = r.tid; j < a.k; j += kTeam) s[j] = s[j] == INFINITY ? 0.f : -INFINITY;
+    if (r.tid == 0) lists.twice[team] = 0;
+    rest = rest_of();
+    m_listed = listed ? 0.f : -INFINITY;
+  }
+  const bool twice = lists.twice[team] != 0;
+  const float m = fmaxf(rest.m, m_listed);
+  const bool empty = m == -INFINITY, has_rest = rest.m > -INFINITY;
+  // listed entries of the slice, each once
+  const auto mine = [&](int j) {
+    if (at[j] < r.lo || at[j] - r.lo >= r.count) return false;
+    if (twice)
+      for (int i = 0; i < j; i++)
+        if (at[i] == at[j]) return false;
+    return true;
+  };
+  const auto weight = [&](int j) { return s[j] > -INFINITY ? fast_exp2(fmaxf((s[j] - m) * r.per, kFar)) : 0.f; };
+  part = 0.f;
+  for (int j = r.tid; j < a.k; j += kTeam)
+    if (mine(j)) part += weight(j);
+  float z_listed = r.team_sum(make_float2(part, 0.f)).x;
+  if (r.blocks > 1) {
+    const float own = z_listed;
+    z_listed = 0.f;
+    r.exchange(own, [&](float x) { z_listed += x; });
+  }
+  const float z_rest = has_rest ? rest.s * fast_exp2(fmaxf((rest.m - m) * r.per, kFar)) : 0.f, z = z_rest + z_listed;
+  const float log_z = empty ? 0.f : logf(z), p_rest = empty ? 0.f : __fdiv_rn(z_rest, z), p_listed = empty ? 0.f : __fdiv_rn(z_listed, z);
+  const float t_rest = a.tail && has_rest ? fmaxf(1.f - t_sum, 0.f) : 0.f;
+
+  if (a.loss && r.rank == 0) {
+    part = 0.f;
+    for (int j = r.tid; j < a.k; j += kTeam) {
+      const float w = t[j] * t_scale;
+      if (w > 0.f) part += w * ((l[j] - l_base) - (s[j] - m > -INFINITY ? __fdiv_rn(s[j] - m, temperature) - log_z : -INFINITY));
+    }
+    float loss = r.team_sum(make_float2(part, 0.f)).x;
+    if (t_rest > 0.f) {
+      const float log_p = z_listed <= z_rest ? -log1pf(__fdiv_rn(z_listed, z_rest)) : __fdiv_rn(rest.m - m, temperature) + logf(rest.s) - log_z;
+      loss += t_rest * (log1pf(-t_sum) - log_p);
+    }
+    if (r.tid == 0) a.loss[row] = isnan(t_sum) ? NAN : loss;
+  }
+  if (!a.dscores) return;
+
+  const float dl = (a.dloss ? a.dloss[row] : a.dloss_all) * (heat ? fminf(__fdiv_rn(1.f, temperature), 3e38f) : 1.f);
+  const float coef = has_rest ? dl * __fdiv_rn(t_sum * p_rest - t_rest * p_listed, rest.s) : 0.f * t_sum;
+  const float m_rest = has_rest ? rest.m : 0.f;
+  const typename R::Out o = r.out(a, row);
+  r.each_group([&](const float(&v)[kAhead][kG], int g) {
+#pragma unroll
+    for (int u = 0; u < kAhead; u++) {
+      const int from = g + u * kTeam;
+      if (from >= r.groups) break;
+      float d[kG];
+#pragma unroll
+      for (int j = 0; j < kG; j++) d[j] = coef * fast_exp2(fmaxf((v[u][j] - m_rest) * r.per, kFar));
+      r.store(o, from, d);
+    }
+  });
+  r.team_sync();
+  const float mass = t_sum + t_rest;
+  for (int j = r.tid; j < a.k; j += kTeam) {
+    if (!mine(j)) continue;
+    float own = t[j];
+    if (twice)
+      for (int i = j + 1; i < a.k; i++)
+        if (at[i] == at[j]) own += t[i];
+    const bool on = s[j] > -INFINITY;
+    store_scalar(o.p, o.dtype, at[j] - r.lo, dl * (on ? mass * __fdiv_rn(weight(j), z) - own * t_scale : 0.f * mass));
+  }
+}
+
+template <typename T>
+emr_status distill(Args a, int sms, cudaStream_t st) {
+  static std::once_flag once;
+  static int fit[kMaxCluster + 1];
+  std::call_once(once, [&] { clusters_at_once(distill_kernel<float, 512>, 512, fit); });
+  int cluster;
+  const int team = plan(a, a.k > List<32>::kMost, sms, fit, &cluster);
+  return team == 32    ? launch_rows(distill_kernel<T, 32>, a, team, cluster, st)
+         : team == 256 ? launch_rows(distill_kernel<T, 256>, a, team, cluster, st)
+                       : launch_rows(distill_kernel<T, 512>, a, team, cluster, st);
+}
+
+}  // namespace
+
+extern "C" emr_status emr_distill(const void* scores, int32_t dtype, int32_t rows, int64_t n, int64_t row_stride, const int32_t* index,
+                                  const void* teacher, int32_t teacher_dtype, int32_t k, const float* temperature, float temperature_all,
+                                  int32_t tail, const float* dloss, float dloss_all, float* loss, void* dscores, int32_t d_dtype,
+                                  int64_t d_stride, void* stream) {
+  const emr_status ok = check_scores(scores, dtype, rows, n, row_stride);
+  if (ok != EMR_OK) return ok;
+  if (!index || !teacher || !dtype_ok(teacher_dtype) || k < 1 || !aligned(index, 4) || !aligned(teacher, dtype_bytes(teacher_dtype)) ||
+      !aligned(temperature, 4) || !aligned(dloss, 4) || !aligned(loss, 4) || (!loss && !dscores) || (!temperature && !(temperature_all > 0.f)))
+    return EMR_ERR_ARG;
+  if (dscores && (!dtype_ok(d_dtype) || d_stride < n || !aligned(dscores, dtype_bytes(d_dtype)) ||
+                  overlap(scores, (rows - 1) * row_stride + n, dtype_bytes(dtype), dscores, (rows - 1) * d_stride + n, dtype_bytes(d_dtype))))
+    return EMR_ERR_ARG;
+  if (k > EMR_MAX_TOP) return EMR_ERR_RANGE;
+  int dev = 0, sms = 0;
+  if (!device_sms(&dev, &sms)) return EMR_ERR_CUDA;
+  Args a{};
+  a.scores = scores, a.n = n, a.row_stride = row_stride, a.rows = rows;
+  a.temperature = temperature, a.temperature_all = temperature_all;
+  a.dscores = dscores, a.d_dtype = dscores ? d_dtype : EMR_F32, a.d_stride = d_stride;
+  a.index = index, a.teacher = teacher, a.teacher_dtype = teacher_dtype, a.k = k, a.tail = tail != 0;
+  a.dloss = dloss, a.dloss_all = dloss_all, a.loss = loss;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (dtype == EMR_F32) return distill<float>(a, sms, st);
+  if (dtype == EMR_BF16) return distill<__nv_bfloat16>(a, sms, st);
+  return distill<__half>(a, sms, st);
+}

@@ -106,10 +106,12 @@ struct Row {
       for (int j = 0; j < kG; j++) s[j] = s[j] == INFINITY ? 0.f : -INFINITY;
     }
   }
-  // fn(scores, g) for kAhead groups, loaded together: scores[u] is group g + u kTeam, -infinity past the slice.
+  // fn(scores, g) for kAhead groups, loaded together: scores[u] is group g + u kTeam, -infinity past the slice. Of the
+  // groups from first to before past, apart by whole turns.
+  static constexpr int kTurn = kTeam * kAhead;
   template <typename Fn>
-  __device__ __forceinline__ void each_group(Fn fn) const {
-    for (int g = tid; g < groups; g += kTeam * kAhead) {
+  __device__ __forceinline__ void each_group(Fn fn, int first, int past) const {
+    for (int g = first + tid; g < past; g += kTurn) {
       Group<T> v[kAhead];
 #pragma unroll
       for (int u = 0; u < kAhead; u++) v[u] = fetch(g + u * kTeam);
@@ -119,6 +121,9 @@ struct Row {
       fn(s, g);
     }
   }
+
+  template <typename Fn>
+  __device__ __forceinline__ void each_group(Fn fn) const { each_group(fn, 0, groups); }
 
   __device__ __forceinline__ void team_sync() const {
     if (kTeam == 32) __syncwarp();
@@ -164,6 +169,8 @@ struct Row {
   // ---- sums --------------------------------------------------------------------------------
 
   __device__ __forceinline__ void begin() { own = {-INFINITY, 0.f, 0.f}, s_low = e_low = 0.f; }
+  // kMean: also the sum of w d.
+  template <bool kMean = true>
   __device__ __forceinline__ void add(const float (&s)[kAhead][kG]) {
     float most = s[0][0];
 #pragma unroll
@@ -182,10 +189,10 @@ struct Row {
       for (int j = 0; j < kG; j++) {
         const float d = fmaxf((s[u][j] - own.m) * per, kFar), x = fast_exp2(d);  // the maximum takes NaN out, too
         w += x;
-        e = fmaf(d, x, e);
+        if (kMean) e = fmaf(d, x, e);
       }
     add_kept(own.s, s_low, w);
-    add_kept(own.e, e_low, e);
+    if (kMean) add_kept(own.e, e_low, e);
   }
   // The row's sums, of all threads' own.
   __device__ Stat total() {

@@ -114,6 +114,7 @@ def lib() -> C.CDLL:
             "emr_sample": [vp, i32, i32, i64, i64, vp, i64, vp, f32, vp, i32, vp, f32, vp, f32, vp, vp, vp],
             "emr_log_probs": [vp, i32, i32, i64, i64, vp, vp, f32, i32, vp, vp, vp, vp, vp],
             "emr_log_probs_grad": [vp, i32, i32, i64, i64, vp, vp, f32, vp, f32, vp, f32, vp, vp, vp, i32, i64, vp],
+            "emr_distill": [vp, i32, i32, i64, i64, vp, vp, i32, i32, vp, f32, i32, vp, f32, vp, vp, i32, i64, vp],
             "emr_version": [],
             "emr_probe_alu": [i32, i32, i32, vp, vp, vp, vp],
         }
@@ -1150,6 +1151,56 @@ def log_probs_grad(scores, targets, dlogp, dentropy=None, temperature=1.0, out_d
         if status:
             _check(status, "emr_log_probs_grad")
     return dscores, logp, entropy
+
+
+# ---- distillation ------------------------------------------------------------------------------
+
+def _distill(scores, index, logp, dloss, temperature, tail, out_dtype, stream):
+    rows = _check_scores(scores)
+    dev, shape = scores.device, scores.shape
+    if not isinstance(index, torch.Tensor) or index.dtype is not torch.int32 or index.dim() != 2 or index.shape[0] != rows or \
+            index.device != dev or not 1 <= index.shape[1] <= MAX_TOP:
+        raise ValueError("index: an int32 tensor [%d, 1 to %d] on the scores' GPU is wanted" % (rows, MAX_TOP))
+    if not isinstance(logp, torch.Tensor) or logp.shape != index.shape or logp.device != dev:
+        raise ValueError("logp: a tensor in the shape of index on the scores' GPU is wanted")
+    k, t_kind = index.shape[1], _dtype(logp.dtype, "logp")
+    hp, heat = _number_or_rows(temperature, rows, dev, "temperature")
+    if hp is None and not heat > 0:
+        raise ValueError("temperature: a number above 0 is wanted, got %r" % (temperature,))
+    grad = dloss is not None
+    wp, w = _number_or_rows(dloss, rows, dev, "dloss") if grad else (None, 0.0)
+    out_kind = _dtype(scores.dtype if out_dtype is None else out_dtype, "out_dtype") if grad else 0
+    away = _away(dev, stream)
+    if away is not None:
+        with away:
+            return _distill(scores, index, logp, dloss, temperature, tail, out_dtype, None)
+    scores, rows, n, stride, kind = _rows_of(scores)
+    index, logp = index.contiguous(), logp.contiguous()
+    dscores = torch.empty(shape, dtype=out_dtype or scores.dtype, device=dev) if grad else None
+    loss = torch.empty(rows, dtype=torch.float32, device=dev)
+    if rows:
+        status = lib().emr_distill(scores.data_ptr(), kind, rows, n, stride, index.data_ptr(), logp.data_ptr(), t_kind, k, hp, heat,
+                                   1 if tail else 0, wp, w, loss.data_ptr(), dscores.data_ptr() if grad else None, out_kind, n,
+                                   torch._C._cuda_getCurrentRawStream(dev.index))
+        if status:
+            _check(status, "emr_distill")
+    return dscores, loss
+
+
+def distill(scores, index, logp, temperature=1.0, tail=True, stream=None):
+    """emr_distill: the loss [rows] of scores [rows, n] (or [n]; float32, bfloat16, float16) against a teacher's best answers,
+    as log_probs(teacher's scores, top=k) gives them: index int32 [rows, k] (below 0: none) and logp [rows, k] (float32,
+    bfloat16, float16), log probabilities at the student's temperature. tail: what they leave over counts as one more answer; without it the teacher is
+    softmax(logp) over them. temperature: a number above 0, or a float32 tensor [rows]."""
+    return _distill(scores, index, logp, None, temperature, tail, None, stream)[1]
+
+
+def distill_grad(scores, index, logp, dloss, temperature=1.0, tail=True, out_dtype=None, stream=None):
+    """emr_distill: (dscores, loss), the gradient of sum(dloss loss) in the shape of scores, of out_dtype (None: the scores' type), with
+    the loss that distill gives, in one pass. dloss: a number, or a float32 tensor [rows]."""
+    if dloss is None:
+        raise ValueError("dloss: a number or a float32 tensor [rows] is wanted")
+    return _distill(scores, index, logp, dloss, temperature, tail, out_dtype, stream)
 
 
 # ---- ALU probes (roofline denominators) -------------------------------------------------
