@@ -745,6 +745,50 @@ emr_status emr_sample(const void *scores, int32_t dtype, int32_t rows, int64_t n
                       const float *min_p, float min_p_all, int32_t *index, float *logp,
                       void *stream);
 
+/* ---- products with 4-bit weights -------------------------------------------------- */
+
+/* Weights as a layer that only answers keeps them: batch matrices [rows][cols] of codes -8 to 7, and one scale (bfloat16)
+ * for each `group` (32, 64 or 128) consecutive columns of a row: entry = scale * code. data (device, 16-byte
+ * aligned, emr_q4_size bytes): [batch][rows / 16][cols / 128] units (rounded up) of 16 rows x 128 columns, each 1024
+ * bytes of codes, held as code + 8, and then the scales. With a row r and a column c of a unit, g = r % 8, s = c / 16, t = c % 16 / 4
+ * and j = c % 4: the code is in the 32-bit word at byte r / 8 * 512 + (4 g + t) * 16 + s / 2 * 4, from bit
+ * s % 2 * 8 + j / 2 * 4 + j % 2 * 16 on; the scale of group i of the unit is at byte 1024 + g * 512 / group + (r / 8 * 128 / group + i) *
+ * 2. What lies past rows and cols is 0. Errors of all calls: EMR_ERR_ARG (null or misaligned pointer, size below 1, negative
+ * stride, sizes that do not match, unknown type or group), EMR_ERR_RANGE (a size above 2^31 - 256, or more blocks than a launch has),
+ * EMR_ERR_CUDA. */
+typedef struct {
+    int32_t batch, group;
+    int64_t rows, cols;
+    uint8_t *data;
+} emr_q4;
+
+/* Bytes of data. Host only. */
+emr_status emr_q4_size(int32_t batch, int64_t rows, int64_t cols, int32_t group, size_t *bytes);
+
+/* Quantise src[b * batch_stride + r * row_stride + c * col_stride] (of dtype) into q: a group's scale is its largest magnitude / 7,
+ * rounded to bfloat16 (nearest even), and a code the entry / scale, rounded to the nearest (even) whole number. A group
+ * whose scale would be below 2^-126 is held as 0; one with an infinity or NaN has scale NaN. */
+emr_status emr_q4_quantize(const void *src, int32_t dtype, int64_t batch_stride, int64_t row_stride,
+                           int64_t col_stride, const emr_q4 *q, void *stream);
+
+/* Lay out given codes (device int8, of which the low four bits count) and scales (device bfloat16 [batch][rows][cols /
+ * group, rounded up] with the given strides) as q. */
+emr_status emr_q4_pack(const int8_t *codes, int64_t batch_stride, int64_t row_stride, int64_t col_stride,
+                       const void *scales, int64_t scale_batch, int64_t scale_row, int64_t scale_col,
+                       const emr_q4 *q, void *stream);
+
+/* The entries that q stands for, as a dense [batch][rows][cols] array of dtype. */
+emr_status emr_q4_dequantize(const emr_q4 *q, void *out, int32_t dtype, void *stream);
+
+/* out[b][m][n] = act(sum_k x[b][m][k] w[b][n][k] + bias[b][n]): x is x_batch matrices [rows][w.cols] of dtype with the given
+ * strides (elements), out dense [batch][rows][w.rows] of out_dtype; an operand with batch 1 serves every b. Products of codes
+ * with x are exact in all types of x, sums are in 32 bits, each group's scaled once. bias: device float [batch][w.rows] or NULL.
+ * act: EMR_ACT_*, as in emr_q8_matmul. Made for few rows, where reading w counts: w is read once for 64 rows (21 of type
+ * EMR_F32), and from L2 again for more. */
+emr_status emr_q4_matmul(const void *x, int32_t dtype, int32_t x_batch, int64_t rows, int64_t batch_stride,
+                         int64_t row_stride, int64_t col_stride, const emr_q4 *w, const float *bias, int32_t act,
+                         void *out, int32_t out_dtype, void *stream);
+
 /* ---- log probabilities of answers ---------------------------------------------- */
 
 /* How likely given answers are, how sure each row is, and its best answers. scores: device [rows][n] of dtype,

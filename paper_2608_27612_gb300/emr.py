@@ -112,6 +112,11 @@ def lib() -> C.CDLL:
             "emr_dense_backward": [vp, vp, i32, i32, i64, vp, vp, vp, vp, vp, i32, vp, sz, vp],
             "emr_device_error": [vp, vp],
             "emr_sample": [vp, i32, i32, i64, i64, vp, i64, vp, f32, vp, i32, vp, f32, vp, f32, vp, vp, vp],
+            "emr_q4_size": [i32, i64, i64, i32, vp],
+            "emr_q4_quantize": [vp, i32, i64, i64, i64, vp, vp],
+            "emr_q4_pack": [vp, i64, i64, i64, vp, i64, i64, i64, vp, vp],
+            "emr_q4_dequantize": [vp, vp, i32, vp],
+            "emr_q4_matmul": [vp, i32, i32, i64, i64, i64, i64, vp, vp, i32, vp, i32, vp],
             "emr_log_probs": [vp, i32, i32, i64, i64, vp, vp, f32, i32, vp, vp, vp, vp, vp],
             "emr_log_probs_grad": [vp, i32, i32, i64, i64, vp, vp, f32, vp, f32, vp, f32, vp, vp, vp, i32, i64, vp],
             "emr_distill": [vp, i32, i32, i64, i64, vp, vp, i32, i32, vp, f32, i32, vp, f32, vp, vp, i32, i64, vp],
@@ -1045,6 +1050,130 @@ def sample(scores, noise, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, stream
         if status:
             _check(status, "emr_sample")
     return index, logp
+
+
+# ---- products with 4-bit weights ---------------------------------------------------------------
+
+class Q4C(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("group", C.c_int32), ("rows", C.c_int64), ("cols", C.c_int64), ("data", C.c_void_p)]
+
+
+class Q4:
+    """Matrices [batch, rows, cols] of 4-bit codes (-8 to 7) with one bfloat16 scale for each `group` (32, 64 or 128) columns of a
+    row (emr_q4), in one piece of memory, `data` (uint8): what a layer that only answers keeps of its weights."""
+
+    def __init__(self, batch: int, rows: int, cols: int, group: int = 32, device="cuda", data=None):
+        n = C.c_size_t()
+        _check(lib().emr_q4_size(batch, rows, cols, group, C.byref(n)), "emr_q4_size")
+        if data is None:
+            data = torch.empty(n.value, dtype=torch.uint8, device=device)
+        elif data.dtype != torch.uint8 or data.numel() < n.value or not data.is_contiguous():
+            raise ValueError("data: a contiguous uint8 tensor of %d values is wanted" % n.value)
+        self.batch, self.rows, self.cols, self.group, self.data = batch, rows, cols, group, data
+        self.c = Q4C(batch, group, rows, cols, data.data_ptr())
+        self.ref = C.byref(self.c)
+        self._home = None  # the stream that this module allocated data on
+
+    @classmethod
+    def of(cls, data, batch: int, rows: int, cols: int, group: int = 32):
+        """The matrices that `data` (uint8, as another Q4's) holds."""
+        return cls(batch, rows, cols, group, data=data)
+
+    @property
+    def device(self):
+        return self.data.device
+
+    @property
+    def shape(self):
+        return self.batch, self.rows, self.cols
+
+
+def _new_q4(shape, group: int, dev) -> Q4:
+    if group not in (32, 64, 128):
+        raise ValueError("group: 32, 64 or 128 is wanted, got %r" % (group,))
+    q = Q4(*shape, group, device=dev)
+    q._home = torch._C._cuda_getCurrentRawStream(dev.index)
+    return q
+
+
+def q4_quantize(w, group: int = 32, stream=None) -> Q4:
+    """emr_q4_quantize: w [batch, rows, cols] or [rows, cols] (float32, bfloat16, float16; any strides) in 4 bits."""
+    w = _matrices(w, "w")
+    kind = _dtype(w.dtype, "w")
+    with _on(w.device, stream):
+        q = _new_q4(w.shape, group, w.device)
+        _check(lib().emr_q4_quantize(w.data_ptr(), kind, *w.stride(), q.ref, _stream(stream)), "emr_q4_quantize")
+    return q
+
+
+def q4_pack(codes, scales, group: int = 32, stream=None) -> Q4:
+    """emr_q4_pack: given codes (int8 -8 to 7, [batch, rows, cols] or [rows, cols]) and scales (bfloat16, [..., rows, cols / group
+    rounded up]) as a Q4."""
+    codes, scales = _matrices(codes, "codes"), _matrices(scales, "scales")
+    batch, rows, cols = codes.shape
+    if group not in (32, 64, 128):
+        raise ValueError("group: 32, 64 or 128 is wanted, got %r" % (group,))
+    if codes.dtype != torch.int8:
+        raise ValueError("codes: int8 is wanted, got %s" % codes.dtype)
+    if scales.dtype != torch.bfloat16 or scales.shape != (batch, rows, (cols + group - 1) // group):
+        raise ValueError("scales: a bfloat16 tensor %s is wanted" % ((batch, rows, (cols + group - 1) // group),))
+    _together(codes.device, scales)
+    with _on(codes.device, stream):
+        q = _new_q4(codes.shape, group, codes.device)
+        _check(lib().emr_q4_pack(codes.data_ptr(), *codes.stride(), scales.data_ptr(), *scales.stride(), q.ref, _stream(stream)),
+               "emr_q4_pack")
+    return q
+
+
+def q4_dequantize(q: Q4, dtype=torch.float32, stream=None):
+    """emr_q4_dequantize: the values that q stands for, a new [batch, rows, cols] tensor."""
+    _together(q.device)
+    kind = _dtype(dtype, "dtype")
+    with _on(q.device, stream):
+        out = torch.empty(q.shape, dtype=dtype, device=q.device)
+        _check(lib().emr_q4_dequantize(q.ref, out.data_ptr(), kind, _stream(stream)), "emr_q4_dequantize")
+    return out
+
+
+def q4_matmul(x, w: Q4, bias=None, act: int = ACT_IDENTITY, out_dtype=torch.float32, out=None, stream=None):
+    """emr_q4_matmul: act(x w^T + bias), [batch, m, w.rows], for x [batch, m, cols], [1, m, cols] or [m, cols] (float32, bfloat16,
+    float16; any strides). An operand of batch 1 serves every batch. bias: float32 [batch, w.rows] or None. Made for the few rows
+    that a layer answers at a time. m = 0 gives an empty result."""
+    x = _matrices(x, "x")
+    nx, m, k = x.shape
+    dev = x.device
+    if k != w.cols or (nx != 1 and w.batch != 1 and nx != w.batch) or nx < 1:
+        raise ValueError("x: [m, %d], [1, m, %d] or [%d, m, %d] is wanted, got %s" % (w.cols, w.cols, w.batch, w.cols, tuple(x.shape)))
+    batch = max(nx, w.batch)
+    kind = _DTYPES.get(x.dtype)
+    if kind is None:
+        _dtype(x.dtype, "x")
+    if not ACT_IDENTITY <= act <= ACT_ABS:
+        raise ValueError("act: one of ACT_* is wanted, got %r" % (act,))
+    if bias is not None and (bias.dtype != torch.float32 or not bias.is_contiguous() or bias.numel() != batch * w.rows or
+                             bias.device != dev):
+        raise ValueError("bias: a contiguous float32 tensor [%d, %d] on the operands' GPU is wanted" % (batch, w.rows))
+    if w.data.device != dev:
+        _together(dev, w)
+    shape = (batch, m, w.rows)
+    if out is not None and (tuple(out.shape) != shape or not out.is_contiguous() or out.device != dev):
+        raise ValueError("out: a contiguous tensor %s is wanted" % (shape,))
+    out_kind = _dtype(out_dtype if out is None else out.dtype, "out")
+    away = _away(dev, stream)
+    if away is not None:
+        with away:
+            return q4_matmul(x, w, bias, act, out_dtype, out)
+    if out is None:
+        out = torch.empty(shape, dtype=out_dtype, device=dev)
+    if m:
+        raw = torch._C._cuda_getCurrentRawStream(dev.index)
+        if w._home is not None and raw != w._home:
+            _lend(dev, w.data)
+        status = lib().emr_q4_matmul(x.data_ptr(), kind, nx, m, *x.stride(), w.ref, bias.data_ptr() if bias is not None else None, act,
+                                     out.data_ptr(), out_kind, raw)
+        if status:
+            _check(status, "emr_q4_matmul")
+    return out
 
 
 # ---- log probabilities of answers ------------------------------------------------------------
