@@ -32,15 +32,45 @@ struct Args : Rows {
   float* loss;
 };
 
-// Shared memory of a row's list, and a bit for each entry of a piece of the slice.
+// Shared memory of a row's list, and a byte for each group of a piece of the slice, a bit of it for each entry.
 template <int kTeam>
 struct List {
   static constexpr int kTeams = kTeam == 32 ? 8 : 1, kMost = kTeam == 32 ? 64 : EMR_MAX_TOP;
-  static constexpr int kBits = kTeam == 32 ? 2048 + 256 : 131072;  // a warp's rows are one piece
+  static constexpr int kBytes = kTeam == 32 ? 288 : 16384;         // of groups of a piece; a warp's rows are one piece
   int at[kTeams][kMost];                                           // -1: none
   float l[kTeams][kMost], t[kTeams][kMost], s[kTeams][kMost];
-  uint32_t bits[kTeams][kBits / 32];
+  uint32_t bits[kTeams][kBytes / 4];
   int twice[kTeams];  // an entry is listed more than once
+};
+
+// Sums of entries that are not listed.
+template <typename R>
+struct AddRest {
+  R& r;
+  const uint8_t* listed;
+  template <typename G, int kN>
+  __device__ __forceinline__ void operator()(const G (&v)[kN], int g) {
+    G x[kN];
+#pragma unroll
+    for (int u = 0; u < kN; u++) {
+      x[u] = v[u];
+      const uint32_t l = listed[g + u * R::kTeamSize];
+      if (l) {
+#pragma unroll
+        for (int j = 0; j < R::kG; j++)
+          if (l >> j & 1) x[u].mask(j);
+      }
+    }
+    r.template add<false>(x);
+  }
+};
+// An entry of the rest in the gradient.
+struct Slope {
+  float m, per, coef;
+  __device__ __forceinline__ float2 operator()(float s0, float s1) const {
+    const float2 d = far2(s0, s1, m, per);
+    return mul2(make_float2(fast_exp2(d.x), fast_exp2(d.y)), make_float2(coef, coef));
+  }
 };
 
 __device__ __forceinline__ float load_scalar(const void* p, int dtype, int64_t i) {
@@ -50,10 +80,9 @@ __device__ __forceinline__ float load_scalar(const void* p, int dtype, int64_t i
 }
 
 template <typename T, int kTeam>
-__global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam) distill_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? 2 : kTeam == 128 ? 8 : 4) distill_kernel(const __grid_constant__ Args a) {
   typedef Row<T, kTeam> R;
-  constexpr int kG = R::kG, kAhead = R::kAhead, kBits = List<kTeam>::kBits;
-  static_assert(kTeam == 32 || kBits % (R::kTurn * kG) == 0, "a piece is whole turns");
+  constexpr int kG = R::kG, kPiece = List<kTeam>::kBytes;
   __shared__ uint4 scratch[kTeam == 32 ? 1 : 64], slots[2 * kMaxCluster];
   __shared__ List<kTeam> lists;
   const int team = kTeam == 32 ? threadIdx.x >> 5 : 0;
@@ -98,51 +127,34 @@ __global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam) distill_kernel(cons
   const float l_base = !a.tail && sums.x > 0.f ? l_max + logf(sums.x) : 0.f;  // log t_j = l_j - l_base
 
   // the rest's sums
-  bool waited = false;
-  const auto rest_of = [&] {
+  Stat rest;
+  float m_listed = s_key ? key_score(s_key) : -INFINITY;
+  for (bool again = false;; again = true) {
     r.begin();
-    const int end = r.groups * kG;
-    for (int from = 0; from < end; from += kBits) {
-      const int size = end - from < kBits ? end - from : kBits;
+    for (int from = 0; from < r.groups; from += kPiece) {
+      const int past = r.groups - from < kPiece ? r.groups : from + kPiece;
       if (from) r.team_sync();
-      for (int w = r.tid; w < (size + 31) / 32; w += kTeam) bits[w] = 0;
+      for (int w = r.tid; w < (past - from + 3) / 4; w += kTeam) bits[w] = 0;
       r.team_sync();
       for (int j = r.tid; j < a.k; j += kTeam) {
-        const int b = at[j] - r.lo + r.skip - from;
-        if (at[j] >= r.lo && at[j] - r.lo < r.count && b >= 0 && b < size) {
-          const uint32_t bit = 1u << (b & 31);
-          if (atomicOr(bits + (b >> 5), bit) & bit) lists.twice[team] = 1;
-        }
+        if (at[j] < r.lo || at[j] - r.lo >= r.count) continue;
+        const int i = at[j] - r.lo + r.skip, b = i / kG - from;
+        if (b < 0 || b >= past - from) continue;
+        const uint32_t bit = 1u << (b % 4 * 8 + i % kG);
+        if (atomicOr(bits + b / 4, bit) & bit) lists.twice[team] = 1;
       }
       r.team_sync();
-      const uint8_t* const of = reinterpret_cast<const uint8_t*>(bits);
-      r.each_group([&](const float(&v)[kAhead][kG], int g) {
-        float x[kAhead][kG];
-#pragma unroll
-        for (int u = 0; u < kAhead; u++) {
-          const int b = (g + u * kTeam) * kG - from;
-          uint32_t listed = 0;
-          if (b < size) listed = of[b >> 3] >> (b & 7);
-#pragma unroll
-          for (int j = 0; j < kG; j++) x[u][j] = listed >> j & 1 ? -INFINITY : v[u][j];
-        }
-        r.template add<false>(x);
-      }, from / kG, (from + size) / kG);
+      AddRest<R> add{r, reinterpret_cast<const uint8_t*>(bits) - from};
+      r.each(add, from ? from : r.head, past, from == 0);
     }
-    if (r.blocks > 1 && !waited) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // the row's other blocks run
-    waited = true;
-    return r.total();
-  };
-  Stat rest = rest_of();
-  float m_listed = s_key ? key_score(s_key) : -INFINITY;
-  if (rest.m == INFINITY || m_listed == INFINITY) {
+    if (!again && r.blocks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // the row's other blocks run
+    rest = r.total();
+    if (rest.m < INFINITY && m_listed < INFINITY) break;
+    m_listed = m_listed == INFINITY ? 0.f : -INFINITY;
     r.top_infinite = true;
-    const bool listed = m_listed == INFINITY;
     r.team_sync();
     for (int j = r.tid; j < a.k; j += kTeam) s[j] = s[j] == INFINITY ? 0.f : -INFINITY;
     if (r.tid == 0) lists.twice[team] = 0;
-    rest = rest_of();
-    m_listed = listed ? 0.f : -INFINITY;
   }
   const bool twice = lists.twice[team] != 0;
   const float m = fmaxf(rest.m, m_listed);
@@ -188,17 +200,7 @@ __global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam) distill_kernel(cons
   const float coef = has_rest ? dl * __fdiv_rn(t_sum * p_rest - t_rest * p_listed, rest.s) : 0.f * t_sum;
   const float m_rest = has_rest ? rest.m : 0.f;
   const typename R::Out o = r.out(a, row);
-  r.each_group([&](const float(&v)[kAhead][kG], int g) {
-#pragma unroll
-    for (int u = 0; u < kAhead; u++) {
-      const int from = g + u * kTeam;
-      if (from >= r.groups) break;
-      float d[kG];
-#pragma unroll
-      for (int j = 0; j < kG; j++) d[j] = coef * fast_exp2(fmaxf((v[u][j] - m_rest) * r.per, kFar));
-      r.store(o, from, d);
-    }
-  });
+  r.put(o, Slope{m_rest, r.per, coef});
   r.team_sync();
   const float mass = t_sum + t_rest;
   for (int j = r.tid; j < a.k; j += kTeam) {
@@ -218,8 +220,9 @@ emr_status distill(Args a, int sms, cudaStream_t st) {
   static int fit[kMaxCluster + 1];
   std::call_once(once, [&] { clusters_at_once(distill_kernel<float, 512>, 512, fit); });
   int cluster;
-  const int team = plan(a, a.k > List<32>::kMost, sms, fit, &cluster);
+  const int team = plan(a, a.k <= List<32>::kMost ? 32 : 128, sizeof(T), sms, fit, &cluster);
   return team == 32    ? launch_rows(distill_kernel<T, 32>, a, team, cluster, st)
+         : team == 128 ? launch_rows(distill_kernel<T, 128>, a, team, cluster, st)
          : team == 256 ? launch_rows(distill_kernel<T, 256>, a, team, cluster, st)
                        : launch_rows(distill_kernel<T, 512>, a, team, cluster, st);
 }

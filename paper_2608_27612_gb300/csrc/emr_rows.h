@@ -22,6 +22,7 @@ struct Group {
   static constexpr int kSize = 16 / int(sizeof(T));
   uint4 u;
   __device__ __forceinline__ void set(int j, T v) { reinterpret_cast<T*>(&u)[j] = v; }
+  __device__ __forceinline__ void mask(int j) { set(j, T(-INFINITY)); }
   __device__ __forceinline__ float get(int j) const { return float(reinterpret_cast<const T*>(&u)[j]); }
 };
 

@@ -6,6 +6,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "emr_act.h"
 #include "emr_q8.h"
 #include "emr_rows.h"
@@ -51,16 +53,45 @@ __device__ __forceinline__ void add_kept(float& x, float& low, float v) {
   low = (sum - x) - more, x = sum;
 }
 
-// One row, by a team of 32 threads (a warp of a block of 8) or of a block, and for a block's team by a cluster of them.
+// Two values at a time.
+__device__ __forceinline__ float2 add2(float2 x, float2 y) {
+  float2 r;
+  asm("{\n\t.reg .b64 a, b, c;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 c, a, b;\n\tmov.b64 {%0, %1}, c;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y));
+  return r;
+}
+__device__ __forceinline__ float2 mul2(float2 x, float2 y) {
+  float2 r;
+  asm("{\n\t.reg .b64 a, b, c;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 c, a, b;\n\tmov.b64 {%0, %1}, c;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y));
+  return r;
+}
+__device__ __forceinline__ float2 fma2(float2 x, float2 y, float2 z) {
+  float2 r;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\tfma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y), "f"(z.x), "f"(z.y));
+  return r;
+}
+// (s - m) / T of two scores in units of log2, masked ones at kFar: the maximum takes NaN out, too.
+__device__ __forceinline__ float2 far2(float s0, float s1, float m, float per) {
+  const float2 d = mul2(add2(make_float2(s0, s1), make_float2(-m, -m)), make_float2(per, per));
+  return make_float2(fmaxf(d.x, kFar), fmaxf(d.y, kFar));
+}
+
+// One row, by a team of 32 threads (a warp of a block of 8) or of a block, and for the largest team by a cluster of blocks.
+// Threads take it in turns of kAhead groups of 16 bytes each, loaded together and without a check, while all threads have as
+// many; the groups that are left, among them those that reach out of the slice, one at a time.
 template <typename T, int kTeam>
 struct Row {
-  static constexpr int kG = Group<T>::kSize, kAhead = 4, kWarps = kTeam / 32;
+  static constexpr int kG = Group<T>::kSize, kAhead = 4, kWarps = kTeam / 32, kTurn = kTeam * kAhead, kTeamSize = kTeam;
   cg::cluster_group cluster;
   int tid, lane, warp, rank, blocks, phase, turn;
   int lo;            // first entry of this block's slice
   int count;         // its entries, the first of them `skip` entries after a multiple of 16 bytes
   int skip, groups;  // groups of 16 bytes that they lie in
+  int head;          // 1 where the first of them reaches out of the slice
   const T* global;   // the slice in memory
+  bool inside;       // the rest of its first and last group lies in the scores' memory, too
   uint4* scratch;    // [2][32], by turns: a turn's values are read by all before the next but one writes
   uint4* slots;      // [2][kMaxCluster]
   bool top_infinite; // only the entries of +infinity count, as score 0
@@ -68,7 +99,7 @@ struct Row {
   Stat own;          // of the thread's entries
   float s_low, e_low;
 
-  __device__ Row(const Rows& a, int64_t row, uint4* scratch_, uint4* slots_) : cluster(cg::this_cluster()), scratch(scratch_), slots(slots_) {
+  __device__ __forceinline__ Row(const Rows& a, int64_t row, uint4* scratch_, uint4* slots_) : cluster(cg::this_cluster()), scratch(scratch_), slots(slots_) {
     lane = threadIdx.x & 31;
     tid = kTeam == 32 ? lane : threadIdx.x;
     warp = tid >> 5;
@@ -77,53 +108,86 @@ struct Row {
     const int64_t at = rank * a.slice, left = a.n - at;
     lo = int(at < a.n ? at : a.n);
     count = int(left < 0 ? 0 : left < a.slice ? left : a.slice);
-    global = static_cast<const T*>(a.scores) + row * a.row_stride + lo;
+    const T* const scores = static_cast<const T*>(a.scores);
+    global = scores + row * a.row_stride + lo;
     skip = int(reinterpret_cast<uintptr_t>(global) % 16 / sizeof(T));
     groups = (skip + count + kG - 1) / kG;
+    inside = global - skip >= scores && global - skip + int64_t(groups) * kG <= scores + (a.rows - 1) * a.row_stride + a.n;
     top_infinite = false;
+    head = skip ? 1 : 0;
   }
   __device__ __forceinline__ float value(T v) const {
     const float s = float(v);
     return top_infinite ? (s == INFINITY ? 0.f : -INFINITY) : s;
   }
-  // One group from memory; past the slice its scores are -infinity.
+  // One group from memory, which may reach out of the slice.
   __device__ __forceinline__ Group<T> fetch(int g) const {
-    Group<T> v;
     const int i = g * kG - skip;
-    if (i >= 0 && i + kG <= count) {
-      v.u = *reinterpret_cast<const uint4*>(global + i);
-    } else {
-#pragma unroll
-      for (int j = 0; j < kG; j++) v.set(j, i + j >= 0 && i + j < count ? global[i + j] : T(-INFINITY));
-    }
+    Group<T> v;
+    if (!inside && (i < 0 || i + kG > count)) v.u = fetch_part(global, i, count);
+    else v.u = *reinterpret_cast<const uint4*>(global + i);
     return v;
   }
-  __device__ __forceinline__ void floats(const Group<T>& v, float (&s)[kG]) const {
+  // The same where what lies around the scores may not be read.
+  __device__ static __noinline__ uint4 fetch_part(const T* global, int i, int count) {
+    Group<T> v;
+#pragma unroll
+    for (int j = 0; j < kG; j++) v.set(j, unsigned(i + j) < unsigned(count) ? global[i + j] : T(0.f));
+    return v.u;
+  }
+  // With a score of +infinity in the row all others do not count.
+  __device__ __forceinline__ void infinite(Group<T>& v) const {
+#pragma unroll
+    for (int j = 0; j < kG; j++) v.set(j, v.get(j) == INFINITY ? T(0.f) : T(-INFINITY));
+  }
+  // One group, -infinity out of the slice.
+  __device__ __forceinline__ Group<T> masked(int g) const {
+    Group<T> v = fetch(g);
+    const int i = g * kG - skip;
+    if (i < 0 || i + kG > count) {
+#pragma unroll
+      for (int j = 0; j < kG; j++)
+        if (unsigned(i + j) >= unsigned(count)) v.mask(j);
+    }
+    if (top_infinite) infinite(v);
+    return v;
+  }
+  __device__ __forceinline__ static void floats(const Group<T>& v, float (&s)[kG]) {
 #pragma unroll
     for (int j = 0; j < kG; j++) s[j] = v.get(j);
-    if (top_infinite) {
-#pragma unroll
-      for (int j = 0; j < kG; j++) s[j] = s[j] == INFINITY ? 0.f : -INFINITY;
-    }
   }
-  // fn(scores, g) for kAhead groups, loaded together: scores[u] is group g + u kTeam, -infinity past the slice. Of the
-  // groups from first to before past, apart by whole turns.
-  static constexpr int kTurn = kTeam * kAhead;
+  // fn(v, g) of an array of groups g, g + kTeam ... that lie in the slice as a whole, or of one group, for those from first
+  // (head or more) to before past, and the first one of all where with_head: after the others.
   template <typename Fn>
-  __device__ __forceinline__ void each_group(Fn fn, int first, int past) const {
-    for (int g = first + tid; g < past; g += kTurn) {
+  __device__ __forceinline__ void each(Fn& fn, int first, int past, bool with_head) const {
+    const int whole = (skip + count) / kG < past ? (skip + count) / kG : past, turns = (whole - first) / kTurn;
+    int g = first + tid;
+    const uint4* from = reinterpret_cast<const uint4*>(global + (g * kG - skip));
+    for (int i = 0; i < turns; i++) {
       Group<T> v[kAhead];
 #pragma unroll
-      for (int u = 0; u < kAhead; u++) v[u] = fetch(g + u * kTeam);
-      float s[kAhead][kG];
+      for (int u = 0; u < kAhead; u++) v[u].u = from[u * kTeam];
+      if (top_infinite) {
 #pragma unroll
-      for (int u = 0; u < kAhead; u++) floats(v[u], s[u]);
-      fn(s, g);
+        for (int u = 0; u < kAhead; u++) infinite(v[u]);
+      }
+      fn(v, g);
+      g += kTurn, from += kTurn;
     }
+    const int end = past + (with_head ? head : 0);
+    if (g >= end) return;
+    Group<T> next = masked(g == past ? 0 : g);
+#pragma unroll 1
+    do {
+      Group<T> v[1] = {next};
+      const int at = g == past ? 0 : g;
+      g += kTeam;
+      if (g < end) next = masked(g == past ? 0 : g);
+      fn(v, at);
+    } while (g < end);
   }
-
   template <typename Fn>
-  __device__ __forceinline__ void each_group(Fn fn) const { each_group(fn, 0, groups); }
+  __device__ __forceinline__ void each(Fn& fn) const { each(fn, head, groups, true); }
 
   __device__ __forceinline__ void team_sync() const {
     if (kTeam == 32) __syncwarp();
@@ -169,30 +233,53 @@ struct Row {
   // ---- sums --------------------------------------------------------------------------------
 
   __device__ __forceinline__ void begin() { own = {-INFINITY, 0.f, 0.f}, s_low = e_low = 0.f; }
-  // kMean: also the sum of w d.
-  template <bool kMean = true>
-  __device__ __forceinline__ void add(const float (&s)[kAhead][kG]) {
-    float most = s[0][0];
+  // The largest of a group's scores; NaN is passed over.
+  __device__ __forceinline__ static float largest(const Group<T>& v) {
+    if constexpr (kG == 4) {
+      return fmaxf(fmaxf(v.get(0), v.get(1)), fmaxf(v.get(2), v.get(3)));
+    } else {
+      typedef std::conditional_t<std::is_same<T, __half>::value, __half2, __nv_bfloat162> T2;
+      const T2* const p = reinterpret_cast<const T2*>(&v.u);
+      const T2 m = __hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3]));
+      return fmaxf(float(m.x), float(m.y));
+    }
+  }
+  // Some entries. kMean: also the sum of w d.
+  template <bool kMean, int kN>
+  __device__ __forceinline__ void add(const Group<T> (&v)[kN]) {
+    float most = largest(v[0]);
 #pragma unroll
-    for (int u = 0; u < kAhead; u++)
-#pragma unroll
-      for (int j = 0; j < kG; j++) most = fmaxf(most, s[u][j]);  // NaN is passed over
+    for (int u = 1; u < kN; u++) most = fmaxf(most, largest(v[u]));
     if (most > own.m) {
       shift(own, most, per);
       s_low = e_low = 0.f;
     }
     if (own.m == -INFINITY) return;
-    float w = 0.f, e = 0.f;
+    float2 w = make_float2(0.f, 0.f), e = w;
 #pragma unroll
-    for (int u = 0; u < kAhead; u++)
+    for (int u = 0; u < kN; u++) {
+      float s[kG];
+      floats(v[u], s);
 #pragma unroll
-      for (int j = 0; j < kG; j++) {
-        const float d = fmaxf((s[u][j] - own.m) * per, kFar), x = fast_exp2(d);  // the maximum takes NaN out, too
-        w += x;
-        if (kMean) e = fmaf(d, x, e);
+      for (int j = 0; j < kG; j += 2) {
+        const float2 d = far2(s[j], s[j + 1], own.m, per), x = make_float2(fast_exp2(d.x), fast_exp2(d.y));
+        w = add2(w, x);
+        if (kMean) e = fma2(d, x, e);
       }
-    add_kept(own.s, s_low, w);
-    if (kMean) add_kept(own.e, e_low, e);
+    }
+    add_kept(own.s, s_low, w.x + w.y);
+    if (kMean) add_kept(own.e, e_low, e.x + e.y);
+  }
+  struct Add {
+    Row& r;
+    template <int kN>
+    __device__ __forceinline__ void operator()(const Group<T> (&v)[kN], int) { r.template add<true>(v); }
+  };
+  // Of all entries.
+  __device__ __forceinline__ void sum_up() {
+    begin();
+    Add add_all{*this};
+    each(add_all);
   }
   // The row's sums, of all threads' own.
   __device__ Stat total() {
@@ -215,13 +302,12 @@ struct Row {
   // Where the row's largest score, m, stands first.
   __device__ int64_t first(float m) {
     uint32_t from_end = 0;
-    each_group([&](const float (&s)[kAhead][kG], int g) {
+    for (int g = tid; g < groups; g += kTeam) {
+      const Group<T> v = masked(g);
 #pragma unroll
-      for (int u = 0; u < kAhead; u++)
-#pragma unroll
-        for (int j = 0; j < kG; j++)
-          if (s[u][j] == m) from_end = max(from_end, 0xffffffffu - uint32_t(lo + (g + u * kTeam) * kG - skip + j));
-    });
+      for (int j = 0; j < kG; j++)
+        if (v.get(j) == m) from_end = max(from_end, 0xffffffffu - uint32_t(lo + g * kG - skip + j));
+    }
     from_end = team_max(from_end);
     if (blocks > 1) {
       const uint32_t part = from_end;
@@ -257,18 +343,59 @@ struct Row {
     for (int k = 0; k < kBytes / 16; k++)
       __stcs(reinterpret_cast<uint4*>(p) + k, make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]));
   }
-  __device__ __forceinline__ void store(const Out& o, int g, const float (&v)[kG]) const {
+  // What f makes of the groups' scores (two at a time) to their places in the gradient.
+  template <int kN, typename F>
+  __device__ __forceinline__ void store(const Out& o, const Group<T> (&v)[kN], int g, F& f) const {
     const int i = g * kG - skip;
-    if (o.whole && i >= 0 && i + kG <= count) {
-      uint8_t* const p = o.p + int64_t(i) * o.size;
-      if (o.dtype == EMR_F32) store_whole<float>(p, v);
-      else if (o.dtype == EMR_BF16) store_whole<__nv_bfloat16>(p, v);
-      else store_whole<__half>(p, v);
+    uint8_t* const p = o.p + int64_t(i) * o.size;
+    if (o.whole && (kN > 1 || (i >= 0 && i + kG <= count))) {
+      if (o.dtype == EMR_F32) store_as<float>(p, v, f);
+      else if (o.dtype == EMR_BF16) store_as<__nv_bfloat16>(p, v, f);
+      else store_as<__half>(p, v, f);
     } else {
 #pragma unroll
-      for (int j = 0; j < kG; j++)
-        if (i + j >= 0 && i + j < count) store_scalar(o.p, o.dtype, i + j, v[j]);
+      for (int u = 0; u < kN; u++) {
+        float s[kG];
+        made(v[u], s, f);
+#pragma unroll
+        for (int j = 0; j < kG; j++) {
+          const int at = i + u * kTeam * kG + j;
+          if (kN > 1 || unsigned(at) < unsigned(count)) store_scalar(o.p, o.dtype, at, s[j]);
+        }
+      }
     }
+  }
+  template <typename F>
+  __device__ __forceinline__ static void made(const Group<T>& v, float (&s)[kG], F& f) {
+    floats(v, s);
+#pragma unroll
+    for (int j = 0; j < kG; j += 2) {
+      const float2 y = f(s[j], s[j + 1]);
+      s[j] = y.x, s[j + 1] = y.y;
+    }
+  }
+  template <typename D, int kN, typename F>
+  __device__ __forceinline__ static void store_as(uint8_t* p, const Group<T> (&v)[kN], F& f) {
+#pragma unroll
+    for (int u = 0; u < kN; u++) {
+      float s[kG];
+      made(v[u], s, f);
+      store_whole<D>(p + u * kTeam * kG * int(sizeof(D)), s);
+    }
+  }
+  // The whole slice.
+  template <typename F>
+  struct Put {
+    const Row& r;
+    const Out& o;
+    F& f;
+    template <int kN>
+    __device__ __forceinline__ void operator()(const Group<T> (&v)[kN], int g) { r.store(o, v, g, f); }
+  };
+  template <typename F>
+  __device__ __forceinline__ void put(const Out& o, F f) const {
+    Put<F> all{*this, o, f};
+    each(all);
   }
 };
 
@@ -306,14 +433,19 @@ void clusters_at_once(K kernel, int threads, int* fit) {
   }
 }
 
-// The team and cluster of a row, and the slice of its blocks. `wide`: what is asked for wants more threads than a warp.
-inline int plan(Rows& a, bool wide, int sms, const int* fit, int* cluster) {
+// The team and cluster of a row, and the slice of its blocks: the same with and without a gradient, so that the values are.
+// least: the smallest team that will do; size: bytes of a score.
+inline int plan(Rows& a, int least, int size, int sms, const int* fit, int* cluster) {
   *cluster = 1;
   a.slice = (a.n + 15) / 16 * 16;
-  if (!wide && a.n <= 2048 && a.rows >= 8 * sms) return 32;
-  if (a.n <= 8192) return 256;
+  if (a.n <= 8192) {
+    if (least <= 32 && a.n <= 1024 && a.rows >= 16 * sms) return 32;
+    return least <= 128 && a.rows >= 4 * sms ? 128 : 256;
+  }
   for (int c = 2; c <= kMaxCluster; c++)
     if (a.rows <= fit[c] && a.n / c >= 4096) *cluster = c;
+  // a row that is read again, for its gradient, should still be in L2
+  while (2 * *cluster <= kMaxCluster && a.n / (2 * *cluster) >= 8192 && 2. * sms / *cluster * double(a.n) * size > double(64 << 20)) *cluster *= 2;
   a.slice = ((a.n + *cluster - 1) / *cluster + 15) / 16 * 16;
   return 512;
 }

@@ -40,59 +40,150 @@ struct Args : Rows {
 // Shared memory of the search for the best.
 template <int kTeam>
 struct Best {
-  static constexpr int kTeams = kTeam == 32 ? 8 : 1, kCap = kTeam == 32 ? 128 : 1024, kTop = kTeam == 32 ? 32 : EMR_MAX_TOP;
+  static constexpr int kTeams = kTeam == 32 ? 8 : 1, kCap = kTeam == 32 ? 128 : kTeam == 512 ? 2048 : 1024;
+  static constexpr int kTop = kTeam == 32 ? 32 : kTeam == 128 ? 64 : EMR_MAX_TOP;
   u64 list[kTeams][kCap], sorted[kTeams][kTop], found[kTeams];
-  uint32_t counts[kTeams][256];
-  int size[kTeams][2];
+  alignas(16) uint32_t counts[kTeams][256];  // read 16 bytes at a time
+  int size[kTeams][2], hits[kTeams];
+  uint16_t who[kTeams][kTeam];
 };
 
 // The search for the best entries of a row, after its sums have been taken.
 template <typename T, int kTeam>
 struct Search : Row<T, kTeam> {
   typedef Row<T, kTeam> R;
-  using R::blocks, R::cluster, R::count, R::each_group, R::exchange, R::fetch, R::floats, R::global, R::groups, R::kAhead, R::kG, R::kWarps, R::lane,
-      R::lo, R::own, R::rank, R::row_sync, R::skip, R::team_sync, R::tid, R::warp;
+  using R::blocks, R::cluster, R::exchange, R::floats, R::groups, R::head, R::kG, R::masked,
+      R::kWarps, R::lane, R::lo, R::own, R::rank, R::row_sync, R::skip, R::team_max, R::team_sync, R::tid, R::warp;
   using R::R;
 
   template <typename V>
   __device__ __forceinline__ V* of_block(V* p, int r) { return blocks > 1 ? cluster.map_shared_rank(p, r) : p; }
   __device__ static u64 entry(uint32_t key, int at) { return (u64(key) << 32) | uint32_t(~at); }
 
-  // A key that at most the k-th largest of the row reaches, from the threads' own largest.
-  __device__ uint32_t floor_key(int k) {
+  // The r-th largest key of a warp's threads, 0 where there are fewer.
+  __device__ __forceinline__ uint32_t warp_kth(uint32_t key, int r) const {
+    for (int i = 1; i < r; i++) {
+      const uint32_t top = __reduce_max_sync(0xffffffffu, key);
+      if (lane == __ffs(int(__ballot_sync(0xffffffffu, key == top))) - 1) key = 0;
+    }
+    return __reduce_max_sync(0xffffffffu, key);
+  }
+  // A key that at least k of the row's threads' own largest reach, and few more: 1 where too few threads have one.
+  __device__ uint32_t floor_key(int k, uint32_t* counts, u64* found) {
     const uint32_t mine = order_key(own.m);
+    if (kTeam == 32) return max(warp_kth(mine, k), 1u);
+    if (blocks == 1) {
+      // every warp's r-th, r such that they have k together
+      const int full = groups / 32 < kWarps ? groups / 32 : kWarps, r = full ? (k + full - 1) / full : 33;
+      if (r <= 32) {
+        const uint32_t low = ~team_max(warp < full ? ~warp_kth(mine, r) : 0u);
+        if (low) return low;
+      }
+    } else {
+      // the same over all blocks, of warps that have as many; then, as that is low, by equal steps from there to the
+      // largest, so that little more than k are left
+      struct Part {
+        uint32_t top, low, warps, none;
+      };
+      const int r = (2 * k + kWarps * blocks - 1) / (kWarps * blocks);
+      const uint32_t kth = r <= 32 ? warp_kth(mine, r) : 0u;
+      Part all{0, 0xffffffffu, 0, 0};
+      const uint32_t low_here = ~team_max(kth ? ~kth : 0u), top_here = team_max(mine);
+      for (int b = tid; b < 256; b += kTeam) counts[b] = 0;
+      const uint32_t warps_here = __syncthreads_count(kth && lane == 0);
+      exchange(Part{top_here, low_here, warps_here, 0}, [&](const Part& x) {
+        all.top = max(all.top, x.top), all.low = min(all.low, x.low), all.warps += x.warps;
+      });
+      if (int64_t(all.warps) * r >= k) {
+        const float top = key_score(all.top), span = top - key_score(all.low);
+        const float steps = span > 0.f ? fminf(255.f / span, 3e38f) : 0.f;
+        if (mine >= all.low) atomicAdd(counts + min(255, int((top - key_score(mine)) * steps)), 1u);
+        row_sync();
+        if (warp == 0) {
+          uint32_t c[8] = {}, sum = 0;
+          for (int b = 0; b < blocks; b++) {
+            const uint4* const of = reinterpret_cast<const uint4*>(of_block(counts, b)) + lane * 2;
+            const uint4 x = of[0], y = of[1];
+            c[0] += x.x, c[1] += x.y, c[2] += x.z, c[3] += x.w, c[4] += y.x, c[5] += y.y, c[6] += y.z, c[7] += y.w;
+          }
+#pragma unroll
+          for (int j = 0; j < 8; j++) sum += c[j];
+          uint32_t before = sum;
+#pragma unroll
+          for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t x = __shfl_up_sync(0xffffffffu, before, o);
+            if (lane >= o) before += x;
+          }
+          before -= sum;
+#pragma unroll
+          for (int j = 0; j < 8; j++) {
+            if (before < uint32_t(k) && uint32_t(k) <= before + c[j]) *found = u64(lane * 8 + j);
+            before += c[j];
+          }
+        }
+        team_sync();
+        const int step = int(*found);
+        // the least key of that step: keys and steps fall together
+        uint32_t least = all.low, past = all.top;
+        while (least < past) {
+          const uint32_t mid = least + (past - least) / 2;
+          if (min(255, int((top - key_score(mid)) * steps)) <= step) past = mid;
+          else least = mid + 1;
+        }
+        row_sync();  // the counts have been read
+        return max(least, 1u);
+      }
+    }
+    // the k-th of a block's threads, bit by bit, and the best of the blocks' own
     uint32_t low = 0;
-    for (int bit = 31; bit >= (kTeam == 32 ? 0 : 16); bit--) {
+    for (int bit = 31; bit >= 12; bit--) {
       const uint32_t more = low | 1u << bit;
-      const int n = kTeam == 32 ? __popc(__ballot_sync(0xffffffffu, mine >= more)) : __syncthreads_count(mine >= more);
-      if (n >= k) low = more;
+      if (__syncthreads_count(mine >= more) >= k) low = more;
     }
     if (blocks > 1) {
       const uint32_t part = low;
       exchange(part, [&](uint32_t x) { low = max(low, x); });
     }
-    return low > 1 ? low : 1;
+    return max(low, 1u);
   }
-  // The entries from `least` on to the list of the row's first block (dropped past its room, but counted), by the
-  // threads of a warp for one of them after the other.
-  __device__ int collect(u64 least, u64* list, int cap, int* size) {
+  // The entries from `least` on to the list of the row's first block (dropped past its room, but counted): the groups of
+  // the threads whose own largest is one of them are shared out over the team.
+  __device__ int collect(u64 least, Best<kTeam>& b, int team, int round) {
     const uint32_t low = uint32_t(least >> 32);
-    uint32_t hits = __ballot_sync(0xffffffffu, order_key(own.m) >= low);
-    u64* const to = of_block(list, 0);
-    int* const places = of_block(size, 0);
-    while (hits) {
-      const int who = __ffs(int(hits)) - 1;
-      hits &= hits - 1;
-      for (int g = warp * 32 + who + lane * kTeam; g < groups; g += 32 * kTeam) {
-        float s[kG];
-        floats(fetch(g), s);
+    const float low_score = key_score(low);
+    const bool hit = order_key(own.m) >= low;
+    const uint32_t hits = __ballot_sync(0xffffffffu, hit);
+    int many;
+    if (kTeam == 32) {
+      many = __popc(hits);
+      if (hit) b.who[team][__popc(hits & ((1u << lane) - 1))] = uint16_t(tid);
+      __syncwarp();
+    } else {
+      int place = 0;
+      if (tid == 0) b.hits[team] = 0;
+      __syncthreads();
+      if (lane == 0 && hits) place = atomicAdd(b.hits + team, __popc(hits));
+      place = __shfl_sync(0xffffffffu, place, 0);
+      if (hit) b.who[team][place + __popc(hits & ((1u << lane) - 1))] = uint16_t(tid);
+      __syncthreads();
+      many = b.hits[team];
+    }
+    u64* const to = of_block(b.list[team], 0);
+    int* const places = of_block(b.size[team] + round, 0);
+    const int each_has = (groups + kTeam - 1) / kTeam;  // groups of a thread at most, the first of all as the last of one
+    for (int i = tid; i < many * each_has; i += kTeam) {
+      const int h = i / each_has, at = head + b.who[team][h] + (i - h * each_has) * kTeam;
+      if (at >= groups + head) continue;
+      const int g = at == groups ? 0 : at;
+      const Group<T> v = masked(g);
 #pragma unroll
-        for (int j = 0; j < kG; j++) {
-          const u64 e = entry(order_key(s[j]), lo + g * kG - skip + j);
-          if (e < least) continue;
-          const int place = atomicAdd(places, 1);
-          if (place < cap) to[place] = e;
-        }
+      for (int j = 0; j < kG; j++) {
+        const float s = v.get(j);
+        if (low > 1 && !(s >= low_score)) continue;
+        const u64 e = entry(order_key(s), lo + g * kG - skip + j);
+        if (e < least) continue;
+        const int place = atomicAdd(places, 1);
+        if (place < b.kCap) to[place] = e;
       }
     }
     row_sync();
@@ -106,23 +197,21 @@ struct Search : Row<T, kTeam> {
       team_sync();
       int bin = -1;  // equal entries that follow each other are counted together
       uint32_t run = 0;
-      each_group([&](const float(&s)[kAhead][kG], int g) {
-#pragma unroll 1
-        for (int u = 0; u < kAhead; u++) {
+      for (int g = tid; g < groups; g += kTeam) {
+        const Group<T> v = masked(g);
 #pragma unroll
-          for (int j = 0; j < kG; j++) {
-            const uint32_t key = order_key(s[u][j]);
-            const u64 e = entry(key, lo + (g + u * kTeam) * kG - skip + j);
-            if (!key || (shift < 56 && e >> (shift + 8) != prefix)) continue;
-            const int b = 255 - int((e >> shift) & 255u);
-            if (b != bin) {
-              if (run) atomicAdd(counts + bin, run);
-              bin = b, run = 0;
-            }
-            run++;
+        for (int j = 0; j < kG; j++) {
+          const uint32_t key = order_key(v.get(j));
+          const u64 e = entry(key, lo + g * kG - skip + j);
+          if (!key || (shift < 56 && e >> (shift + 8) != prefix)) continue;
+          const int b = 255 - int((e >> shift) & 255u);
+          if (b != bin) {
+            if (run) atomicAdd(counts + bin, run);
+            bin = b, run = 0;
           }
+          run++;
         }
-      });
+      }
       if (run) atomicAdd(counts + bin, run);
       row_sync();
       // the step in which the k-th lies: a lane has eight, of all blocks
@@ -161,41 +250,44 @@ struct Search : Row<T, kTeam> {
   // the number of larger ones.
   __device__ void order(int m, const u64* list, u64* sorted, int room) {
     if (rank == 0) {
-      if (kTeam == 32) {
-        for (int j = lane; j < m; j += 32) {
-          const u64 e = list[j];
-          int larger = 0;
-          for (int i = 0; i < m; i++) larger += list[i] > e;
-          if (larger < room) sorted[larger] = e;
-        }
-      } else {
-        for (int j = warp; j < m; j += kWarps) {
-          const u64 e = list[j];
-          int larger = 0;
+      for (int j = tid; j < m; j += kTeam) {
+        const u64 e = list[j];
+        int larger = 0;
 #pragma unroll 4
-          for (int i = lane; i < m; i += 32) larger += list[i] > e;
-          larger = __reduce_add_sync(0xffffffffu, larger);
-          if (lane == 0 && larger < room) sorted[larger] = e;
-        }
+        for (int i = 0; i < m; i++) larger += list[i] > e;
+        if (larger < room) sorted[larger] = e;
       }
     }
     team_sync();
   }
   // The best k of the row, in b.sorted of the row's first block; their number.
   __device__ int best(int k, Best<kTeam>& b, int team) {
-    int m = collect(u64(floor_key(k)) << 32, b.list[team], b.kCap, b.size[team]);
-    if (m > b.kCap) m = collect(kth(k, b.counts[team], b.found + team), b.list[team], b.kCap, b.size[team] + 1);
+    int m = collect(u64(floor_key(k, b.counts[team], b.found + team)) << 32, b, team, 0);
+    if (m > b.kCap) m = collect(kth(k, b.counts[team], b.found + team), b, team, 1);
     order(m, b.list[team], b.sorted[team], b.kTop);
     return m < k ? m : k;
   }
 
 };
 
+// Entries of a gradient: w (k1 d + k0), and the same everywhere.
+struct Slope {
+  float m, per, k1, k0;
+  __device__ __forceinline__ float2 operator()(float s0, float s1) const {
+    const float2 d = far2(s0, s1, m, per);
+    return mul2(make_float2(fast_exp2(d.x), fast_exp2(d.y)), fma2(d, make_float2(k1, k1), make_float2(k0, k0)));
+  }
+};
+struct Same {
+  float v;
+  __device__ __forceinline__ float2 operator()(float, float) const { return make_float2(v, v); }
+};
+
 // What a kernel is asked for besides the sums.
 enum Ask { kSums, kTop, kGradient };
 
 template <typename T, int kTeam, int kAsk>
-__global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam) log_probs_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? 2 : kTeam == 128 ? 8 : 4) log_probs_kernel(const __grid_constant__ Args a) {
   __shared__ uint4 scratch[kTeam == 32 ? 1 : 64], slots[2 * kMaxCluster];
   __shared__ std::conditional_t<kAsk == kTop, Best<kTeam>, uint32_t> best;
   const int team = kTeam == 32 ? threadIdx.x >> 5 : 0;
@@ -214,15 +306,13 @@ __global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam) log_probs_kernel(co
   const float dentropy = kAsk == kGradient ? (a.dentropy ? a.dentropy[row] : a.dentropy_all) : 0.f;
   r.per = greedy ? 0.f : fminf(kLog2E / temperature, 3e38f);
 
-  r.begin();
-  r.each_group([&](const auto& s, int) { r.add(s); });
-  if (r.blocks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-  Stat all = r.total();
-  if (all.m == INFINITY) {
-    r.top_infinite = true;
-    r.begin();
-    r.each_group([&](const auto& s, int) { r.add(s); });
+  Stat all;
+  for (bool again = false;; again = true) {
+    r.sum_up();
+    if (!again && r.blocks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     all = r.total();
+    if (all.m < INFINITY) break;
+    r.top_infinite = true;
   }
   const bool empty = all.m == -INFINITY;
   const float log_z = logf(all.s);
@@ -253,34 +343,24 @@ __global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam) log_probs_kernel(co
     if (a.entropy) a.entropy[row] = entropy;
   }
   if constexpr (kAsk == kGradient) {
-    // p (log p + H) and p from l = log2 p
+    // w (k1 d + k0), with p = w / Z and log p = d ln 2 - log Z
     const float per_t = greedy ? 0.f : fminf(__fdiv_rn(1.f, temperature), 3e38f);
     const float da = target < 0 ? 0.f : target >= a.n ? NAN : dlogp;
-    const float k1 = -dentropy * per_t * kLn2, k0 = -per_t * fmaf(dentropy, entropy, da), hit = da * per_t;
-    const float log2_z = empty ? 0.f : log2f(all.s);
-    const float m = empty ? 0.f : all.m;
-    const int at = target >= r.lo && target - r.lo < r.count ? int(target - r.lo) + r.skip : -1;
+    const float inverse = empty ? 0.f : __fdiv_rn(-per_t, all.s), m = empty ? 0.f : all.m, hit = da * per_t;
+    const float k1 = inverse * dentropy * kLn2, k0 = inverse * fmaf(dentropy, entropy - log_z, da);
     const typename Row<T, kTeam>::Out o = r.out(a, row);
-    constexpr int kG = Row<T, kTeam>::kG;
-    r.each_group([&](const auto& s, int g) {
-#pragma unroll
-      for (int u = 0; u < r.kAhead; u++) {
-        const int from = g + u * kTeam;
-        if (from >= r.groups) break;
-        float v[kG];
-#pragma unroll
-        for (int j = 0; j < kG; j++) {
-          const float l = fmaxf((s[u][j] - m) * r.per, kFar) - log2_z;
-          v[j] = fast_exp2(l) * fmaf(l, k1, k0);
-        }
-        if (unsigned(at - from * kG) < unsigned(kG)) {
-#pragma unroll
-          for (int j = 0; j < kG; j++)
-            if (at == from * kG + j && s[u][j] > -INFINITY) v[j] += hit;
-        }
-        r.store(o, from, v);
-      }
-    });
+    if (empty || isnan(da + dentropy)) {
+      r.put(o, Same{empty && !isnan(da + dentropy) ? 0.f : NAN});
+      return;
+    }
+    r.put(o, Slope{m, r.per, k1, k0});
+    // once more where the answer stands
+    r.team_sync();
+    if (r.tid == 0 && target >= r.lo && target - r.lo < r.count) {
+      const int i = int(target - r.lo);
+      const float s = r.value(r.global[i]);
+      if (s > -INFINITY) store_scalar(o.p, o.dtype, i, Slope{m, r.per, k1, k0}(s, s).x + hit);
+    }
   }
 }
 
@@ -294,9 +374,11 @@ const int* fits() {
 
 template <typename T, int kAsk>
 emr_status log_probs(Args a, int sms, cudaStream_t st) {
+  const int least = kAsk != kTop || a.top <= Best<32>::kTop ? 32 : a.top <= Best<128>::kTop ? 128 : 256;
   int cluster;
-  const int team = plan(a, kAsk == kTop && a.top > Best<32>::kTop, sms, fits(), &cluster);
+  const int team = plan(a, least, sizeof(T), sms, fits(), &cluster);
   return team == 32    ? launch_rows(log_probs_kernel<T, 32, kAsk>, a, team, cluster, st)
+         : team == 128 ? launch_rows(log_probs_kernel<T, 128, kAsk>, a, team, cluster, st)
          : team == 256 ? launch_rows(log_probs_kernel<T, 256, kAsk>, a, team, cluster, st)
                        : launch_rows(log_probs_kernel<T, 512, kAsk>, a, team, cluster, st);
 }
