@@ -750,9 +750,9 @@ emr_status emr_sample(const void *scores, int32_t dtype, int32_t rows, int64_t n
 /* Weights as a layer that only answers keeps them: batch matrices [rows][cols] of codes -8 to 7, and one scale (bfloat16)
  * for each `group` (32, 64 or 128) consecutive columns of a row: entry = scale * code. data (device, 16-byte
  * aligned, emr_q4_size bytes): [batch][rows / 16][cols / 128] units (rounded up) of 16 rows x 128 columns, each 1024
- * bytes of codes, held as code + 8, and then the scales. With a row r and a column c of a unit, g = r % 8, s = c / 16, t = c % 16 / 4
- * and j = c % 4: the code is in the 32-bit word at byte r / 8 * 512 + (4 g + t) * 16 + s / 2 * 4, from bit
- * s % 2 * 8 + j / 2 * 4 + j % 2 * 16 on; the scale of group i of the unit is at byte 1024 + g * 512 / group + (r / 8 * 128 / group + i) *
+ * bytes of codes, held as code + 8, and then the scales. With a row r and a column c of a unit, w = c / 32, t = c % 32 / 8 and j = c % 8:
+ * the code is in the 32-bit word at byte r * 64 + t * 16 + w * 4, from bit j / 2 * 4 + j % 2 * 16 on; the scale of group i
+ * of the unit is at byte 1024 + r % 8 * 512 / group + (r / 8 * 128 / group + i) *
  * 2. What lies past rows and cols is 0. Errors of all calls: EMR_ERR_ARG (null or misaligned pointer, size below 1, negative
  * stride, sizes that do not match, unknown type or group), EMR_ERR_RANGE (a size above 2^31 - 256, or more blocks than a launch has),
  * EMR_ERR_CUDA. */

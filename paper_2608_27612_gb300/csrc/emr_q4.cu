@@ -70,8 +70,8 @@ __global__ void __launch_bounds__(256) q4_kernel(const __grid_constant__ Args a)
       if (row < a.rows && g * a.group < a.cols) scale = float(a.scales[b * a.s_batch + row * a.s_row + g * a.s_col]);
     }
     uint32_t w = q4_place(c[0], c[1], c[2], c[3], q4_shift(lane));
-    w |= __shfl_xor_sync(0xffffffffu, w, 4);
-    if (!(lane & 4)) *word = w;
+    w |= __shfl_xor_sync(0xffffffffu, w, 1);
+    if (!(lane & 1)) *word = w;
     if (lane * 4 % a.group == 0) *scale_at = __float2bfloat16_rn(scale);
   }
 }

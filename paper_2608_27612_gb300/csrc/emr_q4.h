@@ -11,10 +11,10 @@
 
 namespace emr {
 
-// Units of 16 rows x 128 columns follow each other along a row of units: 1024 bytes of codes and, for each row, the
-// scales of its 128 / group groups. A lane's 16 bytes of codes are what it feeds to an m16n8k16 instruction: lane 4 g + t
-// has rows g (first 512 bytes) and g + 8, and of step s (16 columns) columns 16 s + 4 t to + 3. A word holds
-// two steps, as pairs of columns 16 bits apart.
+// Units of 16 rows x 128 columns follow each other along a row of units: 1024 bytes of codes, 64 of a row after the
+// other, and, for each row, the scales of its 128 / group groups. A lane's 16 bytes of codes are what it feeds to m16n8k16
+// instructions: lane 4 g + t has rows g and g + 8, and of the w-th 32 columns the word with columns 8 t to 8 t + 7, as pairs
+// of columns 16 bits apart; the order of columns in an instruction is such that x is read as it lies.
 constexpr int kQ4Rows = 16, kQ4Cols = 128, kQ4Codes = 1024;
 
 __host__ __device__ inline int64_t q4_tiles(int64_t rows) { return (rows + kQ4Rows - 1) / kQ4Rows; }
@@ -26,10 +26,8 @@ __host__ __device__ inline int q4_scale_at(int row, int in_block, int group) {
   return kQ4Codes + (row & 7) * q4_scale_pair(group) + ((row >> 3) * (kQ4Cols / group) + in_block) * 2;
 }
 // Byte of the word with columns 4 q to 4 q + 3 of a block (q < 32) of row r, and the first bit of the first pair.
-__host__ __device__ inline int q4_word_at(int row, int q) {
-  return (row >> 3) * 512 + ((row & 7) * 4 + (q & 3)) * 16 + (q >> 3) * 4;
-}
-__host__ __device__ inline int q4_shift(int q) { return (q >> 2 & 1) * 8; }
+__host__ __device__ inline int q4_word_at(int row, int q) { return row * 64 + (q >> 1 & 3) * 16 + (q >> 3) * 4; }
+__host__ __device__ inline int q4_shift(int q) { return (q & 1) * 8; }
 // Four codes in a word: columns 0 and 1 are the first pair, 2 and 3 the second.
 __device__ __forceinline__ uint32_t q4_place(int c0, int c1, int c2, int c3, int shift) {
   return (uint32_t(c0 + 8 & 15) | uint32_t(c1 + 8 & 15) << 16 | uint32_t(c2 + 8 & 15) << 4 | uint32_t(c3 + 8 & 15) << 20) << shift;

@@ -3,12 +3,13 @@
 // y[m][n] = sum over groups g of scale[n][g] (sum over the group's k of code[n][k] x[m][k]): the inner sums are m16n8k16
 // instructions with 16 rows of W as the instruction's rows and rows of x as its 8 columns, exact products with sums in 32
 // bits, and each is scaled and added in 32 bits. Codes become 16-bit floats by one OR and one subtraction for two (128 + q as bfloat16,
-// 1024 + q as float16). A 32-bit x is three bfloat16 parts of 8 bits each, together all of its 24 bits, as
-// three columns. Bound by reading W: half a byte an entry and 2 / group for its scale, once for up to 64 columns. A warp streams its
-// units (16 rows x 128 columns, one piece of memory) into a ring of its own in shared memory by
-// asynchronous copies, six units ahead; x lies in shared memory in the order in which lanes read it. The warps of a block share rows or
-// the contraction; a cluster of up to 8 blocks shares the contraction of long rows and adds its parts through distributed shared memory in
-// the order of blocks.
+// 1024 + q as float16). A 32-bit x is three bfloat16 parts of 8 bits each, together all of its 24 bits, in three columns.
+// Bound by reading W: half a byte an entry and 2 / group for its scale, once for up to 64 columns. x lies in shared memory, as
+// much of a row as there is room for. A warp streams its units (16 rows x 128 columns, one piece of memory) into a
+// ring of its own by asynchronous copies, five units ahead, and waits for no other warp. The warps of a block share rows of W
+// (`wide`) or, where those are few, the contraction (`teams`); a cluster of up to 8 blocks shares the contraction of few
+// rows further and adds its parts through distributed shared memory in the order of blocks. Where rows are many, a
+// warp takes tile after tile.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
@@ -23,20 +24,21 @@ namespace cg = cooperative_groups;
 using namespace emr;
 
 constexpr int kThreads = 256, kWarps = kThreads / 32, kAhead = 6, kMaxCluster = 8;
-constexpr int kRoomX = 32 * 1024;  // of x in shared memory at a time, twice that for more than 16 columns
 
 struct Params {
   const uint8_t* w;
   int64_t w_batch;  // bytes of a matrix, 0 where all share it
-  int32_t unit, tiles, blocks;
+  int32_t tiles, blocks;
   int64_t N, K, M;
   const void* x;
   int64_t x_batch, x_row, x_col;
-  int32_t x_vector;            // four columns are one aligned piece
-  int32_t step;                // rows of x of a block
-  int32_t wide;                // row tiles of a block, each `kR` tiles of 16
-  int32_t chunk, pitch;        // blocks of x in shared memory at a time, and bytes of a column there
-  int32_t row_blocks;          // blocks along the rows of W
+  int32_t x_whole;     // 16 bytes of a row are one aligned piece
+  int32_t step;        // rows of x of a block
+  int32_t wide, teams; // warps that share rows of W, and the contraction: powers of two
+  int32_t log_teams;
+  int32_t chunk;       // blocks of 128 columns whose x is in shared memory at a time
+  int32_t row_blocks;  // blocks along the rows of a matrix, and all of them
+  int32_t all_blocks;
   const float* bias;
   int32_t act;
   void* out;
@@ -45,6 +47,10 @@ struct Params {
 
 __device__ __forceinline__ void copy16(uint32_t to, const void* from) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+// The first `bytes` of them, and zeros.
+__device__ __forceinline__ void copy16(uint32_t to, const void* from, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
 }
 
 template <bool kHalf>
@@ -71,165 +77,266 @@ __device__ __forceinline__ uint32_t codes(uint32_t w) {
   }
   return r;
 }
-// The three parts of a 32-bit value, as bits of bfloat16: each takes the next 8 bits of its fraction. Infinities and NaN are
-// the first part alone.
-__device__ __forceinline__ void parts(float v, uint32_t (&p)[3]) {
-  const uint32_t u = __float_as_uint(v);
-  p[0] = u >> 16, p[1] = p[2] = 0;
-  if ((u & 0x7f800000u) == 0x7f800000u) {
-    if (u & 0x7fffffu) p[0] = 0x7fc0u;
-    return;
-  }
-  const float left = v - __uint_as_float(u & 0xffff0000u);
-  p[1] = __float_as_uint(left) >> 16;
-  p[2] = __float_as_uint(left - __uint_as_float(__float_as_uint(left) & 0xffff0000u)) >> 16;
+// Two values as pairs of bfloat16: a part of each takes the next 8 bits of its fraction. An infinity is the first part
+// alone, a NaN each.
+__device__ __forceinline__ void split(float v0, float v1, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
+  const uint32_t a = __float_as_uint(v0), b = __float_as_uint(v1);
+  hi = __byte_perm(a, b, 0x7632);
+  const float left0 = fabsf(v0) == INFINITY ? 0.f : v0 - __uint_as_float(a & 0xffff0000u);
+  const float left1 = fabsf(v1) == INFINITY ? 0.f : v1 - __uint_as_float(b & 0xffff0000u);
+  const uint32_t c = __float_as_uint(left0), d = __float_as_uint(left1);
+  mid = __byte_perm(c, d, 0x7632);
+  lo = __byte_perm(__float_as_uint(left0 - __uint_as_float(c & 0xffff0000u)), __float_as_uint(left1 - __uint_as_float(d & 0xffff0000u)), 0x7632);
 }
 
 // T: x. kN: tiles of 8 columns. kPer: groups in 128 columns.
 template <typename T, int kN, int kPer>
-__global__ void __launch_bounds__(kThreads, kN <= 2 ? 3 : 1) q4_few_kernel(const __grid_constant__ Params p) {
+__global__ void __launch_bounds__(kThreads, kN <= 2 ? 2 : 1) q4_few_kernel(const __grid_constant__ Params p) {
   constexpr bool kSplit = sizeof(T) == 4, kHalf = std::is_same<T, __half>::value;
+  constexpr int kParts = kSplit ? 3 : 1;
   constexpr int kR = kN >= 4 ? 2 : 1;  // tiles of 16 rows of a warp, which share what is read of x
   constexpr int kUnit = kQ4Codes + 32 * kPer, kStage = kR * kUnit;
   extern __shared__ __align__(16) uint8_t smem[];
   const auto cluster = cg::this_cluster();
   const int shares = int(cluster.num_blocks()), rank = int(cluster.block_rank());
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-  const int wide = p.wide, teams = kWarps / wide, in_rows = warp % wide, team = warp / wide;
-  const int64_t group = blockIdx.x / unsigned(shares);
-  const int64_t b = group / p.row_blocks;
-  const int tile = (int(group % p.row_blocks) * wide + in_rows) * kR;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+  const int wide = p.wide, teams = p.teams, in_rows = warp & (wide - 1), team = warp >> (3 - p.log_teams);
   const int64_t m0 = int64_t(blockIdx.y) * p.step;
-  const int rows = int(p.M - m0 < p.step ? p.M - m0 : p.step), columns = kSplit ? 3 * rows : rows;
-  const int first = int(int64_t(p.blocks) * rank / shares), last = int(int64_t(p.blocks) * (rank + 1) / shares);
+  const int rows = int(p.M - m0 < p.step ? p.M - m0 : p.step), columns = kParts * rows;
+  const int first = shares == 1 ? 0 : int(unsigned(p.blocks) * unsigned(rank) / unsigned(shares));
+  const int last = shares == 1 ? p.blocks : int(unsigned(p.blocks) * unsigned(rank + 1) / unsigned(shares));
+  // blocks of rows of the block, one after the other
+  const unsigned here = shares == 1 ? blockIdx.x : blockIdx.x / unsigned(shares), grid = shares == 1 ? gridDim.x : gridDim.x / unsigned(shares);
+  const int from = int(grid == unsigned(p.all_blocks) ? here : unsigned(uint64_t(p.all_blocks) * here / grid));
+  const int past = int(grid == unsigned(p.all_blocks) ? here + 1 : unsigned(uint64_t(p.all_blocks) * (here + 1) / grid));
 
+  const int pitch = p.chunk * 256 + 64;  // of a column of x, in bytes: its 16-bit values, and other banks than the one before
   uint8_t* const ring = smem + warp * (kAhead * kStage);
   uint8_t* const xs = smem + kWarps * kAhead * kStage;
-  const uint32_t ring_at = uint32_t(__cvta_generic_to_shared(ring));
-  const uint8_t* const w = p.w + b * p.w_batch + int64_t(tile) * p.blocks * kUnit;
+  const uint32_t ring_at = uint32_t(__cvta_generic_to_shared(ring)) + lane * 16, xs_at = uint32_t(__cvta_generic_to_shared(xs));
 
-  // unit after unit of the warp's share, each kR tiles
-  const int own = first + team < last ? (last - first - team + teams - 1) / teams : 0;
-  const int mine = tile < p.tiles ? own : 0;
-  const auto fetch = [&](int i) {
-    if (i < mine) {
-      const int kb = first + team + i * teams;
-      const uint32_t to = ring_at + i % kAhead * kStage;
+  // the warp's part of the chunk that begins with block c: of teams as many
+  const auto part_of = [&](int c, int team) { return c + ((last - c < p.chunk ? last - c : p.chunk) * team >> p.log_teams); };
+  // The stream of its units, by blocks of rows, chunks and blocks of columns.
+  int s_block = from, s_b = p.row_blocks == p.all_blocks ? 0 : from / p.row_blocks, s_row = from - s_b * p.row_blocks;
+  const int s_first_b = s_b;
+  int s_chunk = first, s_kb = 0, s_end = 0, s_stage = 0, s_tiles = 0;
+  const uint8_t* s_unit = nullptr;
+  const auto seek = [&] {  // to the next part that is not empty
+    while (s_kb == s_end && s_block < past) {
+      const int tile = (s_row * wide + in_rows) * kR;
+      s_tiles = p.tiles - tile;
+      s_kb = part_of(s_chunk, team), s_end = s_tiles > 0 ? part_of(s_chunk, team + 1) : s_kb;
+      s_unit = p.w + s_b * p.w_batch + (int64_t(tile) * p.blocks + s_kb) * kUnit + lane * 16;
+      s_chunk += p.chunk;
+      if (s_chunk >= last) {
+        s_chunk = first, s_block++;
+        if (++s_row == p.row_blocks) s_row = 0, s_b++;
+      }
+    }
+  };
+  const auto issue = [&] {
+    if (s_kb < s_end) {
 #pragma unroll
       for (int r = 0; r < kR; r++) {
-        if (r && tile + r >= p.tiles) break;
-        const uint8_t* const from = w + (int64_t(r) * p.blocks + kb) * kUnit;
-#pragma unroll
-        for (int o = 0; o < kQ4Codes; o += 512) copy16(to + r * kUnit + o + lane * 16, from + o + lane * 16);
-        if (lane < 2 * kPer) copy16(to + r * kUnit + kQ4Codes + lane * 16, from + kQ4Codes + lane * 16);
+        if (r && r >= s_tiles) break;
+        const uint8_t* const unit = s_unit + int64_t(r) * p.blocks * kUnit;
+        const uint32_t to = ring_at + s_stage * kStage + r * kUnit;
+        copy16(to, unit);
+        copy16(to + 512, unit + 512);
+        if (lane < 2 * kPer) copy16(to + kQ4Codes, unit + kQ4Codes);
       }
+      s_stage = s_stage == kAhead - 1 ? 0 : s_stage + 1;
+      s_unit += kUnit;
+      if (++s_kb == s_end) seek();
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  for (int i = 0; i < kAhead - 1; i++) fetch(i);
+  seek();
+#pragma unroll 1
+  for (int i = 0; i < kAhead - 1; i++) issue();
 
-  float sum[kR][kN][4];
-#pragma unroll
-  for (int r = 0; r < kR; r++)
-#pragma unroll
-    for (int n = 0; n < kN; n++)
-#pragma unroll
-      for (int j = 0; j < 4; j++) sum[r][n][j] = 0.f;
-
-  const T* const x = static_cast<const T*>(p.x) + b * p.x_batch + m0 * p.x_row;
-  int i = 0;
-  for (int from = first; from < last; from += p.chunk) {
-    const int size = last - from < p.chunk ? last - from : p.chunk;
-    // x of the chunk: four columns a thread, [column of the instruction][block][two steps][t][step][4]
-    __syncthreads();
-    for (int at = threadIdx.x; at < rows * size * 32; at += kThreads) {
-      const int q = at % (size * 32), m = at / (size * 32);
-      const int64_t k = int64_t(from) * kQ4Cols + q * 4;
-      Four<T> v;
-      const T* const source = x + m * p.x_row + k * p.x_col;
-      if (p.x_vector && k + 4 <= p.K) {
-        v.u = *reinterpret_cast<const decltype(v.u)*>(source);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; j++) v.set(j, k + j < p.K ? source[j * p.x_col] : T(0.f));
+  // x of a chunk: a thread's pieces of 16 bytes, as they lie or, if that cannot be, four at a time through registers
+  const auto stage_x = [&](int b, int c) {
+    constexpr int kPiece = kSplit ? 4 : 8;
+    const int per_row = (last - c < p.chunk ? last - c : p.chunk) * (kQ4Cols / kPiece);
+    const int64_t k0 = int64_t(c) * kQ4Cols;
+    const T* const x = static_cast<const T*>(p.x) + b * p.x_batch + m0 * p.x_row + k0 * p.x_col;
+    const int log_rows = rows > 4 ? 3 : rows > 2 ? 2 : rows > 1 ? 1 : 0, apart = 32 << (3 - log_rows);  // warps of a row: 8, 4, 2 or 1
+    for (int m = warp & ((1 << log_rows) - 1); m < rows; m += 1 << log_rows) {
+      const T* const row = x + m * p.x_row;
+      const int have = int(p.K - k0 < int64_t(per_row) * kPiece ? p.K - k0 : int64_t(per_row) * kPiece);
+      int i = lane + (warp >> log_rows) * 32;
+      if (!kSplit && p.x_whole) {
+        uint32_t to = xs_at + m * pitch + i * 16;
+        for (; i < per_row; i += apart, to += apart * 16) {
+          const int left = have - i * 8;
+          copy16(to, left > 0 ? row + i * 8 : row, left >= 8 ? 16 : left > 0 ? left * 2 : 0);
+        }
+        continue;
       }
-      const int s = q >> 2 & 7;
-      uint8_t* const to = xs + (q >> 5) * 256 + (s >> 1) * 64 + (q & 3) * 16 + (s & 1) * 8;
-      if constexpr (kSplit) {
-        uint32_t e[4][3];
-        parts(v.u.x, e[0]), parts(v.u.y, e[1]), parts(v.u.z, e[2]), parts(v.u.w, e[3]);
+#pragma unroll 1
+      for (; i < per_row; i += 4 * apart) {
+        uint4 piece[4];
 #pragma unroll
-        for (int c = 0; c < 3; c++) *reinterpret_cast<uint2*>(to + (c * rows + m) * p.pitch) = make_uint2(e[0][c] | e[1][c] << 16, e[2][c] | e[3][c] << 16);
-      } else {
-        *reinterpret_cast<uint2*>(to + m * p.pitch) = v.u;
-      }
-    }
-    __syncthreads();
-    for (; i < mine && first + team + i * teams < from + size; i++) {
-      fetch(i + kAhead - 1);
-      asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
-      __syncwarp();
-      const uint8_t* const unit = ring + i % kAhead * kStage;
-      const uint8_t* const x_at = xs + (first + team + i * teams - from) * 256 + t * 16 + g * p.pitch;
-      uint4 code[kR][2];
-      float scale[kR][2 * kPer];
+        for (int u = 0; u < 4; u++) {
+          const int at = (i + u * apart) * kPiece, left = have - at;
+          const T* const from = row + at * p.x_col;
+          if (p.x_whole && left >= kPiece) {
+            piece[u] = *reinterpret_cast<const uint4*>(from);
+          } else {
+            T* const v = reinterpret_cast<T*>(piece + u);
 #pragma unroll
-      for (int r = 0; r < kR; r++) {
-        code[r][0] = *reinterpret_cast<const uint4*>(unit + r * kUnit + lane * 16);
-        code[r][1] = *reinterpret_cast<const uint4*>(unit + r * kUnit + 512 + lane * 16);
-        uint32_t pair[kPer];
-        const uint8_t* const at = unit + r * kUnit + kQ4Codes + g * 4 * kPer;
-#pragma unroll
-        for (int j = 0; j < kPer; j++) pair[j] = reinterpret_cast<const uint32_t*>(at)[j];
-#pragma unroll
-        for (int j = 0; j < 2 * kPer; j++) scale[r][j] = __uint_as_float(j & 1 ? pair[j >> 1] & 0xffff0000u : pair[j >> 1] << 16);
-      }
-#pragma unroll
-      for (int c = 0; c < kPer; c++) {
-        float part[kR][kN][4];
-#pragma unroll
-        for (int r = 0; r < kR; r++)
-#pragma unroll
-          for (int n = 0; n < kN; n++)
-#pragma unroll
-            for (int j = 0; j < 4; j++) part[r][n][j] = 0.f;
-#pragma unroll
-        for (int v = c * (4 / kPer); v < (c + 1) * (4 / kPer); v++) {  // two steps
-          uint32_t a[2][kR][4];
-#pragma unroll
-          for (int r = 0; r < kR; r++) {
-            const uint32_t lo = (&code[r][0].x)[v], hi = (&code[r][1].x)[v];
-#pragma unroll
-            for (int h = 0; h < 2; h++) {
-              a[h][r][0] = codes<kHalf>(lo >> (8 * h)), a[h][r][1] = codes<kHalf>(hi >> (8 * h));
-              a[h][r][2] = codes<kHalf>(lo >> (8 * h + 4)), a[h][r][3] = codes<kHalf>(hi >> (8 * h + 4));
-            }
-          }
-#pragma unroll
-          for (int n = 0; n < kN; n++) {
-            uint4 e = make_uint4(0, 0, 0, 0);
-            if (n * 8 + g < columns) e = *reinterpret_cast<const uint4*>(x_at + v * 64 + n * 8 * p.pitch);
-#pragma unroll
-            for (int r = 0; r < kR; r++) {
-              mma<kHalf>(part[r][n], a[0][r], e.x, e.y);
-              mma<kHalf>(part[r][n], a[1][r], e.z, e.w);
-            }
+            for (int j = 0; j < kPiece; j++) v[j] = j < left ? from[j * p.x_col] : T(0.f);
           }
         }
 #pragma unroll
-        for (int r = 0; r < kR; r++)
+        for (int u = 0; u < 4; u++) {
+          if (i + u * apart >= per_row) break;
+          uint8_t* const to = xs + m * pitch + (i + u * apart) * (kPiece * 2);
+          if constexpr (kSplit) {
+            uint2 part[3];
+            split(__uint_as_float(piece[u].x), __uint_as_float(piece[u].y), part[0].x, part[1].x, part[2].x);
+            split(__uint_as_float(piece[u].z), __uint_as_float(piece[u].w), part[0].y, part[1].y, part[2].y);
 #pragma unroll
-          for (int n = 0; n < kN; n++)
+            for (int q = 0; q < 3; q++) *reinterpret_cast<uint2*>(to + q * rows * pitch) = part[q];
+          } else {
+            *reinterpret_cast<uint4*>(to) = piece[u];
+          }
+        }
+      }
+    }
+    asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
+  };
+
+  float sum[kR][kN][4];
+  const auto clear = [&] {
 #pragma unroll
-            for (int j = 0; j < 4; j++) sum[r][n][j] = fmaf(scale[r][(j >> 1) * kPer + c], part[r][n][j], sum[r][n][j]);
+    for (int r = 0; r < kR; r++)
+#pragma unroll
+      for (int n = 0; n < kN; n++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) sum[r][n][j] = 0.f;
+  };
+  clear();
+  // Output (m, n0 + n) of matrix b, at `at` + m N + n, from what `of` gives for its columns.
+  const auto finish = [&](int b, int64_t n0, int64_t at, int m, int n, auto of) {
+    if (n0 + n >= p.N) return;
+    float z[1] = {of(m)}, d[1];
+#pragma unroll
+    for (int c = 1; c < kParts; c++) z[0] += of(c * rows + m);
+    if (p.bias) z[0] += p.bias[b * p.N + n0 + n];
+    activate<1, false>(p.act, z, d);
+    store_scalar(p.out, p.out_dtype, at + m * p.N + n, z[0]);
+  };
+  // A warp's sums: [column][row].
+  float* const own = reinterpret_cast<float*>(xs + columns * pitch) + warp * (kR * kN * 128);
+
+  int stage = 0;
+  int64_t staged = -1;  // whose x is there
+  int b = s_first_b, row_block = from - b * p.row_blocks;
+  for (int block = from; block < past; block++) {
+    const int tile = (row_block * wide + in_rows) * kR;
+    for (int c = first; c < last; c += p.chunk) {
+      const int64_t wanted = (p.x_batch ? int64_t(b) * p.blocks : 0) + c;
+      if (wanted != staged) {
+        if (staged >= 0) __syncthreads();
+        stage_x(b, c);
+        __syncthreads();
+        staged = wanted;
+      }
+      const int end = tile < p.tiles ? part_of(c, team + 1) : 0;
+      for (int kb = part_of(c, team); kb < end; kb++) {
+        issue();
+        asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
+        __syncwarp();
+        const uint8_t* const unit = ring + stage * kStage;
+        const uint8_t* const e_from = xs + (kb - c) * 256 + t * 16 + g * pitch;
+        stage = stage == kAhead - 1 ? 0 : stage + 1;
+        uint4 code[kR][2];
+        float scale[kR][2 * kPer];
+#pragma unroll
+        for (int r = 0; r < kR; r++) {
+          code[r][0] = *reinterpret_cast<const uint4*>(unit + r * kUnit + lane * 16);
+          code[r][1] = *reinterpret_cast<const uint4*>(unit + r * kUnit + 512 + lane * 16);
+          uint32_t pair[kPer];
+          const uint8_t* const at = unit + r * kUnit + kQ4Codes + g * 4 * kPer;
+#pragma unroll
+          for (int j = 0; j < kPer; j++) pair[j] = reinterpret_cast<const uint32_t*>(at)[j];
+#pragma unroll
+          for (int j = 0; j < 2 * kPer; j++) scale[r][j] = __uint_as_float(j & 1 ? pair[j >> 1] & 0xffff0000u : pair[j >> 1] << 16);
+        }
+#pragma unroll
+        for (int q = 0; q < kPer; q++) {
+          constexpr int kChains = kN == 1 ? 2 : 1;  // sums that do not wait for one another
+          float part[kChains][kR][kN][4];
+#pragma unroll
+          for (int h = 0; h < kChains; h++)
+#pragma unroll
+            for (int r = 0; r < kR; r++)
+#pragma unroll
+              for (int n = 0; n < kN; n++)
+#pragma unroll
+                for (int j = 0; j < 4; j++) part[h][r][n][j] = 0.f;
+#pragma unroll
+          for (int v = q * (4 / kPer); v < (q + 1) * (4 / kPer); v++) {  // 32 columns: two steps of 16
+            uint32_t a[2][kR][4];
+#pragma unroll
+            for (int r = 0; r < kR; r++) {
+              const uint32_t lo = (&code[r][0].x)[v], hi = (&code[r][1].x)[v];
+#pragma unroll
+              for (int h = 0; h < 2; h++) {
+                a[h][r][0] = codes<kHalf>(lo >> (8 * h)), a[h][r][1] = codes<kHalf>(hi >> (8 * h));
+                a[h][r][2] = codes<kHalf>(lo >> (8 * h + 4)), a[h][r][3] = codes<kHalf>(hi >> (8 * h + 4));
+              }
+            }
+#pragma unroll
+            for (int n = 0; n < kN; n++) {
+              uint4 e = make_uint4(0, 0, 0, 0);
+              if (n * 8 + g < columns) e = *reinterpret_cast<const uint4*>(e_from + v * 64 + n * 8 * pitch);
+#pragma unroll
+              for (int r = 0; r < kR; r++) {
+                mma<kHalf>(part[0][r][n], a[0][r], e.x, e.y);
+                mma<kHalf>(part[kChains - 1][r][n], a[1][r], e.z, e.w);
+              }
+            }
+          }
+#pragma unroll
+          for (int r = 0; r < kR; r++)
+#pragma unroll
+            for (int n = 0; n < kN; n++)
+#pragma unroll
+              for (int j = 0; j < 4; j++) {
+                const float all = kChains == 2 ? part[0][r][n][j] + part[kChains - 1][r][n][j] : part[0][r][n][j];
+                sum[r][n][j] = fmaf(scale[r][(j >> 1) * kPer + q], all, sum[r][n][j]);
+              }
+        }
+        __syncwarp();
+      }
+    }
+    if (teams == 1 && shares == 1 && tile < p.tiles) {  // a warp's own outputs
+#pragma unroll
+      for (int r = 0; r < kR; r++)
+#pragma unroll
+        for (int n = 0; n < kN; n++)
+#pragma unroll
+          for (int j = 0; j < 4; j++) own[(n * 8 + 2 * t + (j & 1)) * (kR * 16) + r * 16 + g + 8 * (j >> 1)] = sum[r][n][j];
+      __syncwarp();
+      const int64_t n0 = int64_t(tile) * 16, at = (b * p.M + m0) * p.N + n0;
+      for (int i = lane; i < rows * kR * 16; i += 32) {
+        const int n = i % (kR * 16);
+        finish(b, n0, at, i / (kR * 16), n, [&](int column) { return own[column * (kR * 16) + n]; });
       }
       __syncwarp();
+      clear();
     }
+    if (++row_block == p.row_blocks) row_block = 0, b++;
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
-  __syncthreads();
+  if (teams == 1 && shares == 1) return;
 
-  // the warps' sums: [team][column][row of the block]; then those of the blocks of the cluster
+  // one block of rows: the warps' sums, [team][column][row of the block]; then those of the blocks of the cluster
+  __syncthreads();
   float* const sums = reinterpret_cast<float*>(smem);
   const int tall = wide * kR * 16, room = kN * 8 * tall;
 #pragma unroll
@@ -240,33 +347,34 @@ __global__ void __launch_bounds__(kThreads, kN <= 2 ? 3 : 1) q4_few_kernel(const
       for (int j = 0; j < 4; j++)
         sums[team * room + (n * 8 + 2 * t + (j & 1)) * tall + (in_rows * kR + r) * 16 + g + 8 * (j >> 1)] = sum[r][n][j];
   __syncthreads();
-  const int n0 = int(group % p.row_blocks) * tall;
-  const int here = p.N - n0 < tall ? int(p.N - n0) : tall;
-  const int outs = rows * tall;
+  const int64_t n0 = int64_t(from - s_first_b * p.row_blocks) * tall, out_at = (s_first_b * p.M + m0) * p.N + n0;
+  const int log_tall = __ffs(tall) - 1;
   if (shares > 1) {
-    for (int at = threadIdx.x; at < columns * tall; at += kThreads) {
+    for (int at = tid; at < columns * tall; at += kThreads) {
       float v = sums[at];
       for (int i = 1; i < teams; i++) v += sums[i * room + at];
       sums[at] = v;
     }
     cluster.sync();
-  }
-  const int many = shares > 1 ? shares : teams;
-  for (int at = threadIdx.x + (shares > 1 ? rank * kThreads : 0); at < outs; at += kThreads * (shares > 1 ? shares : 1)) {
-    const int n = at % tall, m = at / tall;
-    if (n >= here) continue;
-    float z[1] = {0.f}, d[1];
-    for (int c = 0; c < (kSplit ? 3 : 1); c++) {
-      float part = 0.f;
-      for (int i = 0; i < many; i++)
-        part += shares > 1 ? cluster.map_shared_rank(sums, i)[c * outs + at] : sums[i * room + c * outs + at];
-      z[0] += part;
+    for (int at = rank * kThreads + tid; at < rows * tall; at += kThreads * shares) {
+      const int n = at & (tall - 1);
+      finish(s_first_b, n0, out_at, at >> log_tall, n, [&](int column) {
+        float v = 0.f;
+        for (int i = 0; i < shares; i++) v += cluster.map_shared_rank(sums, i)[column * tall + n];
+        return v;
+      });
     }
-    if (p.bias) z[0] += p.bias[b * p.N + n0 + n];
-    activate<1, false>(p.act, z, d);
-    store_scalar(p.out, p.out_dtype, (b * p.M + m0 + m) * p.N + n0 + n, z[0]);
+    cluster.sync();  // a block's sums are read by the others
+  } else {
+    for (int at = tid; at < rows * tall; at += kThreads) {
+      const int n = at & (tall - 1);
+      finish(s_first_b, n0, out_at, at >> log_tall, n, [&](int column) {
+        float v = 0.f;
+        for (int i = 0; i < teams; i++) v += sums[i * room + column * tall + n];
+        return v;
+      });
+    }
   }
-  if (shares > 1) cluster.sync();  // a block's sums are read by the others
 }
 
 template <typename T, int kN, int kPer>
@@ -295,30 +403,48 @@ emr_status launch(const Params& p, int per, int64_t blocks, int shares, size_t s
 
 template <typename T>
 emr_status plan(Params p, int64_t batch, int per, int dev, int sms, cudaStream_t st) {
-  constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
-  const int64_t most = 64 / kParts;
-  const int64_t pieces = (p.M + most - 1) / most;
-  p.step = int((p.M + pieces - 1) / pieces);
-  const int columns = p.step * kParts, tiles8 = (columns + 7) / 8;
-  const int kn = tiles8 <= 1 ? 1 : tiles8 <= 2 ? 2 : tiles8 <= 4 ? 4 : 8, kr = kn >= 4 ? 2 : 1;
-  // Rows of a block: x is read by every block, so that its bytes should stay a quarter of the weights'
-  int wide = 1;
-  while (wide < kWarps && int64_t(p.step) * int(sizeof(T)) * 4 > int64_t(wide) * kr * 8) wide *= 2;
-  while (wide > 1 && (p.tiles + wide * kr - 1) / (wide * kr) * batch < sms / 4) wide /= 2;
-  p.wide = wide;
-  p.row_blocks = (p.tiles + wide * kr - 1) / (wide * kr);
-  const int64_t blocks = batch * p.row_blocks;
+  constexpr int kParts = sizeof(T) == 4 ? 3 : 1, kMost = 64 / kParts;
+  const int64_t chunks = (p.M + kMost - 1) / kMost;
+  if (chunks > 65535) return EMR_ERR_RANGE;
+  p.step = int((p.M + chunks - 1) / chunks);
+  const int columns = p.step * kParts, kn = columns <= 8 ? 1 : columns <= 16 ? 2 : columns <= 32 ? 4 : 8, kr = kn >= 4 ? 2 : 1;
+  const int64_t row_tiles = (p.tiles + kr - 1) / kr;
+  const size_t unit = kQ4Codes + 32 * per, ring = size_t(kWarps) * kAhead * kr * unit, sums = size_t(kWarps) * kr * 16 * kn * 8 * 4;
+  // x: beside the rings, in half an SM's shared memory where two blocks share it
+  const size_t most = kn <= 2 ? 110 * 1024 : kMostSmem, room = most - ring;
+  const int fit = int((room - columns * 64) / (size_t(columns) * 256)), fit_direct = int((room - sums - columns * 64) / (size_t(columns) * 256));
+  int64_t blocks;
   int shares = 1;
-  for (int s = 2; s <= kMaxCluster; s++)
-    if (blocks * s <= 2 * sms && p.blocks / s >= 2 * (kWarps / wide)) shares = s;
-  const int share = (p.blocks + shares - 1) / shares;
-  int chunk = (kn > 2 ? 2 : 1) * kRoomX / (columns * 256);
-  chunk = chunk < 1 ? 1 : chunk > share ? share : chunk;
-  p.chunk = chunk, p.pitch = chunk * 256 + 64;
-  const size_t ring = size_t(kWarps) * kAhead * kr * p.unit, sums = size_t(kWarps) * kr * 16 * kn * 8 * 4;
-  size_t smem = ring + size_t(columns) * p.pitch;
+  if (p.blocks <= fit_direct && batch * chunks * row_tiles >= kWarps * sms) {
+    // enough tiles for every warp of an SM: each takes its own, two blocks an SM
+    p.wide = kWarps, p.teams = 1, p.chunk = p.blocks;
+    p.row_blocks = int((row_tiles + kWarps - 1) / kWarps);
+    const int64_t all = batch * p.row_blocks;
+    if (all > INT32_MAX) return EMR_ERR_RANGE;
+    p.all_blocks = int32_t(all);
+    const int64_t room_for = (kn <= 2 ? 2 : 1) * sms / chunks;
+    blocks = p.all_blocks < room_for || room_for < 1 ? p.all_blocks : room_for;
+  } else {
+    // every block reads x: rows of W enough that x is at most half as many bytes
+    int wide = 1;
+    while (wide < kWarps && p.step * int(sizeof(T)) > wide * kr * 4) wide *= 2;
+    p.wide = wide, p.teams = kWarps / wide;
+    p.row_blocks = int((row_tiles + wide - 1) / wide);
+    blocks = batch * p.row_blocks;
+    if (blocks > INT32_MAX) return EMR_ERR_RANGE;
+    p.all_blocks = int32_t(blocks);
+    const int at_once = (kn <= 2 ? 2 : 1) * sms;
+    for (int s = 2; s <= kMaxCluster; s++)
+      if (blocks * s * chunks <= at_once && p.blocks / (s * p.teams) >= 2) shares = s;
+    const int share = (p.blocks + shares - 1) / shares;
+    const int some = p.teams == 1 ? fit_direct : fit, parts = (share + some - 1) / some;
+    p.chunk = (share + parts - 1) / parts;
+  }
+  if (blocks * shares > INT32_MAX) return EMR_ERR_RANGE;
+  for (p.log_teams = 0; (1 << p.log_teams) < p.teams;) p.log_teams++;
+  const bool own = p.teams == 1 && shares == 1;
+  size_t smem = ring + size_t(columns) * (p.chunk * 256 + 64) + (own ? sums : 0);
   if (smem < sums) smem = sums;
-  if (blocks * shares > INT32_MAX || (p.M + p.step - 1) / p.step > 65535) return EMR_ERR_RANGE;
   return kn == 1   ? launch<T, 1>(p, per, blocks, shares, smem, dev, st)
          : kn == 2 ? launch<T, 2>(p, per, blocks, shares, smem, dev, st)
          : kn == 4 ? launch<T, 4>(p, per, blocks, shares, smem, dev, st) : launch<T, 8>(p, per, blocks, shares, smem, dev, st);
@@ -341,14 +467,14 @@ extern "C" emr_status emr_q4_matmul(const void* x, int32_t dtype, int32_t x_batc
   int dev = 0, sms = 0;
   if (!device_sms(&dev, &sms)) return EMR_ERR_CUDA;
   Params p{};
-  p.w = w->data, p.unit = q4_unit(w->group), p.tiles = int32_t(q4_tiles(w->rows)), p.blocks = int32_t(q4_blocks(w->cols));
-  p.w_batch = w->batch == 1 ? 0 : int64_t(p.tiles) * p.blocks * p.unit;
+  p.w = w->data, p.tiles = int32_t(q4_tiles(w->rows)), p.blocks = int32_t(q4_blocks(w->cols));
+  p.w_batch = w->batch == 1 ? 0 : int64_t(p.tiles) * p.blocks * q4_unit(w->group);
   p.N = w->rows, p.K = w->cols, p.M = rows;
   p.x = x, p.x_batch = x_batch == 1 ? 0 : batch_stride, p.x_row = row_stride, p.x_col = col_stride;
   const int64_t batch = x_batch > w->batch ? x_batch : w->batch;
-  const int piece = 4 * dtype_bytes(dtype);
-  p.x_vector = col_stride == 1 && reinterpret_cast<uintptr_t>(x) % piece == 0 && (rows == 1 || row_stride % 4 == 0) &&
-               (x_batch == 1 || batch_stride % 4 == 0);
+  const int piece = 16 / dtype_bytes(dtype);
+  p.x_whole = col_stride == 1 && reinterpret_cast<uintptr_t>(x) % 16 == 0 && (rows == 1 || row_stride % piece == 0) &&
+              (x_batch == 1 || batch_stride % piece == 0);
   p.bias = bias, p.act = act, p.out = out, p.out_dtype = out_dtype;
   const int per = kQ4Cols / w->group;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
