@@ -33,6 +33,35 @@ __device__ __forceinline__ uint32_t q4_place(int c0, int c1, int c2, int c3, int
   return (uint32_t(c0 + 8 & 15) | uint32_t(c1 + 8 & 15) << 16 | uint32_t(c2 + 8 & 15) << 4 | uint32_t(c3 + 8 & 15) << 20) << shift;
 }
 
+// Two 32-bit values as pairs of bfloat16: a part of each takes the next 8 bits of its fraction. An infinity is the first part
+// alone, a NaN each.
+__device__ __forceinline__ void split_pair(float v0, float v1, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
+  const uint32_t a = __float_as_uint(v0), b = __float_as_uint(v1);
+  hi = __byte_perm(a, b, 0x7632);
+  const float left0 = fabsf(v0) == INFINITY ? 0.f : v0 - __uint_as_float(a & 0xffff0000u);
+  const float left1 = fabsf(v1) == INFINITY ? 0.f : v1 - __uint_as_float(b & 0xffff0000u);
+  const uint32_t c = __float_as_uint(left0), d = __float_as_uint(left1);
+  mid = __byte_perm(c, d, 0x7632);
+  lo = __byte_perm(__float_as_uint(left0 - __uint_as_float(c & 0xffff0000u)), __float_as_uint(left1 - __uint_as_float(d & 0xffff0000u)), 0x7632);
+}
+
+// A product as the caller described it. whole: 16 bytes of a row of x are one aligned piece.
+struct Q4Product {
+  const emr_q4* w;
+  const void* x;
+  int32_t dtype, x_batch;
+  int64_t rows, batch_stride, row_stride, col_stride;
+  bool whole;
+  const float* bias;
+  int32_t act;
+  void* out;
+  int32_t out_dtype;
+};
+// Whether it is one for the kernel of many rows (emr_q4_many.cu), the bytes that that needs, and its launch.
+inline bool q4_is_many(const Q4Product& a) { return a.rows > (a.dtype == EMR_F32 ? 8 : 16); }
+size_t q4_many_room(const Q4Product& a);
+emr_status launch_q4_many(const Q4Product& a, void* ws, int dev, int sms, cudaStream_t st);
+
 inline bool q4_ok(const emr_q4* q) {
   return q && q->batch > 0 && q->rows > 0 && q->cols > 0 && q->rows <= kQ8MaxDim && q->cols <= kQ8MaxDim &&
          (q->group == 32 || q->group == 64 || q->group == 128) && q->data && reinterpret_cast<uintptr_t>(q->data) % 16 == 0;

@@ -77,18 +77,6 @@ __device__ __forceinline__ uint32_t codes(uint32_t w) {
   }
   return r;
 }
-// Two values as pairs of bfloat16: a part of each takes the next 8 bits of its fraction. An infinity is the first part
-// alone, a NaN each.
-__device__ __forceinline__ void split(float v0, float v1, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
-  const uint32_t a = __float_as_uint(v0), b = __float_as_uint(v1);
-  hi = __byte_perm(a, b, 0x7632);
-  const float left0 = fabsf(v0) == INFINITY ? 0.f : v0 - __uint_as_float(a & 0xffff0000u);
-  const float left1 = fabsf(v1) == INFINITY ? 0.f : v1 - __uint_as_float(b & 0xffff0000u);
-  const uint32_t c = __float_as_uint(left0), d = __float_as_uint(left1);
-  mid = __byte_perm(c, d, 0x7632);
-  lo = __byte_perm(__float_as_uint(left0 - __uint_as_float(c & 0xffff0000u)), __float_as_uint(left1 - __uint_as_float(d & 0xffff0000u)), 0x7632);
-}
-
 // T: x. kN: tiles of 8 columns. kPer: groups in 128 columns.
 template <typename T, int kN, int kPer>
 __global__ void __launch_bounds__(kThreads, kN <= 2 ? 2 : 1) q4_few_kernel(const __grid_constant__ Params p) {
@@ -196,8 +184,8 @@ __global__ void __launch_bounds__(kThreads, kN <= 2 ? 2 : 1) q4_few_kernel(const
           uint8_t* const to = xs + m * pitch + (i + u * apart) * (kPiece * 2);
           if constexpr (kSplit) {
             uint2 part[3];
-            split(__uint_as_float(piece[u].x), __uint_as_float(piece[u].y), part[0].x, part[1].x, part[2].x);
-            split(__uint_as_float(piece[u].z), __uint_as_float(piece[u].w), part[0].y, part[1].y, part[2].y);
+            split_pair(__uint_as_float(piece[u].x), __uint_as_float(piece[u].y), part[0].x, part[1].x, part[2].x);
+            split_pair(__uint_as_float(piece[u].z), __uint_as_float(piece[u].w), part[0].y, part[1].y, part[2].y);
 #pragma unroll
             for (int q = 0; q < 3; q++) *reinterpret_cast<uint2*>(to + q * rows * pitch) = part[q];
           } else {
@@ -450,34 +438,61 @@ emr_status plan(Params p, int64_t batch, int per, int dev, int sms, cudaStream_t
          : kn == 4 ? launch<T, 4>(p, per, blocks, shares, smem, dev, st) : launch<T, 8>(p, per, blocks, shares, smem, dev, st);
 }
 
-}  // namespace
-
-extern "C" emr_status emr_q4_matmul(const void* x, int32_t dtype, int32_t x_batch, int64_t rows, int64_t batch_stride, int64_t row_stride,
-                                    int64_t col_stride, const emr_q4* w, const float* bias, int32_t act, void* out, int32_t out_dtype,
-                                    void* stream) {
-  if (!q4_ok(w) || !x || !out || rows < 1 || x_batch < 1 || (x_batch != 1 && w->batch != 1 && x_batch != w->batch) || !dtype_ok(dtype) ||
-      !dtype_ok(out_dtype) || batch_stride < 0 || row_stride < 0 || col_stride < 0 || act < EMR_ACT_IDENTITY || act > EMR_ACT_ABS ||
-      reinterpret_cast<uintptr_t>(x) % dtype_bytes(dtype) || reinterpret_cast<uintptr_t>(out) % dtype_bytes(out_dtype) ||
-      reinterpret_cast<uintptr_t>(bias) % 4)
+// The arguments of a product, checked.
+emr_status describe(const void* x, int32_t dtype, int32_t x_batch, int64_t rows, int64_t batch_stride, int64_t row_stride, int64_t col_stride,
+                    const emr_q4* w, emr::Q4Product* a) {
+  if (!q4_ok(w) || !x || rows < 1 || x_batch < 1 || (x_batch != 1 && w->batch != 1 && x_batch != w->batch) || !dtype_ok(dtype) ||
+      batch_stride < 0 || row_stride < 0 || col_stride < 0 || reinterpret_cast<uintptr_t>(x) % dtype_bytes(dtype))
     return EMR_ERR_ARG;
   size_t bytes;
   const emr_status ok = emr_q4_size(w->batch, w->rows, w->cols, w->group, &bytes);
   if (ok != EMR_OK) return ok;
   if (rows > kQ8MaxDim) return EMR_ERR_RANGE;
+  const int piece = 16 / dtype_bytes(dtype);
+  *a = {w, x, dtype, x_batch, rows, batch_stride, row_stride, col_stride, false, nullptr, 0, nullptr, 0};
+  a->whole = col_stride == 1 && reinterpret_cast<uintptr_t>(x) % 16 == 0 && (rows == 1 || row_stride % piece == 0) &&
+             (x_batch == 1 || batch_stride % piece == 0);
+  return double(x_batch) * double(rows) * double(w->cols) > 1e17 ? EMR_ERR_RANGE : EMR_OK;
+}
+
+}  // namespace
+
+extern "C" emr_status emr_q4_matmul_room(const void* x, int32_t dtype, int32_t x_batch, int64_t rows, int64_t batch_stride, int64_t row_stride,
+                                         int64_t col_stride, const emr_q4* w, size_t* bytes) {
+  emr::Q4Product a;
+  if (!bytes) return EMR_ERR_ARG;
+  const emr_status ok = describe(x, dtype, x_batch, rows, batch_stride, row_stride, col_stride, w, &a);
+  if (ok == EMR_OK) *bytes = emr::q4_is_many(a) ? emr::q4_many_room(a) : 0;
+  return ok;
+}
+
+extern "C" emr_status emr_q4_matmul(const void* x, int32_t dtype, int32_t x_batch, int64_t rows, int64_t batch_stride, int64_t row_stride,
+                                    int64_t col_stride, const emr_q4* w, const float* bias, int32_t act, void* out, int32_t out_dtype, void* ws,
+                                    size_t ws_bytes, void* stream) {
+  emr::Q4Product a;
+  const emr_status ok = describe(x, dtype, x_batch, rows, batch_stride, row_stride, col_stride, w, &a);
+  if (ok != EMR_OK) return ok;
+  if (!out || !dtype_ok(out_dtype) || act < EMR_ACT_IDENTITY || act > EMR_ACT_ABS || reinterpret_cast<uintptr_t>(out) % dtype_bytes(out_dtype) ||
+      reinterpret_cast<uintptr_t>(bias) % 4)
+    return EMR_ERR_ARG;
+  a.bias = bias, a.act = act, a.out = out, a.out_dtype = out_dtype;
   int dev = 0, sms = 0;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (emr::q4_is_many(a)) {
+    const size_t room = emr::q4_many_room(a);
+    if (room && (!ws || reinterpret_cast<uintptr_t>(ws) % 16)) return EMR_ERR_ARG;
+    if (ws_bytes < room) return EMR_ERR_CAPACITY;
+    return device_sms(&dev, &sms) ? emr::launch_q4_many(a, ws, dev, sms, st) : EMR_ERR_CUDA;
+  }
   if (!device_sms(&dev, &sms)) return EMR_ERR_CUDA;
   Params p{};
   p.w = w->data, p.tiles = int32_t(q4_tiles(w->rows)), p.blocks = int32_t(q4_blocks(w->cols));
   p.w_batch = w->batch == 1 ? 0 : int64_t(p.tiles) * p.blocks * q4_unit(w->group);
   p.N = w->rows, p.K = w->cols, p.M = rows;
-  p.x = x, p.x_batch = x_batch == 1 ? 0 : batch_stride, p.x_row = row_stride, p.x_col = col_stride;
-  const int64_t batch = x_batch > w->batch ? x_batch : w->batch;
-  const int piece = 16 / dtype_bytes(dtype);
-  p.x_whole = col_stride == 1 && reinterpret_cast<uintptr_t>(x) % 16 == 0 && (rows == 1 || row_stride % piece == 0) &&
-              (x_batch == 1 || batch_stride % piece == 0);
+  p.x = x, p.x_batch = x_batch == 1 ? 0 : batch_stride, p.x_row = row_stride, p.x_col = col_stride, p.x_whole = a.whole;
   p.bias = bias, p.act = act, p.out = out, p.out_dtype = out_dtype;
+  const int64_t batch = x_batch > w->batch ? x_batch : w->batch;
   const int per = kQ4Cols / w->group;
-  const cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (dtype == EMR_F32) return plan<float>(p, batch, per, dev, sms, st);
   if (dtype == EMR_BF16) return plan<__nv_bfloat16>(p, batch, per, dev, sms, st);
   return plan<__half>(p, batch, per, dev, sms, st);

@@ -116,7 +116,8 @@ def lib() -> C.CDLL:
             "emr_q4_quantize": [vp, i32, i64, i64, i64, vp, vp],
             "emr_q4_pack": [vp, i64, i64, i64, vp, i64, i64, i64, vp, vp],
             "emr_q4_dequantize": [vp, vp, i32, vp],
-            "emr_q4_matmul": [vp, i32, i32, i64, i64, i64, i64, vp, vp, i32, vp, i32, vp],
+            "emr_q4_matmul_room": [vp, i32, i32, i64, i64, i64, i64, vp, vp],
+            "emr_q4_matmul": [vp, i32, i32, i64, i64, i64, i64, vp, vp, i32, vp, i32, vp, sz, vp],
             "emr_log_probs": [vp, i32, i32, i64, i64, vp, vp, f32, i32, vp, vp, vp, vp, vp],
             "emr_log_probs_grad": [vp, i32, i32, i64, i64, vp, vp, f32, vp, f32, vp, f32, vp, vp, vp, i32, i64, vp],
             "emr_distill": [vp, i32, i32, i64, i64, vp, vp, i32, i32, vp, f32, i32, vp, f32, vp, vp, i32, i64, vp],
@@ -1169,8 +1170,15 @@ def q4_matmul(x, w: Q4, bias=None, act: int = ACT_IDENTITY, out_dtype=torch.floa
         raw = torch._C._cuda_getCurrentRawStream(dev.index)
         if w._home is not None and raw != w._home:
             _lend(dev, w.data)
-        status = lib().emr_q4_matmul(x.data_ptr(), kind, nx, m, *x.stride(), w.ref, bias.data_ptr() if bias is not None else None, act,
-                                     out.data_ptr(), out_kind, raw)
+        L, x_args, ws, room = lib(), (x.data_ptr(), kind, nx, m, *x.stride(), w.ref), None, 0
+        if m > 8:
+            n = C.c_size_t()
+            _check(L.emr_q4_matmul_room(*x_args, C.byref(n)), "emr_q4_matmul_room")
+            room = n.value
+            if room:
+                ws = torch.empty(room, dtype=torch.uint8, device=dev)
+        status = L.emr_q4_matmul(*x_args, bias.data_ptr() if bias is not None else None, act, out.data_ptr(), out_kind,
+                                 ws.data_ptr() if room else None, room, raw)
         if status:
             _check(status, "emr_q4_matmul")
     return out

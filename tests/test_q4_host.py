@@ -36,7 +36,7 @@ def test_refusals_come_before_any_launch():
         assert L.emr_q4_quantize(FAKE, 0, 20, 5, 1, C.byref(q), None) == emr.EMR_ERR_ARG
         assert L.emr_q4_pack(FAKE, 20, 5, 1, FAKE, 4, 1, 1, C.byref(q), None) == emr.EMR_ERR_ARG
         assert L.emr_q4_dequantize(C.byref(q), FAKE, 0, None) == emr.EMR_ERR_ARG
-        assert L.emr_q4_matmul(FAKE, 0, 1, 2, 10, 5, 1, C.byref(q), None, 0, FAKE, 0, None) == emr.EMR_ERR_ARG
+        assert L.emr_q4_matmul(FAKE, 0, 1, 2, 10, 5, 1, C.byref(q), None, 0, FAKE, 0, None, 0, None) == emr.EMR_ERR_ARG
     ref = C.byref(q4())
     for args in ((None, 0, 20, 5, 1), (FAKE, 3, 20, 5, 1), (FAKE + 2, 0, 20, 5, 1), (FAKE, 0, -1, 5, 1), (FAKE, 0, 20, -5, 1), (FAKE, 0, 20, 5, -1)):
         assert L.emr_q4_quantize(*args, ref, None) == emr.EMR_ERR_ARG
@@ -47,7 +47,7 @@ def test_refusals_come_before_any_launch():
     assert L.emr_q4_dequantize(ref, FAKE + 1, 1, None) == emr.EMR_ERR_ARG
 
 
-OK = [FAKE, 0, 3, 2, 10, 5, 1, q4(batch=3), None, 0, FAKE, 0, None]
+OK = [FAKE, 0, 3, 2, 10, 5, 1, q4(batch=3), None, 0, FAKE, 0, None, 0, None]
 
 
 @pytest.mark.parametrize("i,v,want", [
@@ -60,6 +60,28 @@ def test_refusals_of_the_product(i, v, want):
     args[i] = v
     args[7] = C.byref(args[7])
     assert emr.lib().emr_q4_matmul(*args) == want
+
+
+def room(dtype, rows, x=FAKE, row_stride=8, q=None):
+    n = C.c_size_t()
+    q = q or q4()
+    return emr.lib().emr_q4_matmul_room(x, dtype, 1, rows, 0, row_stride, 1, C.byref(q), C.byref(n)), n.value
+
+
+def test_room():
+    """Nothing for few rows and for rows that are copied as they lie; else x in 16 bits, three parts of float32."""
+    assert room(emr.EMR_F32, 1) == room(emr.EMR_BF16, 1, row_stride=5) == room(emr.EMR_F16, 100) == (emr.EMR_OK, 0)
+    assert room(emr.EMR_F32, 100) == (emr.EMR_OK, 3 * 100 * 128 * 2)
+    assert room(emr.EMR_BF16, 100, row_stride=5) == room(emr.EMR_BF16, 100, FAKE + 2) == (emr.EMR_OK, 100 * 128 * 2)
+    assert room(emr.EMR_F32, 0)[0] == room(3, 1)[0] == room(0, 1, q=q4(group=1))[0] == emr.EMR_ERR_ARG
+    args = list(OK)
+    args[3] = 100
+    args[7] = C.byref(args[7])
+    assert emr.lib().emr_q4_matmul(*args) == emr.EMR_ERR_ARG              # no workspace
+    args[12], args[13] = FAKE, 100
+    assert emr.lib().emr_q4_matmul(*args) == emr.EMR_ERR_CAPACITY
+    args[12] = FAKE + 8
+    assert emr.lib().emr_q4_matmul(*args) == emr.EMR_ERR_ARG
 
 
 def test_by_hand():
