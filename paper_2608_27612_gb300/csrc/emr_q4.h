@@ -33,6 +33,15 @@ __device__ __forceinline__ uint32_t q4_place(int c0, int c1, int c2, int c3, int
   return (uint32_t(c0 + 8 & 15) | uint32_t(c1 + 8 & 15) << 16 | uint32_t(c2 + 8 & 15) << 4 | uint32_t(c3 + 8 & 15) << 20) << shift;
 }
 
+// Two codes, 16 bits apart, as 16-bit floats: 1024 + q or 128 + q with q = code + 8, and the rest taken off.
+template <bool kHalf>
+__device__ __forceinline__ uint32_t codes(uint32_t w) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(w), "r"(0x000f000fu), "r"(kHalf ? 0x64006400u : 0x43004300u));  // (w & mask) | ones
+  if (kHalf) asm("sub.rn.f16x2 %0, %0, %1;" : "+r"(r) : "r"(0x64086408u));
+  else asm("sub.rn.bf16x2 %0, %0, %1;" : "+r"(r) : "r"(0x43084308u));
+  return r;
+}
 // Two 32-bit values as pairs of bfloat16: a part of each takes the next 8 bits of its fraction. An infinity is the first part
 // alone, a NaN each.
 __device__ __forceinline__ void split_pair(float v0, float v1, uint32_t& hi, uint32_t& mid, uint32_t& lo) {

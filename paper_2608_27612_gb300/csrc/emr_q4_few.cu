@@ -64,19 +64,6 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// Two codes, 16 bits apart, as 16-bit floats.
-template <bool kHalf>
-__device__ __forceinline__ uint32_t codes(uint32_t w) {
-  uint32_t r;
-  if (kHalf) {
-    r = (w & 0x000f000fu) | 0x64006400u;
-    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(r), "r"(0x64086408u));
-  } else {
-    r = (w & 0x000f000fu) | 0x43004300u;
-    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(r), "r"(0x43084308u));
-  }
-  return r;
-}
 // T: x. kN: tiles of 8 columns. kPer: groups in 128 columns.
 template <typename T, int kN, int kPer>
 __global__ void __launch_bounds__(kThreads, kN <= 2 ? 2 : 1) q4_few_kernel(const __grid_constant__ Params p) {

@@ -69,10 +69,11 @@ def room(dtype, rows, x=FAKE, row_stride=8, q=None):
 
 
 def test_room():
-    """Nothing for few rows and for rows that are copied as they lie; else x in 16 bits, three parts of float32."""
-    assert room(emr.EMR_F32, 1) == room(emr.EMR_BF16, 1, row_stride=5) == room(emr.EMR_F16, 100) == (emr.EMR_OK, 0)
-    assert room(emr.EMR_F32, 100) == (emr.EMR_OK, 3 * 100 * 128 * 2)
-    assert room(emr.EMR_BF16, 100, row_stride=5) == room(emr.EMR_BF16, 100, FAKE + 2) == (emr.EMR_OK, 100 * 128 * 2)
+    """Nothing for few rows; else x in tiles of rows rounded up to 16, whole blocks of 128 columns, three parts of float32."""
+    assert room(emr.EMR_F32, 8) == room(emr.EMR_BF16, 16, row_stride=5) == (emr.EMR_OK, 0)
+    assert room(emr.EMR_F32, 9) == (emr.EMR_OK, 3 * 16 * 256) and room(emr.EMR_F32, 65) == (emr.EMR_OK, 2 * 3 * 48 * 256)
+    assert room(emr.EMR_BF16, 100, row_stride=5) == room(emr.EMR_F16, 100) == (emr.EMR_OK, 112 * 256)
+    assert room(emr.EMR_F16, 129, q=q4(cols=129)) == (emr.EMR_OK, 2 * 2 * 80 * 256)
     assert room(emr.EMR_F32, 0)[0] == room(3, 1)[0] == room(0, 1, q=q4(group=1))[0] == emr.EMR_ERR_ARG
     args = list(OK)
     args[3] = 100
