@@ -83,10 +83,10 @@ template <typename T, int kTeam>
 __global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? 2 : kTeam == 128 ? 8 : 4) distill_kernel(const __grid_constant__ Args a) {
   typedef Row<T, kTeam> R;
   constexpr int kG = R::kG, kPiece = List<kTeam>::kBytes;
-  __shared__ uint4 scratch[kTeam == 32 ? 1 : 64], slots[2 * kMaxCluster];
+  __shared__ uint4 scratch[kTeam == 32 ? 1 : 64], slots[kTeam == 512 ? 2 * kMaxCluster : 1];
   __shared__ List<kTeam> lists;
   const int team = kTeam == 32 ? threadIdx.x >> 5 : 0;
-  const int64_t row = kTeam == 32 ? int64_t(blockIdx.x) * 8 + team : int64_t(blockIdx.x / cg::this_cluster().num_blocks());
+  const int64_t row = kTeam == 32 ? int64_t(blockIdx.x) * 8 + team : kTeam < 512 ? int64_t(blockIdx.x) : int64_t(blockIdx.x / cg::this_cluster().num_blocks());
   if (kTeam == 32 && row >= a.rows) return;
   R r(a, row, scratch, slots);
   if (r.blocks > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
@@ -123,8 +123,8 @@ __global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? 2 : 
   for (int j = r.tid; j < a.k; j += kTeam) part += t[j] = expf(l[j] - l_max);
   const float2 sums = r.team_sum(make_float2(part, wrong));
   const float t_sum = (!a.tail && sums.x > 0.f ? 1.f : sums.x) + sums.y;
-  const float t_scale = !a.tail && sums.x > 0.f ? __fdiv_rn(1.f, sums.x) : 1.f;
-  const float l_base = !a.tail && sums.x > 0.f ? l_max + logf(sums.x) : 0.f;  // log t_j = l_j - l_base
+  float t_scale = 1.f, l_base = 0.f;  // log t_j = l_j - l_base
+  if (!a.tail && sums.x > 0.f) t_scale = __fdiv_rn(1.f, sums.x), l_base = l_max + logf(sums.x);
 
   // the rest's sums
   Stat rest;
@@ -178,21 +178,27 @@ __global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? 2 : 
     r.exchange(own, [&](float x) { z_listed += x; });
   }
   const float z_rest = has_rest ? rest.s * fast_exp2(fmaxf((rest.m - m) * r.per, kFar)) : 0.f, z = z_rest + z_listed;
-  const float log_z = empty ? 0.f : logf(z), p_rest = empty ? 0.f : __fdiv_rn(z_rest, z), p_listed = empty ? 0.f : __fdiv_rn(z_listed, z);
+  const float inverse = empty ? 0.f : __fdiv_rn(1.f, z), p_rest = z_rest * inverse, p_listed = z_listed * inverse;
   const float t_rest = a.tail && has_rest ? fmaxf(1.f - t_sum, 0.f) : 0.f;
 
   if (a.loss && r.rank == 0) {
     part = 0.f;
-    for (int j = r.tid; j < a.k; j += kTeam) {
-      const float w = t[j] * t_scale;
-      if (w > 0.f) part += w * ((l[j] - l_base) - (s[j] - m > -INFINITY ? __fdiv_rn(s[j] - m, temperature) - log_z : -INFINITY));
+    float log_z = 0.f;
+    if (r.tid < a.k) {  // the others need no logarithm
+      log_z = empty ? 0.f : logf(z);
+      for (int j = r.tid; j < a.k; j += kTeam) {
+        const float w = t[j] * t_scale;
+        if (w > 0.f) part += w * ((l[j] - l_base) - (s[j] - m > -INFINITY ? __fdiv_rn(s[j] - m, temperature) - log_z : -INFINITY));
+      }
     }
     float loss = r.team_sum(make_float2(part, 0.f)).x;
-    if (t_rest > 0.f) {
-      const float log_p = z_listed <= z_rest ? -log1pf(__fdiv_rn(z_listed, z_rest)) : __fdiv_rn(rest.m - m, temperature) + logf(rest.s) - log_z;
-      loss += t_rest * (log1pf(-t_sum) - log_p);
+    if (r.tid == 0) {
+      if (t_rest > 0.f) {
+        const float log_p = z_listed <= z_rest ? -log1pf(__fdiv_rn(z_listed, z_rest)) : __fdiv_rn(rest.m - m, temperature) + logf(rest.s) - log_z;
+        loss += t_rest * (log1pf(-t_sum) - log_p);
+      }
+      a.loss[row] = isnan(t_sum) ? NAN : loss;
     }
-    if (r.tid == 0) a.loss[row] = isnan(t_sum) ? NAN : loss;
   }
   if (!a.dscores) return;
 
@@ -210,7 +216,7 @@ __global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? 2 : 
       for (int i = j + 1; i < a.k; i++)
         if (at[i] == at[j]) own += t[i];
     const bool on = s[j] > -INFINITY;
-    store_scalar(o.p, o.dtype, at[j] - r.lo, dl * (on ? mass * __fdiv_rn(weight(j), z) - own * t_scale : 0.f * mass));
+    store_scalar(o.p, o.dtype, at[j] - r.lo, dl * (on ? mass * (weight(j) * inverse) - own * t_scale : 0.f * mass));
   }
 }
 

@@ -78,12 +78,12 @@ __device__ __forceinline__ float2 far2(float s0, float s1, float m, float per) {
   return make_float2(fmaxf(d.x, kFar), fmaxf(d.y, kFar));
 }
 
-// One row, by a team of 32 threads (a warp of a block of 8) or of a block, and for the largest team by a cluster of blocks.
+// One row, by a team of 8 or 32 threads (of a block of 256) or of a block, and for the largest team by a cluster of blocks.
 // Threads take it in turns of kAhead groups of 16 bytes each, loaded together and without a check, while all threads have as
 // many; the groups that are left, among them those that reach out of the slice, one at a time.
 template <typename T, int kTeam>
 struct Row {
-  static constexpr int kG = Group<T>::kSize, kAhead = 4, kWarps = kTeam / 32, kTurn = kTeam * kAhead, kTeamSize = kTeam;
+  static constexpr int kG = Group<T>::kSize, kAhead = 4, kWarps = kTeam < 32 ? 1 : kTeam / 32, kTurn = kTeam * kAhead, kTeamSize = kTeam;
   cg::cluster_group cluster;
   int tid, lane, warp, rank, blocks, phase, turn;
   int lo;            // first entry of this block's slice
@@ -100,10 +100,10 @@ struct Row {
   float s_low, e_low;
 
   __device__ __forceinline__ Row(const Rows& a, int64_t row, uint4* scratch_, uint4* slots_) : cluster(cg::this_cluster()), scratch(scratch_), slots(slots_) {
-    lane = threadIdx.x & 31;
-    tid = kTeam == 32 ? lane : threadIdx.x;
+    lane = threadIdx.x & (kTeam < 32 ? kTeam - 1 : 31);
+    tid = kTeam <= 32 ? lane : threadIdx.x;
     warp = tid >> 5;
-    rank = kTeam == 32 ? 0 : int(cluster.block_rank()), blocks = kTeam == 32 ? 1 : int(cluster.num_blocks());
+    rank = kTeam < 512 ? 0 : int(cluster.block_rank()), blocks = kTeam < 512 ? 1 : int(cluster.num_blocks());
     phase = turn = 0;
     const int64_t at = rank * a.slice, left = a.n - at;
     lo = int(at < a.n ? at : a.n);
@@ -190,7 +190,7 @@ struct Row {
   __device__ __forceinline__ void each(Fn& fn) const { each(fn, head, groups, true); }
 
   __device__ __forceinline__ void team_sync() const {
-    if (kTeam == 32) __syncwarp();
+    if (kTeam <= 32) __syncwarp();
     else __syncthreads();
   }
   __device__ void row_sync() {
@@ -199,6 +199,11 @@ struct Row {
   }
   // One barrier for each of these: what a warp finds is combined by every warp again.
   __device__ uint32_t team_max(uint32_t v) {
+    if (kTeam < 32) {
+#pragma unroll
+      for (int o = kTeam / 2; o; o >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
+      return v;
+    }
     v = __reduce_max_sync(0xffffffffu, v);
     if (kTeam == 32) return v;
     uint32_t* const part = reinterpret_cast<uint32_t*>(scratch + 32 * (turn ^= 1));
@@ -208,12 +213,12 @@ struct Row {
   }
   __device__ static float2 warp_sum(float2 v) {
 #pragma unroll
-    for (int o = 16; o; o >>= 1) v.x += __shfl_xor_sync(0xffffffffu, v.x, o), v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
+    for (int o = kTeam < 32 ? kTeam / 2 : 16; o; o >>= 1) v.x += __shfl_xor_sync(0xffffffffu, v.x, o), v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
     return v;
   }
   __device__ float2 team_sum(float2 v) {
     v = warp_sum(v);
-    if (kTeam == 32) return v;
+    if (kTeam <= 32) return v;
     float2* const part = reinterpret_cast<float2*>(scratch + 32 * (turn ^= 1));
     if (lane == 0) part[warp] = v;
     __syncthreads();
@@ -402,8 +407,9 @@ struct Row {
 template <typename A>
 emr_status launch_rows(void (*kernel)(A), const A& a, int team, int cluster, cudaStream_t st) {
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(team == 32 ? unsigned((int64_t(a.rows) + 7) / 8) : unsigned(a.rows) * unsigned(cluster));
-  cfg.blockDim = dim3(team == 32 ? 256u : unsigned(team));
+  const int rows = team <= 32 ? 256 / team : 1;  // of a block
+  cfg.gridDim = dim3(unsigned((int64_t(a.rows) + rows - 1) / rows) * unsigned(cluster));
+  cfg.blockDim = dim3(unsigned(team * rows));
   cfg.stream = st;
   cudaLaunchAttribute attr{};
   attr.id = cudaLaunchAttributeClusterDimension;
@@ -439,6 +445,7 @@ inline int plan(Rows& a, int least, int size, int sms, const int* fit, int* clus
   *cluster = 1;
   a.slice = (a.n + 15) / 16 * 16;
   if (a.n <= 8192) {
+    if (least <= 8 && a.n <= 512 && a.rows >= 32 * sms) return 8;
     if (least <= 32 && a.n <= 1024 && a.rows >= 16 * sms) return 32;
     return least <= 128 && a.rows >= 4 * sms ? 128 : 256;
   }

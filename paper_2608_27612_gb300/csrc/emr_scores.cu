@@ -287,12 +287,15 @@ struct Same {
 enum Ask { kSums, kTop, kGradient };
 
 template <typename T, int kTeam, int kAsk>
-__global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? 2 : kTeam == 128 ? 8 : 4) log_probs_kernel(const __grid_constant__ Args a) {
-  __shared__ uint4 scratch[kTeam == 32 ? 1 : 64], slots[2 * kMaxCluster];
+__global__ void __launch_bounds__(kTeam <= 32 ? 256 : kTeam, kTeam == 512 ? 2 : kTeam == 128 ? 8 : 4) log_probs_kernel(const __grid_constant__ Args a) {
+  constexpr int kRows = kTeam <= 32 ? 256 / kTeam : 1;  // of a block
+  __shared__ uint4 scratch[kTeam <= 32 ? 1 : 64], slots[kTeam == 512 ? 2 * kMaxCluster : 1];
   __shared__ std::conditional_t<kAsk == kTop, Best<kTeam>, uint32_t> best;
-  const int team = kTeam == 32 ? threadIdx.x >> 5 : 0;
-  const int64_t row = kTeam == 32 ? int64_t(blockIdx.x) * 8 + team : int64_t(blockIdx.x / cg::this_cluster().num_blocks());
-  if (kTeam == 32 && row >= a.rows) return;
+  const int team = kTeam <= 32 ? threadIdx.x / kTeam : 0;
+  int64_t row = kTeam < 512 ? int64_t(blockIdx.x) * kRows + team : int64_t(blockIdx.x / cg::this_cluster().num_blocks());
+  const bool there = row < a.rows;
+  if (kTeam == 32 && !there) return;
+  if (kTeam < 32 && !there) row = a.rows - 1;  // a warp's teams go together: this one writes nothing
   Search<T, kTeam> r(a, row, scratch, slots);
   if constexpr (kAsk == kTop) {
     if (r.tid < 2) best.size[team][r.tid] = 0;
@@ -315,8 +318,14 @@ __global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? 2 : 
     r.top_infinite = true;
   }
   const bool empty = all.m == -INFINITY;
-  const float log_z = logf(all.s);
-  const float entropy = empty || greedy ? 0.f : fmaxf(log_z - kLn2 * __fdiv_rn(all.e, all.s), 0.f);
+  // what is written for the row, and by whom; the others need no logarithm
+  const bool tells = r.rank == 0 && (r.tid < (kAsk == kTop ? max(a.top, 1) : 1));
+  const bool uncertain = kAsk == kGradient && dentropy != 0.f;
+  float log_z = 0.f, entropy = 0.f;
+  if (tells || uncertain) {
+    log_z = logf(all.s);
+    entropy = empty || greedy ? 0.f : fmaxf(log_z - kLn2 * __fdiv_rn(all.e, all.s), 0.f);
+  }
   const auto log_prob = [&](float s) { return s - all.m > -INFINITY ? __fdiv_rn(s - all.m, temperature) - log_z : -INFINITY; };
 
   const int64_t first = greedy && !empty && a.logp ? r.first(all.m) : -1;
@@ -332,7 +341,7 @@ __global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? 2 : 
     }
     if (r.blocks > 1) r.cluster.sync();  // the list's size was read from the first block
   }
-  if (r.rank == 0 && r.tid == 0) {
+  if (r.rank == 0 && r.tid == 0 && there) {
     if (a.logp) {
       const T* const scores = static_cast<const T*>(a.scores) + row * a.row_stride;
       float v = 0.f;
@@ -347,7 +356,8 @@ __global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? 2 : 
     const float per_t = greedy ? 0.f : fminf(__fdiv_rn(1.f, temperature), 3e38f);
     const float da = target < 0 ? 0.f : target >= a.n ? NAN : dlogp;
     const float inverse = empty ? 0.f : __fdiv_rn(-per_t, all.s), m = empty ? 0.f : all.m, hit = da * per_t;
-    const float k1 = inverse * dentropy * kLn2, k0 = inverse * fmaf(dentropy, entropy - log_z, da);
+    const float k1 = inverse * dentropy * kLn2, k0 = inverse * (uncertain ? fmaf(dentropy, entropy - log_z, da) : da);
+    if (kTeam < 32 && !there) return;
     const typename Row<T, kTeam>::Out o = r.out(a, row);
     if (empty || isnan(da + dentropy)) {
       r.put(o, Same{empty && !isnan(da + dentropy) ? 0.f : NAN});
@@ -374,9 +384,12 @@ const int* fits() {
 
 template <typename T, int kAsk>
 emr_status log_probs(Args a, int sms, cudaStream_t st) {
-  const int least = kAsk != kTop || a.top <= Best<32>::kTop ? 32 : a.top <= Best<128>::kTop ? 128 : 256;
+  const int least = kAsk != kTop ? 8 : a.top <= Best<32>::kTop ? 32 : a.top <= Best<128>::kTop ? 128 : 256;
   int cluster;
   const int team = plan(a, least, sizeof(T), sms, fits(), &cluster);
+  if constexpr (kAsk != kTop) {
+    if (team == 8) return launch_rows(log_probs_kernel<T, 8, kAsk>, a, team, cluster, st);
+  }
   return team == 32    ? launch_rows(log_probs_kernel<T, 32, kAsk>, a, team, cluster, st)
          : team == 128 ? launch_rows(log_probs_kernel<T, 128, kAsk>, a, team, cluster, st)
          : team == 256 ? launch_rows(log_probs_kernel<T, 256, kAsk>, a, team, cluster, st)
