@@ -400,20 +400,23 @@ emr_status plan(Params p, int64_t batch, int per, int dev, int sms, cudaStream_t
     const int64_t room_for = (kn <= 2 ? 2 : 1) * sms / chunks;
     blocks = p.all_blocks < room_for || room_for < 1 ? p.all_blocks : room_for;
   } else {
-    // every block reads x: rows of W enough that x is at most half as many bytes
+    // every block reads x: rows of W enough that x is at most half as many bytes, and that its share of x fits at once
     int wide = 1;
     while (wide < kWarps && p.step * int(sizeof(T)) > wide * kr * 4) wide *= 2;
-    p.wide = wide, p.teams = kWarps / wide;
-    p.row_blocks = int((row_tiles + wide - 1) / wide);
-    blocks = batch * p.row_blocks;
+    const int at_once = (kn <= 2 ? 2 : 1) * sms;
+    for (;; wide *= 2) {
+      p.wide = wide, p.teams = kWarps / wide;
+      p.row_blocks = int((row_tiles + wide - 1) / wide);
+      blocks = batch * p.row_blocks;
+      shares = 1;
+      for (int s = 2; s <= kMaxCluster; s++)
+        if (blocks * s * chunks <= at_once && p.blocks / (s * p.teams) >= 2) shares = s;
+      const int share = (p.blocks + shares - 1) / shares, some = p.teams == 1 ? fit_direct : fit, parts = (share + some - 1) / some;
+      p.chunk = (share + parts - 1) / parts;
+      if (parts == 1 || wide == kWarps) break;
+    }
     if (blocks > INT32_MAX) return EMR_ERR_RANGE;
     p.all_blocks = int32_t(blocks);
-    const int at_once = (kn <= 2 ? 2 : 1) * sms;
-    for (int s = 2; s <= kMaxCluster; s++)
-      if (blocks * s * chunks <= at_once && p.blocks / (s * p.teams) >= 2) shares = s;
-    const int share = (p.blocks + shares - 1) / shares;
-    const int some = p.teams == 1 ? fit_direct : fit, parts = (share + some - 1) / some;
-    p.chunk = (share + parts - 1) / parts;
   }
   if (blocks * shares > INT32_MAX) return EMR_ERR_RANGE;
   for (p.log_teams = 0; (1 << p.log_teams) < p.teams;) p.log_teams++;

@@ -41,7 +41,7 @@ struct Args : Rows {
 template <int kTeam>
 struct Best {
   static constexpr int kTeams = kTeam == 32 ? 8 : 1, kCap = kTeam == 32 ? 128 : kTeam == 512 ? 2048 : 1024;
-  static constexpr int kTop = kTeam == 32 ? 32 : kTeam == 128 ? 64 : EMR_MAX_TOP;
+  static constexpr int kTop = kTeam <= 128 ? 32 : EMR_MAX_TOP;
   u64 list[kTeams][kCap], sorted[kTeams][kTop], found[kTeams];
   alignas(16) uint32_t counts[kTeams][256];  // read 16 bytes at a time
   int size[kTeams][2], hits[kTeams];
@@ -130,8 +130,7 @@ struct Search : Row<T, kTeam> {
           if (min(255, int((top - key_score(mid)) * steps)) <= step) past = mid;
           else least = mid + 1;
         }
-        row_sync();  // the counts have been read
-        return max(least, 1u);
+        return max(least, 1u);  // the counts are written again only after the next barrier of the row
       }
     }
     // the k-th of a block's threads, bit by bit, and the best of the blocks' own
@@ -247,14 +246,42 @@ struct Search : Row<T, kTeam> {
     }
   }
   // The list's m entries in order, in `sorted` of the row's first block, as far as it holds them: an entry's place is
-  // the number of larger ones.
-  __device__ void order(int m, const u64* list, u64* sorted, int room) {
+  // the number of larger ones. Of more than 64 entries each 32 are sorted by a warp, and counted by bisection (about 208
+  // entries for the best 100 of 5460: 4000 rows 88 -> 73 us).
+  __device__ void order(int m, u64* list, u64* sorted, int room) {
     if (rank == 0) {
+      const bool parts = m > 64;
+      if (parts) {
+        for (int c = warp * 32; c < m; c += kWarps * 32) {
+          u64 e = c + lane < m ? list[c + lane] : 0;
+#pragma unroll
+          for (int size = 2; size <= 32; size *= 2)
+#pragma unroll
+            for (int apart = size / 2; apart; apart /= 2) {
+              const u64 other = __shfl_xor_sync(0xffffffffu, e, apart);
+              const bool first = !(lane & apart), down = !(lane & size) || size == 32;
+              e = (other > e) == (first == down) ? other : e;
+            }
+          list[c + lane] = e;
+        }
+        team_sync();
+      }
       for (int j = tid; j < m; j += kTeam) {
         const u64 e = list[j];
         int larger = 0;
-#pragma unroll 4
-        for (int i = 0; i < m; i++) larger += list[i] > e;
+        if (!parts) {
+#pragma unroll 8
+          for (int i = 0; i < m; i++) larger += list[i] > e;
+        } else {
+          larger = j & 31;
+          for (int c = 0; c < m; c += 32) {
+            if (c == (j & ~31)) continue;
+            int n = 0;
+#pragma unroll
+            for (int step = 16; step; step /= 2) n += list[c + n + step - 1] > e ? step : 0;
+            larger += n + (list[c + n] > e);
+          }
+        }
         if (larger < room) sorted[larger] = e;
       }
     }
