@@ -82,8 +82,7 @@ emr_status launch(Args a, const emr_q4* q, cudaStream_t st) {
   a.tiles = q4_tiles(q->rows), a.blocks = q4_blocks(q->cols);
   a.total = int64_t(q->batch) * a.tiles * kQ4Rows * a.blocks;
   const int64_t blocks = (a.total + 7) / 8;
-  q4_kernel<kFrom><<<unsigned(blocks < (1 << 20) ? blocks : 1 << 20), 256, 0, st>>>(a);
-  return cudaPeekAtLastError() == cudaSuccess ? EMR_OK : EMR_ERR_CUDA;
+  return launch_plain(q4_kernel<kFrom>, dim3(unsigned(blocks < (1 << 20) ? blocks : 1 << 20)), 256, st, a);
 }
 
 emr_status sizes_ok(const emr_q4* q) {

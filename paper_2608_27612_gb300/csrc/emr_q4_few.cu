@@ -465,6 +465,10 @@ extern "C" emr_status emr_q4_matmul(const void* x, int32_t dtype, int32_t x_batc
   if (!out || !dtype_ok(out_dtype) || act < EMR_ACT_IDENTITY || act > EMR_ACT_ABS || reinterpret_cast<uintptr_t>(out) % dtype_bytes(out_dtype) ||
       reinterpret_cast<uintptr_t>(bias) % 4)
     return EMR_ERR_ARG;
+  const int64_t batch = x_batch > w->batch ? x_batch : w->batch;
+  if (overlap(x, (x_batch - 1) * batch_stride + (rows - 1) * row_stride + (w->cols - 1) * col_stride + 1, dtype_bytes(dtype), out, batch * rows * w->rows,
+              dtype_bytes(out_dtype)))
+    return EMR_ERR_ARG;
   a.bias = bias, a.act = act, a.out = out, a.out_dtype = out_dtype;
   int dev = 0, sms = 0;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -481,7 +485,6 @@ extern "C" emr_status emr_q4_matmul(const void* x, int32_t dtype, int32_t x_batc
   p.N = w->rows, p.K = w->cols, p.M = rows;
   p.x = x, p.x_batch = x_batch == 1 ? 0 : batch_stride, p.x_row = row_stride, p.x_col = col_stride, p.x_whole = a.whole;
   p.bias = bias, p.act = act, p.out = out, p.out_dtype = out_dtype;
-  const int64_t batch = x_batch > w->batch ? x_batch : w->batch;
   const int per = kQ4Cols / w->group;
   if (dtype == EMR_F32) return plan<float>(p, batch, per, dev, sms, st);
   if (dtype == EMR_BF16) return plan<__nv_bfloat16>(p, batch, per, dev, sms, st);

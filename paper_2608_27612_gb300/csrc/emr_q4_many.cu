@@ -443,13 +443,13 @@ emr_status launch_q4_many(const Q4Product& a, void* ws, int dev, int sms, cudaSt
   const int64_t total = int64_t(a.x_batch) * a.rows * p.blocks * 16, wanted = (total + 255) / 256;
   const unsigned grid = unsigned(wanted < 16 * sms ? wanted : 16 * sms);
   uint8_t* const out = static_cast<uint8_t*>(ws);
-  if (a.dtype == EMR_F32)
-    q4_tiles_kernel<float><<<grid, 256, 0, st>>>(static_cast<const float*>(a.x), a.rows, a.w->cols, p.blocks, a.batch_stride, a.row_stride, a.col_stride,
-                                                 a.whole, p.step, p.width, int(chunks), total, out);
-  else  // of both 16-bit types the bits are copied
-    q4_tiles_kernel<__half><<<grid, 256, 0, st>>>(static_cast<const __half*>(a.x), a.rows, a.w->cols, p.blocks, a.batch_stride, a.row_stride,
-                                                  a.col_stride, a.whole, p.step, p.width, int(chunks), total, out);
-  if (cudaPeekAtLastError() != cudaSuccess) return EMR_ERR_CUDA;
+  // of both 16-bit types the bits are copied
+  const emr_status laid = a.dtype == EMR_F32
+                              ? launch_plain(q4_tiles_kernel<float>, dim3(grid), 256, st, static_cast<const float*>(a.x), a.rows, a.w->cols, p.blocks,
+                                             a.batch_stride, a.row_stride, a.col_stride, a.whole, p.step, p.width, int(chunks), total, out)
+                              : launch_plain(q4_tiles_kernel<__half>, dim3(grid), 256, st, static_cast<const __half*>(a.x), a.rows, a.w->cols, p.blocks,
+                                             a.batch_stride, a.row_stride, a.col_stride, a.whole, p.step, p.width, int(chunks), total, out);
+  if (laid != EMR_OK) return laid;
   p.x = out;
   p.x_batch = a.x_batch == 1 ? 0 : chunks * p.blocks * (int64_t(p.parts) * width * 256);
 

@@ -132,6 +132,22 @@ emr_status launch_after(void (*kernel)(P...), dim3 grid, int threads, size_t sme
   return cudaLaunchKernelEx(&cfg, kernel, P(args)...) == cudaSuccess ? EMR_OK : EMR_ERR_CUDA;
 }
 
+// The same after what came before; its own error only.
+template <typename... P, typename... A>
+emr_status launch_plain(void (*kernel)(P...), dim3 grid, int threads, cudaStream_t st, const A&... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(unsigned(threads));
+  cfg.stream = st;
+  return cudaLaunchKernelEx(&cfg, kernel, P(args)...) == cudaSuccess ? EMR_OK : EMR_ERR_CUDA;
+}
+
+// Whether two arrays of so many elements share memory.
+inline bool overlap(const void* x, int64_t nx, int size_x, const void* y, int64_t ny, int size_y) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(x), b = reinterpret_cast<uintptr_t>(y);
+  return a < b + uint64_t(ny) * size_y && b < a + uint64_t(nx) * size_x;
+}
+
 // The current device and its number of SMs.
 inline bool device_sms(int* dev, int* sms) {
   return cudaGetDevice(dev) == cudaSuccess && cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, *dev) == cudaSuccess;

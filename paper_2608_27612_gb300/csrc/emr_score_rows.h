@@ -436,6 +436,7 @@ void clusters_at_once(K kernel, int threads, int* fit) {
     cfg.numAttrs = 1;
     int n = 0;
     if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess) fit[c] = n;
+    else cudaGetLastError();  // the question's error is not the caller's
   }
 }
 
@@ -462,12 +463,6 @@ inline bool aligned(const void* p, int bytes) { return reinterpret_cast<uintptr_
 inline emr_status check_scores(const void* scores, int32_t dtype, int32_t rows, int64_t n, int64_t row_stride) {
   if (rows < 1 || n < 1 || !scores || !dtype_ok(dtype) || row_stride < 0 || !aligned(scores, dtype_bytes(dtype))) return EMR_ERR_ARG;
   return n > INT32_MAX - (1 << 20) || rows > (1 << 27) ? EMR_ERR_RANGE : EMR_OK;
-}
-
-// Whether two arrays of so many elements share memory.
-inline bool overlap(const void* x, int64_t nx, int size_x, const void* y, int64_t ny, int size_y) {
-  const uintptr_t a = reinterpret_cast<uintptr_t>(x), b = reinterpret_cast<uintptr_t>(y);
-  return a < b + uint64_t(ny) * size_y && b < a + uint64_t(nx) * size_x;
 }
 
 }  // namespace rows

@@ -1001,9 +1001,13 @@ class DenseLayer:
 
 def _per_row(v, rows: int, dtype, device, what: str):
     """Address of a device array of a parameter given for each row."""
+    _check_per_row(v, rows, dtype, device, what)
+    return v.data_ptr()
+
+
+def _check_per_row(v, rows: int, dtype, device, what: str):
     if v.shape != (rows,) or v.dtype != dtype or v.device != device or not v.is_contiguous():
         raise ValueError("%s: a number or a contiguous %s tensor [%d] on the scores' GPU is wanted" % (what, dtype, rows))
-    return v.data_ptr()
 
 
 def sample(scores, noise, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, stream=None):
@@ -1220,17 +1224,20 @@ def _check_scores(scores):
     return scores.shape[0] if scores.dim() == 2 else 1
 
 
-def _number_or_rows(v, rows: int, dev, what: str):
-    """(address, number) of a float parameter that is given for each row or for all."""
+def _check_number_or_rows(v, rows: int, dev, what: str):
     if isinstance(v, torch.Tensor):
-        return _per_row(v, rows, torch.float32, dev, what), 0.0
-    return None, float(v)
+        _check_per_row(v, rows, torch.float32, dev, what)
 
 
-def _targets(targets, rows: int, dev):
+def _number_or_rows(v):
+    """(address, number) of a float parameter that is given for each row or for all."""
+    return (v.data_ptr(), 0.0) if isinstance(v, torch.Tensor) else (None, float(v))
+
+
+def _check_targets(targets, rows: int, dev):
     if not isinstance(targets, torch.Tensor):
         raise ValueError("targets: an int32 tensor [%d] on the scores' GPU is wanted" % rows)
-    return _per_row(targets, rows, torch.int32, dev, "targets")
+    _check_per_row(targets, rows, torch.int32, dev, "targets")
 
 
 def log_probs(scores, targets=None, temperature=1.0, top=0, stream=None) -> LogProbs:
@@ -1241,21 +1248,26 @@ def log_probs(scores, targets=None, temperature=1.0, top=0, stream=None) -> LogP
     dev = scores.device
     if not 0 <= top <= MAX_TOP:
         raise ValueError("top: 0 to %d is wanted, got %r" % (MAX_TOP, top))
-    tp = _targets(targets, rows, dev) if targets is not None else None
-    hp, heat = _number_or_rows(temperature, rows, dev, "temperature")
+    if targets is not None:
+        _check_targets(targets, rows, dev)
+    _check_number_or_rows(temperature, rows, dev, "temperature")
     away = _away(dev, stream)
     if away is not None:
         with away:
             return log_probs(scores, targets, temperature, top)
     scores, rows, n, stride, kind = _rows_of(scores)
-    logp = torch.empty(rows, dtype=torch.float32, device=dev) if tp is not None else None
     entropy = torch.empty(rows, dtype=torch.float32, device=dev)
-    index = torch.empty(rows, top, dtype=torch.int32, device=dev) if top else None
-    best = torch.empty(rows, top, dtype=torch.float32, device=dev) if top else None
+    logp = index = best = tp = lp = ip = bp = None
+    if targets is not None:
+        logp = torch.empty(rows, dtype=torch.float32, device=dev)
+        tp, lp = targets.data_ptr(), logp.data_ptr()
+    if top:
+        index = torch.empty((rows, top), dtype=torch.int32, device=dev)
+        best = torch.empty((rows, top), dtype=torch.float32, device=dev)
+        ip, bp = index.data_ptr(), best.data_ptr()
     if rows:
-        status = lib().emr_log_probs(scores.data_ptr(), kind, rows, n, stride, tp, hp, heat, top,
-                                     logp.data_ptr() if tp is not None else None, entropy.data_ptr(),
-                                     index.data_ptr() if top else None, best.data_ptr() if top else None,
+        hp, heat = _number_or_rows(temperature)
+        status = lib().emr_log_probs(scores.data_ptr(), kind, rows, n, stride, tp, hp, heat, top, lp, entropy.data_ptr(), ip, bp,
                                      torch._C._cuda_getCurrentRawStream(dev.index))
         if status:
             _check(status, "emr_log_probs")
@@ -1268,10 +1280,12 @@ def log_probs_grad(scores, targets, dlogp, dentropy=None, temperature=1.0, out_d
     tensors [rows]; dentropy None: 0. The loss of a step of cross entropy is -logp with dlogp = -1 / rows."""
     rows = _check_scores(scores)
     dev, shape = scores.device, scores.shape
-    tp = _targets(targets, rows, dev)
-    ap, a = _number_or_rows(dlogp, rows, dev, "dlogp")
-    bp, b = _number_or_rows(0.0 if dentropy is None else dentropy, rows, dev, "dentropy")
-    hp, heat = _number_or_rows(temperature, rows, dev, "temperature")
+    _check_targets(targets, rows, dev)
+    _check_number_or_rows(dlogp, rows, dev, "dlogp")
+    if dentropy is None:
+        dentropy = 0.0
+    _check_number_or_rows(dentropy, rows, dev, "dentropy")
+    _check_number_or_rows(temperature, rows, dev, "temperature")
     out_kind = _dtype(scores.dtype if out_dtype is None else out_dtype, "out_dtype")
     away = _away(dev, stream)
     if away is not None:
@@ -1282,9 +1296,9 @@ def log_probs_grad(scores, targets, dlogp, dentropy=None, temperature=1.0, out_d
     logp = torch.empty(rows, dtype=torch.float32, device=dev)
     entropy = torch.empty(rows, dtype=torch.float32, device=dev)
     if rows:
-        status = lib().emr_log_probs_grad(scores.data_ptr(), kind, rows, n, stride, tp, hp, heat, ap, a, bp, b, logp.data_ptr(),
-                                          entropy.data_ptr(), dscores.data_ptr(), out_kind, n,
-                                          torch._C._cuda_getCurrentRawStream(dev.index))
+        status = lib().emr_log_probs_grad(scores.data_ptr(), kind, rows, n, stride, targets.data_ptr(), *_number_or_rows(temperature),
+                                          *_number_or_rows(dlogp), *_number_or_rows(dentropy), logp.data_ptr(), entropy.data_ptr(),
+                                          dscores.data_ptr(), out_kind, n, torch._C._cuda_getCurrentRawStream(dev.index))
         if status:
             _check(status, "emr_log_probs_grad")
     return dscores, logp, entropy
@@ -1301,11 +1315,12 @@ def _distill(scores, index, logp, dloss, temperature, tail, out_dtype, stream):
     if not isinstance(logp, torch.Tensor) or logp.shape != index.shape or logp.device != dev:
         raise ValueError("logp: a tensor in the shape of index on the scores' GPU is wanted")
     k, t_kind = index.shape[1], _dtype(logp.dtype, "logp")
-    hp, heat = _number_or_rows(temperature, rows, dev, "temperature")
-    if hp is None and not heat > 0:
+    _check_number_or_rows(temperature, rows, dev, "temperature")
+    if not isinstance(temperature, torch.Tensor) and not temperature > 0:
         raise ValueError("temperature: a number above 0 is wanted, got %r" % (temperature,))
     grad = dloss is not None
-    wp, w = _number_or_rows(dloss, rows, dev, "dloss") if grad else (None, 0.0)
+    if grad:
+        _check_number_or_rows(dloss, rows, dev, "dloss")
     out_kind = _dtype(scores.dtype if out_dtype is None else out_dtype, "out_dtype") if grad else 0
     away = _away(dev, stream)
     if away is not None:
@@ -1316,8 +1331,8 @@ def _distill(scores, index, logp, dloss, temperature, tail, out_dtype, stream):
     dscores = torch.empty(shape, dtype=out_dtype or scores.dtype, device=dev) if grad else None
     loss = torch.empty(rows, dtype=torch.float32, device=dev)
     if rows:
-        status = lib().emr_distill(scores.data_ptr(), kind, rows, n, stride, index.data_ptr(), logp.data_ptr(), t_kind, k, hp, heat,
-                                   1 if tail else 0, wp, w, loss.data_ptr(), dscores.data_ptr() if grad else None, out_kind, n,
+        status = lib().emr_distill(scores.data_ptr(), kind, rows, n, stride, index.data_ptr(), logp.data_ptr(), t_kind, k,
+                                   *_number_or_rows(temperature), 1 if tail else 0, *_number_or_rows(dloss if grad else 0.0), loss.data_ptr(), dscores.data_ptr() if grad else None, out_kind, n,
                                    torch._C._cuda_getCurrentRawStream(dev.index))
         if status:
             _check(status, "emr_distill")

@@ -47,15 +47,16 @@ def test_refusals_come_before_any_launch():
     assert L.emr_q4_dequantize(ref, FAKE + 1, 1, None) == emr.EMR_ERR_ARG
 
 
-OK = [FAKE, 0, 3, 2, 10, 5, 1, q4(batch=3), None, 0, FAKE, 0, None, 0, None]
+OK = [FAKE, 0, 3, 2, 10, 5, 1, q4(batch=3), None, 0, 2 * FAKE, 0, None, 0, None]
 
 
 @pytest.mark.parametrize("i,v,want", [
     (0, None, emr.EMR_ERR_ARG), (0, FAKE + 2, emr.EMR_ERR_ARG), (1, 3, emr.EMR_ERR_ARG), (2, 0, emr.EMR_ERR_ARG), (2, 2, emr.EMR_ERR_ARG),
     (3, 0, emr.EMR_ERR_ARG), (3, 2 ** 31, emr.EMR_ERR_RANGE), (4, -1, emr.EMR_ERR_ARG), (5, -1, emr.EMR_ERR_ARG), (6, -1, emr.EMR_ERR_ARG),
-    (8, FAKE + 2, emr.EMR_ERR_ARG), (9, 6, emr.EMR_ERR_ARG), (9, -1, emr.EMR_ERR_ARG), (10, None, emr.EMR_ERR_ARG), (10, FAKE + 2, emr.EMR_ERR_ARG),
+    (8, FAKE + 2, emr.EMR_ERR_ARG), (9, 6, emr.EMR_ERR_ARG), (9, -1, emr.EMR_ERR_ARG), (10, None, emr.EMR_ERR_ARG), (10, 2 * FAKE + 2, emr.EMR_ERR_ARG), (10, FAKE + 116, emr.EMR_ERR_ARG), (10, FAKE - 92, emr.EMR_ERR_ARG),
     (11, -1, emr.EMR_ERR_ARG)])
 def test_refusals_of_the_product(i, v, want):
+    """Also an output that lies in x."""
     args = list(OK)
     args[i] = v
     args[7] = C.byref(args[7])
