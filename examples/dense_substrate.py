@@ -54,14 +54,14 @@ def run(genomes: int = 12, patterns: int = 64, steps: int = 30, hidden_depth: in
     g = torch.Generator(device="cuda").manual_seed(seed)
     x = torch.randn(1, patterns, len(sources), device="cuda", generator=g)      # shared by all networks
     wanted = torch.randint(0, w2.shape[1], (patterns,), device="cuda", generator=g).expand(genomes, patterns)
+    target = wanted.reshape(-1).int()
     history = []
     for _ in range(steps):
         h, kept1 = first.forward_train(x)
         scores, kept2 = last.forward_train(h)
-        p = torch.softmax(scores, -1)
-        history.append(float(torch.log(p.gather(-1, wanted[..., None])).mean()))
-        dy = p.scatter_add(-1, wanted[..., None], torch.full_like(p[..., :1], -1.0)) / patterns
-        dh, dw2, db2 = last.backward(dy, kept2)
+        dy, logp, _ = emr.log_probs_grad(scores.view(len(target), -1), target, -1.0 / patterns)
+        history.append(float(logp.mean()))
+        dh, dw2, db2 = last.backward(dy.view_as(scores), kept2)
         _, dw1, db1 = first.backward(dh, kept1)
         for v, d in ((w1, dw1), (b1, db1), (w2, dw2), (b2, db2)):
             v.sub_(rate * d)
