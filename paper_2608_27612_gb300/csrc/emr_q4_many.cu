@@ -25,9 +25,11 @@ namespace {
 namespace cg = cooperative_groups;
 using namespace emr;
 
-constexpr int kUnpack = 8, kScale = 8;  // warps that unpack codes and scale sums; then one that copies x and one that issues
+constexpr int kUnpack = 4, kScale = 8;  // warps that unpack codes and scale sums; then one that copies x and one that issues
+constexpr int kSets = kUnpack / 4, kSums = 32 / kScale;  // blocks of columns unpacked at a time; 16 columns each of a scaling warp's sums
 constexpr int kWarps = kUnpack + kScale + 2, kThreads = 32 * kWarps;
-constexpr int kCodeStages = 4, kScaleStages = 5, kTileStages = 4, kMaxCluster = 8;
+constexpr int kCodeStages = 8 / kSets, kTileStages = 4, kMaxCluster = 8;
+constexpr int kBatch = 512;              // bytes of scales that a warp has copied at a time, of 1024 / group blocks of columns
 constexpr int kColumns = 512;            // of tensor memory: two groups' sums of 128, then the tiles of codes, 64 each
 constexpr int kRowPitch = 80;            // of a row's 64 bytes of codes in shared memory: other banks than the row before
 
@@ -68,7 +70,7 @@ __device__ __forceinline__ void tmem_store32(uint32_t addr, const uint32_t (&r)[
       "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr)
       : "memory");
 }
-__device__ __forceinline__ void tmem_load16(uint32_t addr, uint32_t (&r)[16]) {
+__device__ __forceinline__ void tmem_load16(uint32_t addr, uint32_t* r) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
       : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
@@ -120,17 +122,12 @@ __global__ void __launch_bounds__(kThreads, 1) q4_many_kernel(const __grid_const
   fence_after();
   const uint32_t tmem = tmem_base;
 
-  float sum[4][16];
-#pragma unroll
-  for (int c = 0; c < 4; c++)
-#pragma unroll
-    for (int i = 0; i < 16; i++) sum[c][i] = 0.f;
   const int quarter = warp & 3;                         // rows of tensor memory that a warp may use
-  const int chunks = p.width / 16, each = (chunks + 1) / 2;  // of 16 columns, and a scaling warp's
+  const int chunks = p.width / 16, each = (chunks + kScale / 4 - 1) / (kScale / 4);  // of 16 columns, and a scaling warp's
   const int c0 = (warp - kUnpack) / 4 * each, own = chunks - c0 < each ? chunks - c0 : each;
 
   if (warp < kUnpack) {
-    // every other block of columns
+    // all blocks of columns by turns
     const int tile = block * 8 + quarter * 2, odd = warp >> 2;
     const uint8_t* unit = p.w + b * p.w_batch + (int64_t(tile) * p.blocks + first + odd) * kUnit + lane * 16;
     const int64_t second = int64_t(p.blocks) * kUnit;
@@ -143,18 +140,18 @@ __global__ void __launch_bounds__(kThreads, 1) q4_many_kernel(const __grid_const
         const uint32_t at = to + put * kCodeStage;
         if (one) copy16(at, unit), copy16(at + 8 * kRowPitch, unit + 512);
         if (two) copy16(at + 16 * kRowPitch, unit + second), copy16(at + 24 * kRowPitch, unit + second + 512);
-        unit += 2 * kUnit;
+        unit += kSets * kUnit;
         put = put == kCodeStages - 1 ? 0 : put + 1;
       }
       commit();
     };
 #pragma unroll 1
-    for (int i = 0; i < kCodeStages - 1; i++) issue(first + odd + 2 * i);
+    for (int i = 0; i < kCodeStages - 1; i++) issue(first + odd + kSets * i);
     int get = 0, stage = odd;
     uint32_t round = 0;
     if (stage >= p.stages) stage -= p.stages, round ^= 1;
-    for (int kb = first + odd; kb < last; kb += 2) {
-      issue(kb + 2 * (kCodeStages - 1));
+    for (int kb = first + odd; kb < last; kb += kSets) {
+      issue(kb + kSets * (kCodeStages - 1));
       asm volatile("cp.async.wait_group %0;" ::"n"(kCodeStages - 1) : "memory");
       __syncwarp();
       uint4 c[4];
@@ -182,64 +179,95 @@ __global__ void __launch_bounds__(kThreads, 1) q4_many_kernel(const __grid_const
       fence_before();
       __syncwarp();
       if (lane == 0) arrive(full + 8 * stage);
-      for (int i = 0; i < 2; i++)
+      for (int i = 0; i < kSets; i++)
         if (++stage == p.stages) stage = 0, round ^= 1;
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
   } else if (warp < kUnpack + kScale) {
-    // the scales of its 32 rows, two units, by a ring of the warp's own as the codes
-    const int tile = block * 8 + quarter * 2;
-    const int64_t second = int64_t(p.blocks) * kUnit;
-    const bool copies = lane < 4 * kPer && tile + lane / (2 * kPer) < p.tiles;
-    const uint8_t* from = p.w + b * p.w_batch + (int64_t(tile) * p.blocks + first) * kUnit + kQ4Codes + (lane < 2 * kPer ? lane * 16 : second + (lane - 2 * kPer) * 16);
-    uint8_t* const scales = ring + kUnpack * kCodeStages * kCodeStage + (warp - kUnpack) * (kScaleStages * 64 * kPer);
-    const uint32_t to = smem_at(scales) + lane * 16;
-    int put = 0, get = 0;
-    const auto issue = [&](int kb) {
-      if (kb < last) {
-        if (copies) copy16(to + put * (64 * kPer), from);
-        from += kUnit;
-        put = put == kScaleStages - 1 ? 0 : put + 1;
-      }
-      commit();
+    float sum[kSums][16];  // alive in this branch alone: for all warps they would be spilled
+#pragma unroll
+    for (int c = 0; c < kSums; c++)
+#pragma unroll
+      for (int i = 0; i < 16; i++) sum[c][i] = 0.f;
+    // the scales of its 32 rows, two units, of a batch of blocks while the batch before is used
+    constexpr int kBlocks = 8 / kPer, kPieces = 4 * kPer;
+    const int tile = block * 8 + quarter * 2, piece = lane % kPieces;
+    const bool copies = tile + piece / (2 * kPer) < p.tiles;
+    int ahead = first + lane / kPieces;
+    const uint8_t* from = p.w + b * p.w_batch + ((int64_t(tile) + piece / (2 * kPer)) * p.blocks + ahead) * kUnit + kQ4Codes + piece % (2 * kPer) * 16;
+    uint8_t* const scales = ring + kUnpack * kCodeStages * kCodeStage + (warp - kUnpack) * (2 * kBatch);
+    uint32_t to = smem_at(scales) + lane * 16;
+    const auto issue = [&]() {
+      if (copies && ahead < last) copy16(to, from);
+      ahead += kBlocks, from += kBlocks * kUnit, to ^= kBatch;
     };
-#pragma unroll 1
-    for (int i = 0; i < kScaleStages - 1; i++) issue(first + i);
+    issue();
     const uint8_t* const mine = scales + (lane >> 4) * (32 * kPer) + (q4_scale_at(lane & 15, 0, kQ4Cols / kPer) - kQ4Codes);
     typedef std::conditional_t<kPer == 1, uint16_t, std::conditional_t<kPer == 2, uint32_t, uint2>> Word;
     Ring<2> sums;
     bool ok = true;
+    int in_batch = 0, half = 0;
     for (int kb = first; kb < last && ok; kb++) {
-      issue(kb + kScaleStages - 1);
-      asm volatile("cp.async.wait_group %0;" ::"n"(kScaleStages - 1) : "memory");
-      __syncwarp();
-      const Word now = *reinterpret_cast<const Word*>(mine + get * (64 * kPer));
-      __syncwarp();
-      get = get == kScaleStages - 1 ? 0 : get + 1;
+      if (in_batch == 0) {
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncwarp();
+        issue();
+      }
+      const Word now = *reinterpret_cast<const Word*>(mine + half + in_batch * (64 * kPer));
+      if (++in_batch == kBlocks) in_batch = 0, half ^= kBatch;
 #pragma unroll
       for (int q = 0; q < kPer; q++, sums.next()) {
         if (!(ok = warp_wait(sum_full + 8 * sums.stage, sums.round, stop, 12))) break;
         fence_after();
         const float scale = __uint_as_float(uint32_t(reinterpret_cast<const uint16_t*>(&now)[q]) << 16);
         const uint32_t at = tmem + 128 * sums.stage + 16 * c0 + (uint32_t(quarter * 32) << 16);
+        // 32 columns at a time
 #pragma unroll
-        for (int c = 0; c < 4; c++) {
-          uint32_t v[16];
-          if (c < own) tmem_load16(at + 16 * c, v);
+        for (int c = 0; c < kSums; c += 2) {
+          uint32_t v[2][16];
+          if (c < own) tmem_load16(at + 16 * c, v[0]);
+          if (c + 1 < own) tmem_load16(at + 16 * c + 16, v[1]);
           asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-          if (c == 3) {
+          if (c + 2 >= kSums) {
             fence_before();
             __syncwarp();
             if (lane == 0) bar_arrive(sum_free + 8 * sums.stage);
           }
-          if (c < own) {
 #pragma unroll
-            for (int i = 0; i < 16; i += 2) add_scaled(sum[c][i], sum[c][i + 1], scale, v[i], v[i + 1]);
-          }
+          for (int h = 0; h < 2; h++)
+            if (c + h < own) {
+#pragma unroll
+              for (int i = 0; i < 16; i += 2) add_scaled(sum[c + h][i], sum[c + h][i + 1], scale, v[h][i], v[h][i + 1]);
+            }
         }
       }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
+    if (shares == 1) {
+      const int64_t n = int64_t(block) * 128 + quarter * 32 + lane;
+      const float bias = p.bias && n < p.N ? p.bias[b * p.N + n] : 0.f;
+      const int64_t at = (b * p.M + m0 + c0 * 16) * p.N + n;
+#pragma unroll
+      for (int c = 0; c < kSums; c++) {
+        if (c >= own || n >= p.N) break;
+        float d[16];
+#pragma unroll
+        for (int i = 0; i < 16; i++) sum[c][i] += bias;
+        activate<16, false>(p.act, sum[c], d);
+#pragma unroll
+        for (int i = 0; i < 16; i++)
+          if ((c0 + c) * 16 + i < columns) store_scalar(p.out, p.out_dtype, at + int64_t(c * 16 + i) * p.N, sum[c][i]);
+      }
+    } else {
+      // for the cluster, [column][row], over x: the last of the sums was there after the last product
+      float* const to_all = reinterpret_cast<float*>(sm);
+#pragma unroll
+      for (int c = 0; c < kSums; c++)
+        if (c < own) {
+#pragma unroll
+          for (int i = 0; i < 16; i++) to_all[((c0 + c) * 16 + i) * 128 + quarter * 32 + lane] = sum[c][i];
+        }
+    }
   } else if (warp == kWarps - 2) {
     grid_wait();  // x has been laid out
     const uint8_t* from = p.x + b * p.x_batch + (int64_t(blockIdx.y) * p.blocks + first) * x_stage;
@@ -302,37 +330,9 @@ __global__ void __launch_bounds__(kThreads, 1) q4_many_kernel(const __grid_const
     activate<1, false>(p.act, z, d);
     store_scalar(p.out, p.out_dtype, (b * p.M + m0 + m) * p.N + n, z[0]);
   };
-  const bool scales_sums = warp >= kUnpack && warp < kUnpack + kScale;
-  if (shares == 1) {
-    if (scales_sums) {
-      const int64_t n = int64_t(block) * 128 + quarter * 32 + lane;
-      const float bias = p.bias && n < p.N ? p.bias[b * p.N + n] : 0.f;
-      const int64_t at = (b * p.M + m0 + c0 * 16) * p.N + n;
-#pragma unroll
-      for (int c = 0; c < 4; c++) {
-        if (c >= own || n >= p.N) break;
-        float d[16];
-#pragma unroll
-        for (int i = 0; i < 16; i++) sum[c][i] += bias;
-        activate<16, false>(p.act, sum[c], d);
-#pragma unroll
-        for (int i = 0; i < 16; i++)
-          if ((c0 + c) * 16 + i < columns) store_scalar(p.out, p.out_dtype, at + int64_t(c * 16 + i) * p.N, sum[c][i]);
-      }
-    }
-    return;
-  }
-  // the blocks' sums, [column][row], each block takes every so many columns
-  float* const sums = reinterpret_cast<float*>(sm);
-  if (scales_sums) {
-#pragma unroll
-    for (int c = 0; c < 4; c++)
-      if (c < own) {
-#pragma unroll
-        for (int i = 0; i < 16; i++) sums[((c0 + c) * 16 + i) * 128 + quarter * 32 + lane] = sum[c][i];
-      }
-  }
-  cluster.sync();
+  if (shares == 1) return;
+  const float* const sums = reinterpret_cast<const float*>(sm);
+  cluster.sync();  // each block takes every so many columns
   for (int m = rank + (int(threadIdx.x) >> 7) * shares; m < columns && threadIdx.x < kThreads / 128 * 128; m += shares * (kThreads / 128)) {
     const int n = threadIdx.x & 127;
     float v = 0.f;
@@ -456,7 +456,7 @@ emr_status launch_q4_many(const Q4Product& a, void* ws, int dev, int sms, cudaSt
   int shares = 1;
   for (int s = 2; s <= kMaxCluster; s++)
     if (blocks * s * chunks <= sms && p.blocks / s >= 4) shares = s;
-  const int room = kMostSmem - 1024 - kUnpack * kCodeStages * 32 * kRowPitch - kScale * kScaleStages * 64 * (kQ4Cols / a.w->group), stage = p.parts * p.width * 256;
+  const int room = kMostSmem - 1024 - kUnpack * kCodeStages * 32 * kRowPitch - kScale * 2 * kBatch, stage = p.parts * p.width * 256;
   p.stages = room / stage < kTileStages ? room / stage : kTileStages;
   const int per = kQ4Cols / a.w->group;
   if (a.dtype == EMR_F16)
