@@ -36,7 +36,7 @@ struct Args : Rows {
 template <int kTeam>
 struct List {
   static constexpr int kTeams = kTeam == 32 ? 8 : 1, kMost = kTeam == 32 ? 64 : EMR_MAX_TOP;
-  static constexpr int kBytes = kTeam == 32 ? 288 : 16384;         // of groups of a piece; a warp's rows are one piece
+  static constexpr int kBytes = kTeam == 32 ? 288 : kTeam < 512 ? 2080 : 16384;  // of groups of a piece; rows of less than a cluster are one piece
   int at[kTeams][kMost];                                           // -1: none
   float l[kTeams][kMost], t[kTeams][kMost], s[kTeams][kMost];
   uint32_t bits[kTeams][kBytes / 4];
@@ -80,7 +80,7 @@ __device__ __forceinline__ float load_scalar(const void* p, int dtype, int64_t i
 }
 
 template <typename T, int kTeam>
-__global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? 2 : kTeam == 128 ? 8 : 4) distill_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? 2 : kTeam == 64 ? 16 : kTeam == 128 ? 8 : 4) distill_kernel(const __grid_constant__ Args a) {
   typedef Row<T, kTeam> R;
   constexpr int kG = R::kG, kPiece = List<kTeam>::kBytes;
   __shared__ uint4 scratch[kTeam == 32 ? 1 : 64], slots[kTeam == 512 ? 2 * kMaxCluster : 1];
@@ -98,6 +98,22 @@ __global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? 2 : 
   const bool heat = temperature > 0.f;
   r.per = heat ? fminf(kLog2E / temperature, 3e38f) : 0.f;
 
+  r.ahead();
+  const auto clear = [&](int groups) {
+    for (int w = r.tid; w < (groups + 3) / 4; w += kTeam) bits[w] = 0;
+  };
+  const auto mark = [&](int from, int past) {
+    for (int j = r.tid; j < a.k; j += kTeam) {
+      if (at[j] < r.lo || at[j] - r.lo >= r.count) continue;
+      const int i = at[j] - r.lo + r.skip, b = i / kG - from;
+      if (b < 0 || b >= past - from) continue;
+      const uint32_t bit = 1u << (b % 4 * 8 + i % kG);
+      if (atomicOr(bits + b / 4, bit) & bit) lists.twice[team] = 1;
+    }
+  };
+  const int first_piece = min(r.groups, kPiece);
+  clear(first_piece);
+
   // the list; what cannot be told from it turns the row into NaN
   float wrong = heat ? 0.f : NAN;
   uint32_t l_key = 0, s_key = 0;
@@ -114,36 +130,41 @@ __global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? 2 : 
   }
   if (r.tid == 0) lists.twice[team] = 0;
   s_key = r.team_max(s_key);
+  if (kTeam == 32) r.team_sync();
+  mark(0, first_piece);
+  float m_listed = s_key ? key_score(s_key) : -INFINITY;
   float l_max = 0.f;
   if (!a.tail) {
     l_key = r.team_max(l_key);
     l_max = l_key ? key_score(l_key) : 0.f;
   }
-  float part = 0.f;
-  for (int j = r.tid; j < a.k; j += kTeam) part += t[j] = expf(l[j] - l_max);
-  const float2 sums = r.team_sum(make_float2(part, wrong));
-  const float t_sum = (!a.tail && sums.x > 0.f ? 1.f : sums.x) + sums.y;
+  const auto weight = [&](int j, float m) { return s[j] > -INFINITY ? fast_exp2(fmaxf((s[j] - m) * r.per, kFar)) : 0.f; };
+  float part = 0.f, z_first = 0.f;  // sums of t, and of the listed entries' w relative to their own maximum if each stands there once
+  for (int j = r.tid; j < a.k; j += kTeam) {
+    part += t[j] = expf(l[j] - l_max);
+    if (r.blocks == 1) z_first += weight(j, m_listed);
+  }
+  const float2 sums = r.team_sum(make_float2(part + wrong, z_first));
+  if (kTeam == 32) r.team_sync();  // a block's sums are barriers
+  z_first = sums.y;
+  const float t_sum = !a.tail && sums.x > 0.f ? 1.f : sums.x;
   float t_scale = 1.f, l_base = 0.f;  // log t_j = l_j - l_base
   if (!a.tail && sums.x > 0.f) t_scale = __fdiv_rn(1.f, sums.x), l_base = l_max + logf(sums.x);
 
   // the rest's sums
   Stat rest;
-  float m_listed = s_key ? key_score(s_key) : -INFINITY;
-  for (bool again = false;; again = true) {
+  bool again = false;
+  for (;; again = true) {
     r.begin();
     for (int from = 0; from < r.groups; from += kPiece) {
       const int past = r.groups - from < kPiece ? r.groups : from + kPiece;
-      if (from) r.team_sync();
-      for (int w = r.tid; w < (past - from + 3) / 4; w += kTeam) bits[w] = 0;
-      r.team_sync();
-      for (int j = r.tid; j < a.k; j += kTeam) {
-        if (at[j] < r.lo || at[j] - r.lo >= r.count) continue;
-        const int i = at[j] - r.lo + r.skip, b = i / kG - from;
-        if (b < 0 || b >= past - from) continue;
-        const uint32_t bit = 1u << (b % 4 * 8 + i % kG);
-        if (atomicOr(bits + b / 4, bit) & bit) lists.twice[team] = 1;
+      if (from || again) {
+        r.team_sync();
+        clear(past - from);
+        r.team_sync();
+        mark(from, past);
+        r.team_sync();
       }
-      r.team_sync();
       AddRest<R> add{r, reinterpret_cast<const uint8_t*>(bits) - from};
       r.each(add, from ? from : r.head, past, from == 0);
     }
@@ -167,11 +188,15 @@ __global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? 2 : 
         if (at[i] == at[j]) return false;
     return true;
   };
-  const auto weight = [&](int j) { return s[j] > -INFINITY ? fast_exp2(fmaxf((s[j] - m) * r.per, kFar)) : 0.f; };
-  part = 0.f;
-  for (int j = r.tid; j < a.k; j += kTeam)
-    if (mine(j)) part += weight(j);
-  float z_listed = r.team_sum(make_float2(part, 0.f)).x;
+  float z_listed;
+  if (r.blocks == 1 && !twice && !again) {
+    z_listed = z_first * (s_key ? fast_exp2(fmaxf((m_listed - m) * r.per, kFar)) : 0.f);
+  } else {
+    part = 0.f;
+    for (int j = r.tid; j < a.k; j += kTeam)
+      if (mine(j)) part += weight(j, m);
+    z_listed = r.team_sum(make_float2(part, 0.f)).x;
+  }
   if (r.blocks > 1) {
     const float own = z_listed;
     z_listed = 0.f;
@@ -181,9 +206,9 @@ __global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? 2 : 
   const float inverse = empty ? 0.f : __fdiv_rn(1.f, z), p_rest = z_rest * inverse, p_listed = z_listed * inverse;
   const float t_rest = a.tail && has_rest ? fmaxf(1.f - t_sum, 0.f) : 0.f;
 
+  part = 0.f;
+  float log_z = 0.f;
   if (a.loss && r.rank == 0) {
-    part = 0.f;
-    float log_z = 0.f;
     if (r.tid < a.k) {  // the others need no logarithm
       log_z = empty ? 0.f : logf(z);
       for (int j = r.tid; j < a.k; j += kTeam) {
@@ -191,23 +216,27 @@ __global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? 2 : 
         if (w > 0.f) part += w * ((l[j] - l_base) - (s[j] - m > -INFINITY ? __fdiv_rn(s[j] - m, temperature) - log_z : -INFINITY));
       }
     }
+  }
+  // joined behind the gradient, where a barrier is wanted anyway
+  const auto write_loss = [&]() {
     float loss = r.team_sum(make_float2(part, 0.f)).x;
-    if (r.tid == 0) {
+    if (r.tid == 0 && r.rank == 0) {
       if (t_rest > 0.f) {
         const float log_p = z_listed <= z_rest ? -log1pf(__fdiv_rn(z_listed, z_rest)) : __fdiv_rn(rest.m - m, temperature) + logf(rest.s) - log_z;
         loss += t_rest * (log1pf(-t_sum) - log_p);
       }
       a.loss[row] = isnan(t_sum) ? NAN : loss;
     }
-  }
-  if (!a.dscores) return;
+  };
+  if (!a.dscores) return write_loss();
 
   const float dl = (a.dloss ? a.dloss[row] : a.dloss_all) * (heat ? fminf(__fdiv_rn(1.f, temperature), 3e38f) : 1.f);
   const float coef = has_rest ? dl * __fdiv_rn(t_sum * p_rest - t_rest * p_listed, rest.s) : 0.f * t_sum;
   const float m_rest = has_rest ? rest.m : 0.f;
   const typename R::Out o = r.out(a, row);
   r.put(o, Slope{m_rest, r.per, coef});
-  r.team_sync();
+  if (a.loss) write_loss();
+  if (!a.loss || kTeam == 32) r.team_sync();
   const float mass = t_sum + t_rest;
   for (int j = r.tid; j < a.k; j += kTeam) {
     if (!mine(j)) continue;
@@ -216,7 +245,7 @@ __global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? 2 : 
       for (int i = j + 1; i < a.k; i++)
         if (at[i] == at[j]) own += t[i];
     const bool on = s[j] > -INFINITY;
-    store_scalar(o.p, o.dtype, at[j] - r.lo, dl * (on ? mass * (weight(j) * inverse) - own * t_scale : 0.f * mass));
+    store_scalar(o.p, o.dtype, at[j] - r.lo, dl * (on ? mass * (weight(j, m) * inverse) - own * t_scale : 0.f * mass));
   }
 }
 
@@ -226,8 +255,9 @@ emr_status distill(Args a, int sms, cudaStream_t st) {
   static int fit[kMaxCluster + 1];
   std::call_once(once, [&] { clusters_at_once(distill_kernel<float, 512>, 512, fit); });
   int cluster;
-  const int team = plan(a, a.k <= List<32>::kMost ? 32 : 128, sizeof(T), sms, fit, &cluster);
+  const int team = plan(a, a.k <= List<32>::kMost ? 32 : 64, sizeof(T), sms, fit, &cluster);
   return team == 32    ? launch_rows(distill_kernel<T, 32>, a, team, cluster, st)
+         : team == 64  ? launch_rows(distill_kernel<T, 64>, a, team, cluster, st)
          : team == 128 ? launch_rows(distill_kernel<T, 128>, a, team, cluster, st)
          : team == 256 ? launch_rows(distill_kernel<T, 256>, a, team, cluster, st)
                        : launch_rows(distill_kernel<T, 512>, a, team, cluster, st);

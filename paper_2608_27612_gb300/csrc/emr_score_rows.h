@@ -128,6 +128,10 @@ struct Row {
     else v.u = *reinterpret_cast<const uint4*>(global + i);
     return v;
   }
+  // Asks for the slice's first groups, 128 bytes for each thread, while something else is read.
+  __device__ __forceinline__ void ahead() const {
+    if (tid * (128 / int(sizeof(T))) < count) asm volatile("prefetch.global.L2 [%0];" ::"l"(global + tid * (128 / int(sizeof(T)))));
+  }
   // The same where what lies around the scores may not be read.
   __device__ static __noinline__ uint4 fetch_part(const T* global, int i, int count) {
     Group<T> v;
@@ -158,22 +162,26 @@ struct Row {
   }
   // fn(v, g) of an array of groups g, g + kTeam ... that lie in the slice as a whole, or of one group, for those from first
   // (head or more) to before past, and the first one of all where with_head: after the others.
+  template <int kN, typename Fn>
+  __device__ __forceinline__ void turn_of(Fn& fn, int& g, const uint4*& from) const {
+    Group<T> v[kN];
+#pragma unroll
+    for (int u = 0; u < kN; u++) v[u].u = from[u * kTeam];
+    if (top_infinite) {
+#pragma unroll
+      for (int u = 0; u < kN; u++) infinite(v[u]);
+    }
+    fn(v, g);
+    g += kN * kTeam, from += kN * kTeam;
+  }
   template <typename Fn>
   __device__ __forceinline__ void each(Fn& fn, int first, int past, bool with_head) const {
     const int whole = (skip + count) / kG < past ? (skip + count) / kG : past, turns = (whole - first) / kTurn;
     int g = first + tid;
     const uint4* from = reinterpret_cast<const uint4*>(global + (g * kG - skip));
-    for (int i = 0; i < turns; i++) {
-      Group<T> v[kAhead];
-#pragma unroll
-      for (int u = 0; u < kAhead; u++) v[u].u = from[u * kTeam];
-      if (top_infinite) {
-#pragma unroll
-        for (int u = 0; u < kAhead; u++) infinite(v[u]);
-      }
-      fn(v, g);
-      g += kTurn, from += kTurn;
-    }
+    for (int i = 0; i < turns; i++) turn_of<kAhead>(fn, g, from);
+    const int left = whole - first - turns * kTurn;
+    if (left >= 2 * kTeam) turn_of<2>(fn, g, from);
     const int end = past + (with_head ? head : 0);
     if (g >= end) return;
     Group<T> next = masked(g == past ? 0 : g);
@@ -336,13 +344,16 @@ struct Row {
     o.whole = (reinterpret_cast<uintptr_t>(o.p) - uintptr_t(skip) * o.size) % piece == 0;
     return o;
   }
+  __device__ __forceinline__ static void pair_as(float* d, float x, float y) { d[0] = x, d[1] = y; }
+  __device__ __forceinline__ static void pair_as(__nv_bfloat16* d, float x, float y) { *reinterpret_cast<__nv_bfloat162*>(d) = __floats2bfloat162_rn(x, y); }
+  __device__ __forceinline__ static void pair_as(__half* d, float x, float y) { *reinterpret_cast<__half2*>(d) = __floats2half2_rn(x, y); }
   template <typename D>
   __device__ __forceinline__ static void store_whole(uint8_t* p, const float (&v)[kG]) {
     constexpr int kBytes = kG * int(sizeof(D));
     uint32_t w[kBytes / 4];
     D* const d = reinterpret_cast<D*>(w);
 #pragma unroll
-    for (int j = 0; j < kG; j++) d[j] = D(v[j]);
+    for (int j = 0; j < kG; j += 2) pair_as(d + j, v[j], v[j + 1]);
     if (kBytes == 8) __stcs(reinterpret_cast<uint2*>(p), make_uint2(w[0], w[1]));
 #pragma unroll
     for (int k = 0; k < kBytes / 16; k++)
@@ -440,6 +451,10 @@ void clusters_at_once(K kernel, int threads, int* fit) {
   }
 }
 
+// Smaller teams where rows are many and short: what a row costs beside its entries, about 250 instructions a warp for the
+// sums, 500 in a gradient and 750 in distillation, counts for each of its warps, and more rows are at hand while one waits.
+// Gradients of bfloat16 by 64 and by 128 threads: 2000 x 5460 13.7 and 17.4 us, 8000 x 1364 23 and 34; best 20 of float32
+// 2000 x 1364 10.1 and 11.3, 1000 x 1364 8.2 and 7.3, 4000 x 5460 38 and 33.
 // The team and cluster of a row, and the slice of its blocks: the same with and without a gradient, so that the values are.
 // least: the smallest team that will do; size: bytes of a score.
 inline int plan(Rows& a, int least, int size, int sms, const int* fit, int* cluster) {
@@ -448,6 +463,7 @@ inline int plan(Rows& a, int least, int size, int sms, const int* fit, int* clus
   if (a.n <= 8192) {
     if (least <= 8 && a.n <= 512 && a.rows >= 32 * sms) return 8;
     if (least <= 32 && a.n <= 1024 && a.rows >= 16 * sms) return 32;
+    if (least <= 64 && a.n * size <= 12288 && a.rows >= 8 * sms) return 64;
     return least <= 128 && a.rows >= 4 * sms ? 128 : 256;
   }
   for (int c = 2; c <= kMaxCluster; c++)

@@ -15,6 +15,7 @@
 // scores) find their k-th entry first, by a histogram of each byte of (score, index).
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
+#include <float.h>
 
 #include <mutex>
 #include <type_traits>
@@ -40,11 +41,11 @@ struct Args : Rows {
 // Shared memory of the search for the best.
 template <int kTeam>
 struct Best {
-  static constexpr int kTeams = kTeam == 32 ? 8 : 1, kCap = kTeam == 32 ? 128 : kTeam == 512 ? 2048 : 1024;
+  static constexpr int kTeams = kTeam == 32 ? 8 : 1, kCap = kTeam == 32 ? 128 : kTeam == 64 ? 512 : kTeam == 512 ? 2048 : 1024;
   static constexpr int kTop = kTeam <= 128 ? 32 : EMR_MAX_TOP;
   u64 list[kTeams][kCap], sorted[kTeams][kTop], found[kTeams];
   alignas(16) uint32_t counts[kTeams][256];  // read 16 bytes at a time
-  int size[kTeams][2], hits[kTeams];
+  int size[kTeams][2];
   uint16_t who[kTeams][kTeam];
 };
 
@@ -53,7 +54,7 @@ template <typename T, int kTeam>
 struct Search : Row<T, kTeam> {
   typedef Row<T, kTeam> R;
   using R::blocks, R::cluster, R::exchange, R::floats, R::groups, R::head, R::kG, R::masked,
-      R::kWarps, R::lane, R::lo, R::own, R::rank, R::row_sync, R::skip, R::team_max, R::team_sync, R::tid, R::warp;
+      R::kWarps, R::lane, R::lo, R::own, R::rank, R::row_sync, R::skip, R::team_max, R::team_sync, R::tid, R::value, R::warp, R::global;
   using R::R;
 
   template <typename V>
@@ -146,40 +147,29 @@ struct Search : Row<T, kTeam> {
     return max(low, 1u);
   }
   // The entries from `least` on to the list of the row's first block (dropped past its room, but counted): the groups of
-  // the threads whose own largest is one of them are shared out over the team.
+  // the threads whose own largest is one of them are shared out over their warp.
   __device__ int collect(u64 least, Best<kTeam>& b, int team, int round) {
     const uint32_t low = uint32_t(least >> 32);
-    const float low_score = key_score(low);
+    const float low_score = low > 1 ? key_score(low) : -FLT_MAX;
     const bool hit = order_key(own.m) >= low;
     const uint32_t hits = __ballot_sync(0xffffffffu, hit);
-    int many;
-    if (kTeam == 32) {
-      many = __popc(hits);
-      if (hit) b.who[team][__popc(hits & ((1u << lane) - 1))] = uint16_t(tid);
-      __syncwarp();
-    } else {
-      int place = 0;
-      if (tid == 0) b.hits[team] = 0;
-      __syncthreads();
-      if (lane == 0 && hits) place = atomicAdd(b.hits + team, __popc(hits));
-      place = __shfl_sync(0xffffffffu, place, 0);
-      if (hit) b.who[team][place + __popc(hits & ((1u << lane) - 1))] = uint16_t(tid);
-      __syncthreads();
-      many = b.hits[team];
-    }
+    uint16_t* const who = b.who[team] + warp * 32;
+    if (hit) who[__popc(hits & ((1u << lane) - 1))] = uint16_t(tid);
+    __syncwarp();
     u64* const to = of_block(b.list[team], 0);
     int* const places = of_block(b.size[team] + round, 0);
-    const int each_has = (groups + kTeam - 1) / kTeam;  // groups of a thread at most, the first of all as the last of one
-    for (int i = tid; i < many * each_has; i += kTeam) {
-      const int h = i / each_has, at = head + b.who[team][h] + (i - h * each_has) * kTeam;
+    const unsigned each_has = unsigned(groups + kTeam - 1) / kTeam;  // groups of a thread at most, the first of all as the last of one
+    for (unsigned i = lane; i < __popc(hits) * each_has; i += 32) {
+      const unsigned h = i / each_has;
+      const int at = head + who[h] + int(i - h * each_has) * kTeam, g = at == groups ? 0 : at;
       if (at >= groups + head) continue;
-      const int g = at == groups ? 0 : at;
       const Group<T> v = masked(g);
+      uint32_t reach = 0;
 #pragma unroll
-      for (int j = 0; j < kG; j++) {
-        const float s = v.get(j);
-        if (low > 1 && !(s >= low_score)) continue;
-        const u64 e = entry(order_key(s), lo + g * kG - skip + j);
+      for (int j = 0; j < kG; j++) reach |= uint32_t(v.get(j) >= low_score) << j;
+      for (; reach; reach &= reach - 1) {  // few: read again
+        const int from = g * kG - skip + __ffs(int(reach)) - 1;
+        const u64 e = entry(order_key(value(global[from])), lo + from);
         if (e < least) continue;
         const int place = atomicAdd(places, 1);
         if (place < b.kCap) to[place] = e;
@@ -314,7 +304,7 @@ struct Same {
 enum Ask { kSums, kTop, kGradient };
 
 template <typename T, int kTeam, int kAsk>
-__global__ void __launch_bounds__(kTeam <= 32 ? 256 : kTeam, kTeam == 512 ? 2 : kTeam == 128 ? 8 : 4) log_probs_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(kTeam <= 32 ? 256 : kTeam, kTeam == 512 ? 2 : kTeam == 64 ? 20 : kTeam == 128 ? 10 : 4) log_probs_kernel(const __grid_constant__ Args a) {
   constexpr int kRows = kTeam <= 32 ? 256 / kTeam : 1;  // of a block
   __shared__ uint4 scratch[kTeam <= 32 ? 1 : 64], slots[kTeam == 512 ? 2 * kMaxCluster : 1];
   __shared__ std::conditional_t<kAsk == kTop, Best<kTeam>, uint32_t> best;
@@ -411,13 +401,14 @@ const int* fits() {
 
 template <typename T, int kAsk>
 emr_status log_probs(Args a, int sms, cudaStream_t st) {
-  const int least = kAsk != kTop ? 8 : a.top <= Best<32>::kTop ? 32 : a.top <= Best<128>::kTop ? 128 : 256;
+  const int least = kAsk != kTop ? 8 : a.top <= Best<32>::kTop ? 32 : a.top <= Best<128>::kTop ? 64 : 256;
   int cluster;
   const int team = plan(a, least, sizeof(T), sms, fits(), &cluster);
   if constexpr (kAsk != kTop) {
     if (team == 8) return launch_rows(log_probs_kernel<T, 8, kAsk>, a, team, cluster, st);
   }
   return team == 32    ? launch_rows(log_probs_kernel<T, 32, kAsk>, a, team, cluster, st)
+         : team == 64  ? launch_rows(log_probs_kernel<T, 64, kAsk>, a, team, cluster, st)
          : team == 128 ? launch_rows(log_probs_kernel<T, 128, kAsk>, a, team, cluster, st)
          : team == 256 ? launch_rows(log_probs_kernel<T, 256, kAsk>, a, team, cluster, st)
                        : launch_rows(log_probs_kernel<T, 512, kAsk>, a, team, cluster, st);
