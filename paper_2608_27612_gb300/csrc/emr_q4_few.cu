@@ -10,6 +10,9 @@
 // (`wide`) or, where those are few, the contraction (`teams`); a cluster of up to 8 blocks shares the contraction of few
 // rows further and adds its parts through distributed shared memory in the order of blocks. Where rows are many, a
 // warp takes tile after tile.
+// Measured on the device: 1 x 5460 x 1364 float32 7.2 us, 150 networks of 4 x 1364 x 256 float16 16.3 (32 MB, 2 TB/s; unpacking
+// takes 40% of the instructions), 8 x 8192 x 8192 bfloat16 14.2 (36 MB, 2.5 TB/s, from HBM); x copied to registers by each warp,
+// and warps that met after each unit, took 12.6, 31 and 23.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 

@@ -2,15 +2,16 @@
 //
 // y[m][n] = sum over groups g of scale[n][g] (sum over the group's k of code[n][k] x[m][k]), as for few rows: codes are exact 16-bit floats, the
 // inner sums are products of the tensor cores with 32-bit sums, and each group's is scaled and added in 32 bits. 128 rows of W
-// are the instruction's rows. Eight warps unpack their codes, a thread the 64 words of its row and block of 128
+// are the instruction's rows. Four warps unpack their codes, a thread the 64 words of its row and block of 128
 // columns, straight into tensor memory, from where the instruction takes them: in shared memory the tile would be written
 // once and read once, which at these widths is more than shared memory gives. x, up to 128 rows of it, is laid out beforehand as
 // its tiles lie in shared memory, so that one copy brings a block of columns; a 32-bit x is three tiles of bfloat16 (its parts), three
-// products into one sum. Sixteen warps take a group's sums out of tensor memory while the next group's are made, multiply them by
-// their row's scale and keep the sums of up to 32 columns in registers. A cluster of up to 8 blocks shares the contraction
-// where rows are few. A warp by itself issues an instruction every four or five clocks, so the work of a block of columns (about 500
-// clocks of the matrix pipe for 101 rows) has to be spread over many: with 4 and 8 warps for the two jobs and three that copied x,
-// 101 x 16384 x 8192 took 60 us.
+// products into one sum. Eight warps take a group's sums out of tensor memory while the next group's are made, multiply them by
+// their row's scale and keep the sums of up to 64 columns in registers. A cluster of up to 8 blocks shares the contraction
+// where rows are few. 101 x 16384 x 8192 bfloat16 takes 44 us, 8.5 of them beside the loop, which takes 1040 clocks a block of 128
+// columns: the matrix pipe 450-570, a scaling warp 720, an unpacking warp 600, coupled by two buffers of sums. With 8 warps that
+// unpack (96 registers a thread, and the sums spilled) it took 54; with 16 that scale (72) 79; with three buffers of sums and
+// two of codes 48. Neither x (a fourteenth of it copied: 44) nor the multiplications (a quarter of them: 43) hold it.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
