@@ -767,7 +767,8 @@ emr_status emr_q4_size(int32_t batch, int64_t rows, int64_t cols, int32_t group,
 
 /* Quantise src[b * batch_stride + r * row_stride + c * col_stride] (of dtype) into q: a group's scale is its largest magnitude / 7,
  * rounded to bfloat16 (nearest even), and a code the entry / scale, rounded to the nearest (even) whole number. A group
- * whose scale would be below 2^-126 is held as 0; one with an infinity or NaN has scale NaN. */
+ * whose scale would be below 2^-126 is held as 0; one with an infinity or NaN has scale NaN. src lies outside q's memory, as do
+ * the other arrays of these calls (EMR_ERR_ARG). */
 emr_status emr_q4_quantize(const void *src, int32_t dtype, int64_t batch_stride, int64_t row_stride,
                            int64_t col_stride, const emr_q4 *q, void *stream);
 
@@ -781,11 +782,12 @@ emr_status emr_q4_pack(const int8_t *codes, int64_t batch_stride, int64_t row_st
 emr_status emr_q4_dequantize(const emr_q4 *q, void *out, int32_t dtype, void *stream);
 
 /* out[b][m][n] = act(sum_k x[b][m][k] w[b][n][k] + bias[b][n]): x is x_batch matrices [rows][w.cols] of dtype with the given
- * strides (elements), out dense [batch][rows][w.rows] of out_dtype, outside x's memory; an operand with batch 1 serves every b. Products of codes
+ * strides (elements), out dense [batch][rows][w.rows] of out_dtype, outside x's and w's memory; an operand with batch 1 serves every b. Products of codes
  * with x are exact in all types of x, sums are in 32 bits, each group's scaled once. bias: device float [batch][w.rows] or NULL.
  * act: EMR_ACT_*, as in emr_q8_matmul. Made for the rows that a layer answers at a time, where reading w counts. ws: room of
- * emr_q4_matmul_room bytes (the same arguments; 0 for few rows: up to 16, 8 of type EMR_F32, twice that for 2^26 weights or more), 16-byte aligned. Waits on the device are bounded; emr_device_error tells of one that gave up (none is expected). EMR_ERR_CAPACITY: ws
- * is too small. */
+ * emr_q4_matmul_room bytes (the same arguments; 0 for few rows: up to 16, 8 of type EMR_F32, twice that for 2^26 weights or more),
+ * 16-byte aligned. Waits on the device are bounded; emr_device_error tells of one that gave up (none is expected).
+ * EMR_ERR_CAPACITY: ws is too small. */
 emr_status emr_q4_matmul_room(const void *x, int32_t dtype, int32_t x_batch, int64_t rows, int64_t batch_stride,
                               int64_t row_stride, int64_t col_stride, const emr_q4 *w, size_t *bytes);
 emr_status emr_q4_matmul(const void *x, int32_t dtype, int32_t x_batch, int64_t rows, int64_t batch_stride,

@@ -85,10 +85,13 @@ emr_status launch(Args a, const emr_q4* q, cudaStream_t st) {
   return launch_plain(q4_kernel<kFrom>, dim3(unsigned(blocks < (1 << 20) ? blocks : 1 << 20)), 256, st, a);
 }
 
-emr_status sizes_ok(const emr_q4* q) {
+emr_status sizes_ok(const emr_q4* q, size_t* bytes) {
   if (!q4_ok(q)) return EMR_ERR_ARG;
-  size_t bytes;
-  return emr_q4_size(q->batch, q->rows, q->cols, q->group, &bytes);
+  return emr_q4_size(q->batch, q->rows, q->cols, q->group, bytes);
+}
+// Whether matrices of q's rows and `cols` columns with these strides lie in q's memory.
+bool in_data(const emr_q4* q, size_t bytes, const void* p, int size, int64_t cols, int64_t batch_stride, int64_t row_stride, int64_t col_stride) {
+  return overlap(q->data, int64_t(bytes), 1, p, (q->batch - 1) * batch_stride + (q->rows - 1) * row_stride + (cols - 1) * col_stride + 1, size);
 }
 
 }  // namespace
@@ -104,9 +107,11 @@ extern "C" emr_status emr_q4_size(int32_t batch, int64_t rows, int64_t cols, int
 
 extern "C" emr_status emr_q4_quantize(const void* src, int32_t dtype, int64_t batch_stride, int64_t row_stride, int64_t col_stride,
                                       const emr_q4* q, void* stream) {
-  const emr_status ok = sizes_ok(q);
+  size_t bytes;
+  const emr_status ok = sizes_ok(q, &bytes);
   if (ok != EMR_OK) return ok;
-  if (!src || !dtype_ok(dtype) || reinterpret_cast<uintptr_t>(src) % dtype_bytes(dtype) || batch_stride < 0 || row_stride < 0 || col_stride < 0)
+  if (!src || !dtype_ok(dtype) || reinterpret_cast<uintptr_t>(src) % dtype_bytes(dtype) || batch_stride < 0 || row_stride < 0 || col_stride < 0 ||
+      in_data(q, bytes, src, dtype_bytes(dtype), q->cols, batch_stride, row_stride, col_stride))
     return EMR_ERR_ARG;
   Args a{};
   a.src = src, a.dtype = dtype, a.batch_stride = batch_stride, a.row_stride = row_stride, a.col_stride = col_stride;
@@ -115,10 +120,12 @@ extern "C" emr_status emr_q4_quantize(const void* src, int32_t dtype, int64_t ba
 
 extern "C" emr_status emr_q4_pack(const int8_t* codes, int64_t batch_stride, int64_t row_stride, int64_t col_stride, const void* scales,
                                   int64_t s_batch, int64_t s_row, int64_t s_col, const emr_q4* q, void* stream) {
-  const emr_status ok = sizes_ok(q);
+  size_t bytes;
+  const emr_status ok = sizes_ok(q, &bytes);
   if (ok != EMR_OK) return ok;
   if (!codes || !scales || reinterpret_cast<uintptr_t>(scales) % 2 || batch_stride < 0 || row_stride < 0 || col_stride < 0 || s_batch < 0 ||
-      s_row < 0 || s_col < 0)
+      s_row < 0 || s_col < 0 || in_data(q, bytes, codes, 1, q->cols, batch_stride, row_stride, col_stride) ||
+      in_data(q, bytes, scales, 2, (q->cols + q->group - 1) / q->group, s_batch, s_row, s_col))
     return EMR_ERR_ARG;
   Args a{};
   a.src = codes, a.batch_stride = batch_stride, a.row_stride = row_stride, a.col_stride = col_stride;
@@ -127,9 +134,12 @@ extern "C" emr_status emr_q4_pack(const int8_t* codes, int64_t batch_stride, int
 }
 
 extern "C" emr_status emr_q4_dequantize(const emr_q4* q, void* out, int32_t dtype, void* stream) {
-  const emr_status ok = sizes_ok(q);
+  size_t bytes;
+  const emr_status ok = sizes_ok(q, &bytes);
   if (ok != EMR_OK) return ok;
-  if (!out || !dtype_ok(dtype) || reinterpret_cast<uintptr_t>(out) % dtype_bytes(dtype)) return EMR_ERR_ARG;
+  if (!out || !dtype_ok(dtype) || reinterpret_cast<uintptr_t>(out) % dtype_bytes(dtype) ||
+      in_data(q, bytes, out, dtype_bytes(dtype), q->cols, q->rows * q->cols, q->cols, 1))
+    return EMR_ERR_ARG;
   Args a{};
   a.dtype = dtype, a.out = out;
   return launch<2>(a, q, static_cast<cudaStream_t>(stream));

@@ -38,25 +38,28 @@ def test_refusals_come_before_any_launch():
         assert L.emr_q4_dequantize(C.byref(q), FAKE, 0, None) == emr.EMR_ERR_ARG
         assert L.emr_q4_matmul(FAKE, 0, 1, 2, 10, 5, 1, C.byref(q), None, 0, FAKE, 0, None, 0, None) == emr.EMR_ERR_ARG
     ref = C.byref(q4())
-    for args in ((None, 0, 20, 5, 1), (FAKE, 3, 20, 5, 1), (FAKE + 2, 0, 20, 5, 1), (FAKE, 0, -1, 5, 1), (FAKE, 0, 20, -5, 1), (FAKE, 0, 20, 5, -1)):
+    far = 3 * FAKE
+    for args in ((None, 0, 20, 5, 1), (far, 3, 20, 5, 1), (far + 2, 0, 20, 5, 1), (far, 0, -1, 5, 1), (far, 0, 20, -5, 1), (far, 0, 20, 5, -1),
+                 (FAKE + 16, 0, 20, 5, 1), (FAKE - 56, 0, 20, 5, 1)):
         assert L.emr_q4_quantize(*args, ref, None) == emr.EMR_ERR_ARG
-    for args in ((None, 20, 5, 1, FAKE, 4, 1, 1), (FAKE, 20, 5, 1, None, 4, 1, 1), (FAKE, 20, 5, 1, FAKE + 1, 4, 1, 1), (FAKE, 20, -5, 1, FAKE, 4, 1, 1),
-                 (FAKE, 20, 5, 1, FAKE, 4, -1, 1)):
+    for args in ((None, 20, 5, 1, far, 4, 1, 1), (far, 20, 5, 1, None, 4, 1, 1), (far, 20, 5, 1, far + 1, 4, 1, 1), (far, 20, -5, 1, far, 4, 1, 1),
+                 (far, 20, 5, 1, far, 4, -1, 1), (FAKE, 20, 5, 1, far, 4, 1, 1), (far, 20, 5, 1, FAKE, 4, 1, 1)):
         assert L.emr_q4_pack(*args, ref, None) == emr.EMR_ERR_ARG
-    assert L.emr_q4_dequantize(ref, None, 0, None) == L.emr_q4_dequantize(ref, FAKE, 7, None) == emr.EMR_ERR_ARG
-    assert L.emr_q4_dequantize(ref, FAKE + 1, 1, None) == emr.EMR_ERR_ARG
+    assert L.emr_q4_dequantize(ref, None, 0, None) == L.emr_q4_dequantize(ref, far, 7, None) == emr.EMR_ERR_ARG
+    assert L.emr_q4_dequantize(ref, far + 1, 1, None) == L.emr_q4_dequantize(ref, FAKE, 0, None) == emr.EMR_ERR_ARG
 
 
-OK = [FAKE, 0, 3, 2, 10, 5, 1, q4(batch=3), None, 0, 2 * FAKE, 0, None, 0, None]
+OK = [3 * FAKE, 0, 3, 2, 10, 5, 1, q4(batch=3), None, 0, 2 * FAKE, 0, None, 0, None]
 
 
 @pytest.mark.parametrize("i,v,want", [
-    (0, None, emr.EMR_ERR_ARG), (0, FAKE + 2, emr.EMR_ERR_ARG), (1, 3, emr.EMR_ERR_ARG), (2, 0, emr.EMR_ERR_ARG), (2, 2, emr.EMR_ERR_ARG),
+    (0, None, emr.EMR_ERR_ARG), (0, 3 * FAKE + 2, emr.EMR_ERR_ARG), (1, 3, emr.EMR_ERR_ARG), (2, 0, emr.EMR_ERR_ARG), (2, 2, emr.EMR_ERR_ARG),
     (3, 0, emr.EMR_ERR_ARG), (3, 2 ** 31, emr.EMR_ERR_RANGE), (4, -1, emr.EMR_ERR_ARG), (5, -1, emr.EMR_ERR_ARG), (6, -1, emr.EMR_ERR_ARG),
-    (8, FAKE + 2, emr.EMR_ERR_ARG), (9, 6, emr.EMR_ERR_ARG), (9, -1, emr.EMR_ERR_ARG), (10, None, emr.EMR_ERR_ARG), (10, 2 * FAKE + 2, emr.EMR_ERR_ARG), (10, FAKE + 116, emr.EMR_ERR_ARG), (10, FAKE - 92, emr.EMR_ERR_ARG),
+    (8, FAKE + 2, emr.EMR_ERR_ARG), (9, 6, emr.EMR_ERR_ARG), (9, -1, emr.EMR_ERR_ARG), (10, None, emr.EMR_ERR_ARG), (10, 2 * FAKE + 2, emr.EMR_ERR_ARG), (10, 3 * FAKE + 116, emr.EMR_ERR_ARG), (10, 3 * FAKE - 92, emr.EMR_ERR_ARG),
+    (10, FAKE, emr.EMR_ERR_ARG), (10, FAKE - 4, emr.EMR_ERR_ARG),
     (11, -1, emr.EMR_ERR_ARG)])
 def test_refusals_of_the_product(i, v, want):
-    """Also an output that lies in x."""
+    """Also an output that lies in x or w."""
     args = list(OK)
     args[i] = v
     args[7] = C.byref(args[7])
