@@ -95,6 +95,7 @@ def distill(s, index, l, T=1.0, tail=True, with_gradient=True):
     g = (t.sum() + t_rest) * p
     np.add.at(g, index, -t)
     if t_rest > 0 and lr > -np.inf:
-        g[rest] -= t_rest * np.exp(lp[rest] - lr)
+        e = np.exp(lp[rest] - m)  # lr = m + log(sum) has nothing left of the logarithm where m is -1e38
+        g[rest] -= t_rest * e / e.sum()
     g[~(v > -np.inf)] = 0.0
     return terms.sum(), g / T, np.abs(terms).sum()
