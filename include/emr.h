@@ -785,7 +785,7 @@ emr_status emr_q4_dequantize(const emr_q4 *q, void *out, int32_t dtype, void *st
  * strides (elements), out dense [batch][rows][w.rows] of out_dtype, outside x's and w's memory; an operand with batch 1 serves every b. Products of codes
  * with x are exact in all types of x, sums are in 32 bits, each group's scaled once. bias: device float [batch][w.rows] or NULL.
  * act: EMR_ACT_*, as in emr_q8_matmul. Made for the rows that a layer answers at a time, where reading w counts. ws: room of
- * emr_q4_matmul_room bytes (the same arguments; 0 for few rows: up to 16, 8 of type EMR_F32, twice that for 2^26 weights or more),
+ * emr_q4_matmul_room bytes (the same arguments; 0 for few rows: up to 16, 8 of type EMR_F32, twice that for up to 512 columns),
  * 16-byte aligned. Waits on the device are bounded; emr_device_error tells of one that gave up (none is expected).
  * EMR_ERR_CAPACITY: ws is too small. */
 emr_status emr_q4_matmul_room(const void *x, int32_t dtype, int32_t x_batch, int64_t rows, int64_t batch_stride,

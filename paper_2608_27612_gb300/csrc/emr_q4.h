@@ -67,11 +67,12 @@ struct Q4Product {
   int32_t out_dtype;
 };
 // Whether it is one for the kernel of many rows (emr_q4_many.cu), the bytes that that needs, and its launch. Measured, in us, few and
-// many: 4096 x 4096 with 16 rows of bfloat16 7.8 and 13.0, 24 rows 19 and 14, 10 rows of float32 21 and 16; 16384 x 8192, where
-// the kernel of few rows keeps every SM's copies busy, 32 rows 46 and 61, 64 rows 88 and 66, 16 rows of float32 77 and 80.
+// many: 4096 x 4096 with 16 rows of bfloat16 7.9 and 10.6, 20 rows 19 and 11, 10 rows of float32 21 and 12; 16384 x 8192 with 16 rows
+// 31 and 36, 20 rows 41 and 37, 10 rows of float32 52 and 49; 100 networks of 1364 x 256, where a block's set-up counts for two blocks of
+// columns, 24 rows 31 and 38, 32 rows 37 and 39, 16 rows of float32 34 and 43.
 inline bool q4_is_many(const Q4Product& a) {
-  const bool large = double(a.w->batch) * double(a.w->rows) * double(a.w->cols) >= double(1 << 26);
-  return a.rows > (a.dtype == EMR_F32 ? (large ? 16 : 8) : (large ? 32 : 16));
+  const int most = a.dtype == EMR_F32 ? 8 : 16;
+  return a.rows > (a.w->cols <= 512 ? 2 * most : most);
 }
 size_t q4_many_room(const Q4Product& a);
 emr_status launch_q4_many(const Q4Product& a, void* ws, int dev, int sms, cudaStream_t st);

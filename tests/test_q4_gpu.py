@@ -180,3 +180,22 @@ def test_refusals():
     assert emr.q4_matmul(x[:, :0], q).shape == (2, 0, 10)
     out = torch.full((2, 3, 10), 7.0, device="cuda")
     assert emr.q4_matmul(x, q, out=out) is out and torch.equal(out, emr.q4_matmul(x, q))
+
+
+@pytest.mark.parametrize("m,k", [(17, 600), (33, 500), (129, 700), (70, 8200)])
+def test_many_rows_of_batches(m, k):
+    """The kernel of many rows with biases, activations, operands that all share, strides, and rows of W that fill no tile."""
+    codes, scales = weights(3, 77, k, 32, 18)
+    scales = (scales.float() * 0.01).bfloat16()
+    b = torch.randn(3, 77, device="cuda")
+    for act, dtype in enumerate(TYPES + TYPES):
+        out = TYPES[(act + 1) % 3]
+        check(x_of(3, m, k, 19, dtype), codes, scales, 32, b, act, out)
+        check(x_of(1, m, k, 20, dtype), codes, scales, 32, b, act, out)
+        check(x_of(3, m, k, 21, dtype), codes[:1], scales[:1], 32, b, act, out)
+    wide = x_of(2, m, 2 * k + 5, 22, torch.float32)
+    codes, scales = weights(2, 260, k, 128, 23)
+    for dtype in TYPES:
+        v = wide.to(dtype)
+        for x in (v[:, :, 1:1 + k], v[:, :, :2 * k:2], v[:, :, 8:8 + k], v[:, :1, :k].expand(2, m, k)):
+            check(x, codes, scales, 128)

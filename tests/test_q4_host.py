@@ -74,8 +74,9 @@ def room(dtype, rows, x=FAKE, row_stride=8, q=None):
 
 def test_room():
     """Nothing for few rows; else x in tiles of rows rounded up to 16, whole blocks of 128 columns, three parts of float32."""
-    assert room(emr.EMR_F32, 8) == room(emr.EMR_BF16, 16, row_stride=5) == (emr.EMR_OK, 0)
-    assert room(emr.EMR_F32, 9) == (emr.EMR_OK, 3 * 16 * 256) and room(emr.EMR_F32, 65) == (emr.EMR_OK, 2 * 3 * 48 * 256)
+    assert room(emr.EMR_F32, 16) == room(emr.EMR_BF16, 32, row_stride=5) == room(emr.EMR_F32, 8, q=q4(cols=513)) == (emr.EMR_OK, 0)
+    assert room(emr.EMR_F16, 16, q=q4(cols=513)) == (emr.EMR_OK, 0) and room(emr.EMR_F16, 17, q=q4(cols=513)) == (emr.EMR_OK, 5 * 32 * 256)
+    assert room(emr.EMR_F32, 17) == (emr.EMR_OK, 3 * 32 * 256) and room(emr.EMR_F32, 9, q=q4(cols=513)) == (emr.EMR_OK, 5 * 3 * 16 * 256) and room(emr.EMR_F32, 65) == (emr.EMR_OK, 2 * 3 * 48 * 256)
     assert room(emr.EMR_BF16, 100, row_stride=5) == room(emr.EMR_F16, 100) == (emr.EMR_OK, 112 * 256)
     assert room(emr.EMR_F16, 129, q=q4(cols=129)) == (emr.EMR_OK, 2 * 2 * 80 * 256)
     assert room(emr.EMR_F32, 0)[0] == room(3, 1)[0] == room(0, 1, q=q4(group=1))[0] == emr.EMR_ERR_ARG
