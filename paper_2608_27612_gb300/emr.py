@@ -1202,36 +1202,36 @@ class LogProbs:
     top_logp: torch.Tensor | None
 
 
-def _rows_of(scores):
-    """(scores [rows, n] with neighbouring columns, rows, n, row stride, emr_dtype) of scores [rows, n] or [n]."""
-    if scores.dim() == 1:
-        scores = scores.unsqueeze(0)
-    rows, n = scores.shape
+def _scores(scores):
+    """(rows, n, row stride, emr_dtype) of scores [rows, n] or [n]; the stride is None where columns are no neighbours and a
+    copy is wanted."""
+    if not isinstance(scores, torch.Tensor) or not scores.is_cuda:
+        raise ValueError("scores: a tensor [rows, n] or [n] on the GPU is wanted")
+    shape = scores.shape
+    if len(shape) == 2:
+        rows, n = shape
+        stride, col = scores.stride()
+    elif len(shape) == 1:
+        rows, n = 1, shape[0]
+        stride, col = n, scores.stride(0)
+    else:
+        raise ValueError("scores: a tensor [rows, n] or [n] on the GPU is wanted")
+    if n < 1:
+        raise ValueError("scores: rows of at least one entry are wanted")
     kind = _DTYPES.get(scores.dtype)
     if kind is None:
         _dtype(scores.dtype, "scores")
-    stride, col = scores.stride()
-    if col != 1 and n > 1:
-        scores, stride = scores.contiguous(), n
-    return scores, rows, n, stride, kind
-
-
-def _check_scores(scores):
-    if not isinstance(scores, torch.Tensor) or scores.dim() not in (1, 2) or not scores.is_cuda:
-        raise ValueError("scores: a tensor [rows, n] or [n] on the GPU is wanted")
-    if scores.shape[-1] < 1:
-        raise ValueError("scores: rows of at least one entry are wanted")
-    return scores.shape[0] if scores.dim() == 2 else 1
+    return rows, n, stride if col == 1 or n == 1 else None, kind
 
 
 def _check_number_or_rows(v, rows: int, dev, what: str):
-    if isinstance(v, torch.Tensor):
+    if type(v) is not float and isinstance(v, torch.Tensor):
         _check_per_row(v, rows, torch.float32, dev, what)
 
 
 def _number_or_rows(v):
     """(address, number) of a float parameter that is given for each row or for all."""
-    return (v.data_ptr(), 0.0) if isinstance(v, torch.Tensor) else (None, float(v))
+    return (None, v) if type(v) is float else (v.data_ptr(), 0.0) if isinstance(v, torch.Tensor) else (None, float(v))
 
 
 def _check_targets(targets, rows: int, dev):
@@ -1244,7 +1244,7 @@ def log_probs(scores, targets=None, temperature=1.0, top=0, stream=None) -> LogP
     """emr_log_probs: log probabilities of the answers targets (int32 [rows], below 0: none) under scores [rows, n] (or [n];
     float32, bfloat16, float16), the rows' entropies, and the `top` (up to MAX_TOP) best answers of each row with
     theirs. temperature: a number, or a float32 tensor [rows]."""
-    rows = _check_scores(scores)
+    rows, n, stride, kind = _scores(scores)
     dev = scores.device
     if not 0 <= top <= MAX_TOP:
         raise ValueError("top: 0 to %d is wanted, got %r" % (MAX_TOP, top))
@@ -1255,15 +1255,16 @@ def log_probs(scores, targets=None, temperature=1.0, top=0, stream=None) -> LogP
     if away is not None:
         with away:
             return log_probs(scores, targets, temperature, top)
-    scores, rows, n, stride, kind = _rows_of(scores)
+    if stride is None:
+        scores, stride = scores.contiguous(), n
     entropy = torch.empty(rows, dtype=torch.float32, device=dev)
     logp = index = best = tp = lp = ip = bp = None
     if targets is not None:
-        logp = torch.empty(rows, dtype=torch.float32, device=dev)
+        logp = torch.empty_like(entropy)
         tp, lp = targets.data_ptr(), logp.data_ptr()
     if top:
-        index = torch.empty((rows, top), dtype=torch.int32, device=dev)
         best = torch.empty((rows, top), dtype=torch.float32, device=dev)
+        index = torch.empty_like(best, dtype=torch.int32)
         ip, bp = index.data_ptr(), best.data_ptr()
     if rows:
         hp, heat = _number_or_rows(temperature)
@@ -1278,7 +1279,7 @@ def log_probs_grad(scores, targets, dlogp, dentropy=None, temperature=1.0, out_d
     """emr_log_probs_grad: (dscores, logp, entropy), the gradient of sum(dlogp logp + dentropy entropy) in the shape of scores,
     of out_dtype (None: the scores' type), with the values that log_probs gives. dlogp and dentropy: numbers, or float32
     tensors [rows]; dentropy None: 0. The loss of a step of cross entropy is -logp with dlogp = -1 / rows."""
-    rows = _check_scores(scores)
+    rows, n, stride, kind = _scores(scores)
     dev, shape = scores.device, scores.shape
     _check_targets(targets, rows, dev)
     _check_number_or_rows(dlogp, rows, dev, "dlogp")
@@ -1291,10 +1292,11 @@ def log_probs_grad(scores, targets, dlogp, dentropy=None, temperature=1.0, out_d
     if away is not None:
         with away:
             return log_probs_grad(scores, targets, dlogp, dentropy, temperature, out_dtype)
-    scores, rows, n, stride, kind = _rows_of(scores)
+    if stride is None:
+        scores, stride = scores.contiguous(), n
     dscores = torch.empty(shape, dtype=out_dtype or scores.dtype, device=dev)
     logp = torch.empty(rows, dtype=torch.float32, device=dev)
-    entropy = torch.empty(rows, dtype=torch.float32, device=dev)
+    entropy = torch.empty_like(logp)
     if rows:
         status = lib().emr_log_probs_grad(scores.data_ptr(), kind, rows, n, stride, targets.data_ptr(), *_number_or_rows(temperature),
                                           *_number_or_rows(dlogp), *_number_or_rows(dentropy), logp.data_ptr(), entropy.data_ptr(),
@@ -1307,7 +1309,7 @@ def log_probs_grad(scores, targets, dlogp, dentropy=None, temperature=1.0, out_d
 # ---- distillation ------------------------------------------------------------------------------
 
 def _distill(scores, index, logp, dloss, temperature, tail, out_dtype, stream):
-    rows = _check_scores(scores)
+    rows, n, stride, kind = _scores(scores)
     dev, shape = scores.device, scores.shape
     if not isinstance(index, torch.Tensor) or index.dtype is not torch.int32 or index.dim() != 2 or index.shape[0] != rows or \
             index.device != dev or not 1 <= index.shape[1] <= MAX_TOP:
@@ -1326,7 +1328,8 @@ def _distill(scores, index, logp, dloss, temperature, tail, out_dtype, stream):
     if away is not None:
         with away:
             return _distill(scores, index, logp, dloss, temperature, tail, out_dtype, None)
-    scores, rows, n, stride, kind = _rows_of(scores)
+    if stride is None:
+        scores, stride = scores.contiguous(), n
     index, logp = index.contiguous(), logp.contiguous()
     dscores = torch.empty(shape, dtype=out_dtype or scores.dtype, device=dev) if grad else None
     loss = torch.empty(rows, dtype=torch.float32, device=dev)
