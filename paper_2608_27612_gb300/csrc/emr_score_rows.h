@@ -478,7 +478,7 @@ inline bool aligned(const void* p, int bytes) { return reinterpret_cast<uintptr_
 
 inline emr_status check_scores(const void* scores, int32_t dtype, int32_t rows, int64_t n, int64_t row_stride) {
   if (rows < 1 || n < 1 || !scores || !dtype_ok(dtype) || row_stride < 0 || !aligned(scores, dtype_bytes(dtype))) return EMR_ERR_ARG;
-  return n > INT32_MAX - (1 << 20) || rows > (1 << 27) ? EMR_ERR_RANGE : EMR_OK;
+  return n > (int64_t(1) << 31) - (1 << 20) || rows > (1 << 27) ? EMR_ERR_RANGE : EMR_OK;
 }
 
 }  // namespace rows

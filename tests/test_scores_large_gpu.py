@@ -131,3 +131,40 @@ def test_many_rows_with_strange_values(n, dtype, tail):
         assert np.array_equal(num(a.top_index[r]), OS.best(sn, 8)), r
         g1 = OS.log_p_gradient(sn, t, 1.0, 0.0)
         assert np.all(np.abs(num(dt[r]) - g1) <= 2e-5 * (np.exp(p) + (np.arange(n) == t)) + 2.0 ** -126), r
+
+
+def test_the_longest_row():
+    """2^31 - 2^20 entries, all but four of them equal: sums known in closed form."""
+    n = 2 ** 31 - 2 ** 20
+    s = torch.full((1, n), -1.0, device="cuda", dtype=torch.bfloat16)
+    places = [n // 2, n - 1, 2 ** 30 + 7, 0]
+    values = np.array([5.0, 5.0, 4.0, 3.0])
+    for i, v in zip(places, values):
+        s[0, i] = v
+    target = torch.tensor([n - 1], dtype=torch.int32, device="cuda")
+    z = np.exp(values).sum() + (n - 4) * np.exp(-1.0)
+    lp, low = values - np.log(z), -1.0 - np.log(z)
+    h = -(np.exp(lp) * lp).sum() - (n - 4) * np.exp(low) * low
+    a = emr.log_probs(s, target, top=4)
+    assert a.top_index[0].tolist() == places
+    tol = 6e-6 + 2.4e-7 * abs(lp)
+    assert abs(float(a.logp[0]) - lp[1]) <= tol[1] and np.all(np.abs(num(a.top_logp[0]) - lp) <= tol) and abs(float(a.entropy[0]) - h) < 1e-5 * (1 + h)
+    ds, logp, entropy = emr.log_probs_grad(s, target, -1.0)
+    assert torch.equal(logp, a.logp) and torch.equal(entropy, a.entropy)
+    at = [1, 5, 2 ** 30, n // 2 + 1, n - 2]
+    assert np.all(np.abs(num(ds[0, at]) - np.exp(low)) <= (2e-5 + HALF) * np.exp(low))
+    want = np.exp(lp) - np.array([0, 1, 0, 0])
+    assert np.all(np.abs(num(ds[0, places]) - want) <= 2e-5 * (np.exp(lp) + [0, 1, 0, 0]) + HALF * np.abs(want))
+    del ds
+    index = torch.tensor([[n - 1, n // 2, 0]], dtype=torch.int32, device="cuda")
+    t = np.array([0.4, 0.3, 0.2])
+    l = torch.from_numpy(np.log(t)).float().cuda()[None]
+    ds, loss = emr.distill_grad(s, index, l, 1.0)
+    p, t = np.exp(lp[[1, 0, 3]]), np.exp(num(l[0]))
+    t_r, p_r = 1 - t.sum(), 1 - p.sum()
+    terms = np.append(t * (np.log(t) - np.log(p)), t_r * (np.log(t_r) - np.log(p_r)))
+    assert abs(float(loss[0]) - terms.sum()) <= 4e-5 * (1 + np.abs(terms).sum())
+    assert np.all(np.abs(num(ds[0, [n - 1, n // 2, 0]]) - (p - t)) <= 2e-5 * (p + t) + HALF * np.abs(p - t))
+    e_z = np.exp(-1.0) / (z - np.exp(values[[0, 1, 3]]).sum())
+    want = e_z * (p_r * t.sum() - t_r * p.sum())
+    assert np.all(np.abs(num(ds[0, at]) - want) <= (2e-5 * 2 + 110 * 2.0 ** -24 + HALF) * abs(want) + 2e-5 * e_z)
