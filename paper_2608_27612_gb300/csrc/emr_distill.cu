@@ -12,7 +12,7 @@
 // L1 or L2 and writes once; listed entries are written over after it, k of them. Bound by memory for many rows; for
 // few, by the chain list - scores of its entries - bits - pass - sums.
 // Measured on the device: 2000 x 5460 bfloat16 with lists of 50 19 us (44 MB; a row costs 750 instructions a warp beside its
-// entries), 1000 x 87380 float16 with 64 84 (350 MB, 4.1 TB/s; issue 52%, exponentials 45% of their unit), 250 x 1364 float32
+// entries), 1000 x 87380 float16 with 64 78 (350 MB, 4.5 TB/s; issue 55%, exponentials 48% of their unit), 250 x 1364 float32
 // with 16 6.2.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
@@ -102,6 +102,7 @@ __global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? 2 : 
   r.per = heat ? fminf(kLog2E / temperature, 3e38f) : 0.f;
 
   r.ahead();
+  r.asks = a.dscores != nullptr;
   const auto clear = [&](int groups) {
     for (int w = r.tid; w < (groups + 3) / 4; w += kTeam) bits[w] = 0;
   };
@@ -237,6 +238,7 @@ __global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? 2 : 
   const float coef = has_rest ? dl * __fdiv_rn(t_sum * p_rest - t_rest * p_listed, rest.s) : 0.f * t_sum;
   const float m_rest = has_rest ? rest.m : 0.f;
   const typename R::Out o = r.out(a, row);
+  r.asks = false;
   r.put(o, Slope{m_rest, r.per, coef});
   if (a.loss) write_loss();
   if (!a.loss || kTeam == 32) r.team_sync();

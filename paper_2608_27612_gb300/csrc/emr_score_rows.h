@@ -94,6 +94,8 @@ struct Row {
   bool inside;       // the rest of its first and last group lies in the scores' memory, too
   uint4* scratch;    // [2][32], by turns: a turn's values are read by all before the next but one writes
   uint4* slots;      // [2][kMaxCluster]
+  bool asks;         // in a cluster's first pass of two: for the turn after the next, in L2, by one instruction while a turn is read
+                     // (gradients of 512 x 87380 float32 79 -> 73 us, distillation of 1000 x 87380 float16 84 -> 78; the best answers gain nothing)
   bool top_infinite; // only the entries of +infinity count, as score 0
   float per;         // log2(e) / T
   Stat own;          // of the thread's entries
@@ -113,7 +115,7 @@ struct Row {
     skip = int(reinterpret_cast<uintptr_t>(global) % 16 / sizeof(T));
     groups = (skip + count + kG - 1) / kG;
     inside = global - skip >= scores && global - skip + int64_t(groups) * kG <= scores + (a.rows - 1) * a.row_stride + a.n;
-    top_infinite = false;
+    top_infinite = asks = false;
     head = skip ? 1 : 0;
   }
   __device__ __forceinline__ float value(T v) const {
@@ -179,7 +181,13 @@ struct Row {
     const int whole = (skip + count) / kG < past ? (skip + count) / kG : past, turns = (whole - first) / kTurn;
     int g = first + tid;
     const uint4* from = reinterpret_cast<const uint4*>(global + (g * kG - skip));
-    for (int i = 0; i < turns; i++) turn_of<kAhead>(fn, g, from);
+    const int all = (skip + count) / kG;
+    for (int i = 0; i < turns; i++) {
+      const int at = first + (i + 2) * kTurn;
+      if (kTeam == 512 && asks && tid == 0 && at < all)
+        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(global + (int64_t(at) * kG - skip)), "r"((all - at < kTurn ? all - at : kTurn) * 16) : "memory");
+      turn_of<kAhead>(fn, g, from);
+    }
     const int left = whole - first - turns * kTurn;
     if (left >= 2 * kTeam) turn_of<2>(fn, g, from);
     const int end = past + (with_head ? head : 0);

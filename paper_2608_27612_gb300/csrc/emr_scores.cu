@@ -15,7 +15,7 @@
 // scores) find their k-th entry first, by a histogram of each byte of (score, index).
 // Measured on the device: 4000 x 5460 float32 with its best 20 33 us (87 MB, 2.7 TB/s; 7 instructions an entry for the
 // sums and as many again for the search: issue 57% of the time, the rest latency), 24 x 349524 bfloat16 with its best 100 19 (six
-// meetings of a cluster), gradients of 16000 x 340 bfloat16 10.6 and of 512 x 87380 float32 with the entropy's 79 (358 MB, 4.5 TB/s), one
+// meetings of a cluster), gradients of 16000 x 340 bfloat16 10.6 and of 512 x 87380 float32 with the entropy's 73 (358 MB, 4.9 TB/s), one
 // row of 1364 4.8.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
@@ -329,6 +329,7 @@ __global__ void __launch_bounds__(kTeam <= 32 ? 256 : kTeam, kTeam == 512 ? 2 : 
   const float dlogp = kAsk == kGradient ? (a.dlogp ? a.dlogp[row] : a.dlogp_all) : 0.f;
   const float dentropy = kAsk == kGradient ? (a.dentropy ? a.dentropy[row] : a.dentropy_all) : 0.f;
   r.per = greedy ? 0.f : fminf(kLog2E / temperature, 3e38f);
+  r.asks = kAsk == kGradient;
 
   Stat all;
   for (bool again = false;; again = true) {
@@ -380,6 +381,7 @@ __global__ void __launch_bounds__(kTeam <= 32 ? 256 : kTeam, kTeam == 512 ? 2 : 
     const float k1 = inverse * dentropy * kLn2, k0 = inverse * (uncertain ? fmaf(dentropy, entropy - log_z, da) : da);
     if (kTeam < 32 && !there) return;
     const typename Row<T, kTeam>::Out o = r.out(a, row);
+    r.asks = false;
     if (empty || isnan(da + dentropy)) {
       r.put(o, Same{empty && !isnan(da + dentropy) ? 0.f : NAN});
       return;
