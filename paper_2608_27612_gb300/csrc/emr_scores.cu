@@ -46,7 +46,7 @@ struct Args : Rows {
 template <int kTeam>
 struct Best {
   static constexpr int kTeams = kTeam == 32 ? 8 : 1, kCap = kTeam == 32 ? 128 : kTeam == 64 ? 512 : kTeam == 512 ? 2048 : 1024;
-  static constexpr int kTop = kTeam <= 128 ? 32 : EMR_MAX_TOP;
+  static constexpr int kTop = kTeam <= 64 ? 32 : kTeam == 128 ? 128 : EMR_MAX_TOP;
   u64 list[kTeams][kCap], sorted[kTeams][kTop], found[kTeams];
   alignas(16) uint32_t counts[kTeams][256];  // read 16 bytes at a time
   int size[kTeams][2];
@@ -407,7 +407,11 @@ const int* fits() {
 
 template <typename T, int kAsk>
 emr_status log_probs(Args a, int sms, cudaStream_t st) {
-  const int least = kAsk != kTop ? 8 : a.top <= Best<32>::kTop ? 32 : a.top <= Best<128>::kTop ? 64 : 256;
+  // Longer lists by more threads, as each part of 32 entries is a warp's; but rows that are many keep an SM busy with 128. By 128 and
+  // 256 threads, in us: 40 best of 4000 x 5460 float32 41 and 54, of 1000 x 2000 9.6 and 12; 100 best of 16000 x 340 163 and 257, 4000 x
+  // 5460 74 and 75, 2000 x 8000 59 and 50, 700 x 5460 25 and 19.
+  const int longer = a.top <= 64 || (a.top <= Best<128>::kTop && a.rows >= 24 * sms) ? 128 : 256;
+  const int least = kAsk != kTop ? 8 : a.top <= Best<32>::kTop ? 32 : longer;
   int cluster;
   const int team = plan(a, least, sizeof(T), sms, fits(), &cluster);
   if constexpr (kAsk != kTop) {

@@ -168,3 +168,25 @@ def test_the_longest_row():
     e_z = np.exp(-1.0) / (z - np.exp(values[[0, 1, 3]]).sum())
     want = e_z * (p_r * t.sum() - t_r * p.sum())
     assert np.all(np.abs(num(ds[0, at]) - want) <= (2e-5 * 2 + 110 * 2.0 ** -24 + HALF) * abs(want) + 2e-5 * e_z)
+
+
+@pytest.mark.parametrize("rows,n,dtype", [(700, 45, torch.bfloat16), (700, 701, torch.float32), (1300, 1365, torch.bfloat16), (640, 5461, torch.float16),
+                                          (3700, 340, torch.float32), (3700, 1031, torch.bfloat16)])
+@pytest.mark.parametrize("top", [33, 64, 65, 128, 129])
+def test_long_lists_of_many_rows(rows, n, dtype, top):
+    """The best of rows with masked and equal entries, and with fewer entries than are asked for."""
+    g = torch.Generator(device="cuda").manual_seed(top)
+    s = torch.randn(rows, n, device="cuda", generator=g).to(dtype)
+    s[torch.rand(rows, n, device="cuda", generator=g) < 0.2] = float("-inf")
+    s[0], s[1, 20:], s[2], s[3] = float("-inf"), float("-inf"), 0.5, torch.arange(n, device="cuda") / 64
+    s[4] = -s[3]
+    a = emr.log_probs(s, top=top)
+    v = torch.nan_to_num(s.float(), neginf=-1e30)
+    order = torch.sort(v, dim=1, descending=True, stable=True)
+    k = min(top, n)
+    want = torch.where(order.values[:, :k] > -1e29, order.indices[:, :k], -1)
+    assert torch.equal(a.top_index[:, :k].long(), want) and bool((a.top_index[:, k:] == -1).all())
+    z = torch.log_softmax(s.double(), 1).nan_to_num(nan=float("-inf"))
+    lp = torch.where(want >= 0, z.gather(1, want.clamp(min=0)), float("-inf"))
+    ok = (a.top_logp[:, :k].double() - lp).abs() <= 6e-6 + 2.4e-7 * lp.abs()
+    assert bool((ok | (a.top_logp[:, :k] == lp)).all())
