@@ -205,8 +205,13 @@ struct Row {
   template <typename Fn>
   __device__ __forceinline__ void each(Fn& fn) const { each(fn, head, groups, true); }
 
+  // The lanes of the thread's team within its warp. The teams of a warp part where one row takes a branch and another does not
+  // (an infinity, a temperature of 0), so what they do together names no lane of another team.
+  __device__ __forceinline__ static uint32_t mates() {
+    return kTeam < 32 ? ((1u << (kTeam & 31)) - 1) << (threadIdx.x & 31 & -kTeam) : 0xffffffffu;
+  }
   __device__ __forceinline__ void team_sync() const {
-    if (kTeam <= 32) __syncwarp();
+    if (kTeam <= 32) __syncwarp(mates());
     else __syncthreads();
   }
   __device__ void row_sync() {
@@ -217,7 +222,7 @@ struct Row {
   __device__ uint32_t team_max(uint32_t v) {
     if (kTeam < 32) {
 #pragma unroll
-      for (int o = kTeam / 2; o; o >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
+      for (int o = kTeam / 2; o; o >>= 1) v = max(v, __shfl_xor_sync(mates(), v, o));
       return v;
     }
     v = __reduce_max_sync(0xffffffffu, v);
@@ -229,7 +234,7 @@ struct Row {
   }
   __device__ static float2 warp_sum(float2 v) {
 #pragma unroll
-    for (int o = kTeam < 32 ? kTeam / 2 : 16; o; o >>= 1) v.x += __shfl_xor_sync(0xffffffffu, v.x, o), v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
+    for (int o = kTeam < 32 ? kTeam / 2 : 16; o; o >>= 1) v.x += __shfl_xor_sync(mates(), v.x, o), v.y += __shfl_xor_sync(mates(), v.y, o);
     return v;
   }
   __device__ float2 team_sum(float2 v) {

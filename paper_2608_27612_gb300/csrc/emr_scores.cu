@@ -316,7 +316,7 @@ __global__ void __launch_bounds__(kTeam <= 32 ? 256 : kTeam, kTeam == 512 ? 2 : 
   int64_t row = kTeam < 512 ? int64_t(blockIdx.x) * kRows + team : int64_t(blockIdx.x / cg::this_cluster().num_blocks());
   const bool there = row < a.rows;
   if (kTeam == 32 && !there) return;
-  if (kTeam < 32 && !there) row = a.rows - 1;  // a warp's teams go together: this one writes nothing
+  if (kTeam < 32 && !there) row = a.rows - 1;  // a team without a row takes the last one's and writes nothing
   Search<T, kTeam> r(a, row, scratch, slots);
   if constexpr (kAsk == kTop) {
     if (r.tid < 2) best.size[team][r.tid] = 0;
