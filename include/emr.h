@@ -839,7 +839,8 @@ emr_status emr_log_probs_grad(const void *scores, int32_t dtype, int32_t rows, i
  *              probabilities; loss = sum_j t_j (log t_j - log p[index_j])
  *   tail != 0  what the list leaves over is one more answer: t_j = exp(teacher_j), t_r = max(0, 1 - sum t), p_r = the sum of p
  *              over entries that are not listed; loss as above plus t_r (log t_r - log p_r). t_r is 0 where
- *              no entry that is not listed is left
+ *              no entry that is not listed is left; it is good to 2.5e-11 + 2^-23 t_r of these t, so that a
+ *              list that leaves 1e-7 over is as good as another
  * Terms with t = 0 are 0. With M = sum t + t_r, the gradient of sum_r dloss[r] loss[r] is dloss (M p_i - t_i) / T for listed
  * entries, dloss p_i (M - t_r / p_r) / T for others and 0 for masked ones; neither rises nor falls with T by itself
  * (T * T is often put into dloss). The teacher has no gradient. A row in which an index is n or more, a listed

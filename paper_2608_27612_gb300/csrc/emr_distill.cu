@@ -5,7 +5,7 @@
 // list leaves over counts as one more answer ("tail"), plus t_r (log t_r - log p_r), with t_r = 1 - sum t_j and p_r the
 // sum of p over the rest, the entries that are not listed. dL/ds_i is M p_i - t_i for a listed entry, M = sum t + t_r, and
 // for one of the rest, e_i (M / Z - t_r / z_r) = e_i / z_r (p_r sum t - t_r p_l), p_l being 1 - p_r: without a small difference of
-// sums near 1. For the same reason the rest has sums of its own, in which listed entries are left out by a bit for
+// sums near 1, but for t_r itself, whose sum is kept in two parts (split_exp). For the same reason the rest has sums of its own, in which listed entries are left out by a bit for
 // each entry (one byte of shared memory is looked at for 8 of them), and its own maximum, so that a
 // rest of 1e-30 has a softmax like any other.
 // As for log probabilities, one pass over the row for the sums and, for the gradient, a second one that finds it in
@@ -82,6 +82,39 @@ __device__ __forceinline__ float load_scalar(const void* p, int dtype, int64_t i
   return float(static_cast<const __half*>(p)[i]);
 }
 
+// A teacher's probability e^l, all of it and as high + low. What a list leaves over, 1 - sum t, is often 1e-5 and less, of 32-bit values
+// that are each off by 2^-25 and more; high is a multiple of 2^-22, sums of which are exact up to 4 (beyond that nothing is left over), and
+// low the rest of e^l to 6e-13 e^l: sums of up to 256 parts of at most 2^-23 are off by at most 12 2^-24 2^-15 = 2.2e-11.
+// e^l = 2^(k / 2) e^r, |r| <= ln 2 / 4, with k ln 2 / 2 taken off in two parts (Cody and Waite) and the series r + r^2 (12 + 4 r + r^2) / 24 in two
+// floats a value (Dekker's sums and products), from r^5 on in one: 0.5 us of 2000 lists of 50, where exp in 64 bits takes 4.4.
+struct Parts {
+  float all, high, low;
+};
+__device__ __forceinline__ Parts split_exp(float l) {
+  const float all = expf(l);
+  if (!(all < 2.f)) return {all, all, 0.f};
+  const float high = __fsub_rn(__fadd_rn(all, 3.f), 3.f);
+  if (l < -40.f) return {all, 0.f, all};
+  const float k = rintf(l * (2.f * kLog2E));
+  const float r0 = __fmaf_rn(-k, 0x1.62e4p-2f, l), r = __fmaf_rn(-k, 0x1.7f7d1cp-21f, r0), r_low = __fmaf_rn(-k, 0x1.7f7d1cp-21f, r0 - r);
+  const float tail = __fmaf_rn(__fmaf_rn(__fmaf_rn(r, 1.f / 40320.f, 1.f / 5040.f), r, 1.f / 720.f), r, 1.f / 120.f);
+  const float s = __fmul_rn(r, r), s_low = __fmaf_rn(r, r, -s);
+  const float v = __fmaf_rn(4.f, r, 12.f), v_low = __fmaf_rn(4.f, r, 12.f - v);
+  const float w = __fadd_rn(v, s), w_low = ((v - w) + s) + (v_low + s_low);
+  const float p = __fmul_rn(s, w), p_low = __fmaf_rn(s, w, -p) + __fmaf_rn(s, w_low, s_low * w);
+  constexpr float kPart = 1.f / 24.f, kPartLow = float(1. / 24. - double(kPart));
+  const float q = __fmul_rn(p, kPart), q_low = __fmaf_rn(p, kPart, -q) + __fmaf_rn(p, kPartLow, p_low * kPart);
+  const float a = __fadd_rn(1.f, r), a_low = r - (a - 1.f);
+  const float b = __fadd_rn(a, q), b_low = q - (b - a);
+  const float rest = __fmaf_rn(tail, s * s * r, q_low) + __fmaf_rn(r_low, b, a_low + b_low);
+  constexpr float kRoot = 1.41421356f, kRootLow = float(1.41421356237309504880 - double(kRoot));
+  const int n = int(k);
+  const float root = n & 1 ? kRoot : 1.f, root_low = n & 1 ? kRootLow : 0.f;
+  const float e = __fmul_rn(b, root), e_low = __fmaf_rn(b, root, -e) + __fmaf_rn(b, root_low, rest * root);
+  const float scale = __uint_as_float(uint32_t((n >> 1) + 127) << 23);
+  return {all, high, __fmaf_rn(e, scale, -high) + e_low * scale};
+}
+
 template <typename T, int kTeam>
 __global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? 2 : kTeam == 64 ? 16 : kTeam == 128 ? 8 : 4) distill_kernel(const __grid_constant__ Args a) {
   typedef Row<T, kTeam> R;
@@ -143,17 +176,24 @@ __global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? 2 : 
     l_max = l_key ? key_score(l_key) : 0.f;
   }
   const auto weight = [&](int j, float m) { return s[j] > -INFINITY ? fast_exp2(fmaxf((s[j] - m) * r.per, kFar)) : 0.f; };
-  float part = 0.f, z_first = 0.f;  // sums of t, and of the listed entries' w relative to their own maximum if each stands there once
+  // sums of t, in two parts where 1 - sum t is wanted, and of the listed entries' w relative to their own maximum if each stands there once
+  float part = 0.f, low = 0.f, z_first = 0.f;
   for (int j = r.tid; j < a.k; j += kTeam) {
-    part += t[j] = expf(l[j] - l_max);
+    if (a.tail) {
+      Parts e = split_exp(l[j]);
+      t[j] = e.all, part += e.high, low += e.low;
+    } else {
+      part += t[j] = expf(l[j] - l_max);
+    }
     if (r.blocks == 1) z_first += weight(j, m_listed);
   }
-  const float2 sums = r.team_sum(make_float2(part + wrong, z_first));
+  const float3 sums = r.team_sum(make_float3(part + wrong, low, z_first));
   if (kTeam == 32) r.team_sync();  // a block's sums are barriers
-  z_first = sums.y;
-  const float t_sum = !a.tail && sums.x > 0.f ? 1.f : sums.x;
+  z_first = sums.z;
+  const float t_sum = !a.tail && sums.x > 0.f ? 1.f : sums.x + sums.y;
   float t_scale = 1.f, l_base = 0.f;  // log t_j = l_j - l_base
   if (!a.tail && sums.x > 0.f) t_scale = __fdiv_rn(1.f, sums.x), l_base = l_max + logf(sums.x);
+  const float left = (1.f - sums.x) - sums.y;  // the difference is exact, so this is rounded once
 
   // the rest's sums
   Stat rest;
@@ -208,7 +248,7 @@ __global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? 2 : 
   }
   const float z_rest = has_rest ? rest.s * fast_exp2(fmaxf((rest.m - m) * r.per, kFar)) : 0.f, z = z_rest + z_listed;
   const float inverse = empty ? 0.f : __fdiv_rn(1.f, z), p_rest = z_rest * inverse, p_listed = z_listed * inverse;
-  const float t_rest = a.tail && has_rest ? fmaxf(1.f - t_sum, 0.f) : 0.f;
+  const float t_rest = a.tail && has_rest ? fmaxf(left, 0.f) : 0.f;
 
   part = 0.f;
   float log_z = 0.f;
@@ -227,7 +267,7 @@ __global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? 2 : 
     if (r.tid == 0 && r.rank == 0) {
       if (t_rest > 0.f) {
         const float log_p = z_listed <= z_rest ? -log1pf(__fdiv_rn(z_listed, z_rest)) : __fdiv_rn(rest.m - m, temperature) + logf(rest.s) - log_z;
-        loss += t_rest * (log1pf(-t_sum) - log_p);
+        loss += t_rest * (logf(t_rest) - log_p);
       }
       a.loss[row] = isnan(t_sum) ? NAN : loss;
     }

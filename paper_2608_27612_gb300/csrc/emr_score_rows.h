@@ -232,18 +232,24 @@ struct Row {
     __syncthreads();
     return __reduce_max_sync(0xffffffffu, lane < kWarps ? part[lane] : 0);
   }
-  __device__ static float2 warp_sum(float2 v) {
+  __device__ __forceinline__ static float more(float v, int o) { return v + __shfl_xor_sync(mates(), v, o); }
+  __device__ __forceinline__ static void more(float2& v, int o) { v.x = more(v.x, o), v.y = more(v.y, o); }
+  __device__ __forceinline__ static void more(float3& v, int o) { v.x = more(v.x, o), v.y = more(v.y, o), v.z = more(v.z, o); }
+  template <typename V>
+  __device__ static V warp_sum(V v) {
 #pragma unroll
-    for (int o = kTeam < 32 ? kTeam / 2 : 16; o; o >>= 1) v.x += __shfl_xor_sync(mates(), v.x, o), v.y += __shfl_xor_sync(mates(), v.y, o);
+    for (int o = kTeam < 32 ? kTeam / 2 : 16; o; o >>= 1) more(v, o);
     return v;
   }
-  __device__ float2 team_sum(float2 v) {
+  // Two or three sums.
+  template <typename V>
+  __device__ V team_sum(V v) {
     v = warp_sum(v);
     if (kTeam <= 32) return v;
-    float2* const part = reinterpret_cast<float2*>(scratch + 32 * (turn ^= 1));
+    V* const part = reinterpret_cast<V*>(scratch + 32 * (turn ^= 1));
     if (lane == 0) part[warp] = v;
     __syncthreads();
-    return warp_sum(lane < kWarps ? part[lane] : make_float2(0.f, 0.f));
+    return warp_sum(lane < kWarps ? part[lane] : V{});
   }
   // What every block has, to every block of the row: fn(value of block r), in the order of blocks.
   template <typename V, typename Fn>
