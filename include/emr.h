@@ -714,7 +714,8 @@ emr_status emr_dense_backward(const emr_dense *layer, const void *dy, int32_t dt
                               void *ws, size_t ws_bytes, void *stream);
 
 /* Whether a bounded device-side wait of this library has given up on the current GPU
- * since the last call: *code receives 0, or the number of the wait. Synchronises the stream. */
+ * since the last call: *code receives 0, or the number of the wait. Where waits of several kernels have, each call tells of one
+ * until 0 says that no more are left. Synchronises the stream. */
 emr_status emr_device_error(int32_t *code, void *stream);
 
 /* ---- sampling from scores ----------------------------------------------------- */

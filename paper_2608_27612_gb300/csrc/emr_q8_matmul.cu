@@ -17,6 +17,7 @@
 
 #include "emr_act.h"
 #include "emr_q8.h"
+#include "emr_records.h"
 #include "emr_tc.h"
 
 namespace {
@@ -1030,10 +1031,5 @@ extern "C" emr_status emr_q8_matmul(const emr_q8* a, const emr_q8* w, const floa
 extern "C" emr_status emr_device_error(int32_t* code, void* stream) {
   if (!code) return EMR_ERR_ARG;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  int32_t first = 0, second = 0;
-  emr_status ok = take_wait_error(g_wait_error, &first, st);
-  if (ok == EMR_OK) ok = q4_wait_error(&second, st);
-  if (ok != EMR_OK) return ok;
-  *code = first ? first : second;
-  return EMR_OK;
+  return first_record([&](int32_t* got) { return take_wait_error(g_wait_error, got, st); }, [&](int32_t* got) { return q4_wait_error(got, st); }, code);
 }

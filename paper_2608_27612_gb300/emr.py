@@ -800,7 +800,7 @@ def q8_slope(dy, d: Q8 | None, dz: Q8 | None = None, dzt: Q8 | None = None, db=N
 
 def device_error(stream=None) -> int:
     """emr_device_error: 0, or the number of a device-side wait that gave up since the last call, on the stream's
-    GPU (the current one)."""
+    GPU (the current one). After a number, call again until it is 0: several kernels' waits are told one a call."""
     code = C.c_int32()
     with _on(stream.device, stream) if stream is not None else _NOTHING:
         _check(lib().emr_device_error(C.byref(code), _stream(stream)), "emr_device_error")
