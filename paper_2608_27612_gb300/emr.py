@@ -1135,8 +1135,11 @@ def q4_dequantize(q: Q4, dtype=torch.float32, stream=None):
     _together(q.device)
     kind = _dtype(dtype, "dtype")
     with _on(q.device, stream):
+        raw = torch._C._cuda_getCurrentRawStream(q.device.index)
+        if q._home is not None and raw != q._home:
+            _lend(q.device, q.data)
         out = torch.empty(q.shape, dtype=dtype, device=q.device)
-        _check(lib().emr_q4_dequantize(q.ref, out.data_ptr(), kind, _stream(stream)), "emr_q4_dequantize")
+        _check(lib().emr_q4_dequantize(q.ref, out.data_ptr(), kind, raw), "emr_q4_dequantize")
     return out
 
 
