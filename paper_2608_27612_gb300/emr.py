@@ -615,6 +615,12 @@ def _dtype(t, what: str) -> int:
     return d
 
 
+def _counted(n: int, what: str):
+    """Refuses a count that the library's 32 bits do not hold: passed on, it would be another one."""
+    if n > 0x7fffffff:
+        raise EmrError(EMR_ERR_RANGE, what)
+
+
 def _matrices(x, what: str):
     """x as [batch, rows, cols] on the GPU (a view)."""
     if not isinstance(x, torch.Tensor) or x.dim() not in (2, 3):
@@ -1026,6 +1032,7 @@ def sample(scores, noise, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, stream
     if scores.dim() == 1:
         scores, noise = scores.unsqueeze(0), noise.unsqueeze(0)
     rows, n = scores.shape
+    _counted(rows, "rows")
     kind = _DTYPES.get(scores.dtype)
     if kind is None:
         _dtype(scores.dtype, "scores")
@@ -1068,6 +1075,7 @@ class Q4:
     row (emr_q4), in one piece of memory, `data` (uint8): what a layer that only answers keeps of its weights."""
 
     def __init__(self, batch: int, rows: int, cols: int, group: int = 32, device="cuda", data=None):
+        _counted(batch, "batch")
         n = C.c_size_t()
         _check(lib().emr_q4_size(batch, rows, cols, group, C.byref(n)), "emr_q4_size")
         if data is None:
@@ -1153,6 +1161,7 @@ def q4_matmul(x, w: Q4, bias=None, act: int = ACT_IDENTITY, out_dtype=torch.floa
     if k != w.cols or (nx != 1 and w.batch != 1 and nx != w.batch) or nx < 1:
         raise ValueError("x: [m, %d], [1, m, %d] or [%d, m, %d] is wanted, got %s" % (w.cols, w.cols, w.batch, w.cols, tuple(x.shape)))
     batch = max(nx, w.batch)
+    _counted(nx, "batch")
     kind = _DTYPES.get(x.dtype)
     if kind is None:
         _dtype(x.dtype, "x")
@@ -1221,6 +1230,7 @@ def _scores(scores):
         raise ValueError("scores: a tensor [rows, n] or [n] on the GPU is wanted")
     if n < 1:
         raise ValueError("scores: rows of at least one entry are wanted")
+    _counted(rows, "rows")
     kind = _DTYPES.get(scores.dtype)
     if kind is None:
         _dtype(scores.dtype, "scores")
