@@ -783,7 +783,7 @@ emr_status emr_q4_pack(const int8_t *codes, int64_t batch_stride, int64_t row_st
 emr_status emr_q4_dequantize(const emr_q4 *q, void *out, int32_t dtype, void *stream);
 
 /* out[b][m][n] = act(sum_k x[b][m][k] w[b][n][k] + bias[b][n]): x is x_batch matrices [rows][w.cols] of dtype with the given
- * strides (elements), out dense [batch][rows][w.rows] of out_dtype, outside x's and w's memory; an operand with batch 1 serves every b. Products of codes
+ * strides (elements), out dense [batch][rows][w.rows] of out_dtype, outside x's, w's and bias's memory; an operand with batch 1 serves every b. Products of codes
  * with x are exact in all types of x, sums are in 32 bits, each group's scaled once. bias: device float [batch][w.rows] or NULL.
  * act: EMR_ACT_*, as in emr_q8_matmul. Made for the rows that a layer answers at a time, where reading w counts. ws: room of
  * emr_q4_matmul_room bytes (the same arguments; 0 for few rows: up to 16, 8 of type EMR_F32, twice that for up to 512 columns),

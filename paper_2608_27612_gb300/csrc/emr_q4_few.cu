@@ -471,7 +471,8 @@ extern "C" emr_status emr_q4_matmul(const void* x, int32_t dtype, int32_t x_batc
   const int64_t batch = x_batch > w->batch ? x_batch : w->batch;
   if (overlap(x, (x_batch - 1) * batch_stride + (rows - 1) * row_stride + (w->cols - 1) * col_stride + 1, dtype_bytes(dtype), out, batch * rows * w->rows,
               dtype_bytes(out_dtype)) ||
-      overlap(w->data, w->batch * q4_tiles(w->rows) * q4_blocks(w->cols) * q4_unit(w->group), 1, out, batch * rows * w->rows, dtype_bytes(out_dtype)))
+      overlap(w->data, w->batch * q4_tiles(w->rows) * q4_blocks(w->cols) * q4_unit(w->group), 1, out, batch * rows * w->rows, dtype_bytes(out_dtype)) ||
+      (bias && overlap(bias, batch * w->rows, 4, out, batch * rows * w->rows, dtype_bytes(out_dtype))))  // read by other rows after one is written
     return EMR_ERR_ARG;
   a.bias = bias, a.act = act, a.out = out, a.out_dtype = out_dtype;
   int dev = 0, sms = 0;
