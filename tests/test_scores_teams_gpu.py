@@ -1,5 +1,5 @@
-"""Rows that are short and many belong to teams of 8 threads, four of which share a warp, or to single warps: log probabilities
-and their gradient of such rows against their definitions in float64 (oracle.scores), with rows that take another
+"""Rows that are short and many belong to teams of 8 threads, four of which share a warp, or to single warps: log probabilities,
+their gradient and distillation of such rows against their definitions in float64 (oracle.scores), with rows that take another
 way through the kernel (infinities, nothing left, temperatures of 0 and below, answers past the row) beside ordinary ones of
 the same warp. The numbers of rows follow the GPU's SMs as the kernels' choice of teams does, and fill no block.
 
@@ -7,7 +7,11 @@ Tolerances are those of the calls' own tests, from which the comparisons are tak
 import numpy as np
 import pytest
 import torch
+from test_distill_gpu import check as check_distill
+from test_distill_gpu import inputs as lists
 from test_log_probs_gpu import TYPES, check, check_gradient, inputs
+
+from paper_2608_27612_gb300 import emr
 
 pytestmark = pytest.mark.gpu
 
@@ -91,3 +95,47 @@ def test_strided_rows_and_a_row_of_one_entry():
     one = s[:, :1].contiguous()
     check(one, t % 2, T, rows=looked_at(rows))
     check_gradient(one, t % 2, 1.0, 0.5, T, rows=looked_at(rows))
+
+
+def strange_lists(rows, n, k, seed, dtype):
+    """Students and lists; of the first 64 rows every fourth is a strange one, and so are the last two."""
+    s, index, l = lists(rows, n, k, seed, dtype)
+    for i in range(18):
+        r = 4 * i + i % 4 if i < 16 else rows - 18 + i
+        kind = i % 8
+        if kind == 0:                                 # only two entries of +infinity count, one of them listed
+            s[r, n // 2] = s[r, -1] = float("inf")
+            index[r, 0], index[r, 1:] = n // 2, -1
+        elif kind == 1:                               # nothing left
+            s[r] = float("-inf")
+        elif kind == 2:                               # an infinity among the rest
+            s[r, (int(index[r].max()) + 1) % n] = float("inf")
+        elif kind == 3:                               # a list of one entry, several times
+            index[r], l[r] = n - 1, -3.0
+        elif kind == 4:
+            l[r, k // 2] = float("nan")
+        elif kind == 5:
+            index[r, 0] = n
+        elif kind == 6:                               # nothing wanted
+            index[r] = -1
+        else:                                         # no entry that is not listed
+            s[r], s[r, :k] = float("-inf"), 0.5
+            index[r] = torch.arange(k, dtype=torch.int32)
+    return s, index, l
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("more,n,k", [(3, 40, 6), (6, 513, 64), (1, 700, 33), (7, 1024, 64), (2, 1024, 1)])
+def test_a_warps_distillation(more, n, k, dtype):
+    rows = many(16) + more
+    s, index, l = strange_lists(rows, n, k, 28, dtype)
+    g = torch.Generator(device="cuda").manual_seed(29)
+    w = torch.rand(rows, device="cuda", generator=g)
+    T = torch.from_numpy(np.random.default_rng(30).choice([0.5, 1.0, 2.0], rows).astype(np.float32)).cuda()
+    for tail in (True, False):
+        check_distill(s, index, l, 1.0, tail, w, rows=looked_at(rows))
+        check_distill(s, index, l.bfloat16(), 0.7, tail, 0.5, torch.float32, looked_at(rows))
+    check_distill(s, index, l, T, False, w, rows=looked_at(rows))
+    T[5], T[6] = 0.0, -1.0                            # no distribution
+    loss = emr.distill(s, index, l, T)
+    assert bool(torch.isnan(loss[5:7]).all())
