@@ -253,7 +253,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_many_kernel(const __grid_const
         if (c >= own || n >= p.N) break;
         float d[16];
 #pragma unroll
-        for (int i = 0; i < 16; i++) sum[c][i] += bias;
+        for (int i = 0; i < 16; i++) sum[c][i] = (c0 + c) * 16 + i < columns ? sum[c][i] + bias : 0.f;  // x's tile holds anything there, and sin's way is one for all 16
         activate<16, false>(p.act, sum[c], d);
 #pragma unroll
         for (int i = 0; i < 16; i++)
