@@ -4,7 +4,7 @@
 // instructions with 16 rows of W as the instruction's rows and rows of x as its 8 columns, exact products with sums in 32
 // bits, and each is scaled and added in 32 bits. Codes become 16-bit floats by one OR and one subtraction for two (128 + q as bfloat16,
 // 1024 + q as float16). A 32-bit x is three bfloat16 parts of 8 bits each, together all of its 24 bits, in three columns.
-// Bound by reading W: half a byte an entry and 2 / group for its scale, once for up to 64 columns. x lies in shared memory, as
+// Bound by reading W: half a byte an entry and 2 / group for its scale, once for all columns, 48 at most (q4_is_many). x lies in shared memory, as
 // much of a row as there is room for. A warp streams its units (16 rows x 128 columns, one piece of memory) into a
 // ring of its own by asynchronous copies, five units ahead, and waits for no other warp. The warps of a block share rows of W
 // (`wide`) or, where those are few, the contraction (`teams`); a cluster of up to 8 blocks shares the contraction of few
@@ -36,7 +36,6 @@ struct Params {
   const void* x;
   int64_t x_batch, x_row, x_col;
   int32_t x_whole;     // 16 bytes of a row are one aligned piece
-  int32_t step;        // rows of x of a block
   int32_t wide, teams; // warps that share rows of W, and the contraction: powers of two
   int32_t log_teams;
   int32_t chunk;       // blocks of 128 columns whose x is in shared memory at a time
@@ -79,8 +78,7 @@ __global__ void __launch_bounds__(kThreads, kN <= 2 ? 2 : 1) q4_few_kernel(const
   const int shares = int(cluster.num_blocks()), rank = int(cluster.block_rank());
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   const int wide = p.wide, teams = p.teams, in_rows = warp & (wide - 1), team = warp >> (3 - p.log_teams);
-  const int64_t m0 = int64_t(blockIdx.y) * p.step;
-  const int rows = int(p.M - m0 < p.step ? p.M - m0 : p.step), columns = kParts * rows;
+  const int rows = int(p.M), columns = kParts * rows;
   const int first = shares == 1 ? 0 : int(unsigned(p.blocks) * unsigned(rank) / unsigned(shares));
   const int last = shares == 1 ? p.blocks : int(unsigned(p.blocks) * unsigned(rank + 1) / unsigned(shares));
   // blocks of rows of the block, one after the other
@@ -139,7 +137,7 @@ __global__ void __launch_bounds__(kThreads, kN <= 2 ? 2 : 1) q4_few_kernel(const
     constexpr int kPiece = kSplit ? 4 : 8;
     const int per_row = (last - c < p.chunk ? last - c : p.chunk) * (kQ4Cols / kPiece);
     const int64_t k0 = int64_t(c) * kQ4Cols;
-    const T* const x = static_cast<const T*>(p.x) + b * p.x_batch + m0 * p.x_row + k0 * p.x_col;
+    const T* const x = static_cast<const T*>(p.x) + b * p.x_batch + k0 * p.x_col;
     const int log_rows = rows > 4 ? 3 : rows > 2 ? 2 : rows > 1 ? 1 : 0, apart = 32 << (3 - log_rows);  // warps of a row: 8, 4, 2 or 1
     for (int m = warp & ((1 << log_rows) - 1); m < rows; m += 1 << log_rows) {
       const T* const row = x + m * p.x_row;
@@ -300,7 +298,7 @@ __global__ void __launch_bounds__(kThreads, kN <= 2 ? 2 : 1) q4_few_kernel(const
 #pragma unroll
           for (int j = 0; j < 4; j++) own[(n * 8 + 2 * t + (j & 1)) * (kR * 16) + r * 16 + g + 8 * (j >> 1)] = sum[r][n][j];
       __syncwarp();
-      const int64_t n0 = int64_t(tile) * 16, at = (b * p.M + m0) * p.N + n0;
+      const int64_t n0 = int64_t(tile) * 16, at = b * p.M * p.N + n0;
       for (int i = lane; i < rows * kR * 16; i += 32) {
         const int n = i % (kR * 16);
         finish(b, n0, at, i / (kR * 16), n, [&](int column) { return own[column * (kR * 16) + n]; });
@@ -325,7 +323,7 @@ __global__ void __launch_bounds__(kThreads, kN <= 2 ? 2 : 1) q4_few_kernel(const
       for (int j = 0; j < 4; j++)
         sums[team * room + (n * 8 + 2 * t + (j & 1)) * tall + (in_rows * kR + r) * 16 + g + 8 * (j >> 1)] = sum[r][n][j];
   __syncthreads();
-  const int64_t n0 = int64_t(from - s_first_b * p.row_blocks) * tall, out_at = (s_first_b * p.M + m0) * p.N + n0;
+  const int64_t n0 = int64_t(from - s_first_b * p.row_blocks) * tall, out_at = s_first_b * p.M * p.N + n0;
   const int log_tall = __ffs(tall) - 1;
   if (shares > 1) {
     for (int at = tid; at < columns * tall; at += kThreads) {
@@ -360,7 +358,7 @@ emr_status launch(const Params& p, int64_t blocks, int shares, size_t smem, int 
   static std::atomic<uint64_t> done{0};
   if (!allow_smem(q4_few_kernel<T, kN, kPer>, kMostSmem, dev, done)) return EMR_ERR_CUDA;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(unsigned(blocks * shares), unsigned((p.M + p.step - 1) / p.step));
+  cfg.gridDim = dim3(unsigned(blocks * shares));
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
@@ -381,11 +379,8 @@ emr_status launch(const Params& p, int per, int64_t blocks, int shares, size_t s
 
 template <typename T>
 emr_status plan(Params p, int64_t batch, int per, int dev, int sms, cudaStream_t st) {
-  constexpr int kParts = sizeof(T) == 4 ? 3 : 1, kMost = 64 / kParts;
-  const int64_t chunks = (p.M + kMost - 1) / kMost;
-  if (chunks > 65535) return EMR_ERR_RANGE;
-  p.step = int((p.M + chunks - 1) / chunks);
-  const int columns = p.step * kParts, kn = columns <= 8 ? 1 : columns <= 16 ? 2 : columns <= 32 ? 4 : 8, kr = kn >= 4 ? 2 : 1;
+  constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
+  const int columns = int(p.M) * kParts, kn = columns <= 8 ? 1 : columns <= 16 ? 2 : columns <= 32 ? 4 : 8, kr = kn >= 4 ? 2 : 1;
   const int64_t row_tiles = (p.tiles + kr - 1) / kr;
   const size_t unit = kQ4Codes + 32 * per, ring = size_t(kWarps) * kAhead * kr * unit, sums = size_t(kWarps) * kr * 16 * kn * 8 * 4;
   // x: beside the rings, in half an SM's shared memory where two blocks share it
@@ -393,19 +388,19 @@ emr_status plan(Params p, int64_t batch, int per, int dev, int sms, cudaStream_t
   const int fit = int((room - columns * 64) / (size_t(columns) * 256)), fit_direct = int((room - sums - columns * 64) / (size_t(columns) * 256));
   int64_t blocks;
   int shares = 1;
-  if (p.blocks <= fit_direct && batch * chunks * row_tiles >= kWarps * sms) {
+  if (p.blocks <= fit_direct && batch * row_tiles >= kWarps * sms) {
     // enough tiles for every warp of an SM: each takes its own, two blocks an SM
     p.wide = kWarps, p.teams = 1, p.chunk = p.blocks;
     p.row_blocks = int((row_tiles + kWarps - 1) / kWarps);
     const int64_t all = batch * p.row_blocks;
     if (all > INT32_MAX) return EMR_ERR_RANGE;
     p.all_blocks = int32_t(all);
-    const int64_t room_for = (kn <= 2 ? 2 : 1) * sms / chunks;
-    blocks = p.all_blocks < room_for || room_for < 1 ? p.all_blocks : room_for;
+    const int64_t room_for = (kn <= 2 ? 2 : 1) * sms;
+    blocks = p.all_blocks < room_for ? p.all_blocks : room_for;
   } else {
     // every block reads x: rows of W enough that x is at most half as many bytes, and that its share of x fits at once
     int wide = 1;
-    while (wide < kWarps && p.step * int(sizeof(T)) > wide * kr * 4) wide *= 2;
+    while (wide < kWarps && int(p.M) * int(sizeof(T)) > wide * kr * 4) wide *= 2;
     const int at_once = (kn <= 2 ? 2 : 1) * sms;
     for (;; wide *= 2) {
       p.wide = wide, p.teams = kWarps / wide;
@@ -413,7 +408,7 @@ emr_status plan(Params p, int64_t batch, int per, int dev, int sms, cudaStream_t
       blocks = batch * p.row_blocks;
       shares = 1;
       for (int s = 2; s <= kMaxCluster; s++)
-        if (blocks * s * chunks <= at_once && p.blocks / (s * p.teams) >= 2) shares = s;
+        if (blocks * s <= at_once && p.blocks / (s * p.teams) >= 2) shares = s;
       const int share = (p.blocks + shares - 1) / shares, some = p.teams == 1 ? fit_direct : fit, parts = (share + some - 1) / some;
       p.chunk = (share + parts - 1) / parts;
       if (parts == 1 || wide == kWarps) break;
@@ -426,9 +421,11 @@ emr_status plan(Params p, int64_t batch, int per, int dev, int sms, cudaStream_t
   const bool own = p.teams == 1 && shares == 1;
   size_t smem = ring + size_t(columns) * (p.chunk * 256 + 64) + (own ? sums : 0);
   if (smem < sums) smem = sums;
+  if constexpr (kParts == 3) {  // 16-bit rows, 32 at most, are no more columns
+    if (kn == 8) return launch<T, 8>(p, per, blocks, shares, smem, dev, st);
+  }
   return kn == 1   ? launch<T, 1>(p, per, blocks, shares, smem, dev, st)
-         : kn == 2 ? launch<T, 2>(p, per, blocks, shares, smem, dev, st)
-         : kn == 4 ? launch<T, 4>(p, per, blocks, shares, smem, dev, st) : launch<T, 8>(p, per, blocks, shares, smem, dev, st);
+         : kn == 2 ? launch<T, 2>(p, per, blocks, shares, smem, dev, st) : launch<T, 4>(p, per, blocks, shares, smem, dev, st);
 }
 
 // The arguments of a product, checked.

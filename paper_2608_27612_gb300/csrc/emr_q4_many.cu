@@ -27,9 +27,9 @@ namespace cg = cooperative_groups;
 using namespace emr;
 
 constexpr int kUnpack = 4, kScale = 8;  // warps that unpack codes and scale sums; then one that copies x and one that issues
-constexpr int kSets = kUnpack / 4, kSums = 32 / kScale;  // blocks of columns unpacked at a time; 16 columns each of a scaling warp's sums
+constexpr int kSums = 32 / kScale;  // 16 columns each of a scaling warp's sums
 constexpr int kWarps = kUnpack + kScale + 2, kThreads = 32 * kWarps;
-constexpr int kCodeStages = 8 / kSets, kTileStages = 4, kMaxCluster = 8;
+constexpr int kCodeStages = 8, kTileStages = 4, kMaxCluster = 8;
 constexpr int kBatch = 512;              // bytes of scales that a warp has copied at a time, of 1024 / group blocks of columns
 constexpr int kColumns = 512;            // of tensor memory: two groups' sums of 128, then the tiles of codes, 64 each
 constexpr int kRowPitch = 80;            // of a row's 64 bytes of codes in shared memory: other banks than the row before
@@ -128,9 +128,8 @@ __global__ void __launch_bounds__(kThreads, 1) q4_many_kernel(const __grid_const
   const int c0 = (warp - kUnpack) / 4 * each, own = chunks - c0 < each ? chunks - c0 : each;
 
   if (warp < kUnpack) {
-    // all blocks of columns by turns
-    const int tile = block * 8 + quarter * 2, odd = warp >> 2;
-    const uint8_t* unit = p.w + b * p.w_batch + (int64_t(tile) * p.blocks + first + odd) * kUnit + lane * 16;
+    const int tile = block * 8 + quarter * 2;
+    const uint8_t* unit = p.w + b * p.w_batch + (int64_t(tile) * p.blocks + first) * kUnit + lane * 16;
     const int64_t second = int64_t(p.blocks) * kUnit;
     uint8_t* const codes_at = ring + warp * (kCodeStages * kCodeStage);
     const uint32_t to = smem_at(codes_at) + (lane >> 2) * kRowPitch + (lane & 3) * 16;
@@ -141,18 +140,17 @@ __global__ void __launch_bounds__(kThreads, 1) q4_many_kernel(const __grid_const
         const uint32_t at = to + put * kCodeStage;
         if (one) copy16(at, unit), copy16(at + 8 * kRowPitch, unit + 512);
         if (two) copy16(at + 16 * kRowPitch, unit + second), copy16(at + 24 * kRowPitch, unit + second + 512);
-        unit += kSets * kUnit;
+        unit += kUnit;
         put = put == kCodeStages - 1 ? 0 : put + 1;
       }
       commit();
     };
 #pragma unroll 1
-    for (int i = 0; i < kCodeStages - 1; i++) issue(first + odd + kSets * i);
-    int get = 0, stage = odd;
+    for (int i = 0; i < kCodeStages - 1; i++) issue(first + i);
+    int get = 0, stage = 0;
     uint32_t round = 0;
-    if (stage >= p.stages) stage -= p.stages, round ^= 1;
-    for (int kb = first + odd; kb < last; kb += kSets) {
-      issue(kb + kSets * (kCodeStages - 1));
+    for (int kb = first; kb < last; kb++) {
+      issue(kb + kCodeStages - 1);
       asm volatile("cp.async.wait_group %0;" ::"n"(kCodeStages - 1) : "memory");
       __syncwarp();
       uint4 c[4];
@@ -180,8 +178,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_many_kernel(const __grid_const
       fence_before();
       __syncwarp();
       if (lane == 0) arrive(full + 8 * stage);
-      for (int i = 0; i < kSets; i++)
-        if (++stage == p.stages) stage = 0, round ^= 1;
+      if (++stage == p.stages) stage = 0, round ^= 1;
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
   } else if (warp < kUnpack + kScale) {
