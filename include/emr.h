@@ -809,7 +809,9 @@ emr_status emr_q4_matmul(const void *x, int32_t dtype, int32_t x_batch, int64_t 
  * T <= 0 (and NaN) stands for the limit that emr_sample takes: log p is 0 for the largest score (lowest index) and
  * -infinity for the others. A score of +infinity leaves only the entries that equal it. An entry whose s - s_max is below
  * the range of 32 bits has log p -infinity whatever T. A row with nothing left gives -infinity, entropy 0 and no best. Results are good to 6e-6 + 2^-22 |log p| and do not depend on the order of execution.
- * Scores are read from memory once; a row's candidates for the best again, from L2. Errors: EMR_ERR_ARG (null
+ * A row is gone through once, and its candidates for the best again. Once more, from L2 or, where the rows that are worked on at a
+ * time do not fit there, from memory: a row with a +infinity, T <= 0 with logp asked for, and up to 9 times the best of a row with more
+ * equal scores than the list of candidates holds. Errors: EMR_ERR_ARG (null
  * or misaligned pointer, size below 1, negative stride, unknown type, nothing asked for), EMR_ERR_RANGE (n above
  * 2^31 - 2^20, rows above 2^27, top above EMR_MAX_TOP), EMR_ERR_CUDA. */
 #define EMR_MAX_TOP 256
@@ -821,8 +823,9 @@ emr_status emr_log_probs(const void *scores, int32_t dtype, int32_t rows, int64_
  * dscores[r][i] = (dlogp ([i = target] - p_i) - dentropy p_i (log p_i + entropy)) / T, 0 for masked entries, for
  * rows with T <= 0 and for rows with nothing left; a row whose target is n or more is NaN, and one with a target
  * below 0 has no part of dlogp. dlogp and dentropy: device float [rows], or NULL for the scalar beside them. logp
- * and entropy (NULL for none) receive what emr_log_probs gives, so that a training step reads the scores from
- * memory once. dscores: [rows] rows of d_dtype, d_stride (n or more) elements apart, outside the scores' memory. Errors:
+ * and entropy (NULL for none) receive what emr_log_probs gives, so that a training step needs no other call. A row is gone through
+ * twice, the second time from L2 where the rows that are worked on at a time fit there (of float32 349,524 entries do, 700,001 are read from
+ * memory twice). dscores: [rows] rows of d_dtype, d_stride (n or more) elements apart, outside the scores' memory. Errors:
  * as above. */
 emr_status emr_log_probs_grad(const void *scores, int32_t dtype, int32_t rows, int64_t n, int64_t row_stride,
                               const int32_t *target, const float *temperature, float temperature_all,
@@ -847,8 +850,8 @@ emr_status emr_log_probs_grad(const void *scores, int32_t dtype, int32_t rows, i
  * (T * T is often put into dloss). The teacher has no gradient. A row in which an index is n or more, a listed
  * teacher value is NaN, or T (where it is given for each row) is not above 0 has a loss and a gradient of NaN; a row with nothing left
  * has gradient 0. loss: device float [rows], NULL for none. dloss: device float [rows], or NULL for the scalar beside
- * it. dscores: as for emr_log_probs_grad, NULL for none. Results do not depend on the order of execution. One pass over memory with or
- * without a gradient. Errors: EMR_ERR_ARG (null or misaligned pointer, size below 1, negative stride, unknown
+ * it. dscores: as for emr_log_probs_grad, NULL for none. Results do not depend on the order of execution. A row is gone through once, with a
+ * gradient twice, as by emr_log_probs_grad. Errors: EMR_ERR_ARG (null or misaligned pointer, size below 1, negative stride, unknown
  * type, temperature_all not above 0, nothing asked for), EMR_ERR_RANGE (n above 2^31 - 2^20, rows above 2^27, k above EMR_MAX_TOP),
  * EMR_ERR_CUDA. */
 emr_status emr_distill(const void *scores, int32_t dtype, int32_t rows, int64_t n, int64_t row_stride,

@@ -12,6 +12,8 @@
 // columns: the matrix pipe 450-570, a scaling warp 720, an unpacking warp 600, coupled by two buffers of sums. With 8 warps that
 // unpack (96 registers a thread, and the sums spilled) it took 54; with 16 that scale (72) 79; with three buffers of sums and
 // two of codes 48. Neither x (a fourteenth of it copied: 44) nor the multiplications (a quarter of them: 43) hold it.
+// That is with groups of 128; a hand-over of sums for each 64 columns makes it 55, for each 32 96 (40 rows: 38, 51 and 92), and float32, two blocks of rows of three
+// products each, 113, 143 and 239 (40 rows: 53, 73 and 122).
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 

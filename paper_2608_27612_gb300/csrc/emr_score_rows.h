@@ -78,7 +78,7 @@ __device__ __forceinline__ float2 far2(float s0, float s1, float m, float per) {
   return make_float2(fmaxf(d.x, kFar), fmaxf(d.y, kFar));
 }
 
-// One row, by a team of 8 or 32 threads (of a block of 256) or of a block, and for the largest team by a cluster of blocks.
+// One row, by a team of 8 or 32 threads (of a block of 256) or of a block of 64 to 512, and for the largest team by a cluster of blocks.
 // Threads take it in turns of kAhead groups of 16 bytes each, loaded together and without a check, while all threads have as
 // many; the groups that are left, among them those that reach out of the slice, one at a time.
 template <typename T, int kTeam>
@@ -474,6 +474,19 @@ void clusters_at_once(K kernel, int threads, int* fit) {
 // sums, 500 in a gradient and 750 in distillation, counts for each of its warps, and more rows are at hand while one waits.
 // Gradients of bfloat16 by 64 and by 128 threads: 2000 x 5460 13.7 and 17.4 us, 8000 x 1364 23 and 34; best 20 of float32
 // 2000 x 1364 10.1 and 11.3, 1000 x 1364 8.2 and 7.3, 4000 x 5460 38 and 33.
+// The other steps, in us on the device with 152 SMs, the rule's choice first where nothing else is said.
+// 8 threads or 32, gradients: 4864 x 340 bfloat16 6.2 and 7.5, 9728 x 512 6.5 and 9.0, 4864 x 512 float32 5.8 and 5.2; below, 32 or 8: 2432 x 340
+// 5.2 and 6.2, 4864 x 1024 7.2 and 7.2, but 9728 x 700 13.6 and 9.2.
+// 32 threads or 64, bfloat16: gradients of 2432 x 340 5.2 and 6.8, of 2432 x 1024 4.8 and 5.9; best 5 of 2432 x 1024 5.5 and 7.5, best 20 9.9 and 9.2,
+// but best 32 37.9 and 11.3; distillation with lists of 16 9.1 and 11.3, of 64 18.8 and 16.4. Below, 64 or 32: gradients of 1216 x 340 4.8 and 4.8, of
+// 1216 x 700 5.5 and 4.8.
+// 128 threads or 256: sums of 608 x 5460 bfloat16 4.8 and 4.5, gradients of 608 x 8192 6.5 and 6.9, best 20 8.6 and 8.8; 256 or 128: gradients of
+// 304 x 5460 float32 5.2 and 5.5.
+// 256 threads or a block of 512, float32: sums of 152 x 8192 3.4 and 3.8, gradients 4.1 and 4.5, best 20 7.2 and 7.5. A row of more than 8,192 that gets
+// one block, 512 or 256: gradients of 608 x 40000 39.5 and 47.5, but of 608 x 12000 17.6 and 14.4, best 20 of 608 x 20001 26.3 and 19.9.
+// Clusters of 1, 2, 4 and 8, gradients of float32: 20 x 40000 8.9, 7.9, 6.2 and 7.2 (taken: 8), 64 x 40000 8.9, 7.9, 8.1 and 13.9 (4), 152 x 40000 14.1, 14.5, 22.8
+// and 34.4 (2), 1 x 20001 6.4, 5.8, 5.8 and 6.2 (4); 152 x 12000 5.5, 7.2, 15.4 and 24.9 (2, as best 20, 8.6 and 13.7 of one and two): entries of a block, 4,096
+// at least, could be twice as many.
 // The team and cluster of a row, and the slice of its blocks: the same with and without a gradient, so that the values are.
 // least: the smallest team that will do; size: bytes of a score.
 inline int plan(Rows& a, int least, int size, int sms, const int* fit, int* cluster) {

@@ -5,18 +5,21 @@
 // and the gradient of a logp_t + b H is (a ([i = t] - p_i) - b p_i (log p_i + H)) / T. One pass over a row
 // finds all three sums: a thread keeps its own maximum and its sums relative to that, and moves them when the
 // maximum rises (rarely after its first entries); the threads', and the blocks', are joined in a fixed order. A
-// gradient takes a second pass, which finds the row in L1 or L2, and writes once.
+// gradient takes a second pass, which finds the row in L1 or L2 (those that are worked on at a time: of 349,524 float32 entries
+// still, of 700,001 no longer), and writes once.
 // Bound by memory where there are many rows: about seven operations and one exponential an entry, two of each in
-// a gradient, are a good half of what an SM can do while an entry comes in. A row belongs to a warp where rows
-// are short and many, to a block, or to a cluster of up to 8 blocks where rows are few.
+// a gradient, are a good half of what an SM can do while an entry comes in. A row belongs to 8 threads or a warp where rows
+// are short and many, to a block of 64 to 512, or to a cluster of up to 8 blocks where rows are few.
 // The best k: the k-th largest of the threads' own maxima is at most the k-th largest score, so only threads whose
 // maximum reaches it have their entries looked at again, by their warp, a lane for a group (about 25 of 128 threads for k =
 // 20). What reaches it is collected and ordered. Rows with more such entries than the list holds (equal
 // scores) find their k-th entry first, by a histogram of each byte of (score, index).
-// Measured on the device: 4000 x 5460 float32 with its best 20 33 us (87 MB, 2.7 TB/s; 7 instructions an entry for the
-// sums and as many again for the search: issue 57% of the time, the rest latency), 24 x 349524 bfloat16 with its best 100 19 (six
-// meetings of a cluster), gradients of 16000 x 340 bfloat16 10.6 and of 512 x 87380 float32 with the entropy's 73 (358 MB, 4.9 TB/s), one
-// row of 1364 4.8.
+// Measured on the device: 4000 x 5460 float32 with its best 20 33 us (87 MB, 2.7 TB/s; 21.3 M instructions,
+// 7 an entry for the sums and as many again for the search make 9.6 M of them, the rest, 2,900 a row, is what a row costs beside its entries; issue 57% of
+// the time, the rest latency), without them 20; 24 x 349524 bfloat16 with its best 100 19 (six
+// meetings of a cluster), gradients of 16000 x 340 bfloat16 10.6 (values alone 6.2) and of 512 x 87380 float32 with the entropy's 73 (358 MB, 4.9 TB/s), one
+// row of 1364 with its best 5 4.5. Lists of more entries than a row has groups have it ordered as a whole: the best 100 of 8000 x 700 take 240 of
+// bfloat16 and 81 of float32.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 #include <float.h>
