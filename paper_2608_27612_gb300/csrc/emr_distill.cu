@@ -12,7 +12,7 @@
 // L1 or L2 (where the rows that are worked on at a time fit there) and writes once; listed entries are written over after it, k of them. Bound by memory for many rows; for
 // few, by the chain list - scores of its entries - bits - pass - sums.
 // Measured on the device: 2000 x 5460 bfloat16 with lists of 50 19 us (44 MB; a row costs 750 instructions a warp beside its
-// entries), 1000 x 87380 float16 with 64 78 (350 MB, 4.4 TB/s; issue 55%, exponentials 48% of their unit), 250 x 1364 float32
+// entries), 1000 x 87380 float16 with 64 79 (350 MB, 4.4 TB/s; issue 55%, exponentials 48% of their unit), 250 x 1364 float32
 // with 16 6.2; the loss alone 11.6, 53 and 5.5.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>

@@ -17,7 +17,7 @@
 // Measured on the device: 4000 x 5460 float32 with its best 20 33 us (87 MB, 2.7 TB/s; 21.3 M instructions,
 // 7 an entry for the sums and as many again for the search make 9.6 M of them, the rest, 2,900 a row, is what a row costs beside its entries; issue 57% of
 // the time, the rest latency), without them 20; 24 x 349524 bfloat16 with its best 100 19 (six
-// meetings of a cluster), gradients of 16000 x 340 bfloat16 10.6 (values alone 6.2) and of 512 x 87380 float32 with the entropy's 73 (358 MB, 4.9 TB/s), one
+// meetings of a cluster), gradients of 16000 x 340 bfloat16 10.9 (values alone 6.2) and of 512 x 87380 float32 with the entropy's 73 (358 MB, 4.9 TB/s), one
 // row of 1364 with its best 5 4.5. Lists of more entries than a row has groups have it ordered as a whole: the best 100 of 8000 x 700 take 240 of
 // bfloat16 and 81 of float32.
 #include <cooperative_groups.h>
